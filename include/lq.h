@@ -48,6 +48,9 @@ typedef enum {
 /* v dtype codes (b2 of the configuration tuple). */
 enum { LQ_V_FP32 = 0, LQ_V_BF16 = 1, LQ_V_FP16 = 2 };
 
+/* Element types of the training operators' activations and of the cross entropy's weights. */
+enum { LQ_T_FP32 = 0, LQ_T_BF16 = 1 };
+
 /*
  * Quantization configuration c = (b0, b1, b2, B0, B1) of Section 3.2 (Table 1 lists the paper's
  * search grid; b0 = 8 is the "NF-8" variant of Section 4.2).
@@ -305,6 +308,64 @@ size_t lq_matmul_few_rows_static_scratch_bytes(void);
 int lq_matmul_few_rows_static(const float* X, int64_t m, int64_t d, int64_t k, const uint8_t* codes_packed,
                               const uint8_t* scale_idx, const float* v, lq_config c, const float* L1, const float* L2,
                               int rank, float* Y, void* stream);
+
+/*
+ * ---- Fine-tuning the decomposed layers (Section 3: Q stays fixed, L1 and L2 are trained) ------------------------------
+ *
+ * Activations (X, Y, dY, dX, and W, dW of the cross entropy) are of type `dtype`, LQ_T_FP32 or LQ_T_BF16; L1, L2, T, their
+ * gradients, losses and log-sum-exps are fp32.  Sums, softmax statistics and accumulators are held in fp32 (the total loss in
+ * fp64).  fp32 operands of a product are split into bf16 hi + lo and take three MFMAs (error about 2^-16 of sum |a||b|); with
+ * bf16 activations the decoded weights, and T and U where they meet bf16 results, are rounded to bf16.  All calls only enqueue
+ * kernels on `stream`, are deterministic, and can be captured in a HIP graph after a first call on the device.
+ */
+
+/*
+ * Dropout from a counter-based generator: y[e] = kept ? x[e] * s : 0 (0 whatever x holds), with t = floor(65536 p + 1/2),
+ * s = 65536 / (65536 - t) in fp32 (0 for p = 1) and element e kept iff its 16 random bits are at least t.  They are bits
+ * 16 (e % 2) .. + 15 of word (e % 8) / 2 of Philox4x32 with seven rounds for the counter (e / 8, offset), low words first, and the
+ * key `seed`.  The mask is stored nowhere: the gradient is the same call on dy.  x, y: n values of type dtype, y may be x.
+ * p in [0, 1] (LQ_ERR_ARG).
+ */
+int lq_dropout(const void* x, int64_t n, int dtype, double p, uint64_t seed, uint64_t offset, void* y, void* stream);
+
+/*
+ * Softmax cross entropy over `vocab` classes with its gradients, without an array of logits:
+ *     s_ij = <x_i, w_j>,  row_loss[i] = log sum_j exp(s_ij) - s_i,target,  lse[i] = log sum_j exp(s_ij),
+ *     loss = sum of the row losses, or with mean == 1 their mean over the rows that count,
+ *     dX, dW = gradients of `loss`.
+ *   X        n x d, ldx elements from row to row        W   vocab x d, ldw elements from row to row
+ *   targets  n int64.  A row whose target lies outside [0, vocab) does not count, whatever X holds there: row loss and gradient
+ *            are 0.  If none counts, loss is 0 for sum and mean alike.
+ *   loss 1 fp32, row_loss n fp32, lse n fp32 or NULL, dX n x d or NULL, dW vocab x d or NULL (contiguous, of type dtype)
+ * The vocabulary is walked in pieces; the workspace holds one piece's exponentials.  dX comes out of the same pass as the loss,
+ * dW takes a second one.  n and vocab up to 2^31 - 65537, d up to 2^20 (LQ_ERR_SHAPE).
+ */
+size_t lq_cross_entropy_workspace_bytes(int64_t n, int64_t d, int64_t vocab, int dtype, int want_dx, int want_dw);
+int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* targets, int64_t n, int64_t d,
+                     int64_t vocab, int dtype, int mean, float* loss, float* row_loss, float* lse, void* dX, void* dW,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A decomposed layer in training, with dropout on the adapter's branch:
+ *     T = drop(X) L1,  Y = X Q + T L2,
+ * and backwards
+ *     U = dY L2^T,  dX = dY Q^T + mask s .* (U L1^T),  dL1 = drop(X)^T U,  dL2 = T^T dY,
+ * with drop(X) as lq_dropout computes it for X (m x d, row-major) with the same p, seed and offset (without the rounding of a
+ * bf16 result), and mask s its mask and factor, worked out again and stored nowhere.  p = 0: no dropout.
+ *   X m x d, Y and dY m x k, dX m x d (NULL: not wanted, for a first layer): contiguous, of type dtype, 16-byte aligned
+ *   codes_packed, scale_idx, v    Q as for lq_matmul        L1 d x rank, L2 rank x k (forward: 16-byte aligned)
+ *   T        m x rank fp32, written by the forward and read by the backward call
+ *   rank in [1, 128] (LQ_ERR_RANK); d a multiple of 32, k of the block size; ceil(m / 256) * 256 * max(d, k) and d * k below
+ *   2^31 (LQ_ERR_SHAPE)
+ */
+size_t lq_adapter_workspace_bytes(int64_t m, int64_t d, int64_t k, int rank, int dtype, int backward);
+int lq_adapter_forward(const void* X, int64_t m, int64_t d, int64_t k, const uint8_t* codes_packed, const uint8_t* scale_idx,
+                       const float* v, lq_config c, const float* L1, const float* L2, int rank, int dtype, double p, uint64_t seed,
+                       uint64_t offset, void* Y, float* T, void* workspace, size_t workspace_bytes, void* stream);
+int lq_adapter_backward(const void* dY, const void* X, int64_t m, int64_t d, int64_t k, const uint8_t* codes_packed,
+                        const uint8_t* scale_idx, const float* v, lq_config c, const float* L1, const float* L2, int rank, int dtype,
+                        const float* T, double p, uint64_t seed, uint64_t offset, void* dX, float* dL1, float* dL2, void* workspace,
+                        size_t workspace_bytes, void* stream);
 
 /*
  * Per-kernel timing for benchmarks (off by default).  While enabled, every kernel launch of the library

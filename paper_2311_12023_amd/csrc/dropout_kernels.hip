@@ -1,0 +1,48 @@
+// Dropout of a flat array: y = kept ? scale x : 0 with the mask of philox_device.h.  The gradient is the same operation on dy.
+#include <algorithm>
+
+#include "mfma_device.h"
+#include "philox_device.h"
+#include "profiler.h"
+#include "train.h"
+
+namespace lq {
+
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void dropout_kernel(const T* __restrict__ x, int64_t n, DropoutMask d, T* __restrict__ y) {
+  typedef T vec8 __attribute__((ext_vector_type(8)));
+  const int64_t groups = (n + 7) >> 3;
+  for (int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x; g < groups; g += (int64_t)gridDim.x * 256) {
+    if (VEC && 8 * g + 8 <= n) {
+      const vec8 in = *reinterpret_cast<const vec8*>(x + 8 * g);
+      const PhiloxWords w = philox_words(d, (uint64_t)g);
+      vec8 out;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) out[j] = philox_kept(w, j, d.cut) ? (T)((float)in[j] * d.scale) : (T)0.0f;
+      *reinterpret_cast<vec8*>(y + 8 * g) = out;
+    } else {
+      const PhiloxWords w = philox_words(d, (uint64_t)g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (8 * g + j < n) y[8 * g + j] = philox_kept(w, j, d.cut) ? (T)((float)x[8 * g + j] * d.scale) : (T)0.0f;
+    }
+  }
+}
+
+template <typename T>
+static void launch(const void* x, int64_t n, const DropoutMask& d, void* y, hipStream_t st) {
+  const unsigned wgs = (unsigned)std::min<int64_t>((n + 2047) / 2048, 1 << 20);
+  const bool vec = (((uintptr_t)x | (uintptr_t)y) & 15) == 0;
+  auto kernel = vec ? dropout_kernel<T, true> : dropout_kernel<T, false>;
+  hipLaunchKernelGGL(kernel, dim3(wgs), dim3(256), 0, st, static_cast<const T*>(x), n, d, static_cast<T*>(y));
+}
+
+int launch_dropout(const void* x, int64_t n, int dtype, const DropoutMask& d, void* y, hipStream_t st) {
+  prof::Scope ps(prof::DROPOUT, st, (double)n * 2.0 * type_bytes(dtype));
+  if (dtype == LQ_T_BF16) launch<__bf16>(x, n, d, y, st);
+  else launch<float>(x, n, d, y, st);
+  LQ_HIP_TRY(hipGetLastError());
+  return LQ_OK;
+}
+
+}  // namespace lq

@@ -32,7 +32,16 @@ enum Cls {
   WEIGHT_PLANE = 67,        // weight_plane_kernel (work = bytes)
   COLUMN_GEMM_BASE = 68,    // + mode * 4 + (l/32 - 1): column_gemm_kernel (work = flops of the product)
   COLUMN_SUM = 76,          // column_sum_kernel (work = bytes)
-  NUM_CLASSES = 77
+  DROPOUT = 77,             // dropout_kernel (work = bytes)
+  TRAIN_PLANES = 78,        // row_planes_kernel, column_planes_kernel (work = bytes)
+  SEGMENT_GEMM = 79,        // plain_product_kernel, adapter_dx_kernel (work = flops of the product)
+  LOSS_LOGITS = 80,         // loss_logits_kernel, loss_gradient_kernel (work = flops of the product)
+  LOSS_ACCUMULATE = 81,     // loss_accumulate_kernel (work = flops of the product)
+  LOSS_ROWS = 82,           // the loss's passes over rows and sums (work = bytes)
+  THIN_PROJECT = 83,        // thin_project_kernel (work = bytes)
+  THIN_GRAM = 84,           // thin_gram_kernel (work = bytes)
+  THIN_FINISH = 85,         // sums of partial results of the training operators (work = bytes)
+  NUM_CLASSES = 86
 };
 
 bool enabled();

@@ -15,6 +15,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblq_hip.so")
 
 V_DTYPES = {"fp32": 0, "bf16": 1, "fp16": 2}
+T_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
 class LqError(RuntimeError):
@@ -88,6 +89,16 @@ _lib.lq_matmul_workspace_bytes_precision.argtypes = [_i64, _i64, _i64, _int, _in
 _lib.lq_matmul.argtypes = [_vp, _i64, _i64, _i64, _vp, _vp, _vp, Config, _vp, _vp, _int, _int, _vp, _vp, _sz, _vp]
 _lib.lq_matmul_few_rows_static_scratch_bytes.restype = _sz
 _lib.lq_matmul_few_rows_static.argtypes = [_vp, _i64, _i64, _i64, _vp, _vp, _vp, Config, _vp, _vp, _int, _vp, _vp]
+_lib.lq_dropout.argtypes = [_vp, _i64, _int, C.c_double, C.c_uint64, C.c_uint64, _vp, _vp]
+_lib.lq_cross_entropy_workspace_bytes.restype = _sz
+_lib.lq_cross_entropy_workspace_bytes.argtypes = [_i64, _i64, _i64, _int, _int, _int]
+_lib.lq_cross_entropy.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _int, _int, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.lq_adapter_workspace_bytes.restype = _sz
+_lib.lq_adapter_workspace_bytes.argtypes = [_i64, _i64, _i64, _int, _int, _int]
+_lib.lq_adapter_forward.argtypes = [_vp, _i64, _i64, _i64, _vp, _vp, _vp, Config, _vp, _vp, _int, _int, C.c_double, C.c_uint64,
+                                    C.c_uint64, _vp, _vp, _vp, _sz, _vp]
+_lib.lq_adapter_backward.argtypes = [_vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp, Config, _vp, _vp, _int, _int, _vp, C.c_double,
+                                     C.c_uint64, C.c_uint64, _vp, _vp, _vp, _vp, _sz, _vp]
 
 _lib.lq_profile_enable.argtypes = [_int]
 _lib.lq_profile_class_name.restype = C.c_char_p
@@ -329,6 +340,119 @@ def matmul_few_rows_static(x: torch.Tensor, codes: torch.Tensor, scale_idx: torc
                                           _dev(l1, torch.float32, "l1"), _dev(l2, torch.float32, "l2"), rank,
                                           _dev(out, torch.float32, "out"), _stream()), "lq_matmul_few_rows_static")
     return out
+
+
+def _dtype(t: torch.Tensor, name: str) -> int:
+    if not (isinstance(t, torch.Tensor) and t.dtype in T_DTYPES):
+        raise TypeError(f"{name}: need a tensor of torch.float32 or torch.bfloat16")
+    return T_DTYPES[t.dtype]
+
+
+def _rows(t, dtype, name):
+    """Pointer and row stride of a matrix whose rows are contiguous."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.dim() == 2 and
+            (t.stride(1) == 1 or t.shape[1] == 1) and (t.shape[0] == 1 or t.stride(0) >= t.shape[1])):
+        raise TypeError(f"{name}: need a {dtype} matrix with contiguous rows on the GPU")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _shaped(t, shape, name):
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, need {tuple(shape)}")
+
+
+def _stored(codes, scale_idx, v, cfg, n):
+    """The quantized component's buffers have to hold n weights: the kernels read them by the configuration's sizes."""
+    if (codes.numel() < codes_bytes(n, cfg.bits) or scale_idx.numel() * max(cfg.block, 1) < n or
+            v.numel() * max(cfg.block, 1) * max(cfg.scale_block, 1) < n):
+        raise ValueError("codes, scale_idx or v too small for the matrix")
+
+
+def dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, out: torch.Tensor | None = None) -> torch.Tensor:
+    """y = kept ? x / (1 - p) : 0 with the mask of (seed, offset, element); the gradient is the same call on dy.
+    `out`: tensor like x to write into, x itself among them."""
+    code = _dtype(x, "x")
+    if out is None:
+        out = torch.empty_like(x)
+    _shaped(out, x.shape, "out")
+    _check(_lib.lq_dropout(_dev(x, x.dtype, "x"), x.numel(), code, p, seed, offset, _dev(out, x.dtype, "out"), _stream()),
+           "lq_dropout")
+    return out
+
+
+def cross_entropy_workspace(n: int, d: int, vocab: int, dtype=torch.float32, want_dx: bool = True, want_dw: bool = False,
+                            device="cuda") -> torch.Tensor:
+    return _workspace(_lib.lq_cross_entropy_workspace_bytes(n, d, vocab, T_DTYPES[dtype], int(want_dx), int(want_dw)), device)
+
+
+def cross_entropy(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, mean: bool = True, want_dx: bool = True,
+                  want_dw: bool = False, workspace: torch.Tensor | None = None):
+    """Softmax cross entropy of the logits X W^T, which are never stored, against `targets` (rows with a target outside the
+    vocabulary do not count): -> dict(loss, row_loss, lse, dx, dw), the gradients being those of `loss`, None if not wanted."""
+    code = _dtype(x, "x")
+    (xp, ldx), (wp, ldw) = _rows(x, x.dtype, "x"), _rows(w, x.dtype, "w")
+    n, d = x.shape
+    vocab = w.shape[0]
+    _shaped(w, (vocab, d), "w")
+    _shaped(targets, (n,), "targets")
+    ws = workspace if workspace is not None else cross_entropy_workspace(n, d, vocab, x.dtype, want_dx, want_dw, x.device)
+    out = dict(loss=torch.empty((), dtype=torch.float32, device=x.device),
+               row_loss=torch.empty(n, dtype=torch.float32, device=x.device),
+               lse=torch.empty(n, dtype=torch.float32, device=x.device),
+               dx=torch.empty((n, d), dtype=x.dtype, device=x.device) if want_dx else None,
+               dw=torch.empty((vocab, d), dtype=x.dtype, device=x.device) if want_dw else None)
+    ptr = {name: None if t is None else t.data_ptr() for name, t in out.items()}
+    _check(_lib.lq_cross_entropy(xp, ldx, wp, ldw, _dev(targets, torch.int64, "targets"), n, d, vocab, code, int(mean), ptr["loss"],
+                                 ptr["row_loss"], ptr["lse"], ptr["dx"], ptr["dw"], _aligned_ptr(ws),
+                                 ws.numel() - (_aligned_ptr(ws) - ws.data_ptr()), _stream()), "lq_cross_entropy")
+    return out
+
+
+def adapter_workspace(m: int, d: int, k: int, rank: int, dtype=torch.float32, backward: bool = False, device="cuda") -> torch.Tensor:
+    return _workspace(_lib.lq_adapter_workspace_bytes(m, d, k, rank, T_DTYPES[dtype], int(backward)), device)
+
+
+def adapter_forward(x: torch.Tensor, codes: torch.Tensor, scale_idx: torch.Tensor, v: torch.Tensor, cfg: Config,
+                    l1: torch.Tensor, l2: torch.Tensor, p: float = 0.0, seed: int = 0, offset: int = 0,
+                    workspace: torch.Tensor | None = None):
+    """T = drop(X) L1, Y = X Q + T L2: -> (Y, T); T is what adapter_backward takes."""
+    code = _dtype(x, "x")
+    m, d = x.shape
+    rank, k = l2.shape
+    _shaped(l1, (d, rank), "l1")
+    _stored(codes, scale_idx, v, cfg, d * k)
+    ws = workspace if workspace is not None else adapter_workspace(m, d, k, rank, x.dtype, False, x.device)
+    y = torch.empty((m, k), dtype=x.dtype, device=x.device)
+    t = torch.empty((m, rank), dtype=torch.float32, device=x.device)
+    _check(_lib.lq_adapter_forward(_dev(x, x.dtype, "x"), m, d, k, _dev(codes, torch.uint8, "codes"),
+                                   _dev(scale_idx, torch.uint8, "scale_idx"), _dev(v, torch.float32, "v"), cfg,
+                                   _dev(l1, torch.float32, "l1"), _dev(l2, torch.float32, "l2"), rank, code, p, seed, offset,
+                                   y.data_ptr(), t.data_ptr(), _aligned_ptr(ws),
+                                   ws.numel() - (_aligned_ptr(ws) - ws.data_ptr()), _stream()), "lq_adapter_forward")
+    return y, t
+
+
+def adapter_backward(dy: torch.Tensor, x: torch.Tensor, codes: torch.Tensor, scale_idx: torch.Tensor, v: torch.Tensor, cfg: Config,
+                     l1: torch.Tensor, l2: torch.Tensor, t: torch.Tensor, p: float = 0.0, seed: int = 0, offset: int = 0,
+                     want_dx: bool = True, workspace: torch.Tensor | None = None):
+    """Gradients of adapter_forward with the same p, seed and offset: -> (dX or None, dL1, dL2)."""
+    code = _dtype(x, "x")
+    m, d = x.shape
+    rank, k = l2.shape
+    _shaped(dy, (m, k), "dy")
+    _shaped(l1, (d, rank), "l1")
+    _shaped(t, (m, rank), "t")
+    _stored(codes, scale_idx, v, cfg, d * k)
+    ws = workspace if workspace is not None else adapter_workspace(m, d, k, rank, x.dtype, True, x.device)
+    dx = torch.empty((m, d), dtype=x.dtype, device=x.device) if want_dx else None
+    dl1, dl2 = torch.empty_like(l1), torch.empty_like(l2)
+    _check(_lib.lq_adapter_backward(_dev(dy, x.dtype, "dy"), _dev(x, x.dtype, "x"), m, d, k, _dev(codes, torch.uint8, "codes"),
+                                    _dev(scale_idx, torch.uint8, "scale_idx"), _dev(v, torch.float32, "v"), cfg,
+                                    _dev(l1, torch.float32, "l1"), _dev(l2, torch.float32, "l2"), rank, code,
+                                    _dev(t, torch.float32, "t"), p, seed, offset, None if dx is None else dx.data_ptr(),
+                                    dl1.data_ptr(), dl2.data_ptr(), _aligned_ptr(ws),
+                                    ws.numel() - (_aligned_ptr(ws) - ws.data_ptr()), _stream()), "lq_adapter_backward")
+    return dx, dl1, dl2
 
 
 def assign_configs(err: np.ndarray, storage: np.ndarray, budget_bits: float, node_limit: int = 0):

@@ -1,0 +1,463 @@
+"""GPU parity of the training operators (dropout, softmax cross entropy with its gradients, the adapter product with dropout and
+its gradients) against plain 64-bit definitions on the host.
+
+Tolerances (derived from the arithmetic, before any run).  eps of a product of fp32 operands split into bf16 hi + lo: 4e-5 of
+|a||b| (the bound of the forward product); of bf16 operands, whose products are exact: fp32 accumulation, taken as K 2^-23 with a
+floor of 1e-6.  A logit is off by at most delta = eps |x||w|; the log-sum-exp and a row loss by twice that and a few units of fp32;
+a probability by the factor 1 +- 2 delta.  What goes into a second product in bf16 is rounded by 2^-9 (two planes: 2^-17), the
+result by 2^-9 for bf16 outputs.  Each bound below is that sum, elementwise, with the absolute values of the terms."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+OUT = {"fp32": 2.0 ** -23, "bf16": 2.0 ** -8}       # rounding of a result, with room for a neighbour
+MID = {"fp32": 2.0 ** -16, "bf16": 2.0 ** -8}       # rounding of an operand between two products
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    assert torch.cuda.is_available()
+    from paper_2311_12023_amd import lq
+    return torch, lq
+
+
+def _type(torch, name):
+    return {"fp32": torch.float32, "bf16": torch.bfloat16}[name]
+
+
+def _eps(dtype, depth):
+    return 4e-5 if dtype == "fp32" else max(1e-6, depth * 2.0 ** -23)
+
+
+def _kept(n, p, seed, offset, first=0):
+    """Philox4x32-7 as the header defines the mask, elements first .. first + n - 1 (first a multiple of 8)."""
+    u64, low = np.uint64, np.uint64(0xFFFFFFFF)
+    g = np.arange((n + 7) // 8, dtype=u64) + u64(first // 8)
+    c = [g & low, g >> u64(32), np.full_like(g, offset & 0xFFFFFFFF), np.full_like(g, offset >> 32)]
+    k0, k1 = seed & 0xFFFFFFFF, seed >> 32
+    for _ in range(7):
+        a, b = c[0] * u64(0xD2511F53), c[2] * u64(0xCD9E8D57)
+        c = [(b >> u64(32)) ^ c[1] ^ u64(k0), b & low, (a >> u64(32)) ^ c[3] ^ u64(k1), a & low]
+        k0, k1 = (k0 + 0x9E3779B9) & 0xFFFFFFFF, (k1 + 0xBB67AE85) & 0xFFFFFFFF
+    bits = np.stack(c, 1).astype("<u4").view("<u2").reshape(-1)[:n]
+    return bits >= int(np.floor(65536 * p + 0.5))
+
+
+def _factor(p):
+    cut = int(np.floor(65536 * p + 0.5))
+    return np.float32(65536.0 / (65536 - cut)) if cut < 65536 else np.float32(0)
+
+
+# ---------------------------------------------------------------- dropout
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,p,seed,offset", [(1, 0.5, 1, 0), (7, 0.5, 2, 3), (8, 0.1, 3, 0), (9, 0.9, 4, 0), (2047, 0.05, 5, 1 << 40),
+                                             (100003, 0.3, (1 << 63) + 11, 6), (65536, 0.0, 7, 0), (4099, 1.0, 8, 0),
+                                             (512, 2.0 ** -18, 9, 0), (40000, 1 - 2.0 ** -16, 10, 0)])
+def test_dropout_bit_for_bit(env, dtype, n, p, seed, offset):
+    torch, lq = env
+    x = torch.from_numpy(np.random.default_rng(n).standard_normal(n).astype(np.float32)).to(_type(torch, dtype))
+    want = torch.where(torch.from_numpy(_kept(n, p, seed, offset)), x.float() * float(_factor(p)), torch.zeros(n)).to(x.dtype)
+    got = lq.dropout(x.cuda(), p, seed, offset)
+    assert torch.equal(got.cpu(), want)
+    inplace = x.cuda()
+    assert lq.dropout(inplace, p, seed, offset, out=inplace) is inplace and torch.equal(inplace.cpu(), want)
+
+
+def test_dropout_off_the_vector_alignment(env):
+    torch, lq = env
+    for dtype in (torch.float32, torch.bfloat16):
+        base = torch.randn(1037, device="cuda").to(dtype)
+        for cut in (1, 3, 4):
+            x = base[cut:]
+            assert torch.equal(lq.dropout(x, 0.25, 5), lq.dropout(x.clone(), 0.25, 5))
+
+
+def test_dropout_drops_what_is_not_finite(env):
+    torch, lq = env
+    x = torch.full((4096,), float("nan"), device="cuda")
+    x[::3] = float("inf")
+    y = lq.dropout(x, 0.5, 77).cpu().numpy()
+    kept = _kept(4096, 0.5, 77, 0)
+    assert np.all(y[~kept] == 0) and not np.any(np.isfinite(y[kept]))
+    assert abs(kept.mean() - 0.5) < 0.05
+
+
+def test_dropout_past_32_bit_indices(env):
+    """More than 2^32 bytes, and elements whose group number passes 2^29: the last ones against the definition."""
+    torch, lq = env
+    n = (1 << 32) + 24
+    x = torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    y = lq.dropout(x, 0.5, 3, 4)
+    want = np.where(_kept(4096 + 24, 0.5, 3, 4, first=n - 4096 - 24), 2.0, 0.0)
+    assert np.array_equal(y[-(4096 + 24):].float().cpu().numpy(), want)
+
+
+# ---------------------------------------------------------------- softmax cross entropy
+
+def _loss_reference(x, w, t, mean, delta_eps):
+    """-> loss, row_loss, lse, dx, dw in float64, the bound of a logit's error per row, and the absolute terms of dx and dw."""
+    n, vocab = x.shape[0], w.shape[0]
+    s = x @ w.T
+    counts = (t >= 0) & (t < vocab)
+    top = s.max(1, keepdims=True)
+    e = np.exp(s - top)
+    lse = (top + np.log(e.sum(1, keepdims=True)))[:, 0]
+    p = np.exp(s - lse[:, None])
+    rows = np.nonzero(counts)[0]
+    others = p.copy()
+    others[rows, t[rows]] = 0
+    q = others.sum(1)
+    row_loss = np.zeros(n)
+    row_loss[rows] = lse[rows] - s[rows, t[rows]]
+    f = 1.0 / max(1, rows.size) if mean else 1.0
+    g = others * f
+    g[rows, t[rows]] = -q[rows] * f
+    g[~counts] = 0
+    xs = np.where(counts[:, None], x, 0)
+    delta = delta_eps * (np.abs(x) @ np.abs(w).T).max(1) + 2.0 ** -21 * np.abs(s).max(1)
+    return dict(loss=row_loss.sum() * f, row_loss=row_loss, lse=lse, dx=g @ w, dw=g.T @ xs), delta, np.abs(g) @ np.abs(w), \
+        np.abs(g).T @ (np.abs(xs) * (delta[:, None])), np.abs(g).T @ np.abs(xs), f
+
+
+def _check_loss(env, x, w, t, dtype, mean=True, out=None):
+    """x, w: torch tensors on the GPU of type dtype."""
+    torch, lq = env
+    o = out if out is not None else lq.cross_entropy(x, w, t, mean=mean, want_dx=True, want_dw=True)
+    got = {k: v.double().cpu().numpy() for k, v in o.items() if v is not None}
+    ref, delta, adx, adw_delta, adw, f = _loss_reference(x.double().cpu().numpy(), w.double().cpu().numpy(), t.cpu().numpy(), mean,
+                                                         _eps(dtype, x.shape[1]))
+    for name in ("row_loss", "lse"):
+        assert np.all(np.abs(got[name] - ref[name]) <= 2 * delta + 4e-7 * (1 + np.abs(ref[name]))), name
+    counted = int(((t >= 0) & (t < w.shape[0])).sum())
+    assert abs(got["loss"] - ref["loss"]) <= 2 * f * delta.sum() + 1e-6 * (1 + abs(ref["loss"])) * max(1, 0 if mean else counted)
+    if "dx" in got:
+        # the second product has its own split / accumulation error
+        bound = adx * (6 * delta[:, None] + MID[dtype] + _eps(dtype, w.shape[0])) + OUT[dtype] * np.abs(ref["dx"]) + 1e-30
+        assert np.all(np.abs(got["dx"] - ref["dx"]) <= bound), np.max(np.abs(got["dx"] - ref["dx"]) / bound)
+    if "dw" in got:
+        bound = 6 * adw_delta + adw * (MID[dtype] + _eps(dtype, x.shape[0])) + OUT[dtype] * np.abs(ref["dw"]) + 1e-30
+        assert np.all(np.abs(got["dw"] - ref["dw"]) <= bound), np.max(np.abs(got["dw"] - ref["dw"]) / bound)
+    return got
+
+
+def _loss_inputs(torch, n, d, vocab, dtype, seed, ignored=0.2, lean=10.0):
+    rng = np.random.default_rng(seed)
+    w = rng.standard_normal((vocab, d)) * (2.0 / np.sqrt(d))
+    t = rng.integers(0, vocab, n)
+    x = rng.standard_normal((n, d)) + lean * rng.random((n, 1)) * w[t] / 4
+    t[rng.random(n) < ignored] = -100
+    tensor = lambda a: torch.from_numpy(a.astype(np.float32)).cuda().to(_type(torch, dtype))
+    return tensor(x), tensor(w), torch.from_numpy(t).cuda()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,d,vocab", [
+    (1, 32, 1),              # one class: the loss and the gradients are zero
+    (1, 64, 2),
+    (1, 1, 3),               # one feature
+    (3, 40, 255),            # a class short of a tile, rows that are not whole steps
+    (5, 64, 257),            # one class past a tile
+    (16, 96, 1000),
+    (17, 33, 511),
+    (64, 256, 4099),
+    (65, 100, 700),
+    (255, 64, 513),          # a row short of a tile
+    (257, 96, 300),          # a row past a tile
+    (300, 520, 1030),
+    (700, 64, 50000),        # several pieces, the last one short
+    (33, 1024, 2000),        # a reduction that is cut into ranges
+])
+def test_loss_matches_definition(env, n, d, vocab, dtype):
+    torch, lq = env
+    x, w, t = _loss_inputs(torch, n, d, vocab, dtype, 100 + n + vocab)
+    _check_loss(env, x, w, t, dtype, mean=n % 2 == 0)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_loss_outputs_do_not_depend_on_what_else_is_wanted(env, dtype):
+    torch, lq = env
+    x, w, t = _loss_inputs(torch, 70, 128, 3000, dtype, 7)
+    full = lq.cross_entropy(x, w, t, want_dx=True, want_dw=True)
+    for dx in (False, True):
+        for dw in (False, True):
+            o = lq.cross_entropy(x, w, t, want_dx=dx, want_dw=dw)
+            assert (o["dx"] is not None) == dx and (o["dw"] is not None) == dw
+            _check_loss(env, x, w, t, dtype, out=o)
+            if dx and dw:
+                assert all(torch.equal(o[k], full[k]) for k in o)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_loss_of_rows_in_order_of_growing_logits(env, dtype):
+    """Classes sorted by their logits, over several pieces: the reference a row's sum is relative to grows with every tile, and
+    the largest logits are far from the first."""
+    torch, lq = env
+    n, d, vocab = 600, 64, 70000
+    x, w, t = _loss_inputs(torch, n, d, vocab, dtype, 21)
+    order = torch.argsort(w.float() @ x[0].float())
+    w = w[order].contiguous()
+    x = x * 3
+    x[1] = x[0]
+    x[2] = -x[0]
+    _check_loss(env, x, w, t, dtype)
+
+
+def test_loss_of_certain_rows(env):
+    """Rows that are certain of their target (1 - p near 1e-13) and of another class: loss and gradient keep their relative
+    accuracy."""
+    torch, lq = env
+    d, vocab, n = 64, 5000, 8
+    x, w, t = _loss_inputs(torch, n, d, vocab, "bf16", 31, ignored=0.0, lean=0.0)
+    wt = w[t].float()
+    gain = torch.tensor([10.0, 20.0, 30.0, 40.0, 60.0, -30.0, -60.0, 0.0], device="cuda")[:, None]
+    x = (x.float() * 0.1 + gain * wt / (wt * wt).sum(1, keepdim=True)).bfloat16()
+    got = _check_loss(env, x, w, t, "bf16")
+    s = x.double().cpu().numpy() @ w.double().cpu().numpy().T
+    tt = t.cpu().numpy()
+    for i in range(5):
+        z = np.exp(s[i] - s[i, tt[i]])
+        z[tt[i]] = 0
+        want = np.log1p(z.sum())
+        assert abs(got["row_loss"][i] - want) <= 3e-4 * want, (i, got["row_loss"][i], want)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_loss_with_rows_that_do_not_count(env, dtype):
+    """Rows without a target in the vocabulary, whatever they hold (NaN, infinities, the type's lowest value), change nothing
+    else and get zeros; with none left the loss is zero."""
+    torch, lq = env
+    x, w, t = _loss_inputs(torch, 90, 72, 1500, dtype, 41, ignored=0.0)
+    t[10:40] = torch.tensor([-1, -100, 1500, 1 << 40, -(1 << 62)] * 6, device="cuda")
+    clean = lq.cross_entropy(x, w, t, want_dw=True)
+    x[10:20], x[20:25], x[25:30] = float("nan"), float("inf"), torch.finfo(x.dtype).min
+    o = lq.cross_entropy(x, w, t, want_dw=True)
+    for k in ("loss", "row_loss", "dx", "dw"):
+        assert torch.equal(o[k], clean[k]), k
+    assert torch.all(o["dx"][10:40] == 0) and torch.all(o["row_loss"][10:40] == 0)
+    t[:] = -100
+    o = lq.cross_entropy(x, w, t, want_dw=True)
+    assert float(o["loss"]) == 0 and all(torch.all(o[k] == 0) for k in ("row_loss", "dx", "dw"))
+
+
+def test_loss_keeps_what_is_not_finite_in_its_row(env):
+    torch, lq = env
+    x, w, t = _loss_inputs(torch, 20, 64, 600, "bf16", 51, ignored=0.0)
+    clean = lq.cross_entropy(x, w, t)
+    x[7] = float("nan")
+    o = lq.cross_entropy(x, w, t)
+    rest = [i for i in range(20) if i != 7]
+    assert torch.equal(o["row_loss"][rest], clean["row_loss"][rest]) and torch.equal(o["dx"][rest], clean["dx"][rest])
+    assert torch.isnan(o["row_loss"][7]) and torch.isnan(o["loss"]) and torch.all(torch.isnan(o["dx"][7]))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_loss_takes_rows_with_strides(env, dtype):
+    """Slices of wider matrices, on and off the 16-byte addresses, bit for bit what contiguous copies give."""
+    torch, lq = env
+    x, w, t = _loss_inputs(torch, 50, 96, 900, dtype, 61)
+    want = lq.cross_entropy(x, w, t, want_dw=True)
+    for pad, at in ((16, 8), (5, 1), (24, 0)):
+        wide_x, wide_w = torch.full((50, 96 + pad), float("nan"), device="cuda").to(x.dtype), \
+            torch.full((900, 96 + pad), float("nan"), device="cuda").to(x.dtype)
+        wide_x[:, at:at + 96], wide_w[:, at:at + 96] = x, w
+        o = lq.cross_entropy(wide_x[:, at:at + 96], wide_w[:, at:at + 96], t, want_dw=True)
+        assert all(torch.equal(o[k], want[k]) for k in o), (pad, at)
+
+
+def test_loss_gradient_against_differences(env):
+    """Central differences of the loss itself, fp32."""
+    torch, lq = env
+    x, w, t = _loss_inputs(torch, 12, 48, 300, "fp32", 71)
+    o = lq.cross_entropy(x, w, t, mean=False, want_dw=True)
+    rng = np.random.default_rng(1)
+    for which, grad in ((x, o["dx"]), (w, o["dw"])):
+        dirn = torch.from_numpy(rng.standard_normal(tuple(which.shape)).astype(np.float32)).cuda()
+        h = 1e-2
+        ends = []
+        for sign in (1, -1):
+            moved = which + sign * h * dirn
+            a, b = (moved, w) if which is x else (x, moved)
+            ends.append(lq.cross_entropy(a, b, t, mean=False, want_dx=False)["row_loss"].double().sum())
+        slope, want = float(ends[0] - ends[1]) / (2 * h), float((grad.double() * dirn.double()).sum())
+        # third derivative of the loss along the direction: at most the cube of the logits' spread (about 10), times h^2 / 6
+        assert abs(slope - want) <= 12 * 10.0 ** 3 * h * h / 6 * 0.1 + 1e-2, (slope, want)
+
+
+def test_loss_is_deterministic_and_ignores_workspace_contents(env):
+    torch, lq = env
+    x, w, t = _loss_inputs(torch, 600, 160, 30000, "bf16", 81)
+    ws = lq.cross_entropy_workspace(600, 160, 30000, torch.bfloat16, want_dw=True)
+    ws.fill_(0)
+    a = lq.cross_entropy(x, w, t, want_dw=True, workspace=ws)
+    ws.fill_(0xff)
+    b = lq.cross_entropy(x, w, t, want_dw=True, workspace=ws)
+    assert all(torch.equal(a[k], b[k]) for k in a)
+
+
+# ---------------------------------------------------------------- adapter products
+
+def _adapter_inputs(torch, lq, m, d, k, cfg, rank, dtype, seed):
+    rng = np.random.default_rng(seed)
+    tensor = lambda a: torch.from_numpy(np.ascontiguousarray(a, np.float32)).cuda()
+    c = lq.config(*cfg)
+    stored = lq.nf_quantize(tensor(rng.standard_normal((d, k)) * 0.05).reshape(-1), c)
+    x = tensor(rng.standard_normal((m, d))).to(_type(torch, dtype))
+    dy = tensor(rng.standard_normal((m, k))).to(_type(torch, dtype))
+    return c, stored, x, dy, tensor(rng.standard_normal((d, rank)) * 0.1), tensor(rng.standard_normal((rank, k)) * 0.1)
+
+
+SHAPES = [
+    (1, 32, 64, (4, 16, 16), 1),
+    (5, 64, 48, (3, 16, 16), 7),             # k = 48: the reduction over dY ends inside a step
+    (37, 96, 128, (4, 64, 256), 32),
+    (64, 160, 144, (2, 16, 16), 33),
+    (65, 256, 384, (8, 64, 64), 64),
+    (130, 1056, 272, (8, 16, 64), 40),
+    (257, 288, 512, (4, 32, 64), 65),        # ranks past 64 and up to the largest
+    (300, 128, 320, (3, 64, 256), 128),
+    (520, 512, 1040, (4, 16, 256), 16),
+    (1025, 96, 64, (4, 64, 16), 8),
+]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("p", [0.0, 0.3])
+@pytest.mark.parametrize("m,d,k,cfg,rank", SHAPES)
+def test_adapter_matches_definition(env, m, d, k, cfg, rank, p, dtype):
+    torch, lq = env
+    c, stored, x, dy, l1, l2 = _adapter_inputs(torch, lq, m, d, k, cfg, rank, dtype, m + d)
+    seed, offset = (1 << 40) + m, 17
+    y, t = lq.adapter_forward(x, *stored, c, l1, l2, p, seed, offset)
+    dx, dl1, dl2 = lq.adapter_backward(dy, x, *stored, c, l1, l2, t, p, seed, offset)
+    f64 = lambda a: a.double().cpu().numpy()
+    q = f64(lq.nf_dequantize(*stored, d * k, c)).reshape(d, k)
+    X, DY, L1, L2, T = f64(x), f64(dy), f64(l1), f64(l2), f64(t)
+    mask = _kept(m * d, p, seed, offset).reshape(m, d) * float(_factor(p))
+    xd = X * mask
+    thin = 4e-5                                       # split products whatever the type of X
+    main = 4e-5 if dtype == "fp32" else 2.0 ** -8     # the weights (and T, U, L1, L2 where they meet them) rounded to bf16
+    out = OUT[dtype]
+    A = np.abs
+
+    def close(got, want, scale, eps, rounded):
+        bound = eps * scale + rounded * A(want) + 1e-30
+        assert got.shape == want.shape and np.all(A(got - want) <= bound), np.max(A(got - want) / bound)
+
+    close(T, xd @ L1, A(xd) @ A(L1), thin, 2.0 ** -23)
+    close(f64(y), X @ q + T @ L2, A(X) @ A(q) + A(T) @ A(L2), main, out)
+    u, au = DY @ L2.T, A(DY) @ A(L2).T
+    close(f64(dx), DY @ q.T + mask * (u @ L1.T), A(DY) @ A(q).T + mask * (au @ A(L1).T), main, out)
+    close(f64(dl1), xd.T @ u, A(xd).T @ au, 2 * thin, 2.0 ** -23)
+    close(f64(dl2), T.T @ DY, A(T).T @ A(DY), thin, 2.0 ** -23)
+    none, dl1b, dl2b = lq.adapter_backward(dy, x, *stored, c, l1, l2, t, p, seed, offset, want_dx=False)
+    assert none is None and torch.equal(dl1, dl1b) and torch.equal(dl2, dl2b)
+
+
+def test_adapter_agrees_with_dropout_and_matmul(env):
+    """T is drop(X) L1 of lq_dropout's own drop(X); without dropout Y is lq_matmul's product."""
+    torch, lq = env
+    c, stored, x, dy, l1, l2 = _adapter_inputs(torch, lq, 200, 256, 512, (4, 64, 256), 16, "fp32", 3)
+    y, t = lq.adapter_forward(x, *stored, c, l1, l2, 0.25, 99, 5)
+    _, t0 = lq.adapter_forward(lq.dropout(x, 0.25, 99, 5), *stored, c, l1, l2)
+    scale = (x.abs().double() @ l1.abs().double()) / 0.75
+    assert torch.all((t - t0).abs() <= 8e-5 * scale)
+    y0, _ = lq.adapter_forward(x, *stored, c, l1, l2)
+    ref = lq.matmul(x, *stored, c, 512, l1, l2)
+    q = lq.nf_dequantize(*stored, 256 * 512, c).reshape(256, 512).abs().double()
+    bound = x.abs().double() @ (q + l1.abs().double() @ l2.abs().double())
+    assert torch.all((y0 - ref).abs() <= 8e-5 * bound)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_adapter_drops_what_is_not_finite(env, dtype):
+    """A dropped element's NaN reaches neither T nor dL1 (it does reach Y through X Q, as the formula says)."""
+    torch, lq = env
+    m, d, k, p, seed = 40, 64, 128, 0.5, 12
+    c, stored, x, dy, l1, l2 = _adapter_inputs(torch, lq, m, d, k, (4, 64, 16), 8, dtype, 8)
+    gone = ~torch.from_numpy(_kept(m * d, p, seed, 0).reshape(m, d)).cuda()
+    dirty = torch.where(gone, torch.full_like(x, float("nan")), x)
+    _, t = lq.adapter_forward(x, *stored, c, l1, l2, p, seed)
+    _, td = lq.adapter_forward(dirty, *stored, c, l1, l2, p, seed)
+    assert torch.equal(t, td)
+    a = lq.adapter_backward(dy, x, *stored, c, l1, l2, t, p, seed)
+    b = lq.adapter_backward(dy, dirty, *stored, c, l1, l2, t, p, seed)
+    assert all(torch.equal(i, j) for i, j in zip(a, b))
+
+
+def test_adapter_everything_dropped(env):
+    torch, lq = env
+    c, stored, x, dy, l1, l2 = _adapter_inputs(torch, lq, 33, 64, 128, (4, 64, 16), 8, "fp32", 9)
+    y, t = lq.adapter_forward(x, *stored, c, l1, l2, 1.0, 1)
+    dx, dl1, dl2 = lq.adapter_backward(dy, x, *stored, c, l1, l2, t, 1.0, 1)
+    assert torch.all(t == 0) and torch.all(dl1 == 0) and torch.all(dl2 == 0)
+    q = lq.nf_dequantize(*stored, 64 * 128, c).reshape(64, 128).double()
+    assert torch.all((dx - dy.double() @ q.T).abs() <= 4e-5 * (dy.double().abs() @ q.abs().T))
+
+
+def test_adapter_gradients_against_differences(env):
+    """Central differences of <dY, Y>, which is linear in L1, L2 and X each: the differences are exact up to rounding."""
+    torch, lq = env
+    m, d, k, p, seed = 24, 64, 96, 0.3, 5
+    c, stored, x, dy, l1, l2 = _adapter_inputs(torch, lq, m, d, k, (4, 32, 16), 8, "fp32", 10)
+    _, t = lq.adapter_forward(x, *stored, c, l1, l2, p, seed)
+    grads = lq.adapter_backward(dy, x, *stored, c, l1, l2, t, p, seed)
+    q = lq.nf_dequantize(*stored, d * k, c).reshape(d, k).double()
+    value = lambda a, b, e: float((lq.adapter_forward(a, *stored, c, b, e, p, seed)[0].double() * dy.double()).sum())
+    size = float((dy.abs().double() * (x.abs().double() @ (q.abs() + l1.abs().double() @ l2.abs().double()) / (1 - p))).sum())
+    for i, (which, g) in enumerate(zip((x, l1, l2), grads)):
+        step = torch.from_numpy(np.random.default_rng(i).standard_normal(tuple(which.shape)).astype(np.float32)).cuda() * which.abs()
+        args = [[x, l1, l2], [x, l1, l2]]
+        args[0][i], args[1][i] = which + step, which - step
+        slope = (value(*args[0]) - value(*args[1])) / 2
+        assert abs(slope - float((g.double() * step.double()).sum())) <= 4 * 4e-5 * size, i
+
+
+def test_adapter_is_deterministic_and_ignores_workspace_contents(env):
+    torch, lq = env
+    for dtype in ("fp32", "bf16"):
+        m, d, k, rank = 48, 2048, 256, 16             # few tiles: reductions are cut into ranges
+        c, stored, x, dy, l1, l2 = _adapter_inputs(torch, lq, m, d, k, (3, 64, 256), rank, dtype, 11)
+        outs = []
+        for fill in (0, 0xff):
+            ws = [lq.adapter_workspace(m, d, k, rank, x.dtype, backward=b).fill_(fill) for b in (False, True)]
+            y, t = lq.adapter_forward(x, *stored, c, l1, l2, 0.1, 3, workspace=ws[0])
+            outs.append((y, t) + lq.adapter_backward(dy, x, *stored, c, l1, l2, t, 0.1, 3, workspace=ws[1]))
+        assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+def test_training_operators_in_a_hip_graph(env):
+    """Every call only launches kernels: replays with new inputs, with eager work between them, give the eager results."""
+    torch, lq = env
+    m, d, k, rank, vocab = 40, 256, 128, 16, 700
+    c, stored, x, dy, l1, l2 = _adapter_inputs(torch, lq, m, d, k, (4, 64, 256), rank, "bf16", 12)
+    w = (torch.randn(vocab, k, device="cuda") * 0.1).bfloat16()
+    t = torch.randint(0, vocab, (m,), device="cuda")
+    ws = [lq.adapter_workspace(m, d, k, rank, x.dtype, backward=b) for b in (False, True)]
+    ws.append(lq.cross_entropy_workspace(m, k, vocab, x.dtype, want_dw=True))
+
+    def step():
+        xd = lq.dropout(x, 0.1, 4)
+        y, tt = lq.adapter_forward(xd, *stored, c, l1, l2, 0.1, 3, workspace=ws[0])
+        o = lq.cross_entropy(y, w, t, want_dw=True, workspace=ws[2])
+        return [y, tt, o["loss"], o["dx"], o["dw"], *lq.adapter_backward(o["dx"], xd, *stored, c, l1, l2, tt, 0.1, 3, workspace=ws[1])]
+
+    step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for i in range(4):
+        x.copy_(torch.randn(m, d, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [o.clone() for o in outs]
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
