@@ -314,8 +314,9 @@ int lq_matmul_few_rows_static(const float* X, int64_t m, int64_t d, int64_t k, c
  *
  * Activations (X, Y, dY, dX, and W, dW of the cross entropy) are of type `dtype`, LQ_T_FP32 or LQ_T_BF16; L1, L2, T, their
  * gradients, losses and log-sum-exps are fp32.  Sums, softmax statistics and accumulators are held in fp32 (the total loss in
- * fp64).  fp32 operands of a product are split into bf16 hi + lo and take three MFMAs (error about 2^-16 of sum |a||b|); with
- * bf16 activations the decoded weights, and T and U where they meet bf16 results, are rounded to bf16.  All calls only enqueue
+ * fp64).  fp32 operands of the large products are split into two fp16 planes, after a power of two that brings an operand's
+ * largest magnitude below 2^14 (22 bits; 2^-39 of that magnitude for the smallest), and take three MFMAs; those of the thin products
+ * into three bf16 planes (24 bits).  With bf16 activations the decoded weights are rounded to bf16.  All calls only enqueue
  * kernels on `stream`, are deterministic, and can be captured in a HIP graph after a first call on the device.
  */
 
@@ -338,7 +339,7 @@ int lq_dropout(const void* x, int64_t n, int dtype, double p, uint64_t seed, uin
  *            are 0.  If none counts, loss is 0 for sum and mean alike.
  *   loss 1 fp32, row_loss n fp32, lse n fp32 or NULL, dX n x d or NULL, dW vocab x d or NULL (contiguous, of type dtype)
  * The vocabulary is walked in pieces; the workspace holds one piece's exponentials.  dX comes out of the same pass as the loss,
- * dW takes a second one.  n and vocab up to 2^31 - 65537, d up to 2^20 (LQ_ERR_SHAPE).
+ * dW takes a second one.  n up to 2^23 - 64, vocab up to 2^31 - 65536, d up to 2^20 (LQ_ERR_SHAPE).
  */
 size_t lq_cross_entropy_workspace_bytes(int64_t n, int64_t d, int64_t vocab, int dtype, int want_dx, int want_dw);
 int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* targets, int64_t n, int64_t d,
@@ -355,8 +356,8 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
  *   X m x d, Y and dY m x k, dX m x d (NULL: not wanted, for a first layer): contiguous, of type dtype, 16-byte aligned
  *   codes_packed, scale_idx, v    Q as for lq_matmul        L1 d x rank, L2 rank x k (forward: 16-byte aligned)
  *   T        m x rank fp32, written by the forward and read by the backward call
- *   rank in [1, 128] (LQ_ERR_RANK); d a multiple of 32, k of the block size; ceil(m / 256) * 256 * max(d, k) and d * k below
- *   2^31 (LQ_ERR_SHAPE)
+ *   rank in [1, 128] (LQ_ERR_RANK); d a multiple of 32, k of the block size; m below 2^24, ceil(m / 256) * 256 * max(d, k) and
+ *   d * k below 2^31 (LQ_ERR_SHAPE)
  */
 size_t lq_adapter_workspace_bytes(int64_t m, int64_t d, int64_t k, int rank, int dtype, int backward);
 int lq_adapter_forward(const void* X, int64_t m, int64_t d, int64_t k, const uint8_t* codes_packed, const uint8_t* scale_idx,

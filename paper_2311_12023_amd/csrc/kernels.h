@@ -186,9 +186,6 @@ int launch_qrows(const MvWeights& q, const float* X, int64_t ldx, int64_t K, con
 // this pitch, 372 without; 12000 x 12288 470 and 553).
 inline int64_t plane_pitch(int64_t K) { return (K + 63) / 64 * 64; }
 size_t weight_plane_elems(int64_t pitch, int64_t N);
-// The decoding by itself (t.splits == 0: no partial tiles to add).
-int launch_weight_columns(const MvWeights& q, int64_t K, int64_t N, const float* L2, int rank, int Kd, uint16_t* Wt, uint16_t* Lt,
-                          const ProjectSum& t, hipStream_t st);
 int launch_plane_product(const MvWeights& q, const uint16_t* Xh, int64_t K, const uint16_t* Th, int Kd, const float* L2,
                          int rank, int64_t m, int64_t rows_pad, int64_t N, uint16_t* Wt, uint16_t* Lt, float* Y, int64_t ldy,
                          float* part, size_t part_floats, const ProjectSum& t, hipStream_t st);

@@ -10,6 +10,7 @@
 // logit's distance from log S, loss = log(1 + e^-z) and dX_i = g (1 - p_t) (E W / S - w_t), 1 - p_t = 1 / (1 + e^z), which
 // are as exact for a row that is certain of its target (p_t = 1 - 1e-9) as for any other; 1 - p_t from p_t would be lost there.
 // dW needs p itself, so it takes a second pass over the logits.
+#include "half_planes_device.h"
 #include "mfma_device.h"
 #include "profiler.h"
 #include "segment_gemm.h"
@@ -19,110 +20,125 @@ namespace lq {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
-__global__ __launch_bounds__(256) void loss_begin_kernel(LossRows r, int64_t n) {
+__global__ __launch_bounds__(256) void loss_begin_kernel(LossRows r, int64_t n, uint32_t* tops) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < 2) tops[i] = 0;
   if (i >= n) return;
   r.ref[i] = -__builtin_inff();
   r.sum[i] = 0.0f;
   r.target[i] = 0.0f;
 }
 
-int launch_loss_begin(const LossRows& r, int64_t n, hipStream_t st) {
+int launch_loss_begin(const LossRows& r, int64_t n, uint32_t* tops, hipStream_t st) {
   prof::Scope ps(prof::LOSS_ROWS, st, (double)n * 12.0);
-  hipLaunchKernelGGL(loss_begin_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, r, n);
+  hipLaunchKernelGGL(loss_begin_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, r, n, tops);
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }
 
+// What a logit's accumulator is multiplied by to become s log2 e: the operands' powers of two go out with it.
+__device__ __forceinline__ float logit_factor(const LossScales& s, int64_t token) {
+  return s.x_inv ? LOG2E * s.x_inv[token] * power_of_two(-half_exponent(*s.w_top)) : LOG2E;
+}
+
+// Four neighbouring classes of one token as planes.
+template <bool HALF>
+__device__ __forceinline__ void store_four(uint16_t* hi, uint16_t* lo, floatx4 v) {
+  if constexpr (HALF) {
+    halfx4 h, l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { const HalfPair p = split_half(v[e]); h[e] = p.hi; l[e] = p.lo; }
+    *reinterpret_cast<halfx4*>(hi) = h;
+    *reinterpret_cast<halfx4*>(lo) = l;
+  } else {
+    *reinterpret_cast<bf16x4*>(hi) = __builtin_convertvector(v, bf16x4);
+  }
+}
+
 // ------------------------------------------------------------------------------------------------
-// Logits of a piece.  Classes are the tile's rows and tokens its columns: a lane then holds 64 classes of one token, and the
-// maximum and the sum over the tile are reductions inside lanes, one exchange between the halves of a wavefront and one through
-// LDS between two wavefronts.
+// Logits of a piece.  Classes are the tile's rows and tokens its columns: a lane then holds 32 classes of each of its tokens, and
+// the maximum and the sum over the tile are reductions inside lanes, two exchanges between lanes and one through LDS between two
+// wavefronts.  E is rounded to bf16, 2^-9 of each term of a sum that ends up in the type of X; two fp16 planes where that is fp32.
 struct LogitsArgs {
   SegArgs g;
-  LossPiece p;
+  LossPiece p; LossScales s;
   const float* ref; float* target;
   float* part_ref; float* part_sum;
-  uint16_t* e_hi; uint16_t* e_lo; int64_t e_pitch;
+  uint16_t* e[2]; int64_t e_pitch;
 };
 
-__global__ __launch_bounds__(SEG_THREADS) void loss_logits_kernel(LogitsArgs a) {
+template <typename H>
+__global__ __launch_bounds__(SEG_THREADS, 2) void loss_logits_kernel(LogitsArgs a) {
+  constexpr bool HALF = !std::is_same<H, __bf16>::value;
   extern __shared__ __attribute__((aligned(16))) unsigned char seg_lds[];
   const SegTile t = seg_tile(a.g);
   if (!t.live) return;
-  floatx16 acc[4][2];
+  SegAcc acc;
   seg_clear(acc);
-  const int steps = a.g.seg[2].end;
-  seg_products(a.g, t, 0, steps, seg_lds, acc);
+  seg_products<H>(a.g, t, 0, a.g.pairs, seg_lds, acc);
   __syncthreads();                                   // the LDS now holds exchanges
   float* s_max = reinterpret_cast<float*>(seg_lds);  // [wm][column of the tile]
   float* s_sum = s_max + 2 * SEG_T;
   const int64_t class0 = (int64_t)t.tm * SEG_T + 128 * t.wm;                 // inside the piece
   const int64_t left = a.p.classes - class0;
   const int lim = (int)(left < 0 ? 0 : left < 128 ? left : 128);
-  float base[2];
+  float base[4];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int col = 64 * t.wn + 32 * j + t.ln;
+  for (int j = 0; j < 4; ++j) {
+    const int col = 64 * t.wn + 16 * j + t.l16;
     const int64_t token = (int64_t)t.tn * SEG_T + col;
     const bool live = token < a.p.n;
     const int64_t target = live ? a.p.targets[token] - a.p.v0 - class0 : -1;
     const int at = target >= 0 && target < lim ? (int)target : -1;
+    const float f = live ? logit_factor(a.s, token) : 0.0f;
     float top = -__builtin_inff();
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int row = 32 * i + 8 * (e >> 2) + 4 * t.lh + (e & 3);
-        float x = acc[i][j][e] * LOG2E;
+      for (int e = 0; e < 4; ++e) {
+        const int row = 16 * i + 4 * t.kg + e;
+        float x = acc[i][j][e] * f;
         if (row == at) { a.target[token] = x; x = -__builtin_inff(); }
         if (row >= lim) x = -__builtin_inff();
         acc[i][j][e] = x;
         top = fmaxf(top, x);
       }
+    top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
     s_max[t.wm * SEG_T + col] = top;
     base[j] = live ? a.ref[token] : 0.0f;
   }
   __syncthreads();
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int col = 64 * t.wn + 32 * j + t.ln;
+  for (int j = 0; j < 4; ++j) {
+    const int col = 64 * t.wn + 16 * j + t.l16;
     const int64_t token = (int64_t)t.tn * SEG_T + col;
     const float ref = fmaxf(base[j], ceilf(fmaxf(s_max[col], s_max[SEG_T + col])));
     base[j] = ref;
-    const float from = ref == -__builtin_inff() ? 0.0f : ref;                // nothing but the target so far
+    // nothing but the target so far: any reference will do
+    const float from = (ref == -__builtin_inff() ? 0.0f : ref) - (HALF ? (float)LOSS_E_SHIFT : 0.0f);
     float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
+      for (int e = 0; e < 4; ++e) {
         acc[i][j][e] = __builtin_amdgcn_exp2f(acc[i][j][e] - from);
         sum += acc[i][j][e];
       }
+    sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    s_sum[t.wm * SEG_T + col] = sum;
-    if (a.e_hi && token < a.p.n) {
-      // E in bf16: 2^-9 of each term of a sum that ends up in the type of X, and two planes where that is fp32
-      uint16_t* out = a.e_hi + token * a.e_pitch + class0 + 4 * t.lh;
-      uint16_t* low = a.e_lo + token * a.e_pitch + class0 + 4 * t.lh;
+    s_sum[t.wm * SEG_T + col] = HALF ? sum * power_of_two(-LOSS_E_SHIFT) : sum;
+    if (a.e[0] && token < a.p.n) {
+      const int64_t at = token * a.e_pitch + class0 + 4 * t.kg;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          bf16x2 h0, l0, h1, l1;
-          split_bf16(floatx2{acc[i][j][4 * q], acc[i][j][4 * q + 1]}, h0, l0);
-          split_bf16(floatx2{acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]}, h1, l1);
-          *reinterpret_cast<bf16x4*>(out + 32 * i + 8 * q) = bf16x4{h0[0], h0[1], h1[0], h1[1]};
-          if (a.e_lo) *reinterpret_cast<bf16x4*>(low + 32 * i + 8 * q) = bf16x4{l0[0], l0[1], l1[0], l1[1]};
-        }
+      for (int i = 0; i < 8; ++i) store_four<HALF>(a.e[0] + at + 16 * i, HALF ? a.e[1] + at + 16 * i : nullptr, acc[i][j]);
     }
   }
   __syncthreads();
-  if (t.wm == 0 && t.lh == 0) {
+  if (t.wm == 0 && t.kg == 0) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int col = 64 * t.wn + 32 * j + t.ln;
+    for (int j = 0; j < 4; ++j) {
+      const int col = 64 * t.wn + 16 * j + t.l16;
       const int64_t token = (int64_t)t.tn * SEG_T + col;
       if (token < a.p.n) {
         a.part_ref[(int64_t)t.tm * a.p.n + token] = base[j];
@@ -132,44 +148,51 @@ __global__ __launch_bounds__(SEG_THREADS) void loss_logits_kernel(LogitsArgs a) 
   }
 }
 
-static void fill_segments(SegArgs& g, const Planes& a, const Planes& b, int64_t depth) {
-  int count = 0, end = add_segments(g, &count, 0, a, b, depth);
-  for (; count < 6; ++count) { g.seg[count] = g.seg[0]; g.seg[count].end = end; }
+static int fill_segments(SegArgs& g, const Planes& a, const Planes& b, int64_t depth) {
+  if (depth < 64 || depth % 64) return LQ_ERR_SHAPE;
+  int count = 0;
+  add_segments(g, &count, a, b, depth);
+  return LQ_OK;
 }
-
-int launch_loss_logits(const Planes& w, const Planes& x, int64_t depth, const LossPiece& p, const LossRows& r, float* part_ref,
-                       float* part_sum, uint16_t* e_hi, uint16_t* e_lo, int64_t e_pitch, hipStream_t st) {
-  if (depth < 32 || depth % 32 || p.n < 1 || p.classes < 1) return LQ_ERR_SHAPE;
-  LogitsArgs a{};
-  fill_segments(a.g, w, x, depth);
-  a.g.rows_a = p.classes; a.g.rows_b = p.n;
-  a.g.tiles_m = (int)((p.classes + SEG_T - 1) / SEG_T); a.g.tiles_n = (int)((p.n + SEG_T - 1) / SEG_T); a.g.splits = 1;
-  a.p = p; a.ref = r.ref; a.target = r.target; a.part_ref = part_ref; a.part_sum = part_sum;
-  a.e_hi = e_hi; a.e_lo = e_lo; a.e_pitch = e_pitch;
-  static LdsLimit limit;
-  LQ_TRY(limit.raise(reinterpret_cast<const void*>(loss_logits_kernel), SEG_LDS));
-  prof::Scope ps(prof::LOSS_LOGITS, st, 2.0 * p.n * p.classes * depth);
-  hipLaunchKernelGGL(loss_logits_kernel, dim3(seg_grid(a.g)), dim3(SEG_THREADS), SEG_LDS, st, a);
+template <typename Args>
+static int launch_tiles(void (*kernel)(Args), LdsLimit& limit, const Args& a, hipStream_t st) {
+  LQ_TRY(limit.raise(reinterpret_cast<const void*>(kernel), SEG_LDS));
+  hipLaunchKernelGGL(kernel, dim3(seg_grid(a.g)), dim3(SEG_THREADS), SEG_LDS, st, a);
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }
 
+int launch_loss_logits(const Planes& w, const Planes& x, int64_t depth, const LossPiece& p, const LossRows& r, const LossScales& s,
+                       float* part_ref, float* part_sum, uint16_t* const e[2], int64_t e_pitch, hipStream_t st) {
+  LogitsArgs a{};
+  LQ_TRY(fill_segments(a.g, w, x, depth));
+  LQ_TRY(seg_shape(a.g, p.classes, p.n, 1));
+  a.p = p; a.s = s; a.ref = r.ref; a.target = r.target; a.part_ref = part_ref; a.part_sum = part_sum;
+  a.e[0] = e[0]; a.e[1] = e[1]; a.e_pitch = e_pitch;
+  static LdsLimit limit[2];
+  prof::Scope ps(prof::LOSS_LOGITS, st, 2.0 * p.n * p.classes * depth);
+  return s.x_inv ? launch_tiles(loss_logits_kernel<_Float16>, limit[0], a, st) : launch_tiles(loss_logits_kernel<__bf16>, limit[1], a, st);
+}
+
 // ------------------------------------------------------------------------------------------------
 // A wavefront joins the tiles' sums of one row.  Tiles whose E lies at a smaller power of two than the row's new one are
-// multiplied down, which in bf16 is exact (what leaves the range is below 2^-126 of the largest term).
+// multiplied down, which is exact (what leaves the range of bf16 is below 2^-126 of the largest term, that of fp16 below 2^-38).
 struct JoinArgs {
   LossPiece p; LossRows r;
   const float* part_ref; const float* part_sum; int tiles;
-  uint16_t* e_hi; uint16_t* e_lo; int64_t e_pitch;
+  uint16_t* e[2]; int64_t e_pitch;
 };
 
+template <typename H>
 __device__ __forceinline__ void scale_run(uint16_t* at, float f) {
-  bf16x4 v = *reinterpret_cast<const bf16x4*>(at);
+  typedef H hx4 __attribute__((ext_vector_type(4)));
+  hx4 v = *reinterpret_cast<const hx4*>(at);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) v[k] = (__bf16)((float)v[k] * f);
-  *reinterpret_cast<bf16x4*>(at) = v;
+  for (int k = 0; k < 4; ++k) v[k] = (H)((float)v[k] * f);
+  *reinterpret_cast<hx4*>(at) = v;
 }
 
+template <typename H>
 __global__ __launch_bounds__(256) void loss_join_kernel(JoinArgs a) {
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
@@ -191,28 +214,29 @@ __global__ __launch_bounds__(256) void loss_join_kernel(JoinArgs a) {
     a.r.shift[row] = shift;
     a.r.ref[row] = ref;
   }
-  if (!a.e_hi) return;
+  if (!a.e[0]) return;
   for (int t = 0; t < a.tiles; ++t) {
     const float mine = a.part_ref[(int64_t)t * a.p.n + row];
     if (mine == ref) continue;
     const float f = __builtin_amdgcn_exp2f(mine - from);
     const int64_t at = row * a.e_pitch + (int64_t)t * SEG_T + 4 * lane;
-    scale_run(a.e_hi + at, f);
-    if (a.e_lo) scale_run(a.e_lo + at, f);
+    scale_run<H>(a.e[0] + at, f);
+    if constexpr (!std::is_same<H, __bf16>::value) scale_run<H>(a.e[1] + at, f);
   }
 }
 
-int launch_loss_join(const LossPiece& p, const LossRows& r, const float* part_ref, const float* part_sum, uint16_t* e_hi,
-                     uint16_t* e_lo, int64_t e_pitch, hipStream_t st) {
-  JoinArgs a{p, r, part_ref, part_sum, (int)((p.classes + SEG_T - 1) / SEG_T), e_hi, e_lo, e_pitch};
+int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, const float* part_ref, const float* part_sum,
+                     uint16_t* const e[2], int64_t e_pitch, hipStream_t st) {
+  const JoinArgs a{p, r, part_ref, part_sum, (int)((p.classes + SEG_T - 1) / SEG_T), {e[0], e[1]}, e_pitch};
   prof::Scope ps(prof::LOSS_ROWS, st, (double)p.n * a.tiles * 8.0);
-  hipLaunchKernelGGL(loss_join_kernel, dim3((unsigned)((p.n + 3) / 4)), dim3(256), 0, st, a);
+  auto kernel = half ? loss_join_kernel<_Float16> : loss_join_kernel<__bf16>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((p.n + 3) / 4)), dim3(256), 0, st, a);
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }
 
 // ------------------------------------------------------------------------------------------------
-// acc = acc shift + E W: tokens are the tile's rows, features its columns.
+// acc = acc shift + E W: features are the tile's rows and tokens its columns, so that a lane holds four neighbours of a row of acc.
 struct AccumulateArgs {
   SegArgs g;
   int64_t n, d;
@@ -220,19 +244,36 @@ struct AccumulateArgs {
   float* acc; float* part;
 };
 
-__global__ __launch_bounds__(SEG_THREADS) void loss_accumulate_kernel(AccumulateArgs a) {
+// Four neighbours of a row of `width` floats, whose start is on 16 bytes where width is a multiple of four.
+__device__ __forceinline__ void store_floats(float* at, floatx4 v, int64_t col, int64_t width) {
+  if ((width & 3) == 0) { *reinterpret_cast<floatx4*>(at) = v; return; }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (col + e < width) at[e] = v[e];
+}
+__device__ __forceinline__ floatx4 load_floats(const float* at, int64_t col, int64_t width) {
+  if ((width & 3) == 0) return *reinterpret_cast<const floatx4*>(at);
+  floatx4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = col + e < width ? at[e] : 0.0f;
+  return v;
+}
+
+template <typename H>
+__global__ __launch_bounds__(SEG_THREADS, 2) void loss_accumulate_kernel(AccumulateArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char seg_lds[];
   const SegTile t = seg_tile(a.g);
   if (!t.live) return;
-  floatx16 acc[4][2];
+  SegAcc acc;
   seg_clear(acc);
-  const int steps = a.g.seg[2].end;
-  seg_products(a.g, t, (int)((int64_t)steps * t.split / a.g.splits), (int)((int64_t)steps * (t.split + 1) / a.g.splits), seg_lds, acc);
-  float* part = a.part + (size_t)t.split * (size_t)a.n * (size_t)a.d;
-  seg_each(t, [&](int i, int j, int e, int64_t row, int64_t col) {
-    if (row >= a.n || col >= a.d) return;
-    if (a.g.splits > 1) part[row * a.d + col] = acc[i][j][e];
-    else a.acc[row * a.d + col] = a.first ? acc[i][j][e] : fmaf(a.acc[row * a.d + col], a.shift[row], acc[i][j][e]);
+  seg_products<H>(a.g, t, seg_first(a.g.pairs, t.split, a.g.splits), seg_first(a.g.pairs, t.split + 1, a.g.splits), seg_lds, acc);
+  float* out = a.g.splits > 1 ? a.part + (size_t)t.split * (size_t)a.n * (size_t)a.d : a.acc;
+  const bool add = a.g.splits == 1 && !a.first;
+  seg_each(t, acc, [&](floatx4 v, int64_t col, int64_t token) {
+    if (token >= a.n || col >= a.d) return;
+    float* at = out + token * a.d + col;
+    if (add) v = load_floats(at, col, a.d) * a.shift[token] + v;
+    store_floats(at, v, col, a.d);
   });
 }
 
@@ -246,26 +287,22 @@ __global__ __launch_bounds__(256) void loss_accumulate_sum_kernel(const float* _
   }
 }
 
-int loss_accumulate_splits(int64_t n, int64_t d, int64_t depth, int planes) {
-  return seg_splits(((n + SEG_T - 1) / SEG_T) * ((d + SEG_T - 1) / SEG_T), (int)(depth / 32) * (planes == 2 ? 3 : 1), 64);
+int loss_accumulate_splits(int64_t n, int64_t d, int64_t depth, bool half) {
+  return seg_splits(seg_tiles(n, d), depth / 64 * (half ? 3 : 1), 64);
 }
 
 int launch_loss_accumulate(const Planes& e, const Planes& wt, int64_t depth, int64_t n, int64_t d, const float* shift, bool first,
                            float* acc, float* part, size_t part_floats, hipStream_t st) {
-  if (depth < 32 || depth % 32) return LQ_ERR_SHAPE;
+  const bool half = e.p[1] != nullptr;
   AccumulateArgs a{};
-  fill_segments(a.g, e, wt, depth);
-  a.g.rows_a = n; a.g.rows_b = d;
-  a.g.tiles_m = (int)((n + SEG_T - 1) / SEG_T); a.g.tiles_n = (int)((d + SEG_T - 1) / SEG_T);
-  a.g.splits = loss_accumulate_splits(n, d, depth, e.lo ? 2 : 1);
+  LQ_TRY(fill_segments(a.g, wt, e, depth));
+  LQ_TRY(seg_shape(a.g, d, n, loss_accumulate_splits(n, d, depth, half)));
   if (a.g.splits > 1 && part_floats < (size_t)a.g.splits * (size_t)n * (size_t)d) return LQ_ERR_WORKSPACE;
   a.n = n; a.d = d; a.shift = shift; a.first = first; a.acc = acc; a.part = part;
-  static LdsLimit limit;
-  LQ_TRY(limit.raise(reinterpret_cast<const void*>(loss_accumulate_kernel), SEG_LDS));
+  static LdsLimit limit[2];
   {
     prof::Scope ps(prof::LOSS_ACCUMULATE, st, 2.0 * n * d * depth);
-    hipLaunchKernelGGL(loss_accumulate_kernel, dim3(seg_grid(a.g)), dim3(SEG_THREADS), SEG_LDS, st, a);
-    LQ_HIP_TRY(hipGetLastError());
+    LQ_TRY(half ? launch_tiles(loss_accumulate_kernel<_Float16>, limit[0], a, st) : launch_tiles(loss_accumulate_kernel<__bf16>, limit[1], a, st));
   }
   if (a.g.splits > 1) {
     prof::Scope ps(prof::LOSS_ROWS, st, (double)n * d * 4.0 * (a.g.splits + 2));
@@ -278,8 +315,8 @@ int launch_loss_accumulate(const Planes& e, const Planes& wt, int64_t depth, int
 
 // ------------------------------------------------------------------------------------------------
 // One workgroup finishes the rows: a few bytes each, and the total is added up in 64 bits in a fixed order.
-__global__ __launch_bounds__(1024) void loss_rows_kernel(LossRows r, const int64_t* __restrict__ targets, int64_t n, int64_t vocab,
-                                                         int mean, float* loss, float* row_loss, float* lse, float* factor) {
+__global__ __launch_bounds__(1024) void loss_rows_kernel(LossRows r, LossScales sc, const int64_t* __restrict__ targets, int64_t n, int64_t vocab,
+                                                         int mean, float* loss, float* row_loss, float* lse, float* factors) {
   __shared__ double s_sum[1024];
   __shared__ unsigned long long s_count[1024];
   double sum = 0.0;
@@ -313,40 +350,42 @@ __global__ __launch_bounds__(1024) void loss_rows_kernel(LossRows r, const int64
   if (threadIdx.x == 0) {
     const double f = mean ? 1.0 / (double)(s_count[0] ? s_count[0] : 1) : 1.0;      // no row counts: the mean is 0
     *loss = (float)(s_sum[0] * f);
-    *factor = (float)f;
+    factors[0] = (float)f;
+    factors[1] = sc.xt_top ? (float)f * power_of_two(-LOSS_E_SHIFT) * power_of_two(-half_exponent(*sc.xt_top)) : (float)f;
   }
 }
 
-int launch_loss_rows(const LossRows& r, const int64_t* targets, int64_t n, int64_t vocab, bool mean, float* loss, float* row_loss,
-                     float* lse, float* factor, hipStream_t st) {
+int launch_loss_rows(const LossRows& r, const LossScales& s, const int64_t* targets, int64_t n, int64_t vocab, bool mean, float* loss,
+                     float* row_loss, float* lse, float* factors, hipStream_t st) {
   prof::Scope ps(prof::LOSS_ROWS, st, (double)n * 36.0);
-  hipLaunchKernelGGL(loss_rows_kernel, dim3(1), dim3(1024), 0, st, r, targets, n, vocab, (int)mean, loss, row_loss, lse, factor);
+  hipLaunchKernelGGL(loss_rows_kernel, dim3(1), dim3(1024), 0, st, r, s, targets, n, vocab, (int)mean, loss, row_loss, lse, factors);
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }
 
 // dX_i = g (1 - p_t) (E W / S - w_t): one workgroup per row, its features in turn.
 template <typename T>
-__global__ __launch_bounds__(256) void loss_dx_kernel(LossRows r, const int64_t* __restrict__ targets, int64_t d, int64_t vocab,
+__global__ __launch_bounds__(256) void loss_dx_kernel(LossRows r, LossScales sc, const int64_t* __restrict__ targets, int64_t d, int64_t vocab,
                                                       const float* __restrict__ acc, const T* __restrict__ W, int64_t ldw,
                                                       const float* __restrict__ factor, T* __restrict__ dX) {
   const int64_t row = blockIdx.x, t = targets[row];
   const bool counts = t >= 0 && t < vocab;
   const float s = r.sum[row];
-  const float inv = s == 0.0f ? 0.0f : 1.0f / s;             // no other class: acc is zero
+  float inv = s == 0.0f ? 0.0f : 1.0f / s;                   // no other class: acc is zero
+  if (sc.w_top) inv *= power_of_two(-LOSS_E_SHIFT) * power_of_two(-half_exponent(*sc.w_top));
   const float g = counts ? r.wrong[row] * *factor : 0.0f;
   for (int64_t c = threadIdx.x; c < d; c += 256)
     dX[row * d + c] = counts ? (T)(g * (acc[row * d + c] * inv - (float)W[t * ldw + c])) : (T)0.0f;
 }
 
-int launch_loss_dx(const LossRows& r, const int64_t* targets, int64_t n, int64_t d, int64_t vocab, const float* acc, const void* W,
-                   int64_t ldw, int dtype, const float* factor, void* dX, hipStream_t st) {
+int launch_loss_dx(const LossRows& r, const LossScales& s, const int64_t* targets, int64_t n, int64_t d, int64_t vocab,
+                   const float* acc, const void* W, int64_t ldw, int dtype, const float* factor, void* dX, hipStream_t st) {
   prof::Scope ps(prof::LOSS_ROWS, st, (double)n * d * (4.0 + 2.0 * type_bytes(dtype)));
   if (dtype == LQ_T_BF16)
-    hipLaunchKernelGGL(loss_dx_kernel<__bf16>, dim3((unsigned)n), dim3(256), 0, st, r, targets, d, vocab, acc,
+    hipLaunchKernelGGL(loss_dx_kernel<__bf16>, dim3((unsigned)n), dim3(256), 0, st, r, s, targets, d, vocab, acc,
                        static_cast<const __bf16*>(W), ldw, factor, static_cast<__bf16*>(dX));
   else
-    hipLaunchKernelGGL(loss_dx_kernel<float>, dim3((unsigned)n), dim3(256), 0, st, r, targets, d, vocab, acc,
+    hipLaunchKernelGGL(loss_dx_kernel<float>, dim3((unsigned)n), dim3(256), 0, st, r, s, targets, d, vocab, acc,
                        static_cast<const float*>(W), ldw, factor, static_cast<float*>(dX));
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
@@ -354,57 +393,142 @@ int launch_loss_dx(const LossRows& r, const int64_t* targets, int64_t n, int64_t
 
 // ------------------------------------------------------------------------------------------------
 // The gradient of a piece's logits, transposed: the rows of Gt are classes, their tokens contiguous, as dW = Gt X reads them.
+// Tokens are the tile's rows here, so that a lane holds four neighbours of a row of Gt.
 struct GradientArgs {
   SegArgs g;
-  LossPiece p; LossRows r;
-  const float* factor;
-  uint16_t* hi; uint16_t* lo; int64_t pitch;
+  LossPiece p; LossRows r; LossScales s;
+  uint16_t* out[2]; int64_t pitch;
 };
 
-__global__ __launch_bounds__(SEG_THREADS) void loss_gradient_kernel(GradientArgs a) {
+template <typename H>
+__global__ __launch_bounds__(SEG_THREADS, 2) void loss_gradient_kernel(GradientArgs a) {
+  constexpr bool HALF = !std::is_same<H, __bf16>::value;
   extern __shared__ __attribute__((aligned(16))) unsigned char seg_lds[];
   const SegTile t = seg_tile(a.g);
   if (!t.live) return;
-  floatx16 acc[4][2];
+  SegAcc acc;
   seg_clear(acc);
-  seg_products(a.g, t, 0, a.g.seg[2].end, seg_lds, acc);
-  const int64_t cols = (a.p.n + 63) / 64 * 64;
-  const float factor = *a.factor;
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int64_t token = (int64_t)t.tn * SEG_T + 64 * t.wn + 32 * j + t.ln;
-    if (token >= cols) continue;
-    int64_t target = -1;
-    float lse2 = 0.0f, wrong = 0.0f;
-    if (token < a.p.n) { target = a.p.targets[token]; lse2 = a.r.lse2[token]; wrong = a.r.wrong[token] * factor; }
+  seg_products<H>(a.g, t, 0, a.g.pairs, seg_lds, acc);
+  __syncthreads();
+  // per token of the tile: factor of the logit, log2 of the sum, 1 - p of the target, the target's class inside the piece
+  float* s_f = reinterpret_cast<float*>(seg_lds);
+  float *s_lse = s_f + SEG_T, *s_wrong = s_lse + SEG_T;
+  int* s_at = reinterpret_cast<int*>(s_wrong + SEG_T);
+  const float unit = HALF ? power_of_two(LOSS_E_SHIFT) : 1.0f;
+  if (threadIdx.x < SEG_T) {
+    const int64_t token = (int64_t)t.tm * SEG_T + threadIdx.x;
+    const int64_t target = token < a.p.n ? a.p.targets[token] : -1;
     const bool counts = target >= 0 && target < a.p.vocab;
+    const int64_t at = target - a.p.v0;
+    s_f[threadIdx.x] = counts ? logit_factor(a.s, token) : 0.0f;
+    s_lse[threadIdx.x] = counts ? a.r.lse2[token] : 0.0f;
+    s_wrong[threadIdx.x] = counts ? a.r.wrong[token] * unit : 0.0f;
+    s_at[threadIdx.x] = !counts ? -2 : at >= 0 && at < a.p.classes ? (int)at : -1;
+  }
+  __syncthreads();
+  const int64_t cols = (a.p.n + 63) / 64 * 64;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < 8; ++i) {
+    const int row = 128 * t.wm + 16 * i + 4 * t.kg;
+    const int64_t token = (int64_t)t.tm * SEG_T + row;
+    if (token >= cols) continue;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int64_t row = (int64_t)t.tm * SEG_T + 128 * t.wm + 32 * i + 8 * (e >> 2) + 4 * t.lh + (e & 3);
-        if (row >= a.p.classes) continue;
-        float g = a.p.v0 + row == target ? -wrong : factor * __builtin_amdgcn_exp2f(acc[i][j][e] * LOG2E - lse2);
-        g = counts ? g : 0.0f;
-        const __bf16 h = (__bf16)g;
-        a.hi[row * a.pitch + token] = __builtin_bit_cast(uint16_t, h);
-        if (a.lo) a.lo[row * a.pitch + token] = __builtin_bit_cast(uint16_t, (__bf16)(g - (float)h));
+    for (int j = 0; j < 4; ++j) {
+      const int64_t cls = (int64_t)t.tn * SEG_T + 64 * t.wn + 16 * j + t.l16;
+      if (cls >= a.p.classes) continue;
+      floatx4 g;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int at = s_at[row + e];
+        const float p = __builtin_amdgcn_exp2f(acc[i][j][e] * s_f[row + e] - s_lse[row + e]) * unit;
+        g[e] = at == -2 ? 0.0f : at == (int)cls ? -s_wrong[row + e] : p;     // rows that do not count: whatever they hold
       }
+      const int64_t to = cls * a.pitch + token;
+      store_four<HALF>(a.out[0] + to, HALF ? a.out[1] + to : nullptr, g);
+    }
   }
 }
 
-int launch_loss_gradient(const Planes& w, const Planes& x, int64_t depth, const LossPiece& p, const LossRows& r,
-                         const float* factor, uint16_t* g_hi, uint16_t* g_lo, int64_t g_pitch, hipStream_t st) {
-  if (depth < 32 || depth % 32 || g_pitch < up_to(p.n, 64)) return LQ_ERR_SHAPE;
+int launch_loss_gradient(const Planes& w, const Planes& x, int64_t depth, const LossPiece& p, const LossRows& r, const LossScales& s,
+                         uint16_t* const g[2], int64_t g_pitch, hipStream_t st) {
+  if (g_pitch < up_to(p.n, 64)) return LQ_ERR_SHAPE;
   GradientArgs a{};
-  fill_segments(a.g, w, x, depth);
-  a.g.rows_a = p.classes; a.g.rows_b = p.n;
-  a.g.tiles_m = (int)((p.classes + SEG_T - 1) / SEG_T); a.g.tiles_n = (int)((p.n + SEG_T - 1) / SEG_T); a.g.splits = 1;
-  a.p = p; a.r = r; a.factor = factor; a.hi = g_hi; a.lo = g_lo; a.pitch = g_pitch;
-  static LdsLimit limit;
-  LQ_TRY(limit.raise(reinterpret_cast<const void*>(loss_gradient_kernel), SEG_LDS));
+  LQ_TRY(fill_segments(a.g, x, w, depth));
+  LQ_TRY(seg_shape(a.g, p.n, p.classes, 1));
+  a.p = p; a.r = r; a.s = s; a.out[0] = g[0]; a.out[1] = g[1]; a.pitch = g_pitch;
+  static LdsLimit limit[2];
   prof::Scope ps(prof::LOSS_LOGITS, st, 2.0 * p.n * p.classes * depth);
-  hipLaunchKernelGGL(loss_gradient_kernel, dim3(seg_grid(a.g)), dim3(SEG_THREADS), SEG_LDS, st, a);
+  return s.x_inv ? launch_tiles(loss_gradient_kernel<_Float16>, limit[0], a, st) : launch_tiles(loss_gradient_kernel<__bf16>, limit[1], a, st);
+}
+
+// ------------------------------------------------------------------------------------------------
+// dW's rows of a piece: features are the tile's rows and classes its columns.
+struct DwArgs {
+  SegArgs g;
+  int64_t rows, cols;
+  const float* factor;
+  void* out; float* part;
+};
+
+template <typename H, typename T>
+__global__ __launch_bounds__(SEG_THREADS, 2) void loss_dw_kernel(DwArgs a) {
+  typedef T vec4 __attribute__((ext_vector_type(4)));
+  extern __shared__ __attribute__((aligned(16))) unsigned char seg_lds[];
+  const SegTile t = seg_tile(a.g);
+  if (!t.live) return;
+  SegAcc acc;
+  seg_clear(acc);
+  seg_products<H>(a.g, t, seg_first(a.g.pairs, t.split, a.g.splits), seg_first(a.g.pairs, t.split + 1, a.g.splits), seg_lds, acc);
+  const float f = *a.factor;
+  float* part = a.part + (size_t)t.split * (size_t)a.rows * (size_t)a.cols;
+  seg_each(t, acc, [&](floatx4 v, int64_t col, int64_t row) {
+    if (row >= a.rows || col >= a.cols) return;
+    if (a.g.splits > 1) { store_floats(part + row * a.cols + col, v, col, a.cols); return; }
+    T* at = static_cast<T*>(a.out) + row * a.cols + col;
+    v *= f;
+    if ((a.cols & 3) == 0 && ((uintptr_t)a.out & (4 * sizeof(T) - 1)) == 0) { *reinterpret_cast<vec4*>(at) = __builtin_convertvector(v, vec4); return; }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (col + e < a.cols) at[e] = (T)v[e];
+  });
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void loss_dw_sum_kernel(const float* __restrict__ part, int splits, int64_t total,
+                                                          const float* __restrict__ factor, T* __restrict__ out) {
+  const float f = *factor;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    float v = 0.0f;
+    for (int s = 0; s < splits; ++s) v += part[s * total + i];
+    out[i] = (T)(v * f);
+  }
+}
+
+int loss_dw_splits(int64_t rows, int64_t cols, int64_t depth, bool half) {
+  return seg_splits(seg_tiles(rows, cols), depth / 64 * (half ? 3 : 1), 16);
+}
+
+int launch_loss_dw(const Planes& g, const Planes& xt, int64_t depth, int64_t rows, int64_t cols, const float* factor, int dtype,
+                   void* out, float* part, size_t part_floats, hipStream_t st) {
+  const bool half = g.p[1] != nullptr;
+  DwArgs a{};
+  LQ_TRY(fill_segments(a.g, xt, g, depth));
+  LQ_TRY(seg_shape(a.g, cols, rows, loss_dw_splits(rows, cols, depth, half)));
+  if (a.g.splits > 1 && part_floats < (size_t)a.g.splits * (size_t)rows * (size_t)cols) return LQ_ERR_WORKSPACE;
+  a.rows = rows; a.cols = cols; a.factor = factor; a.out = out; a.part = part;
+  static LdsLimit limit[2];
+  {
+    prof::Scope ps(prof::LOSS_ACCUMULATE, st, 2.0 * rows * cols * depth);
+    LQ_TRY(dtype == LQ_T_FP32 ? launch_tiles(loss_dw_kernel<_Float16, float>, limit[0], a, st)
+                              : launch_tiles(loss_dw_kernel<__bf16, __bf16>, limit[1], a, st));
+  }
+  if (a.g.splits == 1) return LQ_OK;
+  prof::Scope ps(prof::LOSS_ROWS, st, (double)rows * cols * (4.0 * a.g.splits + type_bytes(dtype)));
+  const dim3 grid((unsigned)std::min<int64_t>((rows * cols + 255) / 256, 8192));
+  if (dtype == LQ_T_BF16)
+    hipLaunchKernelGGL(loss_dw_sum_kernel<__bf16>, grid, dim3(256), 0, st, part, a.g.splits, rows * cols, factor, static_cast<__bf16*>(out));
+  else
+    hipLaunchKernelGGL(loss_dw_sum_kernel<float>, grid, dim3(256), 0, st, part, a.g.splits, rows * cols, factor, static_cast<float*>(out));
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }

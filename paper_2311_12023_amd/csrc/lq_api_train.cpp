@@ -36,36 +36,42 @@ static bool bad_type(int dtype) { return dtype != LQ_T_FP32 && dtype != LQ_T_BF1
 static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
 // ---- cross entropy ------------------------------------------------------------------------------------
+// Byte offsets inside a tile of 256 rows are 32 bits wide: rows of a plane are at most this far apart.
+constexpr int64_t MOST_PITCH = (int64_t)1 << 23;
+
 // Classes per piece: E of a piece stays within 64 MiB per plane, so that it is still in the memory-side cache when the next
 // product reads it; pieces of equal size, whole tiles.
 static int64_t piece_classes(int64_t n, int64_t vocab) {
-  const int64_t most = std::max<int64_t>(SEG_T, ((int64_t)1 << 25) / n / SEG_T * SEG_T);
+  const int64_t most = std::min(std::max<int64_t>(SEG_T, ((int64_t)1 << 25) / n / SEG_T * SEG_T), MOST_PITCH / 2);
   const int64_t pieces = (vocab + most - 1) / most;
   return up_to((vocab + pieces - 1) / pieces, SEG_T);
 }
 
 struct LossPlan {
   LossRows rows;
-  float *factor, *part_ref, *part_sum, *acc, *part;
-  uint16_t *x[2], *xt[2], *w[2], *wt[2], *e[2];      // hi, lo
-  int64_t classes, d32, n64;
+  float *factors, *part_ref, *part_sum, *acc, *part, *x_inv;
+  uint32_t* tops;                                    // of W, of the rows of X that count
+  uint16_t *x[2], *xt[2], *w[2], *wt[2], *e[2];
+  int64_t classes, d64, n64;
   size_t part_floats, bytes;
 };
 static LossPlan plan_loss(void* ws, int64_t n, int64_t d, int64_t vocab, int dtype, bool want_dx, bool want_dw) {
   LossPlan p{};
   Arena a(ws);
-  const int planes = type_planes(dtype);
+  const bool half = dtype == LQ_T_FP32;
   p.classes = piece_classes(n, vocab);
-  p.d32 = up_to(d, 32);
+  p.d64 = up_to(d, 64);
   p.n64 = up_to(n, 64);
   for (float** row : {&p.rows.ref, &p.rows.sum, &p.rows.shift, &p.rows.target, &p.rows.wrong, &p.rows.lse2}) *row = a.take<float>(n);
-  p.factor = a.take<float>(1);
+  p.factors = a.take<float>(2);
+  p.tops = a.take<uint32_t>(2);
+  p.x_inv = a.take<float>(half ? n : 0);
   const int64_t tiles = p.classes / SEG_T;
   p.part_ref = a.take<float>(tiles * n);
   p.part_sum = a.take<float>(tiles * n);
-  for (int h = 0; h < planes; ++h) {
-    p.x[h] = a.take<uint16_t>(n * p.d32);
-    p.w[h] = a.take<uint16_t>(p.classes * p.d32);
+  for (int h = 0; h < (half ? 2 : 1); ++h) {
+    p.x[h] = a.take<uint16_t>(n * p.d64);
+    p.w[h] = a.take<uint16_t>(p.classes * p.d64);
     p.xt[h] = a.take<uint16_t>(want_dw ? d * p.n64 : 0);
     p.wt[h] = a.take<uint16_t>(want_dx ? d * p.classes : 0);
     // E of a piece, and in the second pass its gradient
@@ -74,9 +80,9 @@ static LossPlan plan_loss(void* ws, int64_t n, int64_t d, int64_t vocab, int dty
   p.acc = a.take<float>(want_dx ? n * d : 0);
   // The last piece may be shorter and be cut into other numbers of ranges: tiles times ranges stay within 256 in any case.
   const size_t most = (size_t)256 * SEG_T * SEG_T;
-  const int s1 = want_dx ? loss_accumulate_splits(n, d, p.classes, planes) : 1;
+  const int s1 = want_dx ? loss_accumulate_splits(n, d, p.classes, half) : 1;
   p.part_floats = s1 > 1 ? std::min((size_t)s1 * n * d, most) : 0;
-  if (want_dw && plain_product_splits(1, 1, p.n64, planes) > 1)
+  if (want_dw && loss_dw_splits(1, 1, p.n64, half) > 1)
     p.part_floats = std::max(p.part_floats, std::min((size_t)16 * std::min(p.classes, vocab) * d, most));
   p.part = a.take<float>(p.part_floats);
   p.bytes = a.used();
@@ -85,61 +91,84 @@ static LossPlan plan_loss(void* ws, int64_t n, int64_t d, int64_t vocab, int dty
 
 static bool loss_sizes_ok(int64_t n, int64_t d, int64_t vocab) {
   const int64_t lim = (int64_t)1 << 31;
-  return n > 0 && d > 0 && vocab > 0 && n <= lim - 65536 && d <= (1 << 20) && vocab <= lim - 65536;
+  return n > 0 && d > 0 && vocab > 0 && n <= MOST_PITCH - 64 && d <= (1 << 20) && vocab <= lim - 65536;
 }
 
 // ---- adapter products ---------------------------------------------------------------------------------
 struct AdapterPlan {
-  int64_t r32, r64, d64, k32, m64, rows_pad, pitch;
-  uint16_t *x[2], *t[2], *tt[2], *u[2], *ut[2], *q[2], *dy[2], *b[2], *l1[2], *l2t;
-  float *thin, *part, *bscale;
+  int64_t r32, r64, in64, m64;               // in64: the large product's reduction
+  uint16_t *b[3], *a2[3], *b2[3], *ut[3], *tt[3], *q[2], *x[2];
+  float *thin, *part, *inv; uint32_t* top;
   size_t part_floats, bytes;
 };
+// The planes of the large product: `features` rows of weights, m rows of activations, and the low-rank operands of both.
+static void plan_product(AdapterPlan& p, Arena& a, int64_t m, int64_t features, int64_t depth, int dtype) {
+  const bool half = dtype == LQ_T_FP32;
+  p.in64 = up_to(depth, 64);
+  for (int h = 0; h < 2; ++h) {
+    p.q[h] = a.take<uint16_t>(h == 0 || half ? features * p.in64 : 0);
+    p.x[h] = a.take<uint16_t>(half || (h == 0 && depth % 64) ? m * p.in64 : 0);
+  }
+  for (int h = 0; h < 3; ++h) {
+    p.a2[h] = a.take<uint16_t>(features * p.r64);
+    p.b2[h] = a.take<uint16_t>(m * p.r64);
+  }
+  p.inv = a.take<float>(half ? m : 0);
+  p.top = a.take<uint32_t>(1);
+  const int s = adapter_product_splits(features, m, depth, dtype);
+  p.part_floats = s > 1 ? (size_t)s * m * features : 0;
+  p.part = a.take<float>(p.part_floats);
+}
 static AdapterPlan plan_forward(void* ws, int64_t m, int64_t d, int64_t k, int rank, int dtype) {
   AdapterPlan p{};
   Arena a(ws);
-  p.r32 = up_to(rank, 32); p.r64 = up_to(rank, 64); p.d64 = up_to(d, 64); p.rows_pad = up_to(m, 256); p.pitch = plane_pitch(d);
-  const bool split = dtype == LQ_T_FP32;
-  for (int h = 0; h < 2; ++h) {
-    p.b[h] = a.take<uint16_t>(p.r32 * p.d64);                             // L1^T
-    p.t[h] = a.take<uint16_t>(p.rows_pad * p.r32);
-    p.x[h] = a.take<uint16_t>(split ? p.rows_pad * d : 0);
-  }
+  p.r32 = up_to(rank, 32); p.r64 = up_to(rank, 64);
+  for (int h = 0; h < 3; ++h) p.b[h] = a.take<uint16_t>(p.r32 * up_to(d, 64));         // L1^T
   p.thin = a.take<float>((size_t)thin_project_splits(m, d) * m * p.r32);
-  if (split) {
-    p.bscale = a.take<float>(d * k / 16);
-    p.part_floats = qmatmul_part_floats(m, k, (int)(d / 32 + p.r32 / 32));
-  } else {
-    p.q[0] = a.take<uint16_t>(weight_plane_elems(p.pitch, k));
-    p.l2t = a.take<uint16_t>(k * p.r64);
-    const int s = plain_product_splits(m, k, d, 1);
-    p.part_floats = s > 1 ? (size_t)s * m * k : 0;
-  }
-  p.part = a.take<float>(p.part_floats);
+  plan_product(p, a, m, k, d, dtype);
   p.bytes = a.used();
   return p;
 }
 static AdapterPlan plan_backward(void* ws, int64_t m, int64_t d, int64_t k, int rank, int dtype) {
   AdapterPlan p{};
   Arena a(ws);
-  p.r32 = up_to(rank, 32); p.k32 = up_to(k, 32); p.m64 = up_to(m, 64);
-  const int planes = type_planes(dtype);
-  for (int h = 0; h < 2; ++h) {
-    p.b[h] = a.take<uint16_t>(p.r32 * p.k32);                             // L2
-    p.u[h] = a.take<uint16_t>(m * p.r32);
+  p.r32 = up_to(rank, 32); p.r64 = up_to(rank, 64); p.m64 = up_to(m, 64);
+  for (int h = 0; h < 3; ++h) {
+    p.b[h] = a.take<uint16_t>(p.r32 * up_to(k, 64));                                   // L2
     p.ut[h] = a.take<uint16_t>(p.r32 * p.m64);
     p.tt[h] = a.take<uint16_t>(p.r32 * p.m64);
-    p.l1[h] = a.take<uint16_t>(d * p.r32);
-    p.q[h] = a.take<uint16_t>(h < planes ? d * p.k32 : 0);
-    p.dy[h] = a.take<uint16_t>(h < planes && (dtype == LQ_T_FP32 || k % 32) ? m * p.k32 : 0);
   }
-  const size_t thin = std::max({(size_t)thin_project_splits(m, k) * m, (size_t)2 * thin_gram_splits(m, k) * k,
-                                (size_t)2 * thin_gram_splits(m, d) * d});
-  p.thin = a.take<float>(thin * p.r32);
-  const int s = adapter_dx_splits(m, d, k, planes);
-  p.part_floats = s > 1 ? (size_t)s * m * d : 0;
-  p.part = a.take<float>(p.part_floats);
+  p.thin = a.take<float>(std::max({(size_t)thin_project_splits(m, k) * m, (size_t)thin_gram_splits(m, k) * k,
+                                   (size_t)thin_gram_splits(m, d) * d}) * p.r32);
+  plan_product(p, a, m, d, k, dtype);
   p.bytes = a.used();
+  return p;
+}
+
+// The activations' planes (bf16 ones of whole pairs of steps are read where they are) and the weights'.
+static int product_planes(const AdapterPlan& p, const MvWeights& q, int64_t d, int64_t k, bool transposed, const void* x, int64_t m,
+                          int64_t depth, int dtype, Planes* w, Planes* act, hipStream_t st) {
+  const bool half = dtype == LQ_T_FP32;
+  if (half) {
+    const int64_t groups = (d * k + (int64_t)q.block * q.scale_block - 1) / ((int64_t)q.block * q.scale_block);
+    LQ_TRY(launch_zero_words(p.top, 1, st));
+    LQ_TRY(launch_top_magnitude(q.v, groups, 1, groups, nullptr, 0, p.top, st));      // no weight is larger than its group's scale
+  }
+  LQ_TRY(launch_weight_planes(q, d, k, transposed, p.top, p.q[0], half ? p.q[1] : nullptr, p.in64, st));
+  *w = Planes{{p.q[0], half ? p.q[1] : nullptr, nullptr}, p.in64};
+  if (!half && depth % 64 == 0) {
+    *act = Planes{{static_cast<const uint16_t*>(x), nullptr, nullptr}, depth};
+    return LQ_OK;
+  }
+  const PlaneTarget t{{p.x[0], half ? p.x[1] : nullptr, nullptr}, p.in64, m};
+  *act = planes_of(t);
+  return launch_row_planes({x, dtype, depth, m, depth, nullptr}, half ? PLANE_HALF_2 : PLANE_BF16, t, half ? p.inv : nullptr, st);
+}
+
+// The low-rank part in the large product: two of its planes (16 bits) where the result is bf16, all three where it is fp32.
+static Planes low_rank_planes(const PlaneTarget& t, int dtype) {
+  Planes p = planes_of(t);
+  if (dtype == LQ_T_BF16) p.p[2] = nullptr;
   return p;
 }
 
@@ -150,7 +179,7 @@ static int check_adapter(int64_t m, int64_t d, int64_t k, int rank, int dtype, l
   LQ_TRY(check_quant_args(d * k, c));
   if (k % c.block) return LQ_ERR_SHAPE;
   if (bad_type(dtype)) return LQ_ERR_ARG;
-  if (up_to(m, 256) * d >= lim || up_to(m, 256) * k >= lim || d * k >= lim) return LQ_ERR_SHAPE;
+  if (m >= (1 << 24) || up_to(m, 256) * d >= lim || up_to(m, 256) * k >= lim || d * k >= lim) return LQ_ERR_SHAPE;
   return LQ_OK;
 }
 static bool adapter_sizes_ok(int64_t m, int64_t d, int64_t k, int rank, int dtype) {
@@ -189,45 +218,58 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
   const LossPlan p = plan_loss(workspace, n, d, vocab, dtype, dX != nullptr, dW != nullptr);
   if (!workspace || misaligned(workspace, 256) || workspace_bytes < p.bytes) return LQ_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
-  const bool split = dtype == LQ_T_FP32;
-  // bf16 operands whose rows are whole steps on 16-byte addresses are read where they are
-  auto in_place = [&](const void* a, int64_t ld) { return !split && d % 32 == 0 && ld % 8 == 0 && !misaligned(a, 16); };
-  Planes x{p.x[0], p.x[1], p.d32};
-  if (in_place(X, ldx)) x = {static_cast<const uint16_t*>(X), nullptr, ldx};
-  else LQ_TRY(launch_row_planes(X, dtype, ldx, n, d, n, p.x[0], p.x[1], p.d32, st));
-  const bool w_in_place = in_place(W, ldw);
-  LQ_TRY(launch_loss_begin(p.rows, n, st));
-  const char* w0 = static_cast<const char*>(W);
-  auto piece_planes = [&](int64_t v0, int64_t classes, Planes* w) -> int {
-    const void* from = w0 + (size_t)v0 * (size_t)ldw * size;
-    *w = {p.w[0], p.w[1], p.d32};
-    if (w_in_place) { *w = {static_cast<const uint16_t*>(from), nullptr, ldw}; return LQ_OK; }
-    return launch_row_planes(from, dtype, ldw, classes, d, classes, p.w[0], p.w[1], p.d32, st);
-  };
-  for (int64_t v0 = 0; v0 < vocab; v0 += p.classes) {
-    const LossPiece piece{n, v0, std::min(p.classes, vocab - v0), vocab, targets};
-    Planes w;
-    LQ_TRY(piece_planes(v0, piece.classes, &w));
-    uint16_t *e0 = dX ? p.e[0] : nullptr, *e1 = dX ? p.e[1] : nullptr;
-    LQ_TRY(launch_loss_logits(w, x, p.d32, piece, p.rows, p.part_ref, p.part_sum, e0, e1, p.classes, st));
-    LQ_TRY(launch_loss_join(piece, p.rows, p.part_ref, p.part_sum, e0, e1, p.classes, st));
-    if (!dX) continue;
-    LQ_TRY(launch_column_planes(w0 + (size_t)v0 * (size_t)ldw * size, dtype, ldw, piece.classes, d, d, nullptr, 0, p.wt[0], p.wt[1],
-                                p.classes, st));
-    LQ_TRY(launch_loss_accumulate({e0, e1, p.classes}, {p.wt[0], p.wt[1], p.classes}, up_to(piece.classes, 32), n, d, p.rows.shift,
-                                  v0 == 0, p.acc, p.part, p.part_floats, st));
+  const bool half = dtype == LQ_T_FP32;
+  const PlaneKind kind = half ? PLANE_HALF_2 : PLANE_BF16;
+  const LossScales scales{half ? p.x_inv : nullptr, half ? p.tops : nullptr, half && dW ? p.tops + 1 : nullptr};
+  // bf16 operands whose rows are whole pairs of steps on 16-byte addresses are read where they are
+  auto in_place = [&](const void* a, int64_t ld) { return !half && d % 64 == 0 && ld % 8 == 0 && ld <= MOST_PITCH && !misaligned(a, 16); };
+  LQ_TRY(launch_loss_begin(p.rows, n, p.tops, st));
+  Planes x{{static_cast<const uint16_t*>(X), nullptr, nullptr}, ldx};
+  if (!in_place(X, ldx)) {
+    const PlaneTarget t{{p.x[0], p.x[1], nullptr}, p.d64, n};
+    LQ_TRY(launch_row_planes({X, dtype, ldx, n, d, nullptr}, kind, t, half ? p.x_inv : nullptr, st));
+    x = planes_of(t);
   }
-  LQ_TRY(launch_loss_rows(p.rows, targets, n, vocab, mean == 1, loss, row_loss, lse, p.factor, st));
-  if (dX) LQ_TRY(launch_loss_dx(p.rows, targets, n, d, vocab, p.acc, W, ldw, dtype, p.factor, dX, st));
-  if (!dW) return LQ_OK;
-  LQ_TRY(launch_column_planes(X, dtype, ldx, n, d, d, targets, vocab, p.xt[0], p.xt[1], p.n64, st));
+  if (half) LQ_TRY(launch_top_magnitude(W, ldw, vocab, d, nullptr, 0, p.tops, st));
+  const bool w_in_place = in_place(W, ldw);
+  const char* w0 = static_cast<const char*>(W);
+  auto piece_source = [&](int64_t v0, int64_t classes) {
+    return PlaneSource{w0 + (size_t)v0 * (size_t)ldw * size, dtype, ldw, classes, d, p.tops};
+  };
+  auto piece_planes = [&](int64_t v0, int64_t classes, Planes* w) -> int {
+    const PlaneSource from = piece_source(v0, classes);
+    *w = Planes{{static_cast<const uint16_t*>(from.src), nullptr, nullptr}, ldw};
+    if (w_in_place) return LQ_OK;
+    const PlaneTarget t{{p.w[0], p.w[1], nullptr}, p.d64, classes};
+    *w = planes_of(t);
+    return launch_row_planes(from, kind, t, nullptr, st);
+  };
+  uint16_t* const none[2] = {nullptr, nullptr};
   for (int64_t v0 = 0; v0 < vocab; v0 += p.classes) {
     const LossPiece piece{n, v0, std::min(p.classes, vocab - v0), vocab, targets};
     Planes w;
     LQ_TRY(piece_planes(v0, piece.classes, &w));
-    LQ_TRY(launch_loss_gradient(w, x, p.d32, piece, p.rows, p.factor, p.e[0], p.e[1], p.n64, st));
-    LQ_TRY(launch_plain_product({p.e[0], p.e[1], p.n64}, {p.xt[0], p.xt[1], p.n64}, p.n64, Planes{}, Planes{}, 0, piece.classes, d,
-                                dtype, static_cast<char*>(dW) + (size_t)v0 * (size_t)d * size, p.part, p.part_floats, st));
+    LQ_TRY(launch_loss_logits(w, x, p.d64, piece, p.rows, scales, p.part_ref, p.part_sum, dX ? p.e : none, p.classes, st));
+    LQ_TRY(launch_loss_join(piece, p.rows, half, p.part_ref, p.part_sum, dX ? p.e : none, p.classes, st));
+    if (!dX) continue;
+    const PlaneTarget wt{{p.wt[0], p.wt[1], nullptr}, p.classes, d};
+    LQ_TRY(launch_column_planes(piece_source(v0, piece.classes), kind, wt, nullptr, 0, st));
+    LQ_TRY(launch_loss_accumulate(Planes{{p.e[0], p.e[1], nullptr}, p.classes}, planes_of(wt), up_to(piece.classes, 64), n, d,
+                                  p.rows.shift, v0 == 0, p.acc, p.part, p.part_floats, st));
+  }
+  if (scales.xt_top) LQ_TRY(launch_top_magnitude(X, ldx, n, d, targets, vocab, p.tops + 1, st));
+  LQ_TRY(launch_loss_rows(p.rows, scales, targets, n, vocab, mean == 1, loss, row_loss, lse, p.factors, st));
+  if (dX) LQ_TRY(launch_loss_dx(p.rows, scales, targets, n, d, vocab, p.acc, W, ldw, dtype, p.factors, dX, st));
+  if (!dW) return LQ_OK;
+  const PlaneTarget xt{{p.xt[0], p.xt[1], nullptr}, p.n64, d};
+  LQ_TRY(launch_column_planes({X, dtype, ldx, n, d, p.tops + 1}, kind, xt, targets, vocab, st));
+  for (int64_t v0 = 0; v0 < vocab; v0 += p.classes) {
+    const LossPiece piece{n, v0, std::min(p.classes, vocab - v0), vocab, targets};
+    Planes w;
+    LQ_TRY(piece_planes(v0, piece.classes, &w));
+    LQ_TRY(launch_loss_gradient(w, x, p.d64, piece, p.rows, scales, p.e, p.n64, st));
+    LQ_TRY(launch_loss_dw(Planes{{p.e[0], p.e[1], nullptr}, p.n64}, planes_of(xt), p.n64, piece.classes, d, p.factors + 1, dtype,
+                          static_cast<char*>(dW) + (size_t)v0 * (size_t)d * size, p.part, p.part_floats, st));
   }
   return LQ_OK;
 }
@@ -250,20 +292,16 @@ int lq_adapter_forward(const void* X, int64_t m, int64_t d, int64_t k, const uin
   hipStream_t st = (hipStream_t)stream;
   const MvWeights q{codes_packed, scale_idx, v, c.bits, c.block, c.scale_block, scale_levels(c)};
   const int r32 = (int)w.r32;
-  LQ_TRY(launch_column_planes(L1, LQ_T_FP32, rank, d, rank, r32, nullptr, 0, w.b[0], w.b[1], w.d64, st));
-  LQ_TRY(launch_thin_project(X, dtype, m, d, {w.b[0], w.b[1], w.d64}, r32, mask.cut ? &mask : nullptr, w.thin, st));
-  LQ_TRY(launch_thin_finish(w.thin, thin_project_splits(m, d), m, rank, r32, mask.scale, T, w.t[0], w.t[1], nullptr, nullptr, 0, st));
-  if (dtype == LQ_T_FP32) {
-    LQ_TRY(launch_block_scales(scale_idx, v, d * k / c.block, c.scale_block, scale_levels(c), w.bscale, st));
-    LQ_TRY(launch_split_planes(static_cast<const float*>(X), m, d, d, w.rows_pad, d, w.x[0], w.x[1], st));
-    const QmmPart qp{w.x[0], w.x[1], d, codes_packed, w.bscale, c.bits, c.block};
-    const DensePart tp{w.t[0], w.t[1], w.r32, L2, k, rank, k};
-    return launch_qmatmul(qp, tp, m, w.rows_pad, k, static_cast<float*>(Y), k, w.part, w.part_floats, 0, st);
-  }
-  LQ_TRY(launch_weight_columns(q, d, k, nullptr, 0, 0, w.q[0], nullptr, ProjectSum{}, st));
-  LQ_TRY(launch_column_planes(L2, LQ_T_FP32, k, rank, k, k, nullptr, 0, w.l2t, nullptr, w.r64, st));
-  return launch_plain_product({static_cast<const uint16_t*>(X), nullptr, d}, {w.q[0], nullptr, w.pitch}, d,
-                              {w.t[0], nullptr, w.r32}, {w.l2t, nullptr, w.r64}, w.r32, m, k, dtype, Y, w.part, w.part_floats, st);
+  const PlaneTarget l1{{w.b[0], w.b[1], w.b[2]}, up_to(d, 64), w.r32}, none{};
+  const PlaneTarget t{{w.b2[0], w.b2[1], w.b2[2]}, w.r64, m}, l2{{w.a2[0], w.a2[1], w.a2[2]}, w.r64, k};
+  LQ_TRY(launch_column_planes({L1, LQ_T_FP32, rank, d, rank, nullptr}, PLANE_BF16_3, l1, nullptr, 0, st));
+  LQ_TRY(launch_column_planes({L2, LQ_T_FP32, k, rank, k, nullptr}, PLANE_BF16_3, l2, nullptr, 0, st));
+  LQ_TRY(launch_thin_project(X, dtype, m, d, planes_of(l1), r32, mask.cut ? &mask : nullptr, w.thin, st));
+  LQ_TRY(launch_thin_finish(w.thin, thin_project_splits(m, d), m, rank, r32, mask.scale, T, t, none, st));
+  Planes weights, act;
+  LQ_TRY(product_planes(w, q, d, k, true, X, m, d, dtype, &weights, &act, st));
+  return launch_adapter_product(weights, act, w.in64, low_rank_planes(l2, dtype), low_rank_planes(t, dtype), w.r64, {w.inv, w.top}, k, m,
+                                nullptr, dtype, Y, w.part, w.part_floats, st);
 }
 
 int lq_adapter_backward(const void* dY, const void* X, int64_t m, int64_t d, int64_t k, const uint8_t* codes_packed,
@@ -281,24 +319,22 @@ int lq_adapter_backward(const void* dY, const void* X, int64_t m, int64_t d, int
   if (!workspace || misaligned(workspace, 256) || workspace_bytes < w.bytes) return LQ_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
   const int r32 = (int)w.r32;
-  const bool split = dtype == LQ_T_FP32;
-  // U = dY L2^T, its transpose, and that of T
-  LQ_TRY(launch_row_planes(L2, LQ_T_FP32, k, rank, k, r32, w.b[0], w.b[1], w.k32, st));
-  LQ_TRY(launch_thin_project(dY, dtype, m, k, {w.b[0], w.b[1], w.k32}, r32, nullptr, w.thin, st));
-  LQ_TRY(launch_thin_finish(w.thin, thin_project_splits(m, k), m, rank, r32, 1.0f, nullptr, w.u[0], w.u[1], w.ut[0], w.ut[1], w.m64, st));
-  LQ_TRY(launch_thin_finish(T, 0, m, rank, r32, 1.0f, nullptr, nullptr, nullptr, w.tt[0], w.tt[1], w.m64, st));
-  LQ_TRY(launch_thin_gram(dY, dtype, m, k, {w.tt[0], w.tt[1], w.m64}, rank, r32, nullptr, 1.0f, true, w.thin, dL2, st));
-  LQ_TRY(launch_thin_gram(X, dtype, m, d, {w.ut[0], w.ut[1], w.m64}, rank, r32, mask.cut ? &mask : nullptr, mask.scale, false, w.thin,
-                          dL1, st));
-  if (!dX) return LQ_OK;
   const MvWeights q{codes_packed, scale_idx, v, c.bits, c.block, c.scale_block, scale_levels(c)};
-  LQ_TRY(launch_weight_rows(q, d, k, w.q[0], w.q[1], w.k32, st));
-  LQ_TRY(launch_row_planes(L1, LQ_T_FP32, rank, d, rank, d, w.l1[0], split ? w.l1[1] : nullptr, r32, st));
-  Planes dy{w.dy[0], w.dy[1], w.k32};
-  if (!split && k % 32 == 0) dy = {static_cast<const uint16_t*>(dY), nullptr, k};
-  else LQ_TRY(launch_row_planes(dY, dtype, k, m, k, m, w.dy[0], w.dy[1], w.k32, st));
-  return launch_adapter_dx({w.q[0], w.q[1], w.k32}, dy, w.k32, {w.l1[0], split ? w.l1[1] : nullptr, w.r32},
-                           {w.u[0], split ? w.u[1] : nullptr, w.r32}, r32, m, d, mask, dtype, dX, w.part, w.part_floats, st);
+  const PlaneTarget l2{{w.b[0], w.b[1], w.b[2]}, up_to(k, 64), w.r32}, none{};
+  const PlaneTarget u{{w.b2[0], w.b2[1], w.b2[2]}, w.r64, m}, l1{{w.a2[0], w.a2[1], w.a2[2]}, w.r64, d};
+  const PlaneTarget ut{{w.ut[0], w.ut[1], w.ut[2]}, w.m64, w.r32}, tt{{w.tt[0], w.tt[1], w.tt[2]}, w.m64, w.r32};
+  LQ_TRY(launch_row_planes({L2, LQ_T_FP32, k, rank, k, nullptr}, PLANE_BF16_3, l2, nullptr, st));
+  LQ_TRY(launch_thin_project(dY, dtype, m, k, planes_of(l2), r32, nullptr, w.thin, st));
+  LQ_TRY(launch_thin_finish(w.thin, thin_project_splits(m, k), m, rank, r32, 1.0f, nullptr, u, ut, st));
+  LQ_TRY(launch_thin_finish(T, 0, m, rank, r32, 1.0f, nullptr, none, tt, st));
+  LQ_TRY(launch_thin_gram(dY, dtype, m, k, planes_of(tt), rank, r32, nullptr, 1.0f, true, w.thin, dL2, st));
+  LQ_TRY(launch_thin_gram(X, dtype, m, d, planes_of(ut), rank, r32, mask.cut ? &mask : nullptr, mask.scale, false, w.thin, dL1, st));
+  if (!dX) return LQ_OK;
+  LQ_TRY(launch_row_planes({L1, LQ_T_FP32, rank, d, rank, nullptr}, PLANE_BF16_3, l1, nullptr, st));
+  Planes weights, act;
+  LQ_TRY(product_planes(w, q, d, k, false, dY, m, k, dtype, &weights, &act, st));
+  return launch_adapter_product(weights, act, w.in64, low_rank_planes(l1, dtype), low_rank_planes(u, dtype), w.r64, {w.inv, w.top}, d, m,
+                                mask.cut ? &mask : nullptr, dtype, dX, w.part, w.part_floats, st);
 }
 
 }  // extern "C"

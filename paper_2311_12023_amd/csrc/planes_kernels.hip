@@ -249,9 +249,12 @@ static void launch_weight_plane(const WpArgs& a, dim3 grid, hipStream_t st) {
   hipLaunchKernelGGL(weight_plane_kernel<BITS>, grid, dim3(256), 0, st, a);
 }
 
-int launch_weight_columns(const MvWeights& q, int64_t K, int64_t N, const float* L2, int rank, int Kd, uint16_t* Wt, uint16_t* Lt,
-                          const ProjectSum& t, hipStream_t st) {
-  if (K < 32 || K % 32 || N < 16 || N % 16 || K * N >= (1ll << 31)) return LQ_ERR_SHAPE;
+int launch_plane_product(const MvWeights& q, const uint16_t* Xh, int64_t K, const uint16_t* Th, int Kd, const float* L2,
+                         int rank, int64_t m, int64_t rows_pad, int64_t N, uint16_t* Wt, uint16_t* Lt, float* Y, int64_t ldy,
+                         float* part, size_t part_floats, const ProjectSum& t, hipStream_t st) {
+  if (m < 1 || rows_pad < m || rows_pad % PG_T || K < 32 || K % 32 || N < 16 || N % 16 || K * N >= (1ll << 31) ||
+      rows_pad * K >= (1ll << 31))
+    return LQ_ERR_SHAPE;
   if (rank < 0 || (rank > 0 && (Kd < rank || Kd % 32 || Kd > WP_K))) return LQ_ERR_RANK;
   if (q.block < 16 || (q.block & (q.block - 1)) || q.scale_block < 1 || (q.scale_block & (q.scale_block - 1)) || N % q.block)
     return LQ_ERR_CONFIG;
@@ -279,14 +282,6 @@ int launch_weight_columns(const MvWeights& q, int64_t K, int64_t N, const float*
     }
     LQ_HIP_TRY(hipGetLastError());
   }
-  return LQ_OK;
-}
-
-int launch_plane_product(const MvWeights& q, const uint16_t* Xh, int64_t K, const uint16_t* Th, int Kd, const float* L2,
-                         int rank, int64_t m, int64_t rows_pad, int64_t N, uint16_t* Wt, uint16_t* Lt, float* Y, int64_t ldy,
-                         float* part, size_t part_floats, const ProjectSum& t, hipStream_t st) {
-  if (m < 1 || rows_pad < m || rows_pad % PG_T || rows_pad * K >= (1ll << 31)) return LQ_ERR_SHAPE;
-  LQ_TRY(launch_weight_columns(q, K, N, L2, rank, Kd, Wt, Lt, t, st));
   PgArgs a{};
   a.A = Xh; a.B = Wt; a.pitch = plane_pitch(K); a.A2 = Th; a.B2 = Lt; a.pitch2 = rank > 0 ? Kd : 0;
   a.m = m; a.N = N;

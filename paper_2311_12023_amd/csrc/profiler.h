@@ -33,10 +33,10 @@ enum Cls {
   COLUMN_GEMM_BASE = 68,    // + mode * 4 + (l/32 - 1): column_gemm_kernel (work = flops of the product)
   COLUMN_SUM = 76,          // column_sum_kernel (work = bytes)
   DROPOUT = 77,             // dropout_kernel (work = bytes)
-  TRAIN_PLANES = 78,        // row_planes_kernel, column_planes_kernel (work = bytes)
-  SEGMENT_GEMM = 79,        // plain_product_kernel, adapter_dx_kernel (work = flops of the product)
+  TRAIN_PLANES = 78,        // passes that bring operands into planes (work = bytes)
+  ADAPTER_PRODUCT = 79,     // adapter_product_kernel (work = flops of the product)
   LOSS_LOGITS = 80,         // loss_logits_kernel, loss_gradient_kernel (work = flops of the product)
-  LOSS_ACCUMULATE = 81,     // loss_accumulate_kernel (work = flops of the product)
+  LOSS_ACCUMULATE = 81,     // loss_accumulate_kernel, loss_dw_kernel (work = flops of the product)
   LOSS_ROWS = 82,           // the loss's passes over rows and sums (work = bytes)
   THIN_PROJECT = 83,        // thin_project_kernel (work = bytes)
   THIN_GRAM = 84,           // thin_gram_kernel (work = bytes)

@@ -1,13 +1,11 @@
-// Operands of the training operators as bf16 planes: rows as they are, or transposed, so that the reduction index of the product
-// that reads them is contiguous.  Both passes are bound by the bytes they move.
+// Operands of the training operators as 16-bit planes: rows as they are, or transposed, so that the reduction index of the product
+// that reads them is contiguous.  All passes are bound by the bytes they move.
+#include "half_planes_device.h"
 #include "mfma_device.h"
 #include "profiler.h"
 #include "train.h"
 
 namespace lq {
-
-template <typename T>
-__device__ __forceinline__ floatx2 pair_of(T a, T b) { return floatx2{(float)a, (float)b}; }
 
 // Eight values of a row from column c on, zero beyond `cols`.
 template <typename T, bool VEC>
@@ -23,115 +21,248 @@ __device__ __forceinline__ void load8(const T* __restrict__ row, int64_t c, int6
   }
 }
 
-__device__ __forceinline__ void split8(const float (&v)[8], bf16x8& hi, bf16x8& lo) {
+template <int KIND>
+constexpr int plane_count() { return KIND == PLANE_BF16 ? 1 : KIND == PLANE_HALF_2 ? 2 : 3; }
+
+// Two neighbours as they lie in each plane.
+template <int KIND>
+__device__ __forceinline__ void split_pair(float a, float b, float scale, uint32_t (&w)[3]) {
+  if constexpr (KIND == PLANE_HALF_2) {
+    const HalfPair p = split_half(a * scale), q = split_half(b * scale);
+    typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+    w[0] = __builtin_bit_cast(uint32_t, half2{p.hi, q.hi});
+    w[1] = __builtin_bit_cast(uint32_t, half2{p.lo, q.lo});
+  } else {
+    bf16x2 p[3];
+    split_bf16_3(floatx2{a, b}, p);
 #pragma unroll
-  for (int j = 0; j < 8; j += 2) {
-    bf16x2 h, l;
-    split_bf16(floatx2{v[j], v[j + 1]}, h, l);
-    hi[j] = h[0]; hi[j + 1] = h[1];
-    lo[j] = l[0]; lo[j + 1] = l[1];
+    for (int k = 0; k < 3; ++k) w[k] = __builtin_bit_cast(uint32_t, p[k]);
   }
 }
 
-template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void row_planes_kernel(const T* __restrict__ src, int64_t ld, int64_t rows, int64_t cols,
-                                                         int64_t out_rows, uint16_t* __restrict__ hi, uint16_t* __restrict__ lo, int64_t pitch) {
-  const int64_t units = (cols + 31) / 32 * 4, total = out_rows * units;
+struct RowArgs {
+  const void* src; int64_t ld, rows, cols;
+  PlaneTarget t; const uint32_t* top; float* row_inv;
+};
+
+template <int KIND>
+__device__ __forceinline__ void store_split(const RowArgs& a, int64_t row, int64_t c, const float (&v)[8], float scale) {
+  uintx4 out[3];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint32_t w[3] = {0, 0, 0};
+    split_pair<KIND>(v[2 * j], v[2 * j + 1], scale, w);
+#pragma unroll
+    for (int k = 0; k < plane_count<KIND>(); ++k) out[k][j] = w[k];
+  }
+#pragma unroll
+  for (int k = 0; k < plane_count<KIND>(); ++k) *reinterpret_cast<uintx4*>(a.t.p[k] + row * a.t.pitch + c) = out[k];
+}
+
+template <typename T, int KIND, bool VEC>
+__global__ __launch_bounds__(256) void row_planes_kernel(RowArgs a) {
+  const int64_t units = (a.cols + 63) / 64 * 8, total = a.t.rows * units;
+  const float scale = KIND == PLANE_HALF_2 ? power_of_two(half_exponent(*a.top)) : 1.0f;
   for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
     const int64_t row = u / units, c = (u - row * units) * 8;
     float v[8];
-    load8<T, VEC>(src + row * ld, c, row < rows ? cols : 0, v);
-    bf16x8 h, l;
-    split8(v, h, l);
-    *reinterpret_cast<bf16x8*>(hi + row * pitch + c) = h;
-    if (lo) *reinterpret_cast<bf16x8*>(lo + row * pitch + c) = l;
+    load8<T, VEC>(static_cast<const T*>(a.src) + row * a.ld, c, row < a.rows ? a.cols : 0, v);
+    store_split<KIND>(a, row, c, v, scale);
   }
 }
 
-// A workgroup turns 64 x 64 values in LDS; rows of 33 words, so that reading down a column meets different banks.
-constexpr int CP = 64, CP_PITCH = 66;
-template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void column_planes_kernel(const T* __restrict__ src, int64_t ld, int64_t rows, int64_t cols,
-                                                            int64_t out_rows, const int64_t* __restrict__ keep, int64_t keep_below,
-                                                            uint16_t* __restrict__ hi, uint16_t* __restrict__ lo, int64_t pitch,
-                                                            int tiles_r) {
-  __shared__ uint32_t s_hi[CP * CP_PITCH / 2], s_lo[CP * CP_PITCH / 2];
+// fp16 planes with a power of two per row: a wavefront walks its row for the largest magnitude and again, out of the cache, to
+// split it.
+template <bool VEC>
+__global__ __launch_bounds__(256) void row_scaled_planes_kernel(RowArgs a) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (row >= a.rows) return;
+  const float* x = static_cast<const float*>(a.src) + row * a.ld;
+  float v[8];
+  uint32_t top = 0;
+  for (int64_t c = 8 * lane; c < a.cols; c += 512) {
+    load8<float, VEC>(x, c, a.cols, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, finite_magnitude(v[j]));
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+  const int e = half_exponent(top);
+  if (lane == 0) a.row_inv[row] = power_of_two(-e);
+  const float scale = power_of_two(e);
+  for (int64_t c = 8 * lane; c < (a.cols + 63) / 64 * 64; c += 512) {
+    load8<float, VEC>(x, c, a.cols, v);
+    store_split<PLANE_HALF_2>(a, row, c, v, scale);
+  }
+}
+
+// A workgroup turns 64 x 64 values in LDS: a thread packs two rows of eight columns, so that words are written, in rows of 33
+// words: the eight columns and eight row pairs of a wavefront meet 64 different banks.
+struct ColumnArgs {
+  const void* src; int64_t ld, rows, cols;
+  PlaneTarget t; const uint32_t* top;
+  const int64_t* keep; int64_t keep_below;
+  int tiles_r;
+};
+constexpr int CP = 64, CP_WORDS = 33;
+
+template <typename T, int KIND, bool VEC>
+__global__ __launch_bounds__(256) void column_planes_kernel(ColumnArgs a) {
+  constexpr int N = plane_count<KIND>();
+  __shared__ uint32_t s_w[N][CP * CP_WORDS];
   const int tid = threadIdx.x;
-  const int64_t r0 = (int64_t)(blockIdx.x % tiles_r) * CP, c0 = (int64_t)(blockIdx.x / tiles_r) * CP;
+  const int64_t r0 = (int64_t)(blockIdx.x % a.tiles_r) * CP, c0 = (int64_t)(blockIdx.x / a.tiles_r) * CP;
+  const float scale = KIND == PLANE_HALF_2 ? power_of_two(half_exponent(*a.top)) : 1.0f;
+  const int c = (tid & 7) * 8, pair = tid >> 3;
+  float v[2][8];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const int r = (tid >> 3) + 32 * h, c = (tid & 7) * 8;
-    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    bool take = r0 + r < rows;
-    if (take && keep) { const int64_t t = keep[r0 + r]; take = t >= 0 && t < keep_below; }
-    if (take && c0 + c < cols) load8<T, VEC>(src + (r0 + r) * ld, c0 + c, cols, v);
+    const int64_t row = r0 + 2 * pair + h;
+    bool take = row < a.rows;
+    if (take && a.keep) { const int64_t t = a.keep[row]; take = t >= 0 && t < a.keep_below; }
+    load8<T, VEC>(static_cast<const T*>(a.src) + row * a.ld, c0 + c, take ? a.cols : 0, v[h]);
+  }
 #pragma unroll
-    for (int j = 0; j < 8; j += 2) {
-      bf16x2 a, b;
-      split_bf16(floatx2{v[j], v[j + 1]}, a, b);
-      s_hi[r * (CP_PITCH / 2) + (c + j) / 2] = __builtin_bit_cast(uint32_t, a);
-      if (lo) s_lo[r * (CP_PITCH / 2) + (c + j) / 2] = __builtin_bit_cast(uint32_t, b);
-    }
+  for (int j = 0; j < 8; ++j) {
+    uint32_t w[3] = {0, 0, 0};
+    split_pair<KIND>(v[0][j], v[1][j], scale, w);
+#pragma unroll
+    for (int k = 0; k < N; ++k) s_w[k][(c + j) * CP_WORDS + pair] = w[k];
   }
   __syncthreads();
-  const uint16_t* th = reinterpret_cast<const uint16_t*>(s_hi);
-  const uint16_t* tl = reinterpret_cast<const uint16_t*>(s_lo);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const int c = (tid >> 3) + 32 * h, r = (tid & 7) * 8;
-    if (c0 + c >= out_rows) continue;
-    typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
-    u16x8 out;
+    const int col = (tid >> 3) + 32 * h, word = (tid & 7) * 4;
+    if (c0 + col >= a.t.rows) continue;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) out[j] = th[(r + j) * CP_PITCH + c];
-    *reinterpret_cast<u16x8*>(hi + (c0 + c) * pitch + r0 + r) = out;
-    if (lo) {
+    for (int k = 0; k < N; ++k) {
+      uintx4 out;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) out[j] = tl[(r + j) * CP_PITCH + c];
-      *reinterpret_cast<u16x8*>(lo + (c0 + c) * pitch + r0 + r) = out;
+      for (int j = 0; j < 4; ++j) out[j] = s_w[k][col * CP_WORDS + word + j];
+      *reinterpret_cast<uintx4*>(a.t.p[k] + (c0 + col) * a.t.pitch + r0 + 2 * word) = out;
     }
   }
 }
 
-template <typename T>
-static void rows_of(const void* src, int64_t ld, int64_t rows, int64_t cols, int64_t out_rows, uint16_t* hi, uint16_t* lo,
-                    int64_t pitch, hipStream_t st) {
-  const bool vec = ((uintptr_t)src & 15) == 0 && ld * sizeof(T) % 16 == 0;
-  auto kernel = vec ? row_planes_kernel<T, true> : row_planes_kernel<T, false>;
-  const int64_t units = out_rows * ((cols + 31) / 32 * 4);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>((units + 255) / 256, 1 << 16)), dim3(256), 0, st,
-                     static_cast<const T*>(src), ld, rows, cols, out_rows, hi, lo, pitch);
+static bool vectors_fit(const void* src, int64_t ld, int dtype) {
+  return ((uintptr_t)src & 15) == 0 && ld * type_bytes(dtype) % 16 == 0;
+}
+static int check_target(const PlaneSource& s, PlaneKind kind, const PlaneTarget& t, int64_t least) {
+  if (s.rows < 1 || s.cols < 1 || t.pitch % 64 || t.pitch < least) return LQ_ERR_SHAPE;
+  const int n = kind == PLANE_BF16 ? 1 : kind == PLANE_HALF_2 ? 2 : 3;
+  for (int k = 0; k < n; ++k)
+    if (!t.p[k]) return LQ_ERR_NULL;
+  return kind == PLANE_HALF_2 && s.dtype != LQ_T_FP32 ? LQ_ERR_ARG : LQ_OK;
+}
+static double plane_bytes(const PlaneSource& s, PlaneKind kind) {
+  return (double)s.rows * (double)s.cols * (type_bytes(s.dtype) + (kind == PLANE_BF16 ? 2.0 : kind == PLANE_HALF_2 ? 4.0 : 6.0));
 }
 
-int launch_row_planes(const void* src, int dtype, int64_t ld, int64_t rows, int64_t cols, int64_t out_rows, uint16_t* hi,
-                      uint16_t* lo, int64_t pitch, hipStream_t st) {
-  if (pitch % 8 || pitch < (cols + 31) / 32 * 32) return LQ_ERR_SHAPE;
-  prof::Scope ps(prof::TRAIN_PLANES, st, (double)rows * cols * (type_bytes(dtype) + (lo ? 4.0 : 2.0)));
-  if (dtype == LQ_T_BF16) rows_of<__bf16>(src, ld, rows, cols, out_rows, hi, lo, pitch, st);
-  else rows_of<float>(src, ld, rows, cols, out_rows, hi, lo, pitch, st);
+template <typename T, int KIND>
+static void rows_of(const RowArgs& a, bool vec, hipStream_t st) {
+  auto kernel = vec ? row_planes_kernel<T, KIND, true> : row_planes_kernel<T, KIND, false>;
+  const int64_t units = a.t.rows * ((a.cols + 63) / 64 * 8);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>((units + 255) / 256, 1 << 16)), dim3(256), 0, st, a);
+}
+
+int launch_row_planes(const PlaneSource& s, PlaneKind kind, const PlaneTarget& t, float* row_inv, hipStream_t st) {
+  LQ_TRY(check_target(s, kind, t, up_to(s.cols, 64)));
+  const RowArgs a{s.src, s.ld, s.rows, s.cols, t, s.top, row_inv};
+  const bool vec = vectors_fit(s.src, s.ld, s.dtype);
+  prof::Scope ps(prof::TRAIN_PLANES, st, plane_bytes(s, kind));
+  if (kind == PLANE_HALF_2 && row_inv) {
+    auto kernel = vec ? row_scaled_planes_kernel<true> : row_scaled_planes_kernel<false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((s.rows + 3) / 4)), dim3(256), 0, st, a);
+  } else if (kind == PLANE_HALF_2) {
+    if (!s.top) return LQ_ERR_NULL;
+    rows_of<float, PLANE_HALF_2>(a, vec, st);
+  } else if (kind == PLANE_BF16_3) {
+    if (s.dtype != LQ_T_FP32) return LQ_ERR_ARG;
+    rows_of<float, PLANE_BF16_3>(a, vec, st);
+  } else if (s.dtype == LQ_T_BF16) {
+    rows_of<__bf16, PLANE_BF16>(a, vec, st);
+  } else {
+    return LQ_ERR_ARG;
+  }
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }
 
-template <typename T>
-static int columns_of(const void* src, int64_t ld, int64_t rows, int64_t cols, int64_t out_rows, const int64_t* keep, int64_t below,
-                      uint16_t* hi, uint16_t* lo, int64_t pitch, hipStream_t st) {
-  const bool vec = ((uintptr_t)src & 15) == 0 && ld * sizeof(T) % 16 == 0;
-  auto kernel = vec ? column_planes_kernel<T, true> : column_planes_kernel<T, false>;
-  const int64_t tr = (rows + CP - 1) / CP, tc = (out_rows + CP - 1) / CP;
+template <typename T, int KIND>
+static void columns_of(const ColumnArgs& a, bool vec, unsigned grid, hipStream_t st) {
+  auto kernel = vec ? column_planes_kernel<T, KIND, true> : column_planes_kernel<T, KIND, false>;
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, a);
+}
+
+int launch_column_planes(const PlaneSource& s, PlaneKind kind, const PlaneTarget& t, const int64_t* keep, int64_t keep_below,
+                         hipStream_t st) {
+  LQ_TRY(check_target(s, kind, t, up_to(s.rows, CP)));
+  const int64_t tr = (s.rows + CP - 1) / CP, tc = (t.rows + CP - 1) / CP;
   if (tr * tc >= (1ll << 31)) return LQ_ERR_SHAPE;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(tr * tc)), dim3(256), 0, st, static_cast<const T*>(src), ld, rows, cols, out_rows, keep, below,
-                     hi, lo, pitch, (int)tr);
+  const ColumnArgs a{s.src, s.ld, s.rows, s.cols, t, s.top, keep, keep_below, (int)tr};
+  const bool vec = vectors_fit(s.src, s.ld, s.dtype);
+  const unsigned grid = (unsigned)(tr * tc);
+  prof::Scope ps(prof::TRAIN_PLANES, st, plane_bytes(s, kind));
+  if (kind == PLANE_HALF_2) {
+    if (!s.top) return LQ_ERR_NULL;
+    columns_of<float, PLANE_HALF_2>(a, vec, grid, st);
+  } else if (kind == PLANE_BF16_3) {
+    if (s.dtype != LQ_T_FP32) return LQ_ERR_ARG;
+    columns_of<float, PLANE_BF16_3>(a, vec, grid, st);
+  } else if (s.dtype == LQ_T_BF16) {
+    columns_of<__bf16, PLANE_BF16>(a, vec, grid, st);
+  } else {
+    return LQ_ERR_ARG;
+  }
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }
 
-int launch_column_planes(const void* src, int dtype, int64_t ld, int64_t rows, int64_t cols, int64_t out_rows,
-                         const int64_t* keep, int64_t keep_below, uint16_t* hi, uint16_t* lo, int64_t pitch, hipStream_t st) {
-  if (pitch % 8 || pitch < up_to(rows, CP)) return LQ_ERR_SHAPE;
-  prof::Scope ps(prof::TRAIN_PLANES, st, (double)rows * cols * (type_bytes(dtype) + (lo ? 4.0 : 2.0)));
-  if (dtype == LQ_T_BF16) return columns_of<__bf16>(src, ld, rows, cols, out_rows, keep, keep_below, hi, lo, pitch, st);
-  return columns_of<float>(src, ld, rows, cols, out_rows, keep, keep_below, hi, lo, pitch, st);
+// ------------------------------------------------------------------------------------------------
+// The largest of integers does not depend on the order in which an atomic takes them.
+template <bool VEC>
+__global__ __launch_bounds__(256) void top_magnitude_kernel(const float* __restrict__ src, int64_t ld, int64_t rows, int64_t cols,
+                                                            const int64_t* __restrict__ keep, int64_t keep_below,
+                                                            uint32_t* __restrict__ out) {
+  __shared__ uint32_t s_top[4];
+  const int64_t units = (cols + 7) / 8, total = rows * units;
+  uint32_t top = 0;
+  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
+    const int64_t row = u / units, c = (u - row * units) * 8;
+    if (keep) { const int64_t t = keep[row]; if (t < 0 || t >= keep_below) continue; }
+    float v[8];
+    load8<float, VEC>(src + row * ld, c, cols, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, finite_magnitude(v[j]));
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+  if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
+  __syncthreads();
+  if (threadIdx.x == 0) atomicMax(out, max(max(s_top[0], s_top[1]), max(s_top[2], s_top[3])));
+}
+
+int launch_top_magnitude(const void* src, int64_t ld, int64_t rows, int64_t cols, const int64_t* keep, int64_t keep_below,
+                         uint32_t* top, hipStream_t st) {
+  const bool vec = vectors_fit(src, ld, LQ_T_FP32);
+  const int64_t units = rows * ((cols + 7) / 8);
+  auto kernel = vec ? top_magnitude_kernel<true> : top_magnitude_kernel<false>;
+  prof::Scope ps(prof::TRAIN_PLANES, st, (double)rows * (double)cols * 4.0);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>((units + 1023) / 1024, 2048)), dim3(256), 0, st,
+                     static_cast<const float*>(src), ld, rows, cols, keep, keep_below, top);
+  LQ_HIP_TRY(hipGetLastError());
+  return LQ_OK;
+}
+
+__global__ void zero_words_kernel(uint32_t* p, int count) {
+  if ((int)threadIdx.x < count) p[threadIdx.x] = 0;
+}
+int launch_zero_words(uint32_t* p, int count, hipStream_t st) {
+  if (count > 64) return LQ_ERR_ARG;
+  hipLaunchKernelGGL(zero_words_kernel, dim3(1), dim3(64), 0, st, p, count);
+  LQ_HIP_TRY(hipGetLastError());
+  return LQ_OK;
 }
 
 }  // namespace lq
