@@ -215,19 +215,22 @@ __global__ __launch_bounds__(256) void loss_join_kernel(JoinArgs a) {
     a.r.ref[row] = ref;
   }
   if (!a.e[0]) return;
-  for (int t = 0; t < a.tiles; ++t) {
-    const float mine = a.part_ref[(int64_t)t * a.p.n + row];
-    if (mine == ref) continue;
+  for (int t0 = 0; t0 < a.tiles; t0 += 64) {
+    const float mine = t0 + lane < a.tiles ? a.part_ref[(int64_t)(t0 + lane) * a.p.n + row] : ref;
     const float f = __builtin_amdgcn_exp2f(mine - from);
-    const int64_t at = row * a.e_pitch + (int64_t)t * SEG_T + 4 * lane;
-    scale_run<H>(a.e[0] + at, f);
-    if constexpr (!std::is_same<H, __bf16>::value) scale_run<H>(a.e[1] + at, f);
+    for (uint64_t low = __ballot(mine != ref); low; low &= low - 1) {
+      const int t = __builtin_ctzll(low);
+      const float ft = __shfl(f, t);
+      const int64_t at = row * a.e_pitch + (int64_t)(t0 + t) * SEG_T + 4 * lane;
+      scale_run<H>(a.e[0] + at, ft);
+      if constexpr (!std::is_same<H, __bf16>::value) scale_run<H>(a.e[1] + at, ft);
+    }
   }
 }
 
-int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, const float* part_ref, const float* part_sum,
+int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, const float* part_ref, const float* part_sum, int tile,
                      uint16_t* const e[2], int64_t e_pitch, hipStream_t st) {
-  const JoinArgs a{p, r, part_ref, part_sum, (int)((p.classes + SEG_T - 1) / SEG_T), {e[0], e[1]}, e_pitch};
+  const JoinArgs a{p, r, part_ref, part_sum, (int)((p.classes + tile - 1) / tile), {e[0], e[1]}, e_pitch};
   prof::Scope ps(prof::LOSS_ROWS, st, (double)p.n * a.tiles * 8.0);
   auto kernel = half ? loss_join_kernel<_Float16> : loss_join_kernel<__bf16>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)((p.n + 3) / 4)), dim3(256), 0, st, a);

@@ -47,12 +47,16 @@ static int64_t piece_classes(int64_t n, int64_t vocab) {
   return up_to((vocab + pieces - 1) / pieces, SEG_T);
 }
 
+static bool few_by_size(int64_t n, int64_t vocab) { return n <= LOSS_FEW && vocab <= MOST_PITCH / 2; }
+
 struct LossPlan {
   LossRows rows;
   float *factors, *part_ref, *part_sum, *acc, *part, *x_inv;
   uint32_t* tops;                                    // of W, of the rows of X that count
   uint16_t *x[2], *xt[2], *w[2], *wt[2], *e[2];
-  int64_t classes, d64, n64;
+  uint16_t *few_x[3], *few_e[3];                     // the few rows' planes
+  float* few_part;
+  int64_t classes, d64, n64, v64;
   size_t part_floats, bytes;
 };
 static LossPlan plan_loss(void* ws, int64_t n, int64_t d, int64_t vocab, int dtype, bool want_dx, bool want_dw) {
@@ -66,7 +70,14 @@ static LossPlan plan_loss(void* ws, int64_t n, int64_t d, int64_t vocab, int dty
   p.factors = a.take<float>(2);
   p.tops = a.take<uint32_t>(2);
   p.x_inv = a.take<float>(half ? n : 0);
-  const int64_t tiles = p.classes / SEG_T;
+  const bool few = few_by_size(n, vocab);
+  p.v64 = up_to(vocab, 64);
+  const int64_t tiles = std::max(p.classes / SEG_T, few ? p.v64 / LOSS_FEW_TILE : 0);
+  for (int h = 0; h < (half ? 3 : 1); ++h) {
+    p.few_x[h] = a.take<uint16_t>(few ? few_rows(n) * p.d64 : 0);
+    p.few_e[h] = a.take<uint16_t>(few && want_dx ? few_rows(n) * p.v64 : 0);
+  }
+  p.few_part = a.take<float>(few && want_dx ? (size_t)few_dx_splits(vocab, d) * d * few_rows(n) : 0);
   p.part_ref = a.take<float>(tiles * n);
   p.part_sum = a.take<float>(tiles * n);
   for (int h = 0; h < (half ? 2 : 1); ++h) {
@@ -224,15 +235,17 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
   // bf16 operands whose rows are whole pairs of steps on 16-byte addresses are read where they are
   auto in_place = [&](const void* a, int64_t ld) { return !half && d % 64 == 0 && ld % 8 == 0 && ld <= MOST_PITCH && !misaligned(a, 16); };
   LQ_TRY(launch_loss_begin(p.rows, n, p.tops, st));
+  const char* w0 = static_cast<const char*>(W);
+  const bool few = few_by_size(n, vocab);
+  const bool planes = !few || dW;                             // the large products' operands
   Planes x{{static_cast<const uint16_t*>(X), nullptr, nullptr}, ldx};
-  if (!in_place(X, ldx)) {
+  if (planes && !in_place(X, ldx)) {
     const PlaneTarget t{{p.x[0], p.x[1], nullptr}, p.d64, n};
     LQ_TRY(launch_row_planes({X, dtype, ldx, n, d, nullptr}, kind, t, half ? p.x_inv : nullptr, st));
     x = planes_of(t);
   }
-  if (half) LQ_TRY(launch_top_magnitude(W, ldw, vocab, d, nullptr, 0, p.tops, st));
+  if (planes && half) LQ_TRY(launch_top_magnitude(W, ldw, vocab, d, nullptr, 0, p.tops, st));
   const bool w_in_place = in_place(W, ldw);
-  const char* w0 = static_cast<const char*>(W);
   auto piece_source = [&](int64_t v0, int64_t classes) {
     return PlaneSource{w0 + (size_t)v0 * (size_t)ldw * size, dtype, ldw, classes, d, p.tops};
   };
@@ -244,13 +257,22 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
     *w = planes_of(t);
     return launch_row_planes(from, kind, t, nullptr, st);
   };
+  const LossPiece all{n, 0, vocab, vocab, targets};
+  if (few) {
+    const PlaneTarget t{{p.few_x[0], p.few_x[1], p.few_x[2]}, p.d64, few_rows(n)};
+    uint16_t* const e[3] = {dX ? p.few_e[0] : nullptr, dX ? p.few_e[1] : nullptr, dX ? p.few_e[2] : nullptr};
+    uint16_t* const none[2] = {nullptr, nullptr};
+    LQ_TRY(launch_row_planes({X, dtype, ldx, n, d, nullptr}, half ? PLANE_BF16_3 : PLANE_BF16, t, nullptr, st));
+    LQ_TRY(launch_few_logits(W, ldw, dtype, d, planes_of(t), all, p.rows, p.part_ref, p.part_sum, e, p.v64, st));
+    LQ_TRY(launch_loss_join(all, p.rows, half, p.part_ref, p.part_sum, LOSS_FEW_TILE, none, 0, st));
+  }
   uint16_t* const none[2] = {nullptr, nullptr};
-  for (int64_t v0 = 0; v0 < vocab; v0 += p.classes) {
+  for (int64_t v0 = 0; !few && v0 < vocab; v0 += p.classes) {
     const LossPiece piece{n, v0, std::min(p.classes, vocab - v0), vocab, targets};
     Planes w;
     LQ_TRY(piece_planes(v0, piece.classes, &w));
     LQ_TRY(launch_loss_logits(w, x, p.d64, piece, p.rows, scales, p.part_ref, p.part_sum, dX ? p.e : none, p.classes, st));
-    LQ_TRY(launch_loss_join(piece, p.rows, half, p.part_ref, p.part_sum, dX ? p.e : none, p.classes, st));
+    LQ_TRY(launch_loss_join(piece, p.rows, half, p.part_ref, p.part_sum, SEG_T, dX ? p.e : none, p.classes, st));
     if (!dX) continue;
     const PlaneTarget wt{{p.wt[0], p.wt[1], nullptr}, p.classes, d};
     LQ_TRY(launch_column_planes(piece_source(v0, piece.classes), kind, wt, nullptr, 0, st));
@@ -259,7 +281,12 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
   }
   if (scales.xt_top) LQ_TRY(launch_top_magnitude(X, ldx, n, d, targets, vocab, p.tops + 1, st));
   LQ_TRY(launch_loss_rows(p.rows, scales, targets, n, vocab, mean == 1, loss, row_loss, lse, p.factors, st));
-  if (dX) LQ_TRY(launch_loss_dx(p.rows, scales, targets, n, d, vocab, p.acc, W, ldw, dtype, p.factors, dX, st));
+  if (dX && few) {
+    LQ_TRY(launch_few_dx(W, ldw, dtype, d, Planes{{p.few_e[0], p.few_e[1], p.few_e[2]}, p.v64}, all, p.rows, p.part_ref, p.factors,
+                         p.few_part, dX, st));
+  } else if (dX) {
+    LQ_TRY(launch_loss_dx(p.rows, scales, targets, n, d, vocab, p.acc, W, ldw, dtype, p.factors, dX, st));
+  }
   if (!dW) return LQ_OK;
   const PlaneTarget xt{{p.xt[0], p.xt[1], nullptr}, p.n64, d};
   LQ_TRY(launch_column_planes({X, dtype, ldx, n, d, p.tops + 1}, kind, xt, targets, vocab, st));

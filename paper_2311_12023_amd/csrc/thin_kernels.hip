@@ -3,155 +3,28 @@
 // The mask is worked out where an element is loaded (the eight neighbours that share a call of the generator are what a lane loads).
 // Their results are fp32 whatever the type of X: L1, L2, T and U go in as three bf16 planes, X and dY as one where they are bf16
 // and three where they are fp32.
-#include "half_planes_device.h"
-#include "lds_transfer.h"
-#include "mfma_device.h"
 #include "profiler.h"
+#include "thin_device.h"
 #include "train.h"
 
 namespace lq {
 
-template <typename T> constexpr int thin_planes() { return sizeof(T) == 2 ? 1 : 3; }
-
-// Eight neighbours of a row as a lane loads them.
-template <typename T>
-struct Eight { typedef T vec8 __attribute__((ext_vector_type(8))); vec8 v; };
-
-template <typename T, bool DROP>
-__device__ __forceinline__ void apply_mask(Eight<T>& x, const DropoutMask& d, uint64_t group) {
-  if constexpr (DROP) {
-    const PhiloxWords w = philox_words(d, group);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x.v[j] = philox_kept(w, j, d.cut) ? x.v[j] : (T)0.0f;
-  }
-}
-
-template <typename T>
-__device__ __forceinline__ void to_planes(const Eight<T>& x, bf16x8 (&p)[thin_planes<T>()]) {
-  if constexpr (sizeof(T) == 2) p[0] = x.v;
-  else {
-#pragma unroll
-    for (int j = 0; j < 8; j += 2) {
-      bf16x2 s[3];
-      split_bf16_3(floatx2{x.v[j], x.v[j + 1]}, s);
-#pragma unroll
-      for (int k = 0; k < 3; ++k) { p[k][j] = s[k][0]; p[k][j + 1] = s[k][1]; }
-    }
-  }
-}
-
-// acc += a b over the products of planes that count, the smallest first.
-template <int NA>
-__device__ __forceinline__ void thin_multiply(const bf16x8 (&a)[NA], const bf16x8 (&b)[3], floatx4& acc) {
-#pragma unroll
-  for (int s = 2; s >= 0; --s)
-#pragma unroll
-    for (int k = 0; k < NA; ++k)
-      if (s - k >= 0) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[k], b[s - k], acc, 0, 0, 0);
-}
-
-// The other operand's step: 64 reduction indices of r32 rows of three planes, straight into LDS, rows of 128 bytes with unit u of
-// a row at u ^ (row % 8): the 16 rows of an operand read meet different banks.
-template <int RT>
-constexpr uint32_t thin_stage() { return 3u * RT * 16 * 128; }
-template <int RT>
-__device__ __forceinline__ void thin_transfer(const Planes& b, int64_t k, uint32_t lds, int wave, int lane) {
-#pragma unroll
-  for (int q = 0; q < (3 * RT * 2 + 3) / 4; ++q) {                 // pieces of eight rows, dealt to the four wavefronts
-    const int piece = 4 * q + wave;
-    if (piece >= 3 * RT * 2) break;
-    const int plane = piece / (RT * 2), row = (piece - plane * (RT * 2)) * 8 + (lane >> 3), unit = (lane & 7) ^ (row & 7);
-    transfer_to_lds(b.p[plane] + k, (uint32_t)(row * b.pitch * 2 + unit * 16), lds + (uint32_t)piece * 1024u);
-  }
-}
-template <int RT>
-__device__ __forceinline__ void thin_read(const unsigned char* lds, int r, int sub, int l16, int kg, bf16x8 (&b)[3]) {
-#pragma unroll
-  for (int k = 0; k < 3; ++k)
-    b[k] = *reinterpret_cast<const bf16x8*>(lds + (uint32_t)(k * RT * 16 + 16 * r + l16) * 128u + (uint32_t)((4 * sub + kg) ^ (l16 & 7)) * 16u);
-}
-
 // ------------------------------------------------------------------------------------------------
-// part[z] = drop(A) B^T over a range of the reduction, in steps of 64.  A workgroup owns 128 rows, a wavefront 32; A goes from global
-// memory into registers, a step ahead; B through two LDS stages, shared.
+// part[z] = drop(A) B^T over a range of the reduction, in steps of 64.  A workgroup owns 128 rows, a wavefront 32.
 struct ProjectArgs {
-  const void* A; int64_t m, K;
-  Planes b; DropoutMask d;
+  ThinSource a; Planes b;
   float* part; int steps, splits;
 };
 
 template <typename T, int RT, bool DROP>
 __global__ __launch_bounds__(256) void thin_project_kernel(ProjectArgs a) {
-  extern __shared__ __attribute__((aligned(16))) unsigned char thin_lds[];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l16 = lane & 15, kg = lane >> 4;
-  const int64_t row0 = (int64_t)blockIdx.x * 128 + 32 * wave;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  const int64_t row0 = (int64_t)blockIdx.x * 128 + 32 * (threadIdx.x >> 6);
   const int s0 = (int)((int64_t)a.steps * blockIdx.y / a.splits), s1 = (int)((int64_t)a.steps * (blockIdx.y + 1) / a.splits);
-  const T* x[2];
-  uint64_t group[2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int64_t r = row0 + 16 * h + l16, row = r < a.m ? r : a.m - 1;
-    x[h] = static_cast<const T*>(a.A) + row * a.K;
-    group[h] = (uint64_t)row * (uint64_t)(a.K >> 3);
-  }
   floatx4 acc[2][RT];
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int r = 0; r < RT; ++r) acc[h][r] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-  Eight<T> v[2][2];                                   // [half of the step][row tile]
-  auto load = [&](int s) __attribute__((always_inline)) {
-#pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
-      const int64_t k = 64 * (int64_t)s + 32 * sub + 8 * kg;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        v[sub][h].v = {};
-        if (k < a.K) v[sub][h].v = *reinterpret_cast<const typename Eight<T>::vec8*>(x[h] + k);      // K is a multiple of 8
-      }
-    }
-  };
-  if (s0 < s1) {
-    thin_transfer<RT>(a.b, 64 * (int64_t)s0, 0, wave, lane);
-    load(s0);
-  }
-  for (int s = s0; s < s1; ++s) {
-    const uint32_t stage = (uint32_t)((s - s0) & 1) * thin_stage<RT>();
-    bf16x8 p[2][2][thin_planes<T>()];
-#pragma unroll
-    for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        apply_mask<T, DROP>(v[sub][h], a.d, group[h] + (uint64_t)(8 * (int64_t)s + 4 * sub + kg));
-        to_planes<T>(v[sub][h], p[sub][h]);
-      }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();                                  // this step's B is there, and the other stage has been read
-    if (s + 1 < s1) {
-      thin_transfer<RT>(a.b, 64 * (int64_t)(s + 1), thin_stage<RT>() - stage, wave, lane);
-      load(s + 1);
-    }
-#pragma unroll
-    for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        bf16x8 b[3];
-        thin_read<RT>(thin_lds + stage, r, sub, l16, kg, b);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) thin_multiply<thin_planes<T>()>(p[sub][h], b, acc[h][r]);
-      }
-  }
-  float* out = a.part + (size_t)blockIdx.y * (size_t)a.m * (16 * RT);
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int64_t o = row0 + 16 * h + 4 * kg + e;
-      if (o < a.m) {
-#pragma unroll
-        for (int r = 0; r < RT; ++r) out[o * (16 * RT) + 16 * r + l16] = acc[h][r][e];
-      }
-    }
+  thin_clear(acc);
+  if (s0 < s1) thin_rows<T, 2, RT, 3, DROP, true>(a.a, a.b, row0, s0, s1, lds, acc);
+  thin_store(acc, a.part + (size_t)blockIdx.y * (size_t)a.a.m * (16 * RT), row0, a.a.m);
 }
 
 // Two workgroups a CU; a range keeps four steps.
@@ -163,7 +36,7 @@ int thin_project_splits(int64_t m, int64_t K) {
 template <typename T, int RT, bool DROP>
 static int project(const ProjectArgs& a, dim3 grid, hipStream_t st) {
   static LdsLimit limit;
-  constexpr size_t lds = 2 * thin_stage<RT>();
+  constexpr size_t lds = 2 * ThinStage<RT, 3>::BYTES;
   LQ_TRY(limit.raise(reinterpret_cast<const void*>(thin_project_kernel<T, RT, DROP>), lds));
   hipLaunchKernelGGL((thin_project_kernel<T, RT, DROP>), grid, dim3(256), lds, st, a);
   LQ_HIP_TRY(hipGetLastError());
@@ -187,8 +60,8 @@ int launch_thin_project(const void* A, int dtype, int64_t m, int64_t K, const Pl
                         hipStream_t st) {
   if (K < 8 || K % 8 || m < 1 || r32 < 32 || r32 % 32 || r32 > ADAPTER_MAX_RANK || b.pitch % 64 || b.pitch < K) return LQ_ERR_SHAPE;
   ProjectArgs a{};
-  a.A = A; a.m = m; a.K = K; a.b = b; a.part = part;
-  if (d) a.d = *d;
+  a.a = ThinSource{A, K, m, K, d ? *d : DropoutMask{}};
+  a.b = b; a.part = part;
   a.steps = (int)((K + 63) / 64);
   a.splits = thin_project_splits(m, K);
   const dim3 grid((unsigned)((m + 127) / 128), (unsigned)a.splits);
@@ -261,95 +134,21 @@ int launch_thin_finish(const float* part, int splits, int64_t m, int rank, int r
 }
 
 // ------------------------------------------------------------------------------------------------
-// part[z] (K x r32) = drop(A)^T B over a range of rows, in steps of 64.  A workgroup owns 128 columns of A, a wavefront 32.  A thread
-// loads four rows of eight columns, a step ahead, and writes them turned, four rows of a column at a time, into LDS rows of 64 + 8.
+// part[z] (K x r32) = drop(A)^T B over a range of rows, in steps of 64.  A workgroup owns 128 columns of A, a wavefront 32.
 struct GramArgs {
-  const void* A; int64_t m, K;
-  Planes bt; DropoutMask d;
+  ThinSource a; Planes bt;
   float* part; int steps, splits;
 };
-constexpr int TG_PITCH = 72;
-template <typename T, int RT>
-constexpr uint32_t gram_lds() { return 2 * thin_stage<RT>() + thin_planes<T>() * 128u * TG_PITCH * 2u; }
 
 template <typename T, int RT, bool DROP>
 __global__ __launch_bounds__(256) void thin_gram_kernel(GramArgs a) {
-  constexpr int NP = thin_planes<T>();
-  extern __shared__ __attribute__((aligned(16))) unsigned char thin_lds[];
-  __bf16* s_a = reinterpret_cast<__bf16*>(thin_lds + 2 * thin_stage<RT>());             // [plane][column][row]
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l16 = lane & 15, kg = lane >> 4;
-  const int c8 = (threadIdx.x & 15) * 8, r4 = (threadIdx.x >> 4) * 4;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const int64_t c0 = (int64_t)blockIdx.x * 128;
   const int s0 = (int)((int64_t)a.steps * blockIdx.y / a.splits), s1 = (int)((int64_t)a.steps * (blockIdx.y + 1) / a.splits);
-  const bool in = c0 + c8 < a.K;                                                        // K is a multiple of 8
-  const T* x = static_cast<const T*>(a.A) + c0 + c8;
   floatx4 acc[2][RT];
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int r = 0; r < RT; ++r) acc[h][r] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-  Eight<T> v[4];
-  auto load = [&](int s) __attribute__((always_inline)) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int64_t row = 64 * (int64_t)s + r4 + q;
-      v[q].v = {};
-      if (in && row < a.m) v[q].v = *reinterpret_cast<const typename Eight<T>::vec8*>(x + row * a.K);
-    }
-  };
-  if (s0 < s1) {
-    thin_transfer<RT>(a.bt, 64 * (int64_t)s0, 0, wave, lane);
-    load(s0);
-  }
-  for (int s = s0; s < s1; ++s) {
-    const uint32_t stage = (uint32_t)((s - s0) & 1) * thin_stage<RT>();
-    bf16x8 p[4][NP];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int64_t row = 64 * (int64_t)s + r4 + q;
-      apply_mask<T, DROP>(v[q], a.d, (uint64_t)row * (uint64_t)(a.K >> 3) + (uint64_t)((c0 + c8) >> 3));
-      to_planes<T>(v[q], p[q]);
-    }
-    __syncthreads();                                  // the tile of the step before has been read
-#pragma unroll
-    for (int k = 0; k < NP; ++k)
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        *reinterpret_cast<bf16x4*>(s_a + (k * 128 + c8 + j) * TG_PITCH + r4) = bf16x4{p[0][k][j], p[1][k][j], p[2][k][j], p[3][k][j]};
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();                                  // this step's tile and B are there
-    if (s + 1 < s1) {
-      thin_transfer<RT>(a.bt, 64 * (int64_t)(s + 1), thin_stage<RT>() - stage, wave, lane);
-      load(s + 1);
-    }
-#pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
-      bf16x8 t[2][NP];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int k = 0; k < NP; ++k)
-          t[h][k] = *reinterpret_cast<const bf16x8*>(s_a + (k * 128 + 32 * wave + 16 * h + l16) * TG_PITCH + 32 * sub + 8 * kg);
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        bf16x8 b[3];
-        thin_read<RT>(thin_lds + stage, r, sub, l16, kg, b);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) thin_multiply<NP>(t[h], b, acc[h][r]);
-      }
-    }
-  }
-  float* out = a.part + (size_t)blockIdx.y * (size_t)a.K * (16 * RT);
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int64_t o = c0 + 32 * wave + 16 * h + 4 * kg + e;
-      if (o < a.K) {
-#pragma unroll
-        for (int r = 0; r < RT; ++r) out[o * (16 * RT) + 16 * r + l16] = acc[h][r][e];
-      }
-    }
+  thin_clear(acc);
+  if (s0 < s1) thin_columns<T, RT, 3, DROP, true>(a.a, a.bt, c0, s0, s1, lds, acc, KeepStage{});
+  thin_store(acc, a.part + (size_t)blockIdx.y * (size_t)a.a.K * (16 * RT), c0 + 32 * (threadIdx.x >> 6), a.a.K);
 }
 
 struct GramSumArgs { const float* part; int parts; int64_t K; int rank, r32; float scale; int transposed; float* out; };
@@ -389,7 +188,7 @@ int thin_gram_splits(int64_t m, int64_t K) {
 template <typename T, int RT, bool DROP>
 static int gram(const GramArgs& a, dim3 grid, hipStream_t st) {
   static LdsLimit limit;
-  constexpr size_t lds = gram_lds<T, RT>();
+  constexpr size_t lds = thin_columns_lds<T, RT, 3>();
   LQ_TRY(limit.raise(reinterpret_cast<const void*>(thin_gram_kernel<T, RT, DROP>), lds));
   hipLaunchKernelGGL((thin_gram_kernel<T, RT, DROP>), grid, dim3(256), lds, st, a);
   LQ_HIP_TRY(hipGetLastError());
@@ -414,8 +213,8 @@ int launch_thin_gram(const void* A, int dtype, int64_t m, int64_t K, const Plane
   if (K < 8 || K % 8 || m < 1 || r32 < 32 || r32 % 32 || r32 > ADAPTER_MAX_RANK || bt.pitch % 64 || bt.pitch < up_to(m, 64))
     return LQ_ERR_SHAPE;
   GramArgs a{};
-  a.A = A; a.m = m; a.K = K; a.bt = bt; a.part = part;
-  if (d) a.d = *d;
+  a.a = ThinSource{A, K, m, K, d ? *d : DropoutMask{}};
+  a.bt = bt; a.part = part;
   a.steps = (int)((m + 63) / 64);
   a.splits = thin_gram_splits(m, K);
   const dim3 grid((unsigned)((K + 127) / 128), (unsigned)a.splits);

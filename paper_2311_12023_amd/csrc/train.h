@@ -118,8 +118,8 @@ int launch_loss_begin(const LossRows& r, int64_t n, uint32_t* tops, hipStream_t 
 constexpr int LOSS_E_SHIFT = 14;
 int launch_loss_logits(const Planes& w, const Planes& x, int64_t depth, const LossPiece& p, const LossRows& r, const LossScales& s,
                        float* part_ref, float* part_sum, uint16_t* const e[2], int64_t e_pitch, hipStream_t st);
-// Joins the tiles' sums with the row's, brings E to one power of two per row.
-int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, const float* part_ref, const float* part_sum,
+// Joins the sums of tiles of `tile` classes with the row's; with e (tiles of SEG_T classes) brings E to one power of two per row.
+int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, const float* part_ref, const float* part_sum, int tile,
                      uint16_t* const e[2], int64_t e_pitch, hipStream_t st);
 // acc (n x d) = acc shift + E W; first: acc = E W.  part: splits x n x d floats.
 int loss_accumulate_splits(int64_t n, int64_t d, int64_t depth, bool half);
@@ -139,6 +139,19 @@ int launch_loss_gradient(const Planes& w, const Planes& x, int64_t depth, const 
 int loss_dw_splits(int64_t rows, int64_t cols, int64_t depth, bool half);
 int launch_loss_dw(const Planes& g, const Planes& xt, int64_t depth, int64_t rows, int64_t cols, const float* factor, int dtype,
                    void* out, float* part, size_t part_floats, hipStream_t st);
+
+// ---- the same for few rows (loss_few_kernels.hip) ---------------------------------------------------------
+// Up to LOSS_FEW rows the loss is bound by reading W: it is then read where it is, once for the logits and once for dX, the whole
+// vocabulary as one piece.  Planes of X (one for bf16, three for
+// fp32) and E have few_rows(n) rows.  Tiles are LOSS_FEW_TILE classes; E is relative to its tile's power of two.
+constexpr int64_t LOSS_FEW = 128, LOSS_FEW_TILE = 64;
+inline int64_t few_rows(int64_t n) { return n <= 16 ? 16 : n <= 32 ? 32 : n <= 64 ? 64 : 128; }
+int launch_few_logits(const void* W, int64_t ldw, int dtype, int64_t d, const Planes& x, const LossPiece& p, const LossRows& r,
+                      float* part_ref, float* part_sum, uint16_t* const e[3], int64_t e_pitch, hipStream_t st);
+// dX from E and W once r.wrong is there.  part: few_dx_splits(vocab, d) x d x few_rows(n) floats.
+int few_dx_splits(int64_t vocab, int64_t d);
+int launch_few_dx(const void* W, int64_t ldw, int dtype, int64_t d, const Planes& e, const LossPiece& p, const LossRows& r,
+                  const float* part_ref, const float* factors, float* part, void* dX, hipStream_t st);
 
 // ---- adapter products (adapter_kernels.hip, thin_kernels.hip) ---------------------------------------------
 constexpr int ADAPTER_MAX_RANK = 128;
