@@ -53,7 +53,7 @@ template <int BITS, bool HALF>
 __global__ __launch_bounds__(256) void weight_rows_kernel(WeightArgs a) {
   __shared__ float s_code[1 << BITS];
   load_codebook<BITS>(a, s_code);
-  const float scale = HALF ? power_of_two(half_exponent(*a.top)) : 1.0f;
+  const float scale = HALF ? power_of_two(half_exponent_of(a.top, TOP_WORDS)) : 1.0f;
   const int64_t runs = (a.N + 63) / 64 * 4, total = a.K * runs;       // runs of 16 up to a multiple of 64 weights
   for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
     const int64_t row = u / runs, c = (u - row * runs) * 16;
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(256) void weight_columns_kernel(WeightArgs a) {
   __shared__ float s_code[1 << BITS];
   __shared__ uint32_t s_w[HALF ? 2 : 1][WC_N * WC_WORDS];
   load_codebook<BITS>(a, s_code);
-  const float scale = HALF ? power_of_two(half_exponent(*a.top)) : 1.0f;
+  const float scale = HALF ? power_of_two(half_exponent_of(a.top, TOP_WORDS)) : 1.0f;
   const int tid = threadIdx.x, run = tid & 7, pair = tid >> 3;
   const int64_t n0 = (int64_t)blockIdx.x * WC_N, k0 = (int64_t)blockIdx.y * WC_K, col = n0 + 16 * run;
   float w[2][16];
@@ -178,11 +178,12 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void adapter_product_kernel(Adapter
   SegAcc acc;
   seg_clear(acc);
   const int64_t row0 = (int64_t)t.tm * SEG_T + 128 * t.wm + 4 * t.kg, col0 = (int64_t)t.tn * SEG_T + 64 * t.wn + t.l16;
+  const float a_inv = HALF ? power_of_two(-half_exponent_of(a.s.a_top, TOP_WORDS)) : 1.0f;
   float inv[4];                                       // what a token's sums of the fp16 planes are to be multiplied by
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int64_t token = col0 + 16 * j;
-    inv[j] = HALF && token < a.tokens ? a.s.b_inv[token] * power_of_two(-half_exponent(*a.s.a_top)) : 1.0f;
+    inv[j] = HALF && token < a.tokens ? a.s.b_inv[token] * a_inv : 1.0f;
   }
   if (t.split == 0 && a.low.pairs > 0) {
     seg_products<__bf16>(a.low, t, 0, a.low.pairs, seg_lds, acc);

@@ -16,6 +16,13 @@ __device__ __forceinline__ uint32_t finite_magnitude(float v) {
   return b < 0x7f800000u ? b : 0u;
 }
 
+// The exponent for an operand whose largest magnitude is the largest of `count` words.
+__device__ __forceinline__ int half_exponent_of(const uint32_t* __restrict__ tops, int count) {
+  uint32_t top = 0;
+  for (int i = 0; i < count; ++i) top = max(top, tops[i]);
+  return half_exponent(top);
+}
+
 struct HalfPair { _Float16 hi, lo; };
 __device__ __forceinline__ HalfPair split_half(float v) {
   const _Float16 h = (_Float16)v;

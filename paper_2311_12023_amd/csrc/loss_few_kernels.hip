@@ -128,13 +128,25 @@ struct FewDxArgs {
 // E's step brought from its tile's power of two to the row's.
 template <int RT, int NB>
 struct ShiftStage {
+  typedef ThinStage<RT, NB> Stage;
   const FewDxArgs& a;
-  __device__ __forceinline__ void operator()(ThinStage<RT, NB>& s, int step) const {
+  float to[Stage::LOADS], from[Stage::LOADS];            // of the rows that this thread brings
+  __device__ __forceinline__ static int token(int q) { return ((threadIdx.x + 256 * q) >> 3) % (16 * RT); }
+  __device__ __forceinline__ explicit ShiftStage(const FewDxArgs& args) : a(args) {
 #pragma unroll
-    for (int q = 0; q < ThinStage<RT, NB>::LOADS; ++q) {
-      const int row = (threadIdx.x + 256 * q) >> 3, token = row % (16 * RT);
-      if (row >= ThinStage<RT, NB>::ROWS || token >= a.n) continue;
-      const float ref = a.ref[token], f = __builtin_amdgcn_exp2f(a.part_ref[(int64_t)step * a.n + token] - (ref == -__builtin_inff() ? 0.0f : ref));
+    for (int q = 0; q < Stage::LOADS; ++q) {
+      to[q] = token(q) < a.n ? a.ref[token(q)] : 0.0f;
+      if (to[q] == -__builtin_inff()) to[q] = 0.0f;
+    }
+  }
+  __device__ __forceinline__ void load(int step) {
+#pragma unroll
+    for (int q = 0; q < Stage::LOADS; ++q) from[q] = token(q) < a.n ? a.part_ref[(int64_t)step * a.n + token(q)] : 0.0f;
+  }
+  __device__ __forceinline__ void operator()(Stage& s) {
+#pragma unroll
+    for (int q = 0; q < Stage::LOADS; ++q) {
+      const float f = __builtin_amdgcn_exp2f(from[q] - to[q]);
       bf16x8 v = __builtin_bit_cast(bf16x8, s.r[q]);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = (__bf16)((float)v[j] * f);
@@ -151,7 +163,7 @@ __global__ __launch_bounds__(256) void few_dx_kernel(FewDxArgs a) {
   const int s0 = (int)((int64_t)a.steps * blockIdx.y / a.splits), s1 = (int)((int64_t)a.steps * (blockIdx.y + 1) / a.splits);
   floatx4 acc[2][RT];
   thin_clear(acc);
-  if (s0 < s1) thin_columns<T, RT, NB, false, VEC>(a.w, a.e, c0, s0, s1, lds, acc, ShiftStage<RT, NB>{a});
+  if (s0 < s1) thin_columns<T, RT, NB, false, VEC>(a.w, a.e, c0, s0, s1, lds, acc, ShiftStage<RT, NB>(a));
   thin_store(acc, a.part + (size_t)blockIdx.y * (size_t)a.w.K * (16 * RT), c0 + 32 * (threadIdx.x >> 6), a.w.K);
 }
 

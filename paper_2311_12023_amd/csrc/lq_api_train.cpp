@@ -125,7 +125,7 @@ static void plan_product(AdapterPlan& p, Arena& a, int64_t m, int64_t features, 
     p.b2[h] = a.take<uint16_t>(m * p.r64);
   }
   p.inv = a.take<float>(half ? m : 0);
-  p.top = a.take<uint32_t>(1);
+  p.top = a.take<uint32_t>(TOP_WORDS);
   const int s = adapter_product_splits(features, m, depth, dtype);
   p.part_floats = s > 1 ? (size_t)s * m * features : 0;
   p.part = a.take<float>(p.part_floats);
@@ -149,31 +149,33 @@ static AdapterPlan plan_backward(void* ws, int64_t m, int64_t d, int64_t k, int 
     p.ut[h] = a.take<uint16_t>(p.r32 * p.m64);
     p.tt[h] = a.take<uint16_t>(p.r32 * p.m64);
   }
-  p.thin = a.take<float>(std::max({(size_t)thin_project_splits(m, k) * m, (size_t)thin_gram_splits(m, k) * k,
-                                   (size_t)thin_gram_splits(m, d) * d}) * p.r32);
+  p.thin = a.take<float>(std::max((size_t)thin_project_splits(m, k) * m, (size_t)thin_gram_splits(m, k, d) * (k + d)) * p.r32);
   plan_product(p, a, m, d, k, dtype);
   p.bytes = a.used();
   return p;
 }
 
-// The activations' planes (bf16 ones of whole pairs of steps are read where they are) and the weights'.
-static int product_planes(const AdapterPlan& p, const MvWeights& q, int64_t d, int64_t k, bool transposed, const void* x, int64_t m,
-                          int64_t depth, int dtype, Planes* w, Planes* act, hipStream_t st) {
-  const bool half = dtype == LQ_T_FP32;
-  if (half) {
-    const int64_t groups = (d * k + (int64_t)q.block * q.scale_block - 1) / ((int64_t)q.block * q.scale_block);
-    LQ_TRY(launch_zero_words(p.top, 1, st));
-    LQ_TRY(launch_top_magnitude(q.v, groups, 1, groups, nullptr, 0, p.top, st));      // no weight is larger than its group's scale
-  }
-  LQ_TRY(launch_weight_planes(q, d, k, transposed, p.top, p.q[0], half ? p.q[1] : nullptr, p.in64, st));
-  *w = Planes{{p.q[0], half ? p.q[1] : nullptr, nullptr}, p.in64};
-  if (!half && depth % 64 == 0) {
+// What the large product takes its activations from (bf16 ones of whole pairs of steps are read where they are), and the passes
+// for it and for the weights' scale.
+static int activation_planes(const AdapterPlan& p, const MvWeights& q, int64_t weights, const void* x, int64_t m, int64_t depth, int dtype,
+                             PrepareJobs& jobs, Planes* act) {
+  if (dtype == LQ_T_BF16 && depth % 64 == 0) {
     *act = Planes{{static_cast<const uint16_t*>(x), nullptr, nullptr}, depth};
     return LQ_OK;
   }
-  const PlaneTarget t{{p.x[0], half ? p.x[1] : nullptr, nullptr}, p.in64, m};
+  const PlaneTarget t{{p.x[0], dtype == LQ_T_FP32 ? p.x[1] : nullptr, nullptr}, p.in64, m};
+  const PlaneSource s{x, dtype, depth, m, depth, nullptr};
   *act = planes_of(t);
-  return launch_row_planes({x, dtype, depth, m, depth, nullptr}, half ? PLANE_HALF_2 : PLANE_BF16, t, half ? p.inv : nullptr, st);
+  if (dtype == LQ_T_BF16) return jobs.rows(s, t);
+  const int64_t group = (int64_t)q.block * q.scale_block;
+  LQ_TRY(jobs.tops(q.v, (weights + group - 1) / group, p.top));       // no weight is larger than its group's scale
+  return jobs.rows_scaled(s, t, p.inv);
+}
+static int weight_planes(const AdapterPlan& p, const MvWeights& q, int64_t d, int64_t k, bool transposed, int dtype, Planes* w,
+                         hipStream_t st) {
+  uint16_t* lo = dtype == LQ_T_FP32 ? p.q[1] : nullptr;
+  *w = Planes{{p.q[0], lo, nullptr}, p.in64};
+  return launch_weight_planes(q, d, k, transposed, p.top, p.q[0], lo, p.in64, st);
 }
 
 // The low-rank part in the large product: two of its planes (16 bits) where the result is bf16, all three where it is fp32.
@@ -321,12 +323,15 @@ int lq_adapter_forward(const void* X, int64_t m, int64_t d, int64_t k, const uin
   const int r32 = (int)w.r32;
   const PlaneTarget l1{{w.b[0], w.b[1], w.b[2]}, up_to(d, 64), w.r32}, none{};
   const PlaneTarget t{{w.b2[0], w.b2[1], w.b2[2]}, w.r64, m}, l2{{w.a2[0], w.a2[1], w.a2[2]}, w.r64, k};
-  LQ_TRY(launch_column_planes({L1, LQ_T_FP32, rank, d, rank, nullptr}, PLANE_BF16_3, l1, nullptr, 0, st));
-  LQ_TRY(launch_column_planes({L2, LQ_T_FP32, k, rank, k, nullptr}, PLANE_BF16_3, l2, nullptr, 0, st));
-  LQ_TRY(launch_thin_project(X, dtype, m, d, planes_of(l1), r32, mask.cut ? &mask : nullptr, w.thin, st));
-  LQ_TRY(launch_thin_finish(w.thin, thin_project_splits(m, d), m, rank, r32, mask.scale, T, t, none, st));
+  PrepareJobs jobs{};
   Planes weights, act;
-  LQ_TRY(product_planes(w, q, d, k, true, X, m, d, dtype, &weights, &act, st));
+  LQ_TRY(jobs.columns3({L1, LQ_T_FP32, rank, d, rank, nullptr}, l1));
+  LQ_TRY(jobs.columns3({L2, LQ_T_FP32, k, rank, k, nullptr}, l2));
+  LQ_TRY(activation_planes(w, q, d * k, X, m, d, dtype, jobs, &act));
+  LQ_TRY(jobs.launch(st));
+  LQ_TRY(launch_thin_project(X, dtype, m, d, planes_of(l1), r32, mask, w.thin, st));
+  LQ_TRY(launch_thin_finish(w.thin, thin_project_splits(m, d), m, rank, r32, mask.scale, T, t, none, st));
+  LQ_TRY(weight_planes(w, q, d, k, true, dtype, &weights, st));
   return launch_adapter_product(weights, act, w.in64, low_rank_planes(l2, dtype), low_rank_planes(t, dtype), w.r64, {w.inv, w.top}, k, m,
                                 nullptr, dtype, Y, w.part, w.part_floats, st);
 }
@@ -350,16 +355,20 @@ int lq_adapter_backward(const void* dY, const void* X, int64_t m, int64_t d, int
   const PlaneTarget l2{{w.b[0], w.b[1], w.b[2]}, up_to(k, 64), w.r32}, none{};
   const PlaneTarget u{{w.b2[0], w.b2[1], w.b2[2]}, w.r64, m}, l1{{w.a2[0], w.a2[1], w.a2[2]}, w.r64, d};
   const PlaneTarget ut{{w.ut[0], w.ut[1], w.ut[2]}, w.m64, w.r32}, tt{{w.tt[0], w.tt[1], w.tt[2]}, w.m64, w.r32};
-  LQ_TRY(launch_row_planes({L2, LQ_T_FP32, k, rank, k, nullptr}, PLANE_BF16_3, l2, nullptr, st));
-  LQ_TRY(launch_thin_project(dY, dtype, m, k, planes_of(l2), r32, nullptr, w.thin, st));
-  LQ_TRY(launch_thin_finish(w.thin, thin_project_splits(m, k), m, rank, r32, 1.0f, nullptr, u, ut, st));
-  LQ_TRY(launch_thin_finish(T, 0, m, rank, r32, 1.0f, nullptr, none, tt, st));
-  LQ_TRY(launch_thin_gram(dY, dtype, m, k, planes_of(tt), rank, r32, nullptr, 1.0f, true, w.thin, dL2, st));
-  LQ_TRY(launch_thin_gram(X, dtype, m, d, planes_of(ut), rank, r32, mask.cut ? &mask : nullptr, mask.scale, false, w.thin, dL1, st));
-  if (!dX) return LQ_OK;
-  LQ_TRY(launch_row_planes({L1, LQ_T_FP32, rank, d, rank, nullptr}, PLANE_BF16_3, l1, nullptr, st));
+  PrepareJobs jobs{};
   Planes weights, act;
-  LQ_TRY(product_planes(w, q, d, k, false, dY, m, k, dtype, &weights, &act, st));
+  LQ_TRY(jobs.rows3({L2, LQ_T_FP32, k, rank, k, nullptr}, l2));
+  LQ_TRY(jobs.columns3({T, LQ_T_FP32, rank, m, rank, nullptr}, tt));
+  if (dX) {
+    LQ_TRY(jobs.rows3({L1, LQ_T_FP32, rank, d, rank, nullptr}, l1));
+    LQ_TRY(activation_planes(w, q, d * k, dY, m, k, dtype, jobs, &act));
+  }
+  LQ_TRY(jobs.launch(st));
+  LQ_TRY(launch_thin_project(dY, dtype, m, k, planes_of(l2), r32, DropoutMask{}, w.thin, st));
+  LQ_TRY(launch_thin_finish(w.thin, thin_project_splits(m, k), m, rank, r32, 1.0f, nullptr, u, ut, st));
+  LQ_TRY(launch_thin_grams(dY, k, planes_of(tt), dL2, X, d, planes_of(ut), mask, dL1, dtype, m, rank, r32, w.thin, st));
+  if (!dX) return LQ_OK;
+  LQ_TRY(weight_planes(w, q, d, k, false, dtype, &weights, st));
   return launch_adapter_product(weights, act, w.in64, low_rank_planes(l1, dtype), low_rank_planes(u, dtype), w.r64, {w.inv, w.top}, d, m,
                                 mask.cut ? &mask : nullptr, dtype, dX, w.part, w.part_floats, st);
 }

@@ -30,9 +30,11 @@ __device__ __forceinline__ void load_eight(const T* at, int64_t left, Eight<T>& 
   }
 }
 
-template <typename T, bool DROP>
+// MASKED: there may be a mask (a cut of zero keeps everything).
+template <typename T, bool MASKED>
 __device__ __forceinline__ void apply_mask(Eight<T>& x, const DropoutMask& d, uint64_t group) {
-  if constexpr (DROP) {
+  if constexpr (MASKED) {
+    if (d.cut == 0) return;
     const PhiloxWords w = philox_words(d, group);
 #pragma unroll
     for (int j = 0; j < 8; ++j) x.v[j] = philox_kept(w, j, d.cut) ? x.v[j] : (T)0.0f;
@@ -101,7 +103,7 @@ __device__ __forceinline__ void thin_read(const unsigned char* lds, int r, int s
 struct ThinSource { const void* A; int64_t lda, m, K; DropoutMask d; };
 
 // acc[h][r] += drop(A) B^T over steps s0 .. s1 - 1 (s0 < s1) for rows row0 + 16 h ..: element e is row 4 kg + e, column 16 r + l16.
-template <typename T, int H, int RT, int NB, bool DROP, bool VEC>
+template <typename T, int H, int RT, int NB, bool MASKED, bool VEC>
 __device__ __forceinline__ void thin_rows(const ThinSource& a, const Planes& b, int64_t row0, int s0, int s1, unsigned char* lds,
                                           floatx4 (&acc)[H][RT]) {
   typedef ThinStage<RT, NB> Stage;
@@ -142,7 +144,7 @@ __device__ __forceinline__ void thin_rows(const ThinSource& a, const Planes& b, 
     for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
       for (int h = 0; h < H; ++h) {
-        apply_mask<T, DROP>(v[u][sub][h], a.d, group[h] + (uint64_t)(8 * (int64_t)s + 4 * sub + kg));
+        apply_mask<T, MASKED>(v[u][sub][h], a.d, group[h] + (uint64_t)(8 * (int64_t)s + 4 * sub + kg));
         to_planes<T>(v[u][sub][h], p[sub][h]);
       }
     load(parity, s + 2 < last ? s + 2 : last);        // past the end: the last step again, never used
@@ -166,24 +168,28 @@ __device__ __forceinline__ void thin_rows(const ThinSource& a, const Planes& b, 
 
 // acc[h][r] += drop(A)^T B over steps s0 .. s1 - 1 (s0 < s1) of 64 rows for columns c0 + 32 wave + 16 h ..: element e is column
 // 4 kg + e, column 16 r + l16 of B.  A thread loads four rows of eight columns and writes them turned, four rows of a column at a
-// time, into LDS rows of 64 + 8.
-constexpr int TG_PITCH = 72;
+// time.  A column's 64 rows are 128 bytes, its unit u of 16 at u ^ turn(column): the sixteen columns, eight apart, of a write and
+// the sixteen neighbours of an operand read both spread over the banks (rows of 64 + 8 instead, without the turn, met eight at a
+// time in a bank when written).
+__device__ __forceinline__ uint32_t thin_turn(int column) { return (uint32_t)((column >> 3) ^ (column >> 1)) & 7u; }
 template <typename T, int RT, int NB>
-constexpr uint32_t thin_columns_lds() { return 2 * ThinStage<RT, NB>::BYTES + thin_planes<T>() * 128u * TG_PITCH * 2u; }
+constexpr uint32_t thin_columns_lds() { return 2 * ThinStage<RT, NB>::BYTES + thin_planes<T>() * 128u * 128u; }
 
+// adjust.load(s) is called where step s's B is loaded, adjust(stage) before it goes into LDS.
 struct KeepStage {
-  template <class S> __device__ __forceinline__ void operator()(S&, int) const {}
+  __device__ __forceinline__ void load(int) {}
+  template <class S> __device__ __forceinline__ void operator()(S&) {}
 };
-// adjust(stage, s): what becomes of step s's B before it goes into LDS.
-template <typename T, int RT, int NB, bool DROP, bool VEC, class Adjust>
+template <typename T, int RT, int NB, bool MASKED, bool VEC, class Adjust>
 __device__ __forceinline__ void thin_columns(const ThinSource& a, const Planes& b, int64_t c0, int s0, int s1, unsigned char* lds,
                                              floatx4 (&acc)[2][RT], Adjust&& adjust) {
   typedef ThinStage<RT, NB> Stage;
   constexpr int NP = thin_planes<T>();
-  __bf16* s_a = reinterpret_cast<__bf16*>(lds + 2 * Stage::BYTES);                      // [plane][column][row]
+  unsigned char* s_a = lds + 2 * Stage::BYTES;                                          // [plane][column][row]
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l16 = lane & 15, kg = lane >> 4;
   const int c8 = (threadIdx.x & 15) * 8, r4 = (threadIdx.x >> 4) * 4;
   const T* x = static_cast<const T*>(a.A) + c0 + c8;
+  const int col[2] = {32 * wave + l16, 32 * wave + 16 + l16};
   Eight<T> v[2][4];
   Stage stage;
   auto load = [&](auto parity, int s) __attribute__((always_inline)) {
@@ -198,18 +204,20 @@ __device__ __forceinline__ void thin_columns(const ThinSource& a, const Planes& 
   const auto odd = std::integral_constant<int, 1>{};
   const int last = s1 - 1;
   stage.load(b, 64 * (int64_t)s0);
+  adjust.load(s0);
   load(even, s0);
   load(odd, s0 + 1 < last ? s0 + 1 : last);
-  adjust(stage, s0);
+  adjust(stage);
   stage.store(lds);
   stage.load(b, 64 * (int64_t)(s0 + 1 < last ? s0 + 1 : last));
+  adjust.load(s0 + 1 < last ? s0 + 1 : last);
   auto step = [&](auto parity, int s) __attribute__((always_inline)) {
     constexpr int u = decltype(parity)::value;
     bf16x8 p[4][NP];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int64_t row = 64 * (int64_t)s + r4 + q;
-      apply_mask<T, DROP>(v[u][q], a.d, (uint64_t)row * (uint64_t)(a.K >> 3) + (uint64_t)((c0 + c8) >> 3));
+      apply_mask<T, MASKED>(v[u][q], a.d, (uint64_t)row * (uint64_t)(a.K >> 3) + (uint64_t)((c0 + c8) >> 3));
       to_planes<T>(v[u][q], p[q]);
     }
     load(parity, s + 2 < last ? s + 2 : last);
@@ -218,10 +226,12 @@ __device__ __forceinline__ void thin_columns(const ThinSource& a, const Planes& 
     for (int k = 0; k < NP; ++k)
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        *reinterpret_cast<bf16x4*>(s_a + (k * 128 + c8 + j) * TG_PITCH + r4) = bf16x4{p[0][k][j], p[1][k][j], p[2][k][j], p[3][k][j]};
-    adjust(stage, s + 1 < last ? s + 1 : last);
+        *reinterpret_cast<bf16x4*>(s_a + (k * 128 + c8 + j) * 128 + (((uint32_t)(r4 >> 3) ^ thin_turn(c8 + j)) * 16u) + (r4 & 4) * 2) =
+            bf16x4{p[0][k][j], p[1][k][j], p[2][k][j], p[3][k][j]};
+    adjust(stage);
     stage.store(lds + (u ? 0 : Stage::BYTES));
     stage.load(b, 64 * (int64_t)(s + 2 < last ? s + 2 : last));
+    adjust.load(s + 2 < last ? s + 2 : last);
     lds_barrier();                                    // this step's tile is there
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub) {
@@ -230,7 +240,7 @@ __device__ __forceinline__ void thin_columns(const ThinSource& a, const Planes& 
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int k = 0; k < NP; ++k)
-          t[h][k] = *reinterpret_cast<const bf16x8*>(s_a + (k * 128 + 32 * wave + 16 * h + l16) * TG_PITCH + 32 * sub + 8 * kg);
+          t[h][k] = *reinterpret_cast<const bf16x8*>(s_a + (k * 128 + col[h]) * 128 + (((uint32_t)(4 * sub + kg) ^ thin_turn(col[h])) * 16u));
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         bf16x8 w[NB];

@@ -92,7 +92,22 @@ int launch_column_planes(const PlaneSource& s, PlaneKind kind, const PlaneTarget
 // *top = bits of the largest finite magnitude (keep as above); *top is zero before.
 int launch_top_magnitude(const void* src, int64_t ld, int64_t rows, int64_t cols, const int64_t* keep, int64_t keep_below,
                          uint32_t* top, hipStream_t st);                      // fp32
-int launch_zero_words(uint32_t* p, int count, hipStream_t st);
+// Several such passes over small operands in one launch.
+constexpr int TOP_WORDS = 64;
+struct PrepareJobs {
+  struct Job {
+    int what; int wgs;
+    PlaneSource s; PlaneTarget t; float* row_inv; uint32_t* tops; int tiles_r;
+  };
+  Job job[5];
+  int count;
+  int rows3(const PlaneSource& s, const PlaneTarget& t);             // launch_row_planes, PLANE_BF16_3
+  int columns3(const PlaneSource& s, const PlaneTarget& t);          // launch_column_planes, PLANE_BF16_3
+  int rows_scaled(const PlaneSource& s, const PlaneTarget& t, float* row_inv);
+  int rows(const PlaneSource& s, const PlaneTarget& t);              // bf16 into a padded plane
+  int tops(const float* v, int64_t n, uint32_t* words);              // TOP_WORDS words, the largest of which is v's
+  int launch(hipStream_t st) const;
+};
 
 // ---- softmax cross entropy (loss_kernels.hip) -----------------------------------------------------------
 struct LossRows {            // per-row state, n values each
@@ -156,21 +171,22 @@ int launch_few_dx(const void* W, int64_t ldw, int dtype, int64_t d, const Planes
 // ---- adapter products (adapter_kernels.hip, thin_kernels.hip) ---------------------------------------------
 constexpr int ADAPTER_MAX_RANK = 128;
 // part[z] (m x r32) = drop(A) B over range z of the reduction: A m x K of type dtype, contiguous, K a multiple of 8, B as three
-// bf16 planes of r32 rows x up_to(K, 64).  d: NULL without dropout (its factor is left to launch_thin_finish).
+// bf16 planes of r32 rows x up_to(K, 64).  The mask's factor is left to launch_thin_finish.
 int thin_project_splits(int64_t m, int64_t K);
-int launch_thin_project(const void* A, int dtype, int64_t m, int64_t K, const Planes& b, int r32, const DropoutMask* d, float* part,
+int launch_thin_project(const void* A, int dtype, int64_t m, int64_t K, const Planes& b, int r32, const DropoutMask& d, float* part,
                         hipStream_t st);
 // T = scale * sum of the partial results: fp32 m x rank (NULL: not wanted), three planes m x up_to(r32, 64) and three of the
-// transpose, r32 x up_to(m, 64) (p[0] NULL: not wanted).  splits == 0: T is given (m x rank in `part`).
+// transpose, r32 x up_to(m, 64) (p[0] NULL: not wanted).
 int launch_thin_finish(const float* part, int splits, int64_t m, int rank, int r32, float scale, float* T, const PlaneTarget& rows,
                        const PlaneTarget& cols, hipStream_t st);
-// out = scale * drop(A)^T B: A m x K as above, B^T as three planes of r32 rows x up_to(m, 64).  out: K x rank, or rank x K
-// (transposed).  part: thin_gram_splits x K x r32 floats.
-int thin_gram_splits(int64_t m, int64_t K);
-int launch_thin_gram(const void* A, int dtype, int64_t m, int64_t K, const Planes& bt, int rank, int r32, const DropoutMask* d,
-                     float scale, bool transposed, float* part, float* out, hipStream_t st);
+// dL2 (rank x k) = T^T dY and dL1 (d x rank) = drop(X)^T U; T^T and U^T as three planes of r32 rows x up_to(m, 64).
+// part: thin_gram_splits(m, k, d) x (k + d) x r32 floats.
+int thin_gram_splits(int64_t m, int64_t k, int64_t d);
+int launch_thin_grams(const void* dY, int64_t k, const Planes& tt, float* dL2, const void* X, int64_t d, const Planes& ut,
+                      const DropoutMask& mask, float* dL1, int dtype, int64_t m, int rank, int r32, float* part, hipStream_t st);
 // The stored weights (K x N, row-major) as planes, row by row (zero from N to up_to(N, 64)) or transposed (N rows, zero from K to
-// up_to(K, 64)): one bf16 plane, or two fp16 planes times the power of two that *top (of the group scales v) gives.
+// up_to(K, 64)): one bf16 plane, or two fp16 planes times the power of two that the largest of the
+// TOP_WORDS words at `top` (of the group scales v) gives.
 int launch_weight_planes(const MvWeights& q, int64_t K, int64_t N, bool transposed, const uint32_t* top, uint16_t* hi, uint16_t* lo,
                          int64_t pitch, hipStream_t st);
 // out (tokens x features, of type dtype) = B A^T + mask .* (B2 A2^T): A the weights (features x depth), B the activations

@@ -60,10 +60,10 @@ __device__ __forceinline__ void store_split(const RowArgs& a, int64_t row, int64
 }
 
 template <typename T, int KIND, bool VEC>
-__global__ __launch_bounds__(256) void row_planes_kernel(RowArgs a) {
+__device__ __forceinline__ void row_planes(const RowArgs& a, int64_t block, int64_t blocks) {
   const int64_t units = (a.cols + 63) / 64 * 8, total = a.t.rows * units;
   const float scale = KIND == PLANE_HALF_2 ? power_of_two(half_exponent(*a.top)) : 1.0f;
-  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
+  for (int64_t u = block * 256 + threadIdx.x; u < total; u += blocks * 256) {
     const int64_t row = u / units, c = (u - row * units) * 8;
     float v[8];
     load8<T, VEC>(static_cast<const T*>(a.src) + row * a.ld, c, row < a.rows ? a.cols : 0, v);
@@ -71,11 +71,14 @@ __global__ __launch_bounds__(256) void row_planes_kernel(RowArgs a) {
   }
 }
 
+template <typename T, int KIND, bool VEC>
+__global__ __launch_bounds__(256) void row_planes_kernel(RowArgs a) { row_planes<T, KIND, VEC>(a, blockIdx.x, gridDim.x); }
+
 // fp16 planes with a power of two per row: a wavefront walks its row for the largest magnitude and again, out of the cache, to
 // split it.
 template <bool VEC>
-__global__ __launch_bounds__(256) void row_scaled_planes_kernel(RowArgs a) {
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+__device__ __forceinline__ void row_scaled_planes(const RowArgs& a, int64_t block) {
+  const int64_t row = block * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (row >= a.rows) return;
   const float* x = static_cast<const float*>(a.src) + row * a.ld;
@@ -97,6 +100,9 @@ __global__ __launch_bounds__(256) void row_scaled_planes_kernel(RowArgs a) {
   }
 }
 
+template <bool VEC>
+__global__ __launch_bounds__(256) void row_scaled_planes_kernel(RowArgs a) { row_scaled_planes<VEC>(a, blockIdx.x); }
+
 // A workgroup turns 64 x 64 values in LDS: a thread packs two rows of eight columns, so that words are written, in rows of 33
 // words: the eight columns and eight row pairs of a wavefront meet 64 different banks.
 struct ColumnArgs {
@@ -108,11 +114,10 @@ struct ColumnArgs {
 constexpr int CP = 64, CP_WORDS = 33;
 
 template <typename T, int KIND, bool VEC>
-__global__ __launch_bounds__(256) void column_planes_kernel(ColumnArgs a) {
+__device__ __forceinline__ void column_planes(const ColumnArgs& a, uint32_t block, uint32_t (*s_w)[CP * CP_WORDS]) {
   constexpr int N = plane_count<KIND>();
-  __shared__ uint32_t s_w[N][CP * CP_WORDS];
   const int tid = threadIdx.x;
-  const int64_t r0 = (int64_t)(blockIdx.x % a.tiles_r) * CP, c0 = (int64_t)(blockIdx.x / a.tiles_r) * CP;
+  const int64_t r0 = (int64_t)(block % a.tiles_r) * CP, c0 = (int64_t)(block / a.tiles_r) * CP;
   const float scale = KIND == PLANE_HALF_2 ? power_of_two(half_exponent(*a.top)) : 1.0f;
   const int c = (tid & 7) * 8, pair = tid >> 3;
   float v[2][8];
@@ -143,6 +148,12 @@ __global__ __launch_bounds__(256) void column_planes_kernel(ColumnArgs a) {
       *reinterpret_cast<uintx4*>(a.t.p[k] + (c0 + col) * a.t.pitch + r0 + 2 * word) = out;
     }
   }
+}
+
+template <typename T, int KIND, bool VEC>
+__global__ __launch_bounds__(256) void column_planes_kernel(ColumnArgs a) {
+  __shared__ uint32_t s_w[plane_count<KIND>()][CP * CP_WORDS];
+  column_planes<T, KIND, VEC>(a, blockIdx.x, s_w);
 }
 
 static bool vectors_fit(const void* src, int64_t ld, int dtype) {
@@ -255,12 +266,70 @@ int launch_top_magnitude(const void* src, int64_t ld, int64_t rows, int64_t cols
   return LQ_OK;
 }
 
-__global__ void zero_words_kernel(uint32_t* p, int count) {
-  if ((int)threadIdx.x < count) p[threadIdx.x] = 0;
+// ------------------------------------------------------------------------------------------------
+enum { JOB_ROWS3, JOB_COLUMNS3, JOB_ROWS_SCALED, JOB_ROWS, JOB_TOPS };
+
+__global__ __launch_bounds__(256) void prepare_kernel(PrepareJobs jobs) {
+  __shared__ uint32_t s_w[3][CP * CP_WORDS];
+  int block = blockIdx.x, j = 0;
+  while (block >= jobs.job[j].wgs) { block -= jobs.job[j].wgs; ++j; }       // the grid has no workgroup beyond the last job's
+  const PrepareJobs::Job& job = jobs.job[j];
+  const RowArgs r{job.s.src, job.s.ld, job.s.rows, job.s.cols, job.t, nullptr, job.row_inv};
+  switch (job.what) {
+    case JOB_ROWS3: row_planes<float, PLANE_BF16_3, false>(r, block, job.wgs); break;
+    case JOB_COLUMNS3:
+      column_planes<float, PLANE_BF16_3, false>(ColumnArgs{job.s.src, job.s.ld, job.s.rows, job.s.cols, job.t, nullptr, nullptr, 0, job.tiles_r},
+                                                (uint32_t)block, s_w);
+      break;
+    case JOB_ROWS_SCALED: row_scaled_planes<true>(r, block); break;
+    case JOB_ROWS: row_planes<__bf16, PLANE_BF16, true>(r, block, job.wgs); break;
+    default: {
+      const float* v = static_cast<const float*>(job.s.src);
+      uint32_t top = 0;
+      for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < job.s.cols; i += (int64_t)TOP_WORDS * 256) top = max(top, finite_magnitude(v[i]));
+#pragma unroll
+      for (int o = 32; o; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+      if ((threadIdx.x & 63) == 0) s_w[0][threadIdx.x >> 6] = top;
+      __syncthreads();
+      if (threadIdx.x == 0) job.tops[block] = max(max(s_w[0][0], s_w[0][1]), max(s_w[0][2], s_w[0][3]));
+    }
+  }
 }
-int launch_zero_words(uint32_t* p, int count, hipStream_t st) {
-  if (count > 64) return LQ_ERR_ARG;
-  hipLaunchKernelGGL(zero_words_kernel, dim3(1), dim3(64), 0, st, p, count);
+
+static int add_job(PrepareJobs& p, int what, int64_t wgs, const PlaneSource& s, const PlaneTarget& t, float* row_inv, uint32_t* tops, int tiles_r) {
+  if (p.count >= 5 || wgs < 1 || wgs >= (1ll << 30)) return LQ_ERR_SHAPE;
+  p.job[p.count++] = PrepareJobs::Job{what, (int)wgs, s, t, row_inv, tops, tiles_r};
+  return LQ_OK;
+}
+int PrepareJobs::rows3(const PlaneSource& s, const PlaneTarget& t) {
+  LQ_TRY(check_target(s, PLANE_BF16_3, t, up_to(s.cols, 64)));
+  return add_job(*this, JOB_ROWS3, std::min<int64_t>((t.rows * ((s.cols + 63) / 64 * 8) + 255) / 256, 1024), s, t, nullptr, nullptr, 0);
+}
+int PrepareJobs::columns3(const PlaneSource& s, const PlaneTarget& t) {
+  LQ_TRY(check_target(s, PLANE_BF16_3, t, up_to(s.rows, CP)));
+  const int64_t tr = (s.rows + CP - 1) / CP;
+  return add_job(*this, JOB_COLUMNS3, tr * ((t.rows + CP - 1) / CP), s, t, nullptr, nullptr, (int)tr);
+}
+int PrepareJobs::rows_scaled(const PlaneSource& s, const PlaneTarget& t, float* row_inv) {
+  LQ_TRY(check_target(s, PLANE_HALF_2, t, up_to(s.cols, 64)));
+  if (!vectors_fit(s.src, s.ld, s.dtype)) return LQ_ERR_ARG;
+  return add_job(*this, JOB_ROWS_SCALED, (s.rows + 3) / 4, s, t, row_inv, nullptr, 0);
+}
+int PrepareJobs::rows(const PlaneSource& s, const PlaneTarget& t) {
+  LQ_TRY(check_target(s, PLANE_BF16, t, up_to(s.cols, 64)));
+  if (s.dtype != LQ_T_BF16 || !vectors_fit(s.src, s.ld, s.dtype)) return LQ_ERR_ARG;
+  return add_job(*this, JOB_ROWS, std::min<int64_t>((t.rows * ((s.cols + 63) / 64 * 8) + 255) / 256, 8192), s, t, nullptr, nullptr, 0);
+}
+int PrepareJobs::tops(const float* v, int64_t n, uint32_t* words) {
+  return add_job(*this, JOB_TOPS, TOP_WORDS, PlaneSource{v, LQ_T_FP32, n, 1, n, nullptr}, PlaneTarget{}, nullptr, words, 0);
+}
+int PrepareJobs::launch(hipStream_t st) const {
+  int64_t wgs = 0;
+  double bytes = 0.0;
+  for (int j = 0; j < count; ++j) { wgs += job[j].wgs; bytes += (double)job[j].s.rows * (double)job[j].s.cols * 8.0; }
+  if (wgs < 1 || wgs >= (1ll << 31)) return LQ_ERR_SHAPE;
+  prof::Scope ps(prof::TRAIN_PLANES, st, bytes);
+  hipLaunchKernelGGL(prepare_kernel, dim3((unsigned)wgs), dim3(256), 0, st, *this);
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }
