@@ -130,7 +130,7 @@ template <int RT, int NB>
 struct ShiftStage {
   typedef ThinStage<RT, NB> Stage;
   const FewDxArgs& a;
-  float to[Stage::LOADS], from[Stage::LOADS];            // of the rows that this thread brings
+  float to[Stage::LOADS], from[2][Stage::LOADS];         // of the rows that this thread brings
   __device__ __forceinline__ static int token(int q) { return ((threadIdx.x + 256 * q) >> 3) % (16 * RT); }
   __device__ __forceinline__ explicit ShiftStage(const FewDxArgs& args) : a(args) {
 #pragma unroll
@@ -139,14 +139,16 @@ struct ShiftStage {
       if (to[q] == -__builtin_inff()) to[q] = 0.0f;
     }
   }
-  __device__ __forceinline__ void load(int step) {
+  template <class P>
+  __device__ __forceinline__ void load(P, int step) {
 #pragma unroll
-    for (int q = 0; q < Stage::LOADS; ++q) from[q] = token(q) < a.n ? a.part_ref[(int64_t)step * a.n + token(q)] : 0.0f;
+    for (int q = 0; q < Stage::LOADS; ++q) from[P::value][q] = token(q) < a.n ? a.part_ref[(int64_t)step * a.n + token(q)] : 0.0f;
   }
-  __device__ __forceinline__ void operator()(Stage& s) {
+  template <class P>
+  __device__ __forceinline__ void operator()(P, Stage& s) {
 #pragma unroll
     for (int q = 0; q < Stage::LOADS; ++q) {
-      const float f = __builtin_amdgcn_exp2f(from[q] - to[q]);
+      const float f = __builtin_amdgcn_exp2f(from[P::value][q] - to[q]);
       bf16x8 v = __builtin_bit_cast(bf16x8, s.r[q]);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = (__bf16)((float)v[j] * f);
@@ -167,38 +169,31 @@ __global__ __launch_bounds__(256) void few_dx_kernel(FewDxArgs a) {
   thin_store(acc, a.part + (size_t)blockIdx.y * (size_t)a.w.K * (16 * RT), c0 + 32 * (threadIdx.x >> 6), a.w.K);
 }
 
-// dX_i = g (1 - p_t) (E W / S - w_t) from the ranges' parts, 64 features x 16 tokens a workgroup, turned in LDS.
+// dX_i = g (1 - p_t) (E W / S - w_t) from the ranges' parts: 16 features x 16 tokens a workgroup, turned in LDS.
 struct FewSumArgs {
   const float* part; int splits, tokens; int64_t n, d, vocab;
   LossRows r; const int64_t* targets; const float* factors; int64_t ldw;
 };
 template <typename T>
 __global__ __launch_bounds__(256) void few_dx_sum_kernel(FewSumArgs a, const T* __restrict__ W, T* __restrict__ dX) {
-  __shared__ float s_t[64][17];
-  const int c = threadIdx.x & 15, r0 = threadIdx.x >> 4;
+  __shared__ float s_t[16][17];
+  const int c = threadIdx.x & 15, r = threadIdx.x >> 4;
   const size_t stride = (size_t)a.d * a.tokens;
-  float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-  for (int s = 0; s < a.splits; ++s)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int64_t row = (int64_t)blockIdx.x * 64 + r0 + 16 * q;
-      if (row < a.d) v[q] += a.part[s * stride + row * a.tokens + blockIdx.y * 16 + c];
-    }
-#pragma unroll
-  for (int q = 0; q < 4; ++q) s_t[r0 + 16 * q][c] = v[q];
-  __syncthreads();
-  const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int k = (threadIdx.x >> 6) + 4 * q;
-    const int64_t token = (int64_t)blockIdx.y * 16 + k;
-    if (token >= a.n || col >= a.d) continue;
-    const int64_t t = a.targets[token];
-    const bool counts = t >= 0 && t < a.vocab;
-    const float s = a.r.sum[token], inv = s == 0.0f ? 0.0f : 1.0f / s;       // no other class: the sums are zero
-    dX[token * a.d + col] = counts ? (T)(a.r.wrong[token] * a.factors[0] * (s_t[threadIdx.x & 63][k] * inv - (float)W[t * a.ldw + col])) : (T)0.0f;
+  const int64_t row = (int64_t)blockIdx.x * 16 + r;
+  float v = 0.0f;
+  if (row < a.d) {
+    const float* from = a.part + row * a.tokens + blockIdx.y * 16 + c;
+#pragma unroll 16
+    for (int s = 0; s < a.splits; ++s) v += from[s * stride];
   }
+  s_t[r][c] = v;
+  __syncthreads();
+  const int64_t col = (int64_t)blockIdx.x * 16 + c, token = (int64_t)blockIdx.y * 16 + r;
+  if (token >= a.n || col >= a.d) return;
+  const int64_t t = a.targets[token];
+  const bool counts = t >= 0 && t < a.vocab;
+  const float s = a.r.sum[token], inv = s == 0.0f ? 0.0f : 1.0f / s;         // no other class: the sums are zero
+  dX[token * a.d + col] = counts ? (T)(a.r.wrong[token] * a.factors[0] * (s_t[c][r] * inv - (float)W[t * a.ldw + col])) : (T)0.0f;
 }
 
 int few_dx_splits(int64_t vocab, int64_t d) {
@@ -240,7 +235,7 @@ int launch_few_dx(const void* W, int64_t ldw, int dtype, int64_t d, const Planes
     LQ_TRY(dtype == LQ_T_BF16 ? few_dx_of<__bf16>(a, vec, grid, st) : few_dx_of<float>(a, vec, grid, st));
   }
   const FewSumArgs s{part, a.splits, (int)few_rows(p.n), p.n, d, p.vocab, r, p.targets, factors, ldw};
-  const dim3 sums((unsigned)((d + 63) / 64), (unsigned)((p.n + 15) / 16));
+  const dim3 sums((unsigned)((d + 15) / 16), (unsigned)((p.n + 15) / 16));
   prof::Scope ps(prof::LOSS_ROWS, st, (double)p.n * d * (4.0 * a.splits + type_bytes(dtype)));
   if (dtype == LQ_T_BF16)
     hipLaunchKernelGGL(few_dx_sum_kernel<__bf16>, sums, dim3(256), 0, st, s, static_cast<const __bf16*>(W), static_cast<__bf16*>(dX));

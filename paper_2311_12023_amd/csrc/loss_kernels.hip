@@ -20,18 +20,9 @@ namespace lq {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
-__global__ __launch_bounds__(256) void loss_begin_kernel(LossRows r, int64_t n, uint32_t* tops) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i < 2) tops[i] = 0;
-  if (i >= n) return;
-  r.ref[i] = -__builtin_inff();
-  r.sum[i] = 0.0f;
-  r.target[i] = 0.0f;
-}
-
-int launch_loss_begin(const LossRows& r, int64_t n, uint32_t* tops, hipStream_t st) {
-  prof::Scope ps(prof::LOSS_ROWS, st, (double)n * 12.0);
-  hipLaunchKernelGGL(loss_begin_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, r, n, tops);
+__global__ void zero_words_kernel(uint32_t* p) { p[threadIdx.x] = 0; }
+int launch_zero_words(uint32_t* p, int count, hipStream_t st) {
+  hipLaunchKernelGGL(zero_words_kernel, dim3(1), dim3(count), 0, st, p);
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }
@@ -41,7 +32,7 @@ __device__ __forceinline__ float logit_factor(const LossScales& s, int64_t token
   return s.x_inv ? LOG2E * s.x_inv[token] * power_of_two(-half_exponent(*s.w_top)) : LOG2E;
 }
 
-// Four neighbouring classes of one token as planes.
+// Four neighbours as planes (bf16: lo may be NULL).
 template <bool HALF>
 __device__ __forceinline__ void store_four(uint16_t* hi, uint16_t* lo, floatx4 v) {
   if constexpr (HALF) {
@@ -51,14 +42,17 @@ __device__ __forceinline__ void store_four(uint16_t* hi, uint16_t* lo, floatx4 v
     *reinterpret_cast<halfx4*>(hi) = h;
     *reinterpret_cast<halfx4*>(lo) = l;
   } else {
-    *reinterpret_cast<bf16x4*>(hi) = __builtin_convertvector(v, bf16x4);
+    const bf16x4 h = __builtin_convertvector(v, bf16x4);
+    *reinterpret_cast<bf16x4*>(hi) = h;
+    if (lo) *reinterpret_cast<bf16x4*>(lo) = __builtin_convertvector(v - __builtin_convertvector(h, floatx4), bf16x4);
   }
 }
 
 // ------------------------------------------------------------------------------------------------
 // Logits of a piece.  Classes are the tile's rows and tokens its columns: a lane then holds 32 classes of each of its tokens, and
 // the maximum and the sum over the tile are reductions inside lanes, two exchanges between lanes and one through LDS between two
-// wavefronts.  E is rounded to bf16, 2^-9 of each term of a sum that ends up in the type of X; two fp16 planes where that is fp32.
+// wavefronts.  E is rounded to bf16, 2^-8 of each term of a sum that ends up in the type of X; two fp16 planes where that is fp32.
+// What the rounding left out is kept beside it where dW comes from E.
 struct LogitsArgs {
   SegArgs g;
   LossPiece p; LossScales s;
@@ -106,14 +100,16 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void loss_logits_kernel(LogitsArgs 
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
     s_max[t.wm * SEG_T + col] = top;
-    base[j] = live ? a.ref[token] : 0.0f;
+    base[j] = !live ? 0.0f : a.p.v0 == 0 ? -__builtin_inff() : a.ref[token];
   }
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int col = 64 * t.wn + 16 * j + t.l16;
     const int64_t token = (int64_t)t.tn * SEG_T + col;
-    const float ref = fmaxf(base[j], ceilf(fmaxf(s_max[col], s_max[SEG_T + col])));
+    // the row's reference so far serves while E stays inside its type: no tile then has to be brought to another
+    const float top = ceilf(fmaxf(s_max[col], s_max[SEG_T + col])), room = HALF ? (float)LOSS_E_ROOM : 64.0f;
+    const float ref = top <= base[j] + room ? base[j] : top;
     base[j] = ref;
     // nothing but the target so far: any reference will do
     const float from = (ref == -__builtin_inff() ? 0.0f : ref) - (HALF ? (float)LOSS_E_SHIFT : 0.0f);
@@ -131,7 +127,7 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void loss_logits_kernel(LogitsArgs 
     if (a.e[0] && token < a.p.n) {
       const int64_t at = token * a.e_pitch + class0 + 4 * t.kg;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) store_four<HALF>(a.e[0] + at + 16 * i, HALF ? a.e[1] + at + 16 * i : nullptr, acc[i][j]);
+      for (int i = 0; i < 8; ++i) store_four<HALF>(a.e[0] + at + 16 * i, HALF || a.e[1] ? a.e[1] + at + 16 * i : nullptr, acc[i][j]);
     }
   }
   __syncthreads();
@@ -175,8 +171,66 @@ int launch_loss_logits(const Planes& w, const Planes& x, int64_t depth, const Lo
 }
 
 // ------------------------------------------------------------------------------------------------
+// What becomes of the rows when all classes have been seen, and their total in 64 bits and a fixed order.  Called by all threads of
+// one workgroup of 1024.
+struct RowsArgs {
+  LossRows r; LossScales s;
+  const int64_t* targets; int64_t n, vocab; int mean;
+  float* loss; float* row_loss; float* lse; float* factors;
+};
+__device__ __forceinline__ void finish_rows(const RowsArgs& a) {
+  __shared__ double s_sum[1024];
+  __shared__ uint32_t s_count[1024];
+  double sum = 0.0;
+  uint32_t count = 0;
+  for (int64_t i = threadIdx.x; i < a.n; i += 1024) {
+    const int64_t t = a.targets[i];
+    const float others = a.r.ref[i] + log2f(a.r.sum[i]);      // log2 of the sum without the target; -inf: there is no other class
+    float l = 0.0f, wrong = 0.0f, all = others;
+    if (t >= 0 && t < a.vocab) {
+      const float z = a.r.target[i] - others;
+      l = fmaxf(-z, 0.0f) * LN2 + log1pf(exp2f(-fabsf(z)));
+      wrong = 1.0f / (1.0f + exp2f(z));
+      all = fmaxf(a.r.target[i], others) + log1pf(exp2f(-fabsf(z))) * LOG2E;
+      if (z != z) l = all = z;
+      sum += l;
+      ++count;
+    }
+    a.row_loss[i] = l;
+    if (a.lse) a.lse[i] = all * LN2;
+    a.r.wrong[i] = wrong;
+    a.r.lse2[i] = all;
+  }
+  s_sum[threadIdx.x] = sum;
+  s_count[threadIdx.x] = count;
+  __syncthreads();
+  for (int o = 512; o; o >>= 1) {
+    if ((int)threadIdx.x < o) { s_sum[threadIdx.x] += s_sum[threadIdx.x + o]; s_count[threadIdx.x] += s_count[threadIdx.x + o]; }
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) {
+    const double f = a.mean ? 1.0 / (double)(s_count[0] ? s_count[0] : 1) : 1.0;      // no row counts: the mean is 0
+    *a.loss = (float)(s_sum[0] * f);
+    a.factors[0] = (float)f;
+    a.factors[1] = a.s.xt_top ? (float)f * power_of_two(-LOSS_G_SHIFT) * power_of_two(-half_exponent(*a.s.xt_top)) : (float)f;
+  }
+}
+
+__global__ __launch_bounds__(1024) void loss_rows_kernel(RowsArgs a) { finish_rows(a); }
+
+int launch_loss_rows(const LossRows& r, const LossScales& s, const int64_t* targets, int64_t n, int64_t vocab, bool mean, float* loss,
+                     float* row_loss, float* lse, float* factors, hipStream_t st) {
+  const RowsArgs a{r, s, targets, n, vocab, (int)mean, loss, row_loss, lse, factors};
+  prof::Scope ps(prof::LOSS_ROWS, st, (double)n * 36.0);
+  hipLaunchKernelGGL(loss_rows_kernel, dim3(1), dim3(1024), 0, st, a);
+  LQ_HIP_TRY(hipGetLastError());
+  return LQ_OK;
+}
+
+// ------------------------------------------------------------------------------------------------
 // A wavefront joins the tiles' sums of one row.  Tiles whose E lies at a smaller power of two than the row's new one are
-// multiplied down, which is exact (what leaves the range of bf16 is below 2^-126 of the largest term, that of fp16 below 2^-38).
+// multiplied down, which is exact (what leaves the range of bf16 is below 2^-126 of the largest term, that of fp16 below 2^-37).
+// In the first piece that is all of them, and a launch of its own does it; later it is a row whose logits outgrow its reference.
 struct JoinArgs {
   LossPiece p; LossRows r;
   const float* part_ref; const float* part_sum; int tiles;
@@ -193,28 +247,28 @@ __device__ __forceinline__ void scale_run(uint16_t* at, float f) {
 }
 
 template <typename H>
-__global__ __launch_bounds__(256) void loss_join_kernel(JoinArgs a) {
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (row >= a.p.n) return;
-  const float old = a.r.ref[row];
+__device__ __forceinline__ void join_row(const JoinArgs& a, int64_t row, int lane) {
+  const bool first = a.p.v0 == 0;
+  const float old = first ? -__builtin_inff() : a.r.ref[row];
   float ref = old;
+#pragma unroll 4
   for (int t = lane; t < a.tiles; t += 64) ref = fmaxf(ref, a.part_ref[(int64_t)t * a.p.n + row]);
 #pragma unroll
   for (int o = 32; o; o >>= 1) ref = fmaxf(ref, __shfl_xor(ref, o));
   const float from = ref == -__builtin_inff() ? 0.0f : ref;
   float sum = 0.0f;
+#pragma unroll 4
   for (int t = lane; t < a.tiles; t += 64)
     sum += a.part_sum[(int64_t)t * a.p.n + row] * __builtin_amdgcn_exp2f(a.part_ref[(int64_t)t * a.p.n + row] - from);
 #pragma unroll
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
   if (lane == 0) {
     const float shift = __builtin_amdgcn_exp2f(old - from);
-    a.r.sum[row] = a.r.sum[row] * shift + sum;
+    a.r.sum[row] = first ? sum : a.r.sum[row] * shift + sum;
     a.r.shift[row] = shift;
     a.r.ref[row] = ref;
   }
-  if (!a.e[0]) return;
+  if (!a.e[0] || first) return;
   for (int t0 = 0; t0 < a.tiles; t0 += 64) {
     const float mine = t0 + lane < a.tiles ? a.part_ref[(int64_t)(t0 + lane) * a.p.n + row] : ref;
     const float f = __builtin_amdgcn_exp2f(mine - from);
@@ -223,8 +277,39 @@ __global__ __launch_bounds__(256) void loss_join_kernel(JoinArgs a) {
       const float ft = __shfl(f, t);
       const int64_t at = row * a.e_pitch + (int64_t)(t0 + t) * SEG_T + 4 * lane;
       scale_run<H>(a.e[0] + at, ft);
-      if constexpr (!std::is_same<H, __bf16>::value) scale_run<H>(a.e[1] + at, ft);
+      if (a.e[1]) scale_run<H>(a.e[1] + at, ft);
     }
+  }
+}
+
+template <typename H>
+__global__ __launch_bounds__(256) void loss_join_kernel(JoinArgs a) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row < a.p.n) join_row<H>(a, row, threadIdx.x & 63);
+}
+
+// Up to 16 rows, whole vocabulary: one workgroup joins and finishes them.
+__global__ __launch_bounds__(1024) void loss_join_rows_kernel(JoinArgs a, RowsArgs rows) {
+  const int64_t row = threadIdx.x >> 6;
+  if (row < a.p.n) join_row<__bf16>(a, row, threadIdx.x & 63);
+  __threadfence_block();
+  __syncthreads();
+  finish_rows(rows);
+}
+
+// 256 classes x 16 tokens a workgroup.
+template <typename H>
+__global__ __launch_bounds__(256) void loss_shift_kernel(JoinArgs a) {
+  const int64_t token = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  if (token >= a.p.n) return;
+  const float ref = a.r.ref[token], mine = a.part_ref[(int64_t)blockIdx.y * a.p.n + token];
+  if (mine == ref) return;
+  const float f = __builtin_amdgcn_exp2f(mine - ref);
+  const int64_t at = token * a.e_pitch + (int64_t)blockIdx.y * SEG_T + 4 * (threadIdx.x & 15);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    scale_run<H>(a.e[0] + at + 64 * q, f);
+    if (a.e[1]) scale_run<H>(a.e[1] + at + 64 * q, f);
   }
 }
 
@@ -234,6 +319,22 @@ int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, const flo
   prof::Scope ps(prof::LOSS_ROWS, st, (double)p.n * a.tiles * 8.0);
   auto kernel = half ? loss_join_kernel<_Float16> : loss_join_kernel<__bf16>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)((p.n + 3) / 4)), dim3(256), 0, st, a);
+  LQ_HIP_TRY(hipGetLastError());
+  if (!e[0] || p.v0 != 0) return LQ_OK;
+  if (a.tiles > 65535) return LQ_ERR_SHAPE;
+  auto shift = half ? loss_shift_kernel<_Float16> : loss_shift_kernel<__bf16>;
+  hipLaunchKernelGGL(shift, dim3((unsigned)((p.n + 15) / 16), (unsigned)a.tiles), dim3(256), 0, st, a);
+  LQ_HIP_TRY(hipGetLastError());
+  return LQ_OK;
+}
+
+int launch_loss_join_rows(const LossPiece& p, const LossRows& r, const float* part_ref, const float* part_sum, int tile, bool mean,
+                          float* loss, float* row_loss, float* lse, float* factors, hipStream_t st) {
+  if (p.n > 16 || p.v0 != 0 || p.classes != p.vocab) return LQ_ERR_SHAPE;
+  const JoinArgs a{p, r, part_ref, part_sum, (int)((p.classes + tile - 1) / tile), {nullptr, nullptr}, 0};
+  const RowsArgs rows{r, LossScales{}, p.targets, p.n, p.vocab, (int)mean, loss, row_loss, lse, factors};
+  prof::Scope ps(prof::LOSS_ROWS, st, (double)p.n * a.tiles * 8.0);
+  hipLaunchKernelGGL(loss_join_rows_kernel, dim3(1), dim3(1024), 0, st, a, rows);
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }
@@ -316,80 +417,47 @@ int launch_loss_accumulate(const Planes& e, const Planes& wt, int64_t depth, int
   return LQ_OK;
 }
 
-// ------------------------------------------------------------------------------------------------
-// One workgroup finishes the rows: a few bytes each, and the total is added up in 64 bits in a fixed order.
-__global__ __launch_bounds__(1024) void loss_rows_kernel(LossRows r, LossScales sc, const int64_t* __restrict__ targets, int64_t n, int64_t vocab,
-                                                         int mean, float* loss, float* row_loss, float* lse, float* factors) {
-  __shared__ double s_sum[1024];
-  __shared__ unsigned long long s_count[1024];
-  double sum = 0.0;
-  unsigned long long count = 0;
-  for (int64_t i = threadIdx.x; i < n; i += 1024) {
-    const bool counts = targets[i] >= 0 && targets[i] < vocab;
-    const float others = r.ref[i] + log2f(r.sum[i]);        // log2 of the sum without the target; -inf: there is no other class
-    float l = 0.0f, wrong = 0.0f, all = others;
-    if (counts) {
-      const float z = r.target[i] - others;
-      l = fmaxf(-z, 0.0f) * LN2 + log1pf(exp2f(-fabsf(z)));
-      if (z != z) l = z;
-      wrong = 1.0f / (1.0f + exp2f(z));
-      all = fmaxf(r.target[i], others) + log1pf(exp2f(-fabsf(z))) * LOG2E;
-      if (z != z) all = z;
-      sum += l;
-      ++count;
-    }
-    row_loss[i] = l;
-    if (lse) lse[i] = all * LN2;
-    r.wrong[i] = wrong;
-    r.lse2[i] = all;
-  }
-  s_sum[threadIdx.x] = sum;
-  s_count[threadIdx.x] = count;
-  __syncthreads();
-  for (int o = 512; o; o >>= 1) {
-    if ((int)threadIdx.x < o) { s_sum[threadIdx.x] += s_sum[threadIdx.x + o]; s_count[threadIdx.x] += s_count[threadIdx.x + o]; }
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) {
-    const double f = mean ? 1.0 / (double)(s_count[0] ? s_count[0] : 1) : 1.0;      // no row counts: the mean is 0
-    *loss = (float)(s_sum[0] * f);
-    factors[0] = (float)f;
-    factors[1] = sc.xt_top ? (float)f * power_of_two(-LOSS_E_SHIFT) * power_of_two(-half_exponent(*sc.xt_top)) : (float)f;
-  }
-}
-
-int launch_loss_rows(const LossRows& r, const LossScales& s, const int64_t* targets, int64_t n, int64_t vocab, bool mean, float* loss,
-                     float* row_loss, float* lse, float* factors, hipStream_t st) {
-  prof::Scope ps(prof::LOSS_ROWS, st, (double)n * 36.0);
-  hipLaunchKernelGGL(loss_rows_kernel, dim3(1), dim3(1024), 0, st, r, s, targets, n, vocab, (int)mean, loss, row_loss, lse, factors);
-  LQ_HIP_TRY(hipGetLastError());
-  return LQ_OK;
-}
-
-// dX_i = g (1 - p_t) (E W / S - w_t): one workgroup per row, its features in turn.
-template <typename T>
-__global__ __launch_bounds__(256) void loss_dx_kernel(LossRows r, LossScales sc, const int64_t* __restrict__ targets, int64_t d, int64_t vocab,
-                                                      const float* __restrict__ acc, const T* __restrict__ W, int64_t ldw,
-                                                      const float* __restrict__ factor, T* __restrict__ dX) {
+// dX_i = g (1 - p_t) (E W / S - w_t): one workgroup per row, its features in turn; VEC: four at a time.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void loss_dx_kernel(LossRows r, LossScales sc, const int64_t* __restrict__ targets, int64_t d,
+                                                      int64_t vocab, const float* __restrict__ acc, const T* __restrict__ W,
+                                                      int64_t ldw, const float* __restrict__ factor, T* __restrict__ dX) {
+  typedef T vec4 __attribute__((ext_vector_type(4)));
   const int64_t row = blockIdx.x, t = targets[row];
   const bool counts = t >= 0 && t < vocab;
   const float s = r.sum[row];
   float inv = s == 0.0f ? 0.0f : 1.0f / s;                   // no other class: acc is zero
   if (sc.w_top) inv *= power_of_two(-LOSS_E_SHIFT) * power_of_two(-half_exponent(*sc.w_top));
   const float g = counts ? r.wrong[row] * *factor : 0.0f;
-  for (int64_t c = threadIdx.x; c < d; c += 256)
-    dX[row * d + c] = counts ? (T)(g * (acc[row * d + c] * inv - (float)W[t * ldw + c])) : (T)0.0f;
+  if constexpr (VEC) {
+    for (int64_t c = 4 * threadIdx.x; c < d; c += 1024) {
+      vec4 out = {};
+      if (counts) {
+        const floatx4 w = __builtin_convertvector(*reinterpret_cast<const vec4*>(W + t * ldw + c), floatx4);
+        out = __builtin_convertvector(g * (*reinterpret_cast<const floatx4*>(acc + row * d + c) * inv - w), vec4);
+      }
+      *reinterpret_cast<vec4*>(dX + row * d + c) = out;
+    }
+  } else {
+    for (int64_t c = threadIdx.x; c < d; c += 256)
+      dX[row * d + c] = counts ? (T)(g * (acc[row * d + c] * inv - (float)W[t * ldw + c])) : (T)0.0f;
+  }
+}
+
+template <typename T>
+static void dx_of(const LossRows& r, const LossScales& s, const int64_t* targets, int64_t n, int64_t d, int64_t vocab, const float* acc,
+                  const void* W, int64_t ldw, const float* factor, void* dX, hipStream_t st) {
+  const bool vec = d % 4 == 0 && ldw % 4 == 0 && (((uintptr_t)W | (uintptr_t)dX) & (4 * sizeof(T) - 1)) == 0;
+  auto kernel = vec ? loss_dx_kernel<T, true> : loss_dx_kernel<T, false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(256), 0, st, r, s, targets, d, vocab, acc, static_cast<const T*>(W), ldw, factor,
+                     static_cast<T*>(dX));
 }
 
 int launch_loss_dx(const LossRows& r, const LossScales& s, const int64_t* targets, int64_t n, int64_t d, int64_t vocab,
                    const float* acc, const void* W, int64_t ldw, int dtype, const float* factor, void* dX, hipStream_t st) {
   prof::Scope ps(prof::LOSS_ROWS, st, (double)n * d * (4.0 + 2.0 * type_bytes(dtype)));
-  if (dtype == LQ_T_BF16)
-    hipLaunchKernelGGL(loss_dx_kernel<__bf16>, dim3((unsigned)n), dim3(256), 0, st, r, s, targets, d, vocab, acc,
-                       static_cast<const __bf16*>(W), ldw, factor, static_cast<__bf16*>(dX));
-  else
-    hipLaunchKernelGGL(loss_dx_kernel<float>, dim3((unsigned)n), dim3(256), 0, st, r, s, targets, d, vocab, acc,
-                       static_cast<const float*>(W), ldw, factor, static_cast<float*>(dX));
+  if (dtype == LQ_T_BF16) dx_of<__bf16>(r, s, targets, n, d, vocab, acc, W, ldw, factor, dX, st);
+  else dx_of<float>(r, s, targets, n, d, vocab, acc, W, ldw, factor, dX, st);
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }
@@ -417,7 +485,7 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void loss_gradient_kernel(GradientA
   float* s_f = reinterpret_cast<float*>(seg_lds);
   float *s_lse = s_f + SEG_T, *s_wrong = s_lse + SEG_T;
   int* s_at = reinterpret_cast<int*>(s_wrong + SEG_T);
-  const float unit = HALF ? power_of_two(LOSS_E_SHIFT) : 1.0f;
+  const float unit = HALF ? power_of_two(LOSS_G_SHIFT) : 1.0f;
   if (threadIdx.x < SEG_T) {
     const int64_t token = (int64_t)t.tm * SEG_T + threadIdx.x;
     const int64_t target = token < a.p.n ? a.p.targets[token] : -1;
@@ -462,6 +530,75 @@ int launch_loss_gradient(const Planes& w, const Planes& x, int64_t depth, const 
   static LdsLimit limit[2];
   prof::Scope ps(prof::LOSS_LOGITS, st, 2.0 * p.n * p.classes * depth);
   return s.x_inv ? launch_tiles(loss_gradient_kernel<_Float16>, limit[0], a, st) : launch_tiles(loss_gradient_kernel<__bf16>, limit[1], a, st);
+}
+
+// ------------------------------------------------------------------------------------------------
+// The same from E (both planes), where one piece is the whole vocabulary: p = E (1 - p_t) / S, a pass over E for a product less
+// (2047 x 32000, d = 4096).  A workgroup turns 64 tokens x 64 classes in LDS, a thread two tokens of eight classes.
+struct FromEArgs {
+  LossPiece p; LossRows r;
+  const uint16_t* e[2]; int64_t e_pitch;
+  uint16_t* out[2]; int64_t pitch;
+  int tiles_r;
+};
+template <typename H>
+__global__ __launch_bounds__(256) void loss_gradient_from_e_kernel(FromEArgs a) {
+  constexpr bool HALF = !std::is_same<H, __bf16>::value;
+  constexpr int WORDS = 33;
+  typedef H hx8 __attribute__((ext_vector_type(8)));
+  typedef H hx2 __attribute__((ext_vector_type(2)));
+  __shared__ uint32_t s_w[HALF ? 2 : 1][64 * WORDS];
+  const int c = (threadIdx.x & 7) * 8, pair = threadIdx.x >> 3;
+  const int64_t r0 = (int64_t)(blockIdx.x % a.tiles_r) * 64, c0 = (int64_t)(blockIdx.x / a.tiles_r) * 64;
+  float g[2][8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) g[h][j] = 0.0f;
+    const int64_t token = r0 + 2 * pair + h, t = token < a.p.n ? a.p.targets[token] : -1;
+    if (t < 0 || t >= a.p.vocab) continue;                   // rows that do not count: whatever they hold
+    const float s = a.r.sum[token], wrong = a.r.wrong[token];
+    const float f = s == 0.0f ? 0.0f : wrong / s * (HALF ? power_of_two(LOSS_G_SHIFT - LOSS_E_SHIFT) : 1.0f);
+    const int64_t at = token * a.e_pitch + c0 + c;           // rows of E end on whole tiles
+    const hx8 hi = *reinterpret_cast<const hx8*>(a.e[0] + at);
+    const hx8 lo = *reinterpret_cast<const hx8*>(a.e[1] + at);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      g[h][j] = ((float)hi[j] + (float)lo[j]) * f;
+      if (c0 + c + j == t) g[h][j] = -wrong * (HALF ? power_of_two(LOSS_G_SHIFT) : 1.0f);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const hx2 hi = {(H)g[0][j], (H)g[1][j]};
+    s_w[0][(c + j) * WORDS + pair] = __builtin_bit_cast(uint32_t, hi);
+    if constexpr (HALF) s_w[HALF ? 1 : 0][(c + j) * WORDS + pair] = __builtin_bit_cast(uint32_t, hx2{(H)(g[0][j] - (float)hi[0]), (H)(g[1][j] - (float)hi[1])});
+  }
+  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int col = (threadIdx.x >> 3) + 32 * h, word = (threadIdx.x & 7) * 4;
+    if (c0 + col >= a.p.classes) continue;
+#pragma unroll
+    for (int k = 0; k < (HALF ? 2 : 1); ++k) {
+      uintx4 out;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) out[j] = s_w[k][col * WORDS + word + j];
+      *reinterpret_cast<uintx4*>(a.out[k] + (c0 + col) * a.pitch + r0 + 2 * word) = out;
+    }
+  }
+}
+
+int launch_loss_gradient_from_e(const LossPiece& p, const LossRows& r, bool half, uint16_t* const e[2], int64_t e_pitch,
+                                uint16_t* const g[2], int64_t g_pitch, hipStream_t st) {
+  const int64_t tr = (p.n + 63) / 64, tc = (p.classes + 63) / 64;
+  if (p.v0 != 0 || p.classes != p.vocab || g_pitch < up_to(p.n, 64) || tr * tc >= (1ll << 31)) return LQ_ERR_SHAPE;
+  const FromEArgs a{p, r, {e[0], e[1]}, e_pitch, {g[0], g[1]}, g_pitch, (int)tr};
+  prof::Scope ps(prof::TRAIN_PLANES, st, (double)p.n * p.classes * (half ? 8.0 : 6.0));
+  auto kernel = half ? loss_gradient_from_e_kernel<_Float16> : loss_gradient_from_e_kernel<__bf16>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(tr * tc)), dim3(256), 0, st, a);
+  LQ_HIP_TRY(hipGetLastError());
+  return LQ_OK;
 }
 
 // ------------------------------------------------------------------------------------------------

@@ -39,21 +39,21 @@ static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)
 // Byte offsets inside a tile of 256 rows are 32 bits wide: rows of a plane are at most this far apart.
 constexpr int64_t MOST_PITCH = (int64_t)1 << 23;
 
-// Classes per piece: E of a piece stays within 64 MiB per plane, so that it is still in the memory-side cache when the next
-// product reads it; pieces of equal size, whole tiles.
+// Classes per piece: E of a piece stays within 2^26 values (128 MiB per plane); pieces of equal size, whole tiles.
 static int64_t piece_classes(int64_t n, int64_t vocab) {
-  const int64_t most = std::min(std::max<int64_t>(SEG_T, ((int64_t)1 << 25) / n / SEG_T * SEG_T), MOST_PITCH / 2);
+  const int64_t most = std::min(std::max<int64_t>(SEG_T, ((int64_t)1 << 26) / n / SEG_T * SEG_T), MOST_PITCH / 2);
   const int64_t pieces = (vocab + most - 1) / most;
   return up_to((vocab + pieces - 1) / pieces, SEG_T);
 }
 
-static bool few_by_size(int64_t n, int64_t vocab) { return n <= LOSS_FEW && vocab <= MOST_PITCH / 2; }
+static bool few_by_size(int64_t n, int64_t vocab, bool want_dw) { return n <= LOSS_FEW && vocab <= MOST_PITCH / 2 && !want_dw; }
 
 struct LossPlan {
   LossRows rows;
   float *factors, *part_ref, *part_sum, *acc, *part, *x_inv;
   uint32_t* tops;                                    // of W, of the rows of X that count
-  uint16_t *x[2], *xt[2], *w[2], *wt[2], *e[2];
+  uint16_t *x[2], *xt[2], *w[2], *wt[2], *e[2], *g[2];
+  bool whole;                                        // one piece is the whole vocabulary
   uint16_t *few_x[3], *few_e[3];                     // the few rows' planes
   float* few_part;
   int64_t classes, d64, n64, v64;
@@ -64,13 +64,14 @@ static LossPlan plan_loss(void* ws, int64_t n, int64_t d, int64_t vocab, int dty
   Arena a(ws);
   const bool half = dtype == LQ_T_FP32;
   p.classes = piece_classes(n, vocab);
+  p.whole = p.classes >= vocab;
   p.d64 = up_to(d, 64);
   p.n64 = up_to(n, 64);
   for (float** row : {&p.rows.ref, &p.rows.sum, &p.rows.shift, &p.rows.target, &p.rows.wrong, &p.rows.lse2}) *row = a.take<float>(n);
   p.factors = a.take<float>(2);
   p.tops = a.take<uint32_t>(2);
   p.x_inv = a.take<float>(half ? n : 0);
-  const bool few = few_by_size(n, vocab);
+  const bool few = few_by_size(n, vocab, want_dw);
   p.v64 = up_to(vocab, 64);
   const int64_t tiles = std::max(p.classes / SEG_T, few ? p.v64 / LOSS_FEW_TILE : 0);
   for (int h = 0; h < (half ? 3 : 1); ++h) {
@@ -80,13 +81,14 @@ static LossPlan plan_loss(void* ws, int64_t n, int64_t d, int64_t vocab, int dty
   p.few_part = a.take<float>(few && want_dx ? (size_t)few_dx_splits(vocab, d) * d * few_rows(n) : 0);
   p.part_ref = a.take<float>(tiles * n);
   p.part_sum = a.take<float>(tiles * n);
+  p.e[1] = a.take<uint16_t>(!half && want_dw && p.whole ? n * p.classes : 0);      // dW comes from E then
   for (int h = 0; h < (half ? 2 : 1); ++h) {
     p.x[h] = a.take<uint16_t>(n * p.d64);
     p.w[h] = a.take<uint16_t>(p.classes * p.d64);
     p.xt[h] = a.take<uint16_t>(want_dw ? d * p.n64 : 0);
     p.wt[h] = a.take<uint16_t>(want_dx ? d * p.classes : 0);
-    // E of a piece, and in the second pass its gradient
-    p.e[h] = a.take<uint16_t>(std::max(want_dx ? n * p.classes : 0, want_dw ? p.classes * p.n64 : 0));
+    p.e[h] = a.take<uint16_t>(want_dx || (want_dw && p.whole) ? n * p.classes : 0);
+    p.g[h] = a.take<uint16_t>(want_dw ? p.classes * p.n64 : 0);
   }
   p.acc = a.take<float>(want_dx ? n * d : 0);
   // The last piece may be shorter and be cut into other numbers of ranges: tiles times ranges stay within 256 in any case.
@@ -236,17 +238,16 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
   const LossScales scales{half ? p.x_inv : nullptr, half ? p.tops : nullptr, half && dW ? p.tops + 1 : nullptr};
   // bf16 operands whose rows are whole pairs of steps on 16-byte addresses are read where they are
   auto in_place = [&](const void* a, int64_t ld) { return !half && d % 64 == 0 && ld % 8 == 0 && ld <= MOST_PITCH && !misaligned(a, 16); };
-  LQ_TRY(launch_loss_begin(p.rows, n, p.tops, st));
+  if (half) LQ_TRY(launch_zero_words(p.tops, 2, st));
   const char* w0 = static_cast<const char*>(W);
-  const bool few = few_by_size(n, vocab);
-  const bool planes = !few || dW;                             // the large products' operands
+  const bool few = few_by_size(n, vocab, dW != nullptr);
   Planes x{{static_cast<const uint16_t*>(X), nullptr, nullptr}, ldx};
-  if (planes && !in_place(X, ldx)) {
+  if (!few && !in_place(X, ldx)) {
     const PlaneTarget t{{p.x[0], p.x[1], nullptr}, p.d64, n};
     LQ_TRY(launch_row_planes({X, dtype, ldx, n, d, nullptr}, kind, t, half ? p.x_inv : nullptr, st));
     x = planes_of(t);
   }
-  if (planes && half) LQ_TRY(launch_top_magnitude(W, ldw, vocab, d, nullptr, 0, p.tops, st));
+  if (!few && half) LQ_TRY(launch_top_magnitude(W, ldw, vocab, d, nullptr, 0, p.tops, st));
   const bool w_in_place = in_place(W, ldw);
   auto piece_source = [&](int64_t v0, int64_t classes) {
     return PlaneSource{w0 + (size_t)v0 * (size_t)ldw * size, dtype, ldw, classes, d, p.tops};
@@ -260,29 +261,34 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
     return launch_row_planes(from, kind, t, nullptr, st);
   };
   const LossPiece all{n, 0, vocab, vocab, targets};
+  const bool join_rows = few && n <= 16;
   if (few) {
     const PlaneTarget t{{p.few_x[0], p.few_x[1], p.few_x[2]}, p.d64, few_rows(n)};
     uint16_t* const e[3] = {dX ? p.few_e[0] : nullptr, dX ? p.few_e[1] : nullptr, dX ? p.few_e[2] : nullptr};
     uint16_t* const none[2] = {nullptr, nullptr};
     LQ_TRY(launch_row_planes({X, dtype, ldx, n, d, nullptr}, half ? PLANE_BF16_3 : PLANE_BF16, t, nullptr, st));
     LQ_TRY(launch_few_logits(W, ldw, dtype, d, planes_of(t), all, p.rows, p.part_ref, p.part_sum, e, p.v64, st));
-    LQ_TRY(launch_loss_join(all, p.rows, half, p.part_ref, p.part_sum, LOSS_FEW_TILE, none, 0, st));
+    if (join_rows)
+      LQ_TRY(launch_loss_join_rows(all, p.rows, p.part_ref, p.part_sum, LOSS_FEW_TILE, mean == 1, loss, row_loss, lse, p.factors, st));
+    else
+      LQ_TRY(launch_loss_join(all, p.rows, half, p.part_ref, p.part_sum, LOSS_FEW_TILE, none, 0, st));
   }
   uint16_t* const none[2] = {nullptr, nullptr};
+  const bool want_e = dX || (dW && p.whole);
   for (int64_t v0 = 0; !few && v0 < vocab; v0 += p.classes) {
     const LossPiece piece{n, v0, std::min(p.classes, vocab - v0), vocab, targets};
     Planes w;
     LQ_TRY(piece_planes(v0, piece.classes, &w));
-    LQ_TRY(launch_loss_logits(w, x, p.d64, piece, p.rows, scales, p.part_ref, p.part_sum, dX ? p.e : none, p.classes, st));
-    LQ_TRY(launch_loss_join(piece, p.rows, half, p.part_ref, p.part_sum, SEG_T, dX ? p.e : none, p.classes, st));
+    LQ_TRY(launch_loss_logits(w, x, p.d64, piece, p.rows, scales, p.part_ref, p.part_sum, want_e ? p.e : none, p.classes, st));
+    LQ_TRY(launch_loss_join(piece, p.rows, half, p.part_ref, p.part_sum, SEG_T, want_e ? p.e : none, p.classes, st));
     if (!dX) continue;
     const PlaneTarget wt{{p.wt[0], p.wt[1], nullptr}, p.classes, d};
     LQ_TRY(launch_column_planes(piece_source(v0, piece.classes), kind, wt, nullptr, 0, st));
-    LQ_TRY(launch_loss_accumulate(Planes{{p.e[0], p.e[1], nullptr}, p.classes}, planes_of(wt), up_to(piece.classes, 64), n, d,
+    LQ_TRY(launch_loss_accumulate(Planes{{p.e[0], half ? p.e[1] : nullptr, nullptr}, p.classes}, planes_of(wt), up_to(piece.classes, 64), n, d,
                                   p.rows.shift, v0 == 0, p.acc, p.part, p.part_floats, st));
   }
   if (scales.xt_top) LQ_TRY(launch_top_magnitude(X, ldx, n, d, targets, vocab, p.tops + 1, st));
-  LQ_TRY(launch_loss_rows(p.rows, scales, targets, n, vocab, mean == 1, loss, row_loss, lse, p.factors, st));
+  if (!join_rows) LQ_TRY(launch_loss_rows(p.rows, scales, targets, n, vocab, mean == 1, loss, row_loss, lse, p.factors, st));
   if (dX && few) {
     LQ_TRY(launch_few_dx(W, ldw, dtype, d, Planes{{p.few_e[0], p.few_e[1], p.few_e[2]}, p.v64}, all, p.rows, p.part_ref, p.factors,
                          p.few_part, dX, st));
@@ -294,10 +300,14 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
   LQ_TRY(launch_column_planes({X, dtype, ldx, n, d, p.tops + 1}, kind, xt, targets, vocab, st));
   for (int64_t v0 = 0; v0 < vocab; v0 += p.classes) {
     const LossPiece piece{n, v0, std::min(p.classes, vocab - v0), vocab, targets};
-    Planes w;
-    LQ_TRY(piece_planes(v0, piece.classes, &w));
-    LQ_TRY(launch_loss_gradient(w, x, p.d64, piece, p.rows, scales, p.e, p.n64, st));
-    LQ_TRY(launch_loss_dw(Planes{{p.e[0], p.e[1], nullptr}, p.n64}, planes_of(xt), p.n64, piece.classes, d, p.factors + 1, dtype,
+    if (p.whole) {
+      LQ_TRY(launch_loss_gradient_from_e(piece, p.rows, half, p.e, p.classes, p.g, p.n64, st));
+    } else {
+      Planes w;
+      LQ_TRY(piece_planes(v0, piece.classes, &w));
+      LQ_TRY(launch_loss_gradient(w, x, p.d64, piece, p.rows, scales, p.g, p.n64, st));
+    }
+    LQ_TRY(launch_loss_dw(Planes{{p.g[0], p.g[1], nullptr}, p.n64}, planes_of(xt), p.n64, piece.classes, d, p.factors + 1, dtype,
                           static_cast<char*>(dW) + (size_t)v0 * (size_t)d * size, p.part, p.part_floats, st));
   }
   return LQ_OK;

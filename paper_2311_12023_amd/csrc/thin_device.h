@@ -1,7 +1,7 @@
 // Products of a tall matrix A (read once, from global memory) with a narrow one: A B^T over A's rows, and A^T B over its columns.
 // B comes as planes with the reduction index contiguous and goes through two LDS stages of 64 reduction indices; A goes through
-// registers, two steps ahead, where it is masked and split.  Barriers are written out: the compiler's own would wait for the loads
-// that are under way.
+// registers, where it is masked and split.  Both are loaded two steps ahead, B before A: loads are waited for in their order.
+// Barriers are written out: the compiler's own would wait for all that are under way.
 #pragma once
 #include "dense_device.h"
 #include "half_planes_device.h"
@@ -117,7 +117,7 @@ __device__ __forceinline__ void thin_rows(const ThinSource& a, const Planes& b, 
     group[h] = (uint64_t)row * (uint64_t)(a.K >> 3);
   }
   Eight<T> v[2][2][H];                                // [parity of the step][half of it][row tile]
-  Stage stage;
+  Stage stage[2];
   auto load = [&](auto odd, int s) __attribute__((always_inline)) {
     constexpr int u = decltype(odd)::value;
 #pragma unroll
@@ -132,11 +132,12 @@ __device__ __forceinline__ void thin_rows(const ThinSource& a, const Planes& b, 
   const auto even = std::integral_constant<int, 0>{};
   const auto odd = std::integral_constant<int, 1>{};
   const int last = s1 - 1;
-  stage.load(b, 64 * (int64_t)s0);
+  const int second = s0 + 1 < last ? s0 + 1 : last;
+  stage[0].load(b, 64 * (int64_t)s0);
   load(even, s0);
-  load(odd, s0 + 1 < last ? s0 + 1 : last);
-  stage.store(lds);
-  stage.load(b, 64 * (int64_t)(s0 + 1 < last ? s0 + 1 : last));
+  stage[1].load(b, 64 * (int64_t)second);
+  load(odd, second);
+  stage[0].store(lds);
   auto step = [&](auto parity, int s) __attribute__((always_inline)) {
     constexpr int u = decltype(parity)::value;
     bf16x8 p[2][H][thin_planes<T>()];
@@ -147,10 +148,11 @@ __device__ __forceinline__ void thin_rows(const ThinSource& a, const Planes& b, 
         apply_mask<T, MASKED>(v[u][sub][h], a.d, group[h] + (uint64_t)(8 * (int64_t)s + 4 * sub + kg));
         to_planes<T>(v[u][sub][h], p[sub][h]);
       }
-    load(parity, s + 2 < last ? s + 2 : last);        // past the end: the last step again, never used
+    const int ahead = s + 2 < last ? s + 2 : last;    // past the end: the last step again, never used
+    stage[u].load(b, 64 * (int64_t)ahead);
+    load(parity, ahead);
     lds_barrier();                                    // this step's B is there, and the other stage has been read
-    stage.store(lds + (u ? 0 : Stage::BYTES));
-    stage.load(b, 64 * (int64_t)(s + 2 < last ? s + 2 : last));
+    stage[u ^ 1].store(lds + (u ? 0 : Stage::BYTES));
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
@@ -175,10 +177,10 @@ __device__ __forceinline__ uint32_t thin_turn(int column) { return (uint32_t)((c
 template <typename T, int RT, int NB>
 constexpr uint32_t thin_columns_lds() { return 2 * ThinStage<RT, NB>::BYTES + thin_planes<T>() * 128u * 128u; }
 
-// adjust.load(s) is called where step s's B is loaded, adjust(stage) before it goes into LDS.
+// adjust.load(parity, s) is called where step s's B is loaded, adjust(parity, stage) before it goes into LDS.
 struct KeepStage {
-  __device__ __forceinline__ void load(int) {}
-  template <class S> __device__ __forceinline__ void operator()(S&) {}
+  template <class P> __device__ __forceinline__ void load(P, int) {}
+  template <class P, class S> __device__ __forceinline__ void operator()(P, S&) {}
 };
 template <typename T, int RT, int NB, bool MASKED, bool VEC, class Adjust>
 __device__ __forceinline__ void thin_columns(const ThinSource& a, const Planes& b, int64_t c0, int s0, int s1, unsigned char* lds,
@@ -191,7 +193,7 @@ __device__ __forceinline__ void thin_columns(const ThinSource& a, const Planes& 
   const T* x = static_cast<const T*>(a.A) + c0 + c8;
   const int col[2] = {32 * wave + l16, 32 * wave + 16 + l16};
   Eight<T> v[2][4];
-  Stage stage;
+  Stage stage[2];
   auto load = [&](auto parity, int s) __attribute__((always_inline)) {
     constexpr int u = decltype(parity)::value;
 #pragma unroll
@@ -203,14 +205,15 @@ __device__ __forceinline__ void thin_columns(const ThinSource& a, const Planes& 
   const auto even = std::integral_constant<int, 0>{};
   const auto odd = std::integral_constant<int, 1>{};
   const int last = s1 - 1;
-  stage.load(b, 64 * (int64_t)s0);
-  adjust.load(s0);
+  const int second = s0 + 1 < last ? s0 + 1 : last;
+  stage[0].load(b, 64 * (int64_t)s0);
+  adjust.load(even, s0);
   load(even, s0);
-  load(odd, s0 + 1 < last ? s0 + 1 : last);
-  adjust(stage);
-  stage.store(lds);
-  stage.load(b, 64 * (int64_t)(s0 + 1 < last ? s0 + 1 : last));
-  adjust.load(s0 + 1 < last ? s0 + 1 : last);
+  stage[1].load(b, 64 * (int64_t)second);
+  adjust.load(odd, second);
+  load(odd, second);
+  adjust(even, stage[0]);
+  stage[0].store(lds);
   auto step = [&](auto parity, int s) __attribute__((always_inline)) {
     constexpr int u = decltype(parity)::value;
     bf16x8 p[4][NP];
@@ -220,7 +223,10 @@ __device__ __forceinline__ void thin_columns(const ThinSource& a, const Planes& 
       apply_mask<T, MASKED>(v[u][q], a.d, (uint64_t)row * (uint64_t)(a.K >> 3) + (uint64_t)((c0 + c8) >> 3));
       to_planes<T>(v[u][q], p[q]);
     }
-    load(parity, s + 2 < last ? s + 2 : last);
+    const int ahead = s + 2 < last ? s + 2 : last;    // past the end: the last step again, never used
+    stage[u].load(b, 64 * (int64_t)ahead);
+    adjust.load(parity, ahead);
+    load(parity, ahead);
     lds_barrier();                                    // the tile and the stage of the step before have been read
 #pragma unroll
     for (int k = 0; k < NP; ++k)
@@ -228,10 +234,8 @@ __device__ __forceinline__ void thin_columns(const ThinSource& a, const Planes& 
       for (int j = 0; j < 8; ++j)
         *reinterpret_cast<bf16x4*>(s_a + (k * 128 + c8 + j) * 128 + (((uint32_t)(r4 >> 3) ^ thin_turn(c8 + j)) * 16u) + (r4 & 4) * 2) =
             bf16x4{p[0][k][j], p[1][k][j], p[2][k][j], p[3][k][j]};
-    adjust(stage);
-    stage.store(lds + (u ? 0 : Stage::BYTES));
-    stage.load(b, 64 * (int64_t)(s + 2 < last ? s + 2 : last));
-    adjust.load(s + 2 < last ? s + 2 : last);
+    adjust(std::integral_constant<int, u ^ 1>{}, stage[u ^ 1]);
+    stage[u ^ 1].store(lds + (u ? 0 : Stage::BYTES));
     lds_barrier();                                    // this step's tile is there
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub) {

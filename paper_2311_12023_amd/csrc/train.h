@@ -127,15 +127,18 @@ struct LossPiece {           // the classes v0 .. v0 + classes - 1 of a call
   int64_t n, v0, classes, vocab;
   const int64_t* targets;
 };
-int launch_loss_begin(const LossRows& r, int64_t n, uint32_t* tops, hipStream_t st);      // tops: two words, set to zero
+int launch_zero_words(uint32_t* p, int count, hipStream_t st);
 // E[i][j] = 2^(s_ij log2 e - part_ref), 0 for the target and beyond the piece, as planes (NULL: not wanted), and per tile of 256
-// classes and row: part_ref, part_sum.  fp32: E is stored times 2^LOSS_E_SHIFT.
-constexpr int LOSS_E_SHIFT = 14;
+// classes and row: part_ref, part_sum.  bf16: e[1], what the rounding of E left out, may be NULL.  fp32: E is stored times 2^LOSS_E_SHIFT and may reach 2^LOSS_E_ROOM.
+constexpr int LOSS_E_SHIFT = 13, LOSS_E_ROOM = 2, LOSS_G_SHIFT = 14;
 int launch_loss_logits(const Planes& w, const Planes& x, int64_t depth, const LossPiece& p, const LossRows& r, const LossScales& s,
                        float* part_ref, float* part_sum, uint16_t* const e[2], int64_t e_pitch, hipStream_t st);
 // Joins the sums of tiles of `tile` classes with the row's; with e (tiles of SEG_T classes) brings E to one power of two per row.
 int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, const float* part_ref, const float* part_sum, int tile,
                      uint16_t* const e[2], int64_t e_pitch, hipStream_t st);
+// Joins and finishes up to 16 rows in one launch (the whole vocabulary as one piece, no E to bring to another power of two).
+int launch_loss_join_rows(const LossPiece& p, const LossRows& r, const float* part_ref, const float* part_sum, int tile, bool mean,
+                          float* loss, float* row_loss, float* lse, float* factors, hipStream_t st);
 // acc (n x d) = acc shift + E W; first: acc = E W.  part: splits x n x d floats.
 int loss_accumulate_splits(int64_t n, int64_t d, int64_t depth, bool half);
 int launch_loss_accumulate(const Planes& e, const Planes& wt, int64_t depth, int64_t n, int64_t d, const float* shift, bool first,
@@ -146,10 +149,13 @@ int launch_loss_rows(const LossRows& r, const LossScales& s, const int64_t* targ
                      float* row_loss, float* lse, float* factors, hipStream_t st);
 int launch_loss_dx(const LossRows& r, const LossScales& s, const int64_t* targets, int64_t n, int64_t d, int64_t vocab,
                    const float* acc, const void* W, int64_t ldw, int dtype, const float* factors, void* dX, hipStream_t st);
-// Gt[j][i] = p_ij - [j = target_i] as planes of `classes` rows (fp32: times 2^LOSS_E_SHIFT), zero for rows that do not count and up
+// Gt[j][i] = p_ij - [j = target_i] as planes of `classes` rows (fp32: times 2^LOSS_G_SHIFT), zero for rows that do not count and up
 // to up_to(n, 64).
 int launch_loss_gradient(const Planes& w, const Planes& x, int64_t depth, const LossPiece& p, const LossRows& r, const LossScales& s,
                          uint16_t* const g[2], int64_t g_pitch, hipStream_t st);
+// The same from E where one piece is the whole vocabulary.
+int launch_loss_gradient_from_e(const LossPiece& p, const LossRows& r, bool half, uint16_t* const e[2], int64_t e_pitch,
+                                uint16_t* const g[2], int64_t g_pitch, hipStream_t st);
 // dW's rows: out (rows x cols, contiguous, of type dtype) = *factor A B^T.  part: splits x rows x cols floats.
 int loss_dw_splits(int64_t rows, int64_t cols, int64_t depth, bool half);
 int launch_loss_dw(const Planes& g, const Planes& xt, int64_t depth, int64_t rows, int64_t cols, const float* factor, int dtype,

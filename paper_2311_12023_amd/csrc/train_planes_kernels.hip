@@ -239,6 +239,7 @@ __global__ __launch_bounds__(256) void top_magnitude_kernel(const float* __restr
   __shared__ uint32_t s_top[4];
   const int64_t units = (cols + 7) / 8, total = rows * units;
   uint32_t top = 0;
+#pragma unroll 4
   for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
     const int64_t row = u / units, c = (u - row * units) * 8;
     if (keep) { const int64_t t = keep[row]; if (t < 0 || t >= keep_below) continue; }
