@@ -86,21 +86,29 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void loss_logits_kernel(LogitsArgs 
     const int at = target >= 0 && target < lim ? (int)target : -1;
     const float f = live ? logit_factor(a.s, token) : 0.0f;
     float top = -__builtin_inff();
+    if (__any(at >= 0) || lim < 128) {                // a target among these classes, or the vocabulary's end: seldom
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int row = 16 * i + 4 * t.kg + e;
-        float x = acc[i][j][e] * f;
-        if (row == at) { a.target[token] = x; x = -__builtin_inff(); }
-        if (row >= lim) x = -__builtin_inff();
-        acc[i][j][e] = x;
-        top = fmaxf(top, x);
+        for (int e = 0; e < 4; ++e) {
+          const int row = 16 * i + 4 * t.kg + e;
+          float x = acc[i][j][e] * f;
+          if (row == at) { a.target[token] = x; x = -__builtin_inff(); }
+          if (row >= lim) x = -__builtin_inff();
+          acc[i][j][e] = x;
+          top = fmaxf(top, x);
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        acc[i][j] *= f;
+        top = fmaxf(top, fmaxf(fmaxf(acc[i][j][0], acc[i][j][1]), fmaxf(acc[i][j][2], acc[i][j][3])));
       }
+    }
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
     s_max[t.wm * SEG_T + col] = top;
-    base[j] = !live ? 0.0f : a.p.v0 == 0 ? -__builtin_inff() : a.ref[token];
+    base[j] = !live ? 0.0f : a.p.v0 == 0 && HALF ? -__builtin_inff() : a.ref[token];
   }
   __syncthreads();
 #pragma unroll
@@ -142,6 +150,44 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void loss_logits_kernel(LogitsArgs 
       }
     }
   }
+}
+
+// A wavefront per row.
+template <bool VEC>
+__global__ __launch_bounds__(256) void loss_reference_kernel(const __bf16* __restrict__ X, int64_t ldx, const __bf16* __restrict__ W,
+                                                             int64_t ldw, int64_t d, LossPiece p, float* __restrict__ ref) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (row >= p.n) return;
+  int64_t c = p.targets[row];
+  if (c < 0 || c >= p.vocab) c = row % p.vocab;
+  const __bf16 *x = X + row * ldx, *w = W + c * ldw;
+  float sum = 0.0f;
+  if constexpr (VEC) {
+#pragma unroll 2
+    for (int64_t k = 8 * lane; k < d; k += 512) {
+      const bf16x8 a = *reinterpret_cast<const bf16x8*>(x + k), b = *reinterpret_cast<const bf16x8*>(w + k);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum = fmaf((float)a[j], (float)b[j], sum);
+    }
+  } else {
+    for (int64_t k = lane; k < d; k += 64) sum = fmaf((float)x[k], (float)w[k], sum);
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+  sum = ceilf(sum * LOG2E);
+  if (lane == 0) ref[row] = fabsf(sum) < 1e30f ? sum : -__builtin_inff();       // NaN too: the tiles find one
+}
+
+int launch_loss_reference(const void* X, int64_t ldx, const void* W, int64_t ldw, int64_t d, const LossPiece& p, const LossRows& r,
+                          hipStream_t st) {
+  const bool vec = d % 8 == 0 && ldx % 8 == 0 && ldw % 8 == 0 && (((uintptr_t)X | (uintptr_t)W) & 15) == 0;
+  auto kernel = vec ? loss_reference_kernel<true> : loss_reference_kernel<false>;
+  prof::Scope ps(prof::LOSS_ROWS, st, (double)p.n * d * 4.0);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((p.n + 3) / 4)), dim3(256), 0, st, static_cast<const __bf16*>(X), ldx,
+                     static_cast<const __bf16*>(W), ldw, d, p, r.ref);
+  LQ_HIP_TRY(hipGetLastError());
+  return LQ_OK;
 }
 
 static int fill_segments(SegArgs& g, const Planes& a, const Planes& b, int64_t depth) {
@@ -230,11 +276,13 @@ int launch_loss_rows(const LossRows& r, const LossScales& s, const int64_t* targ
 // ------------------------------------------------------------------------------------------------
 // A wavefront joins the tiles' sums of one row.  Tiles whose E lies at a smaller power of two than the row's new one are
 // multiplied down, which is exact (what leaves the range of bf16 is below 2^-126 of the largest term, that of fp16 below 2^-37).
-// In the first piece that is all of them, and a launch of its own does it; later it is a row whose logits outgrow its reference.
+// Without a reference from the start that is all of them in the first piece, and a launch of its own does it; else it is a row whose
+// logits outgrow its reference.
 struct JoinArgs {
   LossPiece p; LossRows r;
   const float* part_ref; const float* part_sum; int tiles;
   uint16_t* e[2]; int64_t e_pitch;
+  int told;
 };
 
 template <typename H>
@@ -246,10 +294,11 @@ __device__ __forceinline__ void scale_run(uint16_t* at, float f) {
   *reinterpret_cast<hx4*>(at) = v;
 }
 
+// told: the row has a reference from the start (launch_loss_reference).
 template <typename H>
 __device__ __forceinline__ void join_row(const JoinArgs& a, int64_t row, int lane) {
   const bool first = a.p.v0 == 0;
-  const float old = first ? -__builtin_inff() : a.r.ref[row];
+  const float old = first && !a.told ? -__builtin_inff() : a.r.ref[row];
   float ref = old;
 #pragma unroll 4
   for (int t = lane; t < a.tiles; t += 64) ref = fmaxf(ref, a.part_ref[(int64_t)t * a.p.n + row]);
@@ -268,7 +317,7 @@ __device__ __forceinline__ void join_row(const JoinArgs& a, int64_t row, int lan
     a.r.shift[row] = shift;
     a.r.ref[row] = ref;
   }
-  if (!a.e[0] || first) return;
+  if (!a.e[0] || (first && !a.told)) return;
   for (int t0 = 0; t0 < a.tiles; t0 += 64) {
     const float mine = t0 + lane < a.tiles ? a.part_ref[(int64_t)(t0 + lane) * a.p.n + row] : ref;
     const float f = __builtin_amdgcn_exp2f(mine - from);
@@ -313,14 +362,14 @@ __global__ __launch_bounds__(256) void loss_shift_kernel(JoinArgs a) {
   }
 }
 
-int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, const float* part_ref, const float* part_sum, int tile,
+int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, bool told, const float* part_ref, const float* part_sum, int tile,
                      uint16_t* const e[2], int64_t e_pitch, hipStream_t st) {
-  const JoinArgs a{p, r, part_ref, part_sum, (int)((p.classes + tile - 1) / tile), {e[0], e[1]}, e_pitch};
+  const JoinArgs a{p, r, part_ref, part_sum, (int)((p.classes + tile - 1) / tile), {e[0], e[1]}, e_pitch, told};
   prof::Scope ps(prof::LOSS_ROWS, st, (double)p.n * a.tiles * 8.0);
   auto kernel = half ? loss_join_kernel<_Float16> : loss_join_kernel<__bf16>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)((p.n + 3) / 4)), dim3(256), 0, st, a);
   LQ_HIP_TRY(hipGetLastError());
-  if (!e[0] || p.v0 != 0) return LQ_OK;
+  if (!e[0] || p.v0 != 0 || told) return LQ_OK;
   if (a.tiles > 65535) return LQ_ERR_SHAPE;
   auto shift = half ? loss_shift_kernel<_Float16> : loss_shift_kernel<__bf16>;
   hipLaunchKernelGGL(shift, dim3((unsigned)((p.n + 15) / 16), (unsigned)a.tiles), dim3(256), 0, st, a);
@@ -331,7 +380,7 @@ int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, const flo
 int launch_loss_join_rows(const LossPiece& p, const LossRows& r, const float* part_ref, const float* part_sum, int tile, bool mean,
                           float* loss, float* row_loss, float* lse, float* factors, hipStream_t st) {
   if (p.n > 16 || p.v0 != 0 || p.classes != p.vocab) return LQ_ERR_SHAPE;
-  const JoinArgs a{p, r, part_ref, part_sum, (int)((p.classes + tile - 1) / tile), {nullptr, nullptr}, 0};
+  const JoinArgs a{p, r, part_ref, part_sum, (int)((p.classes + tile - 1) / tile), {nullptr, nullptr}, 0, 0};
   const RowsArgs rows{r, LossScales{}, p.targets, p.n, p.vocab, (int)mean, loss, row_loss, lse, factors};
   prof::Scope ps(prof::LOSS_ROWS, st, (double)p.n * a.tiles * 8.0);
   hipLaunchKernelGGL(loss_join_rows_kernel, dim3(1), dim3(1024), 0, st, a, rows);
@@ -370,7 +419,7 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void loss_accumulate_kernel(Accumul
   if (!t.live) return;
   SegAcc acc;
   seg_clear(acc);
-  seg_products<H>(a.g, t, seg_first(a.g.pairs, t.split, a.g.splits), seg_first(a.g.pairs, t.split + 1, a.g.splits), seg_lds, acc);
+  seg_products<H, true>(a.g, t, seg_first(a.g.pairs, t.split, a.g.splits), seg_first(a.g.pairs, t.split + 1, a.g.splits), seg_lds, acc);
   float* out = a.g.splits > 1 ? a.part + (size_t)t.split * (size_t)a.n * (size_t)a.d : a.acc;
   const bool add = a.g.splits == 1 && !a.first;
   seg_each(t, acc, [&](floatx4 v, int64_t col, int64_t token) {
@@ -395,12 +444,15 @@ int loss_accumulate_splits(int64_t n, int64_t d, int64_t depth, bool half) {
   return seg_splits(seg_tiles(n, d), depth / 64 * (half ? 3 : 1), 64);
 }
 
-int launch_loss_accumulate(const Planes& e, const Planes& wt, int64_t depth, int64_t n, int64_t d, const float* shift, bool first,
+int launch_loss_accumulate(const Planes& e, const Planes& w, int64_t classes, int64_t n, int64_t d, const float* shift, bool first,
                            float* acc, float* part, size_t part_floats, hipStream_t st) {
   const bool half = e.p[1] != nullptr;
+  const int64_t depth = up_to(classes, 64);
+  if (w.pitch % 8 || w.pitch < up_to(d, 8) || e.pitch < depth) return LQ_ERR_SHAPE;
   AccumulateArgs a{};
-  LQ_TRY(fill_segments(a.g, wt, e, depth));
+  LQ_TRY(fill_segments(a.g, w, e, depth));
   LQ_TRY(seg_shape(a.g, d, n, loss_accumulate_splits(n, d, depth, half)));
+  a.g.rows_a = up_to(d, 8); a.g.depth_a = classes;           // whole units of W's rows
   if (a.g.splits > 1 && part_floats < (size_t)a.g.splits * (size_t)n * (size_t)d) return LQ_ERR_WORKSPACE;
   a.n = n; a.d = d; a.shift = shift; a.first = first; a.acc = acc; a.part = part;
   static LdsLimit limit[2];

@@ -52,7 +52,7 @@ struct LossPlan {
   LossRows rows;
   float *factors, *part_ref, *part_sum, *acc, *part, *x_inv;
   uint32_t* tops;                                    // of W, of the rows of X that count
-  uint16_t *x[2], *xt[2], *w[2], *wt[2], *e[2], *g[2];
+  uint16_t *x[2], *xt[2], *w[2], *e[2], *g[2];
   bool whole;                                        // one piece is the whole vocabulary
   uint16_t *few_x[3], *few_e[3];                     // the few rows' planes
   float* few_part;
@@ -86,7 +86,6 @@ static LossPlan plan_loss(void* ws, int64_t n, int64_t d, int64_t vocab, int dty
     p.x[h] = a.take<uint16_t>(n * p.d64);
     p.w[h] = a.take<uint16_t>(p.classes * p.d64);
     p.xt[h] = a.take<uint16_t>(want_dw ? d * p.n64 : 0);
-    p.wt[h] = a.take<uint16_t>(want_dx ? d * p.classes : 0);
     p.e[h] = a.take<uint16_t>(want_dx || (want_dw && p.whole) ? n * p.classes : 0);
     p.g[h] = a.take<uint16_t>(want_dw ? p.classes * p.n64 : 0);
   }
@@ -271,21 +270,20 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
     if (join_rows)
       LQ_TRY(launch_loss_join_rows(all, p.rows, p.part_ref, p.part_sum, LOSS_FEW_TILE, mean == 1, loss, row_loss, lse, p.factors, st));
     else
-      LQ_TRY(launch_loss_join(all, p.rows, half, p.part_ref, p.part_sum, LOSS_FEW_TILE, none, 0, st));
+      LQ_TRY(launch_loss_join(all, p.rows, half, false, p.part_ref, p.part_sum, LOSS_FEW_TILE, none, 0, st));
   }
   uint16_t* const none[2] = {nullptr, nullptr};
+  if (!few && !half) LQ_TRY(launch_loss_reference(X, ldx, W, ldw, d, all, p.rows, st));
   const bool want_e = dX || (dW && p.whole);
   for (int64_t v0 = 0; !few && v0 < vocab; v0 += p.classes) {
     const LossPiece piece{n, v0, std::min(p.classes, vocab - v0), vocab, targets};
     Planes w;
     LQ_TRY(piece_planes(v0, piece.classes, &w));
     LQ_TRY(launch_loss_logits(w, x, p.d64, piece, p.rows, scales, p.part_ref, p.part_sum, want_e ? p.e : none, p.classes, st));
-    LQ_TRY(launch_loss_join(piece, p.rows, half, p.part_ref, p.part_sum, SEG_T, want_e ? p.e : none, p.classes, st));
+    LQ_TRY(launch_loss_join(piece, p.rows, half, !half, p.part_ref, p.part_sum, SEG_T, want_e ? p.e : none, p.classes, st));
     if (!dX) continue;
-    const PlaneTarget wt{{p.wt[0], p.wt[1], nullptr}, p.classes, d};
-    LQ_TRY(launch_column_planes(piece_source(v0, piece.classes), kind, wt, nullptr, 0, st));
-    LQ_TRY(launch_loss_accumulate(Planes{{p.e[0], half ? p.e[1] : nullptr, nullptr}, p.classes}, planes_of(wt), up_to(piece.classes, 64), n, d,
-                                  p.rows.shift, v0 == 0, p.acc, p.part, p.part_floats, st));
+    LQ_TRY(launch_loss_accumulate(Planes{{p.e[0], half ? p.e[1] : nullptr, nullptr}, p.classes}, w, piece.classes, n, d, p.rows.shift,
+                                  v0 == 0, p.acc, p.part, p.part_floats, st));
   }
   if (scales.xt_top) LQ_TRY(launch_top_magnitude(X, ldx, n, d, targets, vocab, p.tops + 1, st));
   if (!join_rows) LQ_TRY(launch_loss_rows(p.rows, scales, targets, n, vocab, mean == 1, loss, row_loss, lse, p.factors, st));

@@ -58,7 +58,12 @@ __device__ __forceinline__ int seg_first(int pairs, int split, int splits) { ret
 // of 32 x 32 x 16 take the same cycles, but the chip, which lowers its clock under this load, holds 1.9 GHz with these and 1.65 with
 // those (1368 against 1220 TFLOP/s, call after call).  Rows are 64 bytes, unit u of a row stored at u ^ ((row / 4) % 4): the
 // 16 lanes that read one unit of 16 rows fall into different banks.
-template <typename H>
+//
+// TURNED: A's planes have its rows contiguous and the reduction index from row to row (W as it is stored, for E W), so a step is 32
+// rows of 512 bytes in LDS and operands come out by transposed reads: 16 lanes read four reduction indices of 16 rows of A, a
+// lane gets the four of its own.  The 32-byte chunk c of reduction index k is stored at c ^ (k % 4 + 4 (k / 8 % 2)): the sixteen
+// indices that a read touches spread over the banks.  A pass that turned W beforehand took 47 us per 16384 x 4096 of it.
+template <typename H, bool TURNED = false>
 __device__ __forceinline__ void seg_products(const SegArgs& a, const SegTile& t, int s0, int s1, unsigned char* lds, SegAcc& acc) {
   typedef H hx8 __attribute__((ext_vector_type(8)));
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -72,43 +77,82 @@ __device__ __forceinline__ void seg_products(const SegArgs& a, const SegTile& t,
     const int64_t la = a.rows_a - 1 - arow, lb = a.rows_b - 1 - brow;
     ra[q] = r < la ? r : (int)la;
     rb[q] = r < lb ? r : (int)lb;
+    if constexpr (TURNED) {
+      // reduction indices 4 wave + 2 q + l / 32 of a step, unit l % 32 ^ chunk swizzle; a unit past the rows is the last one again
+      const int k = 4 * wave + 2 * q + (lane >> 5), u = (lane & 31) ^ (((k & 3) + 4 * ((k >> 3) & 1)) * 2);
+      ra[q] = 8 * u <= la - 7 ? 8 * u : (int)la - 7;
+    }
   }
   const uint16_t *pa, *pb;
-  uint32_t va[2], vb[2];
-  int next = s0, seg = 0, end;
+  uint32_t va[TURNED ? 4 : 2], vb[2];
+  int next = s0, seg = 0, end, left = 0;         // left: TURNED, reduction indices of A from the present pair on
+  auto place = [&]() __attribute__((always_inline)) {      // TURNED: indices past the end are the last one again (B is zero there)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int k = 4 * wave + 2 * (q & 1) + (lane >> 5) + 32 * (q >> 1);
+      va[TURNED ? q : 0] = (uint32_t)((k < left ? k : left - 1) * a.seg[seg].pitch_a * 2 + ra[q & 1] * 2);
+    }
+  };
   auto enter = [&](int64_t k) {
     const Segment& g = a.seg[seg];
-    pa = g.A + arow * g.pitch_a + k;
+    if constexpr (TURNED) {
+      pa = g.A + k * g.pitch_a + arow;
+      left = (int)(a.depth_a - k);
+      place();
+    } else {
+      pa = g.A + arow * g.pitch_a + k;
+    }
     pb = g.B + brow * g.pitch_b + k;
     end = g.end;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      va[q] = (uint32_t)(ra[q] * g.pitch_a * 2 + unit * 16);
+      if constexpr (!TURNED) va[q] = (uint32_t)(ra[q] * g.pitch_a * 2 + unit * 16);
       vb[q] = (uint32_t)(rb[q] * g.pitch_b * 2 + unit * 16);
     }
   };
   while (s0 >= a.seg[seg].end) ++seg;
   enter(64 * (int64_t)(s0 - (seg ? a.seg[seg - 1].end : 0)));
   auto transfer = [&](int part, int half, uint32_t slot) __attribute__((always_inline)) {     // a quarter of a step's transfers
-    transfer_to_lds((part < 2 ? pa : pb) + 32 * half, part < 2 ? va[part & 1] : vb[part & 1],
-                    slot + (part < 2 ? 0u : SEG_TILE) + (uint32_t)wave * 2048u + 1024u * (part & 1));
+    if (part < 2)
+      transfer_to_lds(TURNED ? pa : pa + 32 * half, va[TURNED ? part + 2 * half : part], slot + (uint32_t)wave * 2048u + 1024u * part);
+    else
+      transfer_to_lds(pb + 32 * half, vb[part & 1], slot + SEG_TILE + (uint32_t)wave * 2048u + 1024u * (part & 1));
   };
   auto advance = [&]() {                         // past the end: the last pair again, into slots that nobody reads any more
     if (next + 1 >= s1) return;
     ++next;
-    if (next == end) { ++seg; enter(0); }
-    else { pa += 64; pb += 64; }
+    if (next == end) { ++seg; enter(0); return; }
+    pb += 64;
+    if constexpr (TURNED) {
+      pa += 64 * a.seg[seg].pitch_a;
+      left -= 64;
+      if (left < 64) place();
+    } else {
+      pa += 64;
+    }
   };
   const uint32_t u0 = (uint32_t)(t.kg ^ ((t.l16 >> 2) & 3)) * 16u;
-  const uint32_t aoff = (uint32_t)(128 * t.wm + t.l16) * 64u + u0, boff = SEG_TILE + (uint32_t)(64 * t.wn + t.l16) * 64u + u0;
+  // TURNED: index 8 kg + l16 / 4 of a step (and four further), chunk 8 wm + i: the swizzle takes in the indices' low bits and kg
+  const uint32_t turn = (uint32_t)((t.l16 >> 2) + 4 * (t.kg & 1));
+  const uint32_t aoff = TURNED ? (uint32_t)(8 * t.kg + (t.l16 >> 2)) * 512u + 8u * (t.l16 & 3) : (uint32_t)(128 * t.wm + t.l16) * 64u + u0, boff = SEG_TILE + (uint32_t)(64 * t.wn + t.l16) * 64u + u0;
   hx8 x[2][8], y[2][4];                          // operands of the present and the next step
-  auto read = [&](uint32_t slot, int g, int part) __attribute__((always_inline)) {     // one of twelve, in the order of their use
-    if (part == 0 || part > 4) {
-      const int i = part ? part - 4 : 0;
-      x[g][i] = *reinterpret_cast<const hx8*>(lds + (slot + aoff) + 1024u * i);
+  auto read_x = [&](uint32_t slot, int g, int i, int half) __attribute__((always_inline)) {
+    if constexpr (TURNED) {
+      typedef short shortx4 __attribute__((ext_vector_type(4)));
+      typedef H hx4 __attribute__((ext_vector_type(4)));
+      const uint32_t at = slot + aoff + (((uint32_t)(8 * t.wm + i) ^ turn) * 32u) + 2048u * half;
+      const hx4 v = __builtin_bit_cast(hx4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)(lds + at)));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[g][i][4 * half + e] = v[e];
     } else {
-      y[g][part - 1] = *reinterpret_cast<const hx8*>(lds + (slot + boff) + 1024u * (part - 1));
+      x[g][i] = *reinterpret_cast<const hx8*>(lds + (slot + aoff) + 1024u * i);
     }
+  };
+  constexpr int XR = TURNED ? 2 : 1, READS = 8 * XR + 4;         // operand reads of a step, in the order of their use
+  auto read = [&](uint32_t slot, int g, int part) __attribute__((always_inline)) {
+    if (part < XR) read_x(slot, g, 0, part);
+    else if (part < XR + 4) y[g][part - XR] = *reinterpret_cast<const hx8*>(lds + (slot + boff) + 1024u * (part - XR));
+    else read_x(slot, g, (part - 4) / XR, (part - 4) % XR);
   };
   auto after = [](uint32_t slot) { return slot == (SEG_SLOTS - 1) * SEG_STAGE ? 0u : slot + SEG_STAGE; };
 #pragma unroll
@@ -122,7 +166,7 @@ __device__ __forceinline__ void seg_products(const SegArgs& a, const SegTile& t,
   }
   asm volatile("s_waitcnt vmcnt(8)\n\ts_barrier" ::: "memory");     // 8 transfers a pair: the first pair's are done
 #pragma unroll
-  for (int part = 0; part < 12; ++part) read(0, 0, part);
+  for (int part = 0; part < READS; ++part) read(0, 0, part);
   uint32_t rd = SEG_STAGE, wr = 4 * SEG_STAGE;   // the slot read next; the first of the two that are refilled next
   auto step = [&](auto odd) __attribute__((always_inline)) {
     constexpr int u = decltype(odd)::value;
@@ -138,8 +182,8 @@ __device__ __forceinline__ void seg_products(const SegArgs& a, const SegTile& t,
       else
         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[u][i], y[u][j], acc[i][j], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
-      if ((n % 5 == 1 || n % 5 == 3) && n < 30) {                  // past the end: a slot's old contents, never used
-        read(rd, u ^ 1, n / 5 * 2 + (n % 5 == 3));
+      if (n < 30 && (n + 1) * READS / 30 > n * READS / 30) {       // past the end: a slot's old contents, never used
+        read(rd, u ^ 1, n * READS / 30);
         __builtin_amdgcn_sched_barrier(0);
       }
       if (n % 4 == 2 && u == 0) {

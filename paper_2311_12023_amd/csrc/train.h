@@ -30,6 +30,7 @@ struct Segment {
 struct SegArgs {
   Segment seg[6];
   int64_t rows_a, rows_b;
+  int64_t depth_a;               // reduction indices that A has, where it is read turned
   int tiles_m, tiles_n, splits, pairs;
 };
 
@@ -134,15 +135,21 @@ constexpr int LOSS_E_SHIFT = 13, LOSS_E_ROOM = 2, LOSS_G_SHIFT = 14;
 int launch_loss_logits(const Planes& w, const Planes& x, int64_t depth, const LossPiece& p, const LossRows& r, const LossScales& s,
                        float* part_ref, float* part_sum, uint16_t* const e[2], int64_t e_pitch, hipStream_t st);
 // Joins the sums of tiles of `tile` classes with the row's; with e (tiles of SEG_T classes) brings E to one power of two per row.
-int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, const float* part_ref, const float* part_sum, int tile,
+// told: r.ref has been set by launch_loss_reference.
+int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, bool told, const float* part_ref, const float* part_sum, int tile,
                      uint16_t* const e[2], int64_t e_pitch, hipStream_t st);
 // Joins and finishes up to 16 rows in one launch (the whole vocabulary as one piece, no E to bring to another power of two).
 int launch_loss_join_rows(const LossPiece& p, const LossRows& r, const float* part_ref, const float* part_sum, int tile, bool mean,
                           float* loss, float* row_loss, float* lse, float* factors, hipStream_t st);
-// acc (n x d) = acc shift + E W; first: acc = E W.  part: splits x n x d floats.
+// acc (n x d) = acc shift + E W; first: acc = E W.  W: `classes` rows of at least up_to(d, 8) elements; E is zero from there to
+// up_to(classes, 64).  part: splits x n x d floats.
 int loss_accumulate_splits(int64_t n, int64_t d, int64_t depth, bool half);
-int launch_loss_accumulate(const Planes& e, const Planes& wt, int64_t depth, int64_t n, int64_t d, const float* shift, bool first,
+int launch_loss_accumulate(const Planes& e, const Planes& w, int64_t classes, int64_t n, int64_t d, const float* shift, bool first,
                            float* acc, float* part, size_t part_floats, hipStream_t st);
+// What rows of X are relative to before a logit is known (bf16): the power of two of their target's logit, of another class's where
+// they have none.  With 64 to spare on either side that serves E (see loss_logits_kernel).
+int launch_loss_reference(const void* X, int64_t ldx, const void* W, int64_t ldw, int64_t d, const LossPiece& p, const LossRows& r,
+                          hipStream_t st);
 // Row losses, log-sum-exps, their total and what the gradients need: r.wrong, r.lse2, factors[0] = the gradient's factor,
 // factors[1] = that of dW's product.
 int launch_loss_rows(const LossRows& r, const LossScales& s, const int64_t* targets, int64_t n, int64_t vocab, bool mean, float* loss,
