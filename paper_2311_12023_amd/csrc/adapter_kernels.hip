@@ -170,7 +170,6 @@ struct AdapterArgs {
 
 template <typename H, typename T>
 __global__ __launch_bounds__(SEG_THREADS, 2) void adapter_product_kernel(AdapterArgs a) {
-  typedef T vec4 __attribute__((ext_vector_type(4)));
   constexpr bool HALF = !std::is_same<H, __bf16>::value;
   extern __shared__ __attribute__((aligned(16))) unsigned char seg_lds[];
   const SegTile t = seg_tile(a.g);
@@ -214,14 +213,25 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void adapter_product_kernel(Adapter
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int64_t token = col0 + 16 * j;
-    if (token >= a.tokens) continue;
+    const bool live = token < a.tokens;
+    if (sizeof(T) == 2 && a.g.splits == 1) {          // eight neighbouring features a lane: blocks i and i + 1
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const uintx4 v = seg_pair_blocks(__builtin_bit_cast(uintx2, __builtin_convertvector(acc[i][j], bf16x4)),
+                                         __builtin_bit_cast(uintx2, __builtin_convertvector(acc[i + 1][j], bf16x4)));
+        const int64_t row = row0 - 4 * t.kg + 16 * (i + (t.kg & 1)) + 8 * (t.kg >> 1);
+        if (live && row < a.features) *reinterpret_cast<uintx4*>(static_cast<uint16_t*>(a.out) + token * a.features + row) = v;
+      }
+      continue;
+    }
+    if (!live) continue;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int64_t row = row0 + 16 * i;
       if (row >= a.features) continue;                // features are a multiple of 16
       const floatx4 v = HALF ? acc[i][j] * inv[j] : acc[i][j];
-      if (a.g.splits > 1) *reinterpret_cast<floatx4*>(part + token * a.features + row) = v;
-      else *reinterpret_cast<vec4*>(static_cast<T*>(a.out) + token * a.features + row) = __builtin_convertvector(v, vec4);
+      float* out = a.g.splits > 1 ? part : static_cast<float*>(a.out);
+      *reinterpret_cast<floatx4*>(out + token * a.features + row) = v;
     }
   }
 }

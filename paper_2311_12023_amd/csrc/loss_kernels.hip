@@ -32,20 +32,28 @@ __device__ __forceinline__ float logit_factor(const LossScales& s, int64_t token
   return s.x_inv ? LOG2E * s.x_inv[token] * power_of_two(-half_exponent(*s.w_top)) : LOG2E;
 }
 
-// Four neighbours as planes (bf16: lo may be NULL).
+// Two blocks of four neighbours a lane as planes, eight neighbours a lane (bf16: lo may be NULL).
 template <bool HALF>
-__device__ __forceinline__ void store_four(uint16_t* hi, uint16_t* lo, floatx4 v) {
+__device__ __forceinline__ void split_four(floatx4 v, uintx2& hi, uintx2& lo) {
   if constexpr (HALF) {
     halfx4 h, l;
 #pragma unroll
     for (int e = 0; e < 4; ++e) { const HalfPair p = split_half(v[e]); h[e] = p.hi; l[e] = p.lo; }
-    *reinterpret_cast<halfx4*>(hi) = h;
-    *reinterpret_cast<halfx4*>(lo) = l;
+    hi = __builtin_bit_cast(uintx2, h);
+    lo = __builtin_bit_cast(uintx2, l);
   } else {
     const bf16x4 h = __builtin_convertvector(v, bf16x4);
-    *reinterpret_cast<bf16x4*>(hi) = h;
-    if (lo) *reinterpret_cast<bf16x4*>(lo) = __builtin_convertvector(v - __builtin_convertvector(h, floatx4), bf16x4);
+    hi = __builtin_bit_cast(uintx2, h);
+    lo = __builtin_bit_cast(uintx2, __builtin_convertvector(v - __builtin_convertvector(h, floatx4), bf16x4));
   }
+}
+template <bool HALF>
+__device__ __forceinline__ void store_blocks(uint16_t* hi, uint16_t* lo, floatx4 first, floatx4 second) {
+  uintx2 h0, l0, h1, l1;
+  split_four<HALF>(first, h0, l0);
+  split_four<HALF>(second, h1, l1);
+  *reinterpret_cast<uintx4*>(hi) = seg_pair_blocks(h0, h1);
+  if (HALF || lo) *reinterpret_cast<uintx4*>(lo) = seg_pair_blocks(l0, l1);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -133,9 +141,9 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void loss_logits_kernel(LogitsArgs 
     sum += __shfl_xor(sum, 32);
     s_sum[t.wm * SEG_T + col] = HALF ? sum * power_of_two(-LOSS_E_SHIFT) : sum;
     if (a.e[0] && token < a.p.n) {
-      const int64_t at = token * a.e_pitch + class0 + 4 * t.kg;
+      const int64_t at = token * a.e_pitch + class0 + 16 * (t.kg & 1) + 8 * (t.kg >> 1);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) store_four<HALF>(a.e[0] + at + 16 * i, HALF || a.e[1] ? a.e[1] + at + 16 * i : nullptr, acc[i][j]);
+      for (int i = 0; i < 8; i += 2) store_blocks<HALF>(a.e[0] + at + 16 * i, a.e[1] ? a.e[1] + at + 16 * i : nullptr, acc[i][j], acc[i + 1][j]);
     }
   }
   __syncthreads();
@@ -551,23 +559,29 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void loss_gradient_kernel(GradientA
   __syncthreads();
   const int64_t cols = (a.p.n + 63) / 64 * 64;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int row = 128 * t.wm + 16 * i + 4 * t.kg;
-    const int64_t token = (int64_t)t.tm * SEG_T + row;
-    if (token >= cols) continue;
+  for (int j = 0; j < 4; ++j) {
+    const int64_t cls = (int64_t)t.tn * SEG_T + 64 * t.wn + 16 * j + t.l16;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t cls = (int64_t)t.tn * SEG_T + 64 * t.wn + 16 * j + t.l16;
-      if (cls >= a.p.classes) continue;
-      floatx4 g;
+    for (int i = 0; i < 8; i += 2) {
+      floatx4 g[2];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int at = s_at[row + e];
-        const float p = __builtin_amdgcn_exp2f(acc[i][j][e] * s_f[row + e] - s_lse[row + e]) * unit;
-        g[e] = at == -2 ? 0.0f : at == (int)cls ? -s_wrong[row + e] : p;     // rows that do not count: whatever they hold
-      }
-      const int64_t to = cls * a.pitch + token;
-      store_four<HALF>(a.out[0] + to, HALF ? a.out[1] + to : nullptr, g);
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int row = 128 * t.wm + 16 * (i + q) + 4 * t.kg + e, at = s_at[row];
+          const float p = __builtin_amdgcn_exp2f(acc[i + q][j][e] * s_f[row] - s_lse[row]) * unit;
+          g[q][e] = at == -2 ? 0.0f : at == (int)cls ? -s_wrong[row] : p;     // rows that do not count: whatever they hold
+        }
+      // a block of 32 tokens lies inside the padded rows or beyond them
+      const int64_t token = (int64_t)t.tm * SEG_T + 128 * t.wm + 16 * i, to = cls * a.pitch + token + 16 * (t.kg & 1) + 8 * (t.kg >> 1);
+      uint16_t* hi = cls < a.p.classes && token < cols ? a.out[0] + to : nullptr;
+      uintx2 h0, l0, h1, l1;
+      split_four<HALF>(g[0], h0, l0);
+      split_four<HALF>(g[1], h1, l1);
+      const uintx4 h = seg_pair_blocks(h0, h1), l = seg_pair_blocks(l0, l1);
+      if (!hi) continue;
+      *reinterpret_cast<uintx4*>(hi) = h;
+      if constexpr (HALF) *reinterpret_cast<uintx4*>(a.out[1] + to) = l;
     }
   }
 }

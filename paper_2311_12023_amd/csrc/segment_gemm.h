@@ -201,6 +201,14 @@ __device__ __forceinline__ void seg_products(const SegArgs& a, const SegTile& t,
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");       // nothing lands in LDS any more
 }
 
+// Two blocks of 16-bit values, four neighbours (of 16) a lane, become one block of eight neighbours a lane: lanes of even kg hold
+// values 8 (kg / 2) .. of the first block then, those of odd kg the same of the second.
+__device__ __forceinline__ uintx4 seg_pair_blocks(uintx2 first, uintx2 second) {
+  const auto a = __builtin_amdgcn_permlane16_swap(first[0], second[0], false, false);
+  const auto b = __builtin_amdgcn_permlane16_swap(first[1], second[1], false, false);
+  return uintx4{a[0], b[0], a[1], b[1]};
+}
+
 // f(v, row, column) for the wavefront's blocks: v holds rows row .. row + 3 of one column.
 template <class F>
 __device__ __forceinline__ void seg_each(const SegTile& t, const SegAcc& acc, F&& f) {
