@@ -160,61 +160,41 @@ int launch_weight_planes(const MvWeights& q, int64_t K, int64_t N, bool transpos
 // The low-rank part goes into the accumulators first and is masked there, then the weights' part is added to it: no second set of
 // accumulators, no array of U L1^T.  Features are the tile's rows and tokens its columns, so that a lane holds four neighbouring
 // features of a token and the lane 16 further the next four: a group of the generator.
+//
+// Work is dealt out in stretches of pairs of steps, all tiles' one after the other, a tile's low-rank pairs before its others: a
+// stretch may end inside a tile, whose parts a second kernel then adds up (the mask goes onto each part of the low-rank sum).
 struct AdapterArgs {
   SegArgs g, low;
   AdapterScales s;
   int64_t features, tokens;
   int masked; DropoutMask mask;
-  void* out; float* part;
+  int stretches, per, more;        // pairs of a stretch, and how many of the first have one more
+  void* out; float* part;          // two tiles a stretch: of the tile it begins in, of the tile it ends in
 };
+constexpr int64_t PART_TILE = (int64_t)SEG_T * SEG_T;
 
-template <typename H, typename T>
-__global__ __launch_bounds__(SEG_THREADS, 2) void adapter_product_kernel(AdapterArgs a) {
-  constexpr bool HALF = !std::is_same<H, __bf16>::value;
-  extern __shared__ __attribute__((aligned(16))) unsigned char seg_lds[];
-  const SegTile t = seg_tile(a.g);
-  if (!t.live) return;
-  SegAcc acc;
-  seg_clear(acc);
-  const int64_t row0 = (int64_t)t.tm * SEG_T + 128 * t.wm + 4 * t.kg, col0 = (int64_t)t.tn * SEG_T + 64 * t.wn + t.l16;
+__device__ __forceinline__ int stretch_begin(const AdapterArgs& a, int w) { return a.per * w + (w < a.more ? w : a.more); }
+
+// What the sums of the fp16 planes of a token are to be multiplied by.
+template <bool HALF>
+__device__ __forceinline__ void token_factors(const AdapterArgs& a, int64_t col0, float (&inv)[4]) {
   const float a_inv = HALF ? power_of_two(-half_exponent_of(a.s.a_top, TOP_WORDS)) : 1.0f;
-  float inv[4];                                       // what a token's sums of the fp16 planes are to be multiplied by
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int64_t token = col0 + 16 * j;
     inv[j] = HALF && token < a.tokens ? a.s.b_inv[token] * a_inv : 1.0f;
   }
-  if (t.split == 0 && a.low.pairs > 0) {
-    seg_products<__bf16>(a.low, t, 0, a.low.pairs, seg_lds, acc);
-    if (HALF || a.masked) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint64_t group = (uint64_t)(col0 + 16 * j) * (uint64_t)(a.features >> 3) + (uint64_t)(row0 >> 3);
-        const float scale = (a.masked ? a.mask.scale : 1.0f) * (HALF ? 1.0f / inv[j] : 1.0f);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (a.masked) {
-            const PhiloxWords w = philox_words(a.mask, group + 2 * i);
-            const uint32_t w0 = t.kg & 1 ? w.w[2] : w.w[0], w1 = t.kg & 1 ? w.w[3] : w.w[1];
-            acc[i][j][0] = (w0 & 0xffffu) >= a.mask.cut ? acc[i][j][0] * scale : 0.0f;
-            acc[i][j][1] = (w0 >> 16) >= a.mask.cut ? acc[i][j][1] * scale : 0.0f;
-            acc[i][j][2] = (w1 & 0xffffu) >= a.mask.cut ? acc[i][j][2] * scale : 0.0f;
-            acc[i][j][3] = (w1 >> 16) >= a.mask.cut ? acc[i][j][3] * scale : 0.0f;
-          } else {
-            acc[i][j] *= scale;
-          }
-        }
-      }
-    }
-    __syncthreads();                                  // the LDS has been read by everyone
-  }
-  seg_products<H>(a.g, t, seg_first(a.g.pairs, t.split, a.g.splits), seg_first(a.g.pairs, t.split + 1, a.g.splits), seg_lds, acc);
-  float* part = a.part + (size_t)t.split * (size_t)a.tokens * (size_t)a.features;
+}
+
+// A finished tile's blocks to `out`.
+template <typename T>
+__device__ __forceinline__ void store_tile(const AdapterArgs& a, const SegAcc& acc, const SegTile& t, int64_t row0, int64_t col0,
+                                           const float (&inv)[4]) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int64_t token = col0 + 16 * j;
     const bool live = token < a.tokens;
-    if (sizeof(T) == 2 && a.g.splits == 1) {          // eight neighbouring features a lane: blocks i and i + 1
+    if constexpr (sizeof(T) == 2) {                   // eight neighbouring features a lane: blocks i and i + 1
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
         const uintx4 v = seg_pair_blocks(__builtin_bit_cast(uintx2, __builtin_convertvector(acc[i][j], bf16x4)),
@@ -222,39 +202,140 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void adapter_product_kernel(Adapter
         const int64_t row = row0 - 4 * t.kg + 16 * (i + (t.kg & 1)) + 8 * (t.kg >> 1);
         if (live && row < a.features) *reinterpret_cast<uintx4*>(static_cast<uint16_t*>(a.out) + token * a.features + row) = v;
       }
-      continue;
-    }
-    if (!live) continue;
+    } else if (live) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t row = row0 + 16 * i;
-      if (row >= a.features) continue;                // features are a multiple of 16
-      const floatx4 v = HALF ? acc[i][j] * inv[j] : acc[i][j];
-      float* out = a.g.splits > 1 ? part : static_cast<float*>(a.out);
-      *reinterpret_cast<floatx4*>(out + token * a.features + row) = v;
+      for (int i = 0; i < 8; ++i) {
+        const int64_t row = row0 + 16 * i;            // features are a multiple of 16
+        if (row < a.features) *reinterpret_cast<floatx4*>(static_cast<float*>(a.out) + token * a.features + row) = acc[i][j] * inv[j];
+      }
     }
   }
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void adapter_sum_kernel(const float* __restrict__ part, int splits, int64_t quads, T* __restrict__ out) {
-  typedef T vec4 __attribute__((ext_vector_type(4)));
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < quads; i += (int64_t)gridDim.x * 256) {
-    floatx4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = 0; s < splits; ++s) v += reinterpret_cast<const floatx4*>(part)[s * quads + i];
-    reinterpret_cast<vec4*>(out)[i] = __builtin_convertvector(v, vec4);
+template <typename H, typename T>
+__global__ __launch_bounds__(SEG_THREADS, 2) void adapter_product_kernel(AdapterArgs a) {
+  constexpr bool HALF = !std::is_same<H, __bf16>::value;
+  extern __shared__ __attribute__((aligned(16))) unsigned char seg_lds[];
+  const int w = seg_piece(a.stretches);
+  if (w < 0) return;
+  const int low = a.low.pairs, pairs = low + a.g.pairs;       // of a tile
+  const int begin = stretch_begin(a, w), stop = stretch_begin(a, w + 1);
+  for (int pos = begin; pos < stop;) {
+    const int u = pos / pairs, s0 = pos - u * pairs, s1 = stop - pos < pairs - s0 ? s0 + stop - pos : pairs;
+    const SegTile t = seg_tile_at(a.g, u);
+    const int64_t row0 = (int64_t)t.tm * SEG_T + 128 * t.wm + 4 * t.kg, col0 = (int64_t)t.tn * SEG_T + 64 * t.wn + t.l16;
+    SegAcc acc;
+    seg_clear(acc);
+    float inv[4];
+    token_factors<HALF>(a, col0, inv);
+    if (s0 < low) {
+      seg_products<__bf16>(a.low, t, s0, s1 < low ? s1 : low, seg_lds, acc);
+      if (HALF || a.masked) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint64_t group = (uint64_t)(col0 + 16 * j) * (uint64_t)(a.features >> 3) + (uint64_t)(row0 >> 3);
+          const float scale = (a.masked ? a.mask.scale : 1.0f) * (HALF ? 1.0f / inv[j] : 1.0f);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if (a.masked) {
+              const PhiloxWords p = philox_words(a.mask, group + 2 * i);
+              const uint32_t w0 = t.kg & 1 ? p.w[2] : p.w[0], w1 = t.kg & 1 ? p.w[3] : p.w[1];
+              acc[i][j][0] = (w0 & 0xffffu) >= a.mask.cut ? acc[i][j][0] * scale : 0.0f;
+              acc[i][j][1] = (w0 >> 16) >= a.mask.cut ? acc[i][j][1] * scale : 0.0f;
+              acc[i][j][2] = (w1 & 0xffffu) >= a.mask.cut ? acc[i][j][2] * scale : 0.0f;
+              acc[i][j][3] = (w1 >> 16) >= a.mask.cut ? acc[i][j][3] * scale : 0.0f;
+            } else {
+              acc[i][j] *= scale;
+            }
+          }
+        }
+      }
+      __syncthreads();                                // the LDS has been read by everyone
+    }
+    if (s1 > low) seg_products<H>(a.g, t, s0 > low ? s0 - low : 0, s1 - low, seg_lds, acc);
+    if (s0 == 0 && s1 == pairs) {
+      store_tile<T>(a, acc, t, row0, col0, inv);
+    } else {
+      floatx4* part = reinterpret_cast<floatx4*>(a.part + (2 * (int64_t)w + (pos == begin ? 0 : 1)) * PART_TILE) + threadIdx.x;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (col0 + 16 * j < a.tokens) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) part[(4 * i + j) * SEG_THREADS] = acc[i][j];
+        }
+    }
+    pos += s1 - s0;
+    __syncthreads();                                  // the LDS has been read by everyone
   }
 }
 
-int adapter_product_splits(int64_t features, int64_t tokens, int64_t depth, int dtype) {
-  return seg_splits(seg_tiles(features, tokens), up_to(depth, 64) / 64 * (dtype == LQ_T_FP32 ? 3 : 1), 16);
+// The parts of a tile that stretches end in, added in their order, the loads of four under way together.  A workgroup takes one of the
+// eight block rows.
+template <typename T>
+__global__ __launch_bounds__(SEG_THREADS) void adapter_join_kernel(AdapterArgs a) {
+  constexpr bool HALF = sizeof(T) == 4;
+  typedef T vec4 __attribute__((ext_vector_type(4)));
+  const int pairs = a.low.pairs + a.g.pairs, u = blockIdx.x, first = u * pairs, last = first + pairs, i = blockIdx.y;
+  int w = first / (a.per + 1);                        // not behind the stretch that the tile begins in
+  while (stretch_begin(a, w + 1) <= first) ++w;
+  if (stretch_begin(a, w + 1) >= last) return;        // whole: stored by the product
+  int end = w + 1;
+  while (end < a.stretches && stretch_begin(a, end) < last) ++end;
+  const SegTile t = seg_tile_at(a.g, u);
+  const int64_t row = (int64_t)t.tm * SEG_T + 128 * t.wm + 16 * i + 4 * t.kg, col0 = (int64_t)t.tn * SEG_T + 64 * t.wn + t.l16;
+  // of the tile that a stretch begins in, or, for the first one here, of that it ends in
+  const int head = stretch_begin(a, w) < first ? 1 : 0;
+  const floatx4* part = reinterpret_cast<const floatx4*>(a.part + 2 * (int64_t)w * PART_TILE) + threadIdx.x;
+  constexpr int64_t NEXT = 2 * PART_TILE / 4;
+  float inv[4];
+  token_factors<HALF>(a, col0, inv);
+  floatx4 v[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int p = 0; p < end - w; p += 4) {
+    floatx4 x[4][4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[q][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (p + q < end - w && col0 + 16 * j < a.tokens)
+          x[q][j] = part[(p + q) * NEXT + (p + q == 0 ? head : 0) * (PART_TILE / 4) + (4 * i + j) * SEG_THREADS];
+      }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] += x[q][j];
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int64_t token = col0 + 16 * j;
+    if (token < a.tokens && row < a.features)
+      *reinterpret_cast<vec4*>(static_cast<T*>(a.out) + token * a.features + row) = __builtin_convertvector(v[j] * inv[j], vec4);
+  }
+}
+
+// A stretch for every tile where that keeps half the chip busy, else one for every CU, of three pairs of steps at least.  Leaving CUs
+// idle costs less than their share, since the others then hold a higher clock: 1000 tokens x 11008 features, 172 tiles, fp32, the
+// whole call 402 us with a tile each, 432 with 256 stretches.
+static int tile_pairs(int64_t depth, int64_t depth2, int dtype) {
+  return (int)(depth / 64 * (dtype == LQ_T_FP32 ? 3 : 1) + depth2 / 64 * (dtype == LQ_T_FP32 ? 6 : 3));
+}
+static int adapter_stretches(int64_t features, int64_t tokens, int64_t depth, int64_t depth2, int dtype) {
+  const int64_t tiles = seg_tiles(features, tokens), rounds = (tiles + 255) / 256;
+  if (2 * tiles >= 256 * rounds) return (int)tiles;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(256, tiles * tile_pairs(depth, depth2, dtype) / 3));
+}
+size_t adapter_part_floats(int64_t features, int64_t tokens, int64_t depth, int64_t depth2, int dtype) {
+  const int s = adapter_stretches(features, tokens, depth, depth2, dtype);
+  return s == seg_tiles(features, tokens) ? 0 : (size_t)2 * s * PART_TILE;
 }
 
 template <typename H, typename T>
 static int launch_adapter(const AdapterArgs& a, hipStream_t st) {
   static LdsLimit limit;
   LQ_TRY(limit.raise(reinterpret_cast<const void*>(adapter_product_kernel<H, T>), SEG_LDS));
-  hipLaunchKernelGGL((adapter_product_kernel<H, T>), dim3(seg_grid(a.g)), dim3(SEG_THREADS), SEG_LDS, st, a);
+  hipLaunchKernelGGL((adapter_product_kernel<H, T>), dim3((unsigned)((a.stretches + 7) / 8 * 8)), dim3(SEG_THREADS), SEG_LDS, st, a);
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }
@@ -268,25 +349,27 @@ int launch_adapter_product(const Planes& a, const Planes& b, int64_t depth, cons
   add_segments(p.g, &count, a, b, depth);
   count = 0;
   add_segments(p.low, &count, a2, b2, depth2);
-  const int splits = adapter_product_splits(features, tokens, depth, dtype);
-  LQ_TRY(seg_shape(p.g, features, tokens, splits));
-  LQ_TRY(seg_shape(p.low, features, tokens, splits));
-  if (splits > 1 && part_floats < (size_t)splits * (size_t)tokens * (size_t)features) return LQ_ERR_WORKSPACE;
+  LQ_TRY(seg_shape(p.g, features, tokens, 1));
+  LQ_TRY(seg_shape(p.low, features, tokens, 1));
+  if (part_floats < adapter_part_floats(features, tokens, depth, depth2, dtype)) return LQ_ERR_WORKSPACE;
   p.s = s; p.features = features; p.tokens = tokens; p.out = out; p.part = part;
   p.masked = mask != nullptr;
   if (mask) p.mask = *mask;
+  const int64_t total = seg_tiles(features, tokens) * (p.low.pairs + p.g.pairs);
+  if (total >= (1ll << 31) - 256) return LQ_ERR_SHAPE;
+  p.stretches = adapter_stretches(features, tokens, depth, depth2, dtype);
+  p.per = (int)(total / p.stretches);
+  p.more = (int)(total % p.stretches);
   {
     prof::Scope ps(prof::ADAPTER_PRODUCT, st, 2.0 * features * tokens * (depth + depth2));
     LQ_TRY(dtype == LQ_T_BF16 ? (launch_adapter<__bf16, __bf16>(p, st)) : (launch_adapter<_Float16, float>(p, st)));
   }
-  if (splits == 1) return LQ_OK;
-  const int64_t quads = tokens * features / 4;
-  prof::Scope ps(prof::THIN_FINISH, st, (double)quads * 4 * (4.0 * splits + type_bytes(dtype)));
-  const dim3 grid((unsigned)std::min<int64_t>((quads + 255) / 256, 8192));
-  if (dtype == LQ_T_BF16)
-    hipLaunchKernelGGL(adapter_sum_kernel<__bf16>, grid, dim3(256), 0, st, part, splits, quads, static_cast<__bf16*>(out));
-  else
-    hipLaunchKernelGGL(adapter_sum_kernel<float>, grid, dim3(256), 0, st, part, splits, quads, static_cast<float*>(out));
+  const int64_t tiles = seg_tiles(features, tokens);
+  if (p.stretches == tiles) return LQ_OK;
+  prof::Scope ps(prof::THIN_FINISH, st, (double)tiles * PART_TILE * 12.0);
+  const dim3 grid((unsigned)tiles, 8);
+  if (dtype == LQ_T_BF16) hipLaunchKernelGGL(adapter_join_kernel<__bf16>, grid, dim3(SEG_THREADS), 0, st, p);
+  else hipLaunchKernelGGL(adapter_join_kernel<float>, grid, dim3(SEG_THREADS), 0, st, p);
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }

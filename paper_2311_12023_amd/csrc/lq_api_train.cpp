@@ -127,8 +127,7 @@ static void plan_product(AdapterPlan& p, Arena& a, int64_t m, int64_t features, 
   }
   p.inv = a.take<float>(half ? m : 0);
   p.top = a.take<uint32_t>(TOP_WORDS);
-  const int s = adapter_product_splits(features, m, depth, dtype);
-  p.part_floats = s > 1 ? (size_t)s * m * features : 0;
+  p.part_floats = adapter_part_floats(features, m, p.in64, p.r64, dtype);
   p.part = a.take<float>(p.part_floats);
 }
 static AdapterPlan plan_forward(void* ws, int64_t m, int64_t d, int64_t k, int rank, int dtype) {

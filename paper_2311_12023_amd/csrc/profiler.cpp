@@ -61,7 +61,7 @@ static const char* const kNames[NUM_CLASSES] = {
     "column_gemm_kernel<2,1>", "column_gemm_kernel<4,1>", "column_gemm_kernel<6,1>", "column_gemm_kernel<8,1>", "column_sum_kernel",
     "dropout_kernel", "row_planes_kernel+column_planes_kernel", "adapter_product_kernel",
     "loss_logits_kernel+loss_gradient_kernel", "loss_accumulate_kernel+loss_dw_kernel", "loss_rows_kernel+loss_join_kernel+loss_dx_kernel",
-    "thin_project_kernel", "thin_gram_kernel", "thin_finish_kernel+thin_gram_sum_kernel+adapter_sum_kernel"};
+    "thin_project_kernel", "thin_gram_kernel", "thin_finish_kernel+thin_gram_sum_kernel+adapter_join_kernel"};
 
 }  // namespace prof
 }  // namespace lq

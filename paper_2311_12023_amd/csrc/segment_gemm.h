@@ -19,21 +19,33 @@ struct SegTile {
 };
 typedef floatx4 SegAcc[8][4];
 
-// (tile, range) pairs are dealt to the 8 XCDs in contiguous stretches, four row tiles down before the next column, so that the
-// tiles an XCD works on at a time share operands in its L2.
-__device__ __forceinline__ SegTile seg_tile(const SegArgs& a) {
+// The wavefront's part of tile u, tiles in an order that goes down four row tiles before the next column.
+__device__ __forceinline__ SegTile seg_tile_at(const SegArgs& a, int u) {
   SegTile t;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   t.wm = wave >> 2; t.wn = wave & 3; t.l16 = lane & 15; t.kg = lane >> 4;
-  const int items = a.tiles_m * a.tiles_n * a.splits, per = (items + 7) / 8;
-  const int item = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
-  t.live = (int)(blockIdx.x >> 3) < per && item < items;
-  const int u = item / a.splits;
-  t.split = item - u * a.splits;
+  t.split = 0;
+  t.live = true;
   const int band = u / (4 * a.tiles_n), rows = a.tiles_m - 4 * band < 4 ? a.tiles_m - 4 * band : 4;
   const int inside = u - band * 4 * a.tiles_n;
   t.tm = 4 * band + inside % rows;
   t.tn = inside / rows;
+  return t;
+}
+
+// `count` pieces of work are dealt to the 8 XCDs in contiguous stretches, so that the tiles an XCD works on at a time share operands
+// in its L2.  -> this workgroup's piece, or -1.
+__device__ __forceinline__ int seg_piece(int count) {
+  const int per = (count + 7) / 8, item = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+  return (int)(blockIdx.x >> 3) < per && item < count ? item : -1;
+}
+
+// One (tile, range) pair a workgroup.
+__device__ __forceinline__ SegTile seg_tile(const SegArgs& a) {
+  const int item = seg_piece(a.tiles_m * a.tiles_n * a.splits), u = item < 0 ? 0 : item / a.splits;
+  SegTile t = seg_tile_at(a, u);
+  t.split = item - u * a.splits;
+  t.live = item >= 0;
   return t;
 }
 

@@ -27,10 +27,10 @@ __global__ __launch_bounds__(256) void thin_project_kernel(ProjectArgs a) {
   thin_store(acc, a.part + (size_t)blockIdx.y * (size_t)a.a.m * (16 * RT), row0, a.a.m);
 }
 
-// As many ranges as leave two workgroups a CU, each with four steps.
+// As many ranges as leave two workgroups a CU, each with two steps.
 int thin_project_splits(int64_t m, int64_t K) {
   const int64_t wgs = (m + 127) / 128, steps = (K + 63) / 64;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({512 / wgs, steps / 4, 16}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({512 / wgs, steps / 2, 16}));
 }
 
 template <typename T, int RT>

@@ -205,7 +205,7 @@ int launch_weight_planes(const MvWeights& q, int64_t K, int64_t N, bool transpos
 // out (tokens x features, of type dtype) = B A^T + mask .* (B2 A2^T): A the weights (features x depth), B the activations
 // (tokens x depth), A2 and B2 the low-rank part (depth2; three planes each).  mask: NULL for none.  fp32: b_inv, a_top scale A B.
 struct AdapterScales { const float* b_inv; const uint32_t* a_top; };
-int adapter_product_splits(int64_t features, int64_t tokens, int64_t depth, int dtype);
+size_t adapter_part_floats(int64_t features, int64_t tokens, int64_t depth, int64_t depth2, int dtype);
 int launch_adapter_product(const Planes& a, const Planes& b, int64_t depth, const Planes& a2, const Planes& b2, int64_t depth2,
                            const AdapterScales& s, int64_t features, int64_t tokens, const DropoutMask* mask, int dtype, void* out,
                            float* part, size_t part_floats, hipStream_t st);
