@@ -68,8 +68,8 @@ __device__ __forceinline__ int seg_first(int pairs, int split, int splits) { ret
 // without products: 128 us, with steps on their own 167).  One barrier per step: past it everyone has the operands of the step in
 // registers, and its slot is free; the operands of the next step are read between the products.  Products are 16 x 16 x 32: blocks
 // of 32 x 32 x 16 take the same cycles, but the chip, which lowers its clock under this load, holds 1.9 GHz with these and 1.65 with
-// those (1368 against 1220 TFLOP/s, call after call).  Rows are 64 bytes, unit u of a row stored at u ^ ((row / 4) % 4): the
-// 16 lanes that read one unit of 16 rows fall into different banks.
+// those (1368 against 1220 TFLOP/s, call after call).  Rows are 64 bytes, unit u of a row stored at u ^ ((row / 2) % 4): reads
+// of 16 rows x 4 units take 4 cycles of the LDS (with (row / 4) % 4, which serves 32 rows x 2 units, 8).
 //
 // TURNED: A's planes have its rows contiguous and the reduction index from row to row (W as it is stored, for E W), so a step is 32
 // rows of 512 bytes in LDS and operands come out by transposed reads: 16 lanes read four reduction indices of 16 rows of A, a
@@ -80,7 +80,7 @@ __device__ __forceinline__ void seg_products(const SegArgs& a, const SegTile& t,
   typedef H hx8 __attribute__((ext_vector_type(8)));
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   // this wavefront's transfers: rows 32 wave .. + 31 of both tiles; lane l brings unit l % 4 ^ swizzle of row l / 4
-  const int lrow = lane >> 2, unit = (lane & 3) ^ ((lrow >> 2) & 3);
+  const int lrow = lane >> 2, unit = (lane & 3) ^ ((lrow >> 1) & 3);
   const int64_t arow = (int64_t)t.tm * SEG_T, brow = (int64_t)t.tn * SEG_T;
   int ra[2], rb[2];
 #pragma unroll
@@ -143,7 +143,7 @@ __device__ __forceinline__ void seg_products(const SegArgs& a, const SegTile& t,
       pa += 64;
     }
   };
-  const uint32_t u0 = (uint32_t)(t.kg ^ ((t.l16 >> 2) & 3)) * 16u;
+  const uint32_t u0 = (uint32_t)(t.kg ^ ((t.l16 >> 1) & 3)) * 16u;
   // TURNED: index 8 kg + l16 / 4 of a step (and four further), chunk 8 wm + i: the swizzle takes in the indices' low bits and kg
   const uint32_t turn = (uint32_t)((t.l16 >> 2) + 4 * (t.kg & 1));
   const uint32_t aoff = TURNED ? (uint32_t)(8 * t.kg + (t.l16 >> 2)) * 512u + 8u * (t.l16 & 3) : (uint32_t)(128 * t.wm + t.l16) * 64u + u0, boff = SEG_TILE + (uint32_t)(64 * t.wn + t.l16) * 64u + u0;
