@@ -158,7 +158,7 @@ struct ShiftStage {
 };
 
 template <typename T, int RT, bool VEC>
-__global__ __launch_bounds__(256) void few_dx_kernel(FewDxArgs a) {
+__global__ __launch_bounds__(256, (thin_columns_waves<T, RT>())) void few_dx_kernel(FewDxArgs a) {
   constexpr int NB = thin_planes<T>();
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const int64_t c0 = (int64_t)blockIdx.x * 128;

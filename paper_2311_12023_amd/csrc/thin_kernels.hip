@@ -126,7 +126,7 @@ struct GramArgs {
 };
 
 template <typename T, int RT>
-__global__ __launch_bounds__(256) void thin_gram_kernel(GramArgs a) {
+__global__ __launch_bounds__(256, (thin_columns_waves<T, RT>())) void thin_gram_kernel(GramArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const int which = (int)blockIdx.x >= a.wgs0, wg = blockIdx.x - (which ? a.wgs0 : 0);
   const ThinSource& src = a.a[which];
