@@ -18,63 +18,73 @@ struct FewLogitsArgs {
   int steps;
 };
 
-// A workgroup owns 64 classes, a wavefront 16, and all tokens.
+// A workgroup owns H tiles of 64 classes, a wavefront 16 of each, and all tokens.  In fp32 X's three planes outweigh W's 64 classes:
+// two tiles share them up to 64 tokens (above, their sums would not fit the registers).
+template <typename T, int RT> constexpr int few_tiles() { return sizeof(T) == 4 && RT <= 4 ? 2 : 1; }
 template <typename T, int RT, bool VEC>
 __global__ __launch_bounds__(256) void few_logits_kernel(FewLogitsArgs a) {
-  constexpr int NB = thin_planes<T>();
+  constexpr int NB = thin_planes<T>(), H = few_tiles<T, RT>(), TILE = LOSS_FEW_TILE;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  __shared__ float s_max[4][16 * RT], s_sum[4][16 * RT];
+  __shared__ float s_max[H][4][16 * RT], s_sum[H][4][16 * RT];
   const int wave = threadIdx.x >> 6, l16 = threadIdx.x & 15, kg = (threadIdx.x & 63) >> 4;
-  const int64_t class0 = (int64_t)blockIdx.x * LOSS_FEW_TILE + 16 * wave + 4 * kg;         // of this lane's four
-  floatx4 acc[1][RT];
+  const int64_t tile0 = (int64_t)blockIdx.x * H, class0 = tile0 * TILE + 16 * wave + 4 * kg;         // of this lane's four
+  floatx4 acc[H][RT];
   thin_clear(acc);
-  thin_rows<T, 1, RT, NB, false, VEC>(a.w, a.x, (int64_t)blockIdx.x * LOSS_FEW_TILE + 16 * wave, 0, a.steps, lds, acc);
+  thin_rows<T, H, TILE, RT, NB, false, VEC>(a.w, a.x, tile0 * TILE + 16 * wave, 0, a.steps, lds, acc);
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     const int64_t token = 16 * r + l16;
     const int64_t target = token < a.p.n ? a.p.targets[token] : -1;
-    float top = -__builtin_inff();
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float x = acc[0][r][e] * LOG2E;
-      if (class0 + e >= a.p.vocab) x = -__builtin_inff();
-      else if (class0 + e == target) { a.target[token] = x; x = -__builtin_inff(); }
-      acc[0][r][e] = x;
-      top = fmaxf(top, x);
-    }
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    s_max[wave][token] = top;
-  }
-  __syncthreads();
+    for (int h = 0; h < H; ++h) {
+      float top = -__builtin_inff();
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    const int64_t token = 16 * r + l16;
-    const float ref = ceilf(fmaxf(fmaxf(s_max[0][token], s_max[1][token]), fmaxf(s_max[2][token], s_max[3][token])));
-    const float from = ref == -__builtin_inff() ? 0.0f : ref;
-    float sum = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      acc[0][r][e] = __builtin_amdgcn_exp2f(acc[0][r][e] - from);
-      sum += acc[0][r][e];
-    }
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    s_sum[wave][token] = sum;
-    if (wave == 0 && kg == 0 && token < a.p.n) a.part_ref[(int64_t)blockIdx.x * a.p.n + token] = ref;
-    if (a.e[0] && token < a.p.n) {                       // rows of E end on whole tiles
-      bf16x2 p0[3], p1[3];
-      split_bf16_3(floatx2{acc[0][r][0], acc[0][r][1]}, p0);
-      split_bf16_3(floatx2{acc[0][r][2], acc[0][r][3]}, p1);
-#pragma unroll
-      for (int k = 0; k < NB; ++k)
-        *reinterpret_cast<bf16x4*>(a.e[k] + token * a.e_pitch + class0) = bf16x4{p0[k][0], p0[k][1], p1[k][0], p1[k][1]};
+      for (int e = 0; e < 4; ++e) {
+        const int64_t c = class0 + TILE * h + e;
+        float x = acc[h][r][e] * LOG2E;
+        if (c >= a.p.vocab) x = -__builtin_inff();
+        else if (c == target) { a.target[token] = x; x = -__builtin_inff(); }
+        acc[h][r][e] = x;
+        top = fmaxf(top, x);
+      }
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      s_max[h][wave][token] = top;
     }
   }
   __syncthreads();
-  const int token = threadIdx.x;
-  if (token < 16 * RT && token < a.p.n)
-    a.part_sum[(int64_t)blockIdx.x * a.p.n + token] = (s_sum[0][token] + s_sum[1][token]) + (s_sum[2][token] + s_sum[3][token]);
+#pragma unroll
+  for (int h = 0; h < H; ++h) {
+    if ((tile0 + h) * TILE >= a.p.vocab) break;          // the same for all of the workgroup
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      const int64_t token = 16 * r + l16;
+      const float ref = ceilf(fmaxf(fmaxf(s_max[h][0][token], s_max[h][1][token]), fmaxf(s_max[h][2][token], s_max[h][3][token])));
+      const float from = ref == -__builtin_inff() ? 0.0f : ref;
+      float sum = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        acc[h][r][e] = __builtin_amdgcn_exp2f(acc[h][r][e] - from);
+        sum += acc[h][r][e];
+      }
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      s_sum[h][wave][token] = sum;
+      if (wave == 0 && kg == 0 && token < a.p.n) a.part_ref[(tile0 + h) * a.p.n + token] = ref;
+      if (a.e[0] && token < a.p.n) {                     // rows of E end on whole tiles
+        bf16x2 p0[3], p1[3];
+        split_bf16_3(floatx2{acc[h][r][0], acc[h][r][1]}, p0);
+        split_bf16_3(floatx2{acc[h][r][2], acc[h][r][3]}, p1);
+#pragma unroll
+        for (int k = 0; k < NB; ++k)
+          *reinterpret_cast<bf16x4*>(a.e[k] + token * a.e_pitch + class0 + TILE * h) = bf16x4{p0[k][0], p0[k][1], p1[k][0], p1[k][1]};
+      }
+    }
+  }
+  __syncthreads();
+  const int h = threadIdx.x / (16 * RT), token = threadIdx.x % (16 * RT);
+  if (h < H && token < a.p.n && (tile0 + h) * TILE < a.p.vocab)
+    a.part_sum[(tile0 + h) * a.p.n + token] = (s_sum[h][0][token] + s_sum[h][1][token]) + (s_sum[h][2][token] + s_sum[h][3][token]);
 }
 
 static bool rows_fit(const void* W, int64_t ldw, int dtype, int64_t d) {
@@ -82,21 +92,22 @@ static bool rows_fit(const void* W, int64_t ldw, int dtype, int64_t d) {
 }
 
 template <typename T, int RT, bool VEC>
-static int few_logits(const FewLogitsArgs& a, dim3 grid, hipStream_t st) {
+static int few_logits(const FewLogitsArgs& a, hipStream_t st) {
   static LdsLimit limit;
   constexpr size_t lds = 2 * ThinStage<RT, thin_planes<T>()>::BYTES;
+  constexpr int64_t classes = few_tiles<T, RT>() * LOSS_FEW_TILE;
   LQ_TRY(limit.raise(reinterpret_cast<const void*>(few_logits_kernel<T, RT, VEC>), lds));
-  hipLaunchKernelGGL((few_logits_kernel<T, RT, VEC>), grid, dim3(256), lds, st, a);
+  hipLaunchKernelGGL((few_logits_kernel<T, RT, VEC>), dim3((unsigned)((a.p.vocab + classes - 1) / classes)), dim3(256), lds, st, a);
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }
 template <typename T>
-static int few_logits_of(const FewLogitsArgs& a, bool vec, dim3 grid, hipStream_t st) {
+static int few_logits_of(const FewLogitsArgs& a, bool vec, hipStream_t st) {
   switch (few_rows(a.p.n)) {
-    case 16: return vec ? few_logits<T, 1, true>(a, grid, st) : few_logits<T, 1, false>(a, grid, st);
-    case 32: return vec ? few_logits<T, 2, true>(a, grid, st) : few_logits<T, 2, false>(a, grid, st);
-    case 64: return vec ? few_logits<T, 4, true>(a, grid, st) : few_logits<T, 4, false>(a, grid, st);
-    default: return vec ? few_logits<T, 8, true>(a, grid, st) : few_logits<T, 8, false>(a, grid, st);
+    case 16: return vec ? few_logits<T, 1, true>(a, st) : few_logits<T, 1, false>(a, st);
+    case 32: return vec ? few_logits<T, 2, true>(a, st) : few_logits<T, 2, false>(a, st);
+    case 64: return vec ? few_logits<T, 4, true>(a, st) : few_logits<T, 4, false>(a, st);
+    default: return vec ? few_logits<T, 8, true>(a, st) : few_logits<T, 8, false>(a, st);
   }
 }
 
@@ -111,10 +122,9 @@ int launch_few_logits(const void* W, int64_t ldw, int dtype, int64_t d, const Pl
   for (int k = 0; k < 3; ++k) a.e[k] = e[k];
   a.e_pitch = e_pitch;
   a.steps = (int)((d + 63) / 64);
-  const dim3 grid((unsigned)((p.vocab + LOSS_FEW_TILE - 1) / LOSS_FEW_TILE));
   prof::Scope ps(prof::LOSS_LOGITS, st, 2.0 * p.n * p.vocab * d);
   const bool vec = rows_fit(W, ldw, dtype, d);
-  return dtype == LQ_T_BF16 ? few_logits_of<__bf16>(a, vec, grid, st) : few_logits_of<float>(a, vec, grid, st);
+  return dtype == LQ_T_BF16 ? few_logits_of<__bf16>(a, vec, st) : few_logits_of<float>(a, vec, st);
 }
 
 // ------------------------------------------------------------------------------------------------

@@ -600,10 +600,12 @@ int launch_loss_gradient(const Planes& w, const Planes& x, int64_t depth, const 
 
 // ------------------------------------------------------------------------------------------------
 // The same from E (both planes), where one piece is the whole vocabulary: p = E (1 - p_t) / S, a pass over E for a product less
-// (2047 x 32000, d = 4096).  A workgroup turns 64 tokens x 64 classes in LDS, a thread two tokens of eight classes.
+// (2047 x 32000, d = 4096).  A workgroup turns 64 tokens x 64 classes in LDS, a thread two tokens of eight classes.  part_ref: E is
+// still relative to its tile's power of two, and goes back relative to the row's (keep: dX needs it) in the same pass.
 struct FromEArgs {
   LossPiece p; LossRows r;
-  const uint16_t* e[2]; int64_t e_pitch;
+  const float* part_ref; int keep;
+  uint16_t* e[2]; int64_t e_pitch;
   uint16_t* out[2]; int64_t pitch;
   int tiles_r;
 };
@@ -622,12 +624,23 @@ __global__ __launch_bounds__(256) void loss_gradient_from_e_kernel(FromEArgs a) 
 #pragma unroll
     for (int j = 0; j < 8; ++j) g[h][j] = 0.0f;
     const int64_t token = r0 + 2 * pair + h, t = token < a.p.n ? a.p.targets[token] : -1;
+    float shift = 1.0f;
+    if constexpr (HALF)
+      if (a.part_ref && token < a.p.n) {
+        const float ref = a.r.ref[token], mine = a.part_ref[c0 / SEG_T * a.p.n + token];
+        if (mine != ref) shift = __builtin_amdgcn_exp2f(mine - ref);
+      }
     if (t < 0 || t >= a.p.vocab) continue;                   // rows that do not count: whatever they hold
     const float s = a.r.sum[token], wrong = a.r.wrong[token];
     const float f = s == 0.0f ? 0.0f : wrong / s * (HALF ? power_of_two(LOSS_G_SHIFT - LOSS_E_SHIFT) : 1.0f);
     const int64_t at = token * a.e_pitch + c0 + c;           // rows of E end on whole tiles
-    const hx8 hi = *reinterpret_cast<const hx8*>(a.e[0] + at);
-    const hx8 lo = *reinterpret_cast<const hx8*>(a.e[1] + at);
+    hx8 hi = *reinterpret_cast<const hx8*>(a.e[0] + at);
+    hx8 lo = *reinterpret_cast<const hx8*>(a.e[1] + at);
+    if (HALF && shift != 1.0f) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) { hi[j] = (H)((float)hi[j] * shift); lo[j] = (H)((float)lo[j] * shift); }
+      if (a.keep) { *reinterpret_cast<hx8*>(a.e[0] + at) = hi; *reinterpret_cast<hx8*>(a.e[1] + at) = lo; }
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       g[h][j] = ((float)hi[j] + (float)lo[j]) * f;
@@ -655,11 +668,12 @@ __global__ __launch_bounds__(256) void loss_gradient_from_e_kernel(FromEArgs a) 
   }
 }
 
-int launch_loss_gradient_from_e(const LossPiece& p, const LossRows& r, bool half, uint16_t* const e[2], int64_t e_pitch,
-                                uint16_t* const g[2], int64_t g_pitch, hipStream_t st) {
+int launch_loss_gradient_from_e(const LossPiece& p, const LossRows& r, bool half, const float* part_ref, bool keep,
+                                uint16_t* const e[2], int64_t e_pitch, uint16_t* const g[2], int64_t g_pitch, hipStream_t st) {
   const int64_t tr = (p.n + 63) / 64, tc = (p.classes + 63) / 64;
   if (p.v0 != 0 || p.classes != p.vocab || g_pitch < up_to(p.n, 64) || tr * tc >= (1ll << 31)) return LQ_ERR_SHAPE;
-  const FromEArgs a{p, r, {e[0], e[1]}, e_pitch, {g[0], g[1]}, g_pitch, (int)tr};
+  if (part_ref && !half) return LQ_ERR_ARG;
+  const FromEArgs a{p, r, part_ref, (int)keep, {e[0], e[1]}, e_pitch, {g[0], g[1]}, g_pitch, (int)tr};
   prof::Scope ps(prof::TRAIN_PLANES, st, (double)p.n * p.classes * (half ? 8.0 : 6.0));
   auto kernel = half ? loss_gradient_from_e_kernel<_Float16> : loss_gradient_from_e_kernel<__bf16>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)(tr * tc)), dim3(256), 0, st, a);

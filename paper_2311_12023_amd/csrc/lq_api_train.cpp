@@ -171,12 +171,10 @@ static int activation_planes(const AdapterPlan& p, const MvWeights& q, int64_t w
   LQ_TRY(jobs.tops(q.v, (weights + group - 1) / group, p.top));       // no weight is larger than its group's scale
   return jobs.rows_scaled(s, t, p.inv);
 }
-static int weight_planes(const AdapterPlan& p, const MvWeights& q, int64_t d, int64_t k, bool transposed, int dtype, Planes* w,
-                         hipStream_t st) {
-  uint16_t* lo = dtype == LQ_T_FP32 ? p.q[1] : nullptr;
-  *w = Planes{{p.q[0], lo, nullptr}, p.in64};
-  return launch_weight_planes(q, d, k, transposed, p.top, p.q[0], lo, p.in64, st);
+static WeightPlanes weight_planes(const AdapterPlan& p, const MvWeights& q, int64_t d, int64_t k, bool transposed, int dtype) {
+  return WeightPlanes{q, d, k, transposed, p.top, p.q[0], dtype == LQ_T_FP32 ? p.q[1] : nullptr, p.in64};
 }
+static Planes planes_of(const WeightPlanes& w) { return Planes{{w.hi, w.lo, nullptr}, w.pitch}; }
 
 // The low-rank part in the large product: two of its planes (16 bits) where the result is bf16, all three where it is fp32.
 static Planes low_rank_planes(const PlaneTarget& t, int dtype) {
@@ -274,18 +272,26 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
   uint16_t* const none[2] = {nullptr, nullptr};
   if (!few && !half) LQ_TRY(launch_loss_reference(X, ldx, W, ldw, d, all, p.rows, st));
   const bool want_e = dX || (dW && p.whole);
+  const bool late = half && dW && p.whole;      // the pass that makes dW's operand of E brings it to one power of two per row as well
+  auto accumulate = [&](const LossPiece& piece, const Planes& w) {
+    return launch_loss_accumulate(Planes{{p.e[0], half ? p.e[1] : nullptr, nullptr}, p.classes}, w, piece.classes, n, d, p.rows.shift,
+                                  piece.v0 == 0, p.acc, p.part, p.part_floats, st);
+  };
+  Planes whole;
   for (int64_t v0 = 0; !few && v0 < vocab; v0 += p.classes) {
     const LossPiece piece{n, v0, std::min(p.classes, vocab - v0), vocab, targets};
     Planes w;
     LQ_TRY(piece_planes(v0, piece.classes, &w));
     LQ_TRY(launch_loss_logits(w, x, p.d64, piece, p.rows, scales, p.part_ref, p.part_sum, want_e ? p.e : none, p.classes, st));
-    LQ_TRY(launch_loss_join(piece, p.rows, half, !half, p.part_ref, p.part_sum, SEG_T, want_e ? p.e : none, p.classes, st));
-    if (!dX) continue;
-    LQ_TRY(launch_loss_accumulate(Planes{{p.e[0], half ? p.e[1] : nullptr, nullptr}, p.classes}, w, piece.classes, n, d, p.rows.shift,
-                                  v0 == 0, p.acc, p.part, p.part_floats, st));
+    LQ_TRY(launch_loss_join(piece, p.rows, half, !half, p.part_ref, p.part_sum, SEG_T, want_e && !late ? p.e : none, p.classes, st));
+    if (late) whole = w;
+    else if (dX) LQ_TRY(accumulate(piece, w));
   }
   if (scales.xt_top) LQ_TRY(launch_top_magnitude(X, ldx, n, d, targets, vocab, p.tops + 1, st));
   if (!join_rows) LQ_TRY(launch_loss_rows(p.rows, scales, targets, n, vocab, mean == 1, loss, row_loss, lse, p.factors, st));
+  if (dW && p.whole)
+    LQ_TRY(launch_loss_gradient_from_e(all, p.rows, half, late ? p.part_ref : nullptr, dX != nullptr, p.e, p.classes, p.g, p.n64, st));
+  if (late && dX) LQ_TRY(accumulate(all, whole));
   if (dX && few) {
     LQ_TRY(launch_few_dx(W, ldw, dtype, d, Planes{{p.few_e[0], p.few_e[1], p.few_e[2]}, p.v64}, all, p.rows, p.part_ref, p.factors,
                          p.few_part, dX, st));
@@ -297,9 +303,7 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
   LQ_TRY(launch_column_planes({X, dtype, ldx, n, d, p.tops + 1}, kind, xt, targets, vocab, st));
   for (int64_t v0 = 0; v0 < vocab; v0 += p.classes) {
     const LossPiece piece{n, v0, std::min(p.classes, vocab - v0), vocab, targets};
-    if (p.whole) {
-      LQ_TRY(launch_loss_gradient_from_e(piece, p.rows, half, p.e, p.classes, p.g, p.n64, st));
-    } else {
+    if (!p.whole) {
       Planes w;
       LQ_TRY(piece_planes(v0, piece.classes, &w));
       LQ_TRY(launch_loss_gradient(w, x, p.d64, piece, p.rows, scales, p.g, p.n64, st));
@@ -331,15 +335,15 @@ int lq_adapter_forward(const void* X, int64_t m, int64_t d, int64_t k, const uin
   const PlaneTarget l1{{w.b[0], w.b[1], w.b[2]}, up_to(d, 64), w.r32}, none{};
   const PlaneTarget t{{w.b2[0], w.b2[1], w.b2[2]}, w.r64, m}, l2{{w.a2[0], w.a2[1], w.a2[2]}, w.r64, k};
   PrepareJobs jobs{};
-  Planes weights, act;
+  Planes act;
   LQ_TRY(jobs.columns3({L1, LQ_T_FP32, rank, d, rank, nullptr}, l1));
   LQ_TRY(jobs.columns3({L2, LQ_T_FP32, k, rank, k, nullptr}, l2));
   LQ_TRY(activation_planes(w, q, d * k, X, m, d, dtype, jobs, &act));
   LQ_TRY(jobs.launch(st));
   LQ_TRY(launch_thin_project(X, dtype, m, d, planes_of(l1), r32, mask, w.thin, st));
-  LQ_TRY(launch_thin_finish(w.thin, thin_project_splits(m, d), m, rank, r32, mask.scale, T, t, none, st));
-  LQ_TRY(weight_planes(w, q, d, k, true, dtype, &weights, st));
-  return launch_adapter_product(weights, act, w.in64, low_rank_planes(l2, dtype), low_rank_planes(t, dtype), w.r64, {w.inv, w.top}, k, m,
+  const WeightPlanes weights = weight_planes(w, q, d, k, true, dtype);
+  LQ_TRY(launch_finish({w.thin, thin_project_splits(m, d), m, rank, r32, mask.scale, T, t, none}, &weights, st));
+  return launch_adapter_product(planes_of(weights), act, w.in64, low_rank_planes(l2, dtype), low_rank_planes(t, dtype), w.r64, {w.inv, w.top}, k, m,
                                 nullptr, dtype, Y, w.part, w.part_floats, st);
 }
 
@@ -363,7 +367,7 @@ int lq_adapter_backward(const void* dY, const void* X, int64_t m, int64_t d, int
   const PlaneTarget u{{w.b2[0], w.b2[1], w.b2[2]}, w.r64, m}, l1{{w.a2[0], w.a2[1], w.a2[2]}, w.r64, d};
   const PlaneTarget ut{{w.ut[0], w.ut[1], w.ut[2]}, w.m64, w.r32}, tt{{w.tt[0], w.tt[1], w.tt[2]}, w.m64, w.r32};
   PrepareJobs jobs{};
-  Planes weights, act;
+  Planes act;
   LQ_TRY(jobs.rows3({L2, LQ_T_FP32, k, rank, k, nullptr}, l2));
   LQ_TRY(jobs.columns3({T, LQ_T_FP32, rank, m, rank, nullptr}, tt));
   if (dX) {
@@ -372,11 +376,15 @@ int lq_adapter_backward(const void* dY, const void* X, int64_t m, int64_t d, int
   }
   LQ_TRY(jobs.launch(st));
   LQ_TRY(launch_thin_project(dY, dtype, m, k, planes_of(l2), r32, DropoutMask{}, w.thin, st));
-  LQ_TRY(launch_thin_finish(w.thin, thin_project_splits(m, k), m, rank, r32, 1.0f, nullptr, u, ut, st));
-  LQ_TRY(launch_thin_grams(dY, k, planes_of(tt), dL2, X, d, planes_of(ut), mask, dL1, dtype, m, rank, r32, w.thin, st));
+  const ThinFinish finish{w.thin, thin_project_splits(m, k), m, rank, r32, 1.0f, nullptr, u, ut};
+  const WeightPlanes weights = weight_planes(w, q, d, k, false, dtype);
+  const bool sums = thin_gram_splits(m, k, d) > 1;
+  LQ_TRY(launch_finish(finish, dX && !sums ? &weights : nullptr, st));
+  ThinGramSum sum;
+  LQ_TRY(launch_thin_grams(dY, k, planes_of(tt), dL2, X, d, planes_of(ut), mask, dL1, dtype, m, rank, r32, w.thin, &sum, st));
+  if (sums) LQ_TRY(launch_gram_sum(sum, dX ? &weights : nullptr, st));
   if (!dX) return LQ_OK;
-  LQ_TRY(weight_planes(w, q, d, k, false, dtype, &weights, st));
-  return launch_adapter_product(weights, act, w.in64, low_rank_planes(l1, dtype), low_rank_planes(u, dtype), w.r64, {w.inv, w.top}, d, m,
+  return launch_adapter_product(planes_of(weights), act, w.in64, low_rank_planes(l1, dtype), low_rank_planes(u, dtype), w.r64, {w.inv, w.top}, d, m,
                                 mask.cut ? &mask : nullptr, dtype, dX, w.part, w.part_floats, st);
 }
 

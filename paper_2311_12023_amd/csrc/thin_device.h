@@ -127,8 +127,8 @@ __device__ __forceinline__ void thin_read(const unsigned char* lds, int r, int s
 // 16-byte addresses and K a multiple of 8.
 struct ThinSource { const void* A; int64_t lda, m, K; DropoutMask d; };
 
-// acc[h][r] += drop(A) B^T over steps s0 .. s1 - 1 (s0 < s1) for rows row0 + 16 h ..: element e is row 4 kg + e, column 16 r + l16.
-template <typename T, int H, int RT, int NB, bool MASKED, bool VEC>
+// acc[h][r] += drop(A) B^T over steps s0 .. s1 - 1 (s0 < s1) for rows row0 + APART h ..: element e is row 4 kg + e, column 16 r + l16.
+template <typename T, int H, int APART, int RT, int NB, bool MASKED, bool VEC>
 __device__ __forceinline__ void thin_rows(const ThinSource& a, const Planes& b, int64_t row0, int s0, int s1, unsigned char* lds,
                                           floatx4 (&acc)[H][RT]) {
   typedef ThinStage<RT, NB> Stage;
@@ -138,7 +138,7 @@ __device__ __forceinline__ void thin_rows(const ThinSource& a, const Planes& b, 
   uint64_t group[H];
 #pragma unroll
   for (int h = 0; h < H; ++h) {
-    const int64_t r = row0 + 16 * h + l16, row = r < a.m ? r : a.m - 1;
+    const int64_t r = row0 + APART * h + l16, row = r < a.m ? r : a.m - 1;
     x[h] = static_cast<const T*>(a.A) + row * a.lda;
     group[h] = (uint64_t)row * (uint64_t)(a.K >> 3);
   }

@@ -160,9 +160,10 @@ int launch_loss_dx(const LossRows& r, const LossScales& s, const int64_t* target
 // to up_to(n, 64).
 int launch_loss_gradient(const Planes& w, const Planes& x, int64_t depth, const LossPiece& p, const LossRows& r, const LossScales& s,
                          uint16_t* const g[2], int64_t g_pitch, hipStream_t st);
-// The same from E where one piece is the whole vocabulary.
-int launch_loss_gradient_from_e(const LossPiece& p, const LossRows& r, bool half, uint16_t* const e[2], int64_t e_pitch,
-                                uint16_t* const g[2], int64_t g_pitch, hipStream_t st);
+// The same from E where one piece is the whole vocabulary.  part_ref (fp32; NULL where E is relative to its rows' powers of two): E is
+// relative to its tiles', and with keep goes back relative to its rows'.
+int launch_loss_gradient_from_e(const LossPiece& p, const LossRows& r, bool half, const float* part_ref, bool keep,
+                                uint16_t* const e[2], int64_t e_pitch, uint16_t* const g[2], int64_t g_pitch, hipStream_t st);
 // dW's rows: out (rows x cols, contiguous, of type dtype) = *factor A B^T.  part: splits x rows x cols floats.
 int loss_dw_splits(int64_t rows, int64_t cols, int64_t depth, bool half);
 int launch_loss_dw(const Planes& g, const Planes& xt, int64_t depth, int64_t rows, int64_t cols, const float* factor, int dtype,
@@ -190,18 +191,28 @@ int launch_thin_project(const void* A, int dtype, int64_t m, int64_t K, const Pl
                         hipStream_t st);
 // T = scale * sum of the partial results: fp32 m x rank (NULL: not wanted), three planes m x up_to(r32, 64) and three of the
 // transpose, r32 x up_to(m, 64) (p[0] NULL: not wanted).
-int launch_thin_finish(const float* part, int splits, int64_t m, int rank, int r32, float scale, float* T, const PlaneTarget& rows,
-                       const PlaneTarget& cols, hipStream_t st);
+struct ThinFinish {
+  const float* part; int splits; int64_t m; int rank, r32; float scale;
+  float* T; PlaneTarget rows, cols;
+};
+// The stored weights (K x N, row-major) as planes, row by row (zero from N to up_to(N, 64)) or transposed (N rows, zero from K to
+// up_to(K, 64)): one bf16 plane, or two fp16 planes times the power of two that the largest of the TOP_WORDS words at `top` (of the
+// group scales v) gives.
+struct WeightPlanes {
+  MvWeights q; int64_t K, N; bool transposed;
+  const uint32_t* top; uint16_t *hi, *lo; int64_t pitch;
+};
 // dL2 (rank x k) = T^T dY and dL1 (d x rank) = drop(X)^T U; T^T and U^T as three planes of r32 rows x up_to(m, 64).
-// part: thin_gram_splits(m, k, d) x (k + d) x r32 floats.
+// part: thin_gram_splits(m, k, d) x (k + d) x r32 floats; with more than one range the results are left in there, and *sum makes
+// them of it.
+struct ThinGramSum { const float* part[2]; int splits; int64_t K[2]; int rank, r32; float scale; float* out[2]; };
 int thin_gram_splits(int64_t m, int64_t k, int64_t d);
 int launch_thin_grams(const void* dY, int64_t k, const Planes& tt, float* dL2, const void* X, int64_t d, const Planes& ut,
-                      const DropoutMask& mask, float* dL1, int dtype, int64_t m, int rank, int r32, float* part, hipStream_t st);
-// The stored weights (K x N, row-major) as planes, row by row (zero from N to up_to(N, 64)) or transposed (N rows, zero from K to
-// up_to(K, 64)): one bf16 plane, or two fp16 planes times the power of two that the largest of the
-// TOP_WORDS words at `top` (of the group scales v) gives.
-int launch_weight_planes(const MvWeights& q, int64_t K, int64_t N, bool transposed, const uint32_t* top, uint16_t* hi, uint16_t* lo,
-                         int64_t pitch, hipStream_t st);
+                      const DropoutMask& mask, float* dL1, int dtype, int64_t m, int rank, int r32, float* part, ThinGramSum* sum,
+                      hipStream_t st);
+// A pass over partial results, and the weights' planes beside it in the same launch (adapter_kernels.hip); weights NULL: not wanted.
+int launch_finish(const ThinFinish& f, const WeightPlanes* weights, hipStream_t st);
+int launch_gram_sum(const ThinGramSum& g, const WeightPlanes* weights, hipStream_t st);
 // out (tokens x features, of type dtype) = B A^T + mask .* (B2 A2^T): A the weights (features x depth), B the activations
 // (tokens x depth), A2 and B2 the low-rank part (depth2; three planes each).  mask: NULL for none.  fp32: b_inv, a_top scale A B.
 struct AdapterScales { const float* b_inv; const uint32_t* a_top; };
