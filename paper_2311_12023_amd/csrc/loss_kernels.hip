@@ -266,7 +266,7 @@ __device__ __forceinline__ void finish_rows(const RowsArgs& a) {
     const double f = a.mean ? 1.0 / (double)(s_count[0] ? s_count[0] : 1) : 1.0;      // no row counts: the mean is 0
     *a.loss = (float)(s_sum[0] * f);
     a.factors[0] = (float)f;
-    a.factors[1] = a.s.xt_top ? (float)f * power_of_two(-LOSS_G_SHIFT) * power_of_two(-half_exponent(*a.s.xt_top)) : (float)f;
+    a.factors[1] = a.s.xt_top ? (float)f * power_of_two(-half_exponent(*a.s.xt_top)) : (float)f;
   }
 }
 
@@ -524,11 +524,12 @@ int launch_loss_dx(const LossRows& r, const LossScales& s, const int64_t* target
 
 // ------------------------------------------------------------------------------------------------
 // The gradient of a piece's logits, transposed: the rows of Gt are classes, their tokens contiguous, as dW = Gt X reads them.
-// Tokens are the tile's rows here, so that a lane holds four neighbours of a row of Gt.
+// Tokens are the tile's rows here, so that a lane holds four neighbours of a row of Gt.  fp32: a class can be improbable in every row,
+// and its planes need a power of two of its own; Gt goes out in fp32 and a pass over its rows makes the planes.
 struct GradientArgs {
   SegArgs g;
   LossPiece p; LossRows r; LossScales s;
-  uint16_t* out[2]; int64_t pitch;
+  void* out; int64_t pitch;
 };
 
 template <typename H>
@@ -545,7 +546,6 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void loss_gradient_kernel(GradientA
   float* s_f = reinterpret_cast<float*>(seg_lds);
   float *s_lse = s_f + SEG_T, *s_wrong = s_lse + SEG_T;
   int* s_at = reinterpret_cast<int*>(s_wrong + SEG_T);
-  const float unit = HALF ? power_of_two(LOSS_G_SHIFT) : 1.0f;
   if (threadIdx.x < SEG_T) {
     const int64_t token = (int64_t)t.tm * SEG_T + threadIdx.x;
     const int64_t target = token < a.p.n ? a.p.targets[token] : -1;
@@ -553,7 +553,7 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void loss_gradient_kernel(GradientA
     const int64_t at = target - a.p.v0;
     s_f[threadIdx.x] = counts ? logit_factor(a.s, token) : 0.0f;
     s_lse[threadIdx.x] = counts ? a.r.lse2[token] : 0.0f;
-    s_wrong[threadIdx.x] = counts ? a.r.wrong[token] * unit : 0.0f;
+    s_wrong[threadIdx.x] = counts ? a.r.wrong[token] : 0.0f;
     s_at[threadIdx.x] = !counts ? -2 : at >= 0 && at < a.p.classes ? (int)at : -1;
   }
   __syncthreads();
@@ -569,30 +569,35 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void loss_gradient_kernel(GradientA
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int row = 128 * t.wm + 16 * (i + q) + 4 * t.kg + e, at = s_at[row];
-          const float p = __builtin_amdgcn_exp2f(acc[i + q][j][e] * s_f[row] - s_lse[row]) * unit;
+          const float p = __builtin_amdgcn_exp2f(acc[i + q][j][e] * s_f[row] - s_lse[row]);
           g[q][e] = at == -2 ? 0.0f : at == (int)cls ? -s_wrong[row] : p;     // rows that do not count: whatever they hold
         }
       // a block of 32 tokens lies inside the padded rows or beyond them
-      const int64_t token = (int64_t)t.tm * SEG_T + 128 * t.wm + 16 * i, to = cls * a.pitch + token + 16 * (t.kg & 1) + 8 * (t.kg >> 1);
-      uint16_t* hi = cls < a.p.classes && token < cols ? a.out[0] + to : nullptr;
-      uintx2 h0, l0, h1, l1;
-      split_four<HALF>(g[0], h0, l0);
-      split_four<HALF>(g[1], h1, l1);
-      const uintx4 h = seg_pair_blocks(h0, h1), l = seg_pair_blocks(l0, l1);
-      if (!hi) continue;
-      *reinterpret_cast<uintx4*>(hi) = h;
-      if constexpr (HALF) *reinterpret_cast<uintx4*>(a.out[1] + to) = l;
+      const int64_t token = (int64_t)t.tm * SEG_T + 128 * t.wm + 16 * i, to = cls * a.pitch + token;
+      const bool live = cls < a.p.classes && token < cols;
+      if constexpr (HALF) {
+        if (!live) continue;
+        float* out = static_cast<float*>(a.out) + to + 4 * t.kg;
+        *reinterpret_cast<floatx4*>(out) = g[0];
+        *reinterpret_cast<floatx4*>(out + 16) = g[1];
+      } else {
+        uintx2 h0, l0, h1, l1;
+        split_four<false>(g[0], h0, l0);
+        split_four<false>(g[1], h1, l1);
+        const uintx4 h = seg_pair_blocks(h0, h1);
+        if (live) *reinterpret_cast<uintx4*>(static_cast<uint16_t*>(a.out) + to + 16 * (t.kg & 1) + 8 * (t.kg >> 1)) = h;
+      }
     }
   }
 }
 
 int launch_loss_gradient(const Planes& w, const Planes& x, int64_t depth, const LossPiece& p, const LossRows& r, const LossScales& s,
-                         uint16_t* const g[2], int64_t g_pitch, hipStream_t st) {
+                         void* g, int64_t g_pitch, hipStream_t st) {
   if (g_pitch < up_to(p.n, 64)) return LQ_ERR_SHAPE;
   GradientArgs a{};
   LQ_TRY(fill_segments(a.g, x, w, depth));
   LQ_TRY(seg_shape(a.g, p.n, p.classes, 1));
-  a.p = p; a.r = r; a.s = s; a.out[0] = g[0]; a.out[1] = g[1]; a.pitch = g_pitch;
+  a.p = p; a.r = r; a.s = s; a.out = g; a.pitch = g_pitch;
   static LdsLimit limit[2];
   prof::Scope ps(prof::LOSS_LOGITS, st, 2.0 * p.n * p.classes * depth);
   return s.x_inv ? launch_tiles(loss_gradient_kernel<_Float16>, limit[0], a, st) : launch_tiles(loss_gradient_kernel<__bf16>, limit[1], a, st);
@@ -601,14 +606,75 @@ int launch_loss_gradient(const Planes& w, const Planes& x, int64_t depth, const 
 // ------------------------------------------------------------------------------------------------
 // The same from E (both planes), where one piece is the whole vocabulary: p = E (1 - p_t) / S, a pass over E for a product less
 // (2047 x 32000, d = 4096).  A workgroup turns 64 tokens x 64 classes in LDS, a thread two tokens of eight classes.  part_ref: E is
-// still relative to its tile's power of two, and goes back relative to the row's (keep: dX needs it) in the same pass.
+// still relative to its tile's power of two, and goes back relative to the row's (keep: dX needs it) in the same pass.  fp32: planes
+// are times a power of two per class, of the largest magnitudes that loss_class_tops_kernel found, and class_inv gets its inverse.
 struct FromEArgs {
   LossPiece p; LossRows r;
   const float* part_ref; int keep;
   uint16_t* e[2]; int64_t e_pitch;
   uint16_t* out[2]; int64_t pitch;
   int tiles_r;
+  float* tops; int ranges; float* class_inv;
 };
+// What a token's E is to be multiplied by to be p: to the row's power of two (shift) and by (1 - p_t) / S.
+__device__ __forceinline__ float tile_shift(const FromEArgs& a, int64_t token, int64_t c) {
+  if (!a.part_ref) return 1.0f;
+  const float ref = a.r.ref[token], mine = a.part_ref[c / SEG_T * a.p.n + token];
+  return mine == ref ? 1.0f : __builtin_amdgcn_exp2f(mine - ref);
+}
+template <bool HALF>
+__device__ __forceinline__ float row_factor(const FromEArgs& a, int64_t token) {
+  const float s = a.r.sum[token];
+  return s == 0.0f ? 0.0f : a.r.wrong[token] / s * (HALF ? power_of_two(-LOSS_E_SHIFT) : 1.0f);
+}
+
+// tops[range][class] = the largest |Gt| among a range of tokens, of E's first plane (as good as a scale has to be): a thread reads
+// eight classes of every fourth token.
+constexpr int TOPS_TOKENS = 64, TOPS_CLASSES = 512;
+__global__ __launch_bounds__(256) void loss_class_tops_kernel(FromEArgs a) {
+  typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+  __shared__ float s_f[2][TOPS_TOKENS];                     // per tile of 256 classes
+  __shared__ int64_t s_t[TOPS_TOKENS];
+  __shared__ uint32_t s_top[4][TOPS_CLASSES];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t c0 = (int64_t)blockIdx.x * TOPS_CLASSES, c = c0 + 8 * lane;
+  const int64_t blocks = (a.p.n + TOPS_TOKENS - 1) / TOPS_TOKENS, b0 = blocks * blockIdx.y / a.ranges, b1 = blocks * (blockIdx.y + 1) / a.ranges;
+  uint32_t top[8] = {};
+  for (int64_t b = b0; b < b1; ++b) {
+    __syncthreads();
+    if (threadIdx.x < TOPS_TOKENS) {
+      const int64_t token = b * TOPS_TOKENS + threadIdx.x, t = token < a.p.n ? a.p.targets[token] : -1;
+      const bool counts = t >= 0 && t < a.p.vocab;
+      s_t[threadIdx.x] = counts ? t : -1;
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        s_f[k][threadIdx.x] = counts && c0 + SEG_T * k < a.e_pitch ? tile_shift(a, token, c0 + SEG_T * k) * row_factor<true>(a, token) : 0.0f;
+    }
+    __syncthreads();
+    if (c >= a.e_pitch) continue;
+#pragma unroll 4
+    for (int i = wave; i < TOPS_TOKENS; i += 4) {
+      const int64_t token = b * TOPS_TOKENS + i, t = s_t[i];
+      if (t < 0) continue;                                  // rows that do not count: whatever they hold
+      const halfx8 e = *reinterpret_cast<const halfx8*>(a.e[0] + token * a.e_pitch + c);
+      const float f = s_f[lane >> 5][i];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top[j] = max(top[j], finite_magnitude((float)e[j] * f));
+      if (t >= c && t < c + 8) {
+        const uint32_t w = finite_magnitude(a.r.wrong[token]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top[j] = t == c + j ? max(top[j], w) : top[j];
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) s_top[wave][8 * lane + j] = top[j];
+  __syncthreads();
+  for (int i = threadIdx.x; i < TOPS_CLASSES; i += 256)
+    if (c0 + i < a.p.classes)
+      a.tops[(int64_t)blockIdx.y * a.p.classes + c0 + i] = __uint_as_float(max(max(s_top[0][i], s_top[1][i]), max(s_top[2][i], s_top[3][i])));
+}
+
 template <typename H>
 __global__ __launch_bounds__(256) void loss_gradient_from_e_kernel(FromEArgs a) {
   constexpr bool HALF = !std::is_same<H, __bf16>::value;
@@ -616,35 +682,42 @@ __global__ __launch_bounds__(256) void loss_gradient_from_e_kernel(FromEArgs a) 
   typedef H hx8 __attribute__((ext_vector_type(8)));
   typedef H hx2 __attribute__((ext_vector_type(2)));
   __shared__ uint32_t s_w[HALF ? 2 : 1][64 * WORDS];
+  __shared__ float s_scale[64];
   const int c = (threadIdx.x & 7) * 8, pair = threadIdx.x >> 3;
   const int64_t r0 = (int64_t)(blockIdx.x % a.tiles_r) * 64, c0 = (int64_t)(blockIdx.x / a.tiles_r) * 64;
+  if constexpr (HALF) {
+    if (threadIdx.x < 64) {
+      uint32_t top = 0;
+      if (c0 + threadIdx.x < a.p.classes)
+        for (int i = 0; i < a.ranges; ++i) top = max(top, __float_as_uint(a.tops[i * a.p.classes + c0 + threadIdx.x]));
+      const int e = half_exponent(top);
+      s_scale[threadIdx.x] = power_of_two(e);
+      if (r0 == 0 && c0 + threadIdx.x < a.p.classes) a.class_inv[c0 + threadIdx.x] = power_of_two(-e);
+    }
+    __syncthreads();
+  }
   float g[2][8];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) g[h][j] = 0.0f;
     const int64_t token = r0 + 2 * pair + h, t = token < a.p.n ? a.p.targets[token] : -1;
-    float shift = 1.0f;
-    if constexpr (HALF)
-      if (a.part_ref && token < a.p.n) {
-        const float ref = a.r.ref[token], mine = a.part_ref[c0 / SEG_T * a.p.n + token];
-        if (mine != ref) shift = __builtin_amdgcn_exp2f(mine - ref);
-      }
     if (t < 0 || t >= a.p.vocab) continue;                   // rows that do not count: whatever they hold
-    const float s = a.r.sum[token], wrong = a.r.wrong[token];
-    const float f = s == 0.0f ? 0.0f : wrong / s * (HALF ? power_of_two(LOSS_G_SHIFT - LOSS_E_SHIFT) : 1.0f);
+    const float f = row_factor<HALF>(a, token), shift = HALF ? tile_shift(a, token, c0) : 1.0f;
     const int64_t at = token * a.e_pitch + c0 + c;           // rows of E end on whole tiles
     hx8 hi = *reinterpret_cast<const hx8*>(a.e[0] + at);
     hx8 lo = *reinterpret_cast<const hx8*>(a.e[1] + at);
-    if (HALF && shift != 1.0f) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) { hi[j] = (H)((float)hi[j] * shift); lo[j] = (H)((float)lo[j] * shift); }
-      if (a.keep) { *reinterpret_cast<hx8*>(a.e[0] + at) = hi; *reinterpret_cast<hx8*>(a.e[1] + at) = lo; }
-    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      g[h][j] = ((float)hi[j] + (float)lo[j]) * f;
-      if (c0 + c + j == t) g[h][j] = -wrong * (HALF ? power_of_two(LOSS_G_SHIFT) : 1.0f);
+      g[h][j] = ((float)hi[j] + (float)lo[j]) * (f * shift);
+      if (c0 + c + j == t) g[h][j] = -a.r.wrong[token];
+      if constexpr (HALF) g[h][j] *= s_scale[c + j];
+    }
+    if (HALF && a.keep && shift != 1.0f) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) { hi[j] = (H)((float)hi[j] * shift); lo[j] = (H)((float)lo[j] * shift); }
+      *reinterpret_cast<hx8*>(a.e[0] + at) = hi;
+      *reinterpret_cast<hx8*>(a.e[1] + at) = lo;
     }
   }
 #pragma unroll
@@ -668,13 +741,21 @@ __global__ __launch_bounds__(256) void loss_gradient_from_e_kernel(FromEArgs a) 
   }
 }
 
+int loss_class_ranges(int64_t n) { return (int)std::min<int64_t>((n + TOPS_TOKENS - 1) / TOPS_TOKENS, 16); }
+
 int launch_loss_gradient_from_e(const LossPiece& p, const LossRows& r, bool half, const float* part_ref, bool keep,
-                                uint16_t* const e[2], int64_t e_pitch, uint16_t* const g[2], int64_t g_pitch, hipStream_t st) {
+                                uint16_t* const e[2], int64_t e_pitch, uint16_t* const g[2], int64_t g_pitch, float* tops,
+                                float* class_inv, hipStream_t st) {
   const int64_t tr = (p.n + 63) / 64, tc = (p.classes + 63) / 64;
-  if (p.v0 != 0 || p.classes != p.vocab || g_pitch < up_to(p.n, 64) || tr * tc >= (1ll << 31)) return LQ_ERR_SHAPE;
-  if (part_ref && !half) return LQ_ERR_ARG;
-  const FromEArgs a{p, r, part_ref, (int)keep, {e[0], e[1]}, e_pitch, {g[0], g[1]}, g_pitch, (int)tr};
+  if (p.v0 != 0 || p.classes != p.vocab || g_pitch < up_to(p.n, 64) || tr * tc >= (1ll << 31) || e_pitch % SEG_T) return LQ_ERR_SHAPE;
+  if (half ? !tops || !class_inv : part_ref != nullptr) return LQ_ERR_ARG;
+  const FromEArgs a{p, r, part_ref, (int)keep, {e[0], e[1]}, e_pitch, {g[0], g[1]}, g_pitch, (int)tr, tops, loss_class_ranges(p.n), class_inv};
   prof::Scope ps(prof::TRAIN_PLANES, st, (double)p.n * p.classes * (half ? 8.0 : 6.0));
+  if (half) {
+    const dim3 grid((unsigned)((p.classes + TOPS_CLASSES - 1) / TOPS_CLASSES), (unsigned)a.ranges);
+    hipLaunchKernelGGL(loss_class_tops_kernel, grid, dim3(256), 0, st, a);
+    LQ_HIP_TRY(hipGetLastError());
+  }
   auto kernel = half ? loss_gradient_from_e_kernel<_Float16> : loss_gradient_from_e_kernel<__bf16>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)(tr * tc)), dim3(256), 0, st, a);
   LQ_HIP_TRY(hipGetLastError());
@@ -686,7 +767,7 @@ int launch_loss_gradient_from_e(const LossPiece& p, const LossRows& r, bool half
 struct DwArgs {
   SegArgs g;
   int64_t rows, cols;
-  const float* factor;
+  const float* factor; const float* class_inv;
   void* out; float* part;
 };
 
@@ -705,6 +786,7 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void loss_dw_kernel(DwArgs a) {
     if (row >= a.rows || col >= a.cols) return;
     if (a.g.splits > 1) { store_floats(part + row * a.cols + col, v, col, a.cols); return; }
     T* at = static_cast<T*>(a.out) + row * a.cols + col;
+    if constexpr (sizeof(T) == 4) v *= a.class_inv[row];
     v *= f;
     if ((a.cols & 3) == 0 && ((uintptr_t)a.out & (4 * sizeof(T) - 1)) == 0) { *reinterpret_cast<vec4*>(at) = __builtin_convertvector(v, vec4); return; }
 #pragma unroll
@@ -714,12 +796,14 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void loss_dw_kernel(DwArgs a) {
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void loss_dw_sum_kernel(const float* __restrict__ part, int splits, int64_t total,
-                                                          const float* __restrict__ factor, T* __restrict__ out) {
+__global__ __launch_bounds__(256) void loss_dw_sum_kernel(const float* __restrict__ part, int splits, int64_t total, int64_t cols,
+                                                          const float* __restrict__ factor, const float* __restrict__ class_inv,
+                                                          T* __restrict__ out) {
   const float f = *factor;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
     float v = 0.0f;
     for (int s = 0; s < splits; ++s) v += part[s * total + i];
+    if constexpr (sizeof(T) == 4) v *= class_inv[i / cols];
     out[i] = (T)(v * f);
   }
 }
@@ -728,14 +812,15 @@ int loss_dw_splits(int64_t rows, int64_t cols, int64_t depth, bool half) {
   return seg_splits(seg_tiles(rows, cols), depth / 64 * (half ? 3 : 1), 16);
 }
 
-int launch_loss_dw(const Planes& g, const Planes& xt, int64_t depth, int64_t rows, int64_t cols, const float* factor, int dtype,
-                   void* out, float* part, size_t part_floats, hipStream_t st) {
+int launch_loss_dw(const Planes& g, const Planes& xt, int64_t depth, int64_t rows, int64_t cols, const float* factor,
+                   const float* class_inv, int dtype, void* out, float* part, size_t part_floats, hipStream_t st) {
   const bool half = g.p[1] != nullptr;
   DwArgs a{};
   LQ_TRY(fill_segments(a.g, xt, g, depth));
   LQ_TRY(seg_shape(a.g, cols, rows, loss_dw_splits(rows, cols, depth, half)));
   if (a.g.splits > 1 && part_floats < (size_t)a.g.splits * (size_t)rows * (size_t)cols) return LQ_ERR_WORKSPACE;
-  a.rows = rows; a.cols = cols; a.factor = factor; a.out = out; a.part = part;
+  if (half != (dtype == LQ_T_FP32) || (half && !class_inv)) return LQ_ERR_ARG;
+  a.rows = rows; a.cols = cols; a.factor = factor; a.class_inv = class_inv; a.out = out; a.part = part;
   static LdsLimit limit[2];
   {
     prof::Scope ps(prof::LOSS_ACCUMULATE, st, 2.0 * rows * cols * depth);
@@ -746,9 +831,11 @@ int launch_loss_dw(const Planes& g, const Planes& xt, int64_t depth, int64_t row
   prof::Scope ps(prof::LOSS_ROWS, st, (double)rows * cols * (4.0 * a.g.splits + type_bytes(dtype)));
   const dim3 grid((unsigned)std::min<int64_t>((rows * cols + 255) / 256, 8192));
   if (dtype == LQ_T_BF16)
-    hipLaunchKernelGGL(loss_dw_sum_kernel<__bf16>, grid, dim3(256), 0, st, part, a.g.splits, rows * cols, factor, static_cast<__bf16*>(out));
+    hipLaunchKernelGGL(loss_dw_sum_kernel<__bf16>, grid, dim3(256), 0, st, part, a.g.splits, rows * cols, cols, factor,
+                       class_inv, static_cast<__bf16*>(out));
   else
-    hipLaunchKernelGGL(loss_dw_sum_kernel<float>, grid, dim3(256), 0, st, part, a.g.splits, rows * cols, factor, static_cast<float*>(out));
+    hipLaunchKernelGGL(loss_dw_sum_kernel<float>, grid, dim3(256), 0, st, part, a.g.splits, rows * cols, cols, factor,
+                       class_inv, static_cast<float*>(out));
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }

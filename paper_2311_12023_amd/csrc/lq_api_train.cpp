@@ -56,6 +56,7 @@ struct LossPlan {
   bool whole;                                        // one piece is the whole vocabulary
   uint16_t *few_x[3], *few_e[3];                     // the few rows' planes
   float* few_part;
+  float *class_tops, *class_inv, *g32;               // fp32: of dW's operand
   int64_t classes, d64, n64, v64;
   size_t part_floats, bytes;
 };
@@ -89,6 +90,9 @@ static LossPlan plan_loss(void* ws, int64_t n, int64_t d, int64_t vocab, int dty
     p.e[h] = a.take<uint16_t>(want_dx || (want_dw && p.whole) ? n * p.classes : 0);
     p.g[h] = a.take<uint16_t>(want_dw ? p.classes * p.n64 : 0);
   }
+  p.class_tops = a.take<float>(half && want_dw && p.whole ? loss_class_ranges(n) * vocab : 0);
+  p.class_inv = a.take<float>(half && want_dw ? p.classes : 0);
+  p.g32 = a.take<float>(half && want_dw && !p.whole ? p.classes * p.n64 : 0);
   p.acc = a.take<float>(want_dx ? n * d : 0);
   // The last piece may be shorter and be cut into other numbers of ranges: tiles times ranges stay within 256 in any case.
   const size_t most = (size_t)256 * SEG_T * SEG_T;
@@ -290,7 +294,8 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
   if (scales.xt_top) LQ_TRY(launch_top_magnitude(X, ldx, n, d, targets, vocab, p.tops + 1, st));
   if (!join_rows) LQ_TRY(launch_loss_rows(p.rows, scales, targets, n, vocab, mean == 1, loss, row_loss, lse, p.factors, st));
   if (dW && p.whole)
-    LQ_TRY(launch_loss_gradient_from_e(all, p.rows, half, late ? p.part_ref : nullptr, dX != nullptr, p.e, p.classes, p.g, p.n64, st));
+    LQ_TRY(launch_loss_gradient_from_e(all, p.rows, half, late ? p.part_ref : nullptr, dX != nullptr, p.e, p.classes, p.g, p.n64,
+                                       p.class_tops, p.class_inv, st));
   if (late && dX) LQ_TRY(accumulate(all, whole));
   if (dX && few) {
     LQ_TRY(launch_few_dx(W, ldw, dtype, d, Planes{{p.few_e[0], p.few_e[1], p.few_e[2]}, p.v64}, all, p.rows, p.part_ref, p.factors,
@@ -306,9 +311,12 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
     if (!p.whole) {
       Planes w;
       LQ_TRY(piece_planes(v0, piece.classes, &w));
-      LQ_TRY(launch_loss_gradient(w, x, p.d64, piece, p.rows, scales, p.g, p.n64, st));
+      LQ_TRY(launch_loss_gradient(w, x, p.d64, piece, p.rows, scales, half ? (void*)p.g32 : p.g[0], p.n64, st));
+      if (half)
+        LQ_TRY(launch_row_planes({p.g32, LQ_T_FP32, p.n64, piece.classes, n, nullptr}, PLANE_HALF_2,
+                                 {{p.g[0], p.g[1], nullptr}, p.n64, piece.classes}, p.class_inv, st));
     }
-    LQ_TRY(launch_loss_dw(Planes{{p.g[0], p.g[1], nullptr}, p.n64}, planes_of(xt), p.n64, piece.classes, d, p.factors + 1, dtype,
+    LQ_TRY(launch_loss_dw(Planes{{p.g[0], p.g[1], nullptr}, p.n64}, planes_of(xt), p.n64, piece.classes, d, p.factors + 1, p.class_inv, dtype,
                           static_cast<char*>(dW) + (size_t)v0 * (size_t)d * size, p.part, p.part_floats, st));
   }
   return LQ_OK;

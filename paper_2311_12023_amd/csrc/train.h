@@ -131,7 +131,7 @@ struct LossPiece {           // the classes v0 .. v0 + classes - 1 of a call
 int launch_zero_words(uint32_t* p, int count, hipStream_t st);
 // E[i][j] = 2^(s_ij log2 e - part_ref), 0 for the target and beyond the piece, as planes (NULL: not wanted), and per tile of 256
 // classes and row: part_ref, part_sum.  bf16: e[1], what the rounding of E left out, may be NULL.  fp32: E is stored times 2^LOSS_E_SHIFT and may reach 2^LOSS_E_ROOM.
-constexpr int LOSS_E_SHIFT = 13, LOSS_E_ROOM = 2, LOSS_G_SHIFT = 14;
+constexpr int LOSS_E_SHIFT = 13, LOSS_E_ROOM = 2;
 int launch_loss_logits(const Planes& w, const Planes& x, int64_t depth, const LossPiece& p, const LossRows& r, const LossScales& s,
                        float* part_ref, float* part_sum, uint16_t* const e[2], int64_t e_pitch, hipStream_t st);
 // Joins the sums of tiles of `tile` classes with the row's; with e (tiles of SEG_T classes) brings E to one power of two per row.
@@ -156,18 +156,21 @@ int launch_loss_rows(const LossRows& r, const LossScales& s, const int64_t* targ
                      float* row_loss, float* lse, float* factors, hipStream_t st);
 int launch_loss_dx(const LossRows& r, const LossScales& s, const int64_t* targets, int64_t n, int64_t d, int64_t vocab,
                    const float* acc, const void* W, int64_t ldw, int dtype, const float* factors, void* dX, hipStream_t st);
-// Gt[j][i] = p_ij - [j = target_i] as planes of `classes` rows (fp32: times 2^LOSS_G_SHIFT), zero for rows that do not count and up
-// to up_to(n, 64).
+// Gt[j][i] = p_ij - [j = target_i], `classes` rows of g_pitch, zero for rows that do not count and up to up_to(n, 64): bf16, or fp32
+// where the operands are.
 int launch_loss_gradient(const Planes& w, const Planes& x, int64_t depth, const LossPiece& p, const LossRows& r, const LossScales& s,
-                         uint16_t* const g[2], int64_t g_pitch, hipStream_t st);
-// The same from E where one piece is the whole vocabulary.  part_ref (fp32; NULL where E is relative to its rows' powers of two): E is
+                         void* g, int64_t g_pitch, hipStream_t st);
+// The same from E where one piece is the whole vocabulary, as planes.  fp32: Gt's rows times a power of two each, whose inverse goes to
+// class_inv (tops: loss_class_ranges(n) x classes floats).  part_ref (fp32; NULL where E is relative to its rows' powers of two): E is
 // relative to its tiles', and with keep goes back relative to its rows'.
+int loss_class_ranges(int64_t n);
 int launch_loss_gradient_from_e(const LossPiece& p, const LossRows& r, bool half, const float* part_ref, bool keep,
-                                uint16_t* const e[2], int64_t e_pitch, uint16_t* const g[2], int64_t g_pitch, hipStream_t st);
-// dW's rows: out (rows x cols, contiguous, of type dtype) = *factor A B^T.  part: splits x rows x cols floats.
+                                uint16_t* const e[2], int64_t e_pitch, uint16_t* const g[2], int64_t g_pitch, float* tops,
+                                float* class_inv, hipStream_t st);
+// dW's rows: out (rows x cols, contiguous, of type dtype) = *factor A B^T, fp32: times class_inv per row.  part: splits x rows x cols floats.
 int loss_dw_splits(int64_t rows, int64_t cols, int64_t depth, bool half);
-int launch_loss_dw(const Planes& g, const Planes& xt, int64_t depth, int64_t rows, int64_t cols, const float* factor, int dtype,
-                   void* out, float* part, size_t part_floats, hipStream_t st);
+int launch_loss_dw(const Planes& g, const Planes& xt, int64_t depth, int64_t rows, int64_t cols, const float* factor,
+                   const float* class_inv, int dtype, void* out, float* part, size_t part_floats, hipStream_t st);
 
 // ---- the same for few rows (loss_few_kernels.hip) ---------------------------------------------------------
 // Up to LOSS_FEW rows the loss is bound by reading W: it is then read where it is, once for the logits and once for dX, the whole
