@@ -682,42 +682,61 @@ __global__ __launch_bounds__(256) void loss_gradient_from_e_kernel(FromEArgs a) 
   typedef H hx8 __attribute__((ext_vector_type(8)));
   typedef H hx2 __attribute__((ext_vector_type(2)));
   __shared__ uint32_t s_w[HALF ? 2 : 1][64 * WORDS];
-  __shared__ float s_scale[64];
+  __shared__ uint32_t s_top[HALF ? 4 : 1][64];
   const int c = (threadIdx.x & 7) * 8, pair = threadIdx.x >> 3;
   const int64_t r0 = (int64_t)(blockIdx.x % a.tiles_r) * 64, c0 = (int64_t)(blockIdx.x / a.tiles_r) * 64;
+  // all loads first: none waits for another
+  hx8 hi[2], lo[2];
+  float f[2], wrong[2], shift[2];
+  int64_t target[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int64_t token = r0 + 2 * pair + h, row = token < a.p.n ? token : a.p.n - 1;
+    const int64_t at = row * a.e_pitch + c0 + c;             // rows of E end on whole tiles
+    hi[h] = *reinterpret_cast<const hx8*>(a.e[0] + at);
+    lo[h] = *reinterpret_cast<const hx8*>(a.e[1] + at);
+    target[h] = token < a.p.n ? a.p.targets[row] : -1;
+    wrong[h] = a.r.wrong[row];
+    f[h] = row_factor<HALF>(a, row);
+    shift[h] = HALF ? tile_shift(a, row, c0) : 1.0f;
+  }
+  float scale[8];
   if constexpr (HALF) {
-    if (threadIdx.x < 64) {
-      uint32_t top = 0;
-      if (c0 + threadIdx.x < a.p.classes)
-        for (int i = 0; i < a.ranges; ++i) top = max(top, __float_as_uint(a.tops[i * a.p.classes + c0 + threadIdx.x]));
-      const int e = half_exponent(top);
-      s_scale[threadIdx.x] = power_of_two(e);
-      if (r0 == 0 && c0 + threadIdx.x < a.p.classes) a.class_inv[c0 + threadIdx.x] = power_of_two(-e);
+    const int k = threadIdx.x & 63, q = threadIdx.x >> 6;
+    uint32_t top = 0;
+    if (c0 + k < a.p.classes) {
+#pragma unroll 4
+      for (int i = q; i < a.ranges; i += 4) top = max(top, __float_as_uint(a.tops[i * a.p.classes + c0 + k]));
     }
+    s_top[q][k] = top;
     __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      scale[j] = power_of_two(half_exponent(max(max(s_top[0][c + j], s_top[1][c + j]), max(s_top[2][c + j], s_top[3][c + j]))));
+    if (r0 == 0 && q == 0 && c0 + k < a.p.classes)
+      a.class_inv[c0 + k] = power_of_two(-half_exponent(max(max(s_top[0][k], s_top[1][k]), max(s_top[2][k], s_top[3][k]))));
   }
   float g[2][8];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
+    const int64_t t = target[h];
+    if (t < 0 || t >= a.p.vocab) {                           // rows that do not count: whatever they hold
 #pragma unroll
-    for (int j = 0; j < 8; ++j) g[h][j] = 0.0f;
-    const int64_t token = r0 + 2 * pair + h, t = token < a.p.n ? a.p.targets[token] : -1;
-    if (t < 0 || t >= a.p.vocab) continue;                   // rows that do not count: whatever they hold
-    const float f = row_factor<HALF>(a, token), shift = HALF ? tile_shift(a, token, c0) : 1.0f;
-    const int64_t at = token * a.e_pitch + c0 + c;           // rows of E end on whole tiles
-    hx8 hi = *reinterpret_cast<const hx8*>(a.e[0] + at);
-    hx8 lo = *reinterpret_cast<const hx8*>(a.e[1] + at);
+      for (int j = 0; j < 8; ++j) g[h][j] = 0.0f;
+      continue;
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      g[h][j] = ((float)hi[j] + (float)lo[j]) * (f * shift);
-      if (c0 + c + j == t) g[h][j] = -a.r.wrong[token];
-      if constexpr (HALF) g[h][j] *= s_scale[c + j];
+      g[h][j] = ((float)hi[h][j] + (float)lo[h][j]) * (f[h] * shift[h]);
+      if (c0 + c + j == t) g[h][j] = -wrong[h];
+      if constexpr (HALF) g[h][j] *= scale[j];
     }
-    if (HALF && a.keep && shift != 1.0f) {
+    if (HALF && a.keep && shift[h] != 1.0f) {
+      const int64_t at = (r0 + 2 * pair + h) * a.e_pitch + c0 + c;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) { hi[j] = (H)((float)hi[j] * shift); lo[j] = (H)((float)lo[j] * shift); }
-      *reinterpret_cast<hx8*>(a.e[0] + at) = hi;
-      *reinterpret_cast<hx8*>(a.e[1] + at) = lo;
+      for (int j = 0; j < 8; ++j) { hi[h][j] = (H)((float)hi[h][j] * shift[h]); lo[h][j] = (H)((float)lo[h][j] * shift[h]); }
+      *reinterpret_cast<hx8*>(a.e[0] + at) = hi[h];
+      *reinterpret_cast<hx8*>(a.e[1] + at) = lo[h];
     }
   }
 #pragma unroll

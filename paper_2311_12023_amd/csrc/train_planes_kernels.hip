@@ -232,19 +232,24 @@ int launch_column_planes(const PlaneSource& s, PlaneKind kind, const PlaneTarget
 
 // ------------------------------------------------------------------------------------------------
 // The largest of integers does not depend on the order in which an atomic takes them.
-template <bool VEC>
+// FLAT: rows one after the other without a gap, each of them taken, as one long row of whole vectors.
+template <bool VEC, bool FLAT>
 __global__ __launch_bounds__(256) void top_magnitude_kernel(const float* __restrict__ src, int64_t ld, int64_t rows, int64_t cols,
                                                             const int64_t* __restrict__ keep, int64_t keep_below,
                                                             uint32_t* __restrict__ out) {
   __shared__ uint32_t s_top[4];
-  const int64_t units = (cols + 7) / 8, total = rows * units;
+  const int64_t units = (cols + 7) / 8, total = FLAT ? rows * cols / 8 : rows * units, step = (int64_t)gridDim.x * 256;
   uint32_t top = 0;
 #pragma unroll 4
-  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
-    const int64_t row = u / units, c = (u - row * units) * 8;
-    if (keep) { const int64_t t = keep[row]; if (t < 0 || t >= keep_below) continue; }
+  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += step) {
     float v[8];
-    load8<float, VEC>(src + row * ld, c, cols, v);
+    if constexpr (FLAT) {
+      load8<float, true>(src, 8 * u, 8 * total, v);
+    } else {
+      const int64_t row = u / units, c = (u - row * units) * 8;
+      if (keep) { const int64_t t = keep[row]; if (t < 0 || t >= keep_below) continue; }
+      load8<float, VEC>(src + row * ld, c, cols, v);
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) top = max(top, finite_magnitude(v[j]));
   }
@@ -257,9 +262,9 @@ __global__ __launch_bounds__(256) void top_magnitude_kernel(const float* __restr
 
 int launch_top_magnitude(const void* src, int64_t ld, int64_t rows, int64_t cols, const int64_t* keep, int64_t keep_below,
                          uint32_t* top, hipStream_t st) {
-  const bool vec = vectors_fit(src, ld, LQ_T_FP32);
+  const bool vec = vectors_fit(src, ld, LQ_T_FP32), flat = vec && !keep && ld == cols && cols % 8 == 0;
   const int64_t units = rows * ((cols + 7) / 8);
-  auto kernel = vec ? top_magnitude_kernel<true> : top_magnitude_kernel<false>;
+  auto kernel = flat ? top_magnitude_kernel<true, true> : vec ? top_magnitude_kernel<true, false> : top_magnitude_kernel<false, false>;
   prof::Scope ps(prof::TRAIN_PLANES, st, (double)rows * (double)cols * 4.0);
   hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>((units + 1023) / 1024, 2048)), dim3(256), 0, st,
                      static_cast<const float*>(src), ld, rows, cols, keep, keep_below, top);
