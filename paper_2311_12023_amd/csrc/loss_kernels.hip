@@ -3,13 +3,13 @@
 //   s_ij = <x_i, w_j>,  loss_i = log sum_j e^s_ij - s_it,  dX_i = g (sum_j p_ij w_j - w_t),  dW_j = sum_i g (p_ij - [j = t_i]) x_i
 //
 // The vocabulary is walked in pieces.  A piece's logits come out of the matrix pipe tile by tile and leave the registers as
-// E_ij = 2^(s_ij log2 e - ref) in bf16 with their sums in fp32; E W, added up over the pieces, is the gradient of X up to a factor
-// per row that is known at the end.  So the loss and dX take one pass, 4 n d V operations, where a pass for the sums and one
+// E_ij = 2^(s_ij log2 e - ref), in bf16 or as two fp16 planes, with their sums in fp32; E W, added up over the pieces, is the gradient
+// of X up to a factor per row that is known at the end.  So the loss and dX take one pass, 4 n d V operations, where a pass for the sums and one
 // for the gradient would take six.  References are whole powers of two: a row's E, its sum and its part of dX move from one
 // reference to a larger one without a rounding.  The target stays out of E: with S the sum over the other classes and z the
 // logit's distance from log S, loss = log(1 + e^-z) and dX_i = g (1 - p_t) (E W / S - w_t), 1 - p_t = 1 / (1 + e^z), which
 // are as exact for a row that is certain of its target (p_t = 1 - 1e-9) as for any other; 1 - p_t from p_t would be lost there.
-// dW needs p itself, so it takes a second pass over the logits.
+// dW needs p itself: it comes from E where one piece is the whole vocabulary, else from a second pass over the logits.
 #include "half_planes_device.h"
 #include "mfma_device.h"
 #include "profiler.h"
@@ -60,13 +60,14 @@ __device__ __forceinline__ void store_blocks(uint16_t* hi, uint16_t* lo, floatx4
 // Logits of a piece.  Classes are the tile's rows and tokens its columns: a lane then holds 32 classes of each of its tokens, and
 // the maximum and the sum over the tile are reductions inside lanes, two exchanges between lanes and one through LDS between two
 // wavefronts.  E is rounded to bf16, 2^-8 of each term of a sum that ends up in the type of X; two fp16 planes where that is fp32.
-// What the rounding left out is kept beside it where dW comes from E.
+// Where dW comes from E, what the rounding left out is kept beside it, and E in fp32 instead of the planes: they end 2^-39 below the
+// largest of 256 classes, and a class can be less probable than that beside it in every row.
 struct LogitsArgs {
   SegArgs g;
   LossPiece p; LossScales s;
   const float* ref; float* target;
   float* part_ref; float* part_sum;
-  uint16_t* e[2]; int64_t e_pitch;
+  uint16_t* e[2]; float* e32; int64_t e_pitch;
 };
 
 template <typename H>
@@ -140,7 +141,11 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void loss_logits_kernel(LogitsArgs 
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
     s_sum[t.wm * SEG_T + col] = HALF ? sum * power_of_two(-LOSS_E_SHIFT) : sum;
-    if (a.e[0] && token < a.p.n) {
+    if (HALF && a.e32 && token < a.p.n) {
+      float* out = a.e32 + token * a.e_pitch + class0 + 4 * t.kg;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) *reinterpret_cast<floatx4*>(out + 16 * i) = acc[i][j];
+    } else if (a.e[0] && token < a.p.n) {
       const int64_t at = token * a.e_pitch + class0 + 16 * (t.kg & 1) + 8 * (t.kg >> 1);
 #pragma unroll
       for (int i = 0; i < 8; i += 2) store_blocks<HALF>(a.e[0] + at + 16 * i, a.e[1] ? a.e[1] + at + 16 * i : nullptr, acc[i][j], acc[i + 1][j]);
@@ -213,12 +218,13 @@ static int launch_tiles(void (*kernel)(Args), LdsLimit& limit, const Args& a, hi
 }
 
 int launch_loss_logits(const Planes& w, const Planes& x, int64_t depth, const LossPiece& p, const LossRows& r, const LossScales& s,
-                       float* part_ref, float* part_sum, uint16_t* const e[2], int64_t e_pitch, hipStream_t st) {
+                       float* part_ref, float* part_sum, uint16_t* const e[2], float* e32, int64_t e_pitch, hipStream_t st) {
   LogitsArgs a{};
   LQ_TRY(fill_segments(a.g, w, x, depth));
   LQ_TRY(seg_shape(a.g, p.classes, p.n, 1));
   a.p = p; a.s = s; a.ref = r.ref; a.target = r.target; a.part_ref = part_ref; a.part_sum = part_sum;
-  a.e[0] = e[0]; a.e[1] = e[1]; a.e_pitch = e_pitch;
+  a.e[0] = e[0]; a.e[1] = e[1]; a.e32 = e32; a.e_pitch = e_pitch;
+  if (e32 && (!s.x_inv || p.v0 != 0)) return LQ_ERR_ARG;
   static LdsLimit limit[2];
   prof::Scope ps(prof::LOSS_LOGITS, st, 2.0 * p.n * p.classes * depth);
   return s.x_inv ? launch_tiles(loss_logits_kernel<_Float16>, limit[0], a, st) : launch_tiles(loss_logits_kernel<__bf16>, limit[1], a, st);
@@ -293,12 +299,15 @@ struct JoinArgs {
   int told;
 };
 
+// v *= 2^e, e <= 0, in two steps: 2^e can leave the range where a value of up to 2^64 times it does not.
 template <typename H>
-__device__ __forceinline__ void scale_run(uint16_t* at, float f) {
+__device__ __forceinline__ void scale_run(uint16_t* at, float e) {
   typedef H hx4 __attribute__((ext_vector_type(4)));
   hx4 v = *reinterpret_cast<const hx4*>(at);
+  const float whole = fmaxf(e, -250.0f), half = floorf(0.5f * whole);
+  const float f = __builtin_amdgcn_exp2f(half), g = __builtin_amdgcn_exp2f(whole - half);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) v[k] = (H)((float)v[k] * f);
+  for (int k = 0; k < 4; ++k) v[k] = (H)((float)v[k] * f * g);
   *reinterpret_cast<hx4*>(at) = v;
 }
 
@@ -328,10 +337,9 @@ __device__ __forceinline__ void join_row(const JoinArgs& a, int64_t row, int lan
   if (!a.e[0] || (first && !a.told)) return;
   for (int t0 = 0; t0 < a.tiles; t0 += 64) {
     const float mine = t0 + lane < a.tiles ? a.part_ref[(int64_t)(t0 + lane) * a.p.n + row] : ref;
-    const float f = __builtin_amdgcn_exp2f(mine - from);
     for (uint64_t low = __ballot(mine != ref); low; low &= low - 1) {
       const int t = __builtin_ctzll(low);
-      const float ft = __shfl(f, t);
+      const float ft = __shfl(mine, t) - from;
       const int64_t at = row * a.e_pitch + (int64_t)(t0 + t) * SEG_T + 4 * lane;
       scale_run<H>(a.e[0] + at, ft);
       if (a.e[1]) scale_run<H>(a.e[1] + at, ft);
@@ -354,19 +362,18 @@ __global__ __launch_bounds__(1024) void loss_join_rows_kernel(JoinArgs a, RowsAr
   finish_rows(rows);
 }
 
-// 256 classes x 16 tokens a workgroup.
-template <typename H>
+// The first piece's E in fp32: 256 classes x 16 tokens a workgroup.
 __global__ __launch_bounds__(256) void loss_shift_kernel(JoinArgs a) {
   const int64_t token = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
   if (token >= a.p.n) return;
   const float ref = a.r.ref[token], mine = a.part_ref[(int64_t)blockIdx.y * a.p.n + token];
   if (mine == ref) return;
-  const float f = __builtin_amdgcn_exp2f(mine - ref);
+  const float f = mine - ref;
   const int64_t at = token * a.e_pitch + (int64_t)blockIdx.y * SEG_T + 4 * (threadIdx.x & 15);
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    scale_run<H>(a.e[0] + at + 64 * q, f);
-    if (a.e[1]) scale_run<H>(a.e[1] + at + 64 * q, f);
+    scale_run<_Float16>(a.e[0] + at + 64 * q, f);
+    scale_run<_Float16>(a.e[1] + at + 64 * q, f);
   }
 }
 
@@ -378,9 +385,8 @@ int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, bool told
   hipLaunchKernelGGL(kernel, dim3((unsigned)((p.n + 3) / 4)), dim3(256), 0, st, a);
   LQ_HIP_TRY(hipGetLastError());
   if (!e[0] || p.v0 != 0 || told) return LQ_OK;
-  if (a.tiles > 65535) return LQ_ERR_SHAPE;
-  auto shift = half ? loss_shift_kernel<_Float16> : loss_shift_kernel<__bf16>;
-  hipLaunchKernelGGL(shift, dim3((unsigned)((p.n + 15) / 16), (unsigned)a.tiles), dim3(256), 0, st, a);
+  if (!half || a.tiles > 65535) return LQ_ERR_SHAPE;
+  hipLaunchKernelGGL(loss_shift_kernel, dim3((unsigned)((p.n + 15) / 16), (unsigned)a.tiles), dim3(256), 0, st, a);
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }
@@ -604,13 +610,14 @@ int launch_loss_gradient(const Planes& w, const Planes& x, int64_t depth, const 
 }
 
 // ------------------------------------------------------------------------------------------------
-// The same from E (both planes), where one piece is the whole vocabulary: p = E (1 - p_t) / S, a pass over E for a product less
-// (2047 x 32000, d = 4096).  A workgroup turns 64 tokens x 64 classes in LDS, a thread two tokens of eight classes.  part_ref: E is
-// still relative to its tile's power of two, and goes back relative to the row's (keep: dX needs it) in the same pass.  fp32: planes
-// are times a power of two per class, of the largest magnitudes that loss_class_tops_kernel found, and class_inv gets its inverse.
+// The same from E, where one piece is the whole vocabulary: p = E (1 - p_t) / S, a pass over E for a product less (2047 x 32000,
+// d = 4096).  A workgroup turns 64 tokens x 64 classes in LDS, a thread two tokens of eight classes.  bf16: E is both planes.  fp32: E
+// is one array relative to its tiles' powers of two; where dX needs them (e[0]), its planes relative to the rows' go out in the
+// same pass.  Gt's planes are times a power of two per class, of the largest magnitudes that loss_class_tops_kernel found, and
+// class_inv gets its inverse.
 struct FromEArgs {
   LossPiece p; LossRows r;
-  const float* part_ref; int keep;
+  const float* part_ref; const float* e32;
   uint16_t* e[2]; int64_t e_pitch;
   uint16_t* out[2]; int64_t pitch;
   int tiles_r;
@@ -618,7 +625,6 @@ struct FromEArgs {
 };
 // What a token's E is to be multiplied by to be p: to the row's power of two (shift) and by (1 - p_t) / S.
 __device__ __forceinline__ float tile_shift(const FromEArgs& a, int64_t token, int64_t c) {
-  if (!a.part_ref) return 1.0f;
   const float ref = a.r.ref[token], mine = a.part_ref[c / SEG_T * a.p.n + token];
   return mine == ref ? 1.0f : __builtin_amdgcn_exp2f(mine - ref);
 }
@@ -628,11 +634,10 @@ __device__ __forceinline__ float row_factor(const FromEArgs& a, int64_t token) {
   return s == 0.0f ? 0.0f : a.r.wrong[token] / s * (HALF ? power_of_two(-LOSS_E_SHIFT) : 1.0f);
 }
 
-// tops[range][class] = the largest |Gt| among a range of tokens, of E's first plane (as good as a scale has to be): a thread reads
-// eight classes of every fourth token.
+// tops[range][class] = the largest |Gt| among a range of tokens: a thread reads eight classes of every fourth token.
 constexpr int TOPS_TOKENS = 64, TOPS_CLASSES = 512;
 __global__ __launch_bounds__(256) void loss_class_tops_kernel(FromEArgs a) {
-  typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+  typedef float floatx8 __attribute__((ext_vector_type(8)));
   __shared__ float s_f[2][TOPS_TOKENS];                     // per tile of 256 classes
   __shared__ int64_t s_t[TOPS_TOKENS];
   __shared__ uint32_t s_top[4][TOPS_CLASSES];
@@ -656,10 +661,10 @@ __global__ __launch_bounds__(256) void loss_class_tops_kernel(FromEArgs a) {
     for (int i = wave; i < TOPS_TOKENS; i += 4) {
       const int64_t token = b * TOPS_TOKENS + i, t = s_t[i];
       if (t < 0) continue;                                  // rows that do not count: whatever they hold
-      const halfx8 e = *reinterpret_cast<const halfx8*>(a.e[0] + token * a.e_pitch + c);
+      const floatx8 e = *reinterpret_cast<const floatx8*>(a.e32 + token * a.e_pitch + c);
       const float f = s_f[lane >> 5][i];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) top[j] = max(top[j], finite_magnitude((float)e[j] * f));
+      for (int j = 0; j < 8; ++j) top[j] = max(top[j], finite_magnitude(e[j] * f));
       if (t >= c && t < c + 8) {
         const uint32_t w = finite_magnitude(a.r.wrong[token]);
 #pragma unroll
@@ -680,21 +685,22 @@ __global__ __launch_bounds__(256) void loss_gradient_from_e_kernel(FromEArgs a) 
   constexpr bool HALF = !std::is_same<H, __bf16>::value;
   constexpr int WORDS = 33;
   typedef H hx8 __attribute__((ext_vector_type(8)));
+  typedef float floatx8 __attribute__((ext_vector_type(8)));
   typedef H hx2 __attribute__((ext_vector_type(2)));
   __shared__ uint32_t s_w[HALF ? 2 : 1][64 * WORDS];
   __shared__ uint32_t s_top[HALF ? 4 : 1][64];
   const int c = (threadIdx.x & 7) * 8, pair = threadIdx.x >> 3;
   const int64_t r0 = (int64_t)(blockIdx.x % a.tiles_r) * 64, c0 = (int64_t)(blockIdx.x / a.tiles_r) * 64;
   // all loads first: none waits for another
-  hx8 hi[2], lo[2];
+  floatx8 e[2];
   float f[2], wrong[2], shift[2];
   int64_t target[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int64_t token = r0 + 2 * pair + h, row = token < a.p.n ? token : a.p.n - 1;
     const int64_t at = row * a.e_pitch + c0 + c;             // rows of E end on whole tiles
-    hi[h] = *reinterpret_cast<const hx8*>(a.e[0] + at);
-    lo[h] = *reinterpret_cast<const hx8*>(a.e[1] + at);
+    if constexpr (HALF) e[h] = *reinterpret_cast<const floatx8*>(a.e32 + at);
+    else e[h] = __builtin_convertvector(*reinterpret_cast<const hx8*>(a.e[0] + at), floatx8) + __builtin_convertvector(*reinterpret_cast<const hx8*>(a.e[1] + at), floatx8);
     target[h] = token < a.p.n ? a.p.targets[row] : -1;
     wrong[h] = a.r.wrong[row];
     f[h] = row_factor<HALF>(a, row);
@@ -727,16 +733,27 @@ __global__ __launch_bounds__(256) void loss_gradient_from_e_kernel(FromEArgs a) 
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      g[h][j] = ((float)hi[h][j] + (float)lo[h][j]) * (f[h] * shift[h]);
+      g[h][j] = e[h][j] * shift[h] * f[h];
       if (c0 + c + j == t) g[h][j] = -wrong[h];
       if constexpr (HALF) g[h][j] *= scale[j];
     }
-    if (HALF && a.keep && shift[h] != 1.0f) {
-      const int64_t at = (r0 + 2 * pair + h) * a.e_pitch + c0 + c;
+  }
+  if constexpr (HALF) {
+    if (a.e[0]) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) { hi[h][j] = (H)((float)hi[h][j] * shift[h]); lo[h][j] = (H)((float)lo[h][j] * shift[h]); }
-      *reinterpret_cast<hx8*>(a.e[0] + at) = hi[h];
-      *reinterpret_cast<hx8*>(a.e[1] + at) = lo[h];
+      for (int h = 0; h < 2; ++h) {
+        const int64_t token = r0 + 2 * pair + h, at = token * a.e_pitch + c0 + c;
+        if (token >= a.p.n) continue;
+        hx8 hi, lo;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {                        // as loss_shift_kernel makes them: dX is the same with and without dW
+          const HalfPair v = split_half(e[h][j]);
+          hi[j] = (H)((float)v.hi * shift[h]);
+          lo[j] = (H)((float)v.lo * shift[h]);
+        }
+        *reinterpret_cast<hx8*>(a.e[0] + at) = hi;
+        *reinterpret_cast<hx8*>(a.e[1] + at) = lo;
+      }
     }
   }
 #pragma unroll
@@ -762,14 +779,15 @@ __global__ __launch_bounds__(256) void loss_gradient_from_e_kernel(FromEArgs a) 
 
 int loss_class_ranges(int64_t n) { return (int)std::min<int64_t>((n + TOPS_TOKENS - 1) / TOPS_TOKENS, 16); }
 
-int launch_loss_gradient_from_e(const LossPiece& p, const LossRows& r, bool half, const float* part_ref, bool keep,
+int launch_loss_gradient_from_e(const LossPiece& p, const LossRows& r, const float* part_ref, const float* e32,
                                 uint16_t* const e[2], int64_t e_pitch, uint16_t* const g[2], int64_t g_pitch, float* tops,
                                 float* class_inv, hipStream_t st) {
   const int64_t tr = (p.n + 63) / 64, tc = (p.classes + 63) / 64;
   if (p.v0 != 0 || p.classes != p.vocab || g_pitch < up_to(p.n, 64) || tr * tc >= (1ll << 31) || e_pitch % SEG_T) return LQ_ERR_SHAPE;
-  if (half ? !tops || !class_inv : part_ref != nullptr) return LQ_ERR_ARG;
-  const FromEArgs a{p, r, part_ref, (int)keep, {e[0], e[1]}, e_pitch, {g[0], g[1]}, g_pitch, (int)tr, tops, loss_class_ranges(p.n), class_inv};
-  prof::Scope ps(prof::TRAIN_PLANES, st, (double)p.n * p.classes * (half ? 8.0 : 6.0));
+  const bool half = e32 != nullptr;
+  if (half ? !tops || !class_inv || !part_ref : !e[0] || !e[1]) return LQ_ERR_ARG;
+  const FromEArgs a{p, r, part_ref, e32, {e[0], e[1]}, e_pitch, {g[0], g[1]}, g_pitch, (int)tr, tops, loss_class_ranges(p.n), class_inv};
+  prof::Scope ps(prof::TRAIN_PLANES, st, (double)p.n * p.classes * (half ? 8.0 : 6.0));      // fp32 with dX: its planes of E beside
   if (half) {
     const dim3 grid((unsigned)((p.classes + TOPS_CLASSES - 1) / TOPS_CLASSES), (unsigned)a.ranges);
     hipLaunchKernelGGL(loss_class_tops_kernel, grid, dim3(256), 0, st, a);

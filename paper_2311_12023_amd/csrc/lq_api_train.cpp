@@ -39,8 +39,13 @@ static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)
 // Byte offsets inside a tile of 256 rows are 32 bits wide: rows of a plane are at most this far apart.
 constexpr int64_t MOST_PITCH = (int64_t)1 << 23;
 
-// Classes per piece: E of a piece stays within 2^26 values (128 MiB per plane); pieces of equal size, whole tiles.
+// Classes per piece, whole tiles.  Up to 2^28 logits the whole vocabulary is one piece, since dW then comes from E and not from a second
+// product (E and dW's operand take 3 GiB at most): 4096 x 4096 by 32000, bf16 2.83 ms for 3.46 in pieces of 2^26, 2048 x 1024 by 50265
+// fp32 2.33 for 3.06; without dW 1.76 for 1.73 and 1.49 for 1.57.  Above, pieces of 2^26, whose E stays within the memory-side cache
+// (4096 x 4096 by 128000 without dW 6.73 ms; pieces of 2^24 7.27, of 2^28 6.88).
 static int64_t piece_classes(int64_t n, int64_t vocab) {
+  const int64_t whole = up_to(vocab, SEG_T);
+  if (n <= ((int64_t)1 << 28) / vocab && whole <= MOST_PITCH / 2) return whole;
   const int64_t most = std::min(std::max<int64_t>(SEG_T, ((int64_t)1 << 26) / n / SEG_T * SEG_T), MOST_PITCH / 2);
   const int64_t pieces = (vocab + most - 1) / most;
   return up_to((vocab + pieces - 1) / pieces, SEG_T);
@@ -56,7 +61,7 @@ struct LossPlan {
   bool whole;                                        // one piece is the whole vocabulary
   uint16_t *few_x[3], *few_e[3];                     // the few rows' planes
   float* few_part;
-  float *class_tops, *class_inv, *g32;               // fp32: of dW's operand
+  float *class_tops, *class_inv, *g32, *e32;         // fp32: for dW's operand
   int64_t classes, d64, n64, v64;
   size_t part_floats, bytes;
 };
@@ -87,11 +92,12 @@ static LossPlan plan_loss(void* ws, int64_t n, int64_t d, int64_t vocab, int dty
     p.x[h] = a.take<uint16_t>(n * p.d64);
     p.w[h] = a.take<uint16_t>(p.classes * p.d64);
     p.xt[h] = a.take<uint16_t>(want_dw ? d * p.n64 : 0);
-    p.e[h] = a.take<uint16_t>(want_dx || (want_dw && p.whole) ? n * p.classes : 0);
+    p.e[h] = a.take<uint16_t>(want_dx || (want_dw && p.whole && !half) ? n * p.classes : 0);
     p.g[h] = a.take<uint16_t>(want_dw ? p.classes * p.n64 : 0);
   }
   p.class_tops = a.take<float>(half && want_dw && p.whole ? loss_class_ranges(n) * vocab : 0);
   p.class_inv = a.take<float>(half && want_dw ? p.classes : 0);
+  p.e32 = a.take<float>(half && want_dw && p.whole ? n * p.classes : 0);
   p.g32 = a.take<float>(half && want_dw && !p.whole ? p.classes * p.n64 : 0);
   p.acc = a.take<float>(want_dx ? n * d : 0);
   // The last piece may be shorter and be cut into other numbers of ranges: tiles times ranges stay within 256 in any case.
@@ -275,8 +281,8 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
   }
   uint16_t* const none[2] = {nullptr, nullptr};
   if (!few && !half) LQ_TRY(launch_loss_reference(X, ldx, W, ldw, d, all, p.rows, st));
-  const bool want_e = dX || (dW && p.whole);
-  const bool late = half && dW && p.whole;      // the pass that makes dW's operand of E brings it to one power of two per row as well
+  const bool late = half && dW && p.whole;      // the pass that makes dW's operand of E makes E's planes as well
+  uint16_t* const* e = (dX || (dW && p.whole)) && !late ? p.e : none;
   auto accumulate = [&](const LossPiece& piece, const Planes& w) {
     return launch_loss_accumulate(Planes{{p.e[0], half ? p.e[1] : nullptr, nullptr}, p.classes}, w, piece.classes, n, d, p.rows.shift,
                                   piece.v0 == 0, p.acc, p.part, p.part_floats, st);
@@ -286,16 +292,16 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
     const LossPiece piece{n, v0, std::min(p.classes, vocab - v0), vocab, targets};
     Planes w;
     LQ_TRY(piece_planes(v0, piece.classes, &w));
-    LQ_TRY(launch_loss_logits(w, x, p.d64, piece, p.rows, scales, p.part_ref, p.part_sum, want_e ? p.e : none, p.classes, st));
-    LQ_TRY(launch_loss_join(piece, p.rows, half, !half, p.part_ref, p.part_sum, SEG_T, want_e && !late ? p.e : none, p.classes, st));
+    LQ_TRY(launch_loss_logits(w, x, p.d64, piece, p.rows, scales, p.part_ref, p.part_sum, e,
+                              late ? p.e32 : nullptr, p.classes, st));
+    LQ_TRY(launch_loss_join(piece, p.rows, half, !half, p.part_ref, p.part_sum, SEG_T, e, p.classes, st));
     if (late) whole = w;
     else if (dX) LQ_TRY(accumulate(piece, w));
   }
   if (scales.xt_top) LQ_TRY(launch_top_magnitude(X, ldx, n, d, targets, vocab, p.tops + 1, st));
   if (!join_rows) LQ_TRY(launch_loss_rows(p.rows, scales, targets, n, vocab, mean == 1, loss, row_loss, lse, p.factors, st));
   if (dW && p.whole)
-    LQ_TRY(launch_loss_gradient_from_e(all, p.rows, half, late ? p.part_ref : nullptr, dX != nullptr, p.e, p.classes, p.g, p.n64,
-                                       p.class_tops, p.class_inv, st));
+    LQ_TRY(launch_loss_gradient_from_e(all, p.rows, p.part_ref, p.e32, p.e, p.classes, p.g, p.n64, p.class_tops, p.class_inv, st));
   if (late && dX) LQ_TRY(accumulate(all, whole));
   if (dX && few) {
     LQ_TRY(launch_few_dx(W, ldw, dtype, d, Planes{{p.few_e[0], p.few_e[1], p.few_e[2]}, p.v64}, all, p.rows, p.part_ref, p.factors,

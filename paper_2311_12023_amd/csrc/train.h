@@ -50,13 +50,6 @@ inline void add_segments(SegArgs& s, int* count, const Planes& a, const Planes& 
       s.seg[(*count)++] = Segment{a.p[i], b.p[j], a.pitch, b.pitch, s.pairs};
     }
 }
-inline int segment_count(int planes_a, int planes_b) {
-  const int most = planes_a > planes_b ? planes_a : planes_b;
-  int n = 0;
-  for (int i = 0; i < planes_a; ++i)
-    for (int j = 0; j < planes_b && i + j < most; ++j) ++n;
-  return n;
-}
 inline int64_t seg_tiles(int64_t rows, int64_t cols) { return ((rows + SEG_T - 1) / SEG_T) * ((cols + SEG_T - 1) / SEG_T); }
 // Ranges that the reduction of a product with few tiles is cut into: the parts fill the chip, each keeps eight pairs of steps.
 inline int seg_splits(int64_t tiles, int64_t pairs, int most) {
@@ -86,7 +79,7 @@ struct PlaneTarget {
 inline Planes planes_of(const PlaneTarget& t) { return {{t.p[0], t.p[1], t.p[2]}, t.pitch}; }
 // Planes with the source's rows, zero from cols up to up_to(cols, 64).
 int launch_row_planes(const PlaneSource& s, PlaneKind kind, const PlaneTarget& t, float* row_inv, hipStream_t st);
-// Planes of the transpose: t.rows rows (zero from `cols` on), zero from `rows` up to up_to(rows, 64).  keep: one int64 per source
+// Planes (BF16 or HALF_2) of the transpose: t.rows rows (zero from `cols` on), zero from `rows` up to up_to(rows, 64).  keep: one int64 per source
 // row; rows whose value lies outside [0, keep_below) are taken as zero, whatever they hold (NULL: all are taken).
 int launch_column_planes(const PlaneSource& s, PlaneKind kind, const PlaneTarget& t, const int64_t* keep, int64_t keep_below,
                          hipStream_t st);
@@ -103,7 +96,7 @@ struct PrepareJobs {
   Job job[5];
   int count;
   int rows3(const PlaneSource& s, const PlaneTarget& t);             // launch_row_planes, PLANE_BF16_3
-  int columns3(const PlaneSource& s, const PlaneTarget& t);          // launch_column_planes, PLANE_BF16_3
+  int columns3(const PlaneSource& s, const PlaneTarget& t);          // three planes of the transpose
   int rows_scaled(const PlaneSource& s, const PlaneTarget& t, float* row_inv);
   int rows(const PlaneSource& s, const PlaneTarget& t);              // bf16 into a padded plane
   int tops(const float* v, int64_t n, uint32_t* words);              // TOP_WORDS words, the largest of which is v's
@@ -130,10 +123,11 @@ struct LossPiece {           // the classes v0 .. v0 + classes - 1 of a call
 };
 int launch_zero_words(uint32_t* p, int count, hipStream_t st);
 // E[i][j] = 2^(s_ij log2 e - part_ref), 0 for the target and beyond the piece, as planes (NULL: not wanted), and per tile of 256
-// classes and row: part_ref, part_sum.  bf16: e[1], what the rounding of E left out, may be NULL.  fp32: E is stored times 2^LOSS_E_SHIFT and may reach 2^LOSS_E_ROOM.
+// classes and row: part_ref, part_sum.  bf16: e[1], what the rounding of E left out, may be NULL.  fp32: E is stored times
+// 2^LOSS_E_SHIFT and may reach 2^LOSS_E_ROOM; e32 (the whole vocabulary): in fp32 instead of planes.
 constexpr int LOSS_E_SHIFT = 13, LOSS_E_ROOM = 2;
 int launch_loss_logits(const Planes& w, const Planes& x, int64_t depth, const LossPiece& p, const LossRows& r, const LossScales& s,
-                       float* part_ref, float* part_sum, uint16_t* const e[2], int64_t e_pitch, hipStream_t st);
+                       float* part_ref, float* part_sum, uint16_t* const e[2], float* e32, int64_t e_pitch, hipStream_t st);
 // Joins the sums of tiles of `tile` classes with the row's; with e (tiles of SEG_T classes) brings E to one power of two per row.
 // told: r.ref has been set by launch_loss_reference.
 int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, bool told, const float* part_ref, const float* part_sum, int tile,
@@ -160,11 +154,11 @@ int launch_loss_dx(const LossRows& r, const LossScales& s, const int64_t* target
 // where the operands are.
 int launch_loss_gradient(const Planes& w, const Planes& x, int64_t depth, const LossPiece& p, const LossRows& r, const LossScales& s,
                          void* g, int64_t g_pitch, hipStream_t st);
-// The same from E where one piece is the whole vocabulary, as planes.  fp32: Gt's rows times a power of two each, whose inverse goes to
-// class_inv (tops: loss_class_ranges(n) x classes floats).  part_ref (fp32; NULL where E is relative to its rows' powers of two): E is
-// relative to its tiles', and with keep goes back relative to its rows'.
+// The same from E where one piece is the whole vocabulary, as planes.  bf16: of both of E's planes.  fp32 (e32, relative to part_ref):
+// Gt's rows times a power of two each, whose inverse goes to class_inv (tops: loss_class_ranges(n) x classes floats), and E's
+// planes relative to its rows' powers of two (e[0] NULL: not wanted).
 int loss_class_ranges(int64_t n);
-int launch_loss_gradient_from_e(const LossPiece& p, const LossRows& r, bool half, const float* part_ref, bool keep,
+int launch_loss_gradient_from_e(const LossPiece& p, const LossRows& r, const float* part_ref, const float* e32,
                                 uint16_t* const e[2], int64_t e_pitch, uint16_t* const g[2], int64_t g_pitch, float* tops,
                                 float* class_inv, hipStream_t st);
 // dW's rows: out (rows x cols, contiguous, of type dtype) = *factor A B^T, fp32: times class_inv per row.  part: splits x rows x cols floats.
@@ -174,8 +168,9 @@ int launch_loss_dw(const Planes& g, const Planes& xt, int64_t depth, int64_t row
 
 // ---- the same for few rows (loss_few_kernels.hip) ---------------------------------------------------------
 // Up to LOSS_FEW rows the loss is bound by reading W: it is then read where it is, once for the logits and once for dX, the whole
-// vocabulary as one piece.  Planes of X (one for bf16, three for
-// fp32) and E have few_rows(n) rows.  Tiles are LOSS_FEW_TILE classes; E is relative to its tile's power of two.
+// vocabulary as one piece.  d = 4096, 32000 classes, bf16, 16 / 64 / 128 rows: 106 / 117 / 171 us, by the products of many rows 158 /
+// 169 / 184; d = 1024, 50265 classes, fp32: 114 / 147 / 295 for 286 / 295 / 310.  Planes of X (one for bf16, three for fp32) and E have few_rows(n) rows.  Tiles are LOSS_FEW_TILE classes;
+// E is relative to its tile's power of two.
 constexpr int64_t LOSS_FEW = 128, LOSS_FEW_TILE = 64;
 inline int64_t few_rows(int64_t n) { return n <= 16 ? 16 : n <= 32 ? 32 : n <= 64 ? 64 : 128; }
 int launch_few_logits(const void* W, int64_t ldw, int dtype, int64_t d, const Planes& x, const LossPiece& p, const LossRows& r,

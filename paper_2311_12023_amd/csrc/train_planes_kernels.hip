@@ -218,10 +218,7 @@ int launch_column_planes(const PlaneSource& s, PlaneKind kind, const PlaneTarget
   if (kind == PLANE_HALF_2) {
     if (!s.top) return LQ_ERR_NULL;
     columns_of<float, PLANE_HALF_2>(a, vec, grid, st);
-  } else if (kind == PLANE_BF16_3) {
-    if (s.dtype != LQ_T_FP32) return LQ_ERR_ARG;
-    columns_of<float, PLANE_BF16_3>(a, vec, grid, st);
-  } else if (s.dtype == LQ_T_BF16) {
+  } else if (kind == PLANE_BF16 && s.dtype == LQ_T_BF16) {
     columns_of<__bf16, PLANE_BF16>(a, vec, grid, st);
   } else {
     return LQ_ERR_ARG;

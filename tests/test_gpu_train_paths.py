@@ -94,6 +94,20 @@ def test_loss_over_several_pieces(env, dtype, order):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("order", ["mixed", "growing", "falling"])
+def test_loss_over_five_pieces(env, dtype, order):
+    """3000 rows x 100003 classes: past the number of logits up to which dW's operand is kept."""
+    torch, lq = env
+    n, d, vocab = 3000, 32, 100003
+    x, w, t = _inputs(torch, n, d, vocab, dtype, 15)
+    if order != "mixed":
+        size = torch.linspace(0.01, 12.0, vocab, device="cuda")[:, None]
+        w = (w.float() * (size if order == "growing" else size.flip(0))).to(w.dtype)
+        t = torch.where(t >= 0, t % 1000, t)
+    _check_loss(torch, lq.cross_entropy(x, w, t, want_dw=True), x, w, t, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_loss_over_several_pieces_whatever_is_wanted(env, dtype):
     torch, lq = env
     x, w, t = _inputs(torch, 1100, 40, 70001, dtype, 6)
