@@ -244,9 +244,9 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
   const LossScales scales{half ? p.x_inv : nullptr, half ? p.tops : nullptr, half && dW ? p.tops + 1 : nullptr};
   // bf16 operands whose rows are whole pairs of steps on 16-byte addresses are read where they are
   auto in_place = [&](const void* a, int64_t ld) { return !half && d % 64 == 0 && ld % 8 == 0 && ld <= MOST_PITCH && !misaligned(a, 16); };
-  if (half) LQ_TRY(launch_zero_words(p.tops, 2, st));
   const char* w0 = static_cast<const char*>(W);
   const bool few = few_by_size(n, vocab, dW != nullptr);
+  if (half && !few) LQ_TRY(launch_zero_words(p.tops, 2, st));
   Planes x{{static_cast<const uint16_t*>(X), nullptr, nullptr}, ldx};
   if (!few && !in_place(X, ldx)) {
     const PlaneTarget t{{p.x[0], p.x[1], nullptr}, p.d64, n};
