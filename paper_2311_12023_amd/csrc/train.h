@@ -169,8 +169,8 @@ int launch_loss_dw(const Planes& g, const Planes& xt, int64_t depth, int64_t row
 // ---- the same for few rows (loss_few_kernels.hip) ---------------------------------------------------------
 // Up to LOSS_FEW rows the loss is bound by reading W: it is then read where it is, once for the logits and once for dX, the whole
 // vocabulary as one piece.  d = 4096, 32000 classes, bf16, 16 / 64 / 128 rows: 106 / 117 / 171 us, by the products of many rows 158 /
-// 169 / 184; d = 1024, 50265 classes, fp32: 114 / 147 / 295 for 286 / 295 / 310.  Planes of X (one for bf16, three for fp32) and E have few_rows(n) rows.  Tiles are LOSS_FEW_TILE classes;
-// E is relative to its tile's power of two.
+// 169 / 184; d = 1024, 50265 classes, fp32: 114 / 147 / 295 for 286 / 295 / 310.  Planes of X (one for bf16, three for fp32) and E have
+// few_rows(n) rows.  Tiles are LOSS_FEW_TILE classes; E is relative to its tile's power of two.
 constexpr int64_t LOSS_FEW = 128, LOSS_FEW_TILE = 64;
 inline int64_t few_rows(int64_t n) { return n <= 16 ? 16 : n <= 32 ? 32 : n <= 64 ? 64 : 128; }
 int launch_few_logits(const void* W, int64_t ldw, int dtype, int64_t d, const Planes& x, const LossPiece& p, const LossRows& r,
