@@ -7,7 +7,8 @@
  *
  * Conventions for every entry point
  *  - Matrix and vector arguments are DEVICE pointers unless the comment says "host".  Matrices are
- *    row-major, contiguous, fp32 (the fine-tuning calls say where theirs are bf16 or have a stride).  `stream` is a hipStream_t passed as void* (NULL = default stream).
+ *    row-major, contiguous, fp32 (the fine-tuning calls say where theirs are bf16 or have a stride).  `stream` is a
+ *    hipStream_t passed as void* (NULL = default stream).
  *  - The caller owns every buffer.  The library allocates no device memory: scratch space comes in
  *    through `workspace` (device, 256-byte aligned), sized by the matching *_workspace_bytes call.
  *    State the library keeps, per process: the immutable code-book tables (uploaded once per device on first
