@@ -56,6 +56,21 @@ __device__ __forceinline__ void store_blocks(uint16_t* hi, uint16_t* lo, floatx4
   if (HALF || lo) *reinterpret_cast<uintx4*>(lo) = seg_pair_blocks(l0, l1);
 }
 
+// Four neighbours of a row of `width` floats, whose start is on 16 bytes where width is a multiple of four.
+__device__ __forceinline__ void store_floats(float* at, floatx4 v, int64_t col, int64_t width) {
+  if ((width & 3) == 0) { *reinterpret_cast<floatx4*>(at) = v; return; }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (col + e < width) at[e] = v[e];
+}
+__device__ __forceinline__ floatx4 load_floats(const float* at, int64_t col, int64_t width) {
+  if ((width & 3) == 0) return *reinterpret_cast<const floatx4*>(at);
+  floatx4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = col + e < width ? at[e] : 0.0f;
+  return v;
+}
+
 // ------------------------------------------------------------------------------------------------
 // Logits of a piece.  Classes are the tile's rows and tokens its columns: a lane then holds 32 classes of each of its tokens, and
 // the maximum and the sum over the tile are reductions inside lanes, two exchanges between lanes and one through LDS between two
@@ -218,17 +233,152 @@ static int launch_tiles(void (*kernel)(Args), LdsLimit& limit, const Args& a, hi
   return LQ_OK;
 }
 
+// ------------------------------------------------------------------------------------------------
+// dW's rows of a piece: features are the tile's rows and classes its columns.  2047 x 4096 by 32000 bf16: 560 us, 0.96 PFLOP/s.
+struct DwArgs {
+  SegArgs g;
+  int64_t rows, cols;
+  const float* factor; const float* class_inv;
+  void* out; float* part;
+};
+
+template <typename H, typename T>
+__global__ __launch_bounds__(SEG_THREADS, 2) void loss_dw_kernel(DwArgs a) {
+  typedef T vec4 __attribute__((ext_vector_type(4)));
+  extern __shared__ __attribute__((aligned(16))) unsigned char seg_lds[];
+  const SegTile t = seg_tile(a.g);
+  if (!t.live) return;
+  SegAcc acc;
+  seg_clear(acc);
+  seg_products<H>(a.g, t, seg_first(a.g.pairs, t.split, a.g.splits), seg_first(a.g.pairs, t.split + 1, a.g.splits), seg_lds, acc);
+  const float f = a.g.splits > 1 ? 0.0f : *a.factor;
+  float* part = a.part + (size_t)t.split * (size_t)a.rows * (size_t)a.cols;
+  seg_each(t, acc, [&](floatx4 v, int64_t col, int64_t row) {
+    if (row >= a.rows || col >= a.cols) return;
+    if (a.g.splits > 1) { store_floats(part + row * a.cols + col, v, col, a.cols); return; }
+    T* at = static_cast<T*>(a.out) + row * a.cols + col;
+    if constexpr (sizeof(T) == 4) v *= a.class_inv[row];
+    v *= f;
+    if ((a.cols & 3) == 0 && ((uintptr_t)a.out & (4 * sizeof(T) - 1)) == 0) { *reinterpret_cast<vec4*>(at) = __builtin_convertvector(v, vec4); return; }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (col + e < a.cols) at[e] = (T)v[e];
+  });
+}
+
+int loss_dw_splits(int64_t rows, int64_t cols, int64_t depth, bool half) {
+  return seg_splits(seg_tiles(rows, cols), depth / 64 * (half ? 3 : 1), 16);
+}
+
+// part (splits x rows x cols) = ranges of B A^T's reduction.
+static int launch_parts(const Planes& a_planes, const Planes& b_planes, int64_t depth, int64_t rows, int64_t cols, bool half, float* part,
+                        hipStream_t st) {
+  DwArgs a{};
+  LQ_TRY(fill_segments(a.g, a_planes, b_planes, depth));
+  LQ_TRY(seg_shape(a.g, cols, rows, loss_dw_splits(rows, cols, depth, half)));
+  if (a.g.splits < 2) return LQ_ERR_SHAPE;
+  a.rows = rows; a.cols = cols; a.part = part;
+  static LdsLimit limit[2];
+  prof::Scope ps(prof::LOSS_LOGITS, st, 2.0 * rows * cols * depth);
+  return half ? launch_tiles(loss_dw_kernel<_Float16, float>, limit[0], a, st) : launch_tiles(loss_dw_kernel<__bf16, __bf16>, limit[1], a, st);
+}
+
+// Classes that a piece's logits have beyond whole rounds of 256 tiles, if those are up to a quarter of a round and their reduction can be
+// cut into four ranges or more: their product fills the chip then (into parts, whose sums loss_tail_kernel turns into what the
+// tiles of loss_logits_kernel become), where its tiles would leave most of the chip idle for as long as a round takes.  The whole call:
+// 1000 x 1024 by 50265 fp32 with dW 1249 us, in one product 1277; 1000 x 4096 by 50265 bf16 789, 820; 300 x 2048 by 33001 bf16 190, 195.
+static int64_t tail_classes(int64_t n, int64_t classes, int64_t depth, bool half) {
+  const int64_t across = (n + SEG_T - 1) / SEG_T, main = seg_tiles(classes, n) / 256 * 256 / across * SEG_T, rest = classes - main;
+  if (main <= 0 || rest <= 0 || seg_tiles(rest, n) > 64 || loss_dw_splits(n, rest, depth, half) < 4) return 0;
+  return rest;
+}
+size_t loss_tail_floats(int64_t n, int64_t classes, int64_t depth, bool half) {
+  const int64_t rest = tail_classes(n, classes, depth, half);
+  return rest ? (size_t)loss_dw_splits(n, rest, depth, half) * (size_t)n * (size_t)rest : 0;
+}
+
+// A wavefront per token and tile of 256 classes.
+struct TailArgs {
+  LogitsArgs l;
+  const float* part; int splits; int64_t first, rest;      // first: class of the piece
+};
+template <typename H>
+__global__ __launch_bounds__(256) void loss_tail_kernel(TailArgs a) {
+  constexpr bool HALF = !std::is_same<H, __bf16>::value;
+  const int lane = threadIdx.x & 63;
+  const int64_t token = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), at = (int64_t)blockIdx.y * SEG_T + 4 * lane, cls = a.first + at;
+  if (token >= a.l.p.n) return;
+  floatx4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (at < a.rest) {
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) x += load_floats(a.part + ((size_t)s * a.l.p.n + token) * a.rest + at, at, a.rest);
+  }
+  const float f = logit_factor(a.l.s, token);
+  const int64_t target = a.l.p.targets[token] - a.l.p.v0 - cls;
+  float top = -__builtin_inff();
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[e] *= f;
+    if (at + e >= a.rest) x[e] = -__builtin_inff();
+    else if (e == target) { a.l.target[token] = x[e]; x[e] = -__builtin_inff(); }
+    top = fmaxf(top, x[e]);
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  top = ceilf(top);
+  const float base = a.l.p.v0 == 0 && HALF ? -__builtin_inff() : a.l.ref[token], room = HALF ? (float)LOSS_E_ROOM : 64.0f;
+  const float ref = top <= base + room ? base : top;
+  const float from = (ref == -__builtin_inff() ? 0.0f : ref) - (HALF ? (float)LOSS_E_SHIFT : 0.0f);
+  float sum = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[e] = __builtin_amdgcn_exp2f(x[e] - from);
+    sum += x[e];
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+  if (lane == 0) {
+    const int64_t tile = a.first / SEG_T + blockIdx.y;
+    a.l.part_ref[tile * a.l.p.n + token] = ref;
+    a.l.part_sum[tile * a.l.p.n + token] = HALF ? sum * power_of_two(-LOSS_E_SHIFT) : sum;
+  }
+  const int64_t to = token * a.l.e_pitch + cls;              // rows of E end on whole tiles
+  if (HALF && a.l.e32) {
+    *reinterpret_cast<floatx4*>(a.l.e32 + to) = x;
+  } else if (a.l.e[0]) {
+    uintx2 hi, lo;
+    split_four<HALF>(x, hi, lo);
+    *reinterpret_cast<uintx2*>(a.l.e[0] + to) = hi;
+    if (HALF || a.l.e[1]) *reinterpret_cast<uintx2*>(a.l.e[1] + to) = lo;
+  }
+}
+
 int launch_loss_logits(const Planes& w, const Planes& x, int64_t depth, const LossPiece& p, const LossRows& r, const LossScales& s,
-                       float* part_ref, float* part_sum, uint16_t* const e[2], float* e32, int64_t e_pitch, hipStream_t st) {
+                       float* part_ref, float* part_sum, uint16_t* const e[2], float* e32, int64_t e_pitch, float* part,
+                       size_t part_floats, hipStream_t st) {
+  const bool half = s.x_inv != nullptr;
+  if (e32 && (!half || p.v0 != 0)) return LQ_ERR_ARG;
+  const int64_t rest = tail_classes(p.n, p.classes, depth, half), main = p.classes - rest;
   LogitsArgs a{};
   LQ_TRY(fill_segments(a.g, w, x, depth));
-  LQ_TRY(seg_shape(a.g, p.classes, p.n, 1));
+  LQ_TRY(seg_shape(a.g, main, p.n, 1));
   a.p = p; a.s = s; a.ref = r.ref; a.target = r.target; a.part_ref = part_ref; a.part_sum = part_sum;
   a.e[0] = e[0]; a.e[1] = e[1]; a.e32 = e32; a.e_pitch = e_pitch;
-  if (e32 && (!s.x_inv || p.v0 != 0)) return LQ_ERR_ARG;
   static LdsLimit limit[2];
-  prof::Scope ps(prof::LOSS_LOGITS, st, 2.0 * p.n * p.classes * depth);
-  return s.x_inv ? launch_tiles(loss_logits_kernel<_Float16>, limit[0], a, st) : launch_tiles(loss_logits_kernel<__bf16>, limit[1], a, st);
+  {
+    prof::Scope ps(prof::LOSS_LOGITS, st, 2.0 * p.n * main * depth);
+    LQ_TRY(half ? launch_tiles(loss_logits_kernel<_Float16>, limit[0], a, st) : launch_tiles(loss_logits_kernel<__bf16>, limit[1], a, st));
+  }
+  if (!rest) return LQ_OK;
+  if (part_floats < loss_tail_floats(p.n, p.classes, depth, half)) return LQ_ERR_WORKSPACE;
+  const Planes tail{{w.p[0] + main * w.pitch, w.p[1] ? w.p[1] + main * w.pitch : nullptr, nullptr}, w.pitch};
+  LQ_TRY(launch_parts(tail, x, depth, p.n, rest, half, part, st));
+  const TailArgs t{a, part, loss_dw_splits(p.n, rest, depth, half), main, rest};
+  prof::Scope ps(prof::LOSS_ROWS, st, (double)p.n * rest * (4.0 * t.splits + 4.0));
+  hipLaunchKernelGGL(half ? loss_tail_kernel<_Float16> : loss_tail_kernel<__bf16>,
+                     dim3((unsigned)((p.n + 3) / 4), (unsigned)((rest + SEG_T - 1) / SEG_T)), dim3(256), 0, st, t);
+  LQ_HIP_TRY(hipGetLastError());
+  return LQ_OK;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -412,21 +562,6 @@ struct AccumulateArgs {
   const float* shift; int first;
   float* acc; float* part;
 };
-
-// Four neighbours of a row of `width` floats, whose start is on 16 bytes where width is a multiple of four.
-__device__ __forceinline__ void store_floats(float* at, floatx4 v, int64_t col, int64_t width) {
-  if ((width & 3) == 0) { *reinterpret_cast<floatx4*>(at) = v; return; }
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (col + e < width) at[e] = v[e];
-}
-__device__ __forceinline__ floatx4 load_floats(const float* at, int64_t col, int64_t width) {
-  if ((width & 3) == 0) return *reinterpret_cast<const floatx4*>(at);
-  floatx4 v;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = col + e < width ? at[e] : 0.0f;
-  return v;
-}
 
 template <typename H>
 __global__ __launch_bounds__(SEG_THREADS, 2) void loss_accumulate_kernel(AccumulateArgs a) {
@@ -806,38 +941,6 @@ int launch_loss_gradient_from_e(const LossPiece& p, const LossRows& r, const flo
 }
 
 // ------------------------------------------------------------------------------------------------
-// dW's rows of a piece: features are the tile's rows and classes its columns.  2047 x 4096 by 32000 bf16: 560 us, 0.96 PFLOP/s.
-struct DwArgs {
-  SegArgs g;
-  int64_t rows, cols;
-  const float* factor; const float* class_inv;
-  void* out; float* part;
-};
-
-template <typename H, typename T>
-__global__ __launch_bounds__(SEG_THREADS, 2) void loss_dw_kernel(DwArgs a) {
-  typedef T vec4 __attribute__((ext_vector_type(4)));
-  extern __shared__ __attribute__((aligned(16))) unsigned char seg_lds[];
-  const SegTile t = seg_tile(a.g);
-  if (!t.live) return;
-  SegAcc acc;
-  seg_clear(acc);
-  seg_products<H>(a.g, t, seg_first(a.g.pairs, t.split, a.g.splits), seg_first(a.g.pairs, t.split + 1, a.g.splits), seg_lds, acc);
-  const float f = *a.factor;
-  float* part = a.part + (size_t)t.split * (size_t)a.rows * (size_t)a.cols;
-  seg_each(t, acc, [&](floatx4 v, int64_t col, int64_t row) {
-    if (row >= a.rows || col >= a.cols) return;
-    if (a.g.splits > 1) { store_floats(part + row * a.cols + col, v, col, a.cols); return; }
-    T* at = static_cast<T*>(a.out) + row * a.cols + col;
-    if constexpr (sizeof(T) == 4) v *= a.class_inv[row];
-    v *= f;
-    if ((a.cols & 3) == 0 && ((uintptr_t)a.out & (4 * sizeof(T) - 1)) == 0) { *reinterpret_cast<vec4*>(at) = __builtin_convertvector(v, vec4); return; }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (col + e < a.cols) at[e] = (T)v[e];
-  });
-}
-
 template <typename T>
 __global__ __launch_bounds__(256) void loss_dw_sum_kernel(const float* __restrict__ part, int splits, int64_t total, int64_t cols,
                                                           const float* __restrict__ factor, const float* __restrict__ class_inv,
@@ -849,10 +952,6 @@ __global__ __launch_bounds__(256) void loss_dw_sum_kernel(const float* __restric
     if constexpr (sizeof(T) == 4) v *= class_inv[i / cols];
     out[i] = (T)(v * f);
   }
-}
-
-int loss_dw_splits(int64_t rows, int64_t cols, int64_t depth, bool half) {
-  return seg_splits(seg_tiles(rows, cols), depth / 64 * (half ? 3 : 1), 16);
 }
 
 static int dw_of(const Planes& g, const Planes& xt, int64_t depth, int64_t rows, int64_t cols, const float* factor,

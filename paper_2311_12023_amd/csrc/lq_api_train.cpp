@@ -106,6 +106,8 @@ static LossPlan plan_loss(void* ws, int64_t n, int64_t d, int64_t vocab, int dty
   p.part_floats = s1 > 1 ? std::min((size_t)s1 * n * d, most) : 0;
   if (want_dw && loss_dw_splits(1, 1, p.n64, half) > 1)
     p.part_floats = std::max(p.part_floats, std::min((size_t)16 * std::min(p.classes, vocab) * d, most));
+  const int64_t first = std::min(p.classes, vocab), last = vocab - (vocab - 1) / p.classes * p.classes;
+  if (!few) p.part_floats = std::max({p.part_floats, loss_tail_floats(n, first, p.d64, half), loss_tail_floats(n, last, p.d64, half)});
   p.part = a.take<float>(p.part_floats);
   p.bytes = a.used();
   return p;
@@ -293,7 +295,7 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
     Planes w;
     LQ_TRY(piece_planes(v0, piece.classes, &w));
     LQ_TRY(launch_loss_logits(w, x, p.d64, piece, p.rows, scales, p.part_ref, p.part_sum, e,
-                              late ? p.e32 : nullptr, p.classes, st));
+                              late ? p.e32 : nullptr, p.classes, p.part, p.part_floats, st));
     LQ_TRY(launch_loss_join(piece, p.rows, half, !half, p.part_ref, p.part_sum, SEG_T, e, p.classes, st));
     if (late) whole = w;
     else if (dX) LQ_TRY(accumulate(piece, w));

@@ -127,7 +127,9 @@ int launch_zero_words(uint32_t* p, int count, hipStream_t st);
 // 2^LOSS_E_SHIFT and may reach 2^LOSS_E_ROOM; e32 (the whole vocabulary): in fp32 instead of planes.
 constexpr int LOSS_E_SHIFT = 13, LOSS_E_ROOM = 2;
 int launch_loss_logits(const Planes& w, const Planes& x, int64_t depth, const LossPiece& p, const LossRows& r, const LossScales& s,
-                       float* part_ref, float* part_sum, uint16_t* const e[2], float* e32, int64_t e_pitch, hipStream_t st);
+                       float* part_ref, float* part_sum, uint16_t* const e[2], float* e32, int64_t e_pitch, float* part,
+                       size_t part_floats, hipStream_t st);
+size_t loss_tail_floats(int64_t n, int64_t classes, int64_t depth, bool half);      // of part: the piece's last classes, in ranges
 // Joins the sums of tiles of `tile` classes with the row's; with e (tiles of SEG_T classes) brings E to one power of two per row.
 // told: r.ref has been set by launch_loss_reference.
 int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, bool told, const float* part_ref, const float* part_sum, int tile,

@@ -118,6 +118,23 @@ def test_loss_over_several_pieces_whatever_is_wanted(env, dtype):
             assert o[name] is None or torch.equal(o[name], full[name]), name
 
 
+@pytest.mark.parametrize("dtype,n,d,vocab", [
+    ("fp32", 300, 704, 33001),               # 258 tiles of logits: two beyond a round, classes that are not a multiple of four
+    ("fp32", 300, 704, 33024),
+    ("bf16", 300, 2048, 33001),
+    ("bf16", 300, 2056, 32772),              # four classes
+    ("fp32", 700, 512, 33001),               # 258 tiles of dW
+    ("bf16", 2100, 512, 33001),
+])
+def test_loss_tiles_beyond_whole_rounds(env, dtype, n, d, vocab):
+    torch, lq = env
+    x, w, t = _inputs(torch, n, d, vocab, dtype, n)
+    t[:20] = torch.arange(vocab - 20, vocab, device="cuda")             # targets among the last classes
+    _check_loss(torch, lq.cross_entropy(x, w, t, want_dw=True), x, w, t, dtype)
+    w[-100:] *= 8                                                       # the largest logits, past references from before
+    _check_loss(torch, lq.cross_entropy(x, w, t, want_dw=True), x, w, t, dtype)
+
+
 # ---------------------------------------------------------------- few rows
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
