@@ -462,21 +462,36 @@ __device__ __forceinline__ void scale_run(uint16_t* at, float e) {
   *reinterpret_cast<hx4*>(at) = v;
 }
 
+constexpr int JOIN_LOADS = 8;      // of a lane, under way together
 // told: the row has a reference from the start (launch_loss_reference).
 template <typename H>
 __device__ __forceinline__ void join_row(const JoinArgs& a, int64_t row, int lane) {
   const bool first = a.p.v0 == 0;
   const float old = first && !a.told ? -__builtin_inff() : a.r.ref[row];
   float ref = old;
-#pragma unroll 4
-  for (int t = lane; t < a.tiles; t += 64) ref = fmaxf(ref, a.part_ref[(int64_t)t * a.p.n + row]);
+  for (int t0 = lane; t0 < a.tiles; t0 += 64 * JOIN_LOADS) {
+    float mine[JOIN_LOADS];
+#pragma unroll
+    for (int q = 0; q < JOIN_LOADS; ++q) mine[q] = t0 + 64 * q < a.tiles ? a.part_ref[(int64_t)(t0 + 64 * q) * a.p.n + row] : -__builtin_inff();
+#pragma unroll
+    for (int q = 0; q < JOIN_LOADS; ++q) ref = fmaxf(ref, mine[q]);
+  }
 #pragma unroll
   for (int o = 32; o; o >>= 1) ref = fmaxf(ref, __shfl_xor(ref, o));
   const float from = ref == -__builtin_inff() ? 0.0f : ref;
   float sum = 0.0f;
-#pragma unroll 4
-  for (int t = lane; t < a.tiles; t += 64)
-    sum += a.part_sum[(int64_t)t * a.p.n + row] * __builtin_amdgcn_exp2f(a.part_ref[(int64_t)t * a.p.n + row] - from);
+  for (int t0 = lane; t0 < a.tiles; t0 += 64 * JOIN_LOADS) {
+    float mine[JOIN_LOADS], part[JOIN_LOADS];
+#pragma unroll
+    for (int q = 0; q < JOIN_LOADS; ++q) {
+      const int64_t at = (int64_t)(t0 + 64 * q) * a.p.n + row;
+      const bool live = t0 + 64 * q < a.tiles;
+      mine[q] = live ? a.part_ref[at] : -__builtin_inff();
+      part[q] = live ? a.part_sum[at] : 0.0f;
+    }
+#pragma unroll
+    for (int q = 0; q < JOIN_LOADS; ++q) sum += part[q] * __builtin_amdgcn_exp2f(mine[q] - from);
+  }
 #pragma unroll
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
   if (lane == 0) {
