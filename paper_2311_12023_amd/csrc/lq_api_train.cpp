@@ -45,7 +45,7 @@ constexpr int64_t MOST_PITCH = (int64_t)1 << 23;
 // (4096 x 4096 by 128000 without dW 6.73 ms; pieces of 2^24 7.27, of 2^28 6.88).
 static int64_t piece_classes(int64_t n, int64_t vocab) {
   const int64_t whole = up_to(vocab, SEG_T);
-  if (n <= ((int64_t)1 << 28) / vocab && whole <= MOST_PITCH / 2) return whole;
+  if (n <= ((int64_t)1 << 28) / whole && whole <= MOST_PITCH / 2) return whole;
   const int64_t most = std::min(std::max<int64_t>(SEG_T, ((int64_t)1 << 26) / n / SEG_T * SEG_T), MOST_PITCH / 2);
   const int64_t pieces = (vocab + most - 1) / most;
   return up_to((vocab + pieces - 1) / pieces, SEG_T);
