@@ -436,16 +436,18 @@ __global__ __launch_bounds__(SEG_THREADS) void adapter_join_kernel(AdapterArgs a
   }
 }
 
-// A stretch for every tile where that keeps half the chip busy, else one for every CU, of three pairs of steps at least.  Leaving CUs
-// idle costs less than their share, since the others then hold a higher clock: 1000 tokens x 11008 features, 172 tiles, fp32, the
-// whole call 402 us with a tile each, 432 with 256 stretches.
+// A stretch for every tile where that keeps half the chip busy, else up to one for every CU, of six pairs of steps at least (50 tokens x
+// 4096 features, depth 1024, fp32, the whole call 42 us; of three, with twice the parts to join, 48), of three where that leaves less
+// than 64 stretches (37 x 768, depth 768: 44 us, of six 45).  Leaving CUs idle costs less than their share, since the others then hold a
+// higher clock: 1000 tokens x 11008 features, 172 tiles, fp32, the whole call 402 us with a tile each, 432 with 256 stretches.
 static int tile_pairs(int64_t depth, int64_t depth2, int dtype) {
   return (int)(depth / 64 * (dtype == LQ_T_FP32 ? 3 : 1) + depth2 / 64 * (dtype == LQ_T_FP32 ? 6 : 3));
 }
 static int adapter_stretches(int64_t features, int64_t tokens, int64_t depth, int64_t depth2, int dtype) {
   const int64_t tiles = seg_tiles(features, tokens), rounds = (tiles + 255) / 256;
   if (2 * tiles >= 256 * rounds) return (int)tiles;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(256, tiles * tile_pairs(depth, depth2, dtype) / 3));
+  const int64_t pairs = tiles * tile_pairs(depth, depth2, dtype);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(256, std::max(pairs / 6, std::min<int64_t>(pairs / 3, 64))));
 }
 size_t adapter_part_floats(int64_t features, int64_t tokens, int64_t depth, int64_t depth2, int dtype) {
   const int s = adapter_stretches(features, tokens, depth, depth2, dtype);
