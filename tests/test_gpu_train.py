@@ -167,7 +167,7 @@ def _loss_inputs(torch, n, d, vocab, dtype, seed, ignored=0.2, lean=10.0):
     (255, 64, 513),          # a row short of a tile
     (257, 96, 300),          # a row past a tile
     (300, 520, 1030),
-    (700, 64, 50000),        # several pieces, the last one short
+    (700, 64, 50000),        # many tiles, the last one short
     (33, 1024, 2000),        # a reduction that is cut into ranges
 ])
 def test_loss_matches_definition(env, n, d, vocab, dtype):
@@ -192,7 +192,7 @@ def test_loss_outputs_do_not_depend_on_what_else_is_wanted(env, dtype):
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_loss_of_rows_in_order_of_growing_logits(env, dtype):
-    """Classes sorted by their logits, over several pieces: the reference a row's sum is relative to grows with every tile, and
+    """Classes sorted by their logits, over many tiles: the reference a row's sum is relative to grows with every tile, and
     the largest logits are far from the first."""
     torch, lq = env
     n, d, vocab = 600, 64, 70000

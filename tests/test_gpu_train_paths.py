@@ -81,8 +81,8 @@ def _inputs(torch, n, d, vocab, dtype, seed, ignored=0.1):
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("order", ["mixed", "growing", "falling"])
 def test_loss_over_several_pieces(env, dtype, order):
-    """1500 rows x 100003 classes, three pieces, the last one short.  growing: the largest logits of a row grow from class to class by
-    a hundred and more in base 2, past any reference that an earlier piece or the target gives."""
+    """1500 rows x 100003 classes, 391 tiles of them, the last one short.  growing: the largest logits of a row grow from class to class
+    by a hundred and more in base 2, past any reference that an earlier tile or the target gives."""
     torch, lq = env
     n, d, vocab = 1500, 32, 100003
     x, w, t = _inputs(torch, n, d, vocab, dtype, 5)
@@ -96,7 +96,7 @@ def test_loss_over_several_pieces(env, dtype, order):
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("order", ["mixed", "growing", "falling"])
 def test_loss_over_five_pieces(env, dtype, order):
-    """3000 rows x 100003 classes: past the number of logits up to which dW's operand is kept."""
+    """3000 rows x 100003 classes: past the number of logits up to which the vocabulary is one piece, and dW takes a second product."""
     torch, lq = env
     n, d, vocab = 3000, 32, 100003
     x, w, t = _inputs(torch, n, d, vocab, dtype, 15)
@@ -108,9 +108,10 @@ def test_loss_over_five_pieces(env, dtype, order):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
-def test_loss_over_several_pieces_whatever_is_wanted(env, dtype):
+@pytest.mark.parametrize("n", [1100, 4100])              # one piece, several
+def test_loss_over_several_pieces_whatever_is_wanted(env, dtype, n):
     torch, lq = env
-    x, w, t = _inputs(torch, 1100, 40, 70001, dtype, 6)
+    x, w, t = _inputs(torch, n, 40, 70001, dtype, 6)
     full = lq.cross_entropy(x, w, t, want_dw=True)
     for dx, dw in ((False, False), (True, False), (False, True)):
         o = lq.cross_entropy(x, w, t, want_dx=dx, want_dw=dw)
