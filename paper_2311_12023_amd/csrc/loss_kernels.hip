@@ -283,13 +283,14 @@ static int launch_parts(const Planes& a_planes, const Planes& b_planes, int64_t 
   return half ? launch_tiles(loss_dw_kernel<_Float16, float>, limit[0], a, st) : launch_tiles(loss_dw_kernel<__bf16, __bf16>, limit[1], a, st);
 }
 
-// Classes that a piece's logits have beyond whole rounds of 256 tiles, if those are up to a quarter of a round and their reduction can be
-// cut into four ranges or more: their product fills the chip then (into parts, whose sums loss_tail_kernel turns into what the
+// Classes that a piece's logits have beyond whole rounds of 256 tiles (all, if there is none), if those are up to a quarter of a round
+// and their reduction can be cut into four ranges or more: their product fills the chip then (into parts, whose sums loss_tail_kernel turns into what the
 // tiles of loss_logits_kernel become), where its tiles would leave most of the chip idle for as long as a round takes.  The whole call:
-// 1000 x 1024 by 50265 fp32 with dW 1249 us, in one product 1277; 1000 x 4096 by 50265 bf16 789, 820; 300 x 2048 by 33001 bf16 190, 195.
+// 1000 x 1024 by 50265 fp32 with dW 1249 us, in one product 1277; 1000 x 4096 by 50265 bf16 789, 820; 300 x 2048 by 33001 bf16 190, 195;
+// 200 x 4096 by 1500 (six tiles) fp32 with dW 162, 356; 500 x 4096 by 8000 (64 tiles) bf16 124, 153.
 static int64_t tail_classes(int64_t n, int64_t classes, int64_t depth, bool half) {
   const int64_t across = (n + SEG_T - 1) / SEG_T, main = seg_tiles(classes, n) / 256 * 256 / across * SEG_T, rest = classes - main;
-  if (main <= 0 || rest <= 0 || seg_tiles(rest, n) > 64 || loss_dw_splits(n, rest, depth, half) < 4) return 0;
+  if (rest <= 0 || seg_tiles(rest, n) > 64 || loss_dw_splits(n, rest, depth, half) < 4) return 0;
   return rest;
 }
 size_t loss_tail_floats(int64_t n, int64_t classes, int64_t depth, bool half) {
@@ -360,12 +361,12 @@ int launch_loss_logits(const Planes& w, const Planes& x, int64_t depth, const Lo
   if (e32 && (!half || p.v0 != 0)) return LQ_ERR_ARG;
   const int64_t rest = tail_classes(p.n, p.classes, depth, half), main = p.classes - rest;
   LogitsArgs a{};
-  LQ_TRY(fill_segments(a.g, w, x, depth));
-  LQ_TRY(seg_shape(a.g, main, p.n, 1));
   a.p = p; a.s = s; a.ref = r.ref; a.target = r.target; a.part_ref = part_ref; a.part_sum = part_sum;
   a.e[0] = e[0]; a.e[1] = e[1]; a.e32 = e32; a.e_pitch = e_pitch;
-  static LdsLimit limit[2];
-  {
+  if (main > 0) {
+    static LdsLimit limit[2];
+    LQ_TRY(fill_segments(a.g, w, x, depth));
+    LQ_TRY(seg_shape(a.g, main, p.n, 1));
     prof::Scope ps(prof::LOSS_LOGITS, st, 2.0 * p.n * main * depth);
     LQ_TRY(half ? launch_tiles(loss_logits_kernel<_Float16>, limit[0], a, st) : launch_tiles(loss_logits_kernel<__bf16>, limit[1], a, st));
   }
