@@ -51,7 +51,11 @@ static int64_t piece_classes(int64_t n, int64_t vocab) {
   return up_to((vocab + pieces - 1) / pieces, SEG_T);
 }
 
-static bool few_by_size(int64_t n, int64_t vocab, bool want_dw) { return n <= LOSS_FEW && vocab <= MOST_PITCH / 2 && !want_dw; }
+// Not where rows are long and classes few: there are too few workgroups then, each with a long way (d = 4096, 1500 classes, fp32, 16 and
+// 128 rows 123 and 159 us, by the products of many rows 89 and 100; 4000 classes 131 and 188 for 135 and 154).
+static bool few_by_size(int64_t n, int64_t d, int64_t vocab, bool want_dw) {
+  return n <= LOSS_FEW && vocab <= MOST_PITCH / 2 && d <= 2 * vocab && !want_dw;
+}
 
 struct LossPlan {
   LossRows rows;
@@ -77,7 +81,7 @@ static LossPlan plan_loss(void* ws, int64_t n, int64_t d, int64_t vocab, int dty
   p.factors = a.take<float>(2);
   p.tops = a.take<uint32_t>(2);
   p.x_inv = a.take<float>(half ? n : 0);
-  const bool few = few_by_size(n, vocab, want_dw);
+  const bool few = few_by_size(n, d, vocab, want_dw);
   p.v64 = up_to(vocab, 64);
   const int64_t tiles = std::max(p.classes / SEG_T, few ? p.v64 / LOSS_FEW_TILE : 0);
   for (int h = 0; h < (half ? 3 : 1); ++h) {
@@ -247,7 +251,7 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
   // bf16 operands whose rows are whole pairs of steps on 16-byte addresses are read where they are
   auto in_place = [&](const void* a, int64_t ld) { return !half && d % 64 == 0 && ld % 8 == 0 && ld <= MOST_PITCH && !misaligned(a, 16); };
   const char* w0 = static_cast<const char*>(W);
-  const bool few = few_by_size(n, vocab, dW != nullptr);
+  const bool few = few_by_size(n, d, vocab, dW != nullptr);
   if (half && !few) LQ_TRY(launch_zero_words(p.tops, 2, st));
   Planes x{{static_cast<const uint16_t*>(X), nullptr, nullptr}, ldx};
   if (!few && !in_place(X, ldx)) {

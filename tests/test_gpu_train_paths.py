@@ -148,6 +148,8 @@ def test_loss_tiles_beyond_whole_rounds(env, dtype, n, d, vocab):
     (65, 24, 4099),
     (128, 520, 777),
     (2, 1, 1),
+    (20, 2056, 1000),        # long rows over few classes
+    (1, 2000, 999),
 ])
 def test_few_rows(env, n, d, vocab, dtype):
     torch, lq = env
