@@ -42,11 +42,11 @@ __global__ __launch_bounds__(256) void few_logits_kernel(FewLogitsArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int64_t c = class0 + TILE * h + e;
-        float x = acc[h][r][e] * LOG2E;
+        float x = acc[h][r][e];
         if (c >= a.p.vocab) x = -__builtin_inff();
-        else if (c == target) { a.target[token] = x; x = -__builtin_inff(); }
+        else if (c == target) { a.target[token] = x * LOG2E; x = -__builtin_inff(); }
         acc[h][r][e] = x;
-        top = fmaxf(top, x);
+        top = fmaxf(top, x * LOG2E);
       }
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(256) void few_logits_kernel(FewLogitsArgs a) {
       float sum = 0.0f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        acc[h][r][e] = __builtin_amdgcn_exp2f(acc[h][r][e] - from);
+        acc[h][r][e] = __builtin_amdgcn_exp2f(fmaf(acc[h][r][e], LOG2E, -from));
         sum += acc[h][r][e];
       }
       sum += __shfl_xor(sum, 16);

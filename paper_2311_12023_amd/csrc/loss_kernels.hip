@@ -397,10 +397,10 @@ __device__ __forceinline__ void finish_rows(const RowsArgs& a) {
   uint32_t count = 0;
   for (int64_t i = threadIdx.x; i < a.n; i += 1024) {
     const int64_t t = a.targets[i];
-    const float others = a.r.ref[i] + log2f(a.r.sum[i]);      // log2 of the sum without the target; -inf: there is no other class
+    const float size = log2f(a.r.sum[i]), others = a.r.ref[i] + size;      // log2 of the sum without the target; -inf: no other class
     float l = 0.0f, wrong = 0.0f, all = others;
     if (t >= 0 && t < a.vocab) {
-      const float z = a.r.target[i] - others;
+      const float z = (a.r.target[i] - a.r.ref[i]) - size;     // the reference is whole: one rounding less than target - others
       l = fmaxf(-z, 0.0f) * LN2 + log1pf(exp2f(-fabsf(z)));
       wrong = 1.0f / (1.0f + exp2f(z));
       all = fmaxf(a.r.target[i], others) + log1pf(exp2f(-fabsf(z))) * LOG2E;
