@@ -13,7 +13,7 @@ constexpr float LOG2E = 1.4426950408889634f;
 struct FewLogitsArgs {
   ThinSource w; Planes x;
   LossPiece p;
-  float* target; float* part_ref; float* part_sum;
+  float* part_ref; float* part_sum;
   uint16_t* e[3]; int64_t e_pitch;
   int steps;
 };
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256) void few_logits_kernel(FewLogitsArgs a) {
         const int64_t c = class0 + TILE * h + e;
         float x = acc[h][r][e];
         if (c >= a.p.vocab) x = -__builtin_inff();
-        else if (c == target) { a.target[token] = x * LOG2E; x = -__builtin_inff(); }
+        else if (c == target) x = -__builtin_inff();      // its logit: when the rows are joined
         acc[h][r][e] = x;
         top = fmaxf(top, x * LOG2E);
       }
@@ -112,14 +112,14 @@ static int few_logits_of(const FewLogitsArgs& a, bool vec, hipStream_t st) {
   }
 }
 
-int launch_few_logits(const void* W, int64_t ldw, int dtype, int64_t d, const Planes& x, const LossPiece& p, const LossRows& r,
-                      float* part_ref, float* part_sum, uint16_t* const e[3], int64_t e_pitch, hipStream_t st) {
+int launch_few_logits(const void* W, int64_t ldw, int dtype, int64_t d, const Planes& x, const LossPiece& p, float* part_ref,
+                      float* part_sum, uint16_t* const e[3], int64_t e_pitch, hipStream_t st) {
   if (p.n > LOSS_FEW || p.v0 != 0 || p.classes != p.vocab || x.pitch < up_to(d, 64) ||
       (e[0] && (e_pitch % LOSS_FEW_TILE || e_pitch < p.vocab)))
     return LQ_ERR_SHAPE;
   FewLogitsArgs a{};
   a.w = ThinSource{W, ldw, p.vocab, d, DropoutMask{}};
-  a.x = x; a.p = p; a.target = r.target; a.part_ref = part_ref; a.part_sum = part_sum;
+  a.x = x; a.p = p; a.part_ref = part_ref; a.part_sum = part_sum;
   for (int k = 0; k < 3; ++k) a.e[k] = e[k];
   a.e_pitch = e_pitch;
   a.steps = (int)((d + 63) / 64);

@@ -449,6 +449,7 @@ struct JoinArgs {
   const float* part_ref; const float* part_sum; int tiles;
   uint16_t* e[2]; int64_t e_pitch;
   int told;
+  LossOperands o;
 };
 
 // v *= 2^e, e <= 0, in two steps: 2^e can leave the range where a value of up to 2^64 times it does not.
@@ -461,6 +462,32 @@ __device__ __forceinline__ void scale_run(uint16_t* at, float e) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) v[k] = (H)((float)v[k] * f * g);
   *reinterpret_cast<hx4*>(at) = v;
+}
+
+// The target's logit of a row by a wavefront, whose lanes' sums are short: along the matrix pipe's chain of d / 32 sums it is off by
+// some 1e-6, which is most of a row loss's error, since those of the other classes cancel in their sum.
+template <typename T>
+__device__ __forceinline__ void join_target(const JoinArgs& a, int64_t row, int lane) {
+  typedef T vec8 __attribute__((ext_vector_type(8)));
+  const int64_t t = a.p.targets[row];
+  if (t < 0 || t >= a.p.vocab) return;
+  const T *x = static_cast<const T*>(a.o.X) + row * a.o.ldx, *w = static_cast<const T*>(a.o.W) + t * a.o.ldw;
+  float sum[2] = {0.0f, 0.0f};
+  if (a.o.vec) {
+#pragma unroll 4
+    for (int64_t k = 8 * lane; k < a.o.d; k += 512) {
+      const vec8 u = *reinterpret_cast<const vec8*>(x + k), v = *reinterpret_cast<const vec8*>(w + k);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j & 1] = fmaf((float)u[j], (float)v[j], sum[j & 1]);
+    }
+  } else {
+#pragma unroll 4
+    for (int64_t k = lane; k < a.o.d; k += 64) sum[0] = fmaf((float)x[k], (float)w[k], sum[0]);
+  }
+  float s = sum[0] + sum[1];
+#pragma unroll
+  for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+  if (lane == 0) a.r.target[row] = s * LOG2E;
 }
 
 constexpr int JOIN_LOADS = 8;      // of a lane, under way together
@@ -517,13 +544,20 @@ __device__ __forceinline__ void join_row(const JoinArgs& a, int64_t row, int lan
 template <typename H>
 __global__ __launch_bounds__(256) void loss_join_kernel(JoinArgs a) {
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row < a.p.n) join_row<H>(a, row, threadIdx.x & 63);
+  if (row >= a.p.n) return;
+  if (a.o.W && a.o.dtype == LQ_T_BF16) join_target<__bf16>(a, row, threadIdx.x & 63);
+  else if (a.o.W) join_target<float>(a, row, threadIdx.x & 63);
+  join_row<H>(a, row, threadIdx.x & 63);
 }
 
 // Up to 16 rows, whole vocabulary: one workgroup joins and finishes them.
 __global__ __launch_bounds__(1024) void loss_join_rows_kernel(JoinArgs a, RowsArgs rows) {
   const int64_t row = threadIdx.x >> 6;
-  if (row < a.p.n) join_row<__bf16>(a, row, threadIdx.x & 63);
+  if (row < a.p.n) {
+    if (a.o.dtype == LQ_T_BF16) join_target<__bf16>(a, row, threadIdx.x & 63);
+    else join_target<float>(a, row, threadIdx.x & 63);
+    join_row<__bf16>(a, row, threadIdx.x & 63);
+  }
   __threadfence_block();
   __syncthreads();
   finish_rows(rows);
@@ -545,8 +579,8 @@ __global__ __launch_bounds__(256) void loss_shift_kernel(JoinArgs a) {
 }
 
 int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, bool told, const float* part_ref, const float* part_sum, int tile,
-                     uint16_t* const e[2], int64_t e_pitch, hipStream_t st) {
-  const JoinArgs a{p, r, part_ref, part_sum, (int)((p.classes + tile - 1) / tile), {e[0], e[1]}, e_pitch, told};
+                     uint16_t* const e[2], int64_t e_pitch, const LossOperands& o, hipStream_t st) {
+  const JoinArgs a{p, r, part_ref, part_sum, (int)((p.classes + tile - 1) / tile), {e[0], e[1]}, e_pitch, told, o};
   prof::Scope ps(prof::LOSS_ROWS, st, (double)p.n * a.tiles * 8.0);
   auto kernel = half ? loss_join_kernel<_Float16> : loss_join_kernel<__bf16>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)((p.n + 3) / 4)), dim3(256), 0, st, a);
@@ -559,9 +593,10 @@ int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, bool told
 }
 
 int launch_loss_join_rows(const LossPiece& p, const LossRows& r, const float* part_ref, const float* part_sum, int tile, bool mean,
-                          float* loss, float* row_loss, float* lse, float* factors, hipStream_t st) {
+                          const LossOperands& o, float* loss, float* row_loss, float* lse, float* factors, hipStream_t st) {
+  if (!o.X || !o.W) return LQ_ERR_NULL;
   if (p.n > 16 || p.v0 != 0 || p.classes != p.vocab) return LQ_ERR_SHAPE;
-  const JoinArgs a{p, r, part_ref, part_sum, (int)((p.classes + tile - 1) / tile), {nullptr, nullptr}, 0, 0};
+  const JoinArgs a{p, r, part_ref, part_sum, (int)((p.classes + tile - 1) / tile), {nullptr, nullptr}, 0, 0, o};
   const RowsArgs rows{r, LossScales{}, p.targets, p.n, p.vocab, (int)mean, loss, row_loss, lse, factors};
   prof::Scope ps(prof::LOSS_ROWS, st, (double)p.n * a.tiles * 8.0);
   hipLaunchKernelGGL(loss_join_rows_kernel, dim3(1), dim3(1024), 0, st, a, rows);

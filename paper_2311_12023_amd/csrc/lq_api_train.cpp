@@ -275,15 +275,17 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
   const LossPiece all{n, 0, vocab, vocab, targets};
   const bool join_rows = few && n <= 16;
   if (few) {
+    const int vec = d % 8 == 0 && ldx % 8 == 0 && ldw % 8 == 0 && !misaligned(X, 8 * size) && !misaligned(W, 8 * size);
+    const LossOperands operands{X, ldx, W, ldw, d, dtype, vec};
     const PlaneTarget t{{p.few_x[0], p.few_x[1], p.few_x[2]}, p.d64, few_rows(n)};
     uint16_t* const e[3] = {dX ? p.few_e[0] : nullptr, dX ? p.few_e[1] : nullptr, dX ? p.few_e[2] : nullptr};
     uint16_t* const none[2] = {nullptr, nullptr};
     LQ_TRY(launch_row_planes({X, dtype, ldx, n, d, nullptr}, half ? PLANE_BF16_3 : PLANE_BF16, t, nullptr, st));
-    LQ_TRY(launch_few_logits(W, ldw, dtype, d, planes_of(t), all, p.rows, p.part_ref, p.part_sum, e, p.v64, st));
+    LQ_TRY(launch_few_logits(W, ldw, dtype, d, planes_of(t), all, p.part_ref, p.part_sum, e, p.v64, st));
     if (join_rows)
-      LQ_TRY(launch_loss_join_rows(all, p.rows, p.part_ref, p.part_sum, LOSS_FEW_TILE, mean == 1, loss, row_loss, lse, p.factors, st));
+      LQ_TRY(launch_loss_join_rows(all, p.rows, p.part_ref, p.part_sum, LOSS_FEW_TILE, mean == 1, operands, loss, row_loss, lse, p.factors, st));
     else
-      LQ_TRY(launch_loss_join(all, p.rows, half, false, p.part_ref, p.part_sum, LOSS_FEW_TILE, none, 0, st));
+      LQ_TRY(launch_loss_join(all, p.rows, half, false, p.part_ref, p.part_sum, LOSS_FEW_TILE, none, 0, operands, st));
   }
   uint16_t* const none[2] = {nullptr, nullptr};
   if (!few && !half) LQ_TRY(launch_loss_reference(X, ldx, W, ldw, d, all, p.rows, st));
@@ -300,7 +302,7 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
     LQ_TRY(piece_planes(v0, piece.classes, &w));
     LQ_TRY(launch_loss_logits(w, x, p.d64, piece, p.rows, scales, p.part_ref, p.part_sum, e,
                               late ? p.e32 : nullptr, p.classes, p.part, p.part_floats, st));
-    LQ_TRY(launch_loss_join(piece, p.rows, half, !half, p.part_ref, p.part_sum, SEG_T, e, p.classes, st));
+    LQ_TRY(launch_loss_join(piece, p.rows, half, !half, p.part_ref, p.part_sum, SEG_T, e, p.classes, LossOperands{}, st));
     if (late) whole = w;
     else if (dX) LQ_TRY(accumulate(piece, w));
   }

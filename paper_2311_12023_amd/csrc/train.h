@@ -130,13 +130,15 @@ int launch_loss_logits(const Planes& w, const Planes& x, int64_t depth, const Lo
                        float* part_ref, float* part_sum, uint16_t* const e[2], float* e32, int64_t e_pitch, float* part,
                        size_t part_floats, hipStream_t st);
 size_t loss_tail_floats(int64_t n, int64_t classes, int64_t depth, bool half);      // of part: the piece's last classes, in ranges
+// X and W for the logits of the targets (W NULL: the tiles have found them).
+struct LossOperands { const void* X; int64_t ldx; const void* W; int64_t ldw, d; int dtype, vec; };
 // Joins the sums of tiles of `tile` classes with the row's; with e (tiles of SEG_T classes) brings E to one power of two per row.
 // told: r.ref has been set by launch_loss_reference.
 int launch_loss_join(const LossPiece& p, const LossRows& r, bool half, bool told, const float* part_ref, const float* part_sum, int tile,
-                     uint16_t* const e[2], int64_t e_pitch, hipStream_t st);
+                     uint16_t* const e[2], int64_t e_pitch, const LossOperands& o, hipStream_t st);
 // Joins and finishes up to 16 rows in one launch (the whole vocabulary as one piece, no E to bring to another power of two).
 int launch_loss_join_rows(const LossPiece& p, const LossRows& r, const float* part_ref, const float* part_sum, int tile, bool mean,
-                          float* loss, float* row_loss, float* lse, float* factors, hipStream_t st);
+                          const LossOperands& o, float* loss, float* row_loss, float* lse, float* factors, hipStream_t st);
 // acc (n x d) = acc shift + E W; first: acc = E W.  W: `classes` rows of at least up_to(d, 8) elements; E is zero from there to
 // up_to(classes, 64).  part: splits x n x d floats.
 int loss_accumulate_splits(int64_t n, int64_t d, int64_t depth, bool half);
@@ -175,8 +177,8 @@ int launch_loss_dw(const Planes& g, const Planes& xt, int64_t depth, int64_t row
 // few_rows(n) rows.  Tiles are LOSS_FEW_TILE classes; E is relative to its tile's power of two.
 constexpr int64_t LOSS_FEW = 128, LOSS_FEW_TILE = 64;
 inline int64_t few_rows(int64_t n) { return n <= 16 ? 16 : n <= 32 ? 32 : n <= 64 ? 64 : 128; }
-int launch_few_logits(const void* W, int64_t ldw, int dtype, int64_t d, const Planes& x, const LossPiece& p, const LossRows& r,
-                      float* part_ref, float* part_sum, uint16_t* const e[3], int64_t e_pitch, hipStream_t st);
+int launch_few_logits(const void* W, int64_t ldw, int dtype, int64_t d, const Planes& x, const LossPiece& p, float* part_ref,
+                      float* part_sum, uint16_t* const e[3], int64_t e_pitch, hipStream_t st);
 // dX from E and W once r.wrong is there.  part: few_dx_splits(vocab, d) x d x few_rows(n) floats.
 int few_dx_splits(int64_t vocab, int64_t d);
 int launch_few_dx(const void* W, int64_t ldw, int dtype, int64_t d, const Planes& e, const LossPiece& p, const LossRows& r,
