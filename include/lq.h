@@ -357,6 +357,8 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
  *   X m x d, Y and dY m x k, dX m x d (NULL: not wanted, for a first layer): contiguous, of type dtype, 16-byte aligned
  *   codes_packed, scale_idx, v    Q as for lq_matmul        L1 d x rank, L2 rank x k (forward: 16-byte aligned)
  *   T        m x rank fp32, written by the forward and read by the backward call
+ *   fp32: rows of X and dY may have any magnitude beside one another (parts of T and U below 2^-125 are lost); where all stored weights are
+ *   below 2^-82, they keep 2^-104, not 22 bits, and a low-rank part of 2^34 times the largest value of its row of X or dY overflows
  *   rank in [1, 128] (LQ_ERR_RANK); d a multiple of 32, k of the block size; m below 2^24, ceil(m / 256) * 256 * max(d, k) and
  *   d * k below 2^31 (LQ_ERR_SHAPE)
  */

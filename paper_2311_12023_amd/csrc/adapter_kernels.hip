@@ -87,6 +87,14 @@ struct WeightArgs {
   const DevTables* tables; const uint32_t* top;
 };
 
+// The exponent that fp32 weights go into their planes with.  At most 80: the low-rank part is brought to the accumulators' unit, 2^14
+// from it per row of activations and this from the weights, and stays below 2^128 unless it is 2^34 times its row's largest value.
+// Weights lose bits to that only if all of them are below 2^-82.
+__device__ __forceinline__ int weight_exponent(const uint32_t* __restrict__ top) {
+  const int e = half_exponent_of(top, TOP_WORDS);
+  return e < 80 ? e : 80;
+}
+
 template <int BITS>
 __device__ __forceinline__ void decode_run(const WeightArgs& a, const float* s_code, int64_t row, int64_t c, float scale, float (&w)[16]) {
   const int64_t e = row * a.N + c, blk = e >> a.block_shift;
@@ -120,7 +128,7 @@ __device__ __forceinline__ void weight_pair(float a, float b, uint32_t& hi, uint
 template <int BITS, bool HALF>
 __device__ __forceinline__ void weight_rows(const WeightArgs& a, uint32_t block, uint32_t wgs, float* s_code) {
   load_codebook<BITS>(a, s_code);
-  const float scale = HALF ? power_of_two(half_exponent_of(a.top, TOP_WORDS)) : 1.0f;
+  const float scale = HALF ? power_of_two(weight_exponent(a.top)) : 1.0f;
   const int64_t runs = (a.N + 63) / 64 * 4, total = a.K * runs;       // runs of 16 up to a multiple of 64 weights
   for (int64_t u = (int64_t)block * 256 + threadIdx.x; u < total; u += (int64_t)wgs * 256) {
     const int64_t row = u / runs, c = (u - row * runs) * 16;
@@ -150,7 +158,7 @@ template <int BITS, bool HALF>
 __device__ __forceinline__ void weight_columns(const WeightArgs& a, uint32_t bx, uint32_t by, float* s_code,
                                                uint32_t (&s_w)[HALF ? 2 : 1][WC_N * WC_WORDS]) {
   load_codebook<BITS>(a, s_code);
-  const float scale = HALF ? power_of_two(half_exponent_of(a.top, TOP_WORDS)) : 1.0f;
+  const float scale = HALF ? power_of_two(weight_exponent(a.top)) : 1.0f;
   const int tid = threadIdx.x, run = tid & 7, pair = tid >> 3;
   const int64_t n0 = (int64_t)bx * WC_N, k0 = (int64_t)by * WC_K, col = n0 + 16 * run;
   float w[2][16];
@@ -296,21 +304,27 @@ constexpr int64_t PART_TILE = (int64_t)SEG_T * SEG_T;
 
 __device__ __forceinline__ int stretch_begin(const AdapterArgs& a, int w) { return a.per * w + (w < a.more ? w : a.more); }
 
-// What the sums of the fp16 planes of a token are to be multiplied by.
+// The sums of the fp16 planes of a token are 2^exps times what they stand for.  The power of two itself need not be a float, nor its
+// inverse: rows of gradients below 2^-97 are ordinary (a token that is certain of its target), so sums are moved by exponents.
 template <bool HALF>
-__device__ __forceinline__ void token_factors(const AdapterArgs& a, int64_t col0, float (&inv)[4]) {
-  const float a_inv = HALF ? power_of_two(-half_exponent_of(a.s.a_top, TOP_WORDS)) : 1.0f;
+__device__ __forceinline__ void token_exponents(const AdapterArgs& a, int64_t col0, int (&exps)[4]) {
+  const int of_weights = HALF ? weight_exponent(a.s.a_top) : 0;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int64_t token = col0 + 16 * j;
-    inv[j] = HALF && token < a.tokens ? a.s.b_inv[token] * a_inv : 1.0f;
+    exps[j] = HALF && token < a.tokens ? of_weights + 127 - (int)(__float_as_uint(a.s.b_inv[token]) >> 23) : 0;
   }
+}
+__device__ __forceinline__ floatx4 times_power_of_two(floatx4 v, int e) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = __builtin_ldexpf(v[k], e);
+  return v;
 }
 
 // A finished tile's blocks to `out`.
 template <typename T>
 __device__ __forceinline__ void store_tile(const AdapterArgs& a, const SegAcc& acc, const SegTile& t, int64_t row0, int64_t col0,
-                                           const float (&inv)[4]) {
+                                           const int (&exps)[4]) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int64_t token = col0 + 16 * j;
@@ -327,7 +341,7 @@ __device__ __forceinline__ void store_tile(const AdapterArgs& a, const SegAcc& a
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int64_t row = row0 + 16 * i;            // features are a multiple of 16
-        if (row < a.features) *reinterpret_cast<floatx4*>(static_cast<float*>(a.out) + token * a.features + row) = acc[i][j] * inv[j];
+        if (row < a.features) *reinterpret_cast<floatx4*>(static_cast<float*>(a.out) + token * a.features + row) = times_power_of_two(acc[i][j], -exps[j]);
       }
     }
   }
@@ -347,15 +361,15 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void adapter_product_kernel(Adapter
     const int64_t row0 = (int64_t)t.tm * SEG_T + 128 * t.wm + 4 * t.kg, col0 = (int64_t)t.tn * SEG_T + 64 * t.wn + t.l16;
     SegAcc acc;
     seg_clear(acc);
-    float inv[4];
-    token_factors<HALF>(a, col0, inv);
+    int exps[4];
+    token_exponents<HALF>(a, col0, exps);
     if (s0 < low) {
       seg_products<__bf16>(a.low, t, s0, s1 < low ? s1 : low, seg_lds, acc);
       if (HALF || a.masked) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint64_t group = (uint64_t)(col0 + 16 * j) * (uint64_t)(a.features >> 3) + (uint64_t)(row0 >> 3);
-          const float scale = (a.masked ? a.mask.scale : 1.0f) * (HALF ? 1.0f / inv[j] : 1.0f);
+          const float scale = a.mask.scale;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             if (a.masked) {
@@ -365,9 +379,8 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void adapter_product_kernel(Adapter
               acc[i][j][1] = (w0 >> 16) >= a.mask.cut ? acc[i][j][1] * scale : 0.0f;
               acc[i][j][2] = (w1 & 0xffffu) >= a.mask.cut ? acc[i][j][2] * scale : 0.0f;
               acc[i][j][3] = (w1 >> 16) >= a.mask.cut ? acc[i][j][3] * scale : 0.0f;
-            } else {
-              acc[i][j] *= scale;
             }
+            if constexpr (HALF) acc[i][j] = times_power_of_two(acc[i][j], exps[j]);
           }
         }
       }
@@ -375,7 +388,7 @@ __global__ __launch_bounds__(SEG_THREADS, 2) void adapter_product_kernel(Adapter
     }
     if (s1 > low) seg_products<H>(a.g, t, s0 > low ? s0 - low : 0, s1 - low, seg_lds, acc);
     if (s0 == 0 && s1 == pairs) {
-      store_tile<T>(a, acc, t, row0, col0, inv);
+      store_tile<T>(a, acc, t, row0, col0, exps);
     } else {
       floatx4* part = reinterpret_cast<floatx4*>(a.part + (2 * (int64_t)w + (pos == begin ? 0 : 1)) * PART_TILE) + threadIdx.x;
 #pragma unroll
@@ -408,8 +421,8 @@ __global__ __launch_bounds__(SEG_THREADS) void adapter_join_kernel(AdapterArgs a
   const int head = stretch_begin(a, w) < first ? 1 : 0;
   const floatx4* part = reinterpret_cast<const floatx4*>(a.part + 2 * (int64_t)w * PART_TILE) + threadIdx.x;
   constexpr int64_t NEXT = 2 * PART_TILE / 4;
-  float inv[4];
-  token_factors<HALF>(a, col0, inv);
+  int exps[4];
+  token_exponents<HALF>(a, col0, exps);
   floatx4 v[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) v[j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -432,7 +445,7 @@ __global__ __launch_bounds__(SEG_THREADS) void adapter_join_kernel(AdapterArgs a
   for (int j = 0; j < 4; ++j) {
     const int64_t token = col0 + 16 * j;
     if (token < a.tokens && row < a.features)
-      *reinterpret_cast<vec4*>(static_cast<T*>(a.out) + token * a.features + row) = __builtin_convertvector(v[j] * inv[j], vec4);
+      *reinterpret_cast<vec4*>(static_cast<T*>(a.out) + token * a.features + row) = __builtin_convertvector(times_power_of_two(v[j], -exps[j]), vec4);
   }
 }
 
