@@ -1,0 +1,84 @@
+"""The cross entropy of few rows (up to 128 without dW take kernels of their own): rows with strides.
+
+Tolerances (derived before any run).  fp32 operands are three bf16 planes, 24 bits, six products per 32 reduction indices, each of which
+rounds by at most 2^-23 of the terms: a logit is off by 2^-24 and that of |x||w|, one of bf16 operands (whose products are exact) by one
+product per 32 indices; 2^-22 |s| for the conversion to the base of the exponential.  A log-sum-exp and a row loss are off by twice
+that and 4e-7, a probability by 1 +- twice that.  E goes into its product with 24 (fp32) or 8 bits (bf16, 2^-8 with room for a
+neighbour), over the classes with one rounding per 32 and plane product; results are rounded by 2^-23 or 2^-8."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+OUT = {"fp32": 2.0 ** -23, "bf16": 2.0 ** -8}
+MID = {"fp32": 2.0 ** -22, "bf16": 2.0 ** -8}
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    assert torch.cuda.is_available()
+    from paper_2311_12023_amd import lq
+    return torch, lq
+
+
+def _type(torch, name):
+    return {"fp32": torch.float32, "bf16": torch.bfloat16}[name]
+
+
+def _eps(dtype, depth):
+    return 2.0 ** -24 + (6 if dtype == "fp32" else 1) * (depth // 32 + 2) * 2.0 ** -23
+
+
+def _check_loss(torch, got, x, w, t, dtype):
+    """got: outputs of the mean loss without dW."""
+    x, w = x.double(), w.double().contiguous()
+    n, vocab = x.shape[0], w.shape[0]
+    counts = (t >= 0) & (t < vocab)
+    x = torch.where(counts[:, None], x, torch.zeros_like(x))
+    s = x @ w.t().contiguous()
+    delta = _eps(dtype, x.shape[1]) * (x.abs() @ w.abs().t().contiguous()).max(1).values + 2.0 ** -22 * s.abs().max(1).values
+    lse = torch.logsumexp(s, 1)
+    rows = torch.nonzero(counts)[:, 0]
+    row_loss = torch.zeros_like(lse)
+    row_loss[rows] = lse[rows] - s[rows, t[rows]]
+    g = torch.exp(s - lse[:, None])
+    g[rows, t[rows]] = 0
+    g[rows, t[rows]] = -g[rows].sum(1)
+    g[~counts] = 0
+    f = 1.0 / max(1, rows.numel())
+    for name, want in (("row_loss", row_loss), ("lse", lse)):
+        gap = (got[name].double() - want).abs()[counts]
+        assert torch.all(gap <= 2 * delta[counts] + 4e-7 * (1 + want[counts].abs())), (name, float(gap.max()))
+    assert torch.all(got["row_loss"][~counts] == 0)
+    total = row_loss.sum() * f
+    assert abs(got["loss"].double() - total) <= 2 * f * delta.sum() + 1e-6 * (1 + abs(total))
+    if got["dx"] is not None:
+        want, terms = g @ w * f, g.abs() @ w.abs() * f
+        bound = terms * (6 * delta[:, None] + MID[dtype] + _eps(dtype, vocab)) + OUT[dtype] * want.abs() + 1e-30
+        worst = ((got["dx"].double() - want).abs() / bound).max()
+        assert worst <= 1, float(worst)
+
+
+def _inputs(torch, n, d, vocab, dtype, seed, ignored=0.1):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(n, d, generator=gen, device="cuda")
+    w = torch.randn(vocab, d, generator=gen, device="cuda") * (2 / d ** 0.5)
+    t = torch.randint(0, vocab, (n,), generator=gen, device="cuda")
+    t[torch.rand(n, generator=gen, device="cuda") < ignored] = -100
+    return x.to(_type(torch, dtype)), w.to(_type(torch, dtype)), t
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,d,vocab", [(1, 96, 64), (5, 72, 70), (16, 1096, 900), (17, 33, 511), (50, 96, 900), (128, 520, 777)])
+def test_rows_with_strides(env, n, d, vocab, dtype):
+    """Slices of wider matrices, on and off the 16-byte addresses, bit for bit what contiguous copies give."""
+    torch, lq = env
+    x, w, t = _inputs(torch, n, d, vocab, dtype, n + d)
+    want = lq.cross_entropy(x, w, t)
+    _check_loss(torch, want, x, w, t, dtype)
+    for pad, at in ((16, 8), (5, 1), (24, 0)):
+        wide_x, wide_w = (torch.full((rows, d + pad), float("nan"), device="cuda").to(x.dtype) for rows in (n, vocab))
+        wide_x[:, at:at + d], wide_w[:, at:at + d] = x, w
+        for a, b in ((wide_x[:, at:at + d], wide_w[:, at:at + d]), (x, wide_w[:, at:at + d]), (wide_x[:, at:at + d], w)):
+            o = lq.cross_entropy(a, b, t)
+            assert all(torch.equal(o[k], want[k]) for k in o if o[k] is not None), (pad, at)
