@@ -223,10 +223,7 @@ __device__ __forceinline__ void thin_columns(const ThinSource& a, const Planes& 
   unsigned char* s_a = lds + Stage::BYTES;                                              // [plane][row][column]
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l16 = lane & 15, kg = lane >> 4;
   const int c8 = (threadIdx.x & 15) * 8, r4 = (threadIdx.x >> 4) * 4;
-  const T* x = static_cast<const T*>(a.A) + c0;
-  uint32_t xat[4];                                    // elements from a step's first row
-#pragma unroll
-  for (int q = 0; q < 4; ++q) xat[q] = (uint32_t)((r4 + q) * a.lda + c8);
+  const T* x = static_cast<const T*>(a.A) + c0 + r4 * a.lda + c8;      // rows may be any distance apart: 64-bit offsets
   Eight<T> v[2][4];
   Stage stage[2];
   const typename Stage::Place place(b);
@@ -235,7 +232,7 @@ __device__ __forceinline__ void thin_columns(const ThinSource& a, const Planes& 
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int64_t row = 64 * (int64_t)s + r4 + q;
-      load_eight<VEC, T>(x + 64 * (int64_t)s * a.lda + xat[q], row < a.m ? a.K - c0 - c8 : 0, v[u][q]);
+      load_eight<VEC, T>(x + (64 * (int64_t)s + q) * a.lda, row < a.m ? a.K - c0 - c8 : 0, v[u][q]);
     }
   };
   const auto even = std::integral_constant<int, 0>{};

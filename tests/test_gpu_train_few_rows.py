@@ -1,4 +1,4 @@
-"""The cross entropy of few rows (up to 128 without dW take kernels of their own): rows with strides.
+"""The cross entropy of few rows (up to 128 without dW take kernels of their own): rows with strides, rows that lie far apart.
 
 Tolerances (derived before any run).  fp32 operands are three bf16 planes, 24 bits, six products per 32 reduction indices, each of which
 rounds by at most 2^-23 of the terms: a logit is off by 2^-24 and that of |x||w|, one of bf16 operands (whose products are exact) by one
@@ -82,3 +82,23 @@ def test_rows_with_strides(env, n, d, vocab, dtype):
         for a, b in ((wide_x[:, at:at + d], wide_w[:, at:at + d]), (x, wide_w[:, at:at + d]), (wide_x[:, at:at + d], w)):
             o = lq.cross_entropy(a, b, t)
             assert all(torch.equal(o[k], want[k]) for k in o if o[k] is not None), (pad, at)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("gap", [68_174_088, 90_000_001])
+def test_rows_of_weights_far_apart(env, gap, dtype):
+    """A few columns of a very wide matrix: within a step of 64 classes offsets pass 2^32 elements (rows on and off 16-byte addresses).
+    What lies between is not a number."""
+    torch, lq = env
+    n, d, vocab = 5, 72, 70
+    x, w, t = _inputs(torch, n, d, vocab, dtype, gap % 97)
+    buffer = torch.empty(vocab * gap, dtype=x.dtype, device="cuda")
+    for lo in range(0, buffer.numel(), 1 << 30):
+        buffer[lo:lo + (1 << 30)] = float("nan")
+    wide = buffer.view(vocab, gap)[:, 8:8 + d]
+    wide.copy_(w)
+    for want_dw in (False, True):
+        far, near = lq.cross_entropy(x, wide, t, want_dw=want_dw), lq.cross_entropy(x, w, t, want_dw=want_dw)
+        assert all(torch.equal(far[k], near[k]) for k in near if near[k] is not None)
+        if not want_dw:
+            _check_loss(torch, far, x, w, t, dtype)
