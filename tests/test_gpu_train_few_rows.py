@@ -1,4 +1,5 @@
-"""The cross entropy of few rows (up to 128 without dW take kernels of their own): rows with strides, rows that lie far apart.
+"""The cross entropy of few rows (up to 128 without dW take kernels of their own): rows with strides, rows that lie far
+apart, rows that do not count, certain rows, workspaces, graphs.
 
 Tolerances (derived before any run).  fp32 operands are three bf16 planes, 24 bits, six products per 32 reduction indices, each of which
 rounds by at most 2^-23 of the terms: a logit is off by 2^-24 and that of |x||w|, one of bf16 operands (whose products are exact) by one
@@ -102,3 +103,100 @@ def test_rows_of_weights_far_apart(env, gap, dtype):
         assert all(torch.equal(far[k], near[k]) for k in near if near[k] is not None)
         if not want_dw:
             _check_loss(torch, far, x, w, t, dtype)
+
+
+SIZES = [(1, 64, 300), (16, 96, 1000), (17, 33, 511), (50, 72, 1500), (128, 520, 777)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,d,vocab", SIZES)
+def test_rows_that_do_not_count(env, n, d, vocab, dtype):
+    """Whatever they hold (NaN, infinities, the type's lowest value), they change nothing else and get zeros; with none left the loss is
+    zero."""
+    torch, lq = env
+    x, w, t = _inputs(torch, n, d, vocab, dtype, n, ignored=0.0)
+    t[1::3] = torch.tensor([-1, -100, vocab, 1 << 40, -(1 << 62)] * 10, device="cuda")[:t[1::3].numel()]
+    clean = lq.cross_entropy(x, w, t)
+    _check_loss(torch, clean, x, w, t, dtype)
+    dirty = x.clone()
+    dirty[1::9], dirty[4::9], dirty[7::9] = float("nan"), float("inf"), torch.finfo(x.dtype).min
+    o = lq.cross_entropy(dirty, w, t)
+    assert all(torch.equal(o[k], clean[k]) for k in ("loss", "row_loss", "dx"))
+    assert torch.all(o["dx"][1::3] == 0) and torch.all(o["row_loss"][1::3] == 0)
+    t[:] = -100
+    o = lq.cross_entropy(dirty, w, t)
+    assert float(o["loss"]) == 0 and torch.all(o["row_loss"] == 0) and torch.all(o["dx"] == 0)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,d,vocab", SIZES)
+def test_workspace_contents_and_other_outputs(env, n, d, vocab, dtype):
+    """Neither what the workspace held before nor whether dX is wanted changes a bit."""
+    torch, lq = env
+    x, w, t = _inputs(torch, n, d, vocab, dtype, n)
+    ws = lq.cross_entropy_workspace(n, d, vocab, x.dtype)
+    outs = [lq.cross_entropy(x, w, t, workspace=ws.fill_(fill)) for fill in (0, 0xff, 0x7f)]
+    assert all(torch.equal(o[k], outs[0][k]) for o in outs[1:] for k in ("loss", "row_loss", "lse", "dx"))
+    ws = lq.cross_entropy_workspace(n, d, vocab, x.dtype, want_dx=False).fill_(0xff)
+    o = lq.cross_entropy(x, w, t, want_dx=False, workspace=ws)
+    assert o["dx"] is None and all(torch.equal(o[k], outs[0][k]) for k in ("loss", "row_loss", "lse"))
+    full, only = (lq.cross_entropy(x, w, t, want_dx=dx, want_dw=True) for dx in (True, False))       # dW: the kernels of many rows
+    assert only["dx"] is None and all(torch.equal(only[k], full[k]) for k in ("loss", "row_loss", "lse", "dw"))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n", [8, 24, 128, 140])         # 140: the kernels of many rows
+def test_certain_rows(env, n, dtype):
+    """Rows that are certain of their target (1 - p down to 1e-26) and of another class: loss and gradient keep their relative accuracy.
+    The row loss is log(1 + e^-z), so its relative error is what z is off by, 2 delta, and a few units of fp32."""
+    torch, lq = env
+    d, vocab = 64, 5000
+    x, w, t = _inputs(torch, n, d, vocab, dtype, n, ignored=0.0)
+    wt = w[t].float()
+    gain = torch.tensor([10.0, 20.0, 30.0, 40.0, 60.0, -30.0, -60.0, 0.0], device="cuda")[torch.arange(n, device="cuda") % 8][:, None]
+    x = (x.float() * 0.1 + gain * wt / (wt * wt).sum(1, keepdim=True)).to(x.dtype)
+    got = lq.cross_entropy(x, w, t)
+    eps = 2.0 ** -20 if dtype == "fp32" and n > 128 else 0.0          # two fp16 planes an operand there
+    X, W = x.double(), w.double()
+    s = X @ W.t().contiguous()
+    delta = (eps + _eps(dtype, d)) * (X.abs() @ W.abs().t().contiguous()).max(1).values + 2.0 ** -22 * s.abs().max(1).values
+    rows = torch.arange(n, device="cuda")
+    others = torch.exp(s - s[rows, t][:, None])
+    others[rows, t] = 0
+    total = others.sum(1, keepdim=True)
+    want = torch.log1p(total[:, 0])
+    assert torch.all((got["row_loss"].double() - want).abs() <= want * (2 * delta + 2e-6) + 1e-37)
+    g = others / (1 + total) / n
+    terms = g @ W.abs() + g.sum(1, keepdim=True) * W[t].abs()
+    want = g @ W - g.sum(1, keepdim=True) * W[t]
+    bound = terms * (6 * delta[:, None] + max(MID[dtype], eps) + _eps(dtype, vocab)) + OUT[dtype] * want.abs() + 1e-37
+    worst = ((got["dx"].double() - want).abs() / bound).max()
+    assert worst <= 1, float(worst)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n", [3, 40])
+def test_in_a_hip_graph(env, n, dtype):
+    """Replays with new inputs, eager work between them, give the eager results."""
+    torch, lq = env
+    x, w, t = _inputs(torch, n, 128, 900, dtype, n)
+    ws = lq.cross_entropy_workspace(n, 128, 900, x.dtype)
+    step = lambda: lq.cross_entropy(x, w, t, workspace=ws)
+    step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for i in range(4):
+        x.copy_(torch.randn(n, 128, device="cuda"))
+        t.copy_(torch.randint(0, 900, (n,), device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = {k: v.clone() for k, v in outs.items() if v is not None}
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(got[k], want[k]) for k in got), i
