@@ -51,10 +51,20 @@ static int64_t piece_classes(int64_t n, int64_t vocab) {
   return up_to((vocab + pieces - 1) / pieces, SEG_T);
 }
 
-// Not where rows are long and classes few: there are too few workgroups then, each with a long way (d = 4096, 1500 classes, fp32, 16 and
-// 128 rows 123 and 159 us, by the products of many rows 89 and 100; 4000 classes 131 and 188 for 135 and 154).
-static bool few_by_size(int64_t n, int64_t d, int64_t vocab, bool want_dw) {
-  return n <= LOSS_FEW && vocab <= MOST_PITCH / 2 && d <= 2 * vocab && !want_dw;
+// Few rows by their own kernels or by the products of many rows; us of the former and the latter, without dX / with it where both are
+// given.  Where rows are long and classes few, the former have few workgroups, each with a long way.
+// fp32, 64 rows: d = 1024, 700 classes 42 / 62 and 40 / 69; d = 2048, 1500 classes 67 / 86 and 49 / 78, 4500 68 / 95 and 66 / 104; d = 4096,
+// 3000 classes 118 / 147 and 81 / 119, 6000 117 / 154 and 118 / 171; d = 8192, 6000 classes 217 / 273 and 208 / 292.
+// bf16, up to 64 rows: d = 2048, 6000 classes 29 / 46 and 32 / 58; d = 4096, 6000 classes 45 / 64 and 35 / 63, 12000 46 / 72 and 42 / 80.
+// bf16, more rows, which take the former twice as long: up to 64 tiles of classes the logits of rows of 2048 and more go in ranges
+// (tail_classes), the tiles of up to 65536 classes are one round of the chip.  128 rows: d = 2048, 6000 classes 38 / 64 and 33 / 62, 18000
+// 45 / 84 and 55 / 97, 32000 48 / 103 and 55 / 109, 40000 59 / 123 and 57 / 116, 128000 191 / 376 and 148 / 297; d = 1024, 6000 classes
+// 27 / 46 and 35 / 65; d = 512, 40000 classes 32 / 60 and 29 / 74.
+static bool few_by_size(int64_t n, int64_t d, int64_t vocab, bool half, bool want_dw) {
+  if (n > LOSS_FEW || vocab > MOST_PITCH / 2 || want_dw) return false;
+  if (half) return d * (6500 - vocab) <= 8000000;
+  if (n <= 64) return d < 2560 || vocab > 10000;
+  return vocab <= 64 * SEG_T ? d < 2048 : vocab <= 36000 || d <= 512;
 }
 
 struct LossPlan {
@@ -81,7 +91,7 @@ static LossPlan plan_loss(void* ws, int64_t n, int64_t d, int64_t vocab, int dty
   p.factors = a.take<float>(2);
   p.tops = a.take<uint32_t>(2);
   p.x_inv = a.take<float>(half ? n : 0);
-  const bool few = few_by_size(n, d, vocab, want_dw);
+  const bool few = few_by_size(n, d, vocab, half, want_dw);
   p.v64 = up_to(vocab, 64);
   const int64_t tiles = std::max(p.classes / SEG_T, few ? p.v64 / LOSS_FEW_TILE : 0);
   for (int h = 0; h < (half ? 3 : 1); ++h) {
@@ -251,7 +261,7 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
   // bf16 operands whose rows are whole pairs of steps on 16-byte addresses are read where they are
   auto in_place = [&](const void* a, int64_t ld) { return !half && d % 64 == 0 && ld % 8 == 0 && ld <= MOST_PITCH && !misaligned(a, 16); };
   const char* w0 = static_cast<const char*>(W);
-  const bool few = few_by_size(n, d, vocab, dW != nullptr);
+  const bool few = few_by_size(n, d, vocab, half, dW != nullptr);
   if (half && !few) LQ_TRY(launch_zero_words(p.tops, 2, st));
   Planes x{{static_cast<const uint16_t*>(X), nullptr, nullptr}, ldx};
   if (!few && !in_place(X, ldx)) {
