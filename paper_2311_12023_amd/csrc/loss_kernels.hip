@@ -473,24 +473,23 @@ __device__ __forceinline__ void join_target(const JoinArgs& a, int64_t row, int 
   if (t < 0 || t >= a.p.vocab) return;
   const T *x = static_cast<const T*>(a.o.X) + row * a.o.ldx, *w = static_cast<const T*>(a.o.W) + t * a.o.ldw;
   float sum[2] = {0.0f, 0.0f};
-  auto walk = [&](auto vec) __attribute__((always_inline)) {     // the same order on and off the vectors' addresses: the same bits
+  auto add = [&](const vec8& u, const vec8& v) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j & 1] = fmaf((float)u[j], (float)v[j], sum[j & 1]);
+  };
+  if (a.o.vec) {
 #pragma unroll 4
+    for (int64_t k = 8 * lane; k < a.o.d; k += 512) add(*reinterpret_cast<const vec8*>(x + k), *reinterpret_cast<const vec8*>(w + k));
+  } else {                                            // in the same order: the same bits
+#pragma unroll 1
     for (int64_t k = 8 * lane; k < a.o.d; k += 512) {
       vec8 u = {}, v = {};
-      if constexpr (decltype(vec)::value) {
-        u = *reinterpret_cast<const vec8*>(x + k);
-        v = *reinterpret_cast<const vec8*>(w + k);
-      } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (k + j < a.o.d) { u[j] = x[k + j]; v[j] = w[k + j]; }
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sum[j & 1] = fmaf((float)u[j], (float)v[j], sum[j & 1]);
+      for (int j = 0; j < 8; ++j)
+        if (k + j < a.o.d) { u[j] = x[k + j]; v[j] = w[k + j]; }
+      add(u, v);
     }
-  };
-  if (a.o.vec) walk(std::true_type{});
-  else walk(std::false_type{});
+  }
   float s = sum[0] + sum[1];
 #pragma unroll
   for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
