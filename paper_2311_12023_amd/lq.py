@@ -342,6 +342,12 @@ def matmul_few_rows_static(x: torch.Tensor, codes: torch.Tensor, scale_idx: torc
     return out
 
 
+def _type_code(dtype, name: str) -> int:
+    if dtype not in T_DTYPES:
+        raise TypeError(f"{name}: need torch.float32 or torch.bfloat16")
+    return T_DTYPES[dtype]
+
+
 def _dtype(t: torch.Tensor, name: str) -> int:
     if not (isinstance(t, torch.Tensor) and t.dtype in T_DTYPES):
         raise TypeError(f"{name}: need a tensor of torch.float32 or torch.bfloat16")
@@ -382,7 +388,7 @@ def dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, out: torch.Te
 
 def cross_entropy_workspace(n: int, d: int, vocab: int, dtype=torch.float32, want_dx: bool = True, want_dw: bool = False,
                             device="cuda") -> torch.Tensor:
-    return _workspace(_lib.lq_cross_entropy_workspace_bytes(n, d, vocab, T_DTYPES[dtype], int(want_dx), int(want_dw)), device)
+    return _workspace(_lib.lq_cross_entropy_workspace_bytes(n, d, vocab, _type_code(dtype, "dtype"), int(want_dx), int(want_dw)), device)
 
 
 def cross_entropy(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, mean: bool = True, want_dx: bool = True,
@@ -409,7 +415,7 @@ def cross_entropy(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, mean:
 
 
 def adapter_workspace(m: int, d: int, k: int, rank: int, dtype=torch.float32, backward: bool = False, device="cuda") -> torch.Tensor:
-    return _workspace(_lib.lq_adapter_workspace_bytes(m, d, k, rank, T_DTYPES[dtype], int(backward)), device)
+    return _workspace(_lib.lq_adapter_workspace_bytes(m, d, k, rank, _type_code(dtype, "dtype"), int(backward)), device)
 
 
 def adapter_forward(x: torch.Tensor, codes: torch.Tensor, scale_idx: torch.Tensor, v: torch.Tensor, cfg: Config,
