@@ -362,6 +362,14 @@ def _rows(t, dtype, name):
     return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
 
 
+def _space(ws):
+    """Aligned start and bytes of a caller's workspace: the kernels write there, so it has to be one piece of the GPU's memory."""
+    if not (isinstance(ws, torch.Tensor) and ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous()):
+        raise TypeError("workspace: need a contiguous torch.uint8 tensor on the GPU")
+    at = _aligned_ptr(ws)
+    return at, max(0, ws.numel() - (at - ws.data_ptr()))
+
+
 def _shaped(t, shape, name):
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name}: shape {tuple(t.shape)}, need {tuple(shape)}")
@@ -409,8 +417,7 @@ def cross_entropy(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, mean:
                dw=torch.empty((vocab, d), dtype=x.dtype, device=x.device) if want_dw else None)
     ptr = {name: None if t is None else t.data_ptr() for name, t in out.items()}
     _check(_lib.lq_cross_entropy(xp, ldx, wp, ldw, _dev(targets, torch.int64, "targets"), n, d, vocab, code, int(mean), ptr["loss"],
-                                 ptr["row_loss"], ptr["lse"], ptr["dx"], ptr["dw"], _aligned_ptr(ws),
-                                 ws.numel() - (_aligned_ptr(ws) - ws.data_ptr()), _stream()), "lq_cross_entropy")
+                                 ptr["row_loss"], ptr["lse"], ptr["dx"], ptr["dw"], *_space(ws), _stream()), "lq_cross_entropy")
     return out
 
 
@@ -433,8 +440,7 @@ def adapter_forward(x: torch.Tensor, codes: torch.Tensor, scale_idx: torch.Tenso
     _check(_lib.lq_adapter_forward(_dev(x, x.dtype, "x"), m, d, k, _dev(codes, torch.uint8, "codes"),
                                    _dev(scale_idx, torch.uint8, "scale_idx"), _dev(v, torch.float32, "v"), cfg,
                                    _dev(l1, torch.float32, "l1"), _dev(l2, torch.float32, "l2"), rank, code, p, seed, offset,
-                                   y.data_ptr(), t.data_ptr(), _aligned_ptr(ws),
-                                   ws.numel() - (_aligned_ptr(ws) - ws.data_ptr()), _stream()), "lq_adapter_forward")
+                                   y.data_ptr(), t.data_ptr(), *_space(ws), _stream()), "lq_adapter_forward")
     return y, t
 
 
@@ -456,8 +462,7 @@ def adapter_backward(dy: torch.Tensor, x: torch.Tensor, codes: torch.Tensor, sca
                                     _dev(scale_idx, torch.uint8, "scale_idx"), _dev(v, torch.float32, "v"), cfg,
                                     _dev(l1, torch.float32, "l1"), _dev(l2, torch.float32, "l2"), rank, code,
                                     _dev(t, torch.float32, "t"), p, seed, offset, None if dx is None else dx.data_ptr(),
-                                    dl1.data_ptr(), dl2.data_ptr(), _aligned_ptr(ws),
-                                    ws.numel() - (_aligned_ptr(ws) - ws.data_ptr()), _stream()), "lq_adapter_backward")
+                                    dl1.data_ptr(), dl2.data_ptr(), *_space(ws), _stream()), "lq_adapter_backward")
     return dx, dl1, dl2
 
 
