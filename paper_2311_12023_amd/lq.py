@@ -197,6 +197,13 @@ def _aligned_ptr(ws: torch.Tensor) -> int:
     return (p + 255) & ~255
 
 
+def _bytes_left(ws: torch.Tensor) -> int:
+    """Bytes of a workspace from its first aligned one on; none where it ends before that."""
+    if not ws.is_cuda:
+        raise TypeError("workspace: need a tensor on the GPU")
+    return max(0, ws.numel() - (_aligned_ptr(ws) - ws.data_ptr()))
+
+
 def factorize(a: torch.Tensor, rank: int, row_w=None, col_w=None, seed: int = 0, params: SvdParams | None = None,
               workspace: torch.Tensor | None = None):
     """Factorize(A, F, r): -> (L1 d x r, L2 r x k, sigma numpy float64[r])."""
@@ -208,7 +215,7 @@ def factorize(a: torch.Tensor, rank: int, row_w=None, col_w=None, seed: int = 0,
     sigma = np.zeros(max(rank, 1))
     _check(_lib.lq_factorize(_dev(a, torch.float32, "a"), d, k, rank, _dev(row_w, torch.float32, "row_w"),
                              _dev(col_w, torch.float32, "col_w"), seed, _pp(params), l1.data_ptr(), l2.data_ptr(),
-                             sigma.ctypes.data, _aligned_ptr(ws), ws.numel() - (_aligned_ptr(ws) - ws.data_ptr()),
+                             sigma.ctypes.data, _aligned_ptr(ws), _bytes_left(ws),
                              _stream()), "lq_factorize")
     return l1, l2, sigma
 
@@ -239,8 +246,7 @@ def decompose(w: torch.Tensor, rank: int, cfg: Config, iters: int, early_stop: b
                              _pp(params), out["L1"].data_ptr(), out["L2"].data_ptr(), out["codes"].data_ptr(),
                              out["scale_idx"].data_ptr(), out["v"].data_ptr(),
                              None if out["Q"] is None else out["Q"].data_ptr(), C.addressof(err), trace.ctypes.data,
-                             C.addressof(done), sigma.ctypes.data, _aligned_ptr(ws),
-                             ws.numel() - (_aligned_ptr(ws) - ws.data_ptr()), _stream()), "lq_decompose")
+                             C.addressof(done), sigma.ctypes.data, _aligned_ptr(ws), _bytes_left(ws), _stream()), "lq_decompose")
     out.update(err=err.value, trace=trace, iters_done=done.value, sigma=sigma)
     return out
 
@@ -262,8 +268,7 @@ def error_table(w: torch.Tensor, rank: int, cfgs, iters: int, early_stop: bool =
     _check(_lib.lq_error_table(_dev(w, torch.float32, "w"), d, k, rank, C.addressof(arr), len(cfgs), iters,
                                int(early_stop), _dev(row_w, torch.float32, "row_w"),
                                _dev(col_w, torch.float32, "col_w"), seed, _pp(params), e.ctypes.data, s.ctypes.data,
-                               None if tr is None else tr.ctypes.data, _aligned_ptr(ws),
-                               ws.numel() - (_aligned_ptr(ws) - ws.data_ptr()), _stream()), "lq_error_table")
+                               None if tr is None else tr.ctypes.data, _aligned_ptr(ws), _bytes_left(ws), _stream()), "lq_error_table")
     return (e, s, tr) if want_trace else (e, s)
 
 
@@ -274,7 +279,7 @@ def fisher_row_col(f: torch.Tensor):
     row_w = torch.empty(d, dtype=torch.float32, device=f.device)
     col_w = torch.empty(k, dtype=torch.float32, device=f.device)
     _check(_lib.lq_fisher_row_col(_dev(f, torch.float32, "f"), d, k, row_w.data_ptr(), col_w.data_ptr(),
-                                  _aligned_ptr(ws), ws.numel() - (_aligned_ptr(ws) - ws.data_ptr()), _stream()),
+                                  _aligned_ptr(ws), _bytes_left(ws), _stream()),
            "lq_fisher_row_col")
     return row_w, col_w
 
@@ -321,8 +326,7 @@ def matmul(x: torch.Tensor, codes: torch.Tensor, scale_idx: torch.Tensor, v: tor
     _check(_lib.lq_matmul(_dev(x, torch.float32, "x"), m, d, k, _dev(codes, torch.uint8, "codes"),
                           _dev(scale_idx, torch.uint8, "scale_idx"), _dev(v, torch.float32, "v"), cfg,
                           _dev(l1, torch.float32, "l1"), _dev(l2, torch.float32, "l2"), rank, precision,
-                          _dev(out, torch.float32, "out"), _aligned_ptr(ws),
-                          ws.numel() - (_aligned_ptr(ws) - ws.data_ptr()), _stream()), "lq_matmul")
+                          _dev(out, torch.float32, "out"), _aligned_ptr(ws), _bytes_left(ws), _stream()), "lq_matmul")
     return out
 
 
@@ -366,8 +370,7 @@ def _space(ws):
     """Aligned start and bytes of a caller's workspace: the kernels write there, so it has to be one piece of the GPU's memory."""
     if not (isinstance(ws, torch.Tensor) and ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous()):
         raise TypeError("workspace: need a contiguous torch.uint8 tensor on the GPU")
-    at = _aligned_ptr(ws)
-    return at, max(0, ws.numel() - (at - ws.data_ptr()))
+    return _aligned_ptr(ws), _bytes_left(ws)
 
 
 def _shaped(t, shape, name):

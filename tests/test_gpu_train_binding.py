@@ -35,3 +35,17 @@ def test_workspaces(env):
                 call(torch.empty(few, dtype=torch.uint8, device="cuda"))
         with pytest.raises(lq.LqError):
             call(torch.empty(100, dtype=torch.uint8, device="cuda")[3:])         # ends before its first aligned byte
+
+
+def test_workspaces_of_the_other_calls(env):
+    torch, lq = env
+    c = lq.config(4, 64, 256)
+    a = torch.randn(128, 256, device="cuda")
+    calls = [lambda ws: lq.factorize(a, 8, workspace=ws), lambda ws: lq.decompose(a, 8, c, 2, workspace=ws),
+             lambda ws: lq.error_table(a, 8, [c], 2, workspace=ws)]
+    for call in calls:
+        with pytest.raises(lq.LqError):
+            call(torch.empty(100, dtype=torch.uint8, device="cuda")[3:])
+        with pytest.raises(TypeError):
+            call(torch.empty(1 << 24, dtype=torch.uint8))
+        call(None)
