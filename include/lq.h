@@ -340,7 +340,10 @@ int lq_dropout(const void* x, int64_t n, int dtype, double p, uint64_t seed, uin
  *            are 0.  If none counts, loss is 0 for sum and mean alike.
  *   loss 1 fp32, row_loss n fp32, lse n fp32 or NULL, dX n x d or NULL, dW vocab x d or NULL (contiguous, of type dtype)
  * The vocabulary is walked in pieces; the workspace holds one piece's exponentials (up to 2^28 logits make one piece, more are cut
- * into pieces of 2^26).  dX comes out of the same pass as the loss; dW takes a second one where there are several pieces.  n up to 2^23 - 64, vocab up to 2^31 - 65536, d up to 2^20 (LQ_ERR_SHAPE).
+ * into pieces of 2^26, or of 256 classes from 2^18 rows on).  dX comes out of the same pass as the loss; dW takes a second one where
+ * there are several pieces.  n up to 2^23 - 64, vocab up to 2^31 - 65536, d up to 2^20 (LQ_ERR_SHAPE).
+ * Up to 128 rows without dW may take kernels of their own (by rows, d, vocab and dtype): asking for dW can then change the last bits of
+ * the other outputs.  Otherwise no output depends on which others are wanted.
  */
 size_t lq_cross_entropy_workspace_bytes(int64_t n, int64_t d, int64_t vocab, int dtype, int want_dx, int want_dw);
 int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, const int64_t* targets, int64_t n, int64_t d,
@@ -354,6 +357,8 @@ int lq_cross_entropy(const void* X, int64_t ldx, const void* W, int64_t ldw, con
  *     U = dY L2^T,  dX = dY Q^T + mask s .* (U L1^T),  dL1 = drop(X)^T U,  dL2 = T^T dY,
  * with drop(X) as lq_dropout computes it for X (m x d, row-major) with the same p, seed and offset (without the rounding of a
  * bf16 result), and mask s its mask and factor, worked out again and stored nowhere.  p = 0: no dropout.
+ * Both calls decode all of Q into the workspace, which few rows of a large layer do not repay: where neither T nor dropout is wanted,
+ * lq_matmul is the call (24 rows, 4096 x 11008 in 4 bits, rank 64, fp32: 31 us and 130; 1024 rows 288 and 325).
  *   X m x d, Y and dY m x k, dX m x d (NULL: not wanted, for a first layer): contiguous, of type dtype, 16-byte aligned
  *   codes_packed, scale_idx, v    Q as for lq_matmul        L1 d x rank, L2 rank x k (forward: 16-byte aligned)
  *   T        m x rank fp32, written by the forward and read by the backward call

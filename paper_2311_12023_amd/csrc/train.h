@@ -172,9 +172,9 @@ int launch_loss_dw(const Planes& g, const Planes& xt, int64_t depth, int64_t row
 
 // ---- the same for few rows (loss_few_kernels.hip) ---------------------------------------------------------
 // Up to LOSS_FEW rows the loss is bound by reading W: it is then read where it is, once for the logits and once for dX, the whole
-// vocabulary as one piece.  d = 4096, 32000 classes, bf16, 16 / 64 / 128 rows: 106 / 117 / 171 us, by the products of many rows 158 /
-// 169 / 184; d = 1024, 50265 classes, fp32: 114 / 147 / 295 for 286 / 295 / 310.  Planes of X (one for bf16, three for fp32) and E have
-// few_rows(n) rows.  Tiles are LOSS_FEW_TILE classes; E is relative to its tile's power of two.
+// vocabulary as one piece (which sizes: few_by_size in lq_api_train.cpp).  d = 4096, 32000 classes, bf16, 16 / 64 / 128 rows: 106 / 117 /
+// 171 us, by the products of many rows 158 / 169 / 184; d = 1024, 50265 classes, fp32: 114 / 147 / 295 for 286 / 295 / 310.  Planes of X
+// (one for bf16, three for fp32) and E have few_rows(n) rows.  Tiles are LOSS_FEW_TILE classes; E is relative to its tile's power of two.
 constexpr int64_t LOSS_FEW = 128, LOSS_FEW_TILE = 64;
 inline int64_t few_rows(int64_t n) { return n <= 16 ? 16 : n <= 32 ? 32 : n <= 64 ? 64 : 128; }
 int launch_few_logits(const void* W, int64_t ldw, int dtype, int64_t d, const Planes& x, const LossPiece& p, float* part_ref,
@@ -187,7 +187,7 @@ int launch_few_dx(const void* W, int64_t ldw, int dtype, int64_t d, const Planes
 // ---- adapter products (adapter_kernels.hip, thin_kernels.hip) ---------------------------------------------
 constexpr int ADAPTER_MAX_RANK = 128;
 // part[z] (m x r32) = drop(A) B over range z of the reduction: A m x K of type dtype, contiguous, K a multiple of 8, B as three
-// bf16 planes of r32 rows x up_to(K, 64).  The mask's factor is left to launch_thin_finish.
+// bf16 planes of r32 rows x up_to(K, 64).  The mask's factor is left to launch_finish.
 int thin_project_splits(int64_t m, int64_t K);
 int launch_thin_project(const void* A, int dtype, int64_t m, int64_t K, const Planes& b, int r32, const DropoutMask& d, float* part,
                         hipStream_t st);

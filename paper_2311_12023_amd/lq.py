@@ -405,7 +405,8 @@ def cross_entropy_workspace(n: int, d: int, vocab: int, dtype=torch.float32, wan
 def cross_entropy(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, mean: bool = True, want_dx: bool = True,
                   want_dw: bool = False, workspace: torch.Tensor | None = None):
     """Softmax cross entropy of the logits X W^T, which are never stored, against `targets` (rows with a target outside the
-    vocabulary do not count): -> dict(loss, row_loss, lse, dx, dw), the gradients being those of `loss`, None if not wanted."""
+    vocabulary do not count): -> dict(loss, row_loss, lse, dx, dw), the gradients being those of `loss`, None if not wanted.
+    Up to 128 rows, asking for dw may change the other outputs' last bits."""
     code = _dtype(x, "x")
     (xp, ldx), (wp, ldw) = _rows(x, x.dtype, "x"), _rows(w, x.dtype, "w")
     n, d = x.shape
@@ -431,7 +432,8 @@ def adapter_workspace(m: int, d: int, k: int, rank: int, dtype=torch.float32, ba
 def adapter_forward(x: torch.Tensor, codes: torch.Tensor, scale_idx: torch.Tensor, v: torch.Tensor, cfg: Config,
                     l1: torch.Tensor, l2: torch.Tensor, p: float = 0.0, seed: int = 0, offset: int = 0,
                     workspace: torch.Tensor | None = None):
-    """T = drop(X) L1, Y = X Q + T L2: -> (Y, T); T is what adapter_backward takes."""
+    """T = drop(X) L1, Y = X Q + T L2: -> (Y, T); T is what adapter_backward takes.  Without a need for T or dropout, few rows of a
+    large layer go faster through matmul, which decodes no copy of Q."""
     code = _dtype(x, "x")
     m, d = x.shape
     rank, k = l2.shape
