@@ -317,8 +317,8 @@ int lq_matmul_few_rows_static(const float* X, int64_t m, int64_t d, int64_t k, c
  * gradients, losses and log-sum-exps are fp32.  Sums, softmax statistics and accumulators are held in fp32 (the total loss in
  * fp64).  fp32 operands of the large products are split into two fp16 planes, after a power of two that brings an operand's
  * largest magnitude below 2^14 (22 bits; 2^-39 of that magnitude for the smallest), and take three MFMAs; those of the thin products
- * into three bf16 planes (24 bits; magnitudes above 3.389e38, bf16's largest, count as not finite there).  With bf16 activations the decoded weights are rounded to bf16.  All calls only enqueue
- * kernels on `stream`, are deterministic, and can be captured in a HIP graph after a first call on the device.
+ * into three bf16 planes (24 bits; magnitudes above 3.389e38, bf16's largest, count as not finite there).  With bf16 activations
+ * the decoded weights are rounded to bf16.  All calls only enqueue kernels on `stream`, are deterministic, and can be captured in a HIP graph after a first call on the device.
  */
 
 /*
