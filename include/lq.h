@@ -7,7 +7,7 @@
  *
  * Conventions for every entry point
  *  - Matrix and vector arguments are DEVICE pointers unless the comment says "host".  Matrices are
- *    row-major, contiguous, fp32 (the fine-tuning calls say where theirs are bf16 or have a stride).  `stream` is a
+ *    row-major, contiguous, fp32 (the fine-tuning and 8-bit calls say where theirs are of another type or have a stride).  `stream` is a
  *    hipStream_t passed as void* (NULL = default stream).
  *  - The caller owns every buffer.  The library allocates no device memory: scratch space comes in
  *    through `workspace` (device, 256-byte aligned), sized by the matching *_workspace_bytes call.
@@ -19,7 +19,7 @@
  *    anything is launched, so a call that fails validation has no effect on any buffer.
  *    Device data is not inspected: non-finite weights, or non-positive Fisher weights, give
  *    unspecified numbers (never an out-of-bounds access).
- *  - lq_nf_quantize / lq_nf_dequantize / lq_matmul and the fine-tuning calls only enqueue work on `stream`.  lq_factorize, lq_decompose
+ *  - lq_nf_quantize / lq_nf_dequantize / lq_matmul, the fine-tuning and the 8-bit calls only enqueue work on `stream`.  lq_factorize, lq_decompose
  *    and lq_error_table write host outputs and therefore synchronize `stream` before returning.
  *  - Calls that share a workspace, or that overlap on outputs, must not run concurrently.
  */
@@ -375,6 +375,129 @@ int lq_adapter_backward(const void* dY, const void* X, int64_t m, int64_t d, int
                         const uint8_t* scale_idx, const float* v, lq_config c, const float* L1, const float* L2, int rank, int dtype,
                         const float* T, double p, uint64_t seed, uint64_t offset, void* dX, float* dL1, float* dL2, void* workspace,
                         size_t workspace_bytes, void* stream);
+
+/*
+ * ---- Layers trained and run in 8 bits ----------------------------------------------------------------------------------
+ *
+ * A matrix in 8 bits is codes of the OCP e4m3 format (a sign, four exponent bits, three fraction bits; largest value 448, no inf,
+ * 0x7f NaN) with one fp32 scale per block of 128: the value is code x scale.  Blocks are 128 neighbours of a row ("rows"), or tiles of
+ * 128 x 128 ("tiles"), counted from the matrix's start; the last ones may be short.  Rows serve operands that change with every call
+ * (activations and their gradients), tiles weights, whose transpose then has the same codes and scales.
+ * Arithmetic (fixed, so that codes are reproducible bit for bit): with amax the block's largest magnitude,
+ * scale = max(fl32(amax / 448), 2^-126), code = e4m3(fl32(x fl32(1 / scale))), nearest, ties to even.  A block that holds an inf or a NaN
+ * has scale NaN, and so has every sum that it enters.
+ * Products add up a block of 128 in the matrix unit, whose sums are good to about 2^-16 of a block's largest term, and the blocks in
+ * fp32; results are bf16, since more bits would hold that error.  They are right where they are below 2^96; where a scale times another
+ * is below 2^-156 they may be 0.  All calls only enqueue kernels on `stream` and are deterministic.
+ */
+
+/*
+ * Codes and scales of X (m x d, rows ldx elements apart, of type dtype) and of its transpose, from one pass over X.
+ *   codes    m x d, ld_codes bytes from row to row, or NULL; bytes d .. up to the next multiple of 16 of each row are written too
+ *   scale    tiles == 0: of row i and block b at scale[b * m + i];  tiles == 1: of tile (i, b) at scale[i * ceil(d / 128) + b]
+ *   codes_t  d x m, ld_codes_t bytes from row to row (rounded up likewise), or NULL
+ *   scale_t  tiles == 0: X^T's own rows, of row j and block b at scale_t[b * d + j]; tiles == 1: NULL (scale serves it with its indices
+ *            exchanged)
+ * At least one of codes and codes_t.  scale is needed with codes, and with tiles; scale_t with codes_t in rows.  codes, codes_t on 16-byte
+ * addresses, ld_codes >= d and ld_codes_t >= m multiples of 16 (LQ_ERR_ARG; LQ_ERR_SHAPE if smaller).  m, d up to 2^30, ldx below 2^40.
+ */
+int lq_fp8_quantize(const void* X, int64_t m, int64_t d, int64_t ldx, int dtype, int tiles, uint8_t* codes, int64_t ld_codes, float* scale,
+                    uint8_t* codes_t, int64_t ld_codes_t, float* scale_t, void* stream);
+
+/* An operand of the products below: codes on a 16-byte address with rows `ld` bytes apart (a multiple of 16; bytes of a row past its
+ * length may hold anything), the scale of row i and block b at scale[(tiles ? i / 128 : i) * scale_row + b * scale_block]. */
+typedef struct {
+  const uint8_t* codes;
+  int64_t ld;
+  const float* scale;
+  int64_t scale_row, scale_block;
+  int32_t tiles;
+} lq_fp8_matrix;
+
+/*
+ * Y = A B^T with A m x k and B n x k in 8 bits, along k in blocks of 128.  Y m x n bf16, rows ldy elements apart.
+ *   workspace  lq_fp8_matmul_workspace_bytes(m, n, k) bytes (0: may be NULL)
+ * m, n up to 2^30, k up to 2^22, ld up to 2^22 (LQ_ERR_SHAPE).
+ */
+size_t lq_fp8_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
+int lq_fp8_matmul(const lq_fp8_matrix* A, const lq_fp8_matrix* B, int64_t m, int64_t n, int64_t k, void* Y, int64_t ldy, void* workspace,
+                  size_t workspace_bytes, void* stream);
+
+/*
+ * A layer in 8 bits, Y = X W^T, and its gradients
+ *     dX = dY W,  dW = dY^T X,
+ * with X and dY quantized in rows inside the calls: along k for Y, along n for dX, along m (both) for dW.
+ *   X m x k, dY m x n: of types x_dtype and dy_dtype, rows ldx and ldy elements apart        W n x k, Wt (W^T) k x n: in 8 bits
+ *   Y m x n, dX m x k, dW n x k: bf16, contiguous.  dX or dW may be NULL: not wanted (with dX Wt is needed, with dW X)
+ *   m up to 2^22 in the backward call, which sums over it
+ */
+size_t lq_fp8_forward_workspace_bytes(int64_t m, int64_t n, int64_t k);
+int lq_fp8_forward(const void* X, int64_t ldx, int x_dtype, const lq_fp8_matrix* W, int64_t m, int64_t n, int64_t k, void* Y, void* workspace,
+                   size_t workspace_bytes, void* stream);
+size_t lq_fp8_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int want_dx, int want_dw);
+int lq_fp8_backward(const void* dY, int64_t ldy, int dy_dtype, const void* X, int64_t ldx, int x_dtype, const lq_fp8_matrix* Wt, int64_t m,
+                    int64_t n, int64_t k, void* dX, void* dW, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * ---- The optimizer's step ---------------------------------------------------------------------------------------------
+ *
+ * Both calls take any number of tensors; their descriptions (host memory) are read before the call returns.
+ */
+
+/* One gradient: n values of type dtype. */
+typedef struct {
+  const void* g;
+  int64_t n;
+  int32_t dtype;
+} lq_gradient;
+
+/*
+ * norm[0] = 2-norm of all gradients together (squares added up in fp64 in a fixed order, rounded once to fp32), and what to multiply the
+ * gradients by so that it is at most max_norm: norm[1] = min(1, fl32(max_norm / fl32(norm[0] + 1e-6))), NaN where norm[0] is not finite.
+ * max_norm > 0, inf for none (LQ_ERR_ARG).  norm: 2 fp32.  workspace: lq_grad_norm_workspace_bytes(grads, count) bytes.
+ */
+size_t lq_grad_norm_workspace_bytes(const lq_gradient* grads, int64_t count);
+int lq_grad_norm(const lq_gradient* grads, int64_t count, double max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * One tensor of an AdamW step: n parameters p of type p_dtype and their gradient g of type g_dtype.
+ *   m, v     state_bits == 32: n fp32 each (first and second moment).  state_bits == 8: n e4m3 codes each, of the first moment and
+ *            of the square root of the second, with scales m_scale, v_scale per block of 256 (ceil(n / 256) fp32 each); zeros to begin with
+ *   copy     n bf16 values that p is also written to, rounded, or NULL; p is fp32 then
+ */
+typedef struct {
+  void* p; const void* g; void* m; void* v;
+  float* m_scale; float* v_scale;
+  void* copy;
+  int64_t n;
+  int32_t p_dtype, g_dtype;
+} lq_adamw_tensor;
+
+/* lr_device, step_device: NULL, or device memory whose value counts instead of lr or step when the kernels run (for captured graphs). */
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay;
+  int64_t step;                    /* 1 for the first step */
+  const float* lr_device; const int64_t* step_device;
+  uint64_t seed;
+} lq_adamw_params;
+
+/*
+ * AdamW (Loshchilov and Hutter, 2019) over `count` tensors at once.  Arithmetic in fp32, every operation rounded (fixed, so that results
+ * are reproducible bit for bit; factors of beta, lr and step are worked out in fp64 and rounded once):
+ *     g = fl(coef g);  m = fl(fl(beta1 m) + fl((1 - beta1) g));  v = fl(fl(beta2 v) + fl(fl((1 - beta2) g) g));
+ *     p = fl(fl(p (1 - lr weight_decay)) - fl(lr / (1 - beta1^step) fl(m / fl(fl(sqrt(v) (1 - beta2^step)^-1/2) + eps))))
+ * and p is rounded to its type.  8-bit states are read as fl(code scale), v being the square of that, and written back from the new
+ * m and r = fl(sqrt v), which p uses unrounded: scales as for lq_fp8_quantize over blocks of 256; m to the nearest code.  For r, with
+ * x = min(fl(r fl(1 / scale)), 448) between the values lo and lo + step of neighbouring codes, the upper one is taken iff
+ * fl(fl((x - lo) (x + lo)) 65536) > u step (2 lo + step): with chance (x^2 - lo^2) / ((lo + step)^2 - lo^2), so that v is right on
+ * average (to the nearest code it would stand still wherever a step changes it by less than half a code's distance); x > 0 becomes the least
+ * value at least.  u are the 16 bits that lq_dropout's generator gives for the tensor's element with the key `seed` and offset
+ * (step mod 2^32) + 2^32 (the tensor's index in the call).
+ *   coef   device, one fp32 that multiplies every gradient (lq_grad_norm's norm + 1), or NULL.  Where it is not finite, nothing is changed.
+ * Refused (LQ_ERR_ARG): beta outside [0, 1), eps < 0, values that are not finite, step < 1, count over 2^24, state_bits neither 8 nor 32,
+ * memory that is written and belongs to two tensors or is read as a gradient, coef, lr or step as well.  n of a tensor may be 0, then its pointers are not looked at.
+ */
+int lq_adamw(const lq_adamw_tensor* tensors, int64_t count, int state_bits, const lq_adamw_params* params, const float* coef, void* stream);
 
 /*
  * Per-kernel timing for benchmarks (off by default).  While enabled, every kernel launch of the library

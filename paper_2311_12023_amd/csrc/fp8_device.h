@@ -1,0 +1,33 @@
+// e4m3 codes and their scales.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "mfma_device.h"
+
+namespace lq {
+
+// Magnitudes are compared as bit patterns: NaN ranks above inf, inf above all numbers.
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// Scale of a block whose largest magnitude has the bits `top`: the largest code is 448.
+__device__ __forceinline__ float fp8_scale(uint32_t top) {
+  const float s = fmaxf(__uint_as_float(top) / 448.0f, 0x1p-126f);
+  return top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : s;
+}
+
+// Codes of two neighbours in the lower or upper half of `old`.  |a|, |b| <= 448 (1 + 2^-22), which rounds to 448: nothing saturates.
+template <bool HIGH>
+__device__ __forceinline__ uint32_t fp8_pair(float a, float b, uint32_t old) {
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, (int)old, HIGH);
+}
+__device__ __forceinline__ uint32_t fp8_four(float a, float b, float c, float d) { return fp8_pair<true>(c, d, fp8_pair<false>(a, b, 0)); }
+
+// Values of the four codes of a word.
+__device__ __forceinline__ floatx4 fp8_values(uint32_t w) {
+  const floatx2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  return floatx4{lo[0], lo[1], hi[0], hi[1]};
+}
+
+}  // namespace lq

@@ -41,7 +41,13 @@ enum Cls {
   THIN_PROJECT = 83,        // thin_project_kernel (work = bytes)
   THIN_GRAM = 84,           // thin_gram_kernel (work = bytes)
   THIN_FINISH = 85,         // sums of partial results of the training operators (work = bytes)
-  NUM_CLASSES = 86
+  FP8_QUANTIZE = 86,        // fp8_quantize_kernel (work = bytes)
+  FP8_ROWS = 87,            // fp8_rows_kernel (work = bytes)
+  FP8_PRODUCT = 88,         // fp8_product_kernel (work = flops of the product)
+  FP8_JOIN = 89,            // fp8_join_kernel (work = bytes)
+  GRAD_NORM = 90,           // grad_squares_kernel, grad_norm_kernel (work = bytes)
+  ADAMW = 91,               // adamw_kernel (work = bytes)
+  NUM_CLASSES = 92
 };
 
 bool enabled();

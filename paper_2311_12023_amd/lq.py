@@ -49,6 +49,29 @@ class SvdParams(C.Structure):
                 ("warm_power_fine", C.c_int32)]
 
 
+class Fp8Matrix(C.Structure):
+    """lq_fp8_matrix."""
+    _fields_ = [("codes", C.c_void_p), ("ld", C.c_int64), ("scale", C.c_void_p), ("scale_row", C.c_int64),
+                ("scale_block", C.c_int64), ("tiles", C.c_int32)]
+
+
+class Gradient(C.Structure):
+    """lq_gradient."""
+    _fields_ = [("g", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
+
+
+class AdamWTensor(C.Structure):
+    """lq_adamw_tensor."""
+    _fields_ = [(name, C.c_void_p) for name in ("p", "g", "m", "v", "m_scale", "v_scale", "copy")] + [
+        ("n", C.c_int64), ("p_dtype", C.c_int32), ("g_dtype", C.c_int32)]
+
+
+class AdamWParams(C.Structure):
+    """lq_adamw_params."""
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double),
+                ("step", C.c_int64), ("lr_device", C.c_void_p), ("step_device", C.c_void_p), ("seed", C.c_uint64)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2311_12023_amd.build`")
 _lib = C.CDLL(LIB_PATH)
@@ -99,6 +122,18 @@ _lib.lq_adapter_forward.argtypes = [_vp, _i64, _i64, _i64, _vp, _vp, _vp, Config
                                     C.c_uint64, _vp, _vp, _vp, _sz, _vp]
 _lib.lq_adapter_backward.argtypes = [_vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp, Config, _vp, _vp, _int, _int, _vp, C.c_double,
                                      C.c_uint64, C.c_uint64, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.lq_fp8_quantize.argtypes = [_vp, _i64, _i64, _i64, _int, _int, _vp, _i64, _vp, _vp, _i64, _vp, _vp]
+for _name, _args in (("matmul", [_i64] * 3), ("forward", [_i64] * 3), ("backward", [_i64] * 3 + [_int] * 2)):
+    getattr(_lib, f"lq_fp8_{_name}_workspace_bytes").restype = _sz
+    getattr(_lib, f"lq_fp8_{_name}_workspace_bytes").argtypes = _args
+_MP = C.POINTER(Fp8Matrix)
+_lib.lq_fp8_matmul.argtypes = [_MP, _MP, _i64, _i64, _i64, _vp, _i64, _vp, _sz, _vp]
+_lib.lq_fp8_forward.argtypes = [_vp, _i64, _int, _MP, _i64, _i64, _i64, _vp, _vp, _sz, _vp]
+_lib.lq_fp8_backward.argtypes = [_vp, _i64, _int, _vp, _i64, _int, _MP, _i64, _i64, _i64, _vp, _vp, _vp, _sz, _vp]
+_lib.lq_grad_norm_workspace_bytes.restype = _sz
+_lib.lq_grad_norm_workspace_bytes.argtypes = [_vp, _i64]
+_lib.lq_grad_norm.argtypes = [_vp, _i64, C.c_double, _vp, _vp, _sz, _vp]
+_lib.lq_adamw.argtypes = [_vp, _i64, _int, C.POINTER(AdamWParams), _vp, _vp]
 
 _lib.lq_profile_enable.argtypes = [_int]
 _lib.lq_profile_class_name.restype = C.c_char_p
@@ -469,6 +504,216 @@ def adapter_backward(dy: torch.Tensor, x: torch.Tensor, codes: torch.Tensor, sca
                                     _dev(t, torch.float32, "t"), p, seed, offset, None if dx is None else dx.data_ptr(),
                                     dl1.data_ptr(), dl2.data_ptr(), *_space(ws), _stream()), "lq_adapter_backward")
     return dx, dl1, dl2
+
+
+FP8 = torch.float8_e4m3fn
+
+
+def _blocks(n: int) -> int:
+    return -(-n // 128)
+
+
+def _codes_like(rows: int, cols: int, device) -> torch.Tensor:
+    """rows x cols codes whose rows begin on 16-byte addresses."""
+    return torch.empty((rows, -(-cols // 16) * 16), dtype=FP8, device=device)[:, :cols]
+
+
+def fp8_quantize(x: torch.Tensor, tiles: bool = False, both: bool = False):
+    """Codes (torch.float8_e4m3fn) and fp32 scales of a matrix in blocks of 128 along its rows (scale: rows x blocks), or in tiles of
+    128 x 128 (scale: blocks x blocks): -> (codes, scale), or with both=True those of its transpose as well, from the same pass:
+    (codes, scale, codes_t, scale_t)."""
+    code = _dtype(x, "x")
+    xp, ldx = _rows(x, x.dtype, "x")
+    m, d = x.shape
+    _here(x)
+    q = _codes_like(m, d, x.device)
+    scale = torch.empty((_blocks(m), _blocks(d)) if tiles else (_blocks(d), m), dtype=torch.float32, device=x.device)
+    qt = _codes_like(d, m, x.device) if both else None
+    scale_t = torch.empty((_blocks(m), d), dtype=torch.float32, device=x.device) if both and not tiles else None
+    _check(_lib.lq_fp8_quantize(xp, m, d, ldx, code, int(tiles), q.data_ptr(), -(-d // 16) * 16, scale.data_ptr(),
+                                qt.data_ptr() if both else None, -(-m // 16) * 16 if both else 0,
+                                None if scale_t is None else scale_t.data_ptr(), _stream()), "lq_fp8_quantize")
+    out = (q, scale) if tiles else (q, scale.t())
+    return out + ((qt, scale.t() if tiles else scale_t.t()) if both else ())
+
+
+def _here(*tensors):
+    """The calls launch on the current device's stream: operands elsewhere are refused."""
+    for t in tensors:
+        if t is not None and t.get_device() != torch._C._cuda_getDevice():
+            raise ValueError(f"tensor on {t.device}, the current device is cuda:{torch._C._cuda_getDevice()}")
+
+
+def _fp8_matrix(codes, scale, name):
+    """lq_fp8_matrix of codes and scales; the scales' shape says whether they are of rows or of tiles."""
+    if not (isinstance(codes, torch.Tensor) and codes.is_cuda and codes.dtype == FP8 and codes.dim() == 2):
+        raise TypeError(f"{name}: need a {FP8} matrix on the GPU")
+    if not (isinstance(scale, torch.Tensor) and scale.is_cuda and scale.dtype == torch.float32 and scale.dim() == 2):
+        raise TypeError(f"{name}: need a torch.float32 matrix of scales on the GPU")
+    _here(codes, scale)
+    rows, cols = codes.shape
+    ld = codes.stride(0) if rows > 1 else -(-cols // 16) * 16
+    if (codes.stride(1) != 1 and cols > 1) or ld % 16 or ld < cols or codes.data_ptr() % 16:
+        raise ValueError(f"{name}: rows have to begin on 16-byte addresses and be contiguous (as fp8_quantize lays them out)")
+    if tuple(scale.shape) not in ((rows, _blocks(cols)), (_blocks(rows), _blocks(cols))):
+        raise ValueError(f"{name}: scales of shape {tuple(scale.shape)} for {rows} x {cols} codes")
+    return Fp8Matrix(codes.data_ptr(), ld, scale.data_ptr(), scale.stride(0), scale.stride(1), int(scale.shape[0] != rows))
+
+
+def fp8_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor, out: torch.Tensor | None = None,
+               workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Y = A B^T (bf16) of two matrices in 8 bits, A m x k and B n x k, each with scales of rows or of tiles (fp8_quantize)."""
+    am, bm = _fp8_matrix(a, a_scale, "a"), _fp8_matrix(b, b_scale, "b")
+    (m, k), n = a.shape, b.shape[0]
+    _shaped(b, (n, k), "b")
+    if out is None:
+        out = torch.empty((m, n), dtype=torch.bfloat16, device=a.device)
+    _shaped(out, (m, n), "out")
+    yp, ldy = _rows(out, torch.bfloat16, "out")
+    ws = workspace if workspace is not None else _workspace(_lib.lq_fp8_matmul_workspace_bytes(m, n, k), a.device)
+    _check(_lib.lq_fp8_matmul(C.byref(am), C.byref(bm), m, n, k, yp, ldy, *_space(ws), _stream()), "lq_fp8_matmul")
+    return out
+
+
+def fp8_workspace(m: int, n: int, k: int, backward: bool = False, want_dx: bool = True, want_dw: bool = True, device="cuda") -> torch.Tensor:
+    """Workspace of fp8_forward, or of fp8_backward, for m rows through a layer of k inputs and n outputs."""
+    return _workspace(_lib.lq_fp8_backward_workspace_bytes(m, n, k, int(want_dx), int(want_dw)) if backward else
+                      _lib.lq_fp8_forward_workspace_bytes(m, n, k), device)
+
+
+def fp8_forward(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Y = X W^T (bf16) with X (m x k, fp32 or bf16) quantized along its rows inside the call and W (n x k) in 8 bits."""
+    code = _dtype(x, "x")
+    xp, ldx = _rows(x, x.dtype, "x")
+    wm = _fp8_matrix(w, w_scale, "w")
+    _here(x)
+    (m, k), n = x.shape, w.shape[0]
+    _shaped(w, (n, k), "w")
+    ws = workspace if workspace is not None else fp8_workspace(m, n, k, device=x.device)
+    y = torch.empty((m, n), dtype=torch.bfloat16, device=x.device)
+    _check(_lib.lq_fp8_forward(xp, ldx, code, C.byref(wm), m, n, k, y.data_ptr(), *_space(ws), _stream()), "lq_fp8_forward")
+    return y
+
+
+def fp8_backward(dy: torch.Tensor, x: torch.Tensor | None, wt: torch.Tensor | None = None, wt_scale: torch.Tensor | None = None,
+                 want_dx: bool = True, want_dw: bool = True, workspace: torch.Tensor | None = None):
+    """Gradients of fp8_forward, bf16: -> (dX = dY W or None, dW = dY^T X or None).  wt, wt_scale: W^T (k x n) in 8 bits, as
+    fp8_quantize(w, tiles=True, both=True) gives it, for dX; x for dW."""
+    code = _dtype(dy, "dy")
+    yp, ldy = _rows(dy, dy.dtype, "dy")
+    m, n = dy.shape
+    _here(dy, x if want_dw else None, workspace)
+    if not (want_dx or want_dw):
+        raise ValueError("fp8_backward: neither gradient is wanted")
+    if (want_dx and wt is None) or (want_dw and x is None):
+        raise ValueError("fp8_backward: dX needs wt, dW needs x")
+    xp, ldx, xcode, wm = None, 0, 0, None
+    if want_dx:
+        wm = _fp8_matrix(wt, wt_scale, "wt")
+        k = wt.shape[0]
+        _shaped(wt, (k, n), "wt")
+    if want_dw:
+        xcode = _dtype(x, "x")
+        xp, ldx = _rows(x, x.dtype, "x")
+        k = wt.shape[0] if want_dx else x.shape[1]
+        _shaped(x, (m, k), "x")
+    ws = workspace if workspace is not None else fp8_workspace(m, n, k, True, want_dx, want_dw, dy.device)
+    dx = torch.empty((m, k), dtype=torch.bfloat16, device=dy.device) if want_dx else None
+    dw = torch.empty((n, k), dtype=torch.bfloat16, device=dy.device) if want_dw else None
+    _check(_lib.lq_fp8_backward(yp, ldy, code, xp, ldx, xcode, None if wm is None else C.byref(wm), m, n, k,
+                                None if dx is None else dx.data_ptr(), None if dw is None else dw.data_ptr(), *_space(ws), _stream()),
+           "lq_fp8_backward")
+    return dx, dw
+
+
+def grad_norm(grads, max_norm: float = float("inf"), workspace: torch.Tensor | None = None):
+    """2-norm of all gradients together and the factor that brings it to max_norm at most (NaN where the norm is not finite, which makes
+    AdamW.step change nothing): -> (norm, coef), fp32 of no dimensions on the GPU.  `workspace`: as grad_norm_workspace(grads)."""
+    table = (Gradient * max(len(grads), 1))()
+    for entry, g in zip(table, grads):
+        entry.dtype = _dtype(g, "grads")
+        entry.g, entry.n = _dev(g, g.dtype, "grads"), g.numel()
+    _here(*grads)
+    device = grads[0].device if grads else "cuda"
+    ws = workspace if workspace is not None else _workspace(_lib.lq_grad_norm_workspace_bytes(C.addressof(table), len(grads)), device)
+    out = torch.empty(2, dtype=torch.float32, device=device)
+    _check(_lib.lq_grad_norm(C.addressof(table), len(grads), max_norm, out.data_ptr(), *_space(ws), _stream()), "lq_grad_norm")
+    return out[0], out[1]
+
+
+class AdamW:
+    """AdamW over many tensors in one call, with states in 32 bits or in 8 (lq_adamw).
+
+    params: contiguous GPU tensors of fp32 or bf16, updated in place.  copies: bf16 tensors (or None) that take each fp32 parameter's
+    rounded value in the same pass.  States start at zero and lie in `buffers` ("m", "v", with bits=8 also "m_scale", "v_scale"), tensor
+    after tensor, each from a multiple of 256 on.  `t` counts the steps taken: an int, or with device_step=True an int64 tensor on the
+    GPU, so that a captured step counts on when it is replayed.  seed: of the rounding of 8-bit states."""
+
+    def __init__(self, params, bits: int = 32, copies=None, seed: int = 0, device_step: bool = False):
+        if bits not in (8, 32):
+            raise ValueError("bits: need 8 or 32")
+        self.params, self.bits, self.seed = list(params), bits, seed
+        if not self.params:
+            raise ValueError("params: none given")
+        self.copies = list(copies) if copies is not None else [None] * len(self.params)
+        if len(self.copies) != len(self.params):
+            raise ValueError("copies: need one for each parameter")
+        device = self.params[0].device
+        starts, total = [], 0
+        for p in self.params:
+            starts.append(total)
+            total += -(-p.numel() // 256) * 256
+        state = FP8 if bits == 8 else torch.float32
+        self._table = (AdamWTensor * len(self.params))()
+        for p, c in zip(self.params, self.copies):
+            _dtype(p, "params"), _dev(p, p.dtype, "params")
+            if p.device != device:
+                raise ValueError("params: on different devices")
+            if c is not None:
+                _dev(c, torch.bfloat16, "copies")
+                _shaped(c, p.shape, "copies")
+        self.buffers = {name: torch.zeros(total, dtype=state, device=device) for name in ("m", "v")}
+        if bits == 8:
+            self.buffers.update({name: torch.zeros(total // 256, dtype=torch.float32, device=device) for name in ("m_scale", "v_scale")})
+        for entry, p, c, at in zip(self._table, self.params, self.copies, starts):
+            entry.p, entry.n, entry.p_dtype = p.data_ptr(), p.numel(), T_DTYPES[p.dtype]
+            entry.copy = None if c is None else c.data_ptr()
+            for name, buffer in self.buffers.items():
+                setattr(entry, name, buffer.data_ptr() + (4 * (at // 256) if name.endswith("scale") else at * buffer.element_size()))
+        self.t = torch.zeros((), dtype=torch.int64, device=device) if device_step else 0
+
+    def step(self, grads, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, coef: torch.Tensor | None = None) -> None:
+        """One step.  grads: one for each parameter, fp32 or bf16, of its size.  lr: a number, or an fp32 tensor of one element on the GPU.
+        coef: such a tensor that multiplies every gradient (grad_norm's); where it is not finite, nothing but `t` changes."""
+        if len(grads) != len(self.params):
+            raise ValueError("grads: need one for each parameter")
+        _here(*self.params[:1])
+        for entry, p, c, g in zip(self._table, self.params, self.copies, grads):
+            entry.p = _dev(p, p.dtype, "params")             # where they are now
+            entry.copy = None if c is None else c.data_ptr()
+            entry.g_dtype = _dtype(g, "grads")
+            entry.g = _dev(g, g.dtype, "grads")
+            if g.numel() != entry.n or p.numel() != entry.n or g.device != p.device:
+                raise ValueError(f"grads: {g.numel()} values on {g.device} for {entry.n} parameters on {p.device}")
+        on_device = isinstance(self.t, torch.Tensor)
+        if not on_device and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("a captured step needs device_step=True: a replay would repeat this step's number")
+        h = AdamWParams(beta1=betas[0], beta2=betas[1], eps=eps, weight_decay=weight_decay, seed=self.seed)
+        if isinstance(lr, torch.Tensor):
+            _shaped(lr.reshape(-1), (1,), "lr")
+            h.lr_device = _dev(lr, torch.float32, "lr")
+        else:
+            h.lr = lr
+        if coef is not None:
+            _shaped(coef.reshape(-1), (1,), "coef")
+        if on_device:
+            self.t += 1
+            h.step_device = self.t.data_ptr()
+        else:
+            h.step = self.t + 1
+        _check(_lib.lq_adamw(C.addressof(self._table), len(grads), self.bits, C.byref(h), _dev(coef, torch.float32, "coef"), _stream()), "lq_adamw")
+        if not on_device:
+            self.t += 1
 
 
 def assign_configs(err: np.ndarray, storage: np.ndarray, budget_bits: float, node_limit: int = 0):

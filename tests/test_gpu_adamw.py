@@ -1,0 +1,266 @@
+"""AdamW over many tensors and the gradients' norm: bit for bit in the arithmetic that the header fixes."""
+import math
+
+import pytest
+import torch
+
+import fp8_reference as R
+from paper_2311_12023_amd import lq
+
+pytestmark = pytest.mark.gpu
+
+HYPER = dict(lr=2e-3, betas=(0.9, 0.99), eps=1e-7, weight_decay=0.05)
+
+
+def _values(n, seed, size=1.0, dtype=torch.float32):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(n, generator=g) * torch.exp(torch.randn(n, generator=g)) * size).to(dtype)
+
+
+def _check(opt, params, grads, old, index, step, coef=None):
+    """One tensor after a step against its values before it; -> nothing."""
+    p, m, v = old
+    lr, betas, eps, decay = HYPER["lr"], HYPER["betas"], HYPER["eps"], HYPER["weight_decay"]
+    wp, wm, wv, wr = R.adamw(p, grads.cpu(), m, v, step, lr, betas, eps, decay, coef)
+    assert torch.equal(params.cpu(), wp.to(params.dtype))
+    got = _state(opt, index)
+    if opt.bits == 32:
+        assert torch.equal(got[0].double().cpu(), wm) and torch.equal(got[1].double().cpu(), wv)
+        return
+    mq, ms, rq, rs = R.state_codes(wm, wr, step, index, opt.seed)
+    for have, want in zip(got, (mq, rq, ms, rs)):
+        assert torch.equal(have.double().cpu(), want)
+
+
+def _state(opt, index):
+    at = sum(-(-p.numel() // 256) * 256 for p in opt.params[:index])
+    n = opt.params[index].numel()
+    m, v = (opt.buffers[k][at:at + n] for k in ("m", "v"))
+    if opt.bits == 32:
+        return m, v
+    blocks = slice(at // 256, at // 256 + -(-n // 256))
+    return m, v, opt.buffers["m_scale"][blocks], opt.buffers["v_scale"][blocks]
+
+
+def _moments(opt, index):
+    """The moments that a step reads, fp64."""
+    got, n = _state(opt, index), opt.params[index].numel()
+    if opt.bits == 32:
+        return [x.double().cpu() for x in got]
+    return R.state_values(got[0], got[2], n), R.f32(R.state_values(got[1], got[3], n).square())
+
+
+SIZES = [1, 2, 255, 256, 257, 1000, 8192, 8193, 20000, 3]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("p_type,g_type,copies", [(torch.float32, torch.float32, False), (torch.float32, torch.bfloat16, True),
+                                                  (torch.bfloat16, torch.float32, False), (torch.bfloat16, torch.bfloat16, False)])
+def test_steps_bit_for_bit(bits, p_type, g_type, copies):
+    params = [_values(n, i, 0.1, p_type).cuda() for i, n in enumerate(SIZES)]
+    held = [torch.zeros_like(p, dtype=torch.bfloat16) for p in params] if copies else None
+    opt = lq.AdamW(params, bits=bits, copies=held, seed=(7 << 40) + 11)
+    for step in (1, 2, 3):
+        grads = [_values(n, 100 * step + i, 10.0 ** -i, g_type).cuda() for i, n in enumerate(SIZES)]
+        old = [(p.double().cpu(), *_moments(opt, i)) for i, p in enumerate(params)]
+        coef = torch.tensor(0.37 if step == 3 else 1.0, device="cuda") if step > 1 else None
+        opt.step(grads, coef=coef, **HYPER)
+        assert opt.t == step
+        for i, p in enumerate(params):
+            _check(opt, p, grads[i], old[i], i, step, None if coef is None else float(coef))
+            if copies:
+                assert torch.equal(held[i], p.bfloat16())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_odd_addresses_and_mixed_types(bits):
+    """Views that begin on any element, of both types in one call."""
+    flat, half = _values(5000, 1).cuda(), _values(5000, 2, 1.0, torch.bfloat16).cuda()
+    grads = [_values(5000, 3).cuda()[3:1003], _values(5000, 4, 1.0, torch.bfloat16).cuda()[1:700], _values(300, 5).cuda()[1:]]
+    params = [flat[1:1001], half[5:704], flat[2001:2300]]
+    rest = flat.clone(), half.clone()
+    opt = lq.AdamW(params, bits=bits)
+    old = [(p.double().cpu(), *_moments(opt, i)) for i, p in enumerate(params)]
+    opt.step(grads, **HYPER)
+    for i, p in enumerate(params):
+        _check(opt, p, grads[i], old[i], i, 1)
+    for now, then, used in ((flat, rest[0], [(1, 1001), (2001, 2300)]), (half, rest[1], [(5, 704)])):
+        untouched = torch.ones(5000, dtype=torch.bool)
+        for a, b in used:
+            untouched[a:b] = False
+        assert torch.equal(now.cpu()[untouched], then.cpu()[untouched])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_many_tensors(bits):
+    """More than go into one launch, with empty ones among them."""
+    sizes = [(37 * i) % 700 for i in range(150)]
+    params = [_values(n, i).cuda() for i, n in enumerate(sizes)]
+    opt = lq.AdamW(params, bits=bits)
+    grads = [_values(n, 500 + i).cuda() for i, n in enumerate(sizes)]
+    old = [(p.double().cpu(), *_moments(opt, i)) for i, p in enumerate(params)]
+    opt.step(grads, **HYPER)
+    for i, p in enumerate(params):
+        if sizes[i]:
+            _check(opt, p, grads[i], old[i], i, 1)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_coefficient_that_is_not_finite_changes_nothing(bits, bad):
+    params = [_values(n, n).cuda() for n in (700, 64)]
+    copies = [p.bfloat16() for p in params]
+    opt = lq.AdamW(params, bits=bits, copies=copies)
+    grads = [_values(n, n + 1).cuda() for n in (700, 64)]
+    opt.step(grads, **HYPER)
+    before = [x.clone() for x in (*params, *copies, *opt.buffers.values())]
+    opt.step(grads, coef=torch.tensor(bad, device="cuda"), **HYPER)
+    for a, b in zip(before, (*params, *copies, *opt.buffers.values())):
+        assert torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+    assert opt.t == 2
+
+
+def test_states_of_zero_and_of_very_different_size():
+    """Blocks of zeros; v whose small elements are below the least code stay above 0."""
+    p, g = torch.ones(1024).cuda(), torch.zeros(1024)
+    g[256:512] = torch.logspace(-12, 3, 256)
+    g[600] = 1e-30
+    opt = lq.AdamW([p], bits=8, seed=3)
+    old = (p.double().cpu(), *_moments(opt, 0))
+    opt.step([g.cuda()], **HYPER)
+    _check(opt, p, g, old, 0, 1)
+    assert (opt.buffers["v"].float()[256:512] > 0).all() and opt.buffers["v"].float()[0] == 0
+
+
+def test_second_moment_is_right_on_average():
+    """After one step every element holds the same v, between two codes: the mean of what is held is v.  n elements rounded apart by
+    chance: the mean is off by a few gap / 2 / sqrt(n)."""
+    n = 256 * 4096
+    g = torch.full((n,), 0.73)
+    g[::256] = 1.0                                             # the blocks' largest: the scale
+    p = torch.zeros(n).cuda()
+    opt = lq.AdamW([p], bits=8, seed=5)
+    opt.step([g.cuda()], **HYPER)
+    held = _moments(opt, 0)[1][1::256]
+    v = 0.01 * 0.73 ** 2
+    lo, hi = held.min().item(), held.max().item()
+    assert lo < v < hi and len(held.unique()) == 2
+    assert abs(held.mean().item() - v) <= 5 * (hi - lo) / 2 / math.sqrt(held.numel()) + 1e-6 * v
+
+
+@pytest.mark.parametrize("bits,tolerance", [(32, 1e-5), (8, 0.2)])
+def test_follows_a_64_bit_run(bits, tolerance):
+    """100 steps against AdamW in 64 bits.  32 bits: roundings of 2^-24 a step on p of order 1 with steps of 1e-2, 100 x 2^-24 and what
+    the moments' relative 2^-23 x 10 changes of the way walked.  8 bits: p's way is off by the rounding of r, 2^-3 of a code at most a
+    step and unbiased, of m, 2^-4: a fifth of the way is far outside what both do over 100 steps."""
+    n = 2000
+    p = _values(n, 1).cuda()
+    start = p.double().cpu()
+    q, m, v = start.clone(), torch.zeros(n).double(), torch.zeros(n).double()
+    opt = lq.AdamW([p], bits=bits, seed=9)
+    for t in range(1, 101):
+        g = (_values(n, 1000 + t) + 0.5 * start.float()).cuda()
+        opt.step([g], lr=1e-2, betas=(0.9, 0.99), eps=1e-8, weight_decay=0.0)
+        gd = g.double().cpu()
+        m, v = 0.9 * m + 0.1 * gd, 0.99 * v + 0.01 * gd * gd
+        q -= 1e-2 * m / (1 - 0.9 ** t) / ((v / (1 - 0.99 ** t)).sqrt() + 1e-8)
+    way = (q - start).norm()
+    assert (p.double().cpu() - q).norm() <= tolerance * way
+
+
+@pytest.mark.parametrize("types", [(torch.float32,), (torch.bfloat16, torch.float32)])
+@pytest.mark.parametrize("sizes", [[1], [3, 0, 17], [16384, 16385, 5], [100] * 300, [1 << 20]])
+def test_norm(types, sizes):
+    grads = [_values(n + 1, i, 10.0 ** (i % 5), types[i % len(types)]).cuda()[i % 2:][:n] for i, n in enumerate(sizes)]
+    want = math.sqrt(sum(g.double().square().sum().item() for g in grads))
+    norm, coef = lq.grad_norm(grads, max_norm=2.0)
+    # fp64 sums and one rounding to fp32
+    assert abs(norm.item() - want) <= 2.0 ** -24 * (1 + 1e-6) * want
+    most = R.f32(torch.tensor(2.0 / float(R.f32(norm.double().cpu() + float(torch.tensor(1e-6))))))
+    assert coef.item() == min(1.0, float(most))
+    again = lq.grad_norm(grads, max_norm=2.0)
+    assert torch.equal(again[0], norm) and torch.equal(again[1], coef)
+    assert lq.grad_norm(grads)[1].item() == 1.0
+
+
+def test_norm_of_extremes():
+    big = torch.full((1000,), 3e38, device="cuda")
+    norm, coef = lq.grad_norm([big[:1]], 1.0)                 # 9e76 is no fp32 number
+    assert norm.item() == big[0].item() and coef.item() > 0
+    assert math.isinf(lq.grad_norm([big], 1.0)[0].item()) and math.isnan(lq.grad_norm([big], 1.0)[1].item())
+    tiny = torch.full((4,), 1e-30, device="cuda")
+    assert abs(lq.grad_norm([tiny], 1.0)[0].item() - 2e-30) < 1e-36
+    for bad in (float("nan"), float("inf")):
+        g = torch.ones(70000, device="cuda")
+        g[69999] = bad
+        norm, coef = lq.grad_norm([g, big[:1]], 1.0)
+        assert not math.isfinite(norm.item()) and math.isnan(coef.item())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_captured_steps(bits):
+    """A graph of norm and step replayed, with the rate on the device, against eager steps."""
+    sizes = (5000, 64)
+    params, again = ([_values(n, n).cuda() for n in sizes] for _ in range(2))
+    grads = [torch.zeros(n, device="cuda") for n in sizes]
+    lr = torch.tensor(1e-2, device="cuda")
+    opts = [lq.AdamW(p, bits=bits, seed=4, device_step=True) for p in (params, again)]
+    ws = torch.empty(4096, dtype=torch.uint8, device="cuda")
+
+    def step(opt):
+        norm, coef = lq.grad_norm(grads, 1.0, workspace=ws)
+        opt.step(grads, lr, coef=coef)
+        return norm
+
+    def draw(seed):
+        for i, g in enumerate(grads):
+            g.copy_(_values(g.numel(), seed + i))
+
+    draw(0)
+    for opt in opts:
+        step(opt)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step(opts[0])
+    for t in range(2, 6):
+        draw(10 * t)
+        lr.fill_(1e-2 / t)
+        graph.replay()
+        torch.cuda.synchronize()
+        norm = step(opts[1])
+        assert torch.equal(norm, captured)
+        for a, b in zip((*params, *opts[0].buffers.values()), (*again, *opts[1].buffers.values())):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+        assert opts[0].t.item() == opts[1].t.item() == t
+    host = lq.AdamW(params)
+    host.step(grads, 1e-3)
+    with pytest.raises(RuntimeError):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            host.step(grads, 1e-3)
+
+
+def test_number_on_the_device_is_the_number_on_the_host():
+    outs = []
+    for device_step in (False, True):
+        p = [_values(3000, 1).cuda()]
+        opt = lq.AdamW(p, bits=8, seed=2, device_step=device_step)
+        for t in range(3):
+            opt.step([_values(3000, 5 + t).cuda()], torch.tensor(0.01, device="cuda") if device_step else 0.01 + 0 * t)
+        outs.append(p[0])
+    # lr is fl(0.01) there and 0.01 here: 2^-24 of three steps of 0.01, and a rounding of p each
+    assert (outs[0] - outs[1]).abs().max() <= 3 * (2.0 ** -23 * 0.011 + 2.0 ** -23 * outs[0].abs().max())
+
+
+def test_large_tensor():
+    """Elements past 2^31 of one tensor."""
+    n = (1 << 31) + 3000
+    p = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    tail = _values(3000, 1, 1.0, torch.bfloat16)
+    g[-3000:] = tail.cuda()
+    opt = lq.AdamW([p], bits=8, seed=1)
+    opt.step([g], **HYPER)
+    wp, wm, wv, wr = R.adamw(torch.zeros(3000), tail, torch.zeros(3000).double(), torch.zeros(3000).double(), 1, HYPER["lr"],
+                             HYPER["betas"], HYPER["eps"], HYPER["weight_decay"])
+    assert torch.equal(p[-3000:].cpu(), wp.bfloat16()) and not p[:-3000].any()
+    assert torch.equal(lq.grad_norm([g])[0].cpu(), tail.double().square().sum().sqrt().float())

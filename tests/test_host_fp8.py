@@ -1,0 +1,170 @@
+"""What the 8-bit layers and the optimizer's step refuse, and the sizes of their workspaces.  Needs no GPU: nothing gets past the
+checks."""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+from paper_2311_12023_amd import lq
+
+L = lq._lib
+P = 4096                                     # never dereferenced: the calls end before a launch
+BIG = 1 << 60
+NAN, INF = float("nan"), float("inf")
+
+
+def _quantize(X=P, m=10, d=100, ldx=100, dtype=0, tiles=0, codes=P, ld=112, scale=P, codes_t=P, ld_t=16, scale_t=P):
+    return L.lq_fp8_quantize(X, m, d, ldx, dtype, tiles, codes, ld, scale, codes_t, ld_t, scale_t, None)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(X=None), -1), (dict(codes=None, codes_t=None), -1), (dict(scale=None), -1), (dict(scale_t=None), -1),
+    (dict(tiles=1, codes=None, scale=None), -1), (dict(m=0), -2), (dict(d=0), -2), (dict(m=-1), -2), (dict(m=1 << 31), -2), (dict(ldx=99), -2),
+    (dict(ld=96), -2), (dict(m=17), -2), (dict(ld=104), -8), (dict(ld_t=24), -8), (dict(codes=P + 8), -8), (dict(codes_t=P + 1), -8),
+    (dict(dtype=2), -8), (dict(tiles=2), -8), (dict(X=P + 2), -8), (dict(X=P + 1, dtype=1), -8), (dict(scale=P + 2), -8),
+    (dict(scale_t=P + 1), -8), (dict(m=1 << 30, ld_t=1 << 30, d=1 << 30, ldx=1 << 30, ld=1 << 30), -2)])
+def test_quantize_refusals(change, status):
+    assert _quantize(**change) == status
+
+
+def _matrix(codes=P, ld=128, scale=P, scale_row=1, scale_block=1, tiles=0):
+    return C.byref(lq.Fp8Matrix(codes, ld, scale, scale_row, scale_block, tiles))
+
+
+BAD_MATRICES = [(dict(codes=None), -1), (dict(scale=None), -1), (dict(ld=96), -2), (dict(ld=1 << 23), -2), (dict(scale_row=-1), -2),
+                (dict(scale_block=-1), -2), (dict(scale_row=1 << 41), -2), (dict(ld=120), -8), (dict(codes=P + 8), -8), (dict(scale=P + 2), -8),
+                (dict(tiles=2), -8), (dict(tiles=-1), -8)]
+
+
+def _matmul(A=None, B=None, m=10, n=20, k=100, Y=P, ldy=20, ws=P, size=BIG):
+    return L.lq_fp8_matmul(A or _matrix(), B or _matrix(), m, n, k, Y, ldy, ws, size, None)
+
+
+@pytest.mark.parametrize("change,status", [(dict(Y=None), -1), (dict(m=0), -2), (dict(n=0), -2), (dict(k=0), -2), (dict(k=1 << 23), -2),
+                                           (dict(m=1 << 31), -2), (dict(ldy=19), -2), (dict(Y=P + 1), -8)])
+def test_matmul_refusals(change, status):
+    assert _matmul(**change) == status
+
+
+@pytest.mark.parametrize("change,status", BAD_MATRICES)
+def test_operand_refusals(change, status):
+    assert _matmul(A=_matrix(**change)) == status and _matmul(B=_matrix(**change)) == status
+    assert _forward(W=_matrix(**change)) == status and _backward(Wt=_matrix(**change)) == status
+
+
+def test_operands_that_are_missing():
+    assert L.lq_fp8_matmul(None, _matrix(), 1, 1, 1, P, 1, P, BIG, None) == -1
+    assert L.lq_fp8_forward(P, 8, 0, None, 1, 1, 8, P, P, BIG, None) == -1
+    assert L.lq_fp8_backward(P, 8, 0, P, 8, 0, None, 1, 8, 8, P, P, P, BIG, None) == -1
+
+
+def _forward(X=P, ldx=100, x_dtype=0, W=None, m=10, n=20, k=100, Y=P, ws=P, size=BIG):
+    return L.lq_fp8_forward(X, ldx, x_dtype, W or _matrix(), m, n, k, Y, ws, size, None)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(X=None), -1), (dict(Y=None), -1), (dict(m=0), -2), (dict(n=-3), -2), (dict(k=0), -2), (dict(ldx=99), -2), (dict(x_dtype=2), -8),
+    (dict(X=P + 2), -8), (dict(Y=P + 1), -8), (dict(ws=None), -6), (dict(ws=P + 16), -6), (dict(size=100), -6)])
+def test_forward_refusals(change, status):
+    assert _forward(**change) == status
+
+
+def _backward(dY=P, ldy=100, dy_dtype=0, X=P, ldx=60, x_dtype=0, Wt=None, m=10, n=100, k=60, dX=P, dW=P, ws=P, size=BIG):
+    return L.lq_fp8_backward(dY, ldy, dy_dtype, X, ldx, x_dtype, Wt or _matrix(), m, n, k, dX, dW, ws, size, None)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dY=None), -1), (dict(dX=None, dW=None), -1), (dict(X=None), -1), (dict(m=0), -2), (dict(m=1 << 23), -2), (dict(n=1 << 23, ldy=1 << 23), -2),
+    (dict(ldy=99), -2), (dict(ldx=59), -2), (dict(dy_dtype=2), -8), (dict(x_dtype=3), -8), (dict(dY=P + 2), -8), (dict(X=P + 2), -8),
+    (dict(dX=P + 1), -8), (dict(dW=P + 1), -8), (dict(ws=None), -6), (dict(ws=P + 16), -6), (dict(size=100), -6)])
+def test_backward_refusals(change, status):
+    assert _backward(**change) == status
+
+
+def test_workspace_sizes():
+    assert L.lq_fp8_forward_workspace_bytes(0, 8, 8) == 0 and L.lq_fp8_backward_workspace_bytes(8, 0, 8, 1, 1) == 0
+    assert L.lq_fp8_matmul_workspace_bytes(8, 8, 1 << 23) == 0
+    for m, n, k in ((1, 1, 1), (37, 768, 100), (1000, 64, 128), (4096, 128, 4096)):
+        need = L.lq_fp8_forward_workspace_bytes(m, n, k)
+        assert need >= m * k and _forward(m=m, n=n, k=k, ldx=k, W=_matrix(ld=4096), size=need - 1) == -6
+        need = [L.lq_fp8_backward_workspace_bytes(m, n, k, a, b) for a, b in ((1, 0), (0, 1), (1, 1))]
+        assert need[0] >= m * n and need[1] >= m * (n + k) and need[2] >= max(need[:2])
+        assert _backward(m=m, n=n, k=k, ldy=n, ldx=k, Wt=_matrix(ld=4096), size=need[2] - 1) == -6
+        need = L.lq_fp8_matmul_workspace_bytes(m, n, k)
+        assert not need or _matmul(m=m, n=n, k=k, ldy=n, A=_matrix(ld=4096), B=_matrix(ld=4096), size=need - 1) == -6
+
+
+def _norm(grads=((P, 100, 0),), count=None, most=1.0, norm=P, ws=P, size=BIG):
+    table = (lq.Gradient * max(1, len(grads)))(*grads)
+    return L.lq_grad_norm(C.addressof(table), len(grads) if count is None else count, most, norm, ws, size, None)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(norm=None), -1), (dict(grads=((None, 5, 0),)), -1), (dict(count=0), -8), (dict(count=1 << 25), -8), (dict(grads=((P, -1, 0),)), -2),
+    (dict(grads=((P, 1 << 41, 0),)), -2), (dict(grads=((P, 4, 2),)), -8), (dict(grads=((P, 4, 0), (P + 2, 4, 0))), -8),
+    (dict(grads=((P + 1, 4, 1),)), -8), (dict(most=0.0), -8), (dict(most=-1.0), -8), (dict(most=NAN), -8), (dict(norm=P + 2), -8),
+    (dict(ws=None), -6), (dict(ws=P + 8), -6), (dict(size=0), -6), (dict(size=8, grads=((P, 1 << 22, 0),)), -6)])
+def test_norm_refusals(change, status):
+    assert _norm(**change) == status
+
+
+def _tensor(p=1 << 20, g=2 << 20, m=3 << 20, v=4 << 20, m_scale=5 << 20, v_scale=6 << 20, copy=None, n=1000, p_dtype=0, g_dtype=0):
+    return lq.AdamWTensor(p, g, m, v, m_scale, v_scale, copy, n, p_dtype, g_dtype)
+
+
+def _step(*tensors, bits=32, coef=None, count=None, **params):
+    table = (lq.AdamWTensor * max(1, len(tensors)))(*tensors)
+    h = lq.AdamWParams(**{**dict(lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, weight_decay=0.0, step=1), **params})
+    return L.lq_adamw(C.addressof(table), len(tensors) if count is None else count, bits, C.byref(h), coef, None)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(p=None), -1), (dict(g=None), -1), (dict(m=None), -1), (dict(v=None), -1), (dict(n=-1), -2), (dict(n=1 << 41), -2),
+    (dict(p_dtype=2), -8), (dict(g_dtype=-1), -8), (dict(p=(1 << 20) + 2), -8), (dict(g=1 + (2 << 20), g_dtype=1), -8), (dict(m=2 + (3 << 20)), -8),
+    (dict(v=2 + (4 << 20)), -8), (dict(copy=1 + (7 << 20)), -8), (dict(copy=7 << 20, p_dtype=1), -8),
+    (dict(m=1 << 20), -8), (dict(v=(3 << 20) + 3996), -8), (dict(copy=(1 << 20) + 3998), -8)])
+def test_step_refuses_tensors(change, status):
+    assert _step(_tensor(**change)) == status
+    assert _step(_tensor(p=11 << 20, m=13 << 20, v=14 << 20), _tensor(**change)) == status
+
+
+@pytest.mark.parametrize("change", [dict(m_scale=None), dict(v_scale=None)])
+def test_step_refuses_states_without_scales(change):
+    assert _step(_tensor(**change), bits=8) == -1
+
+
+@pytest.mark.parametrize("change", [dict(m_scale=(5 << 20) + 2), dict(v_scale=(5 << 20) + 12), dict(m=(1 << 20) + 3999), dict(v_scale=(3 << 20) + 996)])
+def test_step_refuses_pieces_of_8_bit_states(change):
+    assert _step(_tensor(**change), bits=8) == -8
+
+
+@pytest.mark.parametrize("change", [
+    dict(bits=16), dict(bits=0), dict(count=0), dict(count=(1 << 24) + 1), dict(lr=NAN), dict(lr=INF), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0),
+    dict(beta2=NAN), dict(eps=-1e-9), dict(eps=NAN), dict(eps=INF), dict(weight_decay=NAN), dict(step=0), dict(step=-4), dict(coef=P + 2),
+    dict(lr_device=P + 2), dict(step_device=P + 4)])
+def test_step_refuses_parameters(change):
+    assert _step(_tensor(), **change) == -8
+
+
+def test_step_refuses_the_same_tensor_twice():
+    assert _step(_tensor(), _tensor()) == -8
+    other = dict(p=11 << 20, m=13 << 20, v=14 << 20)
+    assert _step(_tensor(), _tensor(**other, copy=(1 << 20) + 500)) == -8      # a copy inside another's parameters
+    assert _step(_tensor(), _tensor(**other, g=(3 << 20) + 8)) == -8           # a gradient inside another's moments
+    assert _step(_tensor(), coef=(1 << 20) + 400) == -8 and _step(_tensor(), step_device=(4 << 20) + 8) == -8
+    assert L.lq_adamw(None, 1, 32, C.byref(lq.AdamWParams()), None, None) == -1 and L.lq_adamw(P, 1, 32, None, None, None) == -1
+
+
+def test_binding_checks_tensors():
+    x, q, s = torch.zeros(4, 64), torch.zeros(4, 64).to(lq.FP8), torch.zeros(4, 1)
+    for call in (lambda: lq.fp8_quantize(x), lambda: lq.fp8_quantize(x.half()), lambda: lq.fp8_matmul(q, s, q, s),
+                 lambda: lq.fp8_forward(x, q, s), lambda: lq.fp8_backward(x, x, q, s), lambda: lq.grad_norm([x]),
+                 lambda: lq.grad_norm([x.double()]), lambda: lq.AdamW([x]), lambda: lq.AdamW([x.long()])):
+        with pytest.raises(TypeError):
+            call()
+    with pytest.raises(ValueError):
+        lq.AdamW([x], bits=4)
+    with pytest.raises(ValueError):
+        lq.AdamW([])
+    assert math.isinf(lq.grad_norm.__defaults__[0])
