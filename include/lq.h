@@ -405,7 +405,8 @@ int lq_fp8_quantize(const void* X, int64_t m, int64_t d, int64_t ldx, int dtype,
                     uint8_t* codes_t, int64_t ld_codes_t, float* scale_t, void* stream);
 
 /* An operand of the products below: codes on a 16-byte address with rows `ld` bytes apart (a multiple of 16; bytes of a row past its
- * length may hold anything), the scale of row i and block b at scale[(tiles ? i / 128 : i) * scale_row + b * scale_block]. */
+ * length may hold anything), the scale of row i and block b at scale[(tiles ? i / 128 : i) * scale_row + b * scale_block],
+ * scale_row up to 2^21. */
 typedef struct {
   const uint8_t* codes;
   int64_t ld;

@@ -32,6 +32,9 @@ struct Fp8Product {
   void* out; int64_t ld;
 };
 int launch_fp8_product(const Fp8Product& p, float* part, size_t part_floats, hipStream_t st);
+// For many columns (fp8_product_kernels.hip).
+int launch_fp8_tiles(const Fp8Product& p, float* part, size_t part_floats, hipStream_t st);
+size_t fp8_tiles_part_floats(int64_t rows, int64_t columns, int64_t k);
 size_t fp8_product_part_floats(int64_t rows, int64_t columns, int64_t k);
 
 // ---- optimizer (adamw_kernels.hip) -------------------------------------------------------------------------

@@ -8,6 +8,11 @@
 
 namespace lq {
 
+typedef int intx8 __attribute__((ext_vector_type(8)));
+
+// Accumulators of products hold 2^30 times the result, so that the product of two small scales stays a normal number.
+constexpr float FP8_LIFT = 0x1p30f, FP8_DROP = 0x1p-30f;
+
 // Magnitudes are compared as bit patterns: NaN ranks above inf, inf above all numbers.
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 

@@ -1,0 +1,281 @@
+// The product of matrices in 8 bits for many rows: 256 x 256 tiles on the matrix unit.
+#include "dense_device.h"
+#include "fp8.h"
+#include "fp8_device.h"
+#include "lds_transfer.h"
+#include "profiler.h"
+#include "segment_gemm.h"
+
+namespace lq {
+
+constexpr int PT = 256, P_THREADS = 512;
+constexpr uint32_t P_SIDE = PT * 128, P_STAGE = 2 * P_SIDE;         // bytes of an operand's block, of both
+constexpr uint32_t P_SCALES = 2 * P_STAGE;                          // behind the stages: scales of the rows and columns of each
+constexpr size_t P_LDS = P_SCALES + 2 * (2 * PT * 4);
+
+struct ProductArgs {
+  Fp8Operand rows, columns;
+  int64_t k;
+  void* out; int64_t ld;
+  float* part;
+  int tiles_r, tiles_c, splits, blocks;
+  bool vec;                                                         // whole 16-byte stores
+};
+struct ProductTile { int tr, tc; };
+__device__ __forceinline__ ProductTile product_tile(const ProductArgs& a, int u) {
+  const int band = u / (4 * a.tiles_c), high = min(a.tiles_r - 4 * band, 4), inside = u - band * 4 * a.tiles_c;
+  return {4 * band + inside % high, inside / high};
+}
+
+// Two blocks of 16 rows of one column (elements 4 kg .. + 3 of each in this lane) to the output.
+__device__ __forceinline__ void product_store(const ProductArgs& a, floatx4 u, floatx4 v, int64_t row, int64_t column, int kg) {
+  const bf16x4 lo = {(__bf16)(u[0] * FP8_DROP), (__bf16)(u[1] * FP8_DROP), (__bf16)(u[2] * FP8_DROP), (__bf16)(u[3] * FP8_DROP)};
+  const bf16x4 hi = {(__bf16)(v[0] * FP8_DROP), (__bf16)(v[1] * FP8_DROP), (__bf16)(v[2] * FP8_DROP), (__bf16)(v[3] * FP8_DROP)};
+  __bf16* out = static_cast<__bf16*>(a.out) + column * a.ld;
+  const uintx4 w = seg_pair_blocks(__builtin_bit_cast(uintx2, lo), __builtin_bit_cast(uintx2, hi));
+  const int64_t first = row + 16 * (kg & 1) + 8 * (kg >> 1);
+  if (column >= a.columns.count) return;
+  if (a.vec && first + 8 <= a.rows.count) {
+    *reinterpret_cast<uintx4*>(out + first) = w;
+  } else {
+    const bf16x8 each = __builtin_bit_cast(bf16x8, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (first + e < a.rows.count) out[first + e] = each[e];
+  }
+}
+
+// A workgroup of eight wavefronts makes a tile, a wavefront 128 x 64 of it (2 x 4) in blocks of 16 x 16.  A block of 128 along k is one
+// matrix instruction, whose four sums a lane are multiplied by the two scales into the accumulators; what it takes is two vector
+// instructions for four sums where the rows' scales are of tiles (one scale for the wavefront's 128 rows), else three.
+//
+// LDS holds two blocks of both operands.  Rows are 128 bytes, unit u of 16 bytes of row r stored at u ^ (r % 8): a read of 16 rows
+// x 4 units touches every bank alike.  Blocks of 16 rows are taken two at a time; before the last two of a block of 128, all its operands are
+// in registers, so one barrier there tells that the next block has landed and that this one's place is free, and the next block's
+// first operands are read under the last products.
+template <bool ROW_TILES>
+__global__ __launch_bounds__(P_THREADS) void fp8_product_kernel(ProductArgs a) {
+  extern __shared__ __align__(16) unsigned char lds[];
+  const int item = seg_piece(a.tiles_r * a.tiles_c * a.splits);
+  if (item < 0) return;
+  const int u = item / a.splits, split = item - u * a.splits;
+  const ProductTile t = product_tile(a, u);
+  const int b0 = (int)((int64_t)a.blocks * split / a.splits), b1 = (int)((int64_t)a.blocks * (split + 1) / a.splits);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int wm = wave >> 2, wn = wave & 3, l16 = lane & 15, kg = lane >> 4;
+  const int64_t row0 = (int64_t)t.tr * PT, column0 = (int64_t)t.tc * PT;
+
+  // transfers: rows 32 wave + 8 q + lane / 8 of either operand, unit lane % 8 ^ (row % 8); rows past the end are the last one again
+  const int unit = (lane & 7) ^ (lane >> 3);
+  uint32_t va[4], vb[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int r = 32 * wave + 8 * q + (lane >> 3);
+    const int64_t la = a.rows.count - 1 - row0, lb = a.columns.count - 1 - column0;
+    va[q] = (uint32_t)((r < la ? r : la) * a.rows.ld + 16 * unit);
+    vb[q] = (uint32_t)((r < lb ? r : lb) * a.columns.ld + 16 * unit);
+  }
+  // units past the row's end read its last one
+  const int rest = (int)(a.k - (int64_t)(a.blocks - 1) * 128);      // bytes of the last block, 1 .. 128
+  const int past = 16 * unit - ((rest - 1) & ~15);
+  const uint32_t back = past > 0 ? (uint32_t)past : 0u;
+  const uint8_t* pa = a.rows.codes + row0 * a.rows.ld;
+  const uint8_t* pb = a.columns.codes + column0 * a.columns.ld;
+  // scales: wavefronts 0 .. 3 those of 64 rows each, 4 .. 7 of the columns
+  const Fp8Operand& so = wave < 4 ? a.rows : a.columns;
+  const int64_t s0 = wave < 4 ? row0 : column0, sr = min(s0 + 64 * (wave & 3) + lane, so.count - 1);
+  const float* ps = so.scale + (s0 >> so.shift) * so.scale_row;
+  const uint32_t vs = (uint32_t)(((sr >> so.shift) - (s0 >> so.shift)) * so.scale_row * 4);
+  const int64_t sblock = so.scale_block;
+  auto transfer = [&](int n, int b, uint32_t stage) __attribute__((always_inline)) {      // piece n of 9 of block b
+    const uint32_t less = b == a.blocks - 1 ? back : 0u;
+    const uint32_t to = stage * P_STAGE + (uint32_t)wave * 4096u;
+    if (n < 4) transfer_to_lds(reinterpret_cast<const uint16_t*>(pa + (int64_t)b * 128), va[n & 3] - less, to + 1024u * n);
+    else if (n < 8) transfer_to_lds(reinterpret_cast<const uint16_t*>(pb + (int64_t)b * 128), vb[n & 3] - less, to + P_SIDE + 1024u * (n - 4));
+    else transfer_word_to_lds(ps + b * sblock, vs, P_SCALES + stage * (2 * PT * 4) + 256u * wave);
+  };
+  // The last block's bytes past k become 0: everyone in what they brought themselves.
+  auto clear_past = [&](uint32_t stage) __attribute__((always_inline)) {
+    // one word after the other: all operands are in registers meanwhile, none are left for more
+    unsigned char* at = lds + stage * P_STAGE + wave * 4096 + 16 * lane;
+#pragma unroll 1
+    for (int n = 0; n < 32; ++n) {
+      const int bytes = rest - 16 * unit - 4 * (n & 3);
+      uint32_t* w = reinterpret_cast<uint32_t*>(at + (n >> 4) * P_SIDE + ((n >> 2) & 3) * 1024 + 4 * (n & 3));
+      if (bytes <= 0) *w = 0;
+      else if (bytes < 4) *w &= (1u << (8 * bytes)) - 1u;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  };
+
+  // operands: row 16 i + l16 (of the wavefront's), units kg and 4 + kg of the block
+  const uint32_t sw = (uint32_t)(l16 & 7), u0 = ((uint32_t)kg ^ sw) * 16u, u1 = ((uint32_t)(4 + kg) ^ sw) * 16u;
+  uint32_t xa = (uint32_t)(128 * wm + l16) * 128u + u0, xb = xa - u0 + u1;
+  uint32_t ya = P_SIDE + (uint32_t)(64 * wn + l16) * 128u + u0, yb = ya - u0 + u1;
+  uint32_t sa = P_SCALES + 4u * (128 * wm + (ROW_TILES ? 0 : 4 * kg)), sb = P_SCALES + 4u * (PT + 64 * wn + l16);
+  auto operand = [&](uint32_t first, uint32_t second) __attribute__((always_inline)) -> intx8 {
+    const uintx4 x = *reinterpret_cast<const uintx4*>(lds + first), y = *reinterpret_cast<const uintx4*>(lds + second);
+    return intx8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+  };
+  float acc[8][4][4];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
+  auto sums = [&](int i, int j) __attribute__((always_inline)) { return floatx4{acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]}; };
+  intx8 x[4], y[4];
+  floatx4 p[2][2], r[4];
+  float s[4], last;                                  // last: the fourth scale of the block before, for its last sums
+  auto read_x = [&](int i) __attribute__((always_inline)) {
+    x[i & 3] = operand(xa + 2048u * i, xb + 2048u * i);
+    if constexpr (!ROW_TILES) r[i & 3] = *reinterpret_cast<const floatx4*>(lds + sa + 64 * i);
+  };
+  auto read_y = [&](int j) __attribute__((always_inline)) { y[j] = operand(ya + 2048u * j, yb + 2048u * j); };
+  auto read_scales = [&]() __attribute__((always_inline)) {
+    const float f = ROW_TILES ? *reinterpret_cast<const float*>(lds + sa) * FP8_LIFT : FP8_LIFT;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s[j] = *reinterpret_cast<const float*>(lds + sb + 64 * j) * f;
+  };
+  auto turn = [&]() __attribute__((always_inline)) {
+    xa ^= P_STAGE; xb ^= P_STAGE; ya ^= P_STAGE; yb ^= P_STAGE;
+    sa ^= 2 * PT * 4; sb ^= 2 * PT * 4;
+  };
+  auto add = [&](int ii, int j, float f) __attribute__((always_inline)) {     // sums of blocks 2 ii, 2 ii + 1 and column block j
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int i = 2 * ii + h;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(ROW_TILES ? p[j & 1][h][e] : p[j & 1][h][e] * r[i & 3][e], f, acc[i][j][e]);
+      // kept here: moved behind a later branch they would leave all of p alive
+      asm volatile("" : "+v"(acc[i][j][0]), "+v"(acc[i][j][1]), "+v"(acc[i][j][2]), "+v"(acc[i][j][3]));
+    }
+  };
+#pragma unroll
+  for (int n = 0; n < 9; ++n) transfer(n, b0, 0);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  if (b0 == a.blocks - 1 && rest < 128) clear_past(0);
+  asm volatile("s_barrier" ::: "memory");
+#pragma unroll
+  for (int n = 0; n < 9; ++n) transfer(n, min(b0 + 1, b1 - 1), 1);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) read_y(j);
+  read_x(0);
+  read_x(1);
+  read_scales();
+  last = 0.0f;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) p[1][h] = r[2 + h] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  uint32_t stage = 0;
+  // Past the last block the last one comes again, into a place whose contents nobody uses any more.
+  for (int b = b0; b < b1; ++b) {
+    const int next = min(b + 2, b1 - 1);
+#pragma unroll
+    for (int ii = 0; ii < 4; ++ii) {
+      if (ii == 3) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        if (rest < 128 && b + 2 >= a.blocks) clear_past(stage ^ 1);
+        asm volatile("s_barrier" ::: "memory");
+        turn();
+        last = s[3];
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          p[j & 1][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x[(2 * ii + h) & 3], y[j], floatx4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (j) add(ii, j - 1, s[j - 1]);
+        else if (ii) add(ii - 1, 3, s[3]);
+        else add(3, 3, last);                        // of the block before
+        __builtin_amdgcn_sched_barrier(0);
+        if (ii < 3) {
+          if (j < 2) read_x(2 * ii + 2 + j);
+        } else {
+          read_y(j);
+          if (j < 2) read_x(j);
+          transfer(2 * j, next, stage);
+          transfer(2 * j + 1, next, stage);
+          if (j == 3) {
+            transfer(8, next, stage);
+            read_scales();
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    stage ^= 1;
+  }
+  add(3, 3, last);
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+
+  const int64_t row = row0 + 128 * wm, column = column0 + 64 * wn + l16;
+  if (a.splits > 1) {
+    floatx4* part = reinterpret_cast<floatx4*>(a.part) + (size_t)item * (PT * PT / 4) + tid;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) part[(i * 4 + j) * P_THREADS] = sums(i, j);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; i += 2)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) product_store(a, sums(i, j), sums(i + 1, j), row + 16 * i, column + 16 * j, kg);
+}
+
+// Sum of a tile's ranges in order; a workgroup takes two blocks of 16 rows of every wavefront's part.
+__global__ __launch_bounds__(P_THREADS) void fp8_join_kernel(ProductArgs a) {
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, wm = wave >> 2, wn = wave & 3, l16 = lane & 15, kg = lane >> 4;
+  const int u = blockIdx.x, i = 2 * blockIdx.y;
+  const ProductTile t = product_tile(a, u);
+  const floatx4* part = reinterpret_cast<const floatx4*>(a.part) + (size_t)u * a.splits * (PT * PT / 4) + tid;
+  const int64_t row = (int64_t)t.tr * PT + 128 * wm + 16 * i, column = (int64_t)t.tc * PT + 64 * wn + l16;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    floatx4 v[2] = {};
+    for (int s = 0; s < a.splits; ++s)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) v[h] += part[(size_t)s * (PT * PT / 4) + ((i + h) * 4 + j) * P_THREADS];
+    product_store(a, v[0], v[1], row, column + 16 * j, kg);
+  }
+}
+
+static int64_t product_tiles(int64_t rows, int64_t columns) { return ((rows + PT - 1) / PT) * ((columns + PT - 1) / PT); }
+// Ranges that the sum is cut into where there are few tiles: they fill the chip, each keeps four blocks.
+static int product_splits(int64_t rows, int64_t columns, int64_t k) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(256 / std::max<int64_t>(1, product_tiles(rows, columns)), fp8_blocks(k) / 4));
+}
+size_t fp8_tiles_part_floats(int64_t rows, int64_t columns, int64_t k) {
+  const int s = product_splits(rows, columns, k);
+  return s > 1 ? (size_t)s * product_tiles(rows, columns) * PT * PT : 0;
+}
+
+template <bool ROW_TILES>
+static int launch(const ProductArgs& a, hipStream_t st) {
+  static LdsLimit limit;
+  LQ_TRY(limit.raise(reinterpret_cast<const void*>(fp8_product_kernel<ROW_TILES>), P_LDS));
+  const unsigned wgs = (unsigned)(((int64_t)a.tiles_r * a.tiles_c * a.splits + 7) / 8 * 8);
+  hipLaunchKernelGGL(fp8_product_kernel<ROW_TILES>, dim3(wgs), dim3(P_THREADS), P_LDS, st, a);
+  LQ_HIP_TRY(hipGetLastError());
+  return LQ_OK;
+}
+
+int launch_fp8_tiles(const Fp8Product& p, float* part, size_t part_floats, hipStream_t st) {
+  if (product_tiles(p.rows.count, p.columns.count) >= ((int64_t)1 << 28)) return LQ_ERR_SHAPE;
+  ProductArgs a{p.rows, p.columns, p.k, p.out, p.ld, part, (int)((p.rows.count + PT - 1) / PT), (int)((p.columns.count + PT - 1) / PT),
+                product_splits(p.rows.count, p.columns.count, p.k), (int)fp8_blocks(p.k), p.ld % 8 == 0 && ((uintptr_t)p.out & 15) == 0};
+  if (part_floats < fp8_tiles_part_floats(p.rows.count, p.columns.count, p.k)) return LQ_ERR_WORKSPACE;
+  {
+    prof::Scope ps(prof::FP8_PRODUCT, st, 2.0 * p.rows.count * p.columns.count * p.k);
+    LQ_TRY(p.rows.shift ? launch<true>(a, st) : launch<false>(a, st));
+  }
+  if (a.splits == 1) return LQ_OK;
+  prof::Scope ps(prof::FP8_JOIN, st, (double)fp8_tiles_part_floats(p.rows.count, p.columns.count, p.k) * 4);
+  hipLaunchKernelGGL(fp8_join_kernel, dim3((unsigned)(a.tiles_r * a.tiles_c), 4), dim3(P_THREADS), 0, st, a);
+  LQ_HIP_TRY(hipGetLastError());
+  return LQ_OK;
+}
+
+}  // namespace lq

@@ -5,11 +5,6 @@
 
 namespace lq {
 
-typedef int intx8 __attribute__((ext_vector_type(8)));
-
-// Accumulators hold 2^LIFT times the result, so that the product of two small scales stays a normal number.
-constexpr float FP8_LIFT = 0x1p30f, FP8_DROP = 0x1p-30f;
-
 // 32 bytes of a row from byte `at` on, zero past its length k; what lies past the last 16 bytes that hold a value is not read.
 __device__ __forceinline__ intx8 fp8_load(const uint8_t* row, int64_t at, int64_t k) {
   uintx4 half[2];
@@ -77,9 +72,13 @@ __global__ __launch_bounds__(256) void fp8_rows_kernel(Fp8Product p) {
   }
 }
 
-size_t fp8_product_part_floats(int64_t rows, int64_t columns, int64_t k) { return 0; }
+constexpr int64_t FEW_COLUMNS = 128;
+size_t fp8_product_part_floats(int64_t rows, int64_t columns, int64_t k) {
+  return columns > FEW_COLUMNS ? fp8_tiles_part_floats(rows, columns, k) : 0;
+}
 
 int launch_fp8_product(const Fp8Product& p, float* part, size_t part_floats, hipStream_t st) {
+  if (p.columns.count > FEW_COLUMNS) return launch_fp8_tiles(p, part, part_floats, st);
   const int64_t row_tiles = (p.rows.count + 15) / 16;
   const int nc = p.columns.count > 16 ? 4 : 1;
   const int64_t waves = row_tiles * ((p.columns.count + 16 * nc - 1) / (16 * nc));

@@ -12,4 +12,9 @@ __device__ __forceinline__ void transfer_to_lds(const uint16_t* base, uint32_t v
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(base) : "memory", "m0");
 }
 
+// The same for 4 bytes a lane: to LDS address lds + 4 * lane.
+__device__ __forceinline__ void transfer_word_to_lds(const float* base, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(voff), "s"(base) : "memory", "m0");
+}
+
 }  // namespace lq

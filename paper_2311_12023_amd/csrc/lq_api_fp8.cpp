@@ -10,12 +10,11 @@ constexpr int64_t MOST_ROWS = (int64_t)1 << 30, MOST_DEPTH = (int64_t)1 << 22, M
 static bool bad_rows(int64_t n) { return n <= 0 || n > MOST_ROWS; }
 static bool bad_depth(int64_t n) { return n <= 0 || n > MOST_DEPTH; }
 
-static int check_matrix(const lq_fp8_matrix* w, int64_t rows, int64_t k) {
+static int check_matrix(const lq_fp8_matrix* w, int64_t k) {
   if (!w || !w->codes || !w->scale) return LQ_ERR_NULL;
-  if (w->ld < k || w->ld > MOST_DEPTH || w->scale_row < 0 || w->scale_block < 0 || w->scale_row > MOST_LD || w->scale_block > MOST_LD)
+  if (w->ld < k || w->ld > MOST_DEPTH || w->scale_row < 0 || w->scale_block < 0 || w->scale_row > MOST_DEPTH / 2 || w->scale_block > MOST_LD)
     return LQ_ERR_SHAPE;
   if (misaligned(w->codes, 16) || w->ld % 16 || misaligned(w->scale, 4) || (w->tiles != 0 && w->tiles != 1)) return LQ_ERR_ARG;
-  (void)rows;
   return LQ_OK;
 }
 static Fp8Operand operand(const lq_fp8_matrix& w, int64_t rows) {
@@ -95,8 +94,8 @@ int lq_fp8_matmul(const lq_fp8_matrix* A, const lq_fp8_matrix* B, int64_t m, int
                   size_t workspace_bytes, void* stream) {
   if (!Y) return LQ_ERR_NULL;
   if (bad_rows(m) || bad_rows(n) || bad_depth(k) || ldy < n || ldy > MOST_LD) return LQ_ERR_SHAPE;
-  LQ_TRY(check_matrix(A, m, k));
-  LQ_TRY(check_matrix(B, n, k));
+  LQ_TRY(check_matrix(A, k));
+  LQ_TRY(check_matrix(B, k));
   if (misaligned(Y, 2)) return LQ_ERR_ARG;
   const size_t floats = fp8_product_part_floats(n, m, k);
   if (no_space(workspace, workspace_bytes, floats * 4)) return LQ_ERR_WORKSPACE;
@@ -112,7 +111,7 @@ int lq_fp8_forward(const void* X, int64_t ldx, int x_dtype, const lq_fp8_matrix*
                    size_t workspace_bytes, void* stream) {
   if (!X || !Y) return LQ_ERR_NULL;
   if (bad_rows(m) || bad_rows(n) || bad_depth(k) || ldx < k || ldx > MOST_LD) return LQ_ERR_SHAPE;
-  LQ_TRY(check_matrix(W, n, k));
+  LQ_TRY(check_matrix(W, k));
   if (bad_type(x_dtype) || misaligned(X, type_bytes(x_dtype)) || misaligned(Y, 2)) return LQ_ERR_ARG;
   const ForwardPlan p = plan_forward(workspace, m, n, k);
   if (no_space(workspace, workspace_bytes, p.bytes)) return LQ_ERR_WORKSPACE;
@@ -135,7 +134,7 @@ int lq_fp8_backward(const void* dY, int64_t ldy, int dy_dtype, const void* X, in
     if (ldx < k || ldx > MOST_LD) return LQ_ERR_SHAPE;
     if (bad_type(x_dtype) || misaligned(X, type_bytes(x_dtype))) return LQ_ERR_ARG;
   }
-  if (dX) LQ_TRY(check_matrix(Wt, k, n));
+  if (dX) LQ_TRY(check_matrix(Wt, n));
   const BackwardPlan p = plan_backward(workspace, m, n, k, dX != nullptr, dW != nullptr);
   if (no_space(workspace, workspace_bytes, p.bytes)) return LQ_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
