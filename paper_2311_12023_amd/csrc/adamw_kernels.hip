@@ -10,7 +10,19 @@ namespace lq {
 // Descriptions of tensors travel as kernel arguments (4 KB at most), a launch for every so many of them: nothing has to be uploaded
 // that a running kernel may still read, and a captured graph keeps its own.
 constexpr int GRADS_A_LAUNCH = 120, TENSORS_A_LAUNCH = 48;
-constexpr int64_t NORM_CHUNK = 16384, STEP_CHUNK = 8192;       // elements a workgroup takes
+// Elements a workgroup takes: one pass of its threads for few (a chain of passes is what a small call waits for), several for many.
+static int64_t chunk_of(double elements, int64_t most) {
+  int64_t chunk = 2048;
+  while (chunk < most && elements > (double)chunk * 2048) chunk *= 2;
+  return chunk;
+}
+template <typename Tensor>
+static double elements_of(const Tensor* t, int64_t count) {
+  double n = 0;
+  for (int64_t i = 0; i < count; ++i) n += (double)t[i].n;
+  return n;
+}
+constexpr int64_t NORM_CHUNK_MOST = 16384, STEP_CHUNK_MOST = 8192;
 
 // ---- the gradients' norm ------------------------------------------------------------------------------------
 struct GradTable {
@@ -18,7 +30,7 @@ struct GradTable {
   int64_t n[GRADS_A_LAUNCH];
   uint32_t first[GRADS_A_LAUNCH + 1];      // first workgroup of each
   uint8_t bf16[GRADS_A_LAUNCH];
-  int count;
+  int count, chunk;
 };
 
 template <typename Table>
@@ -31,12 +43,12 @@ __device__ __forceinline__ int tensor_of(const Table& t, uint32_t wg) {
   return lo;
 }
 
-template <typename T>
-__device__ __forceinline__ double squares(const T* g, int64_t n, int64_t from, int64_t to) {
+template <int THREADS, typename T>
+__device__ __forceinline__ double squares(const T* g, int64_t from, int64_t to) {
   typedef T vec8 __attribute__((ext_vector_type(8)));
   double sum = 0.0;
   const bool vec = ((uintptr_t)g & 15) == 0;
-  for (int64_t i = from + 8 * threadIdx.x; i < to; i += 8 * 256) {
+  for (int64_t i = from + 8 * threadIdx.x; i < to; i += 8 * THREADS) {
     if (vec && i + 8 <= to) {
       const vec8 v = *reinterpret_cast<const vec8*>(g + i);
 #pragma unroll
@@ -48,36 +60,57 @@ __device__ __forceinline__ double squares(const T* g, int64_t n, int64_t from, i
   return sum;
 }
 
+template <int THREADS>
 __device__ __forceinline__ double workgroup_sum(double x) {
-  __shared__ double part[4];
+  __shared__ double part[THREADS / 64];
 #pragma unroll
   for (int s = 1; s < 64; s <<= 1) x += __shfl_xor(x, s);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
   __syncthreads();
-  return (part[0] + part[1]) + (part[2] + part[3]);
+  double sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < THREADS / 64; ++i) sum += part[i];
+  return sum;
+}
+
+__device__ __forceinline__ void write_norm(double sum, float most, float* norm) {
+  const float x = (float)sqrt(sum);
+  norm[0] = x;
+  norm[1] = magnitude(x) >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : fminf(1.0f, most / (x + 1e-6f));
+}
+
+template <int THREADS>
+__device__ __forceinline__ double tensor_squares(const GradTable& t, int i, int64_t from, int64_t to) {
+  return t.bf16[i] ? squares<THREADS>(static_cast<const __bf16*>(t.g[i]), from, to) : squares<THREADS>(static_cast<const float*>(t.g[i]), from, to);
 }
 
 __global__ __launch_bounds__(256) void grad_squares_kernel(GradTable t, double* part) {
   const int i = __builtin_amdgcn_readfirstlane(tensor_of(t, blockIdx.x));
-  const int64_t n = t.n[i], from = (int64_t)(blockIdx.x - t.first[i]) * NORM_CHUNK, to = min(from + NORM_CHUNK, n);
-  const double sum = workgroup_sum(t.bf16[i] ? squares(static_cast<const __bf16*>(t.g[i]), n, from, to)
-                                             : squares(static_cast<const float*>(t.g[i]), n, from, to));
+  const int64_t from = (int64_t)(blockIdx.x - t.first[i]) * t.chunk;
+  const double sum = workgroup_sum<256>(tensor_squares<256>(t, i, from, min(from + t.chunk, t.n[i])));
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
 __global__ __launch_bounds__(256) void grad_norm_kernel(const double* part, int64_t parts, float most, float* norm) {
   double sum = 0.0;
   for (int64_t i = threadIdx.x; i < parts; i += 256) sum += part[i];
-  sum = workgroup_sum(sum);
-  if (threadIdx.x != 0) return;
-  const float x = (float)sqrt(sum);
-  norm[0] = x;
-  norm[1] = magnitude(x) >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : fminf(1.0f, most / (x + 1e-6f));
+  sum = workgroup_sum<256>(sum);
+  if (threadIdx.x == 0) write_norm(sum, most, norm);
+}
+
+// Few values: one workgroup and one launch for all.
+constexpr int FEW_PASSES = 4, FEW_THREADS = 1024;
+__global__ __launch_bounds__(FEW_THREADS) void grad_norm_few_kernel(GradTable t, float most, float* norm) {
+  double sum = 0.0;
+  for (int i = 0; i < t.count; ++i) sum += tensor_squares<FEW_THREADS>(t, i, 0, t.n[i]);
+  sum = workgroup_sum<FEW_THREADS>(sum);
+  if (threadIdx.x == 0) write_norm(sum, most, norm);
 }
 
 size_t grad_norm_parts(const lq_gradient* grads, int64_t count) {
   size_t parts = 0;
-  for (int64_t i = 0; i < count; ++i) parts += (size_t)((grads[i].n + NORM_CHUNK - 1) / NORM_CHUNK);
+  const int64_t chunk = chunk_of(elements_of(grads, count), NORM_CHUNK_MOST);
+  for (int64_t i = 0; i < count; ++i) parts += (size_t)((grads[i].n + chunk - 1) / chunk);
   return parts;
 }
 
@@ -85,13 +118,29 @@ int launch_grad_norm(const lq_gradient* grads, int64_t count, float max_norm, fl
   double bytes = 0;
   for (int64_t i = 0; i < count; ++i) bytes += (double)grads[i].n * type_bytes(grads[i].dtype);
   prof::Scope ps(prof::GRAD_NORM, st, bytes);
+  int64_t passes = 0;
+  for (int64_t i = 0; i < count && passes <= FEW_PASSES; ++i) passes += (grads[i].n + 8 * FEW_THREADS - 1) / (8 * FEW_THREADS);
+  if (passes <= FEW_PASSES) {
+    GradTable t{};
+    for (int64_t i = 0; i < count; ++i) {
+      if (!grads[i].n) continue;
+      t.g[t.count] = grads[i].g;
+      t.n[t.count] = grads[i].n;
+      t.bf16[t.count++] = grads[i].dtype == LQ_T_BF16;
+    }
+    hipLaunchKernelGGL(grad_norm_few_kernel, dim3(1), dim3(FEW_THREADS), 0, st, t, max_norm, norm);
+    LQ_HIP_TRY(hipGetLastError());
+    return LQ_OK;
+  }
   size_t done = 0;
+  const int64_t chunk = chunk_of(elements_of(grads, count), NORM_CHUNK_MOST);
   for (int64_t i = 0; i < count;) {
     GradTable t{};
+    t.chunk = (int)chunk;
     uint64_t wgs = 0;
     for (; i < count && t.count < GRADS_A_LAUNCH; ++i) {
       if (!grads[i].n) continue;
-      const uint64_t more = (uint64_t)((grads[i].n + NORM_CHUNK - 1) / NORM_CHUNK);
+      const uint64_t more = (uint64_t)((grads[i].n + chunk - 1) / chunk);
       if (t.count && wgs + more > 0x7fffffffull) break;
       t.g[t.count] = grads[i].g;
       t.n[t.count] = grads[i].n;
@@ -121,7 +170,7 @@ struct StepTable {
   uint32_t first[TENSORS_A_LAUNCH + 1];
   uint8_t kind[TENSORS_A_LAUNCH];          // bit 0: p bf16, 1: g bf16, 2: on 16-byte addresses
   uint32_t index[TENSORS_A_LAUNCH];        // in the call
-  int count;
+  int count, chunk;
 };
 struct StepFactors {
   float beta1, rest1, beta2, rest2, eps, keep, size, root;     // root: (1 - beta2^step)^-1/2, size: lr / (1 - beta1^step)
@@ -216,8 +265,8 @@ __device__ __forceinline__ float round_square(float x, uint32_t u) {
 }
 
 template <bool CODES, typename P, typename G>
-__device__ __forceinline__ void step_chunk(const StepTensor& t, uint32_t index, bool vec, const StepFactors& f, float coef, bool scaled, int64_t from) {
-  const int64_t to = min(from + STEP_CHUNK, t.n);
+__device__ __forceinline__ void step_chunk(const StepTensor& t, uint32_t index, bool vec, const StepFactors& f, float coef, bool scaled, int64_t from, int chunk) {
+  const int64_t to = min(from + chunk, t.n);
   // whole blocks of a state for every group of 32 lanes, so that its lanes stay together
   for (int64_t i = from + 8 * threadIdx.x; i - 8 * (threadIdx.x & 31) < to; i += 8 * 256) {
     const int count = (int)max((int64_t)0, min((int64_t)8, t.n - i));
@@ -273,14 +322,14 @@ __global__ __launch_bounds__(256) void adamw_kernel(StepTable table, StepArgs a)
   if (magnitude(coef) >= 0x7f800000u) return;
   const int i = __builtin_amdgcn_readfirstlane(tensor_of(table, blockIdx.x));
   const StepTensor t = table.t[i];
-  const int64_t from = (int64_t)(blockIdx.x - table.first[i]) * STEP_CHUNK;
+  const int64_t from = (int64_t)(blockIdx.x - table.first[i]) * table.chunk;
   const int kind = table.kind[i];
   const bool vec = kind & 4, scaled = a.coef != nullptr;
   const uint32_t index = table.index[i];
-  if ((kind & 3) == 0) step_chunk<CODES, float, float>(t, index, vec, f, coef, scaled, from);
-  else if ((kind & 3) == 1) step_chunk<CODES, __bf16, float>(t, index, vec, f, coef, scaled, from);
-  else if ((kind & 3) == 2) step_chunk<CODES, float, __bf16>(t, index, vec, f, coef, scaled, from);
-  else step_chunk<CODES, __bf16, __bf16>(t, index, vec, f, coef, scaled, from);
+  if ((kind & 3) == 0) step_chunk<CODES, float, float>(t, index, vec, f, coef, scaled, from, table.chunk);
+  else if ((kind & 3) == 1) step_chunk<CODES, __bf16, float>(t, index, vec, f, coef, scaled, from, table.chunk);
+  else if ((kind & 3) == 2) step_chunk<CODES, float, __bf16>(t, index, vec, f, coef, scaled, from, table.chunk);
+  else step_chunk<CODES, __bf16, __bf16>(t, index, vec, f, coef, scaled, from, table.chunk);
 }
 
 int launch_adamw(const lq_adamw_tensor* tensors, int64_t count, int state_bits, const lq_adamw_params& h, const float* coef, hipStream_t st) {
@@ -296,13 +345,15 @@ int launch_adamw(const lq_adamw_tensor* tensors, int64_t count, int state_bits, 
   for (int64_t i = 0; i < count; ++i)
     bytes += (double)tensors[i].n * (2 * type_bytes(tensors[i].p_dtype) + type_bytes(tensors[i].g_dtype) + (codes ? 4 : 16) + (tensors[i].copy ? 2 : 0));
   prof::Scope ps(prof::ADAMW, st, bytes);
+  const int64_t chunk = chunk_of(elements_of(tensors, count), STEP_CHUNK_MOST);
   for (int64_t i = 0; i < count;) {
     StepTable t{};
+    t.chunk = (int)chunk;
     uint64_t wgs = 0;
     for (; i < count && t.count < TENSORS_A_LAUNCH; ++i) {
       const lq_adamw_tensor& x = tensors[i];
       if (!x.n) continue;
-      const uint64_t more = (uint64_t)((x.n + STEP_CHUNK - 1) / STEP_CHUNK);
+      const uint64_t more = (uint64_t)((x.n + chunk - 1) / chunk);
       if (t.count && wgs + more > 0x7fffffffull) break;
       uintptr_t low = (uintptr_t)x.p | (uintptr_t)x.g | (uintptr_t)x.copy;
       const uintptr_t states = (uintptr_t)x.m | (uintptr_t)x.v;

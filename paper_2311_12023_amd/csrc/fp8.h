@@ -15,7 +15,8 @@ struct Fp8Quantize {
   uint8_t* codes; int64_t ld; float* scale;
   uint8_t* codes_t; int64_t ld_t; float* scale_t;
 };
-int launch_fp8_quantize(const Fp8Quantize& q, bool tiles, hipStream_t st);
+// One or two matrices, in one launch where their types are the same.
+int launch_fp8_quantize(const Fp8Quantize* q, int count, bool tiles, hipStream_t st);
 
 // ---- products (fp8_rows_kernels.hip) -----------------------------------------------------------------------
 // Out[column][row] = sum_k rows[row][k] columns[column][k], bf16, `ld` elements from column to column: the operand whose index runs
@@ -32,6 +33,10 @@ struct Fp8Product {
   void* out; int64_t ld;
 };
 int launch_fp8_product(const Fp8Product& p, float* part, size_t part_floats, hipStream_t st);
+// For up to 16 columns (fp8_quantizes_columns) with the columns' operand as it is before its quantization: row i of x is column i;
+// p.columns holds their count.
+bool fp8_quantizes_columns(int64_t columns);
+int launch_fp8_product_raw(const Fp8Product& p, const void* x, int64_t ldx, int dtype, float* part, size_t part_floats, hipStream_t st);
 // For many columns (fp8_product_kernels.hip).
 int launch_fp8_tiles(const Fp8Product& p, float* part, size_t part_floats, hipStream_t st);
 size_t fp8_tiles_part_floats(int64_t rows, int64_t columns, int64_t k);

@@ -16,10 +16,19 @@ constexpr float FP8_LIFT = 0x1p30f, FP8_DROP = 0x1p-30f;
 // Magnitudes are compared as bit patterns: NaN ranks above inf, inf above all numbers.
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-// Scale of a block whose largest magnitude has the bits `top`: the largest code is 448.
+// Scale of a block whose largest magnitude has the bits `top`: the largest code is 448.  The quotient, rounded: with y = fl(1 / 448) and
+// q = fl(a y), the rest a - 448 q is a float, and fl(q + rest y) is fl(a / 448) (Markstein, 1990) where it is normal; what is not
+// becomes 2^-126.  Three instructions for the ten of a division.
 __device__ __forceinline__ float fp8_scale(uint32_t top) {
-  const float s = fmaxf(__uint_as_float(top) / 448.0f, 0x1p-126f);
+  const float a = __uint_as_float(top), y = 1.0f / 448.0f, q = a * y;
+  const float s = fmaxf(fmaf(fmaf(-448.0f, q, a), y, q), 0x1p-126f);
   return top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : s;
+}
+// fl(1 / s) of a scale (2^-126 .. 2^120, or NaN): the hardware's reciprocal (one unit in the last place) and one Newton step.
+// That this is the rounded quotient was checked for all 2^23 fractions; scales by powers of two change nothing in this range.
+__device__ __forceinline__ float fp8_inverse(float s) {
+  const float y = __builtin_amdgcn_rcpf(s);
+  return fmaf(fmaf(-s, y, 1.0f), y, y);
 }
 
 // Codes of two neighbours in the lower or upper half of `old`.  |a|, |b| <= 448 (1 + 2^-22), which rounds to 448: nothing saturates.

@@ -27,22 +27,9 @@ __device__ __forceinline__ ProductTile product_tile(const ProductArgs& a, int u)
   return {4 * band + inside % high, inside / high};
 }
 
-// Two blocks of 16 rows of one column (elements 4 kg .. + 3 of each in this lane) to the output.
-__device__ __forceinline__ void product_store(const ProductArgs& a, floatx4 u, floatx4 v, int64_t row, int64_t column, int kg) {
-  const bf16x4 lo = {(__bf16)(u[0] * FP8_DROP), (__bf16)(u[1] * FP8_DROP), (__bf16)(u[2] * FP8_DROP), (__bf16)(u[3] * FP8_DROP)};
-  const bf16x4 hi = {(__bf16)(v[0] * FP8_DROP), (__bf16)(v[1] * FP8_DROP), (__bf16)(v[2] * FP8_DROP), (__bf16)(v[3] * FP8_DROP)};
-  __bf16* out = static_cast<__bf16*>(a.out) + column * a.ld;
-  const uintx4 w = seg_pair_blocks(__builtin_bit_cast(uintx2, lo), __builtin_bit_cast(uintx2, hi));
-  const int64_t first = row + 16 * (kg & 1) + 8 * (kg >> 1);
-  if (column >= a.columns.count) return;
-  if (a.vec && first + 8 <= a.rows.count) {
-    *reinterpret_cast<uintx4*>(out + first) = w;
-  } else {
-    const bf16x8 each = __builtin_bit_cast(bf16x8, w);
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (first + e < a.rows.count) out[first + e] = each[e];
-  }
+// Four rows of one column as they go into the output.
+__device__ __forceinline__ uintx2 product_result(floatx4 v) {
+  return __builtin_bit_cast(uintx2, bf16x4{(__bf16)(v[0] * FP8_DROP), (__bf16)(v[1] * FP8_DROP), (__bf16)(v[2] * FP8_DROP), (__bf16)(v[3] * FP8_DROP)});
 }
 
 // A workgroup of eight wavefronts makes a tile, a wavefront 128 x 64 of it (2 x 4) in blocks of 16 x 16.  A block of 128 along k is one
@@ -210,7 +197,7 @@ __global__ __launch_bounds__(P_THREADS) void fp8_product_kernel(ProductArgs a) {
   add(3, 3, last);
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
 
-  const int64_t row = row0 + 128 * wm, column = column0 + 64 * wn + l16;
+  const int64_t row = row0 + 128 * wm;
   if (a.splits > 1) {
     floatx4* part = reinterpret_cast<floatx4*>(a.part) + (size_t)item * (PT * PT / 4) + tid;
 #pragma unroll
@@ -219,26 +206,61 @@ __global__ __launch_bounds__(P_THREADS) void fp8_product_kernel(ProductArgs a) {
       for (int j = 0; j < 4; ++j) part[(i * 4 + j) * P_THREADS] = sums(i, j);
     return;
   }
+  // The output by way of the LDS, a wavefront's 64 columns of 128 rows (256 bytes, units of 16 bytes turned by the column) for itself: whole
+  // lines of a column, and little code, which a kernel this large otherwise waits for more than for its stores.
+  asm volatile("s_barrier" ::: "memory");            // everyone has read their operands
+  unsigned char* mine = lds + wave * 16384;
 #pragma unroll
-  for (int i = 0; i < 8; i += 2)
+  for (int i = 0; i < 8; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) product_store(a, sums(i, j), sums(i + 1, j), row + 16 * i, column + 16 * j, kg);
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<uintx2*>(mine + (16 * j + l16) * 256 + ((32 * i + 8 * kg) ^ (16 * l16))) = product_result(sums(i, j));
+  __bf16* out = static_cast<__bf16*>(a.out);
+  const int64_t first = column0 + 64 * wn, rows_left = a.rows.count - row, columns_left = a.columns.count - first;
+  if (a.vec && rows_left >= 128) {
+    const int unit16 = lane & 15, c = lane >> 4;
+#pragma unroll 2
+    for (int n = 0; n < 16; ++n) {
+      const int at = 4 * n + c;
+      const uintx4 w = *reinterpret_cast<const uintx4*>(mine + at * 256 + ((16 * unit16) ^ (16 * (at & 15))));
+      if (at < columns_left) *reinterpret_cast<uintx4*>(out + (first + at) * a.ld + row + 8 * unit16) = w;
+    }
+  } else {
+#pragma unroll 1
+    for (int n = 0; n < 128; ++n) {
+      const int at = n >> 1, r16 = 64 * (n & 1) + lane;
+      const __bf16 v = *reinterpret_cast<const __bf16*>(mine + at * 256 + ((2 * r16) ^ (16 * (at & 15))));
+      if (at < columns_left && r16 < rows_left) out[(first + at) * a.ld + row + r16] = v;
+    }
+  }
 }
 
-// Sum of a tile's ranges in order; a workgroup takes two blocks of 16 rows of every wavefront's part.
+// Sum of a tile's ranges in order; a workgroup takes one block of 16 rows and 16 columns of every wavefront's part.
 __global__ __launch_bounds__(P_THREADS) void fp8_join_kernel(ProductArgs a) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, wm = wave >> 2, wn = wave & 3, l16 = lane & 15, kg = lane >> 4;
-  const int u = blockIdx.x, i = 2 * blockIdx.y;
+  const int u = blockIdx.x, i = blockIdx.y >> 2, j = blockIdx.y & 3;
   const ProductTile t = product_tile(a, u);
-  const floatx4* part = reinterpret_cast<const floatx4*>(a.part) + (size_t)u * a.splits * (PT * PT / 4) + tid;
-  const int64_t row = (int64_t)t.tr * PT + 128 * wm + 16 * i, column = (int64_t)t.tc * PT + 64 * wn + l16;
+  const floatx4* part = reinterpret_cast<const floatx4*>(a.part) + (size_t)u * a.splits * (PT * PT / 4) + (i * 4 + j) * P_THREADS + tid;
+  const int64_t row = (int64_t)t.tr * PT + 128 * wm + 16 * i + 4 * kg, column = (int64_t)t.tc * PT + 64 * wn + 16 * j + l16;
+  if (row >= a.rows.count || column >= a.columns.count) return;
+  floatx4 v = {};
+  for (int s = 0; s < a.splits; s += 8) {            // eight under way together
+    floatx4 x[8];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    floatx4 v[2] = {};
-    for (int s = 0; s < a.splits; ++s)
+    for (int q = 0; q < 8; ++q) x[q] = part[(size_t)min(s + q, a.splits - 1) * (PT * PT / 4)];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) v[h] += part[(size_t)s * (PT * PT / 4) + ((i + h) * 4 + j) * P_THREADS];
-    product_store(a, v[0], v[1], row, column + 16 * j, kg);
+    for (int q = 0; q < 8; ++q)
+      if (s + q < a.splits) v += x[q];
+  }
+  const uintx2 w = product_result(v);
+  __bf16* out = static_cast<__bf16*>(a.out) + column * a.ld + row;
+  if (a.vec && row + 4 <= a.rows.count) {
+    *reinterpret_cast<uintx2*>(out) = w;
+  } else {
+    const bf16x4 each = __builtin_bit_cast(bf16x4, w);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (row + e < a.rows.count) out[e] = each[e];
   }
 }
 
@@ -273,7 +295,7 @@ int launch_fp8_tiles(const Fp8Product& p, float* part, size_t part_floats, hipSt
   }
   if (a.splits == 1) return LQ_OK;
   prof::Scope ps(prof::FP8_JOIN, st, (double)fp8_tiles_part_floats(p.rows.count, p.columns.count, p.k) * 4);
-  hipLaunchKernelGGL(fp8_join_kernel, dim3((unsigned)(a.tiles_r * a.tiles_c), 4), dim3(P_THREADS), 0, st, a);
+  hipLaunchKernelGGL(fp8_join_kernel, dim3((unsigned)(a.tiles_r * a.tiles_c), 32), dim3(P_THREADS), 0, st, a);
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }

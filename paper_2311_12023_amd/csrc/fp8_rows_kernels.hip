@@ -1,93 +1,320 @@
-// Products of matrices in 8 bits.
+// Products of matrices in 8 bits for few columns (tokens): bound by reading the rows' operand (the weights) once.
+#include "dense_device.h"
 #include "fp8.h"
 #include "fp8_device.h"
 #include "profiler.h"
 
 namespace lq {
 
-// 32 bytes of a row from byte `at` on, zero past its length k; what lies past the last 16 bytes that hold a value is not read.
-__device__ __forceinline__ intx8 fp8_load(const uint8_t* row, int64_t at, int64_t k) {
-  uintx4 half[2];
+constexpr int64_t FEW_COLUMNS = 128;       // up to which these kernels are taken
+constexpr int R_WAVES = 4;
+
+struct RowsArgs {
+  Fp8Operand rows, columns;                // columns.codes is not read where x is
+  const void* x; int64_t ldx;              // the columns' operand before its quantization
+  int64_t k;
+  void* out; int64_t ld;
+  float* part;
+  int64_t row_groups;
+  int splits, blocks;
+};
+
+// 32 bytes of a row from byte `at` on, in units of 16; units past the row's last one are the last one again.
+__device__ __forceinline__ intx8 rows_load(const uint8_t* row, int64_t at, int64_t last) {
+  const uintx4 x = *reinterpret_cast<const uintx4*>(row + min(at, last)), y = *reinterpret_cast<const uintx4*>(row + min(at + 16, last));
+  return intx8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+}
+// The bytes of those that lie past k become 0.
+__device__ __forceinline__ void rows_clear(intx8& v, int64_t at, int64_t k) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int64_t left = k - (at + 16 * h);
-    half[h] = left > 0 ? *reinterpret_cast<const uintx4*>(row + at + 16 * h) : uintx4{0, 0, 0, 0};
-    if (left < 16) {
+  for (int w = 0; w < 8; ++w) {
+    const int64_t bytes = k - at - 4 * w;
+    v[w] = bytes >= 4 ? v[w] : bytes <= 0 ? 0 : v[w] & ((1 << (8 * (int)bytes)) - 1);
+  }
+}
+
+// ---- the columns' operand quantized by the wavefronts that use it -------------------------------------------------
+// A step of 8 blocks of up to 16 columns: a lane takes 16 neighbours of a column, eight lanes a block.  Codes lie in rows of 1040
+// bytes (reads of 16 columns x 16 bytes touch every bank alike), the scales behind them.
+constexpr int X_PITCH = 8 * 128 + 16;
+constexpr int x_bytes(int columns) { return (columns * (X_PITCH + 8 * 4) + 15) & ~15; }      // of a wavefront
+
+template <typename T>
+struct RawColumn;
+template <>
+struct RawColumn<__bf16> {
+  uint32_t w[8];
+  __device__ __forceinline__ void load(const __bf16* x, int64_t i, int64_t k) {
+    typedef uintx4 unit __attribute__((aligned(2)));
+    if (i + 16 <= k) {
+      const uintx4 a = *reinterpret_cast<const unit*>(x + i), b = *reinterpret_cast<const unit*>(x + i + 8);
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int64_t bytes = left - 4 * w;
-        half[h][w] = bytes >= 4 ? half[h][w] : bytes <= 0 ? 0u : half[h][w] & ((1u << (8 * bytes)) - 1u);
+      for (int j = 0; j < 4; ++j) { w[j] = a[j]; w[4 + j] = b[j]; }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t lo = i + 2 * j < k ? __builtin_bit_cast(uint16_t, x[i + 2 * j]) : 0u;
+        const uint32_t hi = i + 2 * j + 1 < k ? __builtin_bit_cast(uint16_t, x[i + 2 * j + 1]) : 0u;
+        w[j] = lo | hi << 16;
       }
     }
   }
-  return intx8{(int)half[0][0], (int)half[0][1], (int)half[0][2], (int)half[0][3], (int)half[1][0], (int)half[1][1], (int)half[1][2], (int)half[1][3]};
+  __device__ __forceinline__ float value(int j) const { return __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16); }
+};
+template <>
+struct RawColumn<float> {
+  float v[16];
+  __device__ __forceinline__ void load(const float* x, int64_t i, int64_t k) {
+    typedef floatx4 unit __attribute__((aligned(4)));
+    if (i + 16 <= k) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const floatx4 a = *reinterpret_cast<const unit*>(x + i + 4 * q);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[4 * q + j] = a[j];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) v[j] = i + j < k ? x[i + j] : 0.0f;
+    }
+  }
+  __device__ __forceinline__ float value(int j) const { return v[j]; }
+};
+
+template <typename T>
+__device__ __forceinline__ void quantize_column(const RawColumn<T>& raw, int column, unsigned char* codes, float* scales, int lane) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) top = max(top, magnitude(raw.value(j)));
+  top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, XOR1, 0xf, 0xf, false));
+  top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, XOR2, 0xf, 0xf, false));
+  top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, XOR7, 0xf, 0xf, false));
+  const float s = fp8_scale(top), f = fp8_inverse(s);
+  uintx4 c;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    c[q] = fp8_four(raw.value(4 * q) * f, raw.value(4 * q + 1) * f, raw.value(4 * q + 2) * f, raw.value(4 * q + 3) * f);
+  *reinterpret_cast<uintx4*>(codes + column * X_PITCH + 16 * lane) = c;
+  if ((lane & 7) == 0) scales[column * 8 + (lane >> 3)] = s;
 }
 
-// A wavefront makes 16 rows x 16 NC columns; lane l brings byte 32 (l / 16) .. + 31 of a block of row (column) l % 16.
-template <int NC>
-__global__ __launch_bounds__(256) void fp8_rows_kernel(Fp8Product p) {
-  const int lane = threadIdx.x & 63, l16 = lane & 15, kg = lane >> 4;
-  const int64_t row_tiles = (p.rows.count + 15) / 16;
-  const int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), rt = u % row_tiles, ct = u / row_tiles;
-  const int64_t r0 = 16 * rt, c0 = 16 * NC * ct;
-  if (c0 >= p.columns.count) return;
-  const uint8_t* row = p.rows.codes + min(r0 + l16, p.rows.count - 1) * p.rows.ld;
+// ---- the product ---------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void rows_store(const RowsArgs& a, floatx4 v, int64_t row, int64_t column) {
+  if (column >= a.columns.count) return;
+  __bf16* out = static_cast<__bf16*>(a.out) + column * a.ld + row;
+  const bf16x4 w = {(__bf16)(v[0] * FP8_DROP), (__bf16)(v[1] * FP8_DROP), (__bf16)(v[2] * FP8_DROP), (__bf16)(v[3] * FP8_DROP)};
+  if (row + 4 <= a.rows.count && ((uintptr_t)out & 7) == 0) {
+    *reinterpret_cast<bf16x4*>(out) = w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (row + e < a.rows.count) out[e] = w[e];
+  }
+}
+
+// A workgroup makes 16 RT rows x 16 NC columns over its range of the sum, each of its wavefronts a quarter of the range: lane l
+// brings 32 bytes (l / 16) of a block of row (column) l % 16 straight into registers, U blocks of the rows' operand under way at
+// once.  With T (not void) the columns' operand is quantized on the way, by every workgroup for itself: a launch less.
+template <int NC, int RT, int U, bool TILED, typename T>
+__global__ __launch_bounds__(64 * R_WAVES) void fp8_rows_kernel(RowsArgs a) {
+  constexpr bool RAW = !std::is_void<T>::value;
+  extern __shared__ __align__(16) unsigned char lds[];
+  const int lane = threadIdx.x & 63, l16 = lane & 15, kg = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t group = blockIdx.x / a.splits;
+  const int split = (int)(blockIdx.x - group * a.splits);
+  const int w0 = split * R_WAVES + wave, shares = a.splits * R_WAVES;
+  const int b0 = (int)((int64_t)a.blocks * w0 / shares), b1 = (int)((int64_t)a.blocks * (w0 + 1) / shares);
+  const int64_t r0 = group * 16 * RT, last = (a.k - 1) & ~(int64_t)15;
+  const bool ragged = a.k % 128 != 0;
+  const uint8_t* row[RT];
+  constexpr int RS = TILED ? 1 : 4;                  // scales that a lane's four rows of a block have
+  const float* row_scale[RT][RS];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    row[t] = a.rows.codes + min(r0 + 16 * t + l16, a.rows.count - 1) * a.rows.ld;
+#pragma unroll
+    for (int e = 0; e < RS; ++e)
+      row_scale[t][e] = a.rows.scale + (TILED ? r0 >> 7 : min(r0 + 16 * t + 4 * kg + e, a.rows.count - 1) >> a.rows.shift) * a.rows.scale_row;
+  }
   const uint8_t* column[NC];
   const float* column_scale[NC];
 #pragma unroll
   for (int j = 0; j < NC; ++j) {
-    const int64_t i = min(c0 + 16 * j + l16, p.columns.count - 1);
-    column[j] = p.columns.codes + i * p.columns.ld;
-    column_scale[j] = p.columns.scale + (i >> p.columns.shift) * p.columns.scale_row;
+    const int64_t i = min((int64_t)16 * j + l16, a.columns.count - 1);
+    column[j] = a.columns.codes + i * a.columns.ld;
+    column_scale[j] = a.columns.scale + (i >> a.columns.shift) * a.columns.scale_row;
   }
-  const float* row_scale[4];
+  floatx4 acc[RT][NC];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) row_scale[e] = p.rows.scale + (min(r0 + 4 * kg + e, p.rows.count - 1) >> p.rows.shift) * p.rows.scale_row;
-  floatx4 acc[NC];
+  for (int t = 0; t < RT; ++t)
 #pragma unroll
-  for (int j = 0; j < NC; ++j) acc[j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-  const int64_t blocks = (p.k + FP8_BLOCK - 1) / FP8_BLOCK;
-  for (int64_t b = 0; b < blocks; ++b) {
-    const int64_t at = b * FP8_BLOCK + 32 * kg;
-    const intx8 x = fp8_load(row, at, p.k);
-    float s[4];
+    for (int j = 0; j < NC; ++j) acc[t][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int columns = (int)a.columns.count, mine = min(l16, columns - 1);
+  unsigned char* codes = lds + wave * x_bytes(columns);
+  float* scales = reinterpret_cast<float*>(codes + columns * X_PITCH);
+
+  for (int b = b0; b < b1; b += U) {
+    intx8 w[U][RT];
+    float s[U][RT][RS], f[U][NC];
+    auto load_rows = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s[e] = row_scale[e][b * p.rows.scale_block] * FP8_LIFT;
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      const intx8 y = fp8_load(column[j], at, p.k);
-      const float t = column_scale[j][b * p.columns.scale_block];
-      const floatx4 z = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, floatx4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0, 0, 0);
+        for (int t = 0; t < RT; ++t) w[u][t] = rows_load(row[t], (int64_t)min(b + u, b1 - 1) * 128 + 32 * kg, last);
+    };
+    if constexpr (RAW) {
+      const T* x = static_cast<const T*>(a.x);
+      const int64_t i = (int64_t)b * 128 + 16 * lane;
+      RawColumn<T> raw[4];
+      // the first columns' values are asked for before the weights, which they would otherwise wait for
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[j][e] = fmaf(z[e], s[e] * t, acc[j][e]);
+      for (int c = 0; c < 4; ++c)
+        if (c < columns) raw[c].load(x + c * a.ldx, i, a.k);
+      load_rows();
+      for (int c0 = 0; c0 < columns; c0 += 4) {
+        if (c0) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (c0 + c < columns) raw[c].load(x + (c0 + c) * a.ldx, i, a.k);
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (c0 + c < columns) quantize_column(raw[c], c0 + c, codes, scales, lane);
+      }
+    } else {
+      load_rows();
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = min(b + u, b1 - 1);
+#pragma unroll
+      for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int e = 0; e < RS; ++e) s[u][t][e] = row_scale[t][e][at * a.rows.scale_block] * FP8_LIFT;
+      if constexpr (!RAW) {
+#pragma unroll
+        for (int j = 0; j < NC; ++j) f[u][j] = column_scale[j][at * a.columns.scale_block];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (b + u < b1) {
+        const int64_t at = (int64_t)(b + u) * 128 + 32 * kg;
+        const bool end = ragged && b + u == a.blocks - 1;
+        intx8 y[NC];
+        if constexpr (RAW) {
+          const unsigned char* from = codes + mine * X_PITCH + 128 * u + 32 * kg;
+          const uintx4 lo = *reinterpret_cast<const uintx4*>(from), hi = *reinterpret_cast<const uintx4*>(from + 16);
+          y[0] = intx8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+          f[u][0] = scales[mine * 8 + u];
+        } else {
+#pragma unroll
+          for (int j = 0; j < NC; ++j) y[j] = rows_load(column[j], at, last);
+          if (end)
+#pragma unroll
+            for (int j = 0; j < NC; ++j) rows_clear(y[j], at, a.k);
+        }
+        if (end)
+#pragma unroll
+          for (int t = 0; t < RT; ++t) rows_clear(w[u][t], at, a.k);
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+#pragma unroll
+          for (int t = 0; t < RT; ++t) {
+            const floatx4 z = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[u][t], y[j], floatx4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[t][j][e] = fmaf(z[e], s[u][t][e & (RS - 1)] * f[u][j], acc[t][j][e]);
+          }
+      }
     }
   }
-  __bf16* out = static_cast<__bf16*>(p.out);
+
+  // the wavefronts' sums in order
+  floatx4* sums = reinterpret_cast<floatx4*>(lds);
+  if (RAW) __syncthreads();                          // everyone has read the codes
 #pragma unroll
-  for (int j = 0; j < NC; ++j) {
-    const int64_t i = c0 + 16 * j + l16;
+  for (int t = 0; t < RT; ++t)
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (i < p.columns.count && r0 + 4 * kg + e < p.rows.count) out[i * p.ld + r0 + 4 * kg + e] = (__bf16)(acc[j][e] * FP8_DROP);
+    for (int j = 0; j < NC; ++j) sums[((t * NC + j) * R_WAVES + wave) * 64 + lane] = acc[t][j];
+  __syncthreads();
+  for (int q = wave; q < RT * NC; q += R_WAVES) {
+    floatx4 v = sums[q * R_WAVES * 64 + lane];
+#pragma unroll
+    for (int i = 1; i < R_WAVES; ++i) v += sums[(q * R_WAVES + i) * 64 + lane];
+    const int t = q / NC, j = q - t * NC;
+    if (a.splits > 1) reinterpret_cast<floatx4*>(a.part)[((group * RT * NC + q) * a.splits + split) * 64 + lane] = v;
+    else rows_store(a, v, r0 + 16 * t + 4 * kg, 16 * j + l16);
   }
 }
 
-constexpr int64_t FEW_COLUMNS = 128;
+// The ranges' sums in order.
+template <int NC, int RT>
+__global__ __launch_bounds__(256) void fp8_rows_join_kernel(RowsArgs a) {
+  const int lane = threadIdx.x & 63, l16 = lane & 15, kg = lane >> 4;
+  const int64_t q = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (q >= a.row_groups * RT * NC) return;
+  const floatx4* part = reinterpret_cast<const floatx4*>(a.part) + q * a.splits * 64 + lane;
+  floatx4 v = part[0];
+  for (int i = 1; i < a.splits; ++i) v += part[i * 64];
+  const int64_t group = q / (RT * NC);
+  const int t = (int)(q - group * RT * NC) / NC, j = (int)(q - group * RT * NC) % NC;
+  rows_store(a, v, group * 16 * RT + 16 * t + 4 * kg, 16 * j + l16);
+}
+
+struct RowsShape { int nc, rt, splits; int64_t groups; };
+static RowsShape rows_shape(int64_t rows, int64_t columns, int64_t k) {
+  RowsShape s{};
+  s.nc = columns <= 16 ? 1 : columns <= 32 ? 2 : columns <= 64 ? 4 : 8;
+  s.rt = s.nc > 1 && rows >= 32 * 256 ? 2 : 1;
+  s.groups = (rows + 16 * s.rt - 1) / (16 * s.rt);
+  s.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / s.groups, fp8_blocks(k) / (4 * R_WAVES)));
+  return s;
+}
 size_t fp8_product_part_floats(int64_t rows, int64_t columns, int64_t k) {
-  return columns > FEW_COLUMNS ? fp8_tiles_part_floats(rows, columns, k) : 0;
+  if (columns > FEW_COLUMNS) return fp8_tiles_part_floats(rows, columns, k);
+  const RowsShape s = rows_shape(rows, columns, k);
+  return s.splits > 1 ? (size_t)s.groups * s.rt * s.nc * s.splits * 256 : 0;
+}
+bool fp8_quantizes_columns(int64_t columns) { return columns <= 16; }
+
+template <int NC, int RT, int U, bool TILED, typename T>
+static int launch(const RowsArgs& a, hipStream_t st) {
+  constexpr size_t sums = (size_t)NC * RT * R_WAVES * 1024, most = std::max<size_t>(sums, R_WAVES * x_bytes(16));
+  const size_t bytes = std::is_void<T>::value ? sums : std::max<size_t>(sums, R_WAVES * x_bytes((int)a.columns.count));
+  static LdsLimit limit;
+  if (most > 65536) LQ_TRY(limit.raise(reinterpret_cast<const void*>(fp8_rows_kernel<NC, RT, U, TILED, T>), most));
+  hipLaunchKernelGGL((fp8_rows_kernel<NC, RT, U, TILED, T>), dim3((unsigned)(a.row_groups * a.splits)), dim3(64 * R_WAVES), bytes, st, a);
+  LQ_HIP_TRY(hipGetLastError());
+  if (a.splits == 1) return LQ_OK;
+  hipLaunchKernelGGL((fp8_rows_join_kernel<NC, RT>), dim3((unsigned)((a.row_groups * NC * RT + 3) / 4)), dim3(256), 0, st, a);
+  LQ_HIP_TRY(hipGetLastError());
+  return LQ_OK;
+}
+template <bool TILED>
+static int launch_shape(const RowsArgs& a, int nc, int rt, int dtype, hipStream_t st) {
+  if (a.x) return dtype == LQ_T_BF16 ? launch<1, 1, 8, TILED, __bf16>(a, st) : launch<1, 1, 8, TILED, float>(a, st);
+  if (nc == 1) return launch<1, 1, 8, TILED, void>(a, st);
+  if (nc == 2) return rt == 2 ? launch<2, 2, 4, TILED, void>(a, st) : launch<2, 1, 4, TILED, void>(a, st);
+  if (nc == 4) return rt == 2 ? launch<4, 2, 2, TILED, void>(a, st) : launch<4, 1, 4, TILED, void>(a, st);
+  return rt == 2 ? launch<8, 2, 2, TILED, void>(a, st) : launch<8, 1, 2, TILED, void>(a, st);
+}
+
+static int launch_rows(const Fp8Product& p, const void* x, int64_t ldx, int dtype, float* part, size_t part_floats, hipStream_t st) {
+  const RowsShape s = rows_shape(p.rows.count, p.columns.count, p.k);
+  if (part_floats < fp8_product_part_floats(p.rows.count, p.columns.count, p.k)) return LQ_ERR_WORKSPACE;
+  if (s.groups * s.splits >= ((int64_t)1 << 31)) return LQ_ERR_SHAPE;
+  const RowsArgs a{p.rows, p.columns, x, ldx, p.k, p.out, p.ld, part, s.groups, s.splits, (int)fp8_blocks(p.k)};
+  prof::Scope ps(prof::FP8_ROWS, st, (double)p.rows.count * p.k);
+  return p.rows.shift ? launch_shape<true>(a, s.nc, s.rt, dtype, st) : launch_shape<false>(a, s.nc, s.rt, dtype, st);
 }
 
 int launch_fp8_product(const Fp8Product& p, float* part, size_t part_floats, hipStream_t st) {
   if (p.columns.count > FEW_COLUMNS) return launch_fp8_tiles(p, part, part_floats, st);
-  const int64_t row_tiles = (p.rows.count + 15) / 16;
-  const int nc = p.columns.count > 16 ? 4 : 1;
-  const int64_t waves = row_tiles * ((p.columns.count + 16 * nc - 1) / (16 * nc));
-  if (waves >= ((int64_t)1 << 32)) return LQ_ERR_SHAPE;
-  prof::Scope ps(prof::FP8_ROWS, st, (double)p.rows.count * p.k);
-  auto kernel = nc == 4 ? fp8_rows_kernel<4> : fp8_rows_kernel<1>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, p);
-  LQ_HIP_TRY(hipGetLastError());
-  return LQ_OK;
+  return launch_rows(p, nullptr, 0, 0, part, part_floats, st);
+}
+int launch_fp8_product_raw(const Fp8Product& p, const void* x, int64_t ldx, int dtype, float* part, size_t part_floats, hipStream_t st) {
+  if (!fp8_quantizes_columns(p.columns.count)) return LQ_ERR_SHAPE;
+  return launch_rows(p, x, ldx, dtype, part, part_floats, st);
 }
 
 }  // namespace lq

@@ -628,16 +628,20 @@ def fp8_backward(dy: torch.Tensor, x: torch.Tensor | None, wt: torch.Tensor | No
 
 def grad_norm(grads, max_norm: float = float("inf"), workspace: torch.Tensor | None = None):
     """2-norm of all gradients together and the factor that brings it to max_norm at most (NaN where the norm is not finite, which makes
-    AdamW.step change nothing): -> (norm, coef), fp32 of no dimensions on the GPU.  `workspace`: as grad_norm_workspace(grads)."""
+    AdamW.step change nothing): -> (norm, coef), fp32 of no dimensions on the GPU."""
     table = (Gradient * max(len(grads), 1))()
     for entry, g in zip(table, grads):
         entry.dtype = _dtype(g, "grads")
         entry.g, entry.n = _dev(g, g.dtype, "grads"), g.numel()
     _here(*grads)
+    need = _lib.lq_grad_norm_workspace_bytes(C.addressof(table), len(grads))
     device = grads[0].device if grads else "cuda"
-    ws = workspace if workspace is not None else _workspace(_lib.lq_grad_norm_workspace_bytes(C.addressof(table), len(grads)), device)
-    out = torch.empty(2, dtype=torch.float32, device=device)
-    _check(_lib.lq_grad_norm(C.addressof(table), len(grads), max_norm, out.data_ptr(), *_space(ws), _stream()), "lq_grad_norm")
+    if workspace is None:                        # behind the results, in one piece with them
+        out = torch.empty(64 + need // 4, dtype=torch.float32, device=device)
+        space = (out.data_ptr() + 256, need)
+    else:
+        out, space = torch.empty(2, dtype=torch.float32, device=device), _space(workspace)
+    _check(_lib.lq_grad_norm(C.addressof(table), len(grads), max_norm, out.data_ptr(), *space, _stream()), "lq_grad_norm")
     return out[0], out[1]
 
 
@@ -664,7 +668,7 @@ class AdamW:
             starts.append(total)
             total += -(-p.numel() // 256) * 256
         state = FP8 if bits == 8 else torch.float32
-        self._table = (AdamWTensor * len(self.params))()
+        self._table, self._params = (AdamWTensor * len(self.params))(), AdamWParams()
         for p, c in zip(self.params, self.copies):
             _dtype(p, "params"), _dev(p, p.dtype, "params")
             if p.device != device:
@@ -696,16 +700,17 @@ class AdamW:
             if g.numel() != entry.n or p.numel() != entry.n or g.device != p.device:
                 raise ValueError(f"grads: {g.numel()} values on {g.device} for {entry.n} parameters on {p.device}")
         on_device = isinstance(self.t, torch.Tensor)
-        if not on_device and torch.cuda.is_current_stream_capturing():
+        if not on_device and torch._C._cuda_isCurrentStreamCapturing():
             raise RuntimeError("a captured step needs device_step=True: a replay would repeat this step's number")
-        h = AdamWParams(beta1=betas[0], beta2=betas[1], eps=eps, weight_decay=weight_decay, seed=self.seed)
+        h = self._params
+        (h.beta1, h.beta2), h.eps, h.weight_decay, h.seed, h.lr_device = betas, eps, weight_decay, self.seed, None
         if isinstance(lr, torch.Tensor):
-            _shaped(lr.reshape(-1), (1,), "lr")
             h.lr_device = _dev(lr, torch.float32, "lr")
         else:
             h.lr = lr
-        if coef is not None:
-            _shaped(coef.reshape(-1), (1,), "coef")
+        for name, one in (("lr", lr), ("coef", coef)):
+            if isinstance(one, torch.Tensor) and one.numel() != 1:
+                raise ValueError(f"{name}: need one element")
         if on_device:
             self.t += 1
             h.step_device = self.t.data_ptr()

@@ -59,7 +59,7 @@ def test_operands_that_are_missing():
     assert L.lq_fp8_backward(P, 8, 0, P, 8, 0, None, 1, 8, 8, P, P, P, BIG, None) == -1
 
 
-def _forward(X=P, ldx=100, x_dtype=0, W=None, m=10, n=20, k=100, Y=P, ws=P, size=BIG):
+def _forward(X=P, ldx=100, x_dtype=0, W=None, m=40, n=20, k=100, Y=P, ws=P, size=BIG):
     return L.lq_fp8_forward(X, ldx, x_dtype, W or _matrix(), m, n, k, Y, ws, size, None)
 
 
@@ -85,12 +85,13 @@ def test_backward_refusals(change, status):
 def test_workspace_sizes():
     assert L.lq_fp8_forward_workspace_bytes(0, 8, 8) == 0 and L.lq_fp8_backward_workspace_bytes(8, 0, 8, 1, 1) == 0
     assert L.lq_fp8_matmul_workspace_bytes(8, 8, 1 << 23) == 0
-    for m, n, k in ((1, 1, 1), (37, 768, 100), (1000, 64, 128), (4096, 128, 4096)):
+    for m, n, k in ((1, 1, 1), (16, 11008, 4096), (37, 768, 100), (1000, 64, 128), (4096, 128, 4096)):
         need = L.lq_fp8_forward_workspace_bytes(m, n, k)
-        assert need >= m * k and _forward(m=m, n=n, k=k, ldx=k, W=_matrix(ld=4096), size=need - 1) == -6
+        assert need >= m * k * (m > 16)              # a few rows are quantized where they are used
+        assert not need or _forward(m=m, n=n, k=k, ldx=k, W=_matrix(ld=16384), size=need - 1) == -6
         need = [L.lq_fp8_backward_workspace_bytes(m, n, k, a, b) for a, b in ((1, 0), (0, 1), (1, 1))]
-        assert need[0] >= m * n and need[1] >= m * (n + k) and need[2] >= max(need[:2])
-        assert _backward(m=m, n=n, k=k, ldy=n, ldx=k, Wt=_matrix(ld=4096), size=need[2] - 1) == -6
+        assert need[0] >= m * n * (m > 16) and need[1] >= m * (n + k) and need[2] >= need[1] + m * n
+        assert _backward(m=m, n=n, k=k, ldy=n, ldx=k, Wt=_matrix(ld=16384), size=need[2] - 1) == -6
         need = L.lq_fp8_matmul_workspace_bytes(m, n, k)
         assert not need or _matmul(m=m, n=n, k=k, ldy=n, A=_matrix(ld=4096), B=_matrix(ld=4096), size=need - 1) == -6
 
