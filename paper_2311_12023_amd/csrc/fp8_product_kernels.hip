@@ -139,13 +139,14 @@ __global__ __launch_bounds__(P_THREADS) void fp8_product_kernel(ProductArgs a) {
       asm volatile("" : "+v"(acc[i][j][0]), "+v"(acc[i][j][1]), "+v"(acc[i][j][2]), "+v"(acc[i][j][3]));
     }
   };
+  // pieces 4 .. 7 are the columns', the others the rows' and the scales
 #pragma unroll
   for (int n = 0; n < 9; ++n) transfer(n, b0, 0);
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  if (b0 == a.blocks - 1 && rest < 128) clear_past(0);
-  asm volatile("s_barrier" ::: "memory");
 #pragma unroll
   for (int n = 0; n < 9; ++n) transfer(n, min(b0 + 1, b1 - 1), 1);
+  asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
+  if (b0 == a.blocks - 1 && rest < 128) clear_past(0);
+  asm volatile("s_barrier" ::: "memory");
 #pragma unroll
   for (int j = 0; j < 4; ++j) read_y(j);
   read_x(0);
@@ -156,12 +157,16 @@ __global__ __launch_bounds__(P_THREADS) void fp8_product_kernel(ProductArgs a) {
   for (int h = 0; h < 2; ++h) p[1][h] = r[2 + h] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   uint32_t stage = 0;
   // Past the last block the last one comes again, into a place whose contents nobody uses any more.
+  // All columns' operands of a block are in registers when it begins, so their place is free then and takes those of two blocks on while
+  // this one is under way; the rows' is free before its last products.
   for (int b = b0; b < b1; ++b) {
     const int next = min(b + 2, b1 - 1);
 #pragma unroll
     for (int ii = 0; ii < 4; ++ii) {
+      if (ii == 1) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       if (ii == 3) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        // outstanding are at most the four transfers of this block
+        asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)" ::: "memory");
         if (rest < 128 && b + 2 >= a.blocks) clear_past(stage ^ 1);
         asm volatile("s_barrier" ::: "memory");
         turn();
@@ -179,11 +184,11 @@ __global__ __launch_bounds__(P_THREADS) void fp8_product_kernel(ProductArgs a) {
         __builtin_amdgcn_sched_barrier(0);
         if (ii < 3) {
           if (j < 2) read_x(2 * ii + 2 + j);
+          if (ii == 1) transfer(4 + j, next, stage);
         } else {
           read_y(j);
           if (j < 2) read_x(j);
-          transfer(2 * j, next, stage);
-          transfer(2 * j + 1, next, stage);
+          transfer(j, next, stage);
           if (j == 3) {
             transfer(8, next, stage);
             read_scales();
