@@ -9,7 +9,7 @@ namespace lq {
 
 // Descriptions of tensors travel as kernel arguments (4 KB at most), a launch for every so many of them: nothing has to be uploaded
 // that a running kernel may still read, and a captured graph keeps its own.
-constexpr int GRADS_A_LAUNCH = 120, TENSORS_A_LAUNCH = 48;
+constexpr int GRADS_A_LAUNCH = 190, TENSORS_A_LAUNCH = 48;
 // Elements a workgroup takes: one pass of its threads for few (a chain of passes is what a small call waits for), several for many.
 static int64_t chunk_of(double elements, int64_t most) {
   int64_t chunk = 2048;
@@ -48,7 +48,19 @@ __device__ __forceinline__ double squares(const T* g, int64_t from, int64_t to) 
   typedef T vec8 __attribute__((ext_vector_type(8)));
   double sum = 0.0;
   const bool vec = ((uintptr_t)g & 15) == 0;
-  for (int64_t i = from + 8 * threadIdx.x; i < to; i += 8 * THREADS) {
+  int64_t i = from + 8 * threadIdx.x;
+  if (vec) {                                          // four loads under way together
+    for (; i + 3 * 8 * THREADS + 8 <= to; i += 4 * 8 * THREADS) {
+      vec8 v[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = *reinterpret_cast<const vec8*>(g + i + q * 8 * THREADS);
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum = fma((double)(float)v[q][j], (double)(float)v[q][j], sum);
+    }
+  }
+  for (; i < to; i += 8 * THREADS) {
     if (vec && i + 8 <= to) {
       const vec8 v = *reinterpret_cast<const vec8*>(g + i);
 #pragma unroll
@@ -345,12 +357,18 @@ int launch_adamw(const lq_adamw_tensor* tensors, int64_t count, int state_bits, 
   for (int64_t i = 0; i < count; ++i)
     bytes += (double)tensors[i].n * (2 * type_bytes(tensors[i].p_dtype) + type_bytes(tensors[i].g_dtype) + (codes ? 4 : 16) + (tensors[i].copy ? 2 : 0));
   prof::Scope ps(prof::ADAMW, st, bytes);
-  const int64_t chunk = chunk_of(elements_of(tensors, count), STEP_CHUNK_MOST);
   for (int64_t i = 0; i < count;) {
     StepTable t{};
+    int64_t to = i, used = 0;
+    double elements = 0;
+    for (; to < count && used < TENSORS_A_LAUNCH; ++to) {
+      used += tensors[to].n > 0;
+      elements += (double)tensors[to].n;
+    }
+    const int64_t chunk = chunk_of(elements, STEP_CHUNK_MOST);
     t.chunk = (int)chunk;
     uint64_t wgs = 0;
-    for (; i < count && t.count < TENSORS_A_LAUNCH; ++i) {
+    for (; i < to; ++i) {
       const lq_adamw_tensor& x = tensors[i];
       if (!x.n) continue;
       const uint64_t more = (uint64_t)((x.n + chunk - 1) / chunk);

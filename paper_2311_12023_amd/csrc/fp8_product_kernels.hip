@@ -45,7 +45,8 @@ __global__ __launch_bounds__(P_THREADS) void fp8_product_kernel(ProductArgs a) {
   extern __shared__ __align__(16) unsigned char lds[];
   const int item = seg_piece(a.tiles_r * a.tiles_c * a.splits);
   if (item < 0) return;
-  const int u = item / a.splits, split = item - u * a.splits;
+  // ranges first: the tiles of a range share its operands in an XCD's L2
+  const int tiles = a.tiles_r * a.tiles_c, split = item / tiles, u = item - split * tiles;
   const ProductTile t = product_tile(a, u);
   const int b0 = (int)((int64_t)a.blocks * split / a.splits), b1 = (int)((int64_t)a.blocks * (split + 1) / a.splits);
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -83,14 +84,24 @@ __global__ __launch_bounds__(P_THREADS) void fp8_product_kernel(ProductArgs a) {
   };
   // The last block's bytes past k become 0: everyone in what they brought themselves.
   auto clear_past = [&](uint32_t stage) __attribute__((always_inline)) {
-    // one word after the other: all operands are in registers meanwhile, none are left for more
-    unsigned char* at = lds + stage * P_STAGE + wave * 4096 + 16 * lane;
+    // one after the other: all operands are in registers meanwhile, few are left
+    const int left = rest - 16 * unit;
+    if (left < 16) {
+      unsigned char* at = lds + stage * P_STAGE + wave * 4096 + 16 * lane;
 #pragma unroll 1
-    for (int n = 0; n < 32; ++n) {
-      const int bytes = rest - 16 * unit - 4 * (n & 3);
-      uint32_t* w = reinterpret_cast<uint32_t*>(at + (n >> 4) * P_SIDE + ((n >> 2) & 3) * 1024 + 4 * (n & 3));
-      if (bytes <= 0) *w = 0;
-      else if (bytes < 4) *w &= (1u << (8 * bytes)) - 1u;
+      for (int n = 0; n < 8; ++n) {
+        uintx4* v = reinterpret_cast<uintx4*>(at + (n >> 2) * P_SIDE + (n & 3) * 1024);
+        uintx4 w = {0, 0, 0, 0};
+        if (left > 0) {
+          w = *v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int bytes = left - 4 * e;
+            w[e] = bytes >= 4 ? w[e] : bytes <= 0 ? 0u : w[e] & ((1u << (8 * bytes)) - 1u);
+          }
+        }
+        *v = w;
+      }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   };
@@ -115,29 +126,26 @@ __global__ __launch_bounds__(P_THREADS) void fp8_product_kernel(ProductArgs a) {
   intx8 x[4], y[4];
   floatx4 p[2][2], r[4];
   float s[4], last;                                  // last: the fourth scale of the block before, for its last sums
+  float row_scale = 1.0f;                            // of the rows' tile
   auto read_x = [&](int i) __attribute__((always_inline)) {
     x[i & 3] = operand(xa + 2048u * i, xb + 2048u * i);
     if constexpr (!ROW_TILES) r[i & 3] = *reinterpret_cast<const floatx4*>(lds + sa + 64 * i);
   };
   auto read_y = [&](int j) __attribute__((always_inline)) { y[j] = operand(ya + 2048u * j, yb + 2048u * j); };
-  auto read_scales = [&]() __attribute__((always_inline)) {
-    const float f = ROW_TILES ? *reinterpret_cast<const float*>(lds + sa) * FP8_LIFT : FP8_LIFT;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) s[j] = *reinterpret_cast<const float*>(lds + sb + 64 * j) * f;
+  auto read_s = [&](int j) __attribute__((always_inline)) { s[j] = *reinterpret_cast<const float*>(lds + sb + 64 * j); };
+  auto read_row_scale = [&]() __attribute__((always_inline)) {
+    if constexpr (ROW_TILES) row_scale = *reinterpret_cast<const float*>(lds + sa);
   };
   auto turn = [&]() __attribute__((always_inline)) {
     xa ^= P_STAGE; xb ^= P_STAGE; ya ^= P_STAGE; yb ^= P_STAGE;
     sa ^= 2 * PT * 4; sb ^= 2 * PT * 4;
   };
-  auto add = [&](int ii, int j, float f) __attribute__((always_inline)) {     // sums of blocks 2 ii, 2 ii + 1 and column block j
+  auto add = [&](int ii, int j, int h, float f) __attribute__((always_inline)) {       // sums of block 2 ii + h and column block j
+    const int i = 2 * ii + h;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int i = 2 * ii + h;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(ROW_TILES ? p[j & 1][h][e] : p[j & 1][h][e] * r[i & 3][e], f, acc[i][j][e]);
-      // kept here: moved behind a later branch they would leave all of p alive
-      asm volatile("" : "+v"(acc[i][j][0]), "+v"(acc[i][j][1]), "+v"(acc[i][j][2]), "+v"(acc[i][j][3]));
-    }
+    for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(ROW_TILES ? p[j & 1][h][e] : p[j & 1][h][e] * r[i & 3][e], f, acc[i][j][e]);
+    // kept here: moved behind a later branch they would leave all of p alive
+    asm volatile("" : "+v"(acc[i][j][0]), "+v"(acc[i][j][1]), "+v"(acc[i][j][2]), "+v"(acc[i][j][3]));
   };
   // pieces 4 .. 7 are the columns', the others the rows' and the scales
 #pragma unroll
@@ -147,11 +155,13 @@ __global__ __launch_bounds__(P_THREADS) void fp8_product_kernel(ProductArgs a) {
   asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
   if (b0 == a.blocks - 1 && rest < 128) clear_past(0);
   asm volatile("s_barrier" ::: "memory");
+  read_row_scale();
 #pragma unroll
-  for (int j = 0; j < 4; ++j) read_y(j);
-  read_x(0);
-  read_x(1);
-  read_scales();
+  for (int j = 0; j < 4; ++j) {
+    read_y(j);
+    if (j < 2) read_x(j);
+    read_s(j);
+  }
   last = 0.0f;
 #pragma unroll
   for (int h = 0; h < 2; ++h) p[1][h] = r[2 + h] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -167,44 +177,54 @@ __global__ __launch_bounds__(P_THREADS) void fp8_product_kernel(ProductArgs a) {
       if (ii == 3) {
         // outstanding are at most the four transfers of this block
         asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)" ::: "memory");
-        if (rest < 128 && b + 2 >= a.blocks) clear_past(stage ^ 1);
+        if (rest < 128 && b + 2 == a.blocks) clear_past(stage ^ 1);
         asm volatile("s_barrier" ::: "memory");
         turn();
         last = s[3];
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
+        auto product = [&](int h) __attribute__((always_inline)) {
           p[j & 1][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x[(2 * ii + h) & 3], y[j], floatx4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
-        if (j) add(ii, j - 1, s[j - 1]);
-        else if (ii) add(ii - 1, 3, s[3]);
-        else add(3, 3, last);                        // of the block before
-        __builtin_amdgcn_sched_barrier(0);
+          __builtin_amdgcn_sched_barrier(0);
+        };
+        auto sum = [&](int h) __attribute__((always_inline)) {
+          if (j) add(ii, j - 1, h, s[j - 1]);
+          else if (ii) add(ii - 1, 3, h, s[3]);
+          else add(3, 3, h, last);                   // of the block before
+          __builtin_amdgcn_sched_barrier(0);
+        };
+        // 4096 x 4096 by 11008: products and sums in turn 161 us, two by two 164; with scales of rows 196 and 193
+        if constexpr (ROW_TILES) {
+          product(0); sum(0); product(1); sum(1);
+        } else {
+          product(0); product(1); sum(0); sum(1);
+        }
         if (ii < 3) {
+          if (ii == 0) s[j] *= row_scale * FP8_LIFT;
           if (j < 2) read_x(2 * ii + 2 + j);
           if (ii == 1) transfer(4 + j, next, stage);
         } else {
+          // a scale's place is free once its last sums are through
+          if (j == 0) read_row_scale();
+          read_s((j + 3) & 3);
           read_y(j);
           if (j < 2) read_x(j);
           transfer(j, next, stage);
-          if (j == 3) {
-            transfer(8, next, stage);
-            read_scales();
-          }
+          if (j == 3) transfer(8, next, stage);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
     stage ^= 1;
   }
-  add(3, 3, last);
+  add(3, 3, 0, last);
+  add(3, 3, 1, last);
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
 
   const int64_t row = row0 + 128 * wm;
   if (a.splits > 1) {
-    floatx4* part = reinterpret_cast<floatx4*>(a.part) + (size_t)item * (PT * PT / 4) + tid;
+    floatx4* part = reinterpret_cast<floatx4*>(a.part) + ((size_t)u * a.splits + split) * (PT * PT / 4) + tid;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll

@@ -38,7 +38,7 @@ struct Codes {
   Fp8Operand rows(int64_t count) const { return {codes, ld, scale, 1, count, 0, count}; }
 };
 static Codes take_codes(Space& s, int64_t rows, int64_t k) {
-  const int64_t ld = up_to(k, 16);
+  const int64_t ld = up_to(k, 128);          // a block is a line
   uint8_t* c = s.take<uint8_t>(rows * ld);
   return {c, ld, s.take<float>(rows * fp8_blocks(k))};
 }

@@ -24,28 +24,38 @@ static int check_gradients(const lq_gradient* grads, int64_t count) {
   return LQ_OK;
 }
 
-// Whether two pieces of memory that the step writes overlap, or one of them and one that it only reads.
 struct Piece { uintptr_t from, to; };
-static bool overlapping(std::vector<Piece>& written, const std::vector<Piece>& read) {
-  std::sort(written.begin(), written.end(), [](const Piece& a, const Piece& b) { return a.from < b.from; });
-  for (size_t i = 1; i < written.size(); ++i)
-    if (written[i].from < written[i - 1].to) return true;
+static bool before(const Piece& a, const Piece& b) { return a.from < b.from; }
+
+// Whether two pieces of memory that the step writes overlap, or one of them and one that it only reads.  written: by what they are for;
+// one kind's pieces mostly come in order, so that hundreds of tensors take a few passes over them.
+constexpr int KINDS = 6;
+static bool overlapping(std::vector<Piece> (&written)[KINDS], const std::vector<Piece>& read) {
+  std::vector<Piece> all, next;
+  for (std::vector<Piece>& kind : written) {
+    if (!std::is_sorted(kind.begin(), kind.end(), before)) std::sort(kind.begin(), kind.end(), before);
+    next.resize(all.size() + kind.size());
+    std::merge(all.begin(), all.end(), kind.begin(), kind.end(), next.begin(), before);
+    all.swap(next);
+  }
+  for (size_t i = 1; i < all.size(); ++i)
+    if (all[i].from < all[i - 1].to) return true;
   for (const Piece& r : read) {
-    auto next = std::lower_bound(written.begin(), written.end(), r.to, [](const Piece& a, uintptr_t to) { return a.from < to; });
-    if (next != written.begin() && (next - 1)->to > r.from) return true;
+    auto it = std::lower_bound(all.begin(), all.end(), Piece{r.to, 0}, before);
+    if (it != all.begin() && (it - 1)->to > r.from) return true;
   }
   return false;
 }
 
 static int check_tensors(const lq_adamw_tensor* t, int64_t count, bool codes, const lq_adamw_params& h, const float* coef) {
-  std::vector<Piece> written, read;
-  written.reserve((size_t)count * (codes ? 6 : 4));
+  std::vector<Piece> written[KINDS], read;
+  for (std::vector<Piece>& kind : written) kind.reserve((size_t)count);
   read.reserve((size_t)count + 3);
   auto reads = [&](const void* p, int64_t bytes) { if (p) read.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes}); };
   reads(coef, 4);
   reads(h.lr_device, 4);
   reads(h.step_device, 8);
-  auto writes = [&](const void* p, int64_t bytes) { if (p) written.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes}); };
+  auto writes = [&](int kind, const void* p, int64_t bytes) { if (p) written[kind].push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes}); };
   for (int64_t i = 0; i < count; ++i) {
     const lq_adamw_tensor& x = t[i];
     if (x.n < 0 || x.n > MOST_VALUES) return LQ_ERR_SHAPE;
@@ -56,12 +66,12 @@ static int check_tensors(const lq_adamw_tensor* t, int64_t count, bool codes, co
     if (codes ? misaligned(x.m_scale, 4) || misaligned(x.v_scale, 4) : misaligned(x.m, 4) || misaligned(x.v, 4)) return LQ_ERR_ARG;
     if (x.copy && x.p_dtype != LQ_T_FP32) return LQ_ERR_ARG;
     const int64_t blocks = (x.n + STATE_BLOCK - 1) / STATE_BLOCK;
-    writes(x.p, x.n * (int64_t)type_bytes(x.p_dtype));
-    writes(x.m, x.n * (codes ? 1 : 4));
-    writes(x.v, x.n * (codes ? 1 : 4));
-    writes(x.copy, x.n * 2);
+    writes(0, x.p, x.n * (int64_t)type_bytes(x.p_dtype));
+    writes(1, x.m, x.n * (codes ? 1 : 4));
+    writes(2, x.v, x.n * (codes ? 1 : 4));
+    writes(3, x.copy, x.n * 2);
     reads(x.g, x.n * (int64_t)type_bytes(x.g_dtype));
-    if (codes) { writes(x.m_scale, blocks * 4); writes(x.v_scale, blocks * 4); }
+    if (codes) { writes(4, x.m_scale, blocks * 4); writes(5, x.v_scale, blocks * 4); }
   }
   return overlapping(written, read) ? LQ_ERR_ARG : LQ_OK;
 }

@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 import torch
@@ -514,8 +515,16 @@ def _blocks(n: int) -> int:
 
 
 def _codes_like(rows: int, cols: int, device) -> torch.Tensor:
-    """rows x cols codes whose rows begin on 16-byte addresses."""
-    return torch.empty((rows, -(-cols // 16) * 16), dtype=FP8, device=device)[:, :cols]
+    """rows x cols codes whose rows begin on 16-byte addresses; long rows on lines of 128 bytes, a block each."""
+    unit = 128 if cols >= 1024 else 16
+    return torch.empty((rows, -(-cols // unit) * unit), dtype=FP8, device=device)[:, :cols]
+
+
+def _scales_like(rows: int, cols: int, tiles: bool, device) -> torch.Tensor:
+    """Scales of rows x cols codes: of tiles row-major, of rows with the rows next to one another."""
+    if tiles:
+        return torch.empty((_blocks(rows), _blocks(cols)), dtype=torch.float32, device=device)
+    return torch.empty_strided((rows, _blocks(cols)), (1, rows), dtype=torch.float32, device=device)
 
 
 def fp8_quantize(x: torch.Tensor, tiles: bool = False, both: bool = False):
@@ -527,21 +536,21 @@ def fp8_quantize(x: torch.Tensor, tiles: bool = False, both: bool = False):
     m, d = x.shape
     _here(x)
     q = _codes_like(m, d, x.device)
-    scale = torch.empty((_blocks(m), _blocks(d)) if tiles else (_blocks(d), m), dtype=torch.float32, device=x.device)
+    scale = _scales_like(m, d, tiles, x.device)
     qt = _codes_like(d, m, x.device) if both else None
-    scale_t = torch.empty((_blocks(m), d), dtype=torch.float32, device=x.device) if both and not tiles else None
-    _check(_lib.lq_fp8_quantize(xp, m, d, ldx, code, int(tiles), q.data_ptr(), -(-d // 16) * 16, scale.data_ptr(),
-                                qt.data_ptr() if both else None, -(-m // 16) * 16 if both else 0,
+    scale_t = _scales_like(d, m, False, x.device) if both and not tiles else None
+    _check(_lib.lq_fp8_quantize(xp, m, d, ldx, code, int(tiles), q.data_ptr(), q.stride(0), scale.data_ptr(),
+                                qt.data_ptr() if both else None, qt.stride(0) if both else 0,
                                 None if scale_t is None else scale_t.data_ptr(), _stream()), "lq_fp8_quantize")
-    out = (q, scale) if tiles else (q, scale.t())
-    return out + ((qt, scale.t() if tiles else scale_t.t()) if both else ())
+    return (q, scale, qt, scale.t() if tiles else scale_t) if both else (q, scale)
 
 
 def _here(*tensors):
     """The calls launch on the current device's stream: operands elsewhere are refused."""
+    current = torch._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and t.get_device() != torch._C._cuda_getDevice():
-            raise ValueError(f"tensor on {t.device}, the current device is cuda:{torch._C._cuda_getDevice()}")
+        if t is not None and t.get_device() != current:
+            raise ValueError(f"tensor on {t.device}, the current device is cuda:{current}")
 
 
 def _fp8_matrix(codes, scale, name):
@@ -626,22 +635,38 @@ def fp8_backward(dy: torch.Tensor, x: torch.Tensor | None, wt: torch.Tensor | No
     return dx, dw
 
 
+def _gradients(grads):
+    """Addresses, sizes and types of gradients, checked: there may be hundreds, so the checks are made where they are cheap and told
+    apart only where one fails."""
+    places, sizes, types = [], [], []
+    for g in grads[:1]:
+        _dtype(g, "grads"), _dev(g, g.dtype, "grads")
+    current = torch._C._cuda_getDevice() if grads else 0
+    for g in grads:
+        code = T_DTYPES.get(g.dtype) if isinstance(g, torch.Tensor) else None
+        if code is None or g.get_device() != current or not g.is_contiguous():
+            _dtype(g, "grads"), _dev(g, g.dtype, "grads"), _here(g)
+        places.append(g.data_ptr())
+        sizes.append(g.numel())
+        types.append(code)
+    return places, sizes, types
+
+
 def grad_norm(grads, max_norm: float = float("inf"), workspace: torch.Tensor | None = None):
     """2-norm of all gradients together and the factor that brings it to max_norm at most (NaN where the norm is not finite, which makes
     AdamW.step change nothing): -> (norm, coef), fp32 of no dimensions on the GPU."""
-    table = (Gradient * max(len(grads), 1))()
-    for entry, g in zip(table, grads):
-        entry.dtype = _dtype(g, "grads")
-        entry.g, entry.n = _dev(g, g.dtype, "grads"), g.numel()
-    _here(*grads)
-    need = _lib.lq_grad_norm_workspace_bytes(C.addressof(table), len(grads))
+    grads = list(grads)
+    places, sizes, types = _gradients(grads)
+    total = sum(sizes)
+    table = struct.pack("QqQ" * len(grads), *[x for entry in zip(places, sizes, types) for x in entry])      # lq_gradient[]
     device = grads[0].device if grads else "cuda"
-    if workspace is None:                        # behind the results, in one piece with them
+    if workspace is None:                        # behind the results, in one piece with them: 8 bytes for every 2048 values at most
+        need = (total // 2048 + len(grads) + 32) * 8
         out = torch.empty(64 + need // 4, dtype=torch.float32, device=device)
         space = (out.data_ptr() + 256, need)
     else:
         out, space = torch.empty(2, dtype=torch.float32, device=device), _space(workspace)
-    _check(_lib.lq_grad_norm(C.addressof(table), len(grads), max_norm, out.data_ptr(), *space, _stream()), "lq_grad_norm")
+    _check(_lib.lq_grad_norm(table, len(grads), max_norm, out.data_ptr(), *space, _stream()), "lq_grad_norm")
     return out[0], out[1]
 
 
@@ -667,38 +692,50 @@ class AdamW:
         for p in self.params:
             starts.append(total)
             total += -(-p.numel() // 256) * 256
-        state = FP8 if bits == 8 else torch.float32
+        self._sizes = [p.numel() for p in self.params]
         self._table, self._params = (AdamWTensor * len(self.params))(), AdamWParams()
-        for p, c in zip(self.params, self.copies):
-            _dtype(p, "params"), _dev(p, p.dtype, "params")
-            if p.device != device:
-                raise ValueError("params: on different devices")
-            if c is not None:
-                _dev(c, torch.bfloat16, "copies")
-                _shaped(c, p.shape, "copies")
+        self._columns = np.frombuffer(self._table, dtype=np.dtype(AdamWTensor))
+        self._held = self.params + [c for c in self.copies if c is not None]
+        self._describe()
+        state = FP8 if bits == 8 else torch.float32
         self.buffers = {name: torch.zeros(total, dtype=state, device=device) for name in ("m", "v")}
         if bits == 8:
             self.buffers.update({name: torch.zeros(total // 256, dtype=torch.float32, device=device) for name in ("m_scale", "v_scale")})
-        for entry, p, c, at in zip(self._table, self.params, self.copies, starts):
-            entry.p, entry.n, entry.p_dtype = p.data_ptr(), p.numel(), T_DTYPES[p.dtype]
-            entry.copy = None if c is None else c.data_ptr()
+        for entry, at in zip(self._table, starts):
             for name, buffer in self.buffers.items():
                 setattr(entry, name, buffer.data_ptr() + (4 * (at // 256) if name.endswith("scale") else at * buffer.element_size()))
         self.t = torch.zeros((), dtype=torch.int64, device=device) if device_step else 0
 
+    def _describe(self):
+        """Parameters and copies into the table, checked."""
+        for entry, p, c, n in zip(self._table, self.params, self.copies, self._sizes):
+            _dtype(p, "params")
+            entry.p, entry.n, entry.p_dtype = _dev(p, p.dtype, "params"), n, T_DTYPES[p.dtype]
+            if p.device != self.params[0].device:
+                raise ValueError("params: on different devices")
+            if p.numel() != n:
+                raise ValueError("params: another size than at first")
+            if c is not None:
+                _shaped(c, p.shape, "copies")
+            entry.copy = _dev(c, torch.bfloat16, "copies")
+        self._places = [x.data_ptr() for x in self._held]
+
     def step(self, grads, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, coef: torch.Tensor | None = None) -> None:
         """One step.  grads: one for each parameter, fp32 or bf16, of its size.  lr: a number, or an fp32 tensor of one element on the GPU.
         coef: such a tensor that multiplies every gradient (grad_norm's); where it is not finite, nothing but `t` changes."""
-        if len(grads) != len(self.params):
-            raise ValueError("grads: need one for each parameter")
-        _here(*self.params[:1])
-        for entry, p, c, g in zip(self._table, self.params, self.copies, grads):
-            entry.p = _dev(p, p.dtype, "params")             # where they are now
-            entry.copy = None if c is None else c.data_ptr()
-            entry.g_dtype = _dtype(g, "grads")
-            entry.g = _dev(g, g.dtype, "grads")
-            if g.numel() != entry.n or p.numel() != entry.n or g.device != p.device:
-                raise ValueError(f"grads: {g.numel()} values on {g.device} for {entry.n} parameters on {p.device}")
+        grads = list(grads)
+        places, sizes, types = _gradients(grads)
+        if sizes != self._sizes:
+            raise ValueError("grads: need one for each parameter, of its size")
+        _here(self.params[0])
+        now = [x.data_ptr() for x in self._held]
+        if now != self._places:                              # parameters that have moved
+            self._describe()
+        if len(grads) > 16:
+            self._columns["g"], self._columns["g_dtype"] = places, types
+        else:
+            for entry, place, code in zip(self._table, places, types):
+                entry.g, entry.g_dtype = place, code
         on_device = isinstance(self.t, torch.Tensor)
         if not on_device and torch._C._cuda_isCurrentStreamCapturing():
             raise RuntimeError("a captured step needs device_step=True: a replay would repeat this step's number")
