@@ -33,7 +33,7 @@ struct Fp8Product {
   void* out; int64_t ld;
 };
 int launch_fp8_product(const Fp8Product& p, float* part, size_t part_floats, hipStream_t st);
-// For up to 16 columns (fp8_quantizes_columns) with the columns' operand as it is before its quantization: row i of x is column i;
+// For few columns (fp8_quantizes_columns) with the columns' operand as it is before its quantization: row i of x is column i;
 // p.columns holds their count.
 bool fp8_quantizes_columns(int64_t columns);
 int launch_fp8_product_raw(const Fp8Product& p, const void* x, int64_t ldx, int dtype, float* part, size_t part_floats, hipStream_t st);

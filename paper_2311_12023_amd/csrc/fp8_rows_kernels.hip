@@ -8,6 +8,9 @@ namespace lq {
 
 constexpr int64_t FEW_COLUMNS = 128;       // up to which these kernels are taken
 constexpr int R_WAVES = 4;
+// Columns that are quantized where they are used, us for 8 rows so and in a launch before: bf16 768 x 768 8.7 and 8.6, 4096 x 4096 13.8 and
+// 14.7, 11008 x 4096 14.9 and 17.1; fp32 8.5 and 8.7, 15.9 and 14.9, 16.4 and 17.3.  One row 4.8 and 7.3, 9.3 and 13.1, 10.5 and 14.5.
+constexpr int RAW_MOST = 8;
 
 struct RowsArgs {
   Fp8Operand rows, columns;                // columns.codes is not read where x is
@@ -34,8 +37,8 @@ __device__ __forceinline__ void rows_clear(intx8& v, int64_t at, int64_t k) {
 }
 
 // ---- the columns' operand quantized by the wavefronts that use it -------------------------------------------------
-// A step of 8 blocks of up to 16 columns: a lane takes 16 neighbours of a column, eight lanes a block.  Codes lie in rows of 1040
-// bytes (reads of 16 columns x 16 bytes touch every bank alike), the scales behind them.
+// A step of 8 blocks: a lane takes 16 neighbours of a column, eight lanes a block.  Codes lie in rows of 1040 bytes (reads of 16 columns
+// x 16 bytes touch every bank alike), the scales behind them.
 constexpr int X_PITCH = 8 * 128 + 16;
 constexpr int x_bytes(int columns) { return (columns * (X_PITCH + 8 * 4) + 15) & ~15; }      // of a wavefront
 
@@ -114,10 +117,12 @@ __device__ __forceinline__ void rows_store(const RowsArgs& a, floatx4 v, int64_t
 
 // A workgroup makes 16 RT rows x 16 NC columns over its range of the sum, each of its wavefronts a quarter of the range: lane l
 // brings 32 bytes (l / 16) of a block of row (column) l % 16 straight into registers, U blocks of the rows' operand under way at
-// once.  With T (not void) the columns' operand is quantized on the way, by every workgroup for itself: a launch less.
-template <int NC, int RT, int U, bool TILED, typename T>
+// once.  With T (not void) the up to RAWS columns of that operand are quantized on the
+// way, by every workgroup for itself: a launch less.
+template <int NC, int RT, int U, bool TILED, int RAWS, typename T>
 __global__ __launch_bounds__(64 * R_WAVES) void fp8_rows_kernel(RowsArgs a) {
   constexpr bool RAW = !std::is_void<T>::value;
+  static_assert(!RAW || (NC == 1 && U == 8 && RAWS <= RAW_MOST), "a step's layout");
   extern __shared__ __align__(16) unsigned char lds[];
   const int lane = threadIdx.x & 63, l16 = lane & 15, kg = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t group = blockIdx.x / a.splits;
@@ -149,7 +154,7 @@ __global__ __launch_bounds__(64 * R_WAVES) void fp8_rows_kernel(RowsArgs a) {
   for (int t = 0; t < RT; ++t)
 #pragma unroll
     for (int j = 0; j < NC; ++j) acc[t][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-  const int columns = (int)a.columns.count, mine = min(l16, columns - 1);
+  const int columns = (int)a.columns.count;
   unsigned char* codes = lds + wave * x_bytes(columns);
   float* scales = reinterpret_cast<float*>(codes + columns * X_PITCH);
 
@@ -165,22 +170,15 @@ __global__ __launch_bounds__(64 * R_WAVES) void fp8_rows_kernel(RowsArgs a) {
     if constexpr (RAW) {
       const T* x = static_cast<const T*>(a.x);
       const int64_t i = (int64_t)b * 128 + 16 * lane;
-      RawColumn<T> raw[4];
-      // the first columns' values are asked for before the weights, which they would otherwise wait for
+      RawColumn<T> raw[RAWS];
+      // the columns' values are asked for before the weights, which they would otherwise wait for
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
+      for (int c = 0; c < RAWS; ++c)
         if (c < columns) raw[c].load(x + c * a.ldx, i, a.k);
       load_rows();
-      for (int c0 = 0; c0 < columns; c0 += 4) {
-        if (c0) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (c0 + c < columns) raw[c].load(x + (c0 + c) * a.ldx, i, a.k);
-        }
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (c0 + c < columns) quantize_column(raw[c], c0 + c, codes, scales, lane);
-      }
+      for (int c = 0; c < RAWS; ++c)
+        if (c < columns) quantize_column(raw[c], c, codes, scales, lane);
     } else {
       load_rows();
     }
@@ -203,6 +201,7 @@ __global__ __launch_bounds__(64 * R_WAVES) void fp8_rows_kernel(RowsArgs a) {
         const bool end = ragged && b + u == a.blocks - 1;
         intx8 y[NC];
         if constexpr (RAW) {
+          const int mine = min(l16, columns - 1);
           const unsigned char* from = codes + mine * X_PITCH + 128 * u + 32 * kg;
           const uintx4 lo = *reinterpret_cast<const uintx4*>(from), hi = *reinterpret_cast<const uintx4*>(from + 16);
           y[0] = intx8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
@@ -275,15 +274,15 @@ size_t fp8_product_part_floats(int64_t rows, int64_t columns, int64_t k) {
   const RowsShape s = rows_shape(rows, columns, k);
   return s.splits > 1 ? (size_t)s.groups * s.rt * s.nc * s.splits * 256 : 0;
 }
-bool fp8_quantizes_columns(int64_t columns) { return columns <= 16; }
+bool fp8_quantizes_columns(int64_t columns) { return columns <= RAW_MOST; }
 
-template <int NC, int RT, int U, bool TILED, typename T>
+template <int NC, int RT, int U, bool TILED, int RAWS, typename T>
 static int launch(const RowsArgs& a, hipStream_t st) {
-  constexpr size_t sums = (size_t)NC * RT * R_WAVES * 1024, most = std::max<size_t>(sums, R_WAVES * x_bytes(16));
+  constexpr size_t sums = (size_t)NC * RT * R_WAVES * 1024, most = std::max<size_t>(sums, R_WAVES * x_bytes(RAWS));
   const size_t bytes = std::is_void<T>::value ? sums : std::max<size_t>(sums, R_WAVES * x_bytes((int)a.columns.count));
   static LdsLimit limit;
-  if (most > 65536) LQ_TRY(limit.raise(reinterpret_cast<const void*>(fp8_rows_kernel<NC, RT, U, TILED, T>), most));
-  hipLaunchKernelGGL((fp8_rows_kernel<NC, RT, U, TILED, T>), dim3((unsigned)(a.row_groups * a.splits)), dim3(64 * R_WAVES), bytes, st, a);
+  if (most > 65536) LQ_TRY(limit.raise(reinterpret_cast<const void*>(fp8_rows_kernel<NC, RT, U, TILED, RAWS, T>), most));
+  hipLaunchKernelGGL((fp8_rows_kernel<NC, RT, U, TILED, RAWS, T>), dim3((unsigned)(a.row_groups * a.splits)), dim3(64 * R_WAVES), bytes, st, a);
   LQ_HIP_TRY(hipGetLastError());
   if (a.splits == 1) return LQ_OK;
   hipLaunchKernelGGL((fp8_rows_join_kernel<NC, RT>), dim3((unsigned)((a.row_groups * NC * RT + 3) / 4)), dim3(256), 0, st, a);
@@ -292,11 +291,13 @@ static int launch(const RowsArgs& a, hipStream_t st) {
 }
 template <bool TILED>
 static int launch_shape(const RowsArgs& a, int nc, int rt, int dtype, hipStream_t st) {
-  if (a.x) return dtype == LQ_T_BF16 ? launch<1, 1, 8, TILED, __bf16>(a, st) : launch<1, 1, 8, TILED, float>(a, st);
-  if (nc == 1) return launch<1, 1, 8, TILED, void>(a, st);
-  if (nc == 2) return rt == 2 ? launch<2, 2, 4, TILED, void>(a, st) : launch<2, 1, 4, TILED, void>(a, st);
-  if (nc == 4) return rt == 2 ? launch<4, 2, 2, TILED, void>(a, st) : launch<4, 1, 4, TILED, void>(a, st);
-  return rt == 2 ? launch<8, 2, 2, TILED, void>(a, st) : launch<8, 1, 2, TILED, void>(a, st);
+  // half as many columns in registers leave room for half as many wavefronts again: one row, 11008 x 4096, bf16 10.5 and 11.6 us
+  if (a.x && a.columns.count <= 4) return dtype == LQ_T_BF16 ? launch<1, 1, 8, TILED, 4, __bf16>(a, st) : launch<1, 1, 8, TILED, 4, float>(a, st);
+  if (a.x) return dtype == LQ_T_BF16 ? launch<1, 1, 8, TILED, RAW_MOST, __bf16>(a, st) : launch<1, 1, 8, TILED, RAW_MOST, float>(a, st);
+  if (nc == 1) return launch<1, 1, 8, TILED, 0, void>(a, st);
+  if (nc == 2) return rt == 2 ? launch<2, 2, 4, TILED, 0, void>(a, st) : launch<2, 1, 4, TILED, 0, void>(a, st);
+  if (nc == 4) return rt == 2 ? launch<4, 2, 2, TILED, 0, void>(a, st) : launch<4, 1, 4, TILED, 0, void>(a, st);
+  return rt == 2 ? launch<8, 2, 2, TILED, 0, void>(a, st) : launch<8, 1, 2, TILED, 0, void>(a, st);
 }
 
 static int launch_rows(const Fp8Product& p, const void* x, int64_t ldx, int dtype, float* part, size_t part_floats, hipStream_t st) {
