@@ -6,7 +6,10 @@
 
 namespace lq {
 
-constexpr int64_t FEW_COLUMNS = 128;       // up to which these kernels are taken
+// Whether these kernels are taken, us by them and by 256 x 256 tiles (rows x depth, columns): up to 64 columns 4096 x 4096, 64 17 and 23,
+// 4096 x 11008, 64 33 and 32, 1024 x 50265, 64 42 and 40, 32 31 and 38; up to 128 where the sum is short: 768 x 768, 128 11 and 17,
+// 32000 x 1024, 128 30 and 36, 768 x 3000, 128 20 and 19, 11008 x 4096, 128 46 and 34.
+static bool few_columns(int64_t columns, int64_t k) { return columns <= 64 || (columns <= 128 && k <= 3000); }
 constexpr int R_WAVES = 4;
 // Columns that are quantized where they are used, us for 8 rows so and in a launch before: bf16 768 x 768 8.7 and 8.6, 4096 x 4096 13.8 and
 // 14.7, 11008 x 4096 14.9 and 17.1; fp32 8.5 and 8.7, 15.9 and 14.9, 16.4 and 17.3.  One row 4.8 and 7.3, 9.3 and 13.1, 10.5 and 14.5.
@@ -37,10 +40,10 @@ __device__ __forceinline__ void rows_clear(intx8& v, int64_t at, int64_t k) {
 }
 
 // ---- the columns' operand quantized by the wavefronts that use it -------------------------------------------------
-// A step of 8 blocks: a lane takes 16 neighbours of a column, eight lanes a block.  Codes lie in rows of 1040 bytes (reads of 16 columns
-// x 16 bytes touch every bank alike), the scales behind them.
-constexpr int X_PITCH = 8 * 128 + 16;
-constexpr int x_bytes(int columns) { return (columns * (X_PITCH + 8 * 4) + 15) & ~15; }      // of a wavefront
+// A step of U blocks: a lane takes 16 neighbours of a column, eight lanes a block, 8 U a column.  A column's codes are followed by 16
+// bytes (reads of 16 columns x 16 bytes touch every bank alike), all codes by the scales.
+constexpr int x_pitch(int u) { return u * 128 + 16; }
+constexpr int x_bytes(int columns, int u) { return (columns * (x_pitch(u) + u * 4) + 15) & ~15; }      // of a wavefront
 
 template <typename T>
 struct RawColumn;
@@ -84,8 +87,9 @@ struct RawColumn<float> {
   __device__ __forceinline__ float value(int j) const { return v[j]; }
 };
 
-template <typename T>
-__device__ __forceinline__ void quantize_column(const RawColumn<T>& raw, int column, unsigned char* codes, float* scales, int lane) {
+// The lane's 16 values of a column, from the `at`th of the step on.
+template <int U, typename T>
+__device__ __forceinline__ void quantize_column(const RawColumn<T>& raw, int column, unsigned char* codes, float* scales, int at) {
   uint32_t top = 0;
 #pragma unroll
   for (int j = 0; j < 16; ++j) top = max(top, magnitude(raw.value(j)));
@@ -97,8 +101,8 @@ __device__ __forceinline__ void quantize_column(const RawColumn<T>& raw, int col
 #pragma unroll
   for (int q = 0; q < 4; ++q)
     c[q] = fp8_four(raw.value(4 * q) * f, raw.value(4 * q + 1) * f, raw.value(4 * q + 2) * f, raw.value(4 * q + 3) * f);
-  *reinterpret_cast<uintx4*>(codes + column * X_PITCH + 16 * lane) = c;
-  if ((lane & 7) == 0) scales[column * 8 + (lane >> 3)] = s;
+  *reinterpret_cast<uintx4*>(codes + column * x_pitch(U) + at) = c;
+  if (at % 128 == 0) scales[column * U + at / 128] = s;
 }
 
 // ---- the product ---------------------------------------------------------------------------------------------------
@@ -122,7 +126,7 @@ __device__ __forceinline__ void rows_store(const RowsArgs& a, floatx4 v, int64_t
 template <int NC, int RT, int U, bool TILED, int RAWS, typename T>
 __global__ __launch_bounds__(64 * R_WAVES) void fp8_rows_kernel(RowsArgs a) {
   constexpr bool RAW = !std::is_void<T>::value;
-  static_assert(!RAW || (NC == 1 && U == 8 && RAWS <= RAW_MOST), "a step's layout");
+  static_assert(!RAW || (NC == 1 && U <= 8 && RAWS <= RAW_MOST && RAWS % (8 / U) == 0), "a step's layout");
   extern __shared__ __align__(16) unsigned char lds[];
   const int lane = threadIdx.x & 63, l16 = lane & 15, kg = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t group = blockIdx.x / a.splits;
@@ -155,8 +159,8 @@ __global__ __launch_bounds__(64 * R_WAVES) void fp8_rows_kernel(RowsArgs a) {
 #pragma unroll
     for (int j = 0; j < NC; ++j) acc[t][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   const int columns = (int)a.columns.count;
-  unsigned char* codes = lds + wave * x_bytes(columns);
-  float* scales = reinterpret_cast<float*>(codes + columns * X_PITCH);
+  unsigned char* codes = lds + wave * x_bytes(columns, U);
+  float* scales = reinterpret_cast<float*>(codes + columns * x_pitch(U));
 
   for (int b = b0; b < b1; b += U) {
     intx8 w[U][RT];
@@ -169,16 +173,17 @@ __global__ __launch_bounds__(64 * R_WAVES) void fp8_rows_kernel(RowsArgs a) {
     };
     if constexpr (RAW) {
       const T* x = static_cast<const T*>(a.x);
-      const int64_t i = (int64_t)b * 128 + 16 * lane;
-      RawColumn<T> raw[RAWS];
+      constexpr int G = 8 / U, N = RAWS / G;         // columns at a time, times
+      const int at = 16 * (lane % (8 * U)), own = lane / (8 * U);
+      RawColumn<T> raw[N];
       // the columns' values are asked for before the weights, which they would otherwise wait for
 #pragma unroll
-      for (int c = 0; c < RAWS; ++c)
-        if (c < columns) raw[c].load(x + c * a.ldx, i, a.k);
+      for (int c = 0; c < N; ++c)
+        if (G * c + own < columns) raw[c].load(x + (G * c + own) * a.ldx, (int64_t)b * 128 + at, a.k);
       load_rows();
 #pragma unroll
-      for (int c = 0; c < RAWS; ++c)
-        if (c < columns) quantize_column(raw[c], c, codes, scales, lane);
+      for (int c = 0; c < N; ++c)
+        if (G * c + own < columns) quantize_column<U>(raw[c], G * c + own, codes, scales, at);
     } else {
       load_rows();
     }
@@ -202,10 +207,10 @@ __global__ __launch_bounds__(64 * R_WAVES) void fp8_rows_kernel(RowsArgs a) {
         intx8 y[NC];
         if constexpr (RAW) {
           const int mine = min(l16, columns - 1);
-          const unsigned char* from = codes + mine * X_PITCH + 128 * u + 32 * kg;
+          const unsigned char* from = codes + mine * x_pitch(U) + 128 * u + 32 * kg;
           const uintx4 lo = *reinterpret_cast<const uintx4*>(from), hi = *reinterpret_cast<const uintx4*>(from + 16);
           y[0] = intx8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-          f[u][0] = scales[mine * 8 + u];
+          f[u][0] = scales[mine * U + u];
         } else {
 #pragma unroll
           for (int j = 0; j < NC; ++j) y[j] = rows_load(column[j], at, last);
@@ -263,14 +268,20 @@ __global__ __launch_bounds__(256) void fp8_rows_join_kernel(RowsArgs a) {
 struct RowsShape { int nc, rt, splits; int64_t groups; };
 static RowsShape rows_shape(int64_t rows, int64_t columns, int64_t k) {
   RowsShape s{};
+  const int64_t blocks = fp8_blocks(k);
   s.nc = columns <= 16 ? 1 : columns <= 32 ? 2 : columns <= 64 ? 4 : 8;
   s.rt = s.nc > 1 && rows >= 32 * 256 ? 2 : 1;
+  // up to 16 columns: eight blocks under way a wavefront also where its share of the sum is shorter, by more rows
+  if (s.nc == 1)
+    while (s.rt < 4 && blocks * s.rt <= 4 * R_WAVES && rows >= 32 * s.rt * 256) s.rt *= 2;
   s.groups = (rows + 16 * s.rt - 1) / (16 * s.rt);
-  s.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / s.groups, fp8_blocks(k) / (4 * R_WAVES)));
+  // Ranges only where workgroups would leave CUs idle, each wavefront's a step (or half of one, where the columns take their time) at
+  // least; their join is a launch: one row, 4096 x 4096, 5.7 us whole and 9.0 in two ranges.
+  s.splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / s.groups, blocks / ((s.nc == 1 ? 8 : 4) * R_WAVES)));
   return s;
 }
 size_t fp8_product_part_floats(int64_t rows, int64_t columns, int64_t k) {
-  if (columns > FEW_COLUMNS) return fp8_tiles_part_floats(rows, columns, k);
+  if (!few_columns(columns, k)) return fp8_tiles_part_floats(rows, columns, k);
   const RowsShape s = rows_shape(rows, columns, k);
   return s.splits > 1 ? (size_t)s.groups * s.rt * s.nc * s.splits * 256 : 0;
 }
@@ -278,8 +289,8 @@ bool fp8_quantizes_columns(int64_t columns) { return columns <= RAW_MOST; }
 
 template <int NC, int RT, int U, bool TILED, int RAWS, typename T>
 static int launch(const RowsArgs& a, hipStream_t st) {
-  constexpr size_t sums = (size_t)NC * RT * R_WAVES * 1024, most = std::max<size_t>(sums, R_WAVES * x_bytes(RAWS));
-  const size_t bytes = std::is_void<T>::value ? sums : std::max<size_t>(sums, R_WAVES * x_bytes((int)a.columns.count));
+  constexpr size_t sums = (size_t)NC * RT * R_WAVES * 1024, most = std::max<size_t>(sums, R_WAVES * x_bytes(RAWS, U));
+  const size_t bytes = std::is_void<T>::value ? sums : std::max<size_t>(sums, R_WAVES * x_bytes((int)a.columns.count, U));
   static LdsLimit limit;
   if (most > 65536) LQ_TRY(limit.raise(reinterpret_cast<const void*>(fp8_rows_kernel<NC, RT, U, TILED, RAWS, T>), most));
   hipLaunchKernelGGL((fp8_rows_kernel<NC, RT, U, TILED, RAWS, T>), dim3((unsigned)(a.row_groups * a.splits)), dim3(64 * R_WAVES), bytes, st, a);
@@ -289,12 +300,17 @@ static int launch(const RowsArgs& a, hipStream_t st) {
   LQ_HIP_TRY(hipGetLastError());
   return LQ_OK;
 }
+// Up to 16 columns.  Half as many columns in registers leave room for half as many wavefronts again: one row, 11008 x 4096, bf16 10.1 and
+// 11.6 us.
+template <int RT, int U, bool TILED>
+static int launch_one(const RowsArgs& a, int dtype, hipStream_t st) {
+  if (!a.x) return launch<1, RT, U, TILED, 0, void>(a, st);
+  if (a.columns.count <= 4) return dtype == LQ_T_BF16 ? launch<1, RT, U, TILED, 4, __bf16>(a, st) : launch<1, RT, U, TILED, 4, float>(a, st);
+  return dtype == LQ_T_BF16 ? launch<1, RT, U, TILED, RAW_MOST, __bf16>(a, st) : launch<1, RT, U, TILED, RAW_MOST, float>(a, st);
+}
 template <bool TILED>
 static int launch_shape(const RowsArgs& a, int nc, int rt, int dtype, hipStream_t st) {
-  // half as many columns in registers leave room for half as many wavefronts again: one row, 11008 x 4096, bf16 10.5 and 11.6 us
-  if (a.x && a.columns.count <= 4) return dtype == LQ_T_BF16 ? launch<1, 1, 8, TILED, 4, __bf16>(a, st) : launch<1, 1, 8, TILED, 4, float>(a, st);
-  if (a.x) return dtype == LQ_T_BF16 ? launch<1, 1, 8, TILED, RAW_MOST, __bf16>(a, st) : launch<1, 1, 8, TILED, RAW_MOST, float>(a, st);
-  if (nc == 1) return launch<1, 1, 8, TILED, 0, void>(a, st);
+  if (nc == 1) return rt == 4 ? launch_one<4, 2, TILED>(a, dtype, st) : rt == 2 ? launch_one<2, 4, TILED>(a, dtype, st) : launch_one<1, 8, TILED>(a, dtype, st);
   if (nc == 2) return rt == 2 ? launch<2, 2, 4, TILED, 0, void>(a, st) : launch<2, 1, 4, TILED, 0, void>(a, st);
   if (nc == 4) return rt == 2 ? launch<4, 2, 2, TILED, 0, void>(a, st) : launch<4, 1, 4, TILED, 0, void>(a, st);
   return rt == 2 ? launch<8, 2, 2, TILED, 0, void>(a, st) : launch<8, 1, 2, TILED, 0, void>(a, st);
@@ -310,7 +326,7 @@ static int launch_rows(const Fp8Product& p, const void* x, int64_t ldx, int dtyp
 }
 
 int launch_fp8_product(const Fp8Product& p, float* part, size_t part_floats, hipStream_t st) {
-  if (p.columns.count > FEW_COLUMNS) return launch_fp8_tiles(p, part, part_floats, st);
+  if (!few_columns(p.columns.count, p.k)) return launch_fp8_tiles(p, part, part_floats, st);
   return launch_rows(p, nullptr, 0, 0, part, part_floats, st);
 }
 int launch_fp8_product_raw(const Fp8Product& p, const void* x, int64_t ldx, int dtype, float* part, size_t part_floats, hipStream_t st) {

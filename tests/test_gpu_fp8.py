@@ -90,7 +90,8 @@ def _close(got, a, b):
 
 
 SIZES = [(1, 1, 1), (1, 1000, 4096), (3, 17, 5), (16, 16, 128), (17, 100, 129), (50, 4096, 1024), (37, 768, 768), (129, 257, 300),
-         (300, 520, 1111), (1000, 700, 2055), (513, 1025, 640)]
+         (300, 520, 1111), (1000, 700, 2055), (513, 1025, 640), (3, 8200, 1500), (9, 16500, 700), (60, 8195, 260), (100, 9000, 384),
+         (2, 40, 20000), (50, 33, 9999), (129, 130, 5000)]
 
 
 @pytest.mark.parametrize("a_tiles,b_tiles", [(False, True), (False, False), (True, False), (True, True)])
@@ -125,7 +126,7 @@ def test_bytes_past_a_row_do_not_count(m):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("m,n,k", [(1, 300, 1000), (5, 17, 130), (16, 1024, 512), (37, 768, 768), (130, 515, 259), (700, 900, 1030)])
+@pytest.mark.parametrize("m,n,k", [(1, 300, 1000), (5, 17, 130), (8, 16400, 900), (4, 9000, 1999), (8, 70, 9000), (2, 33000, 300), (16, 1024, 512), (37, 768, 768), (130, 515, 259), (700, 900, 1030)])
 def test_layer_and_gradients(dtype, m, n, k):
     x, dy = _matrix(m, k, dtype, 3), _matrix(m, n, dtype, 4) * 1e-3
     w, s, wt, ts = lq.fp8_quantize(_matrix(n, k, torch.float32, 5, 0.0).cuda() * 0.02, tiles=True, both=True)
