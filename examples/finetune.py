@@ -8,9 +8,13 @@ the cross entropy of the target token over the vocabulary is what falls.  Target
     loss, dX over the vocabulary                            lq.cross_entropy
     dX, dL1, dL2, twice                                     lq.adapter_backward
 
-with a mask of its own for every step and place: the seed names the step, the offset the place.  Workspaces are made once.
+with a mask of its own for every step and place: the seed names the step, the offset the place.  Workspaces are made once.  The update is
+written out in torch, or with --bits 32 or 8 (of the optimizer's states) it is
 
-    python examples/finetune.py --steps 60 --dtype bf16
+    norm of all gradients, factor that clips them           lq.grad_norm
+    the update of all factors                               lq.AdamW
+
+    python examples/finetune.py --steps 60 --dtype bf16 --bits 8
 """
 import argparse
 import os
@@ -37,6 +41,17 @@ class Adam:
             p.addcdiv_(m, size, value=-self.lr / (1 - 0.9 ** self.step_count))
 
 
+class ClippedAdamW:
+    """The library's step over all factors at once, gradients clipped to a norm of 1."""
+
+    def __init__(self, params, lr, bits):
+        self.adamw, self.lr = lq.AdamW(params, bits=bits), lr
+
+    def step(self, grads):
+        _, coef = lq.grad_norm(grads, 1.0)
+        self.adamw.step(grads, self.lr, betas=(0.9, 0.99), weight_decay=0.0, coef=coef)
+
+
 class Layer:
     """A decomposed d x k matrix, its adapter and what its calls need."""
 
@@ -59,8 +74,8 @@ class Layer:
 
 
 def finetune(steps=60, dtype=torch.float32, rows=200, width=256, hidden=512, vocab=1000, rank=16, p=0.05, lr=4e-3, seed=0,
-             device="cuda"):
-    """-> the loss of every step."""
+             device="cuda", bits=None):
+    """-> the loss of every step.  bits: None, or those of lq.AdamW's states."""
     gen = torch.Generator().manual_seed(seed)
 
     def normal(*shape, std):
@@ -74,7 +89,8 @@ def finetune(steps=60, dtype=torch.float32, rows=200, width=256, hidden=512, voc
     tokens = torch.randperm(vocab, generator=gen)[:rows].to(device)
     targets = torch.randperm(vocab, generator=gen).to(device)[tokens]
     loss_ws = lq.cross_entropy_workspace(rows, width, vocab, dtype)
-    adam = Adam([w for layer in layers for w in (layer.l1, layer.l2)], lr)
+    factors = [w for layer in layers for w in (layer.l1, layer.l2)]
+    adam = Adam(factors, lr) if bits is None else ClippedAdamW(factors, lr, bits)
     losses = []
     for step in range(steps):
         x = lq.dropout(embedding[tokens], p, seed=step)
@@ -92,8 +108,9 @@ def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--steps", type=int, default=60)
     ap.add_argument("--dtype", choices=("fp32", "bf16"), default="fp32")
+    ap.add_argument("--bits", type=int, choices=(8, 32), default=None)
     a = ap.parse_args()
-    losses = finetune(a.steps, torch.bfloat16 if a.dtype == "bf16" else torch.float32)
+    losses = finetune(a.steps, torch.bfloat16 if a.dtype == "bf16" else torch.float32, bits=a.bits)
     for i in range(0, len(losses), 10):
         print(f"step {i:4d}  loss {losses[i]:.4f}")
     print(f"step {len(losses) - 1:4d}  loss {losses[-1]:.4f}")

@@ -386,8 +386,8 @@ int lq_adapter_backward(const void* dY, const void* X, int64_t m, int64_t d, int
  * Arithmetic (fixed, so that codes are reproducible bit for bit): with amax the block's largest magnitude,
  * scale = max(fl32(amax / 448), 2^-126), code = e4m3(fl32(x fl32(1 / scale))), nearest, ties to even.  A block that holds an inf or a NaN
  * has scale NaN, and so has every sum that it enters.
- * Products add up a block of 128 in the matrix unit, whose sums are good to about 2^-16 of a block's largest term, and the blocks in
- * fp32; results are bf16, since more bits would hold that error.  They are right where they are below 2^96; where a scale times another
+ * Products add up a block of 128 in the matrix unit, whose sums are off by up to 2^-12 of the sum of the terms' magnitudes where codes of
+ * all sizes meet (2^-16 for normally distributed values), and the blocks in fp32; results are bf16, since more bits would hold that error.  They are right where they are below 2^96; where a scale times another
  * is below 2^-156 they may be 0.  All calls only enqueue kernels on `stream` and are deterministic.
  */
 
@@ -399,7 +399,8 @@ int lq_adapter_backward(const void* dY, const void* X, int64_t m, int64_t d, int
  *   scale_t  tiles == 0: X^T's own rows, of row j and block b at scale_t[b * d + j]; tiles == 1: NULL (scale serves it with its indices
  *            exchanged)
  * At least one of codes and codes_t.  scale is needed with codes, and with tiles; scale_t with codes_t in rows.  codes, codes_t on 16-byte
- * addresses, ld_codes >= d and ld_codes_t >= m multiples of 16 (LQ_ERR_ARG; LQ_ERR_SHAPE if smaller).  m, d up to 2^30, ldx below 2^40.
+ * addresses, ld_codes >= d and ld_codes_t >= m multiples of 16 (LQ_ERR_ARG; LQ_ERR_SHAPE if smaller).  m, d up to 2^30,
+ * fewer than 2^23 tiles of 128 x 128, ldx up to 2^40 (LQ_ERR_SHAPE).
  */
 int lq_fp8_quantize(const void* X, int64_t m, int64_t d, int64_t ldx, int dtype, int tiles, uint8_t* codes, int64_t ld_codes, float* scale,
                     uint8_t* codes_t, int64_t ld_codes_t, float* scale_t, void* stream);
@@ -418,7 +419,7 @@ typedef struct {
 /*
  * Y = A B^T with A m x k and B n x k in 8 bits, along k in blocks of 128.  Y m x n bf16, rows ldy elements apart.
  *   workspace  lq_fp8_matmul_workspace_bytes(m, n, k) bytes (0: may be NULL)
- * m, n up to 2^30, k up to 2^22, ld up to 2^22 (LQ_ERR_SHAPE).
+ * m, n up to 2^27, k up to 2^22, ld up to 2^22 (LQ_ERR_SHAPE).
  */
 size_t lq_fp8_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
 int lq_fp8_matmul(const lq_fp8_matrix* A, const lq_fp8_matrix* B, int64_t m, int64_t n, int64_t k, void* Y, int64_t ldy, void* workspace,
@@ -430,7 +431,7 @@ int lq_fp8_matmul(const lq_fp8_matrix* A, const lq_fp8_matrix* B, int64_t m, int
  * with X and dY quantized in rows inside the calls: along k for Y, along n for dX, along m (both) for dW.
  *   X m x k, dY m x n: of types x_dtype and dy_dtype, rows ldx and ldy elements apart        W n x k, Wt (W^T) k x n: in 8 bits
  *   Y m x n, dX m x k, dW n x k: bf16, contiguous.  dX or dW may be NULL: not wanted (with dX Wt is needed, with dW X)
- *   m up to 2^22 in the backward call, which sums over it
+ *   m, n, k up to 2^27, what a product sums over (forward k, dX n, dW m) up to 2^22 (LQ_ERR_SHAPE)
  */
 size_t lq_fp8_forward_workspace_bytes(int64_t m, int64_t n, int64_t k);
 int lq_fp8_forward(const void* X, int64_t ldx, int x_dtype, const lq_fp8_matrix* W, int64_t m, int64_t n, int64_t k, void* Y, void* workspace,
@@ -494,7 +495,8 @@ typedef struct {
  * average (to the nearest code it would stand still wherever a step changes it by less than half a code's distance); x > 0 becomes the least
  * value at least.  u are the 16 bits that lq_dropout's generator gives for the tensor's element with the key `seed` and offset
  * (step mod 2^32) + 2^32 (the tensor's index in the call).
- *   coef   device, one fp32 that multiplies every gradient (lq_grad_norm's norm + 1), or NULL.  Where it is not finite, nothing is changed.
+ *   coef   device, one fp32 that multiplies every gradient (lq_grad_norm's norm + 1), or NULL.  Where it or *lr_device is not finite, or
+ *          *step_device is below 1, nothing is changed.
  * Refused (LQ_ERR_ARG): beta outside [0, 1), eps < 0, values that are not finite, step < 1, count over 2^24, state_bits neither 8 nor 32,
  * memory that is written and belongs to two tensors or is read as a gradient, coef, lr or step as well.  n of a tensor may be 0, then its pointers are not looked at.
  */

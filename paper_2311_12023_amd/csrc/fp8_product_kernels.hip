@@ -32,6 +32,10 @@ __device__ __forceinline__ uintx2 product_result(floatx4 v) {
   return __builtin_bit_cast(uintx2, bf16x4{(__bf16)(v[0] * FP8_DROP), (__bf16)(v[1] * FP8_DROP), (__bf16)(v[2] * FP8_DROP), (__bf16)(v[3] * FP8_DROP)});
 }
 
+// 4096 columns x 11008 rows: depth 4096 161 us, 2.29 PFLOP/s, depth 11008 404 us, 2.46; rows with scales of their own 193 us, 1.92.  The
+// chip's power is the limit: the clock is 2.1 GHz and the matrix units are busy for half of its cycles, waits and barriers taken out change
+// nothing, transfers or sums taken out 17 % and 11 %.
+//
 // A workgroup of eight wavefronts makes a tile, a wavefront 128 x 64 of it (2 x 4) in blocks of 16 x 16.  A block of 128 along k is one
 // matrix instruction, whose four sums a lane are multiplied by the two scales into the accumulators; what it takes is two vector
 // instructions for four sums where the rows' scales are of tiles (one scale for the wavefront's 128 rows), else three.
@@ -290,7 +294,8 @@ __global__ __launch_bounds__(P_THREADS) void fp8_join_kernel(ProductArgs a) {
 }
 
 static int64_t product_tiles(int64_t rows, int64_t columns) { return ((rows + PT - 1) / PT) * ((columns + PT - 1) / PT); }
-// Ranges that the sum is cut into where there are few tiles: they fill the chip, each keeps four blocks.
+// Ranges that the sum is cut into where there are few tiles: they fill the chip, each keeps four blocks (1024 x 1000, depth 50265: 16
+// tiles in 16 ranges 56 us, their join 11; with the ranges of a tile next to one another, which then share nothing in an L2, 75 us).
 static int product_splits(int64_t rows, int64_t columns, int64_t k) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(256 / std::max<int64_t>(1, product_tiles(rows, columns)), fp8_blocks(k) / 4));
 }

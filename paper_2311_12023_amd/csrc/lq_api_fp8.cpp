@@ -6,7 +6,8 @@ namespace lq {
 static bool bad_type(int dtype) { return dtype != LQ_T_FP32 && dtype != LQ_T_BF16; }
 static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
-constexpr int64_t MOST_ROWS = (int64_t)1 << 30, MOST_DEPTH = (int64_t)1 << 22, MOST_LD = (int64_t)1 << 40;
+// A launch has fewer than 2^32 threads, 16 for a row of few rows' products.
+constexpr int64_t MOST_ROWS = (int64_t)1 << 27, MOST_SIDE = (int64_t)1 << 30, MOST_DEPTH = (int64_t)1 << 22, MOST_LD = (int64_t)1 << 40;
 static bool bad_rows(int64_t n) { return n <= 0 || n > MOST_ROWS; }
 static bool bad_depth(int64_t n) { return n <= 0 || n > MOST_DEPTH; }
 
@@ -77,7 +78,7 @@ int lq_fp8_quantize(const void* X, int64_t m, int64_t d, int64_t ldx, int dtype,
   if (!X || (!codes && !codes_t)) return LQ_ERR_NULL;
   if ((codes || tiles == 1) && !scale) return LQ_ERR_NULL;
   if (codes_t && tiles == 0 && !scale_t) return LQ_ERR_NULL;
-  if (bad_rows(m) || bad_rows(d) || ldx < d || ldx > MOST_LD) return LQ_ERR_SHAPE;
+  if (m <= 0 || d <= 0 || m > MOST_SIDE || d > MOST_SIDE || ldx < d || ldx > MOST_LD) return LQ_ERR_SHAPE;
   if ((codes && (ld_codes < d || ld_codes > MOST_LD)) || (codes_t && (ld_codes_t < m || ld_codes_t > MOST_LD))) return LQ_ERR_SHAPE;
   if (bad_type(dtype) || (tiles != 0 && tiles != 1) || misaligned(X, type_bytes(dtype))) return LQ_ERR_ARG;
   if ((codes && (misaligned(codes, 16) || ld_codes % 16)) || (codes_t && (misaligned(codes_t, 16) || ld_codes_t % 16))) return LQ_ERR_ARG;

@@ -579,6 +579,7 @@ def fp8_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale:
         out = torch.empty((m, n), dtype=torch.bfloat16, device=a.device)
     _shaped(out, (m, n), "out")
     yp, ldy = _rows(out, torch.bfloat16, "out")
+    _here(out, workspace)
     ws = workspace if workspace is not None else _workspace(_lib.lq_fp8_matmul_workspace_bytes(m, n, k), a.device)
     _check(_lib.lq_fp8_matmul(C.byref(am), C.byref(bm), m, n, k, yp, ldy, *_space(ws), _stream()), "lq_fp8_matmul")
     return out
@@ -595,7 +596,7 @@ def fp8_forward(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, workspa
     code = _dtype(x, "x")
     xp, ldx = _rows(x, x.dtype, "x")
     wm = _fp8_matrix(w, w_scale, "w")
-    _here(x)
+    _here(x, workspace)
     (m, k), n = x.shape, w.shape[0]
     _shaped(w, (n, k), "w")
     ws = workspace if workspace is not None else fp8_workspace(m, n, k, device=x.device)
@@ -665,6 +666,7 @@ def grad_norm(grads, max_norm: float = float("inf"), workspace: torch.Tensor | N
         out = torch.empty(64 + need // 4, dtype=torch.float32, device=device)
         space = (out.data_ptr() + 256, need)
     else:
+        _here(workspace)
         out, space = torch.empty(2, dtype=torch.float32, device=device), _space(workspace)
     _check(_lib.lq_grad_norm(table, len(grads), max_norm, out.data_ptr(), *space, _stream()), "lq_grad_norm")
     return out[0], out[1]
@@ -746,16 +748,25 @@ class AdamW:
         else:
             h.lr = lr
         for name, one in (("lr", lr), ("coef", coef)):
-            if isinstance(one, torch.Tensor) and one.numel() != 1:
-                raise ValueError(f"{name}: need one element")
+            if isinstance(one, torch.Tensor):
+                if one.numel() != 1:
+                    raise ValueError(f"{name}: need one element")
+                _here(one)
+        scale = _dev(coef, torch.float32, "coef")
         if on_device:
             self.t += 1
             h.step_device = self.t.data_ptr()
         else:
             h.step = self.t + 1
-        _check(_lib.lq_adamw(C.addressof(self._table), len(grads), self.bits, C.byref(h), _dev(coef, torch.float32, "coef"), _stream()), "lq_adamw")
+        status = _lib.lq_adamw(C.addressof(self._table), len(grads), self.bits, C.byref(h), scale, _stream())
+        if status != 0 and on_device:
+            self.t -= 1                                      # a refused step does not count
+        _check(status, "lq_adamw")
         if not on_device:
             self.t += 1
+        tracked = [x for x in self._held if x.requires_grad]
+        if tracked:                                          # a graph that still needs the old values has to say so
+            torch.autograd.graph.increment_version(tracked)
 
 
 def assign_configs(err: np.ndarray, storage: np.ndarray, budget_bits: float, node_limit: int = 0):

@@ -264,3 +264,73 @@ def test_large_tensor():
                              HYPER["betas"], HYPER["eps"], HYPER["weight_decay"])
     assert torch.equal(p[-3000:].cpu(), wp.bfloat16()) and not p[:-3000].any()
     assert torch.equal(lq.grad_norm([g])[0].cpu(), tail.double().square().sum().sqrt().float())
+
+
+def test_what_is_refused_on_the_gpu():
+    p = _values(100, 1).cuda()
+    opt = lq.AdamW([p], device_step=True)
+    g = _values(100, 2).cuda()
+    for call in (lambda: opt.step([g[:50]], 0.1), lambda: opt.step([g, g], 0.1), lambda: opt.step([g], 0.1, coef=torch.ones(2, device="cuda")),
+                 lambda: lq.AdamW([p], copies=[]), lambda: lq.AdamW([p], copies=[p[:50].bfloat16()])):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: opt.step([g.half()], 0.1), lambda: opt.step([g.cpu()], 0.1), lambda: opt.step([_values(200, 1).cuda()[::2]], 0.1),
+                 lambda: lq.AdamW([p[::2]]), lambda: lq.AdamW([p], copies=[p]), lambda: opt.step([g], torch.ones((), dtype=torch.float64, device="cuda"))):
+        with pytest.raises(TypeError):
+            call()
+    before = p.clone()
+    for call in (lambda: opt.step([g], float("nan")), lambda: opt.step([g], 0.1, betas=(1.0, 0.9)), lambda: opt.step([p], 0.1),
+                 lambda: lq.AdamW([p, p]).step([g, g], 0.1), lambda: lq.AdamW([p[:60], p[50:]]).step([g[:60], g[:50]], 0.1)):
+        with pytest.raises(lq.LqError):
+            call()
+    assert opt.t.item() == 0 and torch.equal(p, before)
+
+
+def test_values_on_the_device_that_make_no_step():
+    p, g = _values(3000, 1).cuda(), _values(3000, 2).cuda()
+    opt = lq.AdamW([p], bits=8, device_step=True)
+    opt.step([g], 0.01)
+    before = [x.clone() for x in (p, *opt.buffers.values())]
+    opt.step([g], torch.tensor(float("nan"), device="cuda"))
+    opt.t.fill_(-1)
+    opt.step([g], 0.01)
+    for a, b in zip(before, (p, *opt.buffers.values())):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_a_graph_that_needs_the_old_parameters_fails():
+    p = torch.nn.Parameter(_values(64, 1).cuda())
+    opt = lq.AdamW([p])
+    loss = (p * p).sum()
+    opt.step([_values(64, 2).cuda()], 0.1)
+    with pytest.raises(RuntimeError):
+        loss.backward()
+
+
+def test_parameters_that_move():
+    """p.data set to other memory between steps: the step goes where the parameter is now."""
+    p = torch.nn.Parameter(_values(500, 1).cuda())
+    opt, again = lq.AdamW([p]), _values(500, 1).cuda()
+    ref = lq.AdamW([again])
+    for t in range(3):
+        g = _values(500, 5 + t).cuda()
+        old = p.data
+        p.data = p.data.clone()
+        kept = old.clone()
+        opt.step([g], 0.01)
+        ref.step([g], 0.01)
+        assert torch.equal(old, kept) and torch.equal(p.data, again)
+
+
+def test_another_stream():
+    p, again = _values(100000, 1).cuda(), _values(100000, 1).cuda()
+    a, b, g = lq.AdamW([p], bits=8), lq.AdamW([again], bits=8), _values(100000, 2).cuda()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            a.step([g], 0.01, coef=lq.grad_norm([g], 1.0)[1])
+    torch.cuda.current_stream().wait_stream(side)
+    for _ in range(3):
+        b.step([g], 0.01, coef=lq.grad_norm([g], 1.0)[1])
+    assert torch.equal(p, again)

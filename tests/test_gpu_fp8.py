@@ -207,3 +207,60 @@ def test_graph_and_streams():
     torch.cuda.current_stream().wait_stream(side)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(other, want))
+
+
+def test_scales_that_are_expanded_and_mixed_types():
+    """One scale for a whole matrix is a tensor expanded to the blocks; X and dY of different types."""
+    m, n, k = 70, 150, 260
+    a = _matrix(m, k, torch.float32, 1, 0.0)
+    one = (a.abs().max() / 448).reshape(1, 1).cuda()
+    codes = torch.zeros(m, 272, device="cuda").to(R.FP8)[:, :k]
+    codes.copy_((a.cuda() / one).to(R.FP8))
+    w, s, wt, ts = lq.fp8_quantize(_matrix(n, k, torch.float32, 2).cuda(), tiles=True, both=True)
+    for rows in (m, 3):
+        y = lq.fp8_matmul(codes[:rows], one.expand(rows, 3), w, s)
+        _close(y, R.values(codes[:rows].cpu(), one.expand(rows, 3).cpu()), R.values(w.cpu(), s.cpu()))
+    x, dy = _matrix(m, k, torch.float32, 3), _matrix(m, n, torch.bfloat16, 4)
+    dx, dw = lq.fp8_backward(dy.cuda(), x.cuda(), wt, ts)
+    _close(dx, R.values(*R.quantize(dy)), R.values(wt.cpu(), ts.cpu()))
+    _close(dw, R.values(*R.quantize(dy.t().contiguous())), R.values(*R.quantize(x.t().contiguous())))
+
+
+@pytest.mark.parametrize("m", [1, 12, 300])
+@pytest.mark.parametrize("x_size,w_size", [(1e-34, 1.0), (1e-20, 1e-13), (1e25, 1e-25), (3e30, 1e-8)])
+def test_sizes_far_from_one(m, x_size, w_size):
+    x, w = _matrix(m, 300, torch.float32, 1, 0.0) * x_size, _matrix(270, 300, torch.float32, 2, 0.0) * w_size
+    wq, s = lq.fp8_quantize(w.cuda(), tiles=True)
+    _close(lq.fp8_forward(x.cuda(), wq, s), R.values(*R.quantize(x)), R.values(wq.cpu(), s.cpu()))
+
+
+def test_more_values_than_32_bits_count():
+    """A matrix of over 2^31 values: its last rows and columns, both ways."""
+    m, d = 66000, 33000
+    x = torch.zeros((m, d), dtype=torch.bfloat16, device="cuda")
+    x[-40:, -300:] = _matrix(40, 300, torch.bfloat16, 1).cuda()
+    q, s, qt, st = lq.fp8_quantize(x, both=True)
+    corner = torch.zeros(m % 128 + 128, d % 128 + 384)
+    corner[-40:, -300:] = x[-40:, -300:].cpu().float()
+    rows, cols = corner.shape
+    for got, scale, part in ((q, s, corner), (qt, st, corner.t().contiguous())):
+        want, want_s = R.quantize(part)
+        _same(got[-part.shape[0]:, -part.shape[1]:], want)
+        _same(scale[-part.shape[0]:, -want_s.shape[1]:], want_s)
+
+
+def test_refusals_on_the_gpu():
+    w, s = lq.fp8_quantize(torch.ones(64, 100, device="cuda"), tiles=True)
+    x = torch.ones(4, 100, device="cuda")
+    for call in (lambda: lq.fp8_forward(x[:, :90], w, s), lambda: lq.fp8_forward(x, w, s[:, :0]), lambda: lq.fp8_matmul(w, s, w[:, 1:], s),
+                 lambda: lq.fp8_matmul(w, s, w.t(), s), lambda: lq.fp8_backward(x, None), lambda: lq.fp8_backward(x, x, want_dx=False, want_dw=False),
+                 lambda: lq.fp8_backward(x, x[:2], want_dx=False), lambda: lq.fp8_matmul(w, s, w, s, out=torch.empty(64, 65, dtype=torch.bfloat16, device="cuda"))):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: lq.fp8_quantize(x.half()), lambda: lq.fp8_quantize(x[0]), lambda: lq.fp8_quantize(x[:1].expand(4, 100)),
+                 lambda: lq.fp8_forward(x, w.view(torch.uint8), s), lambda: lq.fp8_forward(x, w, s.half()),
+                 lambda: lq.fp8_backward(x, x.half(), want_dx=False), lambda: lq.fp8_forward(x, w, s, workspace=torch.empty(10, device="cuda"))):
+        with pytest.raises(TypeError):
+            call()
+    with pytest.raises(lq.LqError):
+        lq.fp8_quantize(x[:0])

@@ -1,0 +1,114 @@
+"""The 8-bit layer, the norm and the optimizer's step as a training loop uses them, a decomposed layer served in 8 bits, and the example."""
+import os
+
+import pytest
+import torch
+
+import fp8_reference as R
+from paper_2311_12023_amd import lq
+
+pytestmark = pytest.mark.gpu
+
+M, N, K = 300, 200, 390
+STEP = dict(betas=(0.9, 0.99), eps=1e-8, weight_decay=0.01)
+
+
+class Trained:
+    """A layer whose weights are kept in fp32, multiplied in 8 bits and updated from bf16 gradients."""
+
+    def __init__(self, bits, device_step=False):
+        g = torch.Generator().manual_seed(3)
+        self.w = (torch.randn(N, K, generator=g) * 0.05).cuda()
+        self.held = self.w.bfloat16()
+        self.x = torch.randn(M, K, generator=g).bfloat16().cuda()
+        self.goal = torch.randn(M, N, generator=g).bfloat16().cuda()
+        self.lr = torch.tensor(1e-2, device="cuda")
+        self.opt = lq.AdamW([self.w], bits=bits, copies=[self.held], seed=11, device_step=device_step)
+        self.ws = lq.fp8_workspace(M, N, K), lq.fp8_workspace(M, N, K, backward=True)
+
+    def step(self):
+        w, s, wt, ts = lq.fp8_quantize(self.held, tiles=True, both=True)
+        y = lq.fp8_forward(self.x, w, s, workspace=self.ws[0])
+        dy = (y - self.goal) * (1.0 / M)
+        dx, dw = lq.fp8_backward(dy, self.x, wt, ts, workspace=self.ws[1])
+        norm, coef = lq.grad_norm([dw], 1.0)
+        self.opt.step([dw], self.lr, coef=coef, **STEP)
+        return y, dy, dx, dw, norm, coef
+
+
+def _near(got, a, b):
+    """A product in 8 bits: bf16's half step of the result and 2^-12 of the magnitudes' sum."""
+    want, size = a @ b.t(), a.abs() @ b.abs().t()
+    half = torch.finfo(torch.bfloat16).eps / 2
+    assert ((got.double().cpu() - want).abs() <= half * want.abs() + (1 + half) * 2.0 ** -12 * size).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_steps_of_a_layer(bits):
+    layer = Trained(bits)
+    for t in (1, 2, 3):
+        held, p = layer.held.cpu(), layer.w.double().cpu()
+        m, v = (layer.opt.buffers[k] for k in ("m", "v"))
+        if bits == 8:
+            m = R.state_values(m, layer.opt.buffers["m_scale"], m.numel())
+            v = R.f32(R.state_values(v, layer.opt.buffers["v_scale"], v.numel()).square())
+        m, v = (x.double().cpu()[:N * K].reshape(N, K) for x in (m, v))
+        y, dy, dx, dw, norm, coef = layer.step()
+        w = R.values(*R.quantize(held, True))
+        rows = lambda x: R.values(*R.quantize(x.cpu().contiguous()))  # noqa: E731
+        _near(y, rows(layer.x), w)
+        _near(dx, rows(dy), w.t().contiguous())
+        _near(dw, rows(dy.t()), rows(layer.x.t()))
+        assert abs(norm.item() - dw.double().norm().item()) <= 2.0 ** -23 * norm.item()
+        want, _, _, _ = R.adamw(p, dw.cpu(), m, v, t, float(layer.lr), STEP["betas"], STEP["eps"], STEP["weight_decay"], float(coef))
+        # lr is fl(0.01) on the device: its factors are rounded from there, 2^-24 of a step of lr / (1 - 0.9) at most
+        assert (layer.w.double().cpu() - want).abs().max() <= 2.0 ** -23 * (0.1 + want.abs().max())
+        assert torch.equal(layer.held, layer.w.bfloat16())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_captured_loop_is_the_eager_one(bits):
+    a, b = Trained(bits, device_step=True), Trained(bits, device_step=True)
+    a.step(), b.step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = a.step()
+    for _ in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        want = b.step()
+        assert all(torch.equal(x, y) for x, y in zip(out, want))
+        assert torch.equal(a.w, b.w) and torch.equal(a.held, b.held)
+        for x, y in zip(a.opt.buffers.values(), b.opt.buffers.values()):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+@pytest.mark.parametrize("rows", [1, 40, 200])
+def test_a_decomposed_layer_served_in_8_bits(rows):
+    """W = Q + L1 L2 multiplied out once and laid out in tiles: the product is within the roundings of lq.matmul's.  Each code is off by
+    half a step, 2^-4 of its value or 2^-10 of its scale (448 of which are the block's largest), which leaves (1 + 2^-4)^2 - 1 of the
+    magnitudes, and the smallest codes' part."""
+    d, k, rank, cfg = 256, 384, 8, lq.config(4, 32, 64)
+    g = torch.Generator().manual_seed(2)
+    dec = lq.decompose((torch.randn(d, k, generator=g) / 16).cuda(), rank, cfg, 2)
+    x = torch.randn(rows, d, generator=g).cuda()
+    args = (dec["codes"], dec["scale_idx"], dec["v"], cfg, k, dec["L1"], dec["L2"])
+    whole = lq.matmul(torch.eye(d, device="cuda"), *args)
+    _, _, w, s = lq.fp8_quantize(whole, tiles=True, both=True)
+    y = lq.fp8_forward(x, w, s)
+    want, size = lq.matmul(x, *args).double(), x.abs().double() @ whole.abs().double()
+    small = 2.0 ** -10 / 448 * d * x.abs().max().double() * whole.abs().max().double()
+    share = (1 + 2.0 ** -4) ** 2 - 1 + 2.0 ** -12 + 2.0 ** -13
+    assert ((y.double() - want).abs() <= share * size + 2.0 ** -8 * want.abs() + 2 * small).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_the_example_with_the_librarys_step(bits):
+    import importlib.util
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "finetune.py")
+    spec = importlib.util.spec_from_file_location("finetune", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    first, again = example.finetune(steps=4, bits=bits), example.finetune(steps=4, bits=bits)
+    assert first == again and len(first) == 4 and all(x == x for x in first)
+    assert first[0] == example.finetune(steps=1)[0]           # the step comes after the first loss
