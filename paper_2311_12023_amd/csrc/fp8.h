@@ -34,8 +34,9 @@ struct Fp8Product {
 };
 int launch_fp8_product(const Fp8Product& p, float* part, size_t part_floats, hipStream_t st);
 // For few columns (fp8_quantizes_columns) with the columns' operand as it is before its quantization: row i of x is column i;
-// p.columns holds their count.
-bool fp8_quantizes_columns(int64_t columns);
+// p.columns holds their count.  fp8_needs_codes: whether there are operands of so many columns that this does not serve.
+bool fp8_needs_codes(int64_t columns);
+bool fp8_quantizes_columns(const Fp8Product& p);
 int launch_fp8_product_raw(const Fp8Product& p, const void* x, int64_t ldx, int dtype, float* part, size_t part_floats, hipStream_t st);
 // For many columns (fp8_product_kernels.hip).
 int launch_fp8_tiles(const Fp8Product& p, float* part, size_t part_floats, hipStream_t st);

@@ -11,8 +11,8 @@ namespace lq {
 // 32000 x 1024, 128 30 and 36, 768 x 3000, 128 20 and 19, 11008 x 4096, 128 46 and 34.
 static bool few_columns(int64_t columns, int64_t k) { return columns <= 64 || (columns <= 128 && k <= 3000); }
 constexpr int R_WAVES = 4;
-// Columns that are quantized where they are used, us for 8 rows so and in a launch before: bf16 768 x 768 8.7 and 8.6, 4096 x 4096 13.8 and
-// 14.7, 11008 x 4096 14.9 and 17.1; fp32 8.5 and 8.7, 15.9 and 14.9, 16.4 and 17.3.  One row 4.8 and 7.3, 9.3 and 13.1, 10.5 and 14.5.
+// Columns that are quantized where they are used, us for 8 rows so and in a launch before: bf16 768 x 768 3.3 and 7.3, 4096 x 4096 7.8 and
+// 12.5, 11008 x 4096 14.6 and 17.2, 1024 x 50265 26.1 and 25.6; one row 2.9 and 7.3, 5.7 and 9.6, 10.1 and 14.5, 16.1 and 23.3.
 constexpr int RAW_MOST = 8;
 
 struct RowsArgs {
@@ -126,7 +126,7 @@ __device__ __forceinline__ void rows_store(const RowsArgs& a, floatx4 v, int64_t
 template <int NC, int RT, int U, bool TILED, int RAWS, typename T>
 __global__ __launch_bounds__(64 * R_WAVES) void fp8_rows_kernel(RowsArgs a) {
   constexpr bool RAW = !std::is_void<T>::value;
-  static_assert(!RAW || (NC == 1 && U <= 8 && RAWS <= RAW_MOST && RAWS % (8 / U) == 0), "a step's layout");
+  static_assert(!RAW || (RAWS <= 16 * NC && U <= 8 && RAWS % (8 / U) == 0), "a step's layout");
   extern __shared__ __align__(16) unsigned char lds[];
   const int lane = threadIdx.x & 63, l16 = lane & 15, kg = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t group = blockIdx.x / a.splits;
@@ -173,17 +173,27 @@ __global__ __launch_bounds__(64 * R_WAVES) void fp8_rows_kernel(RowsArgs a) {
     };
     if constexpr (RAW) {
       const T* x = static_cast<const T*>(a.x);
-      constexpr int G = 8 / U, N = RAWS / G;         // columns at a time, times
+      constexpr int G = 8 / U, N = RAWS / G < 4 || RAWS <= RAW_MOST ? RAWS / G : 4;         // columns at a time, times
       const int at = 16 * (lane % (8 * U)), own = lane / (8 * U);
       RawColumn<T> raw[N];
-      // the columns' values are asked for before the weights, which they would otherwise wait for
+      auto ask = [&](int c0) __attribute__((always_inline)) {
 #pragma unroll
-      for (int c = 0; c < N; ++c)
-        if (G * c + own < columns) raw[c].load(x + (G * c + own) * a.ldx, (int64_t)b * 128 + at, a.k);
+        for (int c = 0; c < N; ++c)
+          if (c0 + G * c + own < columns) raw[c].load(x + (c0 + G * c + own) * a.ldx, (int64_t)b * 128 + at, a.k);
+      };
+      auto take = [&](int c0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < N; ++c)
+          if (c0 + G * c + own < columns) quantize_column<U>(raw[c], c0 + G * c + own, codes, scales, at);
+      };
+      ask(0);                                        // before the weights, which these values would otherwise wait for
       load_rows();
-#pragma unroll
-      for (int c = 0; c < N; ++c)
-        if (G * c + own < columns) quantize_column<U>(raw[c], G * c + own, codes, scales, at);
+      take(0);
+      if constexpr (RAWS > G * N)
+        for (int c0 = G * N; c0 < columns; c0 += G * N) {
+          ask(c0);
+          take(c0);
+        }
     } else {
       load_rows();
     }
@@ -206,11 +216,14 @@ __global__ __launch_bounds__(64 * R_WAVES) void fp8_rows_kernel(RowsArgs a) {
         const bool end = ragged && b + u == a.blocks - 1;
         intx8 y[NC];
         if constexpr (RAW) {
-          const int mine = min(l16, columns - 1);
-          const unsigned char* from = codes + mine * x_pitch(U) + 128 * u + 32 * kg;
-          const uintx4 lo = *reinterpret_cast<const uintx4*>(from), hi = *reinterpret_cast<const uintx4*>(from + 16);
-          y[0] = intx8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-          f[u][0] = scales[mine * U + u];
+#pragma unroll
+          for (int j = 0; j < NC; ++j) {
+            const int mine = min(16 * j + l16, columns - 1);
+            const unsigned char* from = codes + mine * x_pitch(U) + 128 * u + 32 * kg;
+            const uintx4 lo = *reinterpret_cast<const uintx4*>(from), hi = *reinterpret_cast<const uintx4*>(from + 16);
+            y[j] = intx8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+            f[u][j] = scales[mine * U + u];
+          }
         } else {
 #pragma unroll
           for (int j = 0; j < NC; ++j) y[j] = rows_load(column[j], at, last);
@@ -285,7 +298,16 @@ size_t fp8_product_part_floats(int64_t rows, int64_t columns, int64_t k) {
   const RowsShape s = rows_shape(rows, columns, k);
   return s.splits > 1 ? (size_t)s.groups * s.rt * s.nc * s.splits * 256 : 0;
 }
-bool fp8_quantizes_columns(int64_t columns) { return columns <= RAW_MOST; }
+bool fp8_needs_codes(int64_t columns) { return columns > RAW_MOST; }
+// More of them than RAW_MOST where the sum is short, us so and in two launches: 768 x 768, 9, 16, 32, 64 rows 3.6, 3.9, 5.7, 8.6 and 7.3, 7.5, 8.1,
+// 9.2; 4096 x 256, 16, 32, 64 rows 5.3, 8.3, 13.2 and 6.9, 7.2, 7.8 (fewer wavefronts have a part of the sum); 32000 x 1024, 16, 32, 64 rows
+// 9.1, 16.9, 24.9 and 13.3, 19.0, 20.0.
+bool fp8_quantizes_columns(const Fp8Product& p) {
+  const int64_t columns = p.columns.count, blocks = fp8_blocks(p.k);
+  if (columns <= RAW_MOST) return true;
+  if (!p.rows.shift || blocks > 2 * R_WAVES) return false;
+  return columns <= 16 || (columns <= 32 && blocks > 2) || (columns <= 64 && blocks > R_WAVES && p.rows.count < 32 * 256);
+}
 
 template <int NC, int RT, int U, bool TILED, int RAWS, typename T>
 static int launch(const RowsArgs& a, hipStream_t st) {
@@ -308,9 +330,28 @@ static int launch_one(const RowsArgs& a, int dtype, hipStream_t st) {
   if (a.columns.count <= 4) return dtype == LQ_T_BF16 ? launch<1, RT, U, TILED, 4, __bf16>(a, st) : launch<1, RT, U, TILED, 4, float>(a, st);
   return dtype == LQ_T_BF16 ? launch<1, RT, U, TILED, RAW_MOST, __bf16>(a, st) : launch<1, RT, U, TILED, RAW_MOST, float>(a, st);
 }
+// 9 to 64 columns quantized where they are used: short sums, of which a wavefront has two blocks at most.
+template <int NC, int RT>
+static int launch_short(const RowsArgs& a, int dtype, hipStream_t st) {
+  return dtype == LQ_T_BF16 ? launch<NC, RT, 2, true, 16 * NC, __bf16>(a, st) : launch<NC, RT, 2, true, 16 * NC, float>(a, st);
+}
 template <bool TILED>
 static int launch_shape(const RowsArgs& a, int nc, int rt, int dtype, hipStream_t st) {
-  if (nc == 1) return rt == 4 ? launch_one<4, 2, TILED>(a, dtype, st) : rt == 2 ? launch_one<2, 4, TILED>(a, dtype, st) : launch_one<1, 8, TILED>(a, dtype, st);
+  if (a.x && a.columns.count > RAW_MOST) {
+    if constexpr (TILED) {
+      if (nc == 1) return rt == 4 ? launch_short<1, 4>(a, dtype, st) : rt == 2 ? launch_short<1, 2>(a, dtype, st) : launch_short<1, 1>(a, dtype, st);
+      if (nc == 2) return rt == 2 ? launch_short<2, 2>(a, dtype, st) : launch_short<2, 1>(a, dtype, st);
+      if (nc == 4 && rt == 1) return launch_short<4, 1>(a, dtype, st);
+    }
+    return LQ_ERR_SHAPE;
+  }
+  if (nc == 1) {
+    if (rt == 4) return launch_one<4, 2, TILED>(a, dtype, st);
+    if (rt == 2) return launch_one<2, 4, TILED>(a, dtype, st);
+    // no more blocks at once than a wavefront has: the others would be asked for again
+    const int share = (a.blocks + a.splits * R_WAVES - 1) / (a.splits * R_WAVES);
+    return share <= 2 ? launch_one<1, 2, TILED>(a, dtype, st) : share <= 4 ? launch_one<1, 4, TILED>(a, dtype, st) : launch_one<1, 8, TILED>(a, dtype, st);
+  }
   if (nc == 2) return rt == 2 ? launch<2, 2, 4, TILED, 0, void>(a, st) : launch<2, 1, 4, TILED, 0, void>(a, st);
   if (nc == 4) return rt == 2 ? launch<4, 2, 2, TILED, 0, void>(a, st) : launch<4, 1, 4, TILED, 0, void>(a, st);
   return rt == 2 ? launch<8, 2, 2, TILED, 0, void>(a, st) : launch<8, 1, 2, TILED, 0, void>(a, st);
@@ -330,7 +371,7 @@ int launch_fp8_product(const Fp8Product& p, float* part, size_t part_floats, hip
   return launch_rows(p, nullptr, 0, 0, part, part_floats, st);
 }
 int launch_fp8_product_raw(const Fp8Product& p, const void* x, int64_t ldx, int dtype, float* part, size_t part_floats, hipStream_t st) {
-  if (!fp8_quantizes_columns(p.columns.count)) return LQ_ERR_SHAPE;
+  if (!fp8_quantizes_columns(p)) return LQ_ERR_SHAPE;
   return launch_rows(p, x, ldx, dtype, part, part_floats, st);
 }
 

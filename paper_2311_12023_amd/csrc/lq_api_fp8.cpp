@@ -48,7 +48,7 @@ struct ForwardPlan { Codes x; float* part; size_t part_floats, bytes; };
 static ForwardPlan plan_forward(void* ws, int64_t m, int64_t n, int64_t k) {
   ForwardPlan p{};
   Space s{static_cast<char*>(ws), 0};
-  if (!fp8_quantizes_columns(m)) p.x = take_codes(s, m, k);
+  if (fp8_needs_codes(m)) p.x = take_codes(s, m, k);
   p.part_floats = fp8_product_part_floats(n, m, k);
   p.part = s.take<float>(p.part_floats);
   p.bytes = s.used;
@@ -58,7 +58,7 @@ struct BackwardPlan { Codes dy, dyt, xt; float* part; size_t part_floats, bytes;
 static BackwardPlan plan_backward(void* ws, int64_t m, int64_t n, int64_t k, bool want_dx, bool want_dw) {
   BackwardPlan p{};
   Space s{static_cast<char*>(ws), 0};
-  if (want_dx && (want_dw || !fp8_quantizes_columns(m))) p.dy = take_codes(s, m, n);
+  if (want_dx && (want_dw || fp8_needs_codes(m))) p.dy = take_codes(s, m, n);
   if (want_dw) { p.dyt = take_codes(s, n, m); p.xt = take_codes(s, k, m); }
   p.part_floats = std::max(want_dx ? fp8_product_part_floats(k, m, n) : 0, want_dw ? fp8_product_part_floats(k, n, m) : 0);
   p.part = s.take<float>(p.part_floats);
@@ -118,11 +118,9 @@ int lq_fp8_forward(const void* X, int64_t ldx, int x_dtype, const lq_fp8_matrix*
   const ForwardPlan p = plan_forward(workspace, m, n, k);
   if (no_space(workspace, workspace_bytes, p.bytes)) return LQ_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
-  if (fp8_quantizes_columns(m)) {
-    Fp8Product q{operand(*W, n), {}, k, Y, n};
-    q.columns.count = m;
-    return launch_fp8_product_raw(q, X, ldx, x_dtype, p.part, p.part_floats, st);
-  }
+  Fp8Product raw{operand(*W, n), {}, k, Y, n};
+  raw.columns.count = m;
+  if (fp8_quantizes_columns(raw)) return launch_fp8_product_raw(raw, X, ldx, x_dtype, p.part, p.part_floats, st);
   const Fp8Quantize q{X, m, k, ldx, x_dtype, p.x.codes, p.x.ld, p.x.scale, nullptr, 0, nullptr};
   LQ_TRY(launch_fp8_quantize(&q, 1, false, st));
   return launch_fp8_product({operand(*W, n), p.x.rows(m), k, Y, n}, p.part, p.part_floats, st);
@@ -146,10 +144,10 @@ int lq_fp8_backward(const void* dY, int64_t ldy, int dy_dtype, const void* X, in
   const BackwardPlan p = plan_backward(workspace, m, n, k, dX != nullptr, dW != nullptr);
   if (no_space(workspace, workspace_bytes, p.bytes)) return LQ_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
-  if (dX && !dW && fp8_quantizes_columns(m)) {
-    Fp8Product q{operand(*Wt, k), {}, n, dX, k};
-    q.columns.count = m;
-    return launch_fp8_product_raw(q, dY, ldy, dy_dtype, p.part, p.part_floats, st);
+  if (dX && !dW) {
+    Fp8Product raw{operand(*Wt, k), {}, n, dX, k};
+    raw.columns.count = m;
+    if (fp8_quantizes_columns(raw)) return launch_fp8_product_raw(raw, dY, ldy, dy_dtype, p.part, p.part_floats, st);
   }
   const Fp8Quantize q[2] = {{dY, m, n, ldy, dy_dtype, p.dy.codes, p.dy.ld, p.dy.scale, p.dyt.codes, p.dyt.ld, p.dyt.scale},
                             {X, m, k, ldx, x_dtype, nullptr, 0, nullptr, p.xt.codes, p.xt.ld, p.xt.scale}};
