@@ -121,8 +121,10 @@ __device__ __forceinline__ void rows_store(const RowsArgs& a, floatx4 v, int64_t
 
 // A workgroup makes 16 RT rows x 16 NC columns over its range of the sum, each of its wavefronts a quarter of the range: lane l
 // brings 32 bytes (l / 16) of a block of row (column) l % 16 straight into registers, U blocks of the rows' operand under way at
-// once.  With T (not void) the up to RAWS columns of that operand are quantized on the
-// way, by every workgroup for itself: a launch less.
+// once (32000 x 1024, one row: with eight blocks a wavefront by more rows 8.3 us, 4 TB/s; 11008 x 4096 10.1 us, 4.5 TB/s).  With T (not
+// void) the up to RAWS columns are quantized on the way, by every workgroup for itself: a launch less.  From 17 columns on it is their codes,
+// which every 16 RT rows ask for again, that take longer than the weights (11008 x 4096, 64 columns 25 us); four wavefronts that share them did
+// not help.
 template <int NC, int RT, int U, bool TILED, int RAWS, typename T>
 __global__ __launch_bounds__(64 * R_WAVES) void fp8_rows_kernel(RowsArgs a) {
   constexpr bool RAW = !std::is_void<T>::value;
@@ -301,11 +303,13 @@ size_t fp8_product_part_floats(int64_t rows, int64_t columns, int64_t k) {
 bool fp8_needs_codes(int64_t columns) { return columns > RAW_MOST; }
 // More of them than RAW_MOST where the sum is short, us so and in two launches: 768 x 768, 9, 16, 32, 64 rows 3.6, 3.9, 5.7, 8.6 and 7.3, 7.5, 8.1,
 // 9.2; 4096 x 256, 16, 32, 64 rows 5.3, 8.3, 13.2 and 6.9, 7.2, 7.8 (fewer wavefronts have a part of the sum); 32000 x 1024, 16, 32, 64 rows
-// 9.1, 16.9, 24.9 and 13.3, 19.0, 20.0.
+// 9.1, 16.9, 24.9 and 13.3, 19.0, 20.0.  Up to 16 rows also several such steps one after the other: 1024 x 2000, 16 rows 6.7 and 8.8, 4096 x 4096
+// 10.5 and 12.9, 11008 x 4096 15.1 and 19.1, 4096 x 11008 23.6 and 23.1 (with four blocks a step 9.1, 11.9, 17.5, 31.4).
 bool fp8_quantizes_columns(const Fp8Product& p) {
   const int64_t columns = p.columns.count, blocks = fp8_blocks(p.k);
   if (columns <= RAW_MOST) return true;
-  if (!p.rows.shift || blocks > 2 * R_WAVES) return false;
+  if (!p.rows.shift || blocks > 32) return false;
+  if (blocks > 2 * R_WAVES) return columns <= 16;
   return columns <= 16 || (columns <= 32 && blocks > 2) || (columns <= 64 && blocks > R_WAVES && p.rows.count < 32 * 256);
 }
 
@@ -330,13 +334,15 @@ static int launch_one(const RowsArgs& a, int dtype, hipStream_t st) {
   if (a.columns.count <= 4) return dtype == LQ_T_BF16 ? launch<1, RT, U, TILED, 4, __bf16>(a, st) : launch<1, RT, U, TILED, 4, float>(a, st);
   return dtype == LQ_T_BF16 ? launch<1, RT, U, TILED, RAW_MOST, __bf16>(a, st) : launch<1, RT, U, TILED, RAW_MOST, float>(a, st);
 }
-// 9 to 64 columns quantized where they are used: short sums, of which a wavefront has two blocks at most.
+// 9 to 64 columns quantized where they are used, two blocks of the sum a step.
 template <int NC, int RT>
 static int launch_short(const RowsArgs& a, int dtype, hipStream_t st) {
   return dtype == LQ_T_BF16 ? launch<NC, RT, 2, true, 16 * NC, __bf16>(a, st) : launch<NC, RT, 2, true, 16 * NC, float>(a, st);
 }
 template <bool TILED>
 static int launch_shape(const RowsArgs& a, int nc, int rt, int dtype, hipStream_t st) {
+  // no more blocks at once than a wavefront has: the others would be asked for again
+  const int share = (a.blocks + a.splits * R_WAVES - 1) / (a.splits * R_WAVES);
   if (a.x && a.columns.count > RAW_MOST) {
     if constexpr (TILED) {
       if (nc == 1) return rt == 4 ? launch_short<1, 4>(a, dtype, st) : rt == 2 ? launch_short<1, 2>(a, dtype, st) : launch_short<1, 1>(a, dtype, st);
@@ -348,12 +354,11 @@ static int launch_shape(const RowsArgs& a, int nc, int rt, int dtype, hipStream_
   if (nc == 1) {
     if (rt == 4) return launch_one<4, 2, TILED>(a, dtype, st);
     if (rt == 2) return launch_one<2, 4, TILED>(a, dtype, st);
-    // no more blocks at once than a wavefront has: the others would be asked for again
-    const int share = (a.blocks + a.splits * R_WAVES - 1) / (a.splits * R_WAVES);
     return share <= 2 ? launch_one<1, 2, TILED>(a, dtype, st) : share <= 4 ? launch_one<1, 4, TILED>(a, dtype, st) : launch_one<1, 8, TILED>(a, dtype, st);
   }
+  if (nc == 2 && share <= 2) return rt == 2 ? launch<2, 2, 2, TILED, 0, void>(a, st) : launch<2, 1, 2, TILED, 0, void>(a, st);
   if (nc == 2) return rt == 2 ? launch<2, 2, 4, TILED, 0, void>(a, st) : launch<2, 1, 4, TILED, 0, void>(a, st);
-  if (nc == 4) return rt == 2 ? launch<4, 2, 2, TILED, 0, void>(a, st) : launch<4, 1, 4, TILED, 0, void>(a, st);
+  if (nc == 4) return rt == 2 ? launch<4, 2, 2, TILED, 0, void>(a, st) : share <= 2 ? launch<4, 1, 2, TILED, 0, void>(a, st) : launch<4, 1, 4, TILED, 0, void>(a, st);
   return rt == 2 ? launch<8, 2, 2, TILED, 0, void>(a, st) : launch<8, 1, 2, TILED, 0, void>(a, st);
 }
 
