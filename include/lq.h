@@ -443,7 +443,8 @@ int lq_fp8_backward(const void* dY, int64_t ldy, int dy_dtype, const void* X, in
 /*
  * ---- The optimizer's step ---------------------------------------------------------------------------------------------
  *
- * Both calls take any number of tensors; their descriptions (host memory) are read before the call returns.
+ * Both calls take up to 2^24 tensors (LQ_ERR_ARG) of up to 2^34 values (LQ_ERR_SHAPE); their descriptions (host memory) are read before the
+ * call returns.
  */
 
 /* One gradient: n values of type dtype. */

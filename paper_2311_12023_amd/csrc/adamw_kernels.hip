@@ -1,6 +1,6 @@
 // The optimizer's step over many tensors: the gradients' norm and AdamW with states in 32 or 8 bits.  Bound by bytes: 28 a value in fp32
-// (448 tensors, 1.6e8 values: ten launches, 890 us, 5.0 TB/s), 16 with 8-bit states, bf16 gradients and a bf16 copy (1.3e8 values 400 us,
-// 5.3 TB/s); the norm reads 4 (5.1e7 values 38 us, 5.4 TB/s, and the join of the workgroups' sums).
+// (480 tensors, 1.7e8 values: ten launches, 925 us, 5.1 TB/s), 16 with 8-bit states, bf16 gradients and a bf16 copy (1.3e8 values 381 us,
+// 5.5 TB/s); the norm reads 4 (5.1e7 values 38 us, 5.4 TB/s, and the join of the workgroups' sums).
 #include <cmath>
 
 #include "fp8.h"
@@ -12,19 +12,18 @@ namespace lq {
 // Descriptions of tensors travel as kernel arguments (4 KB at most), a launch for every so many of them: nothing has to be uploaded
 // that a running kernel may still read, and a captured graph keeps its own.
 constexpr int GRADS_A_LAUNCH = 190, TENSORS_A_LAUNCH = 48;
-// Elements a workgroup takes: one pass of its threads for few (a chain of passes is what a small call waits for), several for many.
-static int64_t chunk_of(double elements, int64_t most) {
+// Elements a workgroup takes.  AdamW: one pass of its threads (480 tensors of 1.7e8 values, 32 bits, 925 us, with four passes 956; one
+// of 1.3e8 values, 8 bits, 397 and 408).  The norm: one for few values (a chain of passes is what a small call waits for), several for many,
+// whose sums have to be joined.
+constexpr int STEP_CHUNK = 2048;
+constexpr int64_t NORM_CHUNK_MOST = 16384;
+static int64_t norm_chunk(const lq_gradient* g, int64_t count) {
+  double n = 0;
+  for (int64_t i = 0; i < count; ++i) n += (double)g[i].n;
   int64_t chunk = 2048;
-  while (chunk < most && elements > (double)chunk * 2048) chunk *= 2;
+  while (chunk < NORM_CHUNK_MOST && n > (double)chunk * 2048) chunk *= 2;
   return chunk;
 }
-template <typename Tensor>
-static double elements_of(const Tensor* t, int64_t count) {
-  double n = 0;
-  for (int64_t i = 0; i < count; ++i) n += (double)t[i].n;
-  return n;
-}
-constexpr int64_t NORM_CHUNK_MOST = 16384, STEP_CHUNK_MOST = 8192;
 
 // ---- the gradients' norm ------------------------------------------------------------------------------------
 struct GradTable {
@@ -130,7 +129,7 @@ __global__ __launch_bounds__(FEW_THREADS) void grad_norm_few_kernel(GradTable t,
 
 size_t grad_norm_parts(const lq_gradient* grads, int64_t count) {
   size_t parts = 0;
-  const int64_t chunk = chunk_of(elements_of(grads, count), NORM_CHUNK_MOST);
+  const int64_t chunk = norm_chunk(grads, count);
   for (int64_t i = 0; i < count; ++i) parts += (size_t)((grads[i].n + chunk - 1) / chunk);
   return parts;
 }
@@ -154,7 +153,7 @@ int launch_grad_norm(const lq_gradient* grads, int64_t count, float max_norm, fl
     return LQ_OK;
   }
   size_t done = 0;
-  const int64_t chunk = chunk_of(elements_of(grads, count), NORM_CHUNK_MOST);
+  const int64_t chunk = norm_chunk(grads, count);
   for (int64_t i = 0; i < count;) {
     GradTable t{};
     t.chunk = (int)chunk;
@@ -162,7 +161,7 @@ int launch_grad_norm(const lq_gradient* grads, int64_t count, float max_norm, fl
     for (; i < count && t.count < GRADS_A_LAUNCH; ++i) {
       if (!grads[i].n) continue;
       const uint64_t more = (uint64_t)((grads[i].n + chunk - 1) / chunk);
-      if (t.count && wgs + more > 0x7fffffffull) break;
+      if (t.count && wgs + more > 0xffffffull) break;      // fewer than 2^32 threads
       t.g[t.count] = grads[i].g;
       t.n[t.count] = grads[i].n;
       t.bf16[t.count] = grads[i].dtype == LQ_T_BF16;
@@ -191,7 +190,7 @@ struct StepTable {
   uint32_t first[TENSORS_A_LAUNCH + 1];
   uint8_t kind[TENSORS_A_LAUNCH];          // bit 0: p bf16, 1: g bf16, 2: on 16-byte addresses
   uint32_t index[TENSORS_A_LAUNCH];        // in the call
-  int count, chunk;
+  int count;
 };
 struct StepFactors {
   float beta1, rest1, beta2, rest2, eps, keep, size, root;     // root: (1 - beta2^step)^-1/2, size: lr / (1 - beta1^step)
@@ -212,11 +211,14 @@ __host__ __device__ inline void step_factors(StepFactors& f, double lr, double b
   f.step = (uint32_t)step;
 }
 
-template <typename T>
+// STREAMED: past the caches' replacement, which the 8-bit step's values gain from (1.3e8 values with a bf16 copy 381 us, else 397) and the
+// 32-bit one's lose by (954 and 925).
+template <bool STREAMED, typename T>
 __device__ __forceinline__ void load8(const T* x, int64_t i, int count, bool vec, float (&v)[8]) {
   typedef T vec8 __attribute__((ext_vector_type(8)));
   if (vec && count == 8) {
-    const vec8 in = *reinterpret_cast<const vec8*>(x + i);
+    const vec8* from = reinterpret_cast<const vec8*>(x + i);
+    const vec8 in = STREAMED ? __builtin_nontemporal_load(from) : *from;
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = (float)in[j];
   } else {
@@ -224,14 +226,15 @@ __device__ __forceinline__ void load8(const T* x, int64_t i, int count, bool vec
     for (int j = 0; j < 8; ++j) v[j] = j < count ? (float)x[i + j] : 0.0f;
   }
 }
-template <typename T>
+template <bool STREAMED, typename T>
 __device__ __forceinline__ void store8(T* x, int64_t i, int count, bool vec, const float (&v)[8]) {
   typedef T vec8 __attribute__((ext_vector_type(8)));
   if (vec && count == 8) {
     vec8 out;
 #pragma unroll
     for (int j = 0; j < 8; ++j) out[j] = (T)v[j];
-    *reinterpret_cast<vec8*>(x + i) = out;
+    if (STREAMED) __builtin_nontemporal_store(out, reinterpret_cast<vec8*>(x + i));
+    else *reinterpret_cast<vec8*>(x + i) = out;
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -289,20 +292,23 @@ __device__ __forceinline__ float round_square(float x, uint32_t u) {
 // block of 256 lies in 32 lanes, which find its largest magnitude by five exchanges.  Every operation is rounded (no contraction): square
 // roots and quotients are the exact ones, some 90 instructions a value, a third of what the bytes leave time for.
 template <bool CODES, typename P, typename G>
-__device__ __forceinline__ void step_chunk(const StepTensor& t, uint32_t index, bool vec, const StepFactors& f, float coef, bool scaled, int64_t from, int chunk) {
-  const int64_t to = min(from + chunk, t.n);
-  // whole blocks of a state for every group of 32 lanes, so that its lanes stay together
+__device__ __forceinline__ void step_chunk(const StepTensor& t, uint32_t index, bool vec, const StepFactors& f, float coef, bool scaled, int64_t from) {
+  const int64_t to = min(from + STEP_CHUNK, t.n);
+  // Whole blocks of a state for every group of 32 lanes, so that its lanes stay together.  One pass; left as a loop the 32-bit one takes
+  // eight registers less (61, eight wavefronts a SIMD: 925 us, 945 without), the 8-bit one eighteen more.
   for (int64_t i = from + 8 * threadIdx.x; i - 8 * (threadIdx.x & 31) < to; i += 8 * 256) {
     const int count = (int)max((int64_t)0, min((int64_t)8, t.n - i));
     float p[8], g[8], m[8], v[8], r[8];
-    load8(static_cast<const P*>(t.p), i, count, vec, p);
-    load8(static_cast<const G*>(t.g), i, count, vec, g);
+    load8<CODES>(static_cast<const P*>(t.p), i, count, vec, p);
+    // behind the norm the gradients may still be in the memory-side cache (5.1e7 values, norm and step, 160 us, streamed 164)
+    if (scaled) load8<false>(static_cast<const G*>(t.g), i, count, vec, g);
+    else load8<CODES>(static_cast<const G*>(t.g), i, count, vec, g);
     if constexpr (CODES) {
       load_codes(static_cast<const uint8_t*>(t.m), i, count, vec, t.m_scale[i / STATE_BLOCK], m);
       load_codes(static_cast<const uint8_t*>(t.v), i, count, vec, t.v_scale[i / STATE_BLOCK], v);
     } else {
-      load8(static_cast<const float*>(t.m), i, count, vec, m);
-      load8(static_cast<const float*>(t.v), i, count, vec, v);
+      load8<false>(static_cast<const float*>(t.m), i, count, vec, m);
+      load8<false>(static_cast<const float*>(t.v), i, count, vec, v);
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -313,11 +319,11 @@ __device__ __forceinline__ void step_chunk(const StepTensor& t, uint32_t index, 
       r[j] = sqrtf(v[j]);
       p[j] = p[j] * f.keep - (m[j] / (r[j] * f.root + f.eps)) * f.size;
     }
-    store8(static_cast<P*>(t.p), i, count, vec, p);
-    if (t.copy) store8(static_cast<__bf16*>(t.copy), i, count, vec, p);
+    store8<CODES>(static_cast<P*>(t.p), i, count, vec, p);
+    if (t.copy) store8<CODES>(static_cast<__bf16*>(t.copy), i, count, vec, p);
     if constexpr (!CODES) {
-      store8(static_cast<float*>(t.m), i, count, vec, m);
-      store8(static_cast<float*>(t.v), i, count, vec, v);
+      store8<false>(static_cast<float*>(t.m), i, count, vec, m);
+      store8<false>(static_cast<float*>(t.v), i, count, vec, v);
     } else {
       const float ms = fp8_scale(block_top(m)), vs = fp8_scale(block_top(r));
       const float mi = 1.0f / ms, vi = 1.0f / vs;
@@ -334,6 +340,7 @@ __device__ __forceinline__ void step_chunk(const StepTensor& t, uint32_t index, 
         t.v_scale[i / STATE_BLOCK] = vs;
       }
     }
+    if constexpr (CODES) break;
   }
 }
 
@@ -346,14 +353,14 @@ __global__ __launch_bounds__(256) void adamw_kernel(StepTable table, StepArgs a)
   if (a.lr_device || a.step_device) step_factors(f, a.lr_device ? (double)lr : a.lr, a.beta1, a.beta2, a.decay, step);
   const int i = __builtin_amdgcn_readfirstlane(tensor_of(table, blockIdx.x));
   const StepTensor t = table.t[i];
-  const int64_t from = (int64_t)(blockIdx.x - table.first[i]) * table.chunk;
+  const int64_t from = (int64_t)(blockIdx.x - table.first[i]) * STEP_CHUNK;
   const int kind = table.kind[i];
   const bool vec = kind & 4, scaled = a.coef != nullptr;
   const uint32_t index = table.index[i];
-  if ((kind & 3) == 0) step_chunk<CODES, float, float>(t, index, vec, f, coef, scaled, from, table.chunk);
-  else if ((kind & 3) == 1) step_chunk<CODES, __bf16, float>(t, index, vec, f, coef, scaled, from, table.chunk);
-  else if ((kind & 3) == 2) step_chunk<CODES, float, __bf16>(t, index, vec, f, coef, scaled, from, table.chunk);
-  else step_chunk<CODES, __bf16, __bf16>(t, index, vec, f, coef, scaled, from, table.chunk);
+  if ((kind & 3) == 0) step_chunk<CODES, float, float>(t, index, vec, f, coef, scaled, from);
+  else if ((kind & 3) == 1) step_chunk<CODES, __bf16, float>(t, index, vec, f, coef, scaled, from);
+  else if ((kind & 3) == 2) step_chunk<CODES, float, __bf16>(t, index, vec, f, coef, scaled, from);
+  else step_chunk<CODES, __bf16, __bf16>(t, index, vec, f, coef, scaled, from);
 }
 
 int launch_adamw(const lq_adamw_tensor* tensors, int64_t count, int state_bits, const lq_adamw_params& h, const float* coef, hipStream_t st) {
@@ -371,20 +378,12 @@ int launch_adamw(const lq_adamw_tensor* tensors, int64_t count, int state_bits, 
   prof::Scope ps(prof::ADAMW, st, bytes);
   for (int64_t i = 0; i < count;) {
     StepTable t{};
-    int64_t to = i, used = 0;
-    double elements = 0;
-    for (; to < count && used < TENSORS_A_LAUNCH; ++to) {
-      used += tensors[to].n > 0;
-      elements += (double)tensors[to].n;
-    }
-    const int64_t chunk = chunk_of(elements, STEP_CHUNK_MOST);
-    t.chunk = (int)chunk;
     uint64_t wgs = 0;
-    for (; i < to; ++i) {
+    for (; i < count && t.count < TENSORS_A_LAUNCH; ++i) {
       const lq_adamw_tensor& x = tensors[i];
       if (!x.n) continue;
-      const uint64_t more = (uint64_t)((x.n + chunk - 1) / chunk);
-      if (t.count && wgs + more > 0x7fffffffull) break;
+      const uint64_t more = (uint64_t)((x.n + STEP_CHUNK - 1) / STEP_CHUNK);
+      if (t.count && wgs + more > 0xffffffull) break;      // fewer than 2^32 threads
       uintptr_t low = (uintptr_t)x.p | (uintptr_t)x.g | (uintptr_t)x.copy;
       const uintptr_t states = (uintptr_t)x.m | (uintptr_t)x.v;
       const bool vec = (low & 15) == 0 && (states & (codes ? 7 : 15)) == 0;

@@ -6,7 +6,7 @@
 
 namespace lq {
 
-constexpr int64_t MOST_TENSORS = (int64_t)1 << 24, MOST_VALUES = (int64_t)1 << 40;
+constexpr int64_t MOST_TENSORS = (int64_t)1 << 24, MOST_VALUES = (int64_t)1 << 34;
 
 static bool bad_type(int dtype) { return dtype != LQ_T_FP32 && dtype != LQ_T_BF16; }
 static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
