@@ -1,5 +1,5 @@
 // The optimizer's step over many tensors: the gradients' norm and AdamW with states in 32 or 8 bits.  Bound by bytes: 28 a value in fp32
-// (480 tensors, 1.7e8 values: ten launches, 925 us, 5.1 TB/s), 16 with 8-bit states, bf16 gradients and a bf16 copy (1.3e8 values 381 us,
+// (480 tensors, 1.7e8 values: 925 us, 5.1 TB/s), 16 with 8-bit states, bf16 gradients and a bf16 copy (1.3e8 values 381 us,
 // 5.5 TB/s); the norm reads 4 (5.1e7 values 38 us, 5.4 TB/s, and the join of the workgroups' sums).
 #include <cmath>
 
@@ -11,7 +11,7 @@ namespace lq {
 
 // Descriptions of tensors travel as kernel arguments (4 KB at most), a launch for every so many of them: nothing has to be uploaded
 // that a running kernel may still read, and a captured graph keeps its own.
-constexpr int GRADS_A_LAUNCH = 190, TENSORS_A_LAUNCH = 48;
+constexpr int GRADS_A_LAUNCH = 193, TENSORS_A_LAUNCH = 54;
 // Elements a workgroup takes.  AdamW: one pass of its threads (480 tensors of 1.7e8 values, 32 bits, 925 us, with four passes 956; one
 // of 1.3e8 values, 8 bits, 397 and 408).  The norm: one for few values (a chain of passes is what a small call waits for), several for many,
 // whose sums have to be joined.
@@ -33,6 +33,8 @@ struct GradTable {
   uint8_t bf16[GRADS_A_LAUNCH];
   int count, chunk;
 };
+
+static_assert(sizeof(GradTable) + 24 <= 4096, "kernel arguments");
 
 template <typename Table>
 __device__ __forceinline__ int tensor_of(const Table& t, uint32_t wg) {
@@ -203,6 +205,8 @@ struct StepArgs {
   int64_t step;
   const float* lr_device; const int64_t* step_device; const float* coef;
 };
+
+static_assert(sizeof(StepTable) + sizeof(StepArgs) <= 4096, "kernel arguments");
 
 __host__ __device__ inline void step_factors(StepFactors& f, double lr, double beta1, double beta2, double decay, int64_t step) {
   f.keep = (float)(1.0 - lr * decay);

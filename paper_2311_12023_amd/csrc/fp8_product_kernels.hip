@@ -37,8 +37,8 @@ __device__ __forceinline__ uintx2 product_result(floatx4 v) {
 // nothing, transfers or sums taken out 17 % and 11 %.
 //
 // A workgroup of eight wavefronts makes a tile, a wavefront 128 x 64 of it (2 x 4) in blocks of 16 x 16.  A block of 128 along k is one
-// matrix instruction, whose four sums a lane are multiplied by the two scales into the accumulators; what it takes is two vector
-// instructions for four sums where the rows' scales are of tiles (one scale for the wavefront's 128 rows), else three.
+// matrix instruction, whose four sums a lane are multiplied by the two scales into the accumulators: one vector instruction each where
+// the rows' scales are of tiles (one scale for the wavefront's 128 rows), else two.
 //
 // LDS holds two blocks of both operands.  Rows are 128 bytes, unit u of 16 bytes of row r stored at u ^ (r % 8): a read of 16 rows
 // x 4 units touches every bank alike.  Blocks of 16 rows are taken two at a time; before the last two of a block of 128, all its operands are
