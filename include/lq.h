@@ -388,7 +388,8 @@ int lq_adapter_backward(const void* dY, const void* X, int64_t m, int64_t d, int
  * has scale NaN, and so has every sum that it enters.
  * Products add up a block of 128 in the matrix unit, whose sums are off by up to 2^-12 of the sum of the terms' magnitudes where codes of
  * all sizes meet (2^-16 for normally distributed values), and the blocks in fp32; results are bf16, since more bits would hold that error.  They are right where they are below 2^96; where a scale times another
- * is below 2^-156 they may be 0.  All calls only enqueue kernels on `stream` and are deterministic.
+ * is below 2^-156 they may be 0.  All calls only enqueue kernels on `stream` and are deterministic; the order of a sum goes by the sizes,
+ * so a row's results among few rows and among many can differ in their last bit.
  */
 
 /*
@@ -431,6 +432,7 @@ int lq_fp8_matmul(const lq_fp8_matrix* A, const lq_fp8_matrix* B, int64_t m, int
  * with X and dY quantized in rows inside the calls: along k for Y, along n for dX, along m (both) for dW.
  *   X m x k, dY m x n: of types x_dtype and dy_dtype, rows ldx and ldy elements apart        W n x k, Wt (W^T) k x n: in 8 bits
  *   Y m x n, dX m x k, dW n x k: bf16, contiguous.  dX or dW may be NULL: not wanted (with dX Wt is needed, with dW X)
+ *   workspace  the matching *_workspace_bytes call's bytes for these sizes (0: may be NULL); another number of rows can need more or less
  *   m, n, k up to 2^27, what a product sums over (forward k, dX n, dW m) up to 2^22 (LQ_ERR_SHAPE)
  */
 size_t lq_fp8_forward_workspace_bytes(int64_t m, int64_t n, int64_t k);

@@ -678,7 +678,8 @@ class AdamW:
     params: contiguous GPU tensors of fp32 or bf16, updated in place.  copies: bf16 tensors (or None) that take each fp32 parameter's
     rounded value in the same pass.  States start at zero and lie in `buffers` ("m", "v", with bits=8 also "m_scale", "v_scale"), tensor
     after tensor, each from a multiple of 256 on.  `t` counts the steps taken: an int, or with device_step=True an int64 tensor on the
-    GPU, so that a captured step counts on when it is replayed.  seed: of the rounding of 8-bit states."""
+    GPU, so that a captured step counts on when it is replayed.  seed: of the rounding of 8-bit states.  buffers, t and seed are what a
+    checkpoint needs.  The order of params belongs to the rounding of 8-bit states."""
 
     def __init__(self, params, bits: int = 32, copies=None, seed: int = 0, device_step: bool = False):
         if bits not in (8, 32):

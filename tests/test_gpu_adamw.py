@@ -334,3 +334,23 @@ def test_another_stream():
     for _ in range(3):
         b.step([g], 0.01, coef=lq.grad_norm([g], 1.0)[1])
     assert torch.equal(p, again)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_goes_on_from_what_a_checkpoint_holds(bits):
+    sizes = (3000, 77)
+    params = [_values(n, n).cuda() for n in sizes]
+    opt = lq.AdamW(params, bits=bits, seed=8)
+    grads = [[_values(n, 100 * t + n).cuda() for n in sizes] for t in range(4)]
+    for t in range(2):
+        opt.step(grads[t], 0.01)
+    held = [p.clone() for p in params], {k: b.clone() for k, b in opt.buffers.items()}, opt.t, opt.seed
+    for t in range(2, 4):
+        opt.step(grads[t], 0.01)
+    again = lq.AdamW(held[0], bits=bits, seed=held[3])
+    again.t = held[2]
+    for name, buffer in again.buffers.items():
+        buffer.copy_(held[1][name])
+    for t in range(2, 4):
+        again.step(grads[t], 0.01)
+    assert all(torch.equal(a, b) for a, b in zip(params, held[0]))
