@@ -743,7 +743,8 @@ class AdamW:
         if not on_device and torch._C._cuda_isCurrentStreamCapturing():
             raise RuntimeError("a captured step needs device_step=True: a replay would repeat this step's number")
         h = self._params
-        (h.beta1, h.beta2), h.eps, h.weight_decay, h.seed, h.lr_device = betas, eps, weight_decay, self.seed, None
+        (h.beta1, h.beta2), h.eps, h.weight_decay, h.seed = betas, eps, weight_decay, self.seed
+        h.lr_device = h.step_device = None                   # the last step's
         if isinstance(lr, torch.Tensor):
             h.lr_device = _dev(lr, torch.float32, "lr")
         else:

@@ -1,0 +1,53 @@
+"""What AdamW.step hands to the library when its public state (t, buffers) changes between steps.  Needs no GPU: tensors of the CPU
+stand for the GPU's, and the call is recorded instead of made."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2311_12023_amd import lq
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """-> the calls' numbers, addresses and tables, one dict each."""
+    made = []
+
+    def dev(t, dtype, name):
+        if t is None:
+            return None
+        if not (isinstance(t, torch.Tensor) and t.device.type == "cpu" and t.dtype == dtype and t.is_contiguous()):
+            raise TypeError(name)
+        return t.data_ptr()
+
+    def adamw(table, count, bits, params, coef, stream):
+        h = params._obj
+        entries = (lq.AdamWTensor * count).from_address(table)
+        made.append(dict(step=h.step, step_device=h.step_device, lr_device=h.lr_device,
+                         table=[{n: getattr(e, n) for n, _ in lq.AdamWTensor._fields_} for e in entries]))
+        return 0
+
+    monkeypatch.setattr(lq, "_dev", dev)
+    monkeypatch.setattr(lq, "_stream", lambda: None)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: -1)                  # a CPU tensor's get_device()
+    monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: False)
+    monkeypatch.setattr(lq._lib, "lq_adamw", adamw)
+    return made
+
+
+def _made(bits=32, sizes=(300, 5), **more):
+    params = [torch.zeros(n) for n in sizes]
+    return lq.AdamW(params, bits=bits, **more), [torch.ones(n) for n in sizes]
+
+
+def test_a_number_in_place_of_a_device_number(calls):
+    """t as a checkpoint's number after steps that were counted on the device: the number counts, the tensor is not read any more."""
+    opt, grads = _made(device_step=True)
+    opt.step(grads, 0.1)
+    assert calls[-1]["step_device"] == opt.t.data_ptr() and opt.t.item() == 1
+    opt.t = 40
+    opt.step(grads, 0.1)
+    assert calls[-1]["step_device"] is None and calls[-1]["step"] == 41 and opt.t == 41
+    opt.t = torch.tensor(6)
+    opt.step(grads, 0.1)
+    assert calls[-1]["step_device"] == opt.t.data_ptr() and opt.t.item() == 7
