@@ -756,8 +756,11 @@ class AdamW:
                 _here(one)
         scale = _dev(coef, torch.float32, "coef")
         if on_device:
+            h.step_device = _dev(self.t, torch.int64, "t")
+            if self.t.numel() != 1:
+                raise ValueError("t: need one element")
+            _here(self.t)
             self.t += 1
-            h.step_device = self.t.data_ptr()
         else:
             h.step = self.t + 1
         status = _lib.lq_adamw(C.addressof(self._table), len(grads), self.bits, C.byref(h), scale, _stream())

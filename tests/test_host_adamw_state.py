@@ -51,3 +51,15 @@ def test_a_number_in_place_of_a_device_number(calls):
     opt.t = torch.tensor(6)
     opt.step(grads, 0.1)
     assert calls[-1]["step_device"] == opt.t.data_ptr() and opt.t.item() == 7
+
+
+@pytest.mark.parametrize("t,error", [(torch.zeros((), dtype=torch.int32), TypeError), (torch.zeros(()), TypeError),
+                                     (torch.zeros((), dtype=torch.int64, device="meta"), TypeError), (torch.zeros(2, dtype=torch.int64), ValueError),
+                                     (torch.zeros(0, dtype=torch.int64), ValueError), (1.5, TypeError), (None, TypeError)])
+def test_a_step_number_that_cannot_be_read(calls, t, error):
+    """Of another type, in other memory (here: not the CPU's), of no or several elements: refused before anything is called or counted."""
+    opt, grads = _made()
+    opt.t = t
+    with pytest.raises(error):
+        opt.step(grads, 0.1)
+    assert not calls and opt.t is t and (not isinstance(t, torch.Tensor) or t.is_meta or not t.any())
