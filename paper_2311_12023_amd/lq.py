@@ -677,9 +677,11 @@ class AdamW:
 
     params: contiguous GPU tensors of fp32 or bf16, updated in place.  copies: bf16 tensors (or None) that take each fp32 parameter's
     rounded value in the same pass.  States start at zero and lie in `buffers` ("m", "v", with bits=8 also "m_scale", "v_scale"), tensor
-    after tensor, each from a multiple of 256 on.  `t` counts the steps taken: an int, or with device_step=True an int64 tensor on the
-    GPU, so that a captured step counts on when it is replayed.  seed: of the rounding of 8-bit states.  buffers, t and seed are what a
-    checkpoint needs.  The order of params belongs to the rounding of 8-bit states."""
+    after tensor, each from a multiple of 256 on.  `t` counts the steps taken: an int, or with device_step=True an int64 tensor of one
+    element on the GPU, so that a captured step counts on when it is replayed.  seed: of the rounding of 8-bit states.  buffers, t and seed
+    are what a checkpoint needs: copied into, or replaced by others of their type and size on the GPU, which the next step takes up.  A
+    captured step goes on with the tensors it was captured with, which have to live as long: copy into those.  The order of params belongs to
+    the rounding of 8-bit states."""
 
     def __init__(self, params, bits: int = 32, copies=None, seed: int = 0, device_step: bool = False):
         if bits not in (8, 32):
@@ -700,13 +702,12 @@ class AdamW:
         self._columns = np.frombuffer(self._table, dtype=np.dtype(AdamWTensor))
         self._held = self.params + [c for c in self.copies if c is not None]
         self._describe()
-        state = FP8 if bits == 8 else torch.float32
-        self.buffers = {name: torch.zeros(total, dtype=state, device=device) for name in ("m", "v")}
+        self._starts, state = np.array(starts, dtype=np.uint64), FP8 if bits == 8 else torch.float32
+        self._states = {name: (state, total, 1 if bits == 8 else 4) for name in ("m", "v")}        # type, size, bytes for a value of p
         if bits == 8:
-            self.buffers.update({name: torch.zeros(total // 256, dtype=torch.float32, device=device) for name in ("m_scale", "v_scale")})
-        for entry, at in zip(self._table, starts):
-            for name, buffer in self.buffers.items():
-                setattr(entry, name, buffer.data_ptr() + (4 * (at // 256) if name.endswith("scale") else at * buffer.element_size()))
+            self._states.update({name: (torch.float32, total // 256, 1 / 64) for name in ("m_scale", "v_scale")})
+        self.buffers = {name: torch.zeros(n, dtype=dtype, device=device) for name, (dtype, n, _) in self._states.items()}
+        self._state_places = {}
         self.t = torch.zeros((), dtype=torch.int64, device=device) if device_step else 0
 
     def _describe(self):
@@ -723,6 +724,20 @@ class AdamW:
             entry.copy = _dev(c, torch.bfloat16, "copies")
         self._places = [x.data_ptr() for x in self._held]
 
+    def _find_states(self):
+        """The states' addresses into the table, checked, where others lie in `buffers` than at the last step."""
+        for name, (dtype, n, stride) in self._states.items():
+            buffer = self.buffers.get(name)
+            if buffer is None:
+                raise TypeError(f"buffers: no {name}")
+            place = _dev(buffer, dtype, name)
+            if buffer.numel() != n:
+                raise ValueError(f"buffers: {name} has {buffer.numel()} elements, needs {n}")
+            _here(buffer)
+            if place != self._state_places.get(name):
+                self._columns[name] = place + (self._starts * stride).astype(np.uint64)
+                self._state_places[name] = place
+
     def step(self, grads, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, coef: torch.Tensor | None = None) -> None:
         """One step.  grads: one for each parameter, fp32 or bf16, of its size.  lr: a number, or an fp32 tensor of one element on the GPU.
         coef: such a tensor that multiplies every gradient (grad_norm's); where it is not finite, nothing but `t` changes."""
@@ -734,6 +749,7 @@ class AdamW:
         now = [x.data_ptr() for x in self._held]
         if now != self._places:                              # parameters that have moved
             self._describe()
+        self._find_states()
         if len(grads) > 16:
             self._columns["g"], self._columns["g_dtype"] = places, types
         else:

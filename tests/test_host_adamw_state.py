@@ -63,3 +63,55 @@ def test_a_step_number_that_cannot_be_read(calls, t, error):
     with pytest.raises(error):
         opt.step(grads, 0.1)
     assert not calls and opt.t is t and (not isinstance(t, torch.Tensor) or t.is_meta or not t.any())
+
+
+def _expected(opt, buffers):
+    """The states' addresses of every tensor: its blocks of 256 behind those of the tensors before it."""
+    at, want = 0, []
+    for p in opt.params:
+        want.append({name: b.data_ptr() + (at // 256 * 4 if name.endswith("scale") else at * b.element_size()) for name, b in buffers.items()})
+        at += -(-p.numel() // 256) * 256
+    return want
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("sizes", [(300, 5), (7,) * 20 + (0, 513)])
+def test_states_that_are_replaced(calls, bits, sizes):
+    """A checkpoint's tensors in place of the states, one by one or all at once: the step goes on in them."""
+    opt, grads = _made(bits, sizes)
+    opt.step(grads, 0.1)
+    first = opt.buffers
+    changed = [dict(first), {k: b.clone() for k, b in first.items()}]
+    changed[0]["m"] = first["m"].clone()
+    for buffers in (first, *changed, first):
+        opt.buffers = buffers
+        opt.step(grads, 0.1)
+        for have, want in zip(calls[-1]["table"], _expected(opt, buffers)):
+            assert all(have[name] == place for name, place in want.items())
+    opt.buffers["v"] = first["v"].clone()
+    opt.step(grads, 0.1)
+    for have, want in zip(calls[-1]["table"], _expected(opt, opt.buffers)):
+        assert all(have[name] == place for name, place in want.items())
+
+
+@pytest.mark.parametrize("change,error", [
+    (dict(m=None), TypeError), (dict(v=torch.zeros(1024)), ValueError), (dict(m=torch.zeros(767)), ValueError), (dict(m=torch.zeros(768).half()), TypeError),
+    (dict(v=torch.zeros(768, device="meta")), TypeError), (dict(v=torch.zeros(1536)[::2]), TypeError), (dict(m=[0.0] * 768), TypeError)])
+def test_states_that_do_not_fit(calls, change, error):
+    opt, grads = _made()                                       # 300 and 5 values: three blocks of 256
+    opt.buffers.update(change)
+    with pytest.raises(error):
+        opt.step(grads, 0.1)
+    assert not calls and opt.t == 0
+
+
+@pytest.mark.parametrize("change", [dict(m_scale=torch.zeros(2)), dict(v_scale=torch.zeros(4))])
+def test_scales_that_do_not_fit(calls, change):
+    opt, grads = _made(8, device_step=True)
+    opt.buffers.update(change)
+    with pytest.raises(ValueError):
+        opt.step(grads, 0.1)
+    del opt.buffers["m"]
+    with pytest.raises(TypeError):
+        opt.step(grads, 0.1)
+    assert not calls and opt.t.item() == 0
