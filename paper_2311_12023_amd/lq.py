@@ -785,9 +785,8 @@ class AdamW:
         _check(status, "lq_adamw")
         if not on_device:
             self.t += 1
-        tracked = [x for x in self._held if x.requires_grad]
-        if tracked:                                          # a graph that still needs the old values has to say so
-            torch.autograd.graph.increment_version(tracked)
+        # a graph that has saved old values has to say so, and it saves what requires no gradient too
+        torch.autograd.graph.increment_version(self._held)
 
 
 def assign_configs(err: np.ndarray, storage: np.ndarray, budget_bits: float, node_limit: int = 0):

@@ -80,3 +80,22 @@ def test_states_and_numbers_that_are_refused():
     opt.buffers["m"] = good["m"]
     opt.step(g, 0.1)
     assert good_t.item() == 1 and not _same(p, before)
+
+
+@pytest.mark.parametrize("kind", ["copy", "plain bf16", "plain fp32", "parameter"])
+def test_a_graph_that_has_saved_what_a_step_writes_fails(kind):
+    """Activations that require a gradient times a weight that does not: the product's graph holds the weight."""
+    g = torch.Generator().manual_seed(1)
+    w = torch.randn(6, 16, generator=g).to(torch.bfloat16 if kind == "plain bf16" else torch.float32).cuda()
+    w = torch.nn.Parameter(w) if kind == "parameter" else w
+    held = w.bfloat16() if kind == "copy" else None
+    used = held if kind == "copy" else w
+    opt = lq.AdamW([w], copies=[held])
+    x = torch.randn(3, 16, generator=g).to(used.dtype).cuda().requires_grad_()
+    grad = torch.ones_like(w)
+    (x @ used.t()).sum().backward()                              # nothing was written yet
+    y = (x @ used.t()).sum()
+    opt.step([grad], 0.1)
+    with pytest.raises(RuntimeError):
+        y.backward()
+    (x @ used.t()).sum().backward()                              # one made after the step does not

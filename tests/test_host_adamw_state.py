@@ -115,3 +115,20 @@ def test_scales_that_do_not_fit(calls, change):
     with pytest.raises(TypeError):
         opt.step(grads, 0.1)
     assert not calls and opt.t.item() == 0
+
+
+def test_everything_that_a_step_writes_gets_a_new_version(calls):
+    """Parameters and copies, whether they require gradients or not: a graph that has saved their old values fails instead of using the new."""
+    params = [torch.zeros(4, 3), torch.nn.Parameter(torch.zeros(2)), torch.zeros(5)]
+    copies = [torch.zeros(4, 3, dtype=torch.bfloat16), None, None]
+    with torch.inference_mode():
+        params.append(torch.zeros(2))
+    opt = lq.AdamW(params, copies=copies + [None])
+    written = [*params[:3], copies[0]]
+    before = [x._version for x in written]
+    x = torch.ones(2, 3, dtype=torch.bfloat16, requires_grad=True)
+    y = x @ copies[0].t()
+    opt.step([torch.ones(p.shape) for p in params], 0.1)
+    assert all(x._version > old for x, old in zip(written, before))
+    with pytest.raises(RuntimeError):
+        y.sum().backward()
