@@ -582,6 +582,7 @@ def fp8_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale:
     _here(out, workspace)
     ws = workspace if workspace is not None else _workspace(_lib.lq_fp8_matmul_workspace_bytes(m, n, k), a.device)
     _check(_lib.lq_fp8_matmul(C.byref(am), C.byref(bm), m, n, k, yp, ldy, *_space(ws), _stream()), "lq_fp8_matmul")
+    torch.autograd.graph.increment_version(out)              # for graphs that have saved what lay there
     return out
 
 

@@ -169,3 +169,19 @@ def test_binding_checks_tensors():
     with pytest.raises(ValueError):
         lq.AdamW([])
     assert math.isinf(lq.grad_norm.__defaults__[0])
+
+
+def test_a_product_into_out_gives_it_a_new_version(monkeypatch):
+    """A graph that has saved what lay in `out` fails instead of using the product.  Tensors of the CPU stand for the GPU's, nothing is called."""
+    monkeypatch.setattr(lq, "_fp8_matrix", lambda codes, scale, name: lq.Fp8Matrix())
+    monkeypatch.setattr(lq, "_rows", lambda t, dtype, name: (t.data_ptr(), t.stride(0)))
+    monkeypatch.setattr(lq, "_here", lambda *tensors: None)
+    monkeypatch.setattr(lq, "_stream", lambda: None)
+    monkeypatch.setattr(lq, "_space", lambda ws: (None, 0))
+    monkeypatch.setattr(lq._lib, "lq_fp8_matmul", lambda *args: 0)
+    a, out = torch.zeros(4, 64), torch.zeros(4, 4, dtype=torch.bfloat16)
+    x = torch.ones(2, 4, dtype=torch.bfloat16, requires_grad=True)
+    y = x @ out
+    assert lq.fp8_matmul(a, None, a, None, out=out) is out
+    with pytest.raises(RuntimeError):
+        y.sum().backward()
