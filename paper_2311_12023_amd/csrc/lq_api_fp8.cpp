@@ -10,6 +10,10 @@ static bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)
 constexpr int64_t MOST_ROWS = (int64_t)1 << 27, MOST_SIDE = (int64_t)1 << 30, MOST_DEPTH = (int64_t)1 << 22, MOST_LD = (int64_t)1 << 40;
 static bool bad_rows(int64_t n) { return n <= 0 || n > MOST_ROWS; }
 static bool bad_depth(int64_t n) { return n <= 0 || n > MOST_DEPTH; }
+// A gradient's sizes: dX sums over n, dW over m.
+static bool bad_gradients(int64_t m, int64_t n, int64_t k, bool want_dx, bool want_dw) {
+  return (want_dw ? bad_depth(m) : bad_rows(m)) || (want_dx ? bad_depth(n) : bad_rows(n)) || bad_rows(k);
+}
 
 static int check_matrix(const lq_fp8_matrix* w, int64_t k) {
   if (!w || !w->codes || !w->scale) return LQ_ERR_NULL;
@@ -127,14 +131,14 @@ int lq_fp8_forward(const void* X, int64_t ldx, int x_dtype, const lq_fp8_matrix*
 }
 
 size_t lq_fp8_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int want_dx, int want_dw) {
-  if (bad_depth(m) || bad_depth(n) || bad_rows(k)) return 0;
+  if (bad_gradients(m, n, k, want_dx != 0, want_dw != 0)) return 0;
   return plan_backward(nullptr, m, n, k, want_dx != 0, want_dw != 0).bytes;
 }
 
 int lq_fp8_backward(const void* dY, int64_t ldy, int dy_dtype, const void* X, int64_t ldx, int x_dtype, const lq_fp8_matrix* Wt, int64_t m,
                     int64_t n, int64_t k, void* dX, void* dW, void* workspace, size_t workspace_bytes, void* stream) {
   if (!dY || (!dX && !dW) || (dW && !X)) return LQ_ERR_NULL;
-  if (bad_depth(m) || bad_depth(n) || bad_rows(k) || ldy < n || ldy > MOST_LD) return LQ_ERR_SHAPE;
+  if (bad_gradients(m, n, k, dX != nullptr, dW != nullptr) || ldy < n || ldy > MOST_LD) return LQ_ERR_SHAPE;
   if (bad_type(dy_dtype) || misaligned(dY, type_bytes(dy_dtype)) || misaligned(dX, 2) || misaligned(dW, 2)) return LQ_ERR_ARG;
   if (dW) {
     if (ldx < k || ldx > MOST_LD) return LQ_ERR_SHAPE;

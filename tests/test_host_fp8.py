@@ -185,3 +185,20 @@ def test_a_product_into_out_gives_it_a_new_version(monkeypatch):
     assert lq.fp8_matmul(a, None, a, None, out=out) is out
     with pytest.raises(RuntimeError):
         y.sum().backward()
+
+
+@pytest.mark.parametrize("sizes,wanted", [(dict(m=1 << 23), "dX"), (dict(m=1 << 27, n=64, ldy=64), "dX"), (dict(n=1 << 23, ldy=1 << 23), "dW"),
+                                          (dict(n=1 << 27, ldy=1 << 27, m=40), "dW"), (dict(k=1 << 27, ldx=1 << 27, m=40), "both")])
+def test_gradients_of_as_many_rows_or_columns_as_stated(sizes, wanted):
+    """Only what a wanted product sums over is bound by 2^22: these get as far as the workspace, one more than the limit does not."""
+    dx, dw = wanted != "dW", wanted != "dX"
+    out = dict(dX=P if dx else None, dW=P if dw else None)
+    m, n, k = ({**dict(m=10, n=100, k=60), **sizes}[name] for name in "mnk")
+    need = L.lq_fp8_backward_workspace_bytes(m, n, k, dx, dw)
+    assert need > 0 and _backward(**sizes, **out, size=need - 1) == -6
+    for change in (dict(m=(1 << 27) + 1), dict(n=(1 << 27) + 1, ldy=1 << 28), dict(k=(1 << 27) + 1, ldx=1 << 28)):
+        assert _backward(**{**sizes, **change}, **out) == -2
+    if dw:
+        assert _backward(**{**sizes, "m": (1 << 22) + 1}, **out) == -2 and not L.lq_fp8_backward_workspace_bytes((1 << 22) + 1, n, k, dx, dw)
+    if dx:
+        assert _backward(**{**sizes, "n": (1 << 22) + 1, "ldy": 1 << 23}, **out) == -2 and not L.lq_fp8_backward_workspace_bytes(m, (1 << 22) + 1, k, dx, dw)
