@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import fp8_fractions as F
 import fp8_reference as R
 from paper_2311_12023_amd import lq
 
@@ -36,3 +37,12 @@ def test_gradients_of_more_rows_than_a_sum_may_have():
     _close(want, R.values(*R.quantize(few.t().contiguous())), R.values(*R.quantize(x.t().contiguous())))
     _, got = lq.fp8_backward(few.cuda().repeat(1, many // 1024 + 1)[:, :many], x.cuda(), want_dx=False)
     assert torch.equal(got[:-3].view(-1, 1024, k), want.expand(many // 1024, -1, -1)) and torch.equal(got[-3:], want[:3])
+
+
+def test_every_fraction_of_a_scale():
+    """amax of all 2^23 fractions, with values that show a reciprocal one unit off: the scale is the rounded quotient by 448 and the codes are
+    those of its rounded reciprocal."""
+    for first in range(0, 1 << 23, 1 << 20):
+        x, scale, reciprocal = F.blocks(torch.arange(first, first + (1 << 20), dtype=torch.int32, device="cuda"))
+        q, s = lq.fp8_quantize(x)
+        assert torch.equal(s[:, 0], scale) and torch.equal(q.view(torch.uint8), F.codes(x, reciprocal))
