@@ -387,9 +387,11 @@ int lq_adapter_backward(const void* dY, const void* X, int64_t m, int64_t d, int
  * scale = max(fl32(amax / 448), 2^-126), code = e4m3(fl32(x fl32(1 / scale))), nearest, ties to even.  A block that holds an inf or a NaN
  * has scale NaN, and so has every sum that it enters.
  * Products add up a block of 128 in the matrix unit, whose sums are off by up to 2^-12 of the sum of the terms' magnitudes where codes of
- * all sizes meet (2^-16 for normally distributed values), and the blocks in fp32; results are bf16, since more bits would hold that error.  They are right where they are below 2^96; where a scale times another
- * is below 2^-156 they may be 0.  All calls only enqueue kernels on `stream` and are deterministic; the order of a sum goes by the sizes,
- * so a row's results among few rows and among many can differ in their last bit.
+ * all sizes meet (2^-16 for normally distributed values), and the blocks in fp32; results are bf16, since more bits would hold that error.
+ * They are right where the terms' magnitudes add up to less than 2^96 and no two scales that meet multiply to more, whichever of them is
+ * the large one; where the second operand (B, W, Wt, for dW X) has scales of rows every scale has to be below 2^96 besides (values below
+ * 3.5e31).  Where a scale times another is below 2^-156 results may be 0.  All calls only enqueue kernels on `stream` and are deterministic;
+ * the order of a sum goes by the sizes, so a row's results among few rows and among many can differ in their last bit.
  */
 
 /*

@@ -12,6 +12,12 @@ typedef int intx8 __attribute__((ext_vector_type(8)));
 
 // Accumulators of products hold 2^30 times the result, so that the product of two small scales stays a normal number.
 constexpr float FP8_LIFT = 0x1p30f, FP8_DROP = 0x1p-30f;
+// The lifted product of two scales (NaN where one is): the lift goes to `s` unless that is large, so that it is inf only where the product
+// of both is 2^98 or more.
+__device__ __forceinline__ float fp8_lifted(float s, float f) {
+  const int lift = fabsf(s) >= 0x1p60f ? 0 : 30;
+  return __builtin_amdgcn_ldexpf(s, lift) * __builtin_amdgcn_ldexpf(f, 30 - lift);
+}
 
 // Magnitudes are compared as bit patterns: NaN ranks above inf, inf above all numbers.
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }

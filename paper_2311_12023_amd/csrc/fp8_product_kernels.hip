@@ -130,7 +130,7 @@ __global__ __launch_bounds__(P_THREADS) void fp8_product_kernel(ProductArgs a) {
   intx8 x[4], y[4];
   floatx4 p[2][2], r[4];
   float s[4], last;                                  // last: the fourth scale of the block before, for its last sums
-  float row_scale = 1.0f;                            // of the rows' tile
+  float row_scale = 0.0f;                            // of the rows' tile
   auto read_x = [&](int i) __attribute__((always_inline)) {
     x[i & 3] = operand(xa + 2048u * i, xb + 2048u * i);
     if constexpr (!ROW_TILES) r[i & 3] = *reinterpret_cast<const floatx4*>(lds + sa + 64 * i);
@@ -205,7 +205,7 @@ __global__ __launch_bounds__(P_THREADS) void fp8_product_kernel(ProductArgs a) {
           product(0); product(1); sum(0); sum(1);
         }
         if (ii < 3) {
-          if (ii == 0) s[j] *= row_scale * FP8_LIFT;
+          if (ii == 0) s[j] = ROW_TILES ? fp8_lifted(row_scale, s[j]) : s[j] * FP8_LIFT;
           if (j < 2) read_x(2 * ii + 2 + j);
           if (ii == 1) transfer(4 + j, next, stage);
         } else {

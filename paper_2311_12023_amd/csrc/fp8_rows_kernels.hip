@@ -205,7 +205,7 @@ __global__ __launch_bounds__(64 * R_WAVES) void fp8_rows_kernel(RowsArgs a) {
 #pragma unroll
       for (int t = 0; t < RT; ++t)
 #pragma unroll
-        for (int e = 0; e < RS; ++e) s[u][t][e] = row_scale[t][e][at * a.rows.scale_block] * FP8_LIFT;
+        for (int e = 0; e < RS; ++e) s[u][t][e] = row_scale[t][e][at * a.rows.scale_block];
       if constexpr (!RAW) {
 #pragma unroll
         for (int j = 0; j < NC; ++j) f[u][j] = column_scale[j][at * a.columns.scale_block];
@@ -242,7 +242,7 @@ __global__ __launch_bounds__(64 * R_WAVES) void fp8_rows_kernel(RowsArgs a) {
           for (int t = 0; t < RT; ++t) {
             const floatx4 z = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[u][t], y[j], floatx4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0, 0, 0);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[t][j][e] = fmaf(z[e], s[u][t][e & (RS - 1)] * f[u][j], acc[t][j][e]);
+            for (int e = 0; e < 4; ++e) acc[t][j][e] = fmaf(z[e], fp8_lifted(s[u][t][e & (RS - 1)], f[u][j]), acc[t][j][e]);
           }
       }
     }

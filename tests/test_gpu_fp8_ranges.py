@@ -46,3 +46,63 @@ def test_every_fraction_of_a_scale():
         x, scale, reciprocal = F.blocks(torch.arange(first, first + (1 << 20), dtype=torch.int32, device="cuda"))
         q, s = lq.fp8_quantize(x)
         assert torch.equal(s[:, 0], scale) and torch.equal(q.view(torch.uint8), F.codes(x, reciprocal))
+
+
+def _sized(m, d, seed, size):
+    """Values of one size, with zeros among them: a zero times a scale that is inf would be NaN."""
+    x = _randn(m, d, seed) * size
+    x[:, ::5] = 0.0
+    return x
+
+
+FAR = [(1e-26, 1e33), (1e33, 1e-26), (1e-37, 5e37), (5e37, 1e-37), (1e-8, 3e32), (1e-40, 1e37), (5e37, 1e-40)]
+
+
+@pytest.mark.parametrize("x_size,w_size", FAR)
+@pytest.mark.parametrize("m,n,k", [(1, 270, 300), (7, 270, 300), (12, 40, 1300), (40, 270, 1300), (300, 270, 700), (600, 9000, 300)])
+def test_scales_of_every_size(m, n, k, x_size, w_size):
+    """A layer's forward pass and dX, whose weights have scales of tiles: whichever operand the large scales are in."""
+    x, w = _sized(m, k, 1, x_size), _sized(n, k, 2, w_size)
+    wq, s, wt, ts = lq.fp8_quantize(w.cuda(), tiles=True, both=True)
+    values = R.values(wq.cpu(), s.cpu())
+    _close(lq.fp8_forward(x.cuda(), wq, s), R.values(*R.quantize(x)), values)
+    dy = _sized(m, n, 3, x_size)
+    dx, _ = lq.fp8_backward(dy.cuda(), None, wt, ts, want_dw=False)
+    _close(dx, R.values(*R.quantize(dy)), values.t().contiguous())
+
+
+@pytest.mark.parametrize("a_tiles,b_tiles", [(False, True), (True, True), (False, False), (True, False)])
+@pytest.mark.parametrize("m,n,k", [(2, 270, 300), (40, 270, 1300), (300, 520, 700)])
+@pytest.mark.parametrize("a_size,b_size", FAR)
+def test_products_of_scales_of_every_size(m, n, k, a_size, b_size, a_tiles, b_tiles):
+    """Scales of rows in B: up to 2^96, 448 of which are 3.5e31."""
+    if not b_tiles:
+        a_size, b_size = min(a_size, 5e30), min(b_size, 5e30)
+    a, s = lq.fp8_quantize(_sized(m, k, 1, a_size).cuda(), tiles=a_tiles)
+    b, t = lq.fp8_quantize(_sized(n, k, 2, b_size).cuda(), tiles=b_tiles)
+    assert b_tiles or max(s.max().item(), t.max().item()) < 2.0 ** 96
+    _close(lq.fp8_matmul(a, s, b, t), R.values(a.cpu(), s.cpu()), R.values(b.cpu(), t.cpu()))
+
+
+@pytest.mark.parametrize("m,n,k", [(300, 40, 270), (300, 270, 520), (9, 700, 30)])
+@pytest.mark.parametrize("dy_size,x_size", [(1e-25, 5e30), (5e30, 1e-25), (1e-12, 6e30)])
+def test_gradients_of_weights_of_large_values(m, n, k, dy_size, x_size):
+    dy, x = _sized(m, n, 1, dy_size), _sized(m, k, 2, x_size)
+    _, dw = lq.fp8_backward(dy.cuda(), x.cuda(), want_dx=False)
+    _close(dw, R.values(*R.quantize(dy.t().contiguous())), R.values(*R.quantize(x.t().contiguous())))
+
+
+@pytest.mark.parametrize("tiles", [False, True])
+@pytest.mark.parametrize("m", [1, 40, 300])
+def test_a_large_block_that_is_not_finite(m, tiles):
+    """A scale that is NaN beside one that is larger than 2^60: what it enters is NaN, and nothing else is."""
+    x, w = _sized(m, 300, 1, 1e-20), _sized(270, 300, 2, 1e30)
+    x[0, 140] = float("nan")
+    w[130, 3] = float("inf")
+    wq, s = lq.fp8_quantize(w.cuda(), tiles=tiles)
+    y = lq.fp8_forward(x.cuda(), wq, s)
+    want = torch.zeros(m, 270, dtype=torch.bool)
+    want[0] = True
+    want[:, 128:256 if tiles else 131] |= tiles
+    want[:, 130] = True
+    assert torch.equal(torch.isnan(y).cpu(), want) and torch.isfinite(y.cpu()[~want]).all()
