@@ -673,6 +673,15 @@ def grad_norm(grads, max_norm: float = float("inf"), workspace: torch.Tensor | N
     return out[0], out[1]
 
 
+def _one(t, dtype, name):
+    """Address of a tensor of one element on the current device."""
+    place = _dev(t, dtype, name)
+    if t.numel() != 1:
+        raise ValueError(f"{name}: need one element")
+    _here(t)
+    return place
+
+
 class AdamW:
     """AdamW over many tensors in one call, with states in 32 bits or in 8 (lq_adamw).
 
@@ -708,7 +717,7 @@ class AdamW:
         if bits == 8:
             self._states.update({name: (torch.float32, total // 256, 1 / 64) for name in ("m_scale", "v_scale")})
         self.buffers = {name: torch.zeros(n, dtype=dtype, device=device) for name, (dtype, n, _) in self._states.items()}
-        self._state_places = {}
+        self._used = [("m", self, 0, 0)]                     # nothing yet: the first step looks
         self.t = torch.zeros((), dtype=torch.int64, device=device) if device_step else 0
 
     def _describe(self):
@@ -726,8 +735,10 @@ class AdamW:
         self._places = [x.data_ptr() for x in self._held]
 
     def _find_states(self):
-        """The states' addresses into the table, checked, where others lie in `buffers` than at the last step."""
-        for name, (dtype, n, stride) in self._states.items():
+        """The states' addresses into the table, checked: others may lie in `buffers` than at the last step.  The tensors are kept, so that no
+        other takes their place in memory unseen."""
+        used = []
+        for name, (dtype, n, _) in self._states.items():
             buffer = self.buffers.get(name)
             if buffer is None:
                 raise TypeError(f"buffers: no {name}")
@@ -735,9 +746,10 @@ class AdamW:
             if buffer.numel() != n:
                 raise ValueError(f"buffers: {name} has {buffer.numel()} elements, needs {n}")
             _here(buffer)
-            if place != self._state_places.get(name):
-                self._columns[name] = place + (self._starts * stride).astype(np.uint64)
-                self._state_places[name] = place
+            used.append((name, buffer, place, n))
+        for name, _, place, _ in used:
+            self._columns[name] = place + (self._starts * self._states[name][2]).astype(np.uint64)
+        self._used = used
 
     def step(self, grads, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, coef: torch.Tensor | None = None) -> None:
         """One step.  grads: one for each parameter, fp32 or bf16, of its size.  lr: a number, or an fp32 tensor of one element on the GPU.
@@ -750,7 +762,11 @@ class AdamW:
         now = [x.data_ptr() for x in self._held]
         if now != self._places:                              # parameters that have moved
             self._describe()
-        self._find_states()
+        buffers = self.buffers
+        for name, buffer, place, n in self._used:
+            if buffers.get(name) is not buffer or buffer.data_ptr() != place or buffer.numel() != n:
+                self._find_states()
+                break
         if len(grads) > 16:
             self._columns["g"], self._columns["g_dtype"] = places, types
         else:
@@ -763,20 +779,12 @@ class AdamW:
         (h.beta1, h.beta2), h.eps, h.weight_decay, h.seed = betas, eps, weight_decay, self.seed
         h.lr_device = h.step_device = None                   # the last step's
         if isinstance(lr, torch.Tensor):
-            h.lr_device = _dev(lr, torch.float32, "lr")
+            h.lr_device = _one(lr, torch.float32, "lr")
         else:
             h.lr = lr
-        for name, one in (("lr", lr), ("coef", coef)):
-            if isinstance(one, torch.Tensor):
-                if one.numel() != 1:
-                    raise ValueError(f"{name}: need one element")
-                _here(one)
-        scale = _dev(coef, torch.float32, "coef")
+        scale = None if coef is None else _one(coef, torch.float32, "coef")
         if on_device:
-            h.step_device = _dev(self.t, torch.int64, "t")
-            if self.t.numel() != 1:
-                raise ValueError("t: need one element")
-            _here(self.t)
+            h.step_device = _one(self.t, torch.int64, "t")
             self.t += 1
         else:
             h.step = self.t + 1

@@ -105,6 +105,20 @@ def test_states_that_do_not_fit(calls, change, error):
     assert not calls and opt.t == 0
 
 
+def test_old_states_after_new_ones_were_refused(calls):
+    """One of two that were replaced does not fit: the step is refused, and the old ones put back are used again."""
+    opt, grads = _made()
+    opt.step(grads, 0.1)
+    first = opt.buffers
+    opt.buffers = dict(m=first["m"].clone(), v=torch.zeros(5))
+    with pytest.raises(ValueError):
+        opt.step(grads, 0.1)
+    opt.buffers = first
+    opt.step(grads, 0.1)
+    for have, want in zip(calls[-1]["table"], _expected(opt, first)):
+        assert all(have[name] == place for name, place in want.items())
+
+
 @pytest.mark.parametrize("change", [dict(m_scale=torch.zeros(2)), dict(v_scale=torch.zeros(4))])
 def test_scales_that_do_not_fit(calls, change):
     opt, grads = _made(8, device_step=True)
