@@ -105,6 +105,14 @@ __device__ __forceinline__ void quantize_column(const RawColumn<T>& raw, int col
   if (at % 128 == 0) scales[column * U + at / 128] = s;
 }
 
+// Lanes read from LDS what other lanes of their wavefront have written, and write what those have read.  The wavefront's LDS accesses are
+// carried out in order; this keeps the compiler to it, and costs no instruction.
+__device__ __forceinline__ void wavefront_turn() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // ---- the product ---------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void rows_store(const RowsArgs& a, floatx4 v, int64_t row, int64_t column) {
   if (column >= a.columns.count) return;
@@ -196,6 +204,7 @@ __global__ __launch_bounds__(64 * R_WAVES) void fp8_rows_kernel(RowsArgs a) {
           ask(c0);
           take(c0);
         }
+      wavefront_turn();
     } else {
       load_rows();
     }
@@ -246,6 +255,7 @@ __global__ __launch_bounds__(64 * R_WAVES) void fp8_rows_kernel(RowsArgs a) {
           }
       }
     }
+    if constexpr (RAW) wavefront_turn();             // the next step's codes take these ones' place
   }
 
   // the wavefronts' sums in order
