@@ -46,9 +46,17 @@ __device__ __forceinline__ int tensor_of(const Table& t, uint32_t wg) {
   return lo;
 }
 
+// Eight neighbours, on addresses that are checked for 16 bytes: the vector type's own alignment is its size, 32 for fp32.
+template <typename T>
+struct Eight {
+  typedef T values __attribute__((ext_vector_type(8)));
+  typedef values unit __attribute__((aligned(16)));
+};
+static_assert(alignof(Eight<float>::unit) == 16 && alignof(Eight<__bf16>::unit) == 16, "addresses that the host checks");
+
 template <int THREADS, typename T>
 __device__ __forceinline__ double squares(const T* g, int64_t from, int64_t to) {
-  typedef T vec8 __attribute__((ext_vector_type(8)));
+  typedef typename Eight<T>::unit vec8;
   double sum = 0.0;
   const bool vec = ((uintptr_t)g & 15) == 0;
   int64_t i = from + 8 * threadIdx.x;
@@ -219,7 +227,7 @@ __host__ __device__ inline void step_factors(StepFactors& f, double lr, double b
 // 32-bit one's lose by (954 and 925).
 template <bool STREAMED, typename T>
 __device__ __forceinline__ void load8(const T* x, int64_t i, int count, bool vec, float (&v)[8]) {
-  typedef T vec8 __attribute__((ext_vector_type(8)));
+  typedef typename Eight<T>::unit vec8;
   if (vec && count == 8) {
     const vec8* from = reinterpret_cast<const vec8*>(x + i);
     const vec8 in = STREAMED ? __builtin_nontemporal_load(from) : *from;
@@ -232,7 +240,7 @@ __device__ __forceinline__ void load8(const T* x, int64_t i, int count, bool vec
 }
 template <bool STREAMED, typename T>
 __device__ __forceinline__ void store8(T* x, int64_t i, int count, bool vec, const float (&v)[8]) {
-  typedef T vec8 __attribute__((ext_vector_type(8)));
+  typedef typename Eight<T>::unit vec8;
   if (vec && count == 8) {
     vec8 out;
 #pragma unroll

@@ -99,3 +99,26 @@ def test_a_graph_that_has_saved_what_a_step_writes_fails(kind):
     with pytest.raises(RuntimeError):
         y.backward()
     (x @ used.t()).sum().backward()                              # one made after the step does not
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_addresses_on_16_bytes(bits):
+    """Tensors and states on addresses that are multiples of 16 and not of 32 give what others give."""
+    def at(start, values):
+        held = torch.empty(values.numel() + 64, dtype=values.dtype, device="cuda")
+        while (held[start:].data_ptr() // 16) % 2 != 1 or held[start:].data_ptr() % 16:
+            start += 1
+        held[start:start + values.numel()] = values
+        return held[start:start + values.numel()]
+
+    params, grads = _values(1), _values(2)
+    moved, moved_grads = [at(1, p) for p in params], [at(1, g) for g in grads]
+    opt, other = lq.AdamW(params, bits=bits, seed=5), lq.AdamW(moved, bits=bits, seed=5)
+    if bits == 32:
+        other.buffers = {name: at(1, b) for name, b in other.buffers.items()}
+    for _ in range(2):
+        norm, again = lq.grad_norm(grads, 1.0), lq.grad_norm(moved_grads, 1.0)
+        assert torch.equal(norm[0], again[0])
+        opt.step(grads, 0.01, coef=norm[1])
+        other.step(moved_grads, 0.01, coef=again[1])
+    assert _same(params, moved) and _same(opt.buffers.values(), other.buffers.values())
