@@ -106,3 +106,50 @@ def test_a_large_block_that_is_not_finite(m, tiles):
     want[:, 128:256 if tiles else 131] |= tiles
     want[:, 130] = True
     assert torch.equal(torch.isnan(y).cpu(), want) and torch.isfinite(y.cpu()[~want]).all()
+
+
+def _terms(rows, depth, seed, first):
+    """A matrix whose products with one of the other `first` are whole numbers that bf16 holds: -1, 0 and 1, one in sixteen not 0, and in every
+    block a 7 (scale 2^-6) where the other has a 0.  The last term of every sum is not 0."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randint(0, 2, (rows, depth), generator=g).float() * 2 - 1
+    x *= torch.randint(0, 16, (rows, depth), generator=g) == 0
+    x[:, -1] = 1 - 2 * (torch.arange(rows) % 2)
+    x[:, first::128], x[:, 1 - first::128] = 7.0, 0.0
+    return x
+
+
+def _whole(got, a, b):
+    """Every term counts: sums of up to 256 are bf16 numbers, and one term less is another number."""
+    want = (a.double() @ b.double().t()).float()
+    assert want.abs().max() <= 256 and torch.equal(got.float().cpu(), want)
+
+
+DEPTHS = [3, 131, 1000, 2999, 9999, 20003]
+
+
+@pytest.mark.parametrize("m", [1, 3, 7, 12, 16, 30, 60, 100, 300, 600])
+@pytest.mark.parametrize("k", DEPTHS)
+def test_no_term_is_lost(m, k):
+    """Forward pass and products with all kinds of scales."""
+    n = 270
+    x, w = _terms(m, k, 1, 0), _terms(n, k, 2, 1)
+    tiles, rows = lq.fp8_quantize(w.cuda(), tiles=True), lq.fp8_quantize(w.cuda())
+    _whole(lq.fp8_forward(x.cuda(), *tiles), x, w)
+    _whole(lq.fp8_forward(x.bfloat16().cuda(), *rows), x, w)
+    for a in (lq.fp8_quantize(x.cuda()), lq.fp8_quantize(x.cuda(), tiles=True)):
+        for b in (tiles, rows):
+            _whole(lq.fp8_matmul(*a, *b), x, w)
+
+
+@pytest.mark.parametrize("few", [1, 7, 30, 100, 300])
+@pytest.mark.parametrize("depth", DEPTHS)
+def test_no_term_of_a_gradient_is_lost(few, depth):
+    """dX sums over the outputs, dW over the rows."""
+    dy, w = _terms(few, depth, 1, 0), _terms(270, depth, 2, 1).t().contiguous()
+    _, _, wt, s = lq.fp8_quantize(w.cuda(), tiles=True, both=True)
+    dx, _ = lq.fp8_backward(dy.cuda(), None, wt, s, want_dw=False)
+    _whole(dx, dy, w.t())
+    dy, x = _terms(few, depth, 3, 0), _terms(270, depth, 4, 1)
+    _, dw = lq.fp8_backward(dy.t().contiguous().cuda(), x.t().contiguous().bfloat16().cuda(), want_dx=False)
+    _whole(dw, dy, x)

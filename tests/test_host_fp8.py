@@ -217,3 +217,16 @@ def test_blocks_that_show_a_wrong_reciprocal():
         for steps in (1, -1):
             seen = (F.codes(x, F.next_float(reciprocal, steps)) != right).any(1)
             assert (~seen).sum() <= missed
+
+
+def test_whole_number_operands_show_each_lost_term():
+    """What the GPU's tests of long sums build on: the operands are held exactly, and a sum without its last term is another bf16 number."""
+    import fp8_reference as R
+    import test_gpu_fp8_ranges as G
+    for depth in G.DEPTHS:
+        a, b = G._terms(20, depth, 1, 0), G._terms(30, depth, 2, 1)
+        for x in (a, b):
+            for tiles in (False, True):
+                assert torch.equal(R.values(*R.quantize(x, tiles)), x.double())
+        whole, less = a @ b.t(), a[:, :-1] @ b[:, :-1].t()
+        assert whole.abs().max() <= 256 and torch.equal(whole.bfloat16().float(), whole) and (whole.bfloat16() != less.bfloat16()).all()
