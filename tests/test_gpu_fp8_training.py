@@ -112,3 +112,44 @@ def test_the_example_with_the_librarys_step(bits):
     first, again = example.finetune(steps=4, bits=bits), example.finetune(steps=4, bits=bits)
     assert first == again and len(first) == 4 and all(x == x for x in first)
     assert first[0] == example.finetune(steps=1)[0]           # the step comes after the first loss
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_the_examples_step_updates_the_factors(bits, monkeypatch):
+    """Every step of the example leaves in the factors what the formula gives for the gradients it was handed, clipped; and the losses after
+    the first are others than those of a run that does not learn."""
+    import importlib.util
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "finetune.py")
+    spec = importlib.util.spec_from_file_location("finetune", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    steps = []
+
+    class Watched(example.ClippedAdamW):
+        def step(self, grads):
+            opt = self.adamw
+            old, at = [], 0
+            for p in opt.params:
+                n = p.numel()
+                m, v = (opt.buffers[k][at:at + n] for k in ("m", "v"))
+                if bits == 8:
+                    m, v = (R.state_values(x, opt.buffers[s][at // 256:at // 256 - (-n // 256)], n) for x, s in ((m, "m_scale"), (v, "v_scale")))
+                    v = R.f32(v.square())
+                old.append([x.double().cpu().reshape(p.shape) for x in (p, m, v)])
+                at += -(-n // 256) * 256
+            norm = torch.stack([g.double().norm() for g in grads]).norm().item()
+            super().step(grads)
+            _, coef = lq.grad_norm(grads, 1.0)
+            assert abs(float(coef) - min(1.0, 1.0 / norm)) <= 1e-5
+            for p, g, (was, m, v) in zip(opt.params, grads, old):
+                want, _, _, _ = R.adamw(was, g.cpu(), m, v, opt.t, self.lr, (0.9, 0.99), 1e-8, 0.0, float(coef))
+                assert torch.equal(p.double().cpu(), want) and not torch.equal(want, was)
+            steps.append(opt.t)
+
+    monkeypatch.setattr(example, "ClippedAdamW", Watched)
+    losses = example.finetune(steps=3, bits=bits)
+    assert steps == [1, 2, 3]
+    assert losses[0] == example.finetune(steps=1)[0]
+    monkeypatch.undo()
+    still = example.finetune(steps=3, bits=bits, lr=0.0)
+    assert losses[0] == still[0] and losses[1] != still[1] and losses[2] != still[2]
