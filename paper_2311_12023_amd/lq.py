@@ -722,6 +722,7 @@ class AdamW:
 
     def _describe(self):
         """Parameters and copies into the table, checked."""
+        self._places = None                                  # none known, should one be refused
         for entry, p, c, n in zip(self._table, self.params, self.copies, self._sizes):
             _dtype(p, "params")
             entry.p, entry.n, entry.p_dtype = _dev(p, p.dtype, "params"), n, T_DTYPES[p.dtype]

@@ -146,3 +146,18 @@ def test_everything_that_a_step_writes_gets_a_new_version(calls):
     assert all(x._version > old for x, old in zip(written, before))
     with pytest.raises(RuntimeError):
         y.sum().backward()
+
+
+def test_old_parameters_after_moved_ones_were_refused(calls):
+    """One that moved is taken up, the next does not fit: the step is refused, and the old ones put back are used again."""
+    opt, grads = _made()
+    opt.step(grads, 0.1)
+    old = [p.data for p in opt.params]
+    opt.params[0].data = old[0].clone()
+    opt.params[1].data = torch.zeros(10)[::2]
+    with pytest.raises(TypeError):
+        opt.step(grads, 0.1)
+    for p, data in zip(opt.params, old):
+        p.data = data
+    opt.step(grads, 0.1)
+    assert [entry["p"] for entry in calls[-1]["table"]] == [p.data_ptr() for p in old]
