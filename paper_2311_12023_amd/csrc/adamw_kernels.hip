@@ -1,6 +1,7 @@
 // The optimizer's step over many tensors: the gradients' norm and AdamW with states in 32 or 8 bits.  Bound by bytes: 28 a value in fp32
-// (480 tensors, 1.7e8 values: 925 us, 5.1 TB/s), 16 with 8-bit states, bf16 gradients and a bf16 copy (1.3e8 values 381 us,
-// 5.5 TB/s); the norm reads 4 (5.1e7 values 38 us, 5.4 TB/s, and the join of the workgroups' sums).
+// (480 tensors, 1.7e8 values: 925 us, 5.1 TB/s), 16 with 8-bit states, bf16 gradients and a bf16 copy (1.3e8 values, median 403 us,
+// 5.2 TB/s, smallest 382); the norm reads 4: 5.1e7 values 47 us, 4.4 TB/s (36 where the memory-side cache still holds them), 1.6e8 in 448
+// tensors 160 us in three launches, 4.0 TB/s, whose last workgroups end one after the other; and the join of the workgroups' sums, 5 us.
 #include <cmath>
 
 #include "fp8.h"

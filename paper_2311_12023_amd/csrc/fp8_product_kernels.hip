@@ -32,9 +32,11 @@ __device__ __forceinline__ uintx2 product_result(floatx4 v) {
   return __builtin_bit_cast(uintx2, bf16x4{(__bf16)(v[0] * FP8_DROP), (__bf16)(v[1] * FP8_DROP), (__bf16)(v[2] * FP8_DROP), (__bf16)(v[3] * FP8_DROP)});
 }
 
-// 4096 columns x 11008 rows: depth 4096 161 us, 2.29 PFLOP/s, depth 11008 404 us, 2.46; rows with scales of their own 193 us, 1.92.  The
-// chip's power is the limit: the clock is 2.1 GHz and the matrix units are busy for half of its cycles, waits and barriers taken out change
-// nothing, transfers or sums taken out 17 % and 11 %.
+// 4096 columns x 11008 rows, median and smallest of 40 launches: depth 4096 174 and 161 us (2.12 and 2.29 PFLOP/s), depth 11008 424 and 409
+// (2.34 and 2.43); rows with scales of their own, depth 4096, 205 and 195 (1.80 and 1.89).  The chip's power is the
+// limit: the clock is 2.1 GHz and the matrix units are busy for half of its cycles, waits and barriers taken out change nothing, transfers or
+// sums taken out 17 % and 11 %.  Where rows have scales of their own these have to be below 2^98 in the columns' operand and 2^103 in the
+// rows' one, or a factor on the way overflows: splitting them too would be a third vector instruction for every sum.
 //
 // A workgroup of eight wavefronts makes a tile, a wavefront 128 x 64 of it (2 x 4) in blocks of 16 x 16.  A block of 128 along k is one
 // matrix instruction, whose four sums a lane are multiplied by the two scales into the accumulators: one vector instruction each where
@@ -205,7 +207,7 @@ __global__ __launch_bounds__(P_THREADS) void fp8_product_kernel(ProductArgs a) {
           else add(3, 3, h, last);                   // of the block before
           __builtin_amdgcn_sched_barrier(0);
         };
-        // 4096 x 4096 by 11008: products and sums in turn 161 us, two by two 164; with scales of rows 196 and 193
+        // 4096 x 4096 by 11008, smallest: products and sums in turn 161 us, two by two 164; with scales of rows 196 and 193
         if constexpr (ROW_TILES) {
           product(0); sum(0); product(1); sum(1);
         } else {

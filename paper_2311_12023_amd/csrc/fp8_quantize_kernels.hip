@@ -1,5 +1,5 @@
 // Codes and scales of a matrix and of its transpose in one pass.  Bound by its bytes, X once and the codes once or twice: a tile is one
-// block in either direction, so whatever is wanted comes out of the registers that hold it (11008 x 4096 fp32 to both forms 46 us, 5.9 TB/s;
+// block in either direction, so whatever is wanted comes out of the registers that hold it (11008 x 4096 fp32 to both forms 49 us, 5.5 TB/s;
 // 4096 x 4096 and 11008 x 4096 bf16 in rows, the first both ways, in one launch 48 us, 4.2 TB/s; 1000 x 50265 bf16 on odd addresses 37 us,
 // 4.0 TB/s, by single values 108).  Small ones are a chain of latencies: 1001 x 1027 9 us.  bf16 values stay packed until they are scaled (74
 // registers for 176, six wavefronts a SIMD for two: 4096 x 4096 in rows 19 -> 12 us).
