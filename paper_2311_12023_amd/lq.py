@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import struct
+import weakref
 
 import numpy as np
 import torch
@@ -717,7 +718,7 @@ class AdamW:
         if bits == 8:
             self._states.update({name: (torch.float32, total // 256, 1 / 64) for name in ("m_scale", "v_scale")})
         self.buffers = {name: torch.zeros(n, dtype=dtype, device=device) for name, (dtype, n, _) in self._states.items()}
-        self._used = [("m", self, 0, 0)]                     # nothing yet: the first step looks
+        self._used = [("m", lambda: None, 0, 0)]             # nothing yet: the first step looks
         self.t = torch.zeros((), dtype=torch.int64, device=device) if device_step else 0
 
     def _describe(self):
@@ -736,8 +737,7 @@ class AdamW:
         self._places = [x.data_ptr() for x in self._held]
 
     def _find_states(self):
-        """The states' addresses into the table, checked: others may lie in `buffers` than at the last step.  The tensors are kept, so that no
-        other takes their place in memory unseen."""
+        """The states' addresses into the table, checked: others may lie in `buffers` than at the last step."""
         used = []
         for name, (dtype, n, _) in self._states.items():
             buffer = self.buffers.get(name)
@@ -747,7 +747,7 @@ class AdamW:
             if buffer.numel() != n:
                 raise ValueError(f"buffers: {name} has {buffer.numel()} elements, needs {n}")
             _here(buffer)
-            used.append((name, buffer, place, n))
+            used.append((name, weakref.ref(buffer), place, n))
         for name, _, place, _ in used:
             self._columns[name] = place + (self._starts * self._states[name][2]).astype(np.uint64)
         self._used = used
@@ -764,8 +764,9 @@ class AdamW:
         if now != self._places:                              # parameters that have moved
             self._describe()
         buffers = self.buffers
-        for name, buffer, place, n in self._used:
-            if buffers.get(name) is not buffer or buffer.data_ptr() != place or buffer.numel() != n:
+        for name, ref, place, n in self._used:               # the same tensors, where they were: not others at their address
+            buffer = buffers.get(name)
+            if buffer is None or buffer is not ref() or buffer.data_ptr() != place or buffer.numel() != n:
                 self._find_states()
                 break
         if len(grads) > 16:

@@ -161,3 +161,18 @@ def test_old_parameters_after_moved_ones_were_refused(calls):
         p.data = data
     opt.step(grads, 0.1)
     assert [entry["p"] for entry in calls[-1]["table"]] == [p.data_ptr() for p in old]
+
+
+def test_states_that_were_replaced_are_let_go(calls):
+    """States moved elsewhere between steps, to free their memory: the optimizer does not hold on to them."""
+    import weakref
+    opt, grads = _made(8)
+    opt.step(grads, 0.1)
+    away = {name: b.clone() for name, b in opt.buffers.items()}
+    refs = [weakref.ref(b) for b in opt.buffers.values()]
+    opt.buffers = {}
+    assert all(ref() is None for ref in refs)
+    opt.buffers = away
+    opt.step(grads, 0.1)
+    for have, want in zip(calls[-1]["table"], _expected(opt, away)):
+        assert all(have[name] == place for name, place in want.items())
